@@ -376,6 +376,74 @@ lp_status lp_op_linear(lp_ctx *ctx, int32_t prec, int64_t M, int32_t N, int32_t 
 lp_status lp_op_weight_grad(lp_ctx *ctx, int32_t prec, int64_t M, int32_t N, int32_t K, const void *A, const void *dZ,
                             float *dW);
 
+/* ---- learned node features -------------------------------------------------------------------- */
+
+/* (No counterpart in the paper, whose nodes come with features; graphs without features learn a table.)
+ * Rows of an embedding table, scaled: out[i] = scale * table[ids[i]], rounded once.
+ *   table[rows, width]   : DEVICE, row pitch ld_table elements; table_prec LP_FP32 or LP_BF16
+ *   ids[n_ids]           : DEVICE int32
+ *   padding_id           : ids equal to it give a row of zeros; it need not be a row of the table (-1, say).
+ *                          LP_NO_PADDING: none
+ *   out[n_ids, width]    : DEVICE, row pitch ld_out elements; out_prec LP_FP32 or LP_BF16 (LP_BF16 when the table is)
+ * Any width, pitch and alignment to the element is accepted; rows whose width, pitch and address are multiples of
+ * 16 bytes are the fast ones.  An id outside [0, rows) that is not the padding id gives a row of zeros, and the next
+ * synchronising call (lp_get_stats) returns LP_EINVAL once.  Does not synchronise. */
+#define LP_NO_PADDING INT32_MIN
+lp_status lp_embed(lp_ctx *ctx, int32_t table_prec, const void *table, int64_t rows, int32_t width, int64_t ld_table, const int32_t *ids, int64_t n_ids,
+                   int32_t padding_id, double scale, int32_t out_prec, void *out, int64_t ld_out);
+
+/* Gradient of the table of lp_embed: grad[v] = scale * sum of dout[i] over the i with ids[i] = v; rows that no id names
+ * (and every row, for ids equal to padding_id or outside the table) get nothing: they are set to zero, or left alone when
+ * accumulate != 0 (grad[v] += ...).  The ids are sorted stably and a row's terms are added in the order of i in FP32, so
+ * the result is the same bits in every run; a BF16 gradient is rounded once.
+ *   dout[n_ids, width]   : DEVICE, row pitch ld_dout; dout_prec LP_FP32 or LP_BF16
+ *   grad[rows, width]    : DEVICE, row pitch ld_grad; grad_prec LP_FP32, or LP_BF16 when dout is LP_BF16
+ * Takes workspace from the context (it grows to the largest call; growing synchronises).  Does not synchronise otherwise. */
+lp_status lp_embed_grad(lp_ctx *ctx, int32_t dout_prec, const void *dout, int64_t ld_dout, const int32_t *ids, int64_t n_ids, int32_t padding_id, double scale,
+                        int64_t rows, int32_t width, int32_t grad_prec, void *grad, int64_t ld_grad, int32_t accumulate);
+
+/* ---- orthogonalised updates ------------------------------------------------------------------- */
+
+/* (No counterpart in the paper, which trains with Adam.)
+ * Newton-Schulz orthogonalisation of `batch` matrices [rows, cols]:
+ *   X_0 = U / (|U|_F + eps),  X <- a X + (b A + c A^2) X with A = X X^T, `steps` times (1..64); out = X.
+ * A matrix with more rows than columns is iterated transposed.  A matrix of zeros gives zeros.
+ *   prec     : LP_FP32 or LP_BF16, of U and out.  The products run on the tensor cores with FP32 accumulators: LP_BF16
+ *              holds X, A and b A + c A^2 as FP16 numbers (11 bits), LP_FP32 as pairs of them (22 bits)
+ *   U, out   : DEVICE, row pitch ld_*, matrices stride_* elements apart; out may be U itself
+ *   coeffs   : HOST double[3] = {a, b, c}, or NULL for {3.4445, -4.7750, 2.0315}.  LP_EINVAL when singular values of
+ *              [0, 1] could grow beyond 2 under them
+ * Takes workspace from the context (growing synchronises).  Does not synchronise otherwise. */
+lp_status lp_orthogonalize(lp_ctx *ctx, int32_t prec, int64_t batch, int32_t rows, int32_t cols, const void *U, int64_t ld_u, int64_t stride_u, int32_t steps,
+                           const double *coeffs, double eps, void *out, int64_t ld_out, int64_t stride_out);
+
+typedef struct {
+    int64_t offset;      /* first element in the flat parameter vector */
+    int32_t rows, cols;  /* row-major, y = x W: rows = inputs, cols = outputs */
+} lp_matrix;
+
+typedef struct {
+    double grad_scale;   /* g = grad_scale * grads (1 / number of workers)                                        */
+    double lr, momentum, weight_decay;
+    double coeffs[3];    /* of lp_orthogonalize; all zero = its default                                           */
+    double eps;          /* of lp_orthogonalize                                                                   */
+    double adam_lr, adam_beta1, adam_beta2, adam_eps;
+    int32_t nesterov;
+    int32_t steps;
+} lp_muon_desc;
+
+/* Weight update with orthogonalised momentum for the matrices of a flat float32 parameter vector, Adam for the rest:
+ *   matrices : M' = momentum * M + g;  U = g + momentum * M' (nesterov) or M';  O = orthogonalize(U) in LP_FP32;
+ *              W' = (1 - lr * weight_decay) W - lr * sqrt(max(1, cols / rows)) O;  adam_v is carried over
+ *   others   : M' = b1 M + (1 - b1) g;  v' = b2 v + (1 - b2) g^2;  W' = W - adam_lr (M' / (1 - b1^t)) / (sqrt(v' / (1 - b2^t)) + adam_eps)
+ *   matrices[n_matrices] : HOST; NULL = the weight matrices of the model set by lp_set_model (W, W_self, W_neigh of every
+ *                          layer, W0 and W1 of the MLP predictor)
+ *   params, momentum, adam_v, grads : DEVICE float32 [n_params]; adam_v may be NULL when the matrices cover the vector
+ *   new_*                : DEVICE float32 [n_params], or NULL = update in place
+ * Does not synchronise (except to grow the workspace). */
+lp_status lp_muon_step(lp_ctx *ctx, const lp_muon_desc *desc, const lp_matrix *matrices, int32_t n_matrices, int64_t n_params, const float *params,
+                       const float *momentum, const float *adam_v, const float *grads, int64_t t, float *new_params, float *new_momentum, float *new_adam_v);
+
 /* ---- allocation-free variant ---------------------------------------------------------------- */
 
 /* (No counterpart in the paper: this entry point exists for the callers described below.)

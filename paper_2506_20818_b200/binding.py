@@ -30,6 +30,7 @@ EXPORTS = [
     "lp_weight_grad_static", "lp_sparsify", "lp_get_sparsified",
     "lp_worker_view", "lp_get_worker_view", "lp_hits_at_k", "lp_get_predictor_activations",
     "lp_invalidate_embeddings", "lp_set_wait_limit",
+    "lp_embed", "lp_embed_grad", "lp_orthogonalize", "lp_muon_step",
 ]
 
 PROF_CATEGORIES = ["agg_fwd", "agg_bwd", "gemm_fwd", "gemm_dgrad", "gemm_wgrad", "score", "incidence", "scatter",
@@ -63,6 +64,30 @@ class Profile(C.Structure):
     _fields_ = [("ms", C.c_double * 11), ("bytes", C.c_double * 11), ("flops", C.c_double * 11), ("spans", C.c_int64 * 11)]
 
 
+class Matrix(C.Structure):
+    _fields_ = [("offset", C.c_int64), ("rows", C.c_int32), ("cols", C.c_int32)]
+
+
+class MuonDesc(C.Structure):
+    _fields_ = [("grad_scale", C.c_double), ("lr", C.c_double), ("momentum", C.c_double), ("weight_decay", C.c_double),
+                ("coeffs", C.c_double * 3), ("eps", C.c_double), ("adam_lr", C.c_double), ("adam_beta1", C.c_double),
+                ("adam_beta2", C.c_double), ("adam_eps", C.c_double), ("nesterov", C.c_int32), ("steps", C.c_int32)]
+
+
+LP_NO_PADDING = -(1 << 31)
+
+# argument types of the calls whose latency counts: ctypes converts plain Python numbers by them
+_ARGTYPES = {
+    "lp_embed": [C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_int32, C.c_int64, C.c_void_p, C.c_int64, C.c_int32, C.c_double, C.c_int32,
+                 C.c_void_p, C.c_int64],
+    "lp_embed_grad": [C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int32, C.c_double, C.c_int64, C.c_int32, C.c_int32,
+                      C.c_void_p, C.c_int64, C.c_int32],
+    "lp_orthogonalize": [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_int64, C.c_int32, C.c_void_p, C.c_double,
+                         C.c_void_p, C.c_int64, C.c_int64],
+    "lp_muon_step": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p,
+                     C.c_void_p, C.c_void_p],
+}
+
 _lib = None
 
 
@@ -80,6 +105,8 @@ def load_library() -> C.CDLL:
         for name in EXPORTS:
             if name not in ("lp_last_error", "lp_destroy"):
                 getattr(lib, name).restype = C.c_int
+        for name, types in _ARGTYPES.items():
+            getattr(lib, name).argtypes = types
         _lib = lib
     return _lib
 
@@ -257,6 +284,140 @@ class Context:
         self._ck(self.lib.lp_hits_at_k(self.h, _ptr(pos_scores), C.c_int64(pos_scores.numel()), _ptr(neg_scores), C.c_int64(neg_scores.numel()),
                                        C.c_int64(k), C.byref(out)))
         return float(out.value)
+
+    # ---- learned node features
+    def _refuse(self, message: str):
+        raise LpError(-1, message)
+
+    def _prec(self, dtype, who: str) -> int:
+        if dtype == self._torch.float32:
+            return LP_FP32
+        if dtype == self._torch.bfloat16:
+            return LP_BF16
+        self._refuse(f"{who}: float32 or bfloat16 expected, got {dtype}")
+
+    def _rows(self, x, who: str):
+        """Row pitch of a CUDA matrix whose rows are contiguous."""
+        if not x.is_cuda or x.device.index != self.device:
+            self._refuse(f"{who}: expected a tensor on cuda:{self.device}")
+        if x.dim() != 2:
+            self._refuse(f"{who}: expected a matrix, got {x.dim()} dimensions")
+        if x.shape[1] > 1 and x.stride(1) != 1:
+            self._refuse(f"{who}: the elements of a row must be contiguous")
+        return x.stride(0) if x.shape[0] > 1 else max(x.shape[1], x.stride(0))
+
+    def _ids(self, ids, who: str):
+        if not ids.is_cuda or ids.device.index != self.device or ids.dtype != self._torch.int32 or not ids.is_contiguous():
+            self._refuse(f"{who}: ids must be a contiguous int32 tensor on cuda:{self.device}")
+
+    def _enter(self, *tensors):
+        """Work goes to the context's stream.  Called from another current stream, it waits for what that stream has
+        enqueued so far, and the tensors are kept from reuse until it is done; returns the stream to hand back to."""
+        t = self._torch
+        if t._C._cuda_getCurrentRawStream(self.device) == self.stream.cuda_stream:
+            return None
+        cur = t.cuda.current_stream(self.device)
+        self.stream.wait_stream(cur)
+        for x in tensors:
+            if x is not None:
+                x.record_stream(self.stream)
+        return cur
+
+    def _leave(self, cur):
+        if cur is not None:
+            cur.wait_stream(self.stream)
+
+    def embed(self, table, ids, scale: float = 1.0, padding_id: Optional[int] = None, out_dtype=None, out=None):
+        """scale * table[ids] (ids int32, any shape; rows of zeros for padding_id); see lp_embed."""
+        t = self._torch
+        self._ids(ids, "embed")
+        ldt = self._rows(table, "embed: table")
+        V, D = table.shape
+        N = ids.numel()
+        if out is None:
+            out = t.empty((*ids.shape, D), dtype=out_dtype or table.dtype, device=table.device)
+            ldo = D
+        else:
+            if tuple(out.shape) != (N, D) or (out_dtype is not None and out.dtype != out_dtype):
+                self._refuse(f"embed: out must be [{N}, {D}] of the requested type")
+            ldo = self._rows(out, "embed: out")
+        cur = self._enter(table, ids, out)
+        self._ck(self.lib.lp_embed(self.h, self._prec(table.dtype, "embed: table"), table.data_ptr(), V, D, ldt, ids.data_ptr(), N,
+                                   LP_NO_PADDING if padding_id is None else padding_id, scale, self._prec(out.dtype, "embed: out"), out.data_ptr(),
+                                   ldo))
+        self._leave(cur)
+        return out
+
+    def embed_grad(self, dout, ids, rows: int, scale: float = 1.0, padding_id: Optional[int] = None, grad=None, grad_dtype=None, accumulate: bool = False):
+        """Gradient [rows, width] of the table of embed(); see lp_embed_grad.  accumulate adds to `grad`."""
+        t = self._torch
+        self._ids(ids, "embed_grad")
+        ldd = self._rows(dout, "embed_grad: dout")
+        N, D = dout.shape
+        if ids.numel() != N:
+            self._refuse(f"embed_grad: {ids.numel()} ids for {N} rows of dout")
+        if grad is None:
+            if accumulate:
+                self._refuse("embed_grad: accumulate needs a gradient to add to")
+            grad = t.empty((rows, D), dtype=grad_dtype or t.float32, device=dout.device)
+            ldg = D
+        else:
+            if tuple(grad.shape) != (rows, D) or (grad_dtype is not None and grad.dtype != grad_dtype):
+                self._refuse(f"embed_grad: grad must be [{rows}, {D}] of the requested type")
+            ldg = self._rows(grad, "embed_grad: grad")
+        cur = self._enter(dout, ids, grad)
+        self._ck(self.lib.lp_embed_grad(self.h, self._prec(dout.dtype, "embed_grad: dout"), dout.data_ptr(), ldd, ids.data_ptr(), N,
+                                        LP_NO_PADDING if padding_id is None else padding_id, scale, rows, D, self._prec(grad.dtype, "embed_grad: grad"),
+                                        grad.data_ptr(), ldg, int(accumulate)))
+        self._leave(cur)
+        return grad
+
+    # ---- orthogonalised updates
+    def orthogonalize(self, U, steps: int = 5, coeffs: Optional[Sequence[float]] = None, eps: float = 1e-7, out=None):
+        """Newton-Schulz orthogonalisation of U [..., rows, cols] (float32 or bfloat16); see lp_orthogonalize."""
+        t = self._torch
+        if U.dim() < 2:
+            self._refuse("orthogonalize: expected matrices")
+        shape = U.shape
+        U3 = U if U.dim() == 3 else U.unsqueeze(0) if U.dim() == 2 else U.reshape(-1, shape[-2], shape[-1])
+        if not U3.is_cuda or U3.device.index != self.device or (U3.shape[2] > 1 and U3.stride(2) != 1):
+            self._refuse(f"orthogonalize: expected matrices with contiguous rows on cuda:{self.device}")
+        if out is None:
+            out = t.empty(shape, dtype=U.dtype, device=U.device)
+        elif out.shape != shape or out.dtype != U.dtype or not out.is_cuda or out.dim() > 3 or (shape[-1] > 1 and out.stride(-1) != 1):
+            self._refuse("orthogonalize: out must have the shape, type and device of U, with contiguous rows, and at most three dimensions")
+        O3 = out if out.dim() == 3 else out.unsqueeze(0) if out.dim() == 2 else out.view(-1, shape[-2], shape[-1])
+        batch, rows, cols = U3.shape
+        lds = [x.stride(1) if rows > 1 else cols for x in (U3, O3)]
+        strides = [x.stride(0) if batch > 1 else rows * ld for x, ld in zip((U3, O3), lds)]
+        c = (C.c_double * 3)(*coeffs) if coeffs is not None else None
+        cur = self._enter(U, U3, out)
+        self._ck(self.lib.lp_orthogonalize(self.h, self._prec(U.dtype, "orthogonalize"), batch, rows, cols, U3.data_ptr(), lds[0], strides[0], steps, c, eps,
+                                           O3.data_ptr(), lds[1], strides[1]))
+        self._leave(cur)
+        return out
+
+    def muon_step(self, params, momentum, adam_v, grads, t: int, matrices=None, lr: float = 0.02, mu: float = 0.95, nesterov: bool = True,
+                  weight_decay: float = 0.0, steps: int = 5, coeffs: Optional[Sequence[float]] = None, ns_eps: float = 1e-7, grad_scale: float = 1.0,
+                  adam_lr: float = 1e-3, beta1: float = 0.9, beta2: float = 0.999, adam_eps: float = 1e-8, out=None):
+        """Orthogonalised-momentum update of the weight matrices, Adam for the rest of the flat vector; see lp_muon_step.
+        matrices: (offset, rows, cols) triples, or None for the matrices of the model.  Updates in place, or writes the new
+        (params, momentum, adam_v) to `out`.  Returns (params, momentum, adam_v)."""
+        f32 = self._torch.float32
+        n = params.numel()
+        new = (params, momentum, adam_v) if out is None else tuple(out)
+        for x in (params, momentum, adam_v, grads, *new):
+            if x is not None and (not x.is_cuda or x.device.index != self.device or x.dtype != f32 or x.numel() != n or not x.is_contiguous()):
+                self._refuse(f"muon_step: expected contiguous float32 vectors of {n} elements on cuda:{self.device}")
+        d = MuonDesc(grad_scale, lr, mu, weight_decay, (C.c_double * 3)(*(coeffs or (0.0, 0.0, 0.0))), ns_eps, adam_lr, beta1, beta2, adam_eps, int(nesterov), steps)
+        mats = None
+        if matrices is not None:
+            mats = (Matrix * max(len(matrices), 1))(*matrices)
+        p = [x.data_ptr() if x is not None else None for x in (params, momentum, adam_v, grads, *new)]
+        cur = self._enter(params, momentum, adam_v, grads, *new)
+        self._ck(self.lib.lp_muon_step(self.h, C.byref(d), mats, 0 if matrices is None else len(matrices), n, p[0], p[1], p[2], p[3], t, p[4], p[5], p[6]))
+        self._leave(cur)
+        return new
 
     # ---- inspection
     def stats(self) -> Stats:

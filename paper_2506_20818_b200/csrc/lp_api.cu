@@ -17,6 +17,8 @@
 #include "view.cuh"
 #include "predictor.cuh"
 #include "probe.cuh"
+#include "embed.cuh"
+#include "orthogonal.cuh"
 
 // ----------------------------------------------------------------------------------------------
 // context
@@ -129,6 +131,8 @@ struct lp_ctx {
     uint64_t hk_version = 0, param_version = 0;
     int64_t last_exhausted = 0;
     TcState tc;                         // tensor-core GEMM state (descriptor encoder, device error word)
+    uint8_t *op_ws = nullptr;           // workspace of the embedding gradient and of the orthogonalisation: grows to the largest call
+    size_t op_ws_bytes = 0;
     bf16 *w16 = nullptr, *w16t = nullptr;  // BF16 path: the parameter vector of the current call as BF16, as is and with every weight matrix transposed
     bf16 *w16s = nullptr;                  // ... and with the SAGE layers' [W_self ; W_neigh] stored side by side (see weights_cache_kernel)
     // One-pass SAGE layers l >= 1 on the tensor-core pair kernel take the input gradient as
@@ -298,7 +302,7 @@ extern "C" lp_status lp_create(lp_ctx **out, int32_t device, void *cuda_stream)
     cudaMemset(ctx->err_flag, 0, 256);
     cudaMemset(ctx->exhausted_dev, 0, 256);
     std::string tc_err;
-    if (!tc_init(ctx->tc, tc_err)) {
+    if (!tc_init(ctx->tc, tc_err) || !ns_init(tc_err)) {
         cudaFree(ctx->err_flag); cudaFree(ctx->exhausted_dev); cudaFreeHost(ctx->host_counts);
         delete ctx;
         return fail(nullptr, LP_ECUDA, "lp_create: " + tc_err);
@@ -317,6 +321,7 @@ extern "C" void lp_destroy(lp_ctx *ctx)
     free_list(ctx->view_allocs);
     free_list(ctx->graph_allocs);
     tc_destroy(ctx->tc);
+    cudaFree(ctx->op_ws);
     for (cudaEvent_t e : ctx->ex.prof.pool) cudaEventDestroy(e);
     cudaFree(ctx->err_flag);
     cudaFree(ctx->exhausted_dev);
@@ -1910,7 +1915,7 @@ extern "C" lp_status lp_get_stats(lp_ctx *ctx, lp_stats *out)
         for (int h = 0; h <= ctx->K; ++h) out->block_nodes[h] = ctx->hop[h].n_src;
         for (int h = 1; h <= ctx->K; ++h) out->block_edges[h - 1] = ctx->hop[h].entries;
     }
-    out->workspace_bytes = ctx->graph_bytes + ctx->model_bytes;
+    out->workspace_bytes = ctx->graph_bytes + ctx->model_bytes + (int64_t)ctx->op_ws_bytes;
     out->kernel_launches = ctx->ex.launches;
     return tc_check(ctx->tc, ctx->ex, true, ctx->err);
 }
@@ -2117,6 +2122,260 @@ extern "C" lp_status lp_weight_grad_static(int32_t device, void *cuda_stream, in
     dim3 grid((unsigned)ceil_div64(K, SG_BM), (unsigned)ceil_div64(N, SG_BN), (unsigned)splits);
     launch_dep(gemm_simt_kernel<float, float, float, true, true>, dim3(grid), dim3(SG_THREADS), 0, st, K, N, M, A, K, dZ, N, (float *)nullptr, 0, nullptr, 0, k_chunk, scratch, nullptr, 0);
     launch_dep(reduce_partials_kernel, dim3((unsigned)ceil_div64(tile, 256)), dim3(256), 0, st, scratch, tile, splits, dW, 0);
+    CK_LAUNCH();
+    return LP_OK;
+}
+
+// ----------------------------------------------------------------------------------------------
+// learned node features
+// ----------------------------------------------------------------------------------------------
+// at least `bytes` of device memory that the next call on this context may overwrite
+static lp_status op_workspace(lp_ctx *ctx, size_t bytes, uint8_t **out)
+{
+    if (bytes > ctx->op_ws_bytes) {
+        CK(cudaStreamSynchronize(ctx->ex.st));
+        cudaFree(ctx->op_ws);
+        ctx->op_ws = nullptr;
+        ctx->op_ws_bytes = 0;
+        CK(cudaMalloc((void **)&ctx->op_ws, bytes));
+        ctx->op_ws_bytes = bytes;
+    }
+    *out = ctx->op_ws;
+    return LP_OK;
+}
+
+static bool misaligned(const void *p, int32_t prec) { return ((uintptr_t)p & (prec == LP_FP32 ? 3 : 1)) != 0; }
+
+static lp_status check_table(lp_ctx *ctx, const char *who, int32_t prec_a, int32_t prec_b, int64_t V, int32_t D, int64_t ld_rows, int64_t N, int64_t ld_ids, double scale)
+{
+    const std::string w(who);
+    if ((prec_a != LP_FP32 && prec_a != LP_BF16) || (prec_b != LP_FP32 && prec_b != LP_BF16)) return fail(ctx, LP_EINVAL, w + ": unknown precision");
+    if (V < 1 || V >= ((int64_t)1 << 31) - 1) return fail(ctx, LP_EINVAL, w + ": rows must be in [1, 2^31 - 2]");
+    if (D < 1 || D > (1 << 20)) return fail(ctx, LP_EINVAL, w + ": width must be in [1, 2^20]");
+    if (N < 0 || N >= (int64_t)1 << 31) return fail(ctx, LP_EINVAL, w + ": number of ids must be in [0, 2^31)");
+    if (ld_rows < D || ld_ids < D) return fail(ctx, LP_EINVAL, w + ": a row pitch is smaller than the width");
+    if (!std::isfinite(scale)) return fail(ctx, LP_EINVAL, w + ": scale is not finite");
+    return LP_OK;
+}
+
+extern "C" lp_status lp_embed(lp_ctx *ctx, int32_t table_prec, const void *table, int64_t rows, int32_t width, int64_t ld_table, const int32_t *ids, int64_t n_ids,
+                              int32_t padding_id, double scale, int32_t out_prec, void *out, int64_t ld_out)
+{
+    if (!ctx) return LP_EINVAL;
+    lp_status s = check_table(ctx, "lp_embed", table_prec, out_prec, rows, width, ld_table, n_ids, ld_out, scale);
+    if (s != LP_OK) return s;
+    if (table_prec == LP_BF16 && out_prec == LP_FP32) return fail(ctx, LP_EUNSUPPORTED, "lp_embed: a BF16 table is read as BF16");
+    if (!table || (n_ids > 0 && (!ids || !out))) return fail(ctx, LP_EINVAL, "lp_embed: null array");
+    if (misaligned(table, table_prec) || misaligned(ids, LP_FP32) || misaligned(out, out_prec)) return fail(ctx, LP_EINVAL, "lp_embed: an array is not aligned to its elements");
+    if (n_ids == 0) return LP_OK;
+    CK(cudaSetDevice(ctx->device));
+    const float f = (float)scale;
+    if (table_prec == LP_BF16) embed_launch<bf16, bf16>(ctx->ex, (const bf16 *)table, rows, width, ld_table, ids, n_ids, padding_id, f, (bf16 *)out, ld_out, ctx->err_flag);
+    else if (out_prec == LP_BF16) embed_launch<float, bf16>(ctx->ex, (const float *)table, rows, width, ld_table, ids, n_ids, padding_id, f, (bf16 *)out, ld_out, ctx->err_flag);
+    else embed_launch<float, float>(ctx->ex, (const float *)table, rows, width, ld_table, ids, n_ids, padding_id, f, (float *)out, ld_out, ctx->err_flag);
+    CK_LAUNCH();
+    return LP_OK;
+}
+
+extern "C" lp_status lp_embed_grad(lp_ctx *ctx, int32_t dout_prec, const void *dout, int64_t ld_dout, const int32_t *ids, int64_t n_ids, int32_t padding_id, double scale,
+                                   int64_t rows, int32_t width, int32_t grad_prec, void *grad, int64_t ld_grad, int32_t accumulate)
+{
+    if (!ctx) return LP_EINVAL;
+    lp_status s = check_table(ctx, "lp_embed_grad", dout_prec, grad_prec, rows, width, ld_grad, n_ids, ld_dout, scale);
+    if (s != LP_OK) return s;
+    if (dout_prec == LP_FP32 && grad_prec == LP_BF16) return fail(ctx, LP_EUNSUPPORTED, "lp_embed_grad: a BF16 gradient needs BF16 rows");
+    if (!grad || (n_ids > 0 && (!ids || !dout))) return fail(ctx, LP_EINVAL, "lp_embed_grad: null array");
+    if (misaligned(dout, dout_prec) || misaligned(ids, LP_FP32) || misaligned(grad, grad_prec))
+        return fail(ctx, LP_EINVAL, "lp_embed_grad: an array is not aligned to its elements");
+    if (n_ids == 0 && accumulate) return LP_OK;
+    CK(cudaSetDevice(ctx->device));
+    // one workspace: keys and values (two sets each for the sort), bit per row, digit counts, partial rows of the chunks
+    EmbedGradScratch sc;
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) & ~(size_t)255; return here; };
+    const size_t n4 = sizeof(uint32_t) * (size_t)std::max<int64_t>(n_ids, 1), parts = sizeof(float) * (size_t)ceil_div64(std::max<int64_t>(n_ids, 1), EG_CHUNK) * width;
+    const size_t o_keys = take(n4), o_vals = take(n4), o_keys2 = take(n4), o_vals2 = take(n4), o_named = take(sizeof(uint32_t) * (size_t)ceil_div64(rows, 32));
+    const size_t o_hist = take(sizeof(int) * (size_t)SortScratch::hist_ints(n_ids)), o_scan = take(sizeof(int) * (size_t)SortScratch::scan_ints(n_ids));
+    const size_t o_head = take(parts), o_tail = take(parts);
+    uint8_t *ws = nullptr;
+    s = op_workspace(ctx, at, &ws);
+    if (s != LP_OK) return s;
+    sc.keys = (uint32_t *)(ws + o_keys); sc.vals = (uint32_t *)(ws + o_vals);
+    sc.sort.keys_alt = (uint32_t *)(ws + o_keys2); sc.sort.vals_alt = (uint32_t *)(ws + o_vals2);
+    sc.named = (uint32_t *)(ws + o_named);
+    sc.sort.hist = (int *)(ws + o_hist); sc.sort.scan_tmp = (int *)(ws + o_scan);
+    sc.head = (float *)(ws + o_head); sc.tail = (float *)(ws + o_tail);
+    const float f = (float)scale;
+    if (dout_prec == LP_FP32) embed_grad_launch<float, float>(ctx->ex, (const float *)dout, ld_dout, ids, n_ids, padding_id, f, rows, width, (float *)grad, ld_grad, accumulate, sc, ctx->err_flag);
+    else if (grad_prec == LP_FP32) embed_grad_launch<bf16, float>(ctx->ex, (const bf16 *)dout, ld_dout, ids, n_ids, padding_id, f, rows, width, (float *)grad, ld_grad, accumulate, sc, ctx->err_flag);
+    else embed_grad_launch<bf16, bf16>(ctx->ex, (const bf16 *)dout, ld_dout, ids, n_ids, padding_id, f, rows, width, (bf16 *)grad, ld_grad, accumulate, sc, ctx->err_flag);
+    CK_LAUNCH();
+    return LP_OK;
+}
+
+// ----------------------------------------------------------------------------------------------
+// orthogonalised updates
+// ----------------------------------------------------------------------------------------------
+constexpr int NS_MAX_DIM = 1 << 17;
+constexpr size_t NS_WORKSPACE = (size_t)4 << 30;  // repetitions are taken in groups that fit this (one matrix may need more)
+
+static lp_status check_ns(lp_ctx *ctx, const char *who, int32_t steps, const double *coeffs, double eps, double (&c)[3])
+{
+    const std::string w(who);
+    c[0] = 3.4445; c[1] = -4.7750; c[2] = 2.0315;
+    if (coeffs) { c[0] = coeffs[0]; c[1] = coeffs[1]; c[2] = coeffs[2]; }
+    if (steps < 1 || steps > 64) return fail(ctx, LP_EINVAL, w + ": steps must be in [1, 64]");
+    if (!(eps >= 0.0) || !std::isfinite(eps)) return fail(ctx, LP_EINVAL, w + ": eps must be finite and not negative");
+    if (!ns_coefficients_ok(c[0], c[1], c[2], steps))
+        return fail(ctx, LP_EINVAL, w + ": with these coefficients singular values in [0, 1] can grow beyond 2 (or b A + c A^2 beyond 200)");
+    return LP_OK;
+}
+
+static void ns_orient(NsMat &m, int rows, int cols)
+{
+    m.tall = rows > cols;
+    m.m = std::min(rows, cols);
+    m.n = std::max(rows, cols);
+    m.repeat = 1;
+}
+
+extern "C" lp_status lp_orthogonalize(lp_ctx *ctx, int32_t prec, int64_t batch, int32_t rows, int32_t cols, const void *U, int64_t ld_u, int64_t stride_u, int32_t steps,
+                                      const double *coeffs, double eps, void *out, int64_t ld_out, int64_t stride_out)
+{
+    if (!ctx) return LP_EINVAL;
+    if (prec != LP_FP32 && prec != LP_BF16) return fail(ctx, LP_EINVAL, "lp_orthogonalize: unknown precision");
+    if (batch < 0 || rows < 0 || cols < 0) return fail(ctx, LP_EINVAL, "lp_orthogonalize: negative size");
+    if (rows > NS_MAX_DIM || cols > NS_MAX_DIM) return fail(ctx, LP_EINVAL, "lp_orthogonalize: a matrix has at most 2^17 rows and columns");
+    if (ld_u < cols || ld_out < cols) return fail(ctx, LP_EINVAL, "lp_orthogonalize: a row pitch is smaller than the number of columns");
+    if (batch > 1 && rows > 0 && (stride_u < 0 || stride_out < (rows - 1) * ld_out + cols))
+        return fail(ctx, LP_EINVAL, "lp_orthogonalize: matrices of the result overlap");
+    double c[3];
+    lp_status s = check_ns(ctx, "lp_orthogonalize", steps, coeffs, eps, c);
+    if (s != LP_OK) return s;
+    if (batch == 0 || rows == 0 || cols == 0) return LP_OK;
+    if (!U || !out) return fail(ctx, LP_EINVAL, "lp_orthogonalize: null array");
+    if (misaligned(U, prec) || misaligned(out, prec)) return fail(ctx, LP_EINVAL, "lp_orthogonalize: an array is not aligned to its elements");
+    CK(cudaSetDevice(ctx->device));
+    const int parts = prec == LP_FP32 ? 2 : 1;
+    const size_t elem = prec == LP_FP32 ? 4 : 2;
+    NsGroup g{};
+    g.count = 1;
+    ns_orient(g.mat[0], rows, cols);
+    const size_t one = ns_layout(g).bytes(parts);
+    const int64_t at_once = std::max<int64_t>(1, std::min<int64_t>({batch, (int64_t)(NS_WORKSPACE / one), (int64_t)1 << 16}));
+    for (int64_t b0 = 0; b0 < batch; b0 += at_once) {
+        NsMat &m = g.mat[0];
+        m.repeat = (int)std::min<int64_t>(at_once, batch - b0);
+        m.src_stride = stride_u; m.ld_src = ld_u;
+        m.dst_stride = stride_out; m.ld_dst = ld_out;
+        const NsLayout l = ns_layout(g);
+        uint8_t *ws = nullptr;
+        s = op_workspace(ctx, l.bytes(parts), &ws);
+        if (s != LP_OK) return s;
+        NsSource src{};
+        src.u = (const uint8_t *)U + (size_t)(b0 * stride_u) * elem;
+        src.bf16_u = prec == LP_BF16;
+        const NsTarget to{(uint8_t *)out + (size_t)(b0 * stride_out) * elem, prec == LP_BF16, nullptr, 0.f};
+        std::string err;
+        if (!ns_run(ctx->tc, ctx->ex, src, g, l, parts, steps, c[0], c[1], c[2], eps, to, ws, err)) return fail(ctx, LP_ECUDA, "lp_orthogonalize: " + err);
+    }
+    CK_LAUNCH();
+    return LP_OK;
+}
+
+extern "C" lp_status lp_muon_step(lp_ctx *ctx, const lp_muon_desc *d, const lp_matrix *matrices, int32_t n_matrices, int64_t n_params, const float *params,
+                                  const float *momentum, const float *adam_v, const float *grads, int64_t t, float *new_params, float *new_momentum, float *new_adam_v)
+{
+    if (!ctx) return LP_EINVAL;
+    if (!d) return fail(ctx, LP_EINVAL, "lp_muon_step: desc is NULL");
+    std::vector<lp_matrix> mats;
+    try {
+        if (matrices) {
+            if (n_matrices < 0 || n_params < 0) return fail(ctx, LP_EINVAL, "lp_muon_step: negative size");
+            mats.assign(matrices, matrices + n_matrices);
+        } else {
+            if (!ctx->model_set) return fail(ctx, LP_ESTATE, "lp_muon_step: pass the matrices or set a model first");
+            if (n_params != ctx->n_params) return fail(ctx, LP_EINVAL, "lp_muon_step: n_params differs from the model's");
+            for (int k = 0; k < ctx->K; ++k) {
+                const LayerBuf &L = ctx->layer[k];
+                for (int h = 0; h < L.Kin / L.Fi; ++h) mats.push_back({L.off_w + (int64_t)h * L.Fi * L.Fo, L.Fi, L.Fo});
+            }
+            if (ctx->mlp)
+                for (int j = 0; j < 2; ++j) mats.push_back({ctx->pred[j].off_w, ctx->pred[j].Kin, ctx->pred[j].Fo});
+        }
+        std::sort(mats.begin(), mats.end(), [](const lp_matrix &a, const lp_matrix &b) { return a.offset < b.offset; });
+    } catch (const std::bad_alloc &) {
+        return fail(ctx, LP_ENOMEM, "lp_muon_step: host allocation failed");
+    }
+    int64_t end = 0;
+    bool vectors = false;
+    for (const lp_matrix &m : mats) {
+        if (m.rows < 1 || m.cols < 1 || m.rows > NS_MAX_DIM || m.cols > NS_MAX_DIM) return fail(ctx, LP_EINVAL, "lp_muon_step: a matrix has 1 to 2^17 rows and columns");
+        if (m.offset < end || m.offset > n_params - (int64_t)m.rows * m.cols) return fail(ctx, LP_EINVAL, "lp_muon_step: matrices overlap or leave the parameter vector");
+        vectors |= m.offset > end;
+        end = m.offset + (int64_t)m.rows * m.cols;
+    }
+    vectors |= end < n_params;
+    double c[3];
+    const bool default_coeffs = d->coeffs[0] == 0.0 && d->coeffs[1] == 0.0 && d->coeffs[2] == 0.0;
+    lp_status s = check_ns(ctx, "lp_muon_step", d->steps, default_coeffs ? nullptr : d->coeffs, d->eps, c);
+    if (s != LP_OK) return s;
+    for (double x : {d->grad_scale, d->lr, d->momentum, d->weight_decay, d->adam_lr, d->adam_beta1, d->adam_beta2, d->adam_eps})
+        if (!std::isfinite(x)) return fail(ctx, LP_EINVAL, "lp_muon_step: a hyper-parameter is not finite");
+    if (vectors && t < 1) return fail(ctx, LP_EINVAL, "lp_muon_step: t counts from 1");
+    if (n_params == 0) return LP_OK;
+    if (!params || !momentum || !grads || (vectors && !adam_v)) return fail(ctx, LP_EINVAL, "lp_muon_step: null array");
+    for (const void *q : {(const void *)params, (const void *)momentum, (const void *)adam_v, (const void *)grads, (const void *)new_params, (const void *)new_momentum,
+                          (const void *)new_adam_v})
+        if (misaligned(q, LP_FP32)) return fail(ctx, LP_EINVAL, "lp_muon_step: an array is not aligned to its elements");
+    if (!new_params) new_params = const_cast<float *>(params);
+    if (!new_momentum) new_momentum = const_cast<float *>(momentum);
+    if (!new_adam_v) new_adam_v = const_cast<float *>(adam_v);
+    CK(cudaSetDevice(ctx->device));
+    ctx->param_version += 1;  // embeddings kept for lp_score belong to the old weights
+    ProfScope prof(ctx->ex, LP_PROF_ADAM, (double)n_params * 20.0);
+    const double c1 = 1.0 - std::pow(d->adam_beta1, (double)t), c2 = 1.0 - std::pow(d->adam_beta2, (double)t);
+    int64_t done = 0;
+    for (size_t i0 = 0; i0 == 0 || i0 < mats.size(); i0 += NS_MAX_MATS) {
+        const size_t i1 = std::min(mats.size(), i0 + NS_MAX_MATS);
+        NsGroup g{};
+        NsSpans sp{};
+        auto span = [&](int64_t from, int64_t to) {
+            if (to <= from) return;
+            sp.begin[sp.count] = from;
+            sp.first[sp.count + 1] = sp.first[sp.count] + (to - from);
+            ++sp.count;
+        };
+        for (size_t i = i0; i < i1; ++i) {
+            NsMat &m = g.mat[g.count++];
+            ns_orient(m, mats[i].rows, mats[i].cols);
+            m.src = m.dst = mats[i].offset;
+            m.ld_src = m.ld_dst = mats[i].cols;
+            m.update = (float)(d->lr * std::sqrt(std::max(1.0, (double)mats[i].cols / mats[i].rows)));
+            span(done, mats[i].offset);
+            done = mats[i].offset + (int64_t)mats[i].rows * mats[i].cols;
+        }
+        if (i1 == mats.size()) span(done, n_params);
+        if (g.count > 0) {
+            const NsLayout l = ns_layout(g);
+            uint8_t *ws = nullptr;
+            s = op_workspace(ctx, l.bytes(2), &ws);
+            if (s != LP_OK) return s;
+            NsSource src{};
+            src.grads = grads; src.momentum = momentum; src.new_momentum = new_momentum;
+            src.adam_v = adam_v; src.new_adam_v = adam_v && new_adam_v != adam_v ? new_adam_v : nullptr;
+            src.grad_scale = (float)d->grad_scale; src.mu = (float)d->momentum; src.nesterov = d->nesterov;
+            const NsTarget to{new_params, 0, params, (float)(1.0 - d->lr * d->weight_decay)};
+            std::string err;
+            if (!ns_run(ctx->tc, ctx->ex, src, g, l, 2, d->steps, c[0], c[1], c[2], d->eps, to, ws, err)) return fail(ctx, LP_ECUDA, "lp_muon_step: " + err);
+        }
+        if (sp.count > 0) {
+            launch_dep(ns_adam_kernel, dim3(nblk(sp.first[sp.count])), dim3(256), 0, ctx->ex.st, params, momentum, adam_v, grads, sp, (float)d->grad_scale, (float)d->adam_lr,
+                       (float)d->adam_beta1, (float)(1.0 - d->adam_beta1), (float)d->adam_beta2, (float)(1.0 - d->adam_beta2), (float)d->adam_eps, (float)(1.0 / c1), (float)(1.0 / c2),
+                       new_params, new_momentum, new_adam_v);
+            ctx->ex.launches += 1;
+        }
+    }
     CK_LAUNCH();
     return LP_OK;
 }
