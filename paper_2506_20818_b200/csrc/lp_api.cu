@@ -133,6 +133,7 @@ struct lp_ctx {
     TcState tc;                         // tensor-core GEMM state (descriptor encoder, device error word)
     uint8_t *op_ws = nullptr;           // workspace of the embedding gradient and of the orthogonalisation: grows to the largest call
     size_t op_ws_bytes = 0;
+    NsCounters ns_counters;             // barrier counters of the orthogonalisation's chain kernel
     bf16 *w16 = nullptr, *w16t = nullptr;  // BF16 path: the parameter vector of the current call as BF16, as is and with every weight matrix transposed
     bf16 *w16s = nullptr;                  // ... and with the SAGE layers' [W_self ; W_neigh] stored side by side (see weights_cache_kernel)
     // One-pass SAGE layers l >= 1 on the tensor-core pair kernel take the input gradient as
@@ -295,15 +296,17 @@ extern "C" lp_status lp_create(lp_ctx **out, int32_t device, void *cuda_stream)
     ctx->device = device;
     ctx->ex.st = (cudaStream_t)cuda_stream;
     if (cudaMalloc((void **)&ctx->err_flag, 256) != cudaSuccess || cudaMalloc((void **)&ctx->exhausted_dev, 256) != cudaSuccess ||
-        cudaMallocHost((void **)&ctx->host_counts, 64 * sizeof(int)) != cudaSuccess) {
+        cudaMallocHost((void **)&ctx->host_counts, 64 * sizeof(int)) != cudaSuccess ||
+        cudaMalloc((void **)&ctx->ns_counters.dev, 2 * NSC_BARRIERS * sizeof(unsigned)) != cudaSuccess) {
         delete ctx;
         return fail(nullptr, LP_ENOMEM, "lp_create: allocation failed");
     }
     cudaMemset(ctx->err_flag, 0, 256);
     cudaMemset(ctx->exhausted_dev, 0, 256);
+    cudaMemset(ctx->ns_counters.dev, 0, 2 * NSC_BARRIERS * sizeof(unsigned));
     std::string tc_err;
     if (!tc_init(ctx->tc, tc_err) || !ns_init(tc_err)) {
-        cudaFree(ctx->err_flag); cudaFree(ctx->exhausted_dev); cudaFreeHost(ctx->host_counts);
+        cudaFree(ctx->err_flag); cudaFree(ctx->exhausted_dev); cudaFreeHost(ctx->host_counts); cudaFree(ctx->ns_counters.dev);
         delete ctx;
         return fail(nullptr, LP_ECUDA, "lp_create: " + tc_err);
     }
@@ -322,6 +325,7 @@ extern "C" void lp_destroy(lp_ctx *ctx)
     free_list(ctx->graph_allocs);
     tc_destroy(ctx->tc);
     cudaFree(ctx->op_ws);
+    cudaFree(ctx->ns_counters.dev);
     for (cudaEvent_t e : ctx->ex.prof.pool) cudaEventDestroy(e);
     cudaFree(ctx->err_flag);
     cudaFree(ctx->exhausted_dev);
@@ -2277,7 +2281,10 @@ extern "C" lp_status lp_orthogonalize(lp_ctx *ctx, int32_t prec, int64_t batch, 
         src.bf16_u = prec == LP_BF16;
         const NsTarget to{(uint8_t *)out + (size_t)(b0 * stride_out) * elem, prec == LP_BF16, nullptr, 0.f};
         std::string err;
-        if (!ns_run(ctx->tc, ctx->ex, src, g, l, parts, steps, c[0], c[1], c[2], eps, to, ws, err)) return fail(ctx, LP_ECUDA, "lp_orthogonalize: " + err);
+        NsAdam none{};
+        const bool ok = parts == 2 ? ns_run<2>(ctx->tc, ctx->ex, src, g, l, none, ctx->ns_counters, steps, c[0], c[1], c[2], eps, to, ws, err)
+                                   : ns_run<1>(ctx->tc, ctx->ex, src, g, l, none, ctx->ns_counters, steps, c[0], c[1], c[2], eps, to, ws, err);
+        if (!ok) return fail(ctx, LP_ECUDA, "lp_orthogonalize: " + err);
     }
     CK_LAUNCH();
     return LP_OK;
@@ -2339,8 +2346,14 @@ extern "C" lp_status lp_muon_step(lp_ctx *ctx, const lp_muon_desc *d, const lp_m
     for (size_t i0 = 0; i0 == 0 || i0 < mats.size(); i0 += NS_MAX_MATS) {
         const size_t i1 = std::min(mats.size(), i0 + NS_MAX_MATS);
         NsGroup g{};
-        NsSpans sp{};
+        NsAdam ad{};
+        ad.p = params; ad.m = momentum; ad.v = adam_v; ad.grad = grads;
+        ad.pn = new_params; ad.mn = new_momentum; ad.vn = new_adam_v;
+        ad.scale = (float)d->grad_scale; ad.lr = (float)d->adam_lr; ad.eps = (float)d->adam_eps;
+        ad.b1 = (float)d->adam_beta1; ad.one_minus_b1 = (float)(1.0 - d->adam_beta1); ad.b2 = (float)d->adam_beta2; ad.one_minus_b2 = (float)(1.0 - d->adam_beta2);
+        ad.inv_c1 = (float)(1.0 / c1); ad.inv_c2 = (float)(1.0 / c2);
         auto span = [&](int64_t from, int64_t to) {
+            NsSpans &sp = ad.spans;
             if (to <= from) return;
             sp.begin[sp.count] = from;
             sp.first[sp.count + 1] = sp.first[sp.count] + (to - from);
@@ -2356,25 +2369,18 @@ extern "C" lp_status lp_muon_step(lp_ctx *ctx, const lp_muon_desc *d, const lp_m
             done = mats[i].offset + (int64_t)mats[i].rows * mats[i].cols;
         }
         if (i1 == mats.size()) span(done, n_params);
-        if (g.count > 0) {
-            const NsLayout l = ns_layout(g);
-            uint8_t *ws = nullptr;
-            s = op_workspace(ctx, l.bytes(2), &ws);
-            if (s != LP_OK) return s;
-            NsSource src{};
-            src.grads = grads; src.momentum = momentum; src.new_momentum = new_momentum;
-            src.adam_v = adam_v; src.new_adam_v = adam_v && new_adam_v != adam_v ? new_adam_v : nullptr;
-            src.grad_scale = (float)d->grad_scale; src.mu = (float)d->momentum; src.nesterov = d->nesterov;
-            const NsTarget to{new_params, 0, params, (float)(1.0 - d->lr * d->weight_decay)};
-            std::string err;
-            if (!ns_run(ctx->tc, ctx->ex, src, g, l, 2, d->steps, c[0], c[1], c[2], d->eps, to, ws, err)) return fail(ctx, LP_ECUDA, "lp_muon_step: " + err);
-        }
-        if (sp.count > 0) {
-            launch_dep(ns_adam_kernel, dim3(nblk(sp.first[sp.count])), dim3(256), 0, ctx->ex.st, params, momentum, adam_v, grads, sp, (float)d->grad_scale, (float)d->adam_lr,
-                       (float)d->adam_beta1, (float)(1.0 - d->adam_beta1), (float)d->adam_beta2, (float)(1.0 - d->adam_beta2), (float)d->adam_eps, (float)(1.0 / c1), (float)(1.0 / c2),
-                       new_params, new_momentum, new_adam_v);
-            ctx->ex.launches += 1;
-        }
+        if (g.count == 0 && ad.spans.count == 0) break;
+        const NsLayout l = ns_layout(g);
+        uint8_t *ws = nullptr;
+        s = op_workspace(ctx, l.bytes(2), &ws);
+        if (s != LP_OK) return s;
+        NsSource src{};
+        src.grads = grads; src.momentum = momentum; src.new_momentum = new_momentum;
+        src.adam_v = adam_v; src.new_adam_v = adam_v && new_adam_v != adam_v ? new_adam_v : nullptr;
+        src.grad_scale = (float)d->grad_scale; src.mu = (float)d->momentum; src.nesterov = d->nesterov;
+        const NsTarget to{new_params, 0, params, (float)(1.0 - d->lr * d->weight_decay)};
+        std::string err;
+        if (!ns_run<2>(ctx->tc, ctx->ex, src, g, l, ad, ctx->ns_counters, d->steps, c[0], c[1], c[2], d->eps, to, ws, err)) return fail(ctx, LP_ECUDA, "lp_muon_step: " + err);
     }
     CK_LAUNCH();
     return LP_OK;

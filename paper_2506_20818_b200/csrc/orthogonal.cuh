@@ -7,25 +7,32 @@
 // significant bits where BF16 carries eight, at the same rate, and the range it lacks is not needed here: the values
 // are bounded by the polynomial (the host refuses coefficients for which they are not), so X is held as 2^12 X and A and B
 // as 2^8 A, 2^8 B, which keeps the parts that matter inside the normal numbers of FP16.
-// X is always kept as a pair of FP16 numbers hi + lo (22 bits), and the term a X of every step is taken from both.
-//   BF16 results : the products take the leading parts only, A and B are one FP16 number per value
-//   FP32 results : A and B are pairs too, products hi*hi + hi*lo + lo*hi into one accumulator
-// Why X keeps its low part where the products do not read it: rounding X to eleven bits would add a matrix of full rank, and
-// whatever lies in directions that X hardly has is multiplied by a in every step (3.4^5 = 480 for five).  The errors of the
-// products are of the form dB X and B dX, which vanish in such directions, so they stay at their own size.
+// X is kept twice: in FP32, from which the term a X of every step is taken, and as FP16 operands.
+//   BF16 results : X, A and B are one FP16 number per value in the products
+//   FP32 results : pairs of FP16 numbers hi + lo (22 bits), products hi*lo + lo*hi + hi*hi; the accumulator of the matrix
+//                  instructions rounds towards zero, so it only adds up 32 to 64 terms at a time and those sums are
+//                  added in FP32 registers (1000 x 417: error 1.3e-5 with one accumulator for all of K, 1e-6 this way)
+// Why X keeps more bits than its operands: rounding X to eleven bits would add a matrix of full rank, and whatever lies
+// in directions that X hardly has is multiplied by a in every step (3.4^5 = 480 for five).  The errors of the products are
+// of the form dB X and B dX, which vanish in such directions, so they stay at their own size.  For the same reason X_0 is
+// U times a power of two 2^12 r / |U|, r in [1/2, 1), which is exact; b / r^2 and c / r^4 in the place of b and c keep r X
+// going in the place of X, and the result is divided by r.
 // A matrix with more rows than columns is iterated transposed: m = min(rows, cols), n = max(rows, cols).
-// A and B are symmetric, so only tiles on and above the diagonal are computed and the others are written by mirroring.
 //
 // All matrices of a call lie in common arenas (X: rows of `pitch_x`, A and B: rows of `pitch_a`), each padded with zeros
 // to multiples of 64; the padding stays zero through every product.
 #pragma once
 #include <cuda_fp16.h>
 
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
 #include "common.cuh"
 #include "embed.cuh"
 #include "gemm_tc.cuh"
 
-constexpr int NS_MAX_MATS = 24;       // descriptors in one launch group (they travel as kernel arguments, 4 KiB in all)
+constexpr int NS_MAX_MATS = 16;       // descriptors in one launch group (they travel as kernel arguments, 4 KiB in all)
 constexpr float NS_X_SCALE = 4096.f;  // X is held as 2^12 X
 constexpr float NS_A_SCALE = 256.f;   // A and B as 2^8 A, 2^8 B
 
@@ -35,10 +42,12 @@ struct NsMat {
     int repeat;            // matrices of this shape, `src_stride` elements apart
     int tall;              // rows > cols: the arena holds the transpose
     int row_x, row_a;      // first arena row of the first repetition (mp rows each)
-    int tiles_sym, tiles_x;    // tiles of one repetition: A or B (on and above the diagonal), X
-    int first_sym, first_x;    // tiles before this descriptor
+    int tiles_a, tiles_x;      // tiles of one repetition: A or B, X
+    int first_a, first_x;      // tiles before this descriptor
     int first_norm, first_conv;  // blocks of the norm and conversion kernels before this descriptor
     int norm_blocks, conv_blocks;  // blocks of one repetition
+    int norm_elems;        // elements of one block of the norm kernel
+    int index;             // matrices before this descriptor
     long long src, src_stride, ld_src;  // element offset, distance of repetitions, row pitch of U
     long long dst, dst_stride, ld_dst;  // ... of the result
     float update;          // weight update: lr * sqrt(max(1, cols / rows))
@@ -46,6 +55,13 @@ struct NsMat {
 struct NsGroup {
     int count;
     NsMat mat[NS_MAX_MATS];
+};
+
+struct NsX {             // one of the two buffers of X
+    float *full;
+    __half *hi;
+    size_t lo_off;       // the low parts lie this many elements behind the high ones
+    int pitch;
 };
 
 // which descriptor holds item t, given the running starts
@@ -56,20 +72,12 @@ template <typename F> LP_DEVINL int ns_find(const NsGroup &g, int t, F first)
     return d;
 }
 
-constexpr int NS_X_PARTS = 2;
-
-LP_DEVINL void ns_store_parts(float v, int parts, __half *hi, size_t lo_off)
-{
-    const __half h = __float2half_rn(v);
-    *hi = h;
-    if (parts == 2) hi[lo_off] = __float2half_rn(v - __half2float(h));
-}
-
 // ---------------------------------------------------------------------------------------------
 // what the iteration starts from
 // ---------------------------------------------------------------------------------------------
 constexpr int NS_THREADS = 256;
-constexpr int NS_NORM_ELEMS = 8192;  // elements of one block of the norm kernel
+constexpr int NS_NORM_ELEMS = 2048;   // elements of one block of the norm kernel, more where a matrix would need over 1024 blocks
+constexpr int NS_NORM_BLOCKS = 1024;
 
 struct NsSource {          // where U comes from
     const void *u;         // the matrix itself (plain orthogonalisation)
@@ -86,84 +94,195 @@ struct NsSource {          // where U comes from
 LP_DEVINL float ns_source(const NsSource &s, long long i)
 {
     if (s.grads) {
-        const float m = s.new_momentum[i];
+        const float m = __ldcg(s.new_momentum + i);  // written by other blocks, in the chain kernel of the same launch
         return s.nesterov ? fmaf(s.mu, m, s.grad_scale * s.grads[i]) : m;
     }
     return s.bf16_u ? __bfloat162float(((const bf16 *)s.u)[i]) : ((const float *)s.u)[i];
 }
 
-// partial[b] = sum of squares over the block's elements, in double: no overflow for any FP32 input.  The weight update also
-// writes M' here.
-__global__ void __launch_bounds__(NS_THREADS) ns_norm_kernel(const NsSource s, const __grid_constant__ NsGroup g, double *__restrict__ partial)
+// The weight update's other parameters: Adam over the stretches of the flat vector between the matrices.
+struct NsSpans {
+    int count;
+    long long begin[NS_MAX_MATS + 1], first[NS_MAX_MATS + 2];  // first element, and elements before the stretch; first[count] = all
+};
+struct NsAdam {
+    const float *p, *m, *v, *grad;
+    float *pn, *mn, *vn;
+    float scale, lr, b1, one_minus_b1, b2, one_minus_b2, eps, inv_c1, inv_c2;
+    NsSpans spans;
+};
+constexpr int NS_ADAM_ELEMS = 1024;  // elements of one block
+
+template <int T> LP_DEVINL void ns_sync() { __syncwarp(); asm volatile("bar.sync 1, %0;" ::"n"(T) : "memory"); }  // the threads that share a block of work
+
+// ... the same with the OR of a condition over them, so that all take the same branch after it
+template <int T> LP_DEVINL bool ns_any(bool x)
 {
-    LP_DEP_ENTER();
-    const int t = blockIdx.x;
+    uint32_t r;
+    __syncwarp();
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.aligned.pred q, 1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"((uint32_t)x), "n"(T) : "memory");
+    return r != 0;
+}
+
+template <int T> LP_DEVINL void ns_adam_block(const NsAdam &a, int blk, int tid)
+{
+    for (int u = 0; u < NS_ADAM_ELEMS / T; ++u) {
+        const long long e = (long long)blk * NS_ADAM_ELEMS + u * T + tid;
+        if (e >= a.spans.first[a.spans.count]) return;
+        int s = 0;
+        while (e >= a.spans.first[s + 1]) ++s;
+        const long long i = a.spans.begin[s] + (e - a.spans.first[s]);
+        const float g = a.scale * a.grad[i];
+        const float mi = a.b1 * a.m[i] + a.one_minus_b1 * g;
+        const float vi = a.b2 * a.v[i] + a.one_minus_b2 * g * g;
+        const float pi = a.p[i] - a.lr * (mi * a.inv_c1) / (sqrtf(vi * a.inv_c2) + a.eps);
+        a.mn[i] = mi;
+        a.vn[i] = vi;
+        a.pn[i] = pi;
+    }
+}
+
+// partial[t] = sum of squares over the block's elements, in double: no overflow for any FP32 input.  The weight update also
+// writes M' here.
+template <int T> LP_DEVINL void ns_norm_block(const NsSource &s, const NsGroup &g, int t, int tid, double *__restrict__ partial, double *sw)
+{
     const int d = ns_find(g, t, [](const NsMat &m) { return m.first_norm; });
     const NsMat &mat = g.mat[d];
     const int rep = (t - mat.first_norm) / mat.norm_blocks, blk = (t - mat.first_norm) % mat.norm_blocks;
     const long long rows = mat.tall ? mat.n : mat.m, cols = mat.tall ? mat.m : mat.n;
-    const long long e0 = (long long)blk * NS_NORM_ELEMS, e1 = min(e0 + NS_NORM_ELEMS, rows * cols);
+    const long long e0 = (long long)blk * mat.norm_elems, e1 = min(e0 + mat.norm_elems, rows * cols);
     const long long base = mat.src + rep * mat.src_stride;
     double acc = 0.0;
-    for (long long e = e0 + threadIdx.x; e < e1; e += NS_THREADS) {
-        const long long r = e / cols, i = base + r * mat.ld_src + (e - r * cols);
-        if (s.grads) {
-            s.new_momentum[i] = fmaf(s.mu, s.momentum[i], s.grad_scale * s.grads[i]);
-            if (s.new_adam_v) s.new_adam_v[i] = s.adam_v[i];
+    constexpr int U = 4;  // elements in flight per thread
+    for (long long e = e0 + tid; e < e1; e += U * T) {
+        long long at[U];
+        float x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const long long i = e + u * T;
+            if (mat.ld_src == cols) at[u] = base + i;
+            else { const long long r = i / cols; at[u] = base + r * mat.ld_src + (i - r * cols); }
+            if (i >= e1) at[u] = -1;
         }
-        const double x = (double)ns_source(s, i);
-        acc = fma(x, x, acc);
+        if (s.grads) {
+            float gr[U], mo[U], av[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                gr[u] = at[u] >= 0 ? s.grad_scale * s.grads[at[u]] : 0.f;
+                mo[u] = at[u] >= 0 ? s.momentum[at[u]] : 0.f;
+                if (s.new_adam_v) av[u] = at[u] >= 0 ? s.adam_v[at[u]] : 0.f;
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const float m = fmaf(s.mu, mo[u], gr[u]);
+                if (at[u] >= 0) {
+                    s.new_momentum[at[u]] = m;
+                    if (s.new_adam_v) s.new_adam_v[at[u]] = av[u];
+                }
+                x[u] = s.nesterov ? fmaf(s.mu, m, gr[u]) : m;
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) x[u] = at[u] >= 0 ? ns_source(s, at[u]) : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) acc = fma((double)x[u], (double)x[u], acc);
     }
-    __shared__ double sw[NS_THREADS / 32];
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, o);
-    if ((threadIdx.x & 31) == 0) sw[threadIdx.x >> 5] = acc;
-    __syncthreads();
-    if (threadIdx.x == 0) {
+    if ((tid & 31) == 0) sw[tid >> 5] = acc;
+    ns_sync<T>();
+    if (tid == 0) {
         double sum = 0.0;
-        for (int w = 0; w < NS_THREADS / 32; ++w) sum += sw[w];
+        for (int w = 0; w < T / 32; ++w) sum += sw[w];
         partial[t] = sum;
     }
+    ns_sync<T>();
 }
 
-// X_0 as FP16 parts, oriented and padded with zeros.  A block writes 64 rows x 64 columns of the arena.
-__global__ void __launch_bounds__(NS_THREADS) ns_convert_kernel(const NsSource s, const __grid_constant__ NsGroup g, const double *__restrict__ partial, float eps,
-                                                                __half *__restrict__ X, int pitch_x, size_t lo_off)
+// |U| + eps = 2^e r with r in [1/2, 1): X_0 is held as 2^12 2^-e U, which is 2^12 r times U / (|U| + eps)
+LP_DEVINL void ns_start_scale(double norm, float &r, double &pow2)
 {
-    LP_DEP_ENTER();
-    const int t = blockIdx.x;
+    int e = 0;
+    const double f = frexp(norm, &e);  // norm = f 2^e, f in [1/2, 1)
+    if (norm == 0.0 || !isfinite(norm)) {  // zeros divided by eps = 0, or a norm of infinity or NaN: NaN or zero come out of the products
+        r = 1.f;
+        pow2 = (double)NS_X_SCALE / norm;
+        return;
+    }
+    r = (float)f;
+    pow2 = ldexp((double)NS_X_SCALE, -e);
+}
+
+// X_0, oriented and padded with zeros: 64 rows x 64 columns of the arena.  `tile` holds 64 x 65 floats, `sw` T / 32 doubles.
+template <int PARTS, int T>
+LP_DEVINL void ns_convert_block(const NsSource &s, const NsGroup &g, int t, int tid, const double *partial, double eps, const NsX &X, float *inv_r, float *tile, double *sw)
+{
     const int d = ns_find(g, t, [](const NsMat &m) { return m.first_conv; });
     const NsMat &mat = g.mat[d];
     const int rep = (t - mat.first_conv) / mat.conv_blocks, blk = (t - mat.first_conv) % mat.conv_blocks;
-    __shared__ double sw[NS_THREADS / 32];
-    __shared__ float tile[64][65];
     double acc = 0.0;
-    for (int b = threadIdx.x; b < mat.norm_blocks; b += NS_THREADS) acc += partial[mat.first_norm + rep * mat.norm_blocks + b];
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, o);
-    if ((threadIdx.x & 31) == 0) sw[threadIdx.x >> 5] = acc;
-    __syncthreads();
-    acc = 0.0;
-    for (int w = 0; w < NS_THREADS / 32; ++w) acc += sw[w];
-    const double scale = (double)NS_X_SCALE / (sqrt(acc) + (double)eps);
+    for (int b = tid; b < mat.norm_blocks; b += T) acc += __ldcg(partial + mat.first_norm + rep * mat.norm_blocks + b);
     const int cb = mat.np / 64;
     const int i0 = (blk / cb) * 64, j0 = (blk % cb) * 64;
     const long long base = mat.src + rep * mat.src_stride;
-    const int lx = threadIdx.x & 63, ly = threadIdx.x >> 6;
-    if (mat.tall) {  // U is [n, m]: read rows of U (j), columns i consecutive, and turn the tile in shared memory
-        for (int y = ly; y < 64; y += 4) {
-            const int j = j0 + y, i = i0 + lx;
-            tile[lx][y] = (j < mat.n && i < mat.m) ? ns_source(s, base + (long long)j * mat.ld_src + i) : 0.f;
-        }
-    } else {
-        for (int y = ly; y < 64; y += 4) {
-            const int i = i0 + y, j = j0 + lx;
-            tile[y][lx] = (i < mat.m && j < mat.n) ? ns_source(s, base + (long long)i * mat.ld_src + j) : 0.f;
+    const int lx = tid & 63, ly = tid >> 6;
+    constexpr int R = 4096 / T, STEP = T / 64;  // elements per thread, rows of the tile between them
+    float u[R];
+#pragma unroll
+    for (int k = 0; k < R; ++k) {  // tall: U is [n, m]; its rows are read along i and the tile is turned in shared memory
+        const int y = ly + STEP * k;
+        const int i = mat.tall ? i0 + lx : i0 + y, j = mat.tall ? j0 + y : j0 + lx;
+        u[k] = i < mat.m && j < mat.n ? ns_source(s, base + (mat.tall ? (long long)j * mat.ld_src + i : (long long)i * mat.ld_src + j)) : 0.f;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, o);
+    if ((tid & 31) == 0) sw[tid >> 5] = acc;
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+        const int y = ly + STEP * k;
+        if (mat.tall) tile[lx * 65 + y] = u[k]; else tile[y * 65 + lx] = u[k];
+    }
+    ns_sync<T>();
+    acc = 0.0;
+    for (int w = 0; w < T / 32; ++w) acc += sw[w];
+    float r;
+    double pow2;
+    ns_start_scale(sqrt(acc) + eps, r, pow2);
+    if (blk == 0 && tid == 0) inv_r[mat.index + rep] = 1.f / r;
+    const int px = (tid & 31) * 2;  // two columns per thread
+#pragma unroll
+    for (int y = tid >> 5; y < 64; y += T / 32) {
+        const float a = (float)(tile[y * 65 + px] * pow2), b = (float)(tile[y * 65 + px + 1] * pow2);
+        const size_t at = (size_t)(mat.row_x + rep * mat.mp + i0 + y) * X.pitch + j0 + px;
+        *reinterpret_cast<float2 *>(X.full + at) = make_float2(a, b);
+        const __half2 h = __floats2half2_rn(a, b);
+        *reinterpret_cast<__half2 *>(X.hi + at) = h;
+        if (PARTS == 2) {
+            const float2 f = __half22float2(h);
+            *reinterpret_cast<__half2 *>(X.hi + X.lo_off + at) = __floats2half2_rn(a - f.x, b - f.y);
         }
     }
-    __syncthreads();
-    for (int y = ly; y < 64; y += 4)
-        ns_store_parts((float)((double)tile[y][lx] * scale), NS_X_PARTS, X + (size_t)(mat.row_x + rep * mat.mp + i0 + y) * pitch_x + j0 + lx, lo_off);
+    ns_sync<T>();
+}
+
+// the two steps as kernels of their own, for matrices too large for the chain kernel; blocks from `norm_blocks` on take Adam steps
+__global__ void __launch_bounds__(NS_THREADS) ns_norm_kernel(const NsSource s, const __grid_constant__ NsGroup g, const __grid_constant__ NsAdam adam, int norm_blocks,
+                                                             double *__restrict__ partial)
+{
+    LP_DEP_ENTER();
+    __shared__ double sw[NS_THREADS / 32];
+    if ((int)blockIdx.x < norm_blocks) ns_norm_block<NS_THREADS>(s, g, blockIdx.x, threadIdx.x, partial, sw);
+    else ns_adam_block<NS_THREADS>(adam, blockIdx.x - norm_blocks, threadIdx.x);
+}
+template <int PARTS>
+__global__ void __launch_bounds__(NS_THREADS) ns_convert_kernel(const NsSource s, const __grid_constant__ NsGroup g, const double *partial, double eps, const NsX X,
+                                                                float *inv_r)
+{
+    LP_DEP_ENTER();
+    __shared__ double sw[NS_THREADS / 32];
+    __shared__ float tile[64 * 65];
+    ns_convert_block<PARTS, NS_THREADS>(s, g, blockIdx.x, threadIdx.x, partial, eps, X, inv_r, tile, sw);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -173,14 +292,16 @@ enum { NS_GRAM = 0, NS_POLY = 1, NS_APPLY = 2, NS_LAST = 3 };
 
 struct NsPhase {
     int kind;
-    int parts;                           // FP16 parts that the products read
     float a, b, c;
-    int part_rows_a, part_rows_b;        // rows between the hi and lo parts of the first and second operand's arena
-    int row_off_b;                       // first row of the X buffer that is read (X lives in two buffers used in turn)
-    const __half *addend;                // POLY: A; APPLY, LAST: X
-    __half *out;                         // GRAM: A, POLY: B, APPLY: the other X buffer
-    int pitch;                           // of addend and out
-    size_t lo_off;                       // elements between the parts of addend and out
+    int lo_rows_a, lo_rows_b;            // rows between the hi and lo parts of the first and second operand's arena
+    int x_row0;                          // first row of the X buffer that is read
+    const __half *A;                     // POLY: the addend b A
+    const float *X;                      // APPLY, LAST: the addend a X
+    __half *out;                         // GRAM: A, POLY: B
+    int pitch_a;
+    size_t lo_off_a;                     // elements between the parts of A and B
+    NsX next;                            // APPLY: the other X buffer
+    const float *inv_r;                  // 1 / r of every matrix
     // LAST
     void *dst;
     int bf16_dst;
@@ -202,229 +323,901 @@ static __host__ __device__ inline uint32_t make_idesc_f16(int m, int n, bool b_m
     return d;
 }
 
-// tile t of the upper triangle (rows i <= columns j) of a T x T grid, row by row
-LP_DEVINL void ns_triangle(int t, int T, int &i, int &j)
+// eight FP16 values (one 16-byte piece) as floats, added to v
+LP_DEVINL void ns_add8(const uint4 &w, float *v)
 {
-    i = 0;
-    while (t >= T - i) { t -= T - i; ++i; }
-    j = i + t;
-}
-
-LP_DEVINL void ns_load32(const __half *hi, int parts, size_t lo_off, float *v)
-{
+    const uint32_t x[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        const uint4 w = *reinterpret_cast<const uint4 *>(hi + 8 * q);
-        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&x[k]));
-            v[8 * q + 2 * k] = f.x;
-            v[8 * q + 2 * k + 1] = f.y;
-        }
-    }
-    if (parts == 2) {
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const uint4 w = *reinterpret_cast<const uint4 *>(hi + lo_off + 8 * q);
-            const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&x[k]));
-                v[8 * q + 2 * k] += f.x;
-                v[8 * q + 2 * k + 1] += f.y;
-            }
-        }
+    for (int k = 0; k < 4; ++k) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&x[k]));
+        v[2 * k] += f.x;
+        v[2 * k + 1] += f.y;
     }
 }
-LP_DEVINL void ns_store32(const float *v, int parts, __half *hi, size_t lo_off)
+// 8 values as FP16 parts
+template <int PARTS> LP_DEVINL void ns_store8(const float *v, __half *hi, size_t lo_off)
 {
+    uint32_t h[4], l[4];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        uint32_t h[4], l[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const float x = v[8 * q + 2 * k], y = v[8 * q + 2 * k + 1];
-            const __half2 p = __floats2half2_rn(x, y);
+    for (int k = 0; k < 4; ++k) {
+        const __half2 p = __floats2half2_rn(v[2 * k], v[2 * k + 1]);
+        h[k] = *reinterpret_cast<const uint32_t *>(&p);
+        if (PARTS == 2) {
             const float2 f = __half22float2(p);
-            const __half2 r = __floats2half2_rn(x - f.x, y - f.y);
-            h[k] = *reinterpret_cast<const uint32_t *>(&p);
+            const __half2 r = __floats2half2_rn(v[2 * k] - f.x, v[2 * k + 1] - f.y);
             l[k] = *reinterpret_cast<const uint32_t *>(&r);
         }
-        *reinterpret_cast<uint4 *>(hi + 8 * q) = make_uint4(h[0], h[1], h[2], h[3]);
-        if (parts == 2) *reinterpret_cast<uint4 *>(hi + lo_off + 8 * q) = make_uint4(l[0], l[1], l[2], l[3]);
+    }
+    *reinterpret_cast<uint4 *>(hi) = make_uint4(h[0], h[1], h[2], h[3]);
+    if (PARTS == 2) *reinterpret_cast<uint4 *>(hi + lo_off) = make_uint4(l[0], l[1], l[2], l[3]);
+}
+
+// result columns col .. col + 63 of row `row` (oriented), already divided by the scale of X
+LP_DEVINL void ns_write_result(const NsPhase &p, const NsMat &mat, int rep, int row, int col, const float *v)
+{
+    const long long base = mat.dst + rep * mat.dst_stride;
+    if (mat.tall) {  // neighbouring lanes hold neighbouring rows, which are consecutive in the result
+#pragma unroll
+        for (int i = 0; i < 64; ++i) {
+            if (col + i >= mat.n) break;
+            const long long o = base + (long long)(col + i) * mat.ld_dst + row;
+            if (p.params) ((float *)p.dst)[o] = fmaf(-mat.update, v[i], p.keep * p.params[o]);
+            else if (p.bf16_dst) ((bf16 *)p.dst)[o] = __float2bfloat16_rn(v[i]);
+            else ((float *)p.dst)[o] = v[i];
+        }
+        return;
+    }
+    const long long o = base + (long long)row * mat.ld_dst + col;
+    const bool whole = col + 64 <= mat.n;
+    if (p.bf16_dst) {
+        bf16 *q = (bf16 *)p.dst + o;
+        if (whole && ((uintptr_t)q & 15) == 0) {
+#pragma unroll
+            for (int i = 0; i < 64; i += 8) store_elems<bf16, 8>(q + i, v + i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 64; ++i)
+                if (col + i < mat.n) q[i] = __float2bfloat16_rn(v[i]);
+        }
+        return;
+    }
+    float *q = (float *)p.dst + o;
+    const float *w = p.params ? p.params + o : nullptr;
+    if (whole && (((uintptr_t)q | (uintptr_t)w) & 15) == 0) {
+#pragma unroll
+        for (int i = 0; i < 64; i += 4) {
+            float x[4] = {v[i], v[i + 1], v[i + 2], v[i + 3]};
+            if (w) {
+                float old[4];
+                load_elems<float, 4>(w + i, old);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[k] = fmaf(-mat.update, x[k], p.keep * old[k]);
+            }
+            store_elems<float, 4>(q + i, x);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 64; ++i)
+            if (col + i < mat.n) q[i] = w ? fmaf(-mat.update, v[i], p.keep * w[i]) : v[i];
     }
 }
 
-// One CTA per 128 x 128 tile.  Warp 0 brings the operand tiles in by TMA (both parts of each), warp 1 issues the matrix
-// instructions, all four warps write the result.
-__global__ void __launch_bounds__(TC_THREADS) ns_product_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const NsPhase p,
-                                                                const __grid_constant__ NsGroup g)
+// One CTA per 128 x BN tile of the result.  Warp 0 brings the operand tiles in by TMA (all parts of both), warp 1 issues the
+// matrix instructions, the other BN / 16 warps hold 64 columns of one row per thread and write the result.
+//   chunks: after every block of 64 terms (PARTS = 2) or at the end (PARTS = 1) the accumulator changes hands; two of them
+//           in tensor memory are used in turn, so the next block's products run while the last one is added up
+//   all tiles of A and B are computed although they are symmetric: these kernels run where there are fewer tiles than SMs,
+//           and writing mirrored tiles would only lengthen them
+//   the next kernel of the chain is let in at once (its blocks set themselves up on idle SMs and wait for this one to end)
+template <int BN, int PARTS>
+__global__ void __launch_bounds__(64 + 2 * BN) ns_tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const NsPhase p,
+                                                              const __grid_constant__ NsGroup g)
 {
-    LP_DEP_ENTER();
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t bar_full[8], bar_empty[8], bar_acc;
+    __shared__ __align__(8) uint64_t bar_full[8], bar_empty[8], bar_acc_full[2], bar_acc_empty[2];
     __shared__ uint32_t tmem_base_s;
-    __shared__ int abort_s;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-    const bool sym = p.kind == NS_GRAM || p.kind == NS_POLY;
+    const bool square = p.kind == NS_GRAM || p.kind == NS_POLY;
     const int t = blockIdx.x;
-    const int d = sym ? ns_find(g, t, [](const NsMat &m) { return m.first_sym; }) : ns_find(g, t, [](const NsMat &m) { return m.first_x; });
+    const int d = square ? ns_find(g, t, [](const NsMat &m) { return m.first_a; }) : ns_find(g, t, [](const NsMat &m) { return m.first_x; });
     const NsMat &mat = g.mat[d];
-    const int per = sym ? mat.tiles_sym : mat.tiles_x, first = sym ? mat.first_sym : mat.first_x;
+    const int per = square ? mat.tiles_a : mat.tiles_x, first = square ? mat.first_a : mat.first_x;
     const int rep = (t - first) / per, tt = (t - first) % per;
     const int T = (mat.mp + 127) / 128;
-    int ti, tj;
-    if (sym) ns_triangle(tt, T, ti, tj);
-    else { ti = tt % T; tj = tt / T; }
+    const int ti = tt % T, tj = tt / T;
     const int K = p.kind == NS_GRAM ? mat.np : mat.mp;
     const int num_kb = K / TC_BK;
     const int slot_x = mat.row_x + rep * mat.mp, slot_a = mat.row_a + rep * mat.mp;
-    const int row_a0 = (p.kind == NS_GRAM ? p.row_off_b + slot_x : slot_a) + ti * 128;
-    const bool b_mn = !sym;
-    const int row_b0 = p.kind == NS_GRAM ? p.row_off_b + slot_x + tj * 128 : slot_a + tj * 128;  // K-major second operand
-    const int parts = p.parts, S = p.stages;
-    const uint32_t tile_bytes = 128 * TC_BK * 2;
-    const uint32_t stage_bytes = 2 * parts * tile_bytes;
+    const bool b_mn = !square;
+    const int S = p.stages;
+    constexpr uint32_t a_bytes = 128 * TC_BK * 2, b_bytes = BN * TC_BK * 2, stage_bytes = PARTS * (a_bytes + b_bytes);
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < S; ++s) {
             mbar_init(smem_u32(&bar_full[s]), 1);
             mbar_init(smem_u32(&bar_empty[s]), 1);
         }
-        mbar_init(smem_u32(&bar_acc), 1);
-        abort_s = 0;
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(smem_u32(&bar_acc_full[b]), 1);
+            mbar_init(smem_u32(&bar_acc_empty[b]), BN / 16);
+        }
         fence_barrier_init();
         fence_async_proxy();
+        tma_prefetch_desc(&mapA);
+        tma_prefetch_desc(&mapB);
     }
     if (warp == 0) {
         __syncwarp();
-        tmem_alloc(smem_u32(&tmem_base_s), 128);
+        tmem_alloc(smem_u32(&tmem_base_s), 2 * BN);
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem_d = tmem_base_s;
+    const uint32_t tmem = tmem_base_s;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    LP_DEP_ENTER();
 
-    if (warp == 0 && lane == 0) {
-        for (int kb = 0; kb < num_kb; ++kb) {
-            const int s = kb % S;
-            if (kb >= S && !mbar_wait(smem_u32(&bar_empty[s]), ((kb / S) & 1) ^ 1, p.wait_ns)) {
-                atomicExch(p.err, 1);
-                abort_s = 1;
-                break;
-            }
-            const uint32_t base = smem_u32(smem + (size_t)s * stage_bytes);
-            const uint32_t bar = smem_u32(&bar_full[s]);
-            mbar_expect_tx(bar, stage_bytes + (kb == 0 && t == 0 ? (uint32_t)p.extra_tx : 0u));
-            const int kk = kb * TC_BK;
-            for (int q = 0; q < parts; ++q) {
-                tma_load_2d(base + q * tile_bytes, &mapA, bar, kk, row_a0 + q * p.part_rows_a);
-                const uint32_t sb = base + (parts + q) * tile_bytes;
-                if (!b_mn) {
-                    tma_load_2d(sb, &mapB, bar, kk, row_b0 + q * p.part_rows_b);
-                } else {  // X as the second operand: 64 rows of K, two boxes of 64 columns
-                    const int row = p.row_off_b + slot_x + kk + q * p.part_rows_b;
-                    tma_load_2d(sb, &mapB, bar, tj * 128, row);
-                    tma_load_2d(sb + 8192, &mapB, bar, tj * 128 + 64, row);
+    if (warp == 0) {
+        if (lane == 0) {
+            const int row_a = (p.kind == NS_GRAM ? p.x_row0 + slot_x : slot_a) + ti * 128;
+            const int row_b = p.kind == NS_GRAM ? p.x_row0 + slot_x + tj * BN : p.kind == NS_POLY ? slot_a + tj * BN : p.x_row0 + slot_x;
+            for (int kb = 0; kb < num_kb; ++kb) {
+                const int s = kb % S;
+                if (kb >= S && !mbar_wait(smem_u32(&bar_empty[s]), ((kb / S) & 1) ^ 1, p.wait_ns)) {
+                    atomicExch(p.err, 1);
+                    break;
                 }
-            }
-        }
-    } else if (warp == 1 && lane == 0) {
-        const uint32_t idesc = make_idesc_f16(128, 128, b_mn);
-        bool ok = true;
-        for (int kb = 0; kb < num_kb; ++kb) {
-            const int s = kb % S;
-            if (!mbar_wait(smem_u32(&bar_full[s]), (kb / S) & 1, p.wait_ns)) {
-                atomicExch(p.err, 2);
-                abort_s = 1;
-                ok = false;
-                break;
-            }
-            tc_fence_after();
-            const uint32_t sa = smem_u32(smem + (size_t)s * stage_bytes), sb = sa + parts * tile_bytes;
+                const uint32_t sa = smem_u32(smem + (size_t)s * stage_bytes), sb = sa + PARTS * a_bytes, bar = smem_u32(&bar_full[s]);
+                mbar_expect_tx(bar, stage_bytes + (kb == 0 && t == 0 ? (uint32_t)p.extra_tx : 0u));
+                const int kk = kb * TC_BK;
 #pragma unroll
-            for (int k = 0; k < TC_BK / TC_UMMA_K; ++k) {
-                const uint64_t da = make_smem_desc(sa + k * 32, 16, 1024);
-                const uint64_t db = b_mn ? make_smem_desc(sb + k * 2048, 8192, 1024) : make_smem_desc(sb + k * 32, 16, 1024);
-                umma_bf16(tmem_d, da, db, idesc, (kb | k) != 0 ? 1u : 0u);
-                if (parts == 2) {
-                    const uint64_t la = make_smem_desc(sa + tile_bytes + k * 32, 16, 1024);
-                    const uint64_t lb = b_mn ? make_smem_desc(sb + tile_bytes + k * 2048, 8192, 1024) : make_smem_desc(sb + tile_bytes + k * 32, 16, 1024);
-                    umma_bf16(tmem_d, da, lb, idesc, 1u);
-                    umma_bf16(tmem_d, la, db, idesc, 1u);
-                }
-            }
-            umma_commit(smem_u32(&bar_empty[s]));
-        }
-        if (ok) umma_commit(smem_u32(&bar_acc));
-    }
-    __syncwarp();
-    const bool done = mbar_wait(smem_u32(&bar_acc), 0, p.wait_ns);
-    if (!done) {
-        if (lane == 0) atomicExch(p.err, 3);
-        abort_s = 1;
-    }
-    __syncthreads();
-    if (abort_s == 0) {
-        tc_fence_after();
-        const int row = ti * 128 + warp * 32 + lane;
-        const int slot = sym ? slot_a : slot_x, stored = sym ? parts : NS_X_PARTS;
-        for (int c0 = 0; c0 < 128; c0 += 32) {
-            float v[32];
-            __syncwarp();
-            tmem_ld_32x32(tmem_d + ((uint32_t)(warp * 32) << 16) + c0, v);
-            const int col = tj * 128 + c0;
-            const int width = sym ? mat.mp : mat.np;
-            if (row >= mat.mp || col >= width) continue;
-            const size_t at = (size_t)(slot + row) * p.pitch + col;
-            if (p.kind == NS_GRAM) {
+                for (int q = 0; q < PARTS; ++q) {
+                    tma_load_2d(sa + q * a_bytes, &mapA, bar, kk, row_a + q * p.lo_rows_a);
+                    if (!b_mn) {
+                        tma_load_2d(sb + q * b_bytes, &mapB, bar, kk, row_b + q * p.lo_rows_b);
+                    } else {  // X as the second operand: 64 rows of K, boxes of 64 columns
 #pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] *= NS_A_SCALE / (NS_X_SCALE * NS_X_SCALE);
-            } else {
-                float x[32];
-                ns_load32(p.addend + at, stored, p.lo_off, x);
-                const float f = p.kind == NS_POLY ? p.c / NS_A_SCALE : 1.f / NS_A_SCALE;
-                const float h = p.kind == NS_POLY ? p.b : p.a;
-#pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = fmaf(h, x[i], f * v[i]);
-            }
-            if (p.kind != NS_LAST) {
-                ns_store32(v, stored, p.out + at, p.lo_off);
-                if (sym && ti != tj) {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) ns_store_parts(v[i], stored, p.out + (size_t)(slot + col + i) * p.pitch + row, p.lo_off);
-                }
-            } else if (row < mat.m) {
-                const long long base = mat.dst + rep * mat.dst_stride;
-#pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    if (col + i < mat.n) {
-                        const long long o = base + (mat.tall ? (long long)(col + i) * mat.ld_dst + row : (long long)row * mat.ld_dst + col + i);
-                        const float r = v[i] * (1.f / NS_X_SCALE);
-                        if (p.params) ((float *)p.dst)[o] = fmaf(-mat.update, r, p.keep * p.params[o]);
-                        else if (p.bf16_dst) ((bf16 *)p.dst)[o] = __float2bfloat16_rn(r);
-                        else ((float *)p.dst)[o] = r;
+                        for (int c = 0; c < BN / 64; ++c) tma_load_2d(sb + q * b_bytes + c * 8192, &mapB, bar, tj * BN + c * 64, row_b + kk + q * p.lo_rows_b);
                     }
                 }
             }
         }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            const uint32_t idesc = make_idesc_f16(128, BN, b_mn);
+            bool ok = true;
+            for (int kb = 0; kb < num_kb && ok; ++kb) {
+                const int s = kb % S;
+                const int chunk = PARTS == 2 ? kb : 0, b = chunk & 1;
+                if (PARTS == 2 && kb >= 2 && !mbar_wait(smem_u32(&bar_acc_empty[b]), ((kb >> 1) & 1) ^ 1, p.wait_ns)) {
+                    atomicExch(p.err, 5);
+                    break;
+                }
+                if (!mbar_wait(smem_u32(&bar_full[s]), (kb / S) & 1, p.wait_ns)) {
+                    atomicExch(p.err, 2);
+                    break;
+                }
+                tc_fence_after();
+                const uint32_t sa = smem_u32(smem + (size_t)s * stage_bytes), sb = sa + PARTS * a_bytes;
+                const uint32_t acc = tmem + b * BN;
+                auto product = [&](uint32_t oa, uint32_t ob, int k, uint32_t add) {
+                    const uint64_t da = make_smem_desc(sa + oa + k * 32, 16, 1024);
+                    const uint64_t db = b_mn ? make_smem_desc(sb + ob + k * 2048, 8192, 1024) : make_smem_desc(sb + ob + k * 32, 16, 1024);
+                    umma_bf16(acc, da, db, idesc, add);
+                };
+                if (PARTS == 2) {  // the small terms first
+#pragma unroll
+                    for (int k = 0; k < TC_BK / TC_UMMA_K; ++k) {
+                        product(0, b_bytes, k, k != 0 ? 1u : 0u);
+                        product(a_bytes, 0, k, 1u);
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < TC_BK / TC_UMMA_K; ++k) product(0, 0, k, PARTS == 2 || (kb | k) != 0 ? 1u : 0u);
+                umma_commit(smem_u32(&bar_empty[s]));
+                if (PARTS == 2 || kb + 1 == num_kb) umma_commit(smem_u32(&bar_acc_full[b]));
+            }
+        }
+    } else {
+        const int q = warp & 3, half = (warp - 2) >> 2;
+        const int row = ti * 128 + q * 32 + lane, col = tj * BN + half * 64;
+        const bool live = row < mat.mp && col < (square ? mat.mp : mat.np);
+        // the addend is requested before the products are waited for
+        float v[64], add[64];
+        const size_t at_a = (size_t)(slot_a + row) * p.pitch_a + col, at_x = (size_t)(slot_x + row) * p.next.pitch + col;
+        float factor = NS_A_SCALE / (NS_X_SCALE * NS_X_SCALE), weight = 0.f;
+        const float inv_r = p.inv_r[mat.index + rep];
+#pragma unroll
+        for (int i = 0; i < 64; ++i) add[i] = 0.f;
+        if (p.kind == NS_POLY) {
+            factor = p.c / NS_A_SCALE * (inv_r * inv_r) * (inv_r * inv_r);
+            weight = p.b * (inv_r * inv_r);
+            if (live) {
+#pragma unroll
+                for (int i = 0; i < 64; i += 8) {
+                    ns_add8(*reinterpret_cast<const uint4 *>(p.A + at_a + i), add + i);
+                    if (PARTS == 2) ns_add8(*reinterpret_cast<const uint4 *>(p.A + p.lo_off_a + at_a + i), add + i);
+                }
+            }
+        } else if (!square) {
+            factor = 1.f / NS_A_SCALE;
+            weight = p.a;
+            if (live) {
+#pragma unroll
+                for (int i = 0; i < 64; i += 4) load_elems<float, 4>(p.X + at_x + i, add + i);
+            }
+        }
+        const int chunks = PARTS == 2 ? num_kb : 1;
+        bool ok = true;
+        for (int c = 0; c < chunks; ++c) {
+            const int b = c & 1;
+            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_acc_full[b]), (c >> 1) & 1, p.wait_ns));
+            if (!ok) {
+                if (lane == 0) atomicExch(p.err, 3);
+                break;
+            }
+            tc_fence_after();
+            const uint32_t taddr = tmem + ((uint32_t)(q * 32) << 16) + b * BN + half * 64;
+            uint32_t r[2][32];
+            tmem_ld_32x32_issue(taddr, r[0]);
+            tmem_ld_32x32_issue(taddr + 32, r[1]);
+            tmem_ld_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&bar_acc_empty[b]));
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                v[i] = c == 0 ? __uint_as_float(r[0][i]) : v[i] + __uint_as_float(r[0][i]);
+                v[32 + i] = c == 0 ? __uint_as_float(r[1][i]) : v[32 + i] + __uint_as_float(r[1][i]);
+            }
+        }
+        if (ok && live) {
+#pragma unroll
+            for (int i = 0; i < 64; ++i) v[i] = fmaf(weight, add[i], factor * v[i]);
+            if (square) {
+#pragma unroll
+                for (int i = 0; i < 64; i += 8) ns_store8<PARTS>(v + i, p.out + at_a + i, p.lo_off_a);
+            } else if (p.kind == NS_APPLY) {
+#pragma unroll
+                for (int i = 0; i < 64; i += 4) store_elems<float, 4>(p.next.full + at_x + i, v + i);
+#pragma unroll
+                for (int i = 0; i < 64; i += 8) ns_store8<PARTS>(v + i, p.next.hi + at_x + i, p.next.lo_off);
+            } else if (row < mat.m && col < mat.n) {
+#pragma unroll
+                for (int i = 0; i < 64; ++i) v[i] *= inv_r / NS_X_SCALE;
+                ns_write_result(p, mat, rep, row, col, v);
+            }
+        }
     }
+    __syncwarp();
     tc_fence_before();
     __syncthreads();
     if (warp == 0) {
         __syncwarp();
-        tmem_dealloc(tmem_d, 128);
+        tmem_dealloc(tmem, 2 * BN);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// The whole iteration in one launch, for matrices whose products leave SMs idle.
+//
+// Every launch of a product costs two to three microseconds before its first operand arrives, which is more than such a
+// product takes: 17 launches took 63 us for one 64 x 64 matrix and 134 us for the four matrices of a 128-256-256 encoder.
+// Here the blocks stay resident (cooperative launch) and step from phase to phase -- norm, conversion, and per step A, B and
+// the new X -- through a counter in global memory.  The blocks form clusters of C that split the K range of a 128 x 64 tile:
+// each adds up its share in tensor memory, all of them put the sums into shared memory, and each finishes 64 / C columns
+// from everybody's (distributed shared memory), so that operands, products and epilogue are all spread C ways.
+//   warp 0 operands by TMA, warp 1 matrix instructions, warps 2-17 sums and results (and the first two phases)
+// Every wait is bounded; a block that gives up reports it and leaves, and the others run into their own limits.
+// ---------------------------------------------------------------------------------------------
+constexpr int NSC_THREADS = 576;
+constexpr int NSC_WORKERS = 512;  // threads of warps 2-17
+constexpr int NSC_BN = 64;
+constexpr int NSC_KEPT = 4;  // tiles of A and of X whose description a block keeps
+constexpr int NSC_ACCS = 4;  // accumulators used in turn
+template <int PARTS> constexpr int NSC_ACC_COLS = PARTS * NSC_BN;  // PARTS = 2: the two halves of a 64-term block are added up apart
+constexpr int NSC_SUM_BYTES = 128 * NSC_BN * 4;  // the sums of a tile
+constexpr int NSC_BARRIERS = 256;  // counters of one call: 2 + 3 * steps are used
+
+struct NsChain {
+    int parts_rows_x, parts_rows_a;      // rows between the hi and lo parts of X and of A, B
+    int steps;
+    float a, b, c;
+    double eps;
+    NsX X[2];
+    __half *A, *B;
+    int pitch_a;
+    size_t lo_off_a;
+    double *partial;
+    float *inv_r;
+    int norm_blocks, adam_blocks, conv_blocks, tiles_a, tiles_x;
+    void *dst;
+    int bf16_dst;
+    const float *params;
+    float keep;
+    unsigned *counters, *next_counters;  // NSC_BARRIERS each: this call's (zero) and the next call's (cleared here)
+    int *err;
+    unsigned long long wait_ns;
+    int extra_tx;
+};
+
+LP_DEVINL unsigned ld_acquire_gpu(const unsigned *p)
+{
+    unsigned v;
+    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+LP_DEVINL void red_release_gpu(unsigned *p)
+{
+    asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(p) : "memory");
+}
+LP_DEVINL void fence_async_proxy_global() { asm volatile("fence.proxy.async.global;" ::: "memory"); }
+LP_DEVINL bool counter_wait(const unsigned *p, unsigned want, unsigned long long limit_ns)
+{
+    if (ld_acquire_gpu(p) >= want) return true;
+    const unsigned long long t0 = global_timer_ns();
+    for (;;) {
+        for (int i = 0; i < 16; ++i)
+            if (ld_acquire_gpu(p) >= want) return true;
+        if (global_timer_ns() - t0 > limit_ns) return false;
+    }
+}
+LP_DEVINL void mbar_arrive_cluster(uint32_t cluster_addr)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+LP_DEVINL bool mbar_wait_cluster(uint32_t bar, uint32_t parity, unsigned long long limit_ns)
+{
+    unsigned long long t0 = 0;
+    for (;;) {
+        for (int i = 0; i < 64; ++i) {
+            uint32_t ok;
+            asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.b32 %0, 1, 0, p;\n\t}"
+                         : "=r"(ok)
+                         : "r"(bar), "r"(parity)
+                         : "memory");
+            if (ok) return true;
+        }
+        if (t0 == 0) t0 = global_timer_ns();
+        else if (global_timer_ns() - t0 > limit_ns) return false;
+    }
+}
+// this block's shared memory into that of a block of the cluster, counted in bytes on that block's barrier
+LP_DEVINL void copy_to_cta(uint32_t dst_cluster, uint32_t src, uint32_t bytes, uint32_t bar_cluster)
+{
+    asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst_cluster), "r"(src), "r"(bytes), "r"(bar_cluster)
+                 : "memory");
+}
+// one lane of the (converged) warp, by the instruction whose branch the compiler knows to be taken by a single lane: the operands
+// of the matrix and copy instructions behind it stay in uniform registers (a branch on the lane number: 146 cycles per matrix
+// instruction instead of 50)
+LP_DEVINL bool elect_one()
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
+}
+LP_DEVINL void tmem_ld_32x16(uint32_t taddr, float *v)
+{
+    uint32_t r[16];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
+                   "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(taddr)
+                 : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+LP_DEVINL void tmem_ld_32x8_pair(uint32_t a, uint32_t b, float *v, float *w)
+{
+    uint32_t r[16];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(a)
+                 : "memory");
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(b)
+                 : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        v[i] = __uint_as_float(r[i]);
+        w[i] = __uint_as_float(r[8 + i]);
+    }
+}
+// sum + lost becomes sum + lost + x, the rounding of the new sum added to lost (exact whatever the magnitudes)
+LP_DEVINL void ns_two_sum(float &sum, float &lost, float x)
+{
+    const float t = sum + x, b = t - sum;
+    lost += (sum - (t - b)) + (x - b);
+    sum = t;
+}
+
+// the phase's tiles: where a tile lies and what it is made of
+struct NsTile {
+    int d, rep, ti, tj, slot_x, slot_a, mp, np, m, n, tall, index;
+    LP_DEVINL int num_kb(int kind) const { return (kind == NS_GRAM ? np : mp) / TC_BK; }
+};
+LP_DEVINL NsTile ns_tile(const NsGroup &g, int kind, int t)
+{
+    const bool square = kind == NS_GRAM || kind == NS_POLY;
+    NsTile r;
+    r.d = square ? ns_find(g, t, [](const NsMat &m) { return m.first_a; }) : ns_find(g, t, [](const NsMat &m) { return m.first_x; });
+    const NsMat &mat = g.mat[r.d];
+    const int per = square ? mat.tiles_a : mat.tiles_x, local = t - (square ? mat.first_a : mat.first_x);
+    const int T = (mat.mp + 127) / 128;
+    r.rep = local / per;
+    const int tt = local - r.rep * per;
+    r.ti = tt % T;
+    r.tj = tt / T;
+    r.slot_x = mat.row_x + r.rep * mat.mp;
+    r.slot_a = mat.row_a + r.rep * mat.mp;
+    r.mp = mat.mp; r.np = mat.np; r.m = mat.m; r.n = mat.n;
+    r.tall = mat.tall;
+    r.index = mat.index + r.rep;
+    return r;
+}
+
+// eight columns of the result (kept out of line: the code that every phase runs has to stay in the instruction cache)
+__device__ __noinline__ void ns_result8(const NsChain &p, const NsMat &mat, int rep, int row, int col, const float4 lo, const float4 hi, float scale)
+{
+    float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    const long long base = mat.dst + rep * mat.dst_stride;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= scale;
+    if (mat.tall || col + 8 > mat.n) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (col + i >= mat.n) break;
+            const long long o = base + (mat.tall ? (long long)(col + i) * mat.ld_dst + row : (long long)row * mat.ld_dst + col + i);
+            if (p.params) ((float *)p.dst)[o] = fmaf(-mat.update, v[i], p.keep * p.params[o]);
+            else if (p.bf16_dst) ((bf16 *)p.dst)[o] = __float2bfloat16_rn(v[i]);
+            else ((float *)p.dst)[o] = v[i];
+        }
+        return;
+    }
+    const long long o = base + (long long)row * mat.ld_dst + col;
+    if (p.bf16_dst) {
+        bf16 *q = (bf16 *)p.dst + o;
+        if (((uintptr_t)q & 15) == 0) {
+            store_elems<bf16, 8>(q, v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) q[i] = __float2bfloat16_rn(v[i]);
+        }
+        return;
+    }
+    float *q = (float *)p.dst + o;
+    const bool wide = (((uintptr_t)q | (uintptr_t)(p.params ? p.params + o : nullptr)) & 15) == 0;
+    if (p.params) {
+        float old[8];
+        if (wide) {
+            load_elems<float, 4>(p.params + o, old);
+            load_elems<float, 4>(p.params + o + 4, old + 4);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) old[i] = p.params[o + i];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = fmaf(-mat.update, v[i], p.keep * old[i]);
+    }
+    if (wide) {
+        store_elems<float, 4>(q, v);
+        store_elems<float, 4>(q + 4, v + 4);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = v[i];
+    }
+}
+
+template <int PARTS> constexpr int NSC_STAGE_BYTES = PARTS * (128 + NSC_BN) * TC_BK * 2;
+template <int PARTS> constexpr int NSC_STAGES = PARTS == 2 ? 3 : 6;  // 144 KiB beside 64 KiB of sums (this block's and those it receives)
+
+// the first two phases
+LP_DEVINL void ns_chain_norm(const NsSource &src, const NsGroup &g, const NsAdam &adam, const NsChain &p, int tid, double *sw)
+{
+    for (int t = blockIdx.x; t < p.norm_blocks + p.adam_blocks; t += gridDim.x) {
+        if (t < p.norm_blocks) ns_norm_block<NSC_WORKERS>(src, g, t, tid, p.partial, sw);
+        else ns_adam_block<NSC_WORKERS>(adam, t - p.norm_blocks, tid);
+    }
+}
+template <int PARTS> LP_DEVINL void ns_chain_convert(const NsSource &src, const NsGroup &g, const NsChain &p, int tid, float *tile, double *sw)
+{
+    for (int t = blockIdx.x; t < p.conv_blocks; t += gridDim.x) ns_convert_block<PARTS, NSC_WORKERS>(src, g, t, tid, p.partial, p.eps, p.X[0], p.inv_r, tile, sw);
+}
+
+template <int PARTS, int C>
+__global__ void __launch_bounds__(NSC_THREADS, 1) ns_chain_kernel(const __grid_constant__ CUtensorMap mapX128, const __grid_constant__ CUtensorMap mapX64,
+                                                                  const __grid_constant__ CUtensorMap mapA128, const __grid_constant__ CUtensorMap mapA64,
+                                                                  const __grid_constant__ CUtensorMap mapB128, const __grid_constant__ NsSource src,
+                                                                  const __grid_constant__ NsGroup g,
+                                                                  const __grid_constant__ NsAdam adam, const __grid_constant__ NsChain p)
+{
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t bar_full[8], bar_empty[8], bar_acc_full[NSC_ACCS], bar_acc_empty[NSC_ACCS], bar_xfull, bar_xfree;
+    __shared__ uint32_t tmem_base_s;
+    __shared__ double sw[NSC_WORKERS / 32];
+    __shared__ NsTile kept_s[2][NSC_KEPT], later_s;
+    constexpr int S = NSC_STAGES<PARTS>;
+    constexpr uint32_t a_bytes = 128 * TC_BK * 2, b_bytes = NSC_BN * TC_BK * 2, stage_bytes = NSC_STAGE_BYTES<PARTS>;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    float *mine = reinterpret_cast<float *>(smem + (size_t)S * stage_bytes), *theirs = mine + NSC_SUM_BYTES / 4;
+    const int rank = C > 1 ? (int)cluster_cta_rank() : 0;
+    const int cluster = blockIdx.x / C, n_clusters = gridDim.x / C;
+    const unsigned everybody = gridDim.x;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S; ++s) {
+            mbar_init(smem_u32(&bar_full[s]), 1);
+            mbar_init(smem_u32(&bar_empty[s]), 1);
+        }
+        for (int b = 0; b < NSC_ACCS; ++b) {
+            mbar_init(smem_u32(&bar_acc_full[b]), 1);
+            mbar_init(smem_u32(&bar_acc_empty[b]), NSC_WORKERS / 32);
+        }
+        mbar_init(smem_u32(&bar_xfull), 1);
+        mbar_init(smem_u32(&bar_xfree), C);
+        fence_barrier_init();
+        fence_async_proxy();
+        tma_prefetch_desc(&mapX128);
+        tma_prefetch_desc(&mapX64);
+        tma_prefetch_desc(&mapA128);
+        tma_prefetch_desc(&mapA64);
+        tma_prefetch_desc(&mapB128);
+    }
+    if (warp == 0) {
+        __syncwarp();
+        tmem_alloc(smem_u32(&tmem_base_s), NSC_ACCS * NSC_ACC_COLS<PARTS>);
+    }
+    if (blockIdx.x == 0 && threadIdx.x < NSC_BARRIERS) p.next_counters[threadIdx.x] = 0;
+    // every step visits the same tiles: the first ones of A, B and of X are looked up once
+    if (threadIdx.x >= 64 && threadIdx.x < 64 + 2 * NSC_KEPT) {
+        const int i = (threadIdx.x - 64) % NSC_KEPT, of_x = (threadIdx.x - 64) / NSC_KEPT, t = cluster + i * n_clusters;
+        if (t < (of_x ? p.tiles_x : p.tiles_a)) kept_s[of_x][i] = ns_tile(g, of_x ? NS_APPLY : NS_GRAM, t);
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (C > 1) cluster_barrier();
+    tc_fence_after();
+    const uint32_t tmem = tmem_base_s;
+
+    if (warp == 0) {
+        if (elect_one()) {
+            // ---- operands
+            int s = 0, round = 0;  // stage, and how often the ring has gone round
+            bool ok = true, first = true;
+            for (int k = 0; k < p.steps && ok; ++k) {
+                const int x0 = (k & 1) * PARTS * p.parts_rows_x;
+                for (int kind = NS_GRAM; kind <= NS_APPLY && ok; ++kind) {
+                    const int phase = 2 + 3 * k + kind;
+                    if (!counter_wait(p.counters + phase - 1, everybody, p.wait_ns)) { atomicExch(p.err, 6); ok = false; break; }
+                    fence_async_proxy_global();
+                    const int tiles = kind == NS_APPLY ? p.tiles_x : p.tiles_a;
+                    const CUtensorMap *map_a = kind == NS_GRAM ? &mapX128 : kind == NS_POLY ? &mapA128 : &mapB128;
+                    const CUtensorMap *map_b = kind == NS_POLY ? &mapA64 : &mapX64;
+                    const int lo_a = kind == NS_GRAM ? p.parts_rows_x : p.parts_rows_a, lo_b = kind == NS_POLY ? p.parts_rows_a : p.parts_rows_x;
+                    int i = 0;
+                    for (int t = cluster; t < tiles && ok; t += n_clusters, ++i) {
+                        const NsTile tl = i < NSC_KEPT ? kept_s[kind == NS_APPLY][i] : ns_tile(g, kind, t);
+                        const int kbs = tl.num_kb(kind), kb0 = kbs * rank / C, kb1 = kbs * (rank + 1) / C;
+                        const int row_a = (kind == NS_GRAM ? x0 + tl.slot_x : tl.slot_a) + tl.ti * 128;
+                        // X as the second operand of the new X is read across: 64 rows of K, 64 columns
+                        const int row_b = kind == NS_GRAM ? x0 + tl.slot_x + tl.tj * NSC_BN : kind == NS_POLY ? tl.slot_a + tl.tj * NSC_BN : x0 + tl.slot_x;
+                        for (int kb = kb0; kb < kb1; ++kb) {
+                            if (round > 0 && !mbar_wait(smem_u32(&bar_empty[s]), (round & 1) ^ 1, p.wait_ns)) { atomicExch(p.err, 1); ok = false; break; }
+                            const uint32_t sa = smem_u32(smem) + s * stage_bytes, sb = sa + PARTS * a_bytes, bar = smem_u32(&bar_full[s]);
+                            mbar_expect_tx(bar, stage_bytes + (first && blockIdx.x == 0 ? (uint32_t)p.extra_tx : 0u));
+                            first = false;
+                            const int kk = kb * TC_BK;
+                            const int xb = kind == NS_APPLY ? tl.tj * NSC_BN : kk, yb = kind == NS_APPLY ? row_b + kk : row_b;
+#pragma unroll
+                            for (int q = 0; q < PARTS; ++q) {
+                                tma_load_2d(sa + q * a_bytes, map_a, bar, kk, row_a + q * lo_a);
+                                tma_load_2d(sb + q * b_bytes, map_b, bar, xb, yb + q * lo_b);
+                            }
+                            if (++s == S) { s = 0; ++round; }
+                        }
+                    }
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (elect_one()) {
+            // ---- products
+            int s = 0, round = 0, use = 0;  // stage, rounds of the ring, accumulators handed over
+            bool ok = true;
+            const uint64_t desc_a = make_smem_desc(smem_u32(smem), 16, 1024), desc_bk = make_smem_desc(smem_u32(smem) + PARTS * a_bytes, 16, 1024),
+                           desc_bm = make_smem_desc(smem_u32(smem) + PARTS * a_bytes, 8192, 1024);
+            for (int k = 0; k < p.steps && ok; ++k) {
+                for (int kind = NS_GRAM; kind <= NS_APPLY && ok; ++kind) {
+                    const uint32_t idesc = make_idesc_f16(128, NSC_BN, kind == NS_APPLY);
+                    const uint64_t desc_b = kind == NS_APPLY ? desc_bm : desc_bk;
+                    const uint64_t step_b = kind == NS_APPLY ? 2048 >> 4 : 32 >> 4;  // 16 terms further
+                    const int tiles = kind == NS_APPLY ? p.tiles_x : p.tiles_a;
+                    int i = 0;
+                    for (int t = cluster; t < tiles && ok; t += n_clusters, ++i) {
+                        const NsTile tl = i < NSC_KEPT ? kept_s[kind == NS_APPLY][i] : ns_tile(g, kind, t);
+                        const int kbs = tl.num_kb(kind), kb0 = kbs * rank / C, kb1 = kbs * (rank + 1) / C;
+                        for (int kb = kb0; kb < kb1; ++kb) {
+                            const int b = use % NSC_ACCS;
+                            if ((PARTS == 2 || kb == kb0) && use >= NSC_ACCS && !mbar_wait(smem_u32(&bar_acc_empty[b]), ((use / NSC_ACCS) & 1) ^ 1, p.wait_ns)) {
+                                atomicExch(p.err, 5);
+                                ok = false;
+                                break;
+                            }
+                            if (!mbar_wait(smem_u32(&bar_full[s]), round & 1, p.wait_ns)) { atomicExch(p.err, 2); ok = false; break; }
+                            tc_fence_after();
+                            const uint64_t da = desc_a + ((s * stage_bytes) >> 4), db = desc_b + ((s * stage_bytes) >> 4);
+                            const uint32_t acc = tmem + b * NSC_ACC_COLS<PARTS>;
+                            if (PARTS == 2) {
+#pragma unroll
+                                for (int i = 0; i < TC_BK / TC_UMMA_K; ++i) {  // the small terms first, while the sums are small
+                                    const uint32_t half = acc + (i >> 1) * NSC_BN;
+                                    umma_bf16(half, da + i * 2, db + (b_bytes >> 4) + i * step_b, idesc, i & 1);
+                                    umma_bf16(half, da + (a_bytes >> 4) + i * 2, db + i * step_b, idesc, 1u);
+                                }
+#pragma unroll
+                                for (int i = 0; i < TC_BK / TC_UMMA_K; ++i) umma_bf16(acc + (i >> 1) * NSC_BN, da + i * 2, db + i * step_b, idesc, 1u);
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < TC_BK / TC_UMMA_K; ++i) umma_bf16(acc, da + i * 2, db + i * step_b, idesc, kb != kb0 || i != 0 ? 1u : 0u);
+                            }
+                            umma_commit(smem_u32(&bar_empty[s]));
+                            if (PARTS == 2 || kb + 1 == kb1) {
+                                umma_commit(smem_u32(&bar_acc_full[b]));
+                                ++use;
+                            }
+                            if (++s == S) { s = 0; ++round; }
+                        }
+                    }
+                }
+            }
+        }
+    } else {
+        // ---- norm and conversion, then sums and results
+        const int tid = threadIdx.x - 64;
+        bool ok = true;
+        // ends phase i: everything this block wrote is visible to whoever sees the counter; begins phase i + 1
+        auto arrive = [&](int i) {
+            ns_sync<NSC_WORKERS>();
+            if (tid == 0) red_release_gpu(p.counters + i);
+        };
+        auto await = [&](int i) {
+            bool failed = false;
+            if (tid == 0 && !counter_wait(p.counters + i, everybody, p.wait_ns)) { atomicExch(p.err, 6); failed = true; }
+            return !ns_any<NSC_WORKERS>(failed);
+        };
+        ns_chain_norm(src, g, adam, p, tid, sw);
+        arrive(0);
+        ok = await(0);
+        if (ok) {
+            ns_chain_convert<PARTS>(src, g, p, tid, mine, sw);
+            arrive(1);
+        }
+        const int q = warp & 3, quarter = (warp - 2) >> 2;  // the 32 rows that the warp may read from tensor memory, and its 16 columns
+        int use = 0, tiles_done = 0;
+        for (int k = 0; k < p.steps && ok; ++k) {
+            const NsX &cur = p.X[k & 1], &next = p.X[(k & 1) ^ 1];
+            for (int kind_ = NS_GRAM; kind_ <= NS_APPLY && ok; ++kind_) {
+                const int phase = 2 + 3 * k + kind_;
+                const int kind = kind_ == NS_APPLY && k + 1 == p.steps ? NS_LAST : kind_;
+                const bool square = kind == NS_GRAM || kind == NS_POLY;
+                ok = await(phase - 1);
+                const int tiles = kind_ == NS_APPLY ? p.tiles_x : p.tiles_a;
+                // where the addend is read and the operands of the next phase are written: same rows, columns and pitch
+                const __half *add_h = p.A;
+                const float *add_f = cur.full;
+                __half *out_h = kind == NS_GRAM ? p.A : kind == NS_POLY ? p.B : next.hi;
+                const size_t out_lo = square ? p.lo_off_a : next.lo_off;
+                const int pitch = square ? p.pitch_a : next.pitch;
+                int nth = 0;
+                for (int t = cluster; t < tiles && ok; t += n_clusters, ++nth) {
+                    if (nth >= NSC_KEPT) {
+                        if (tid == 0) later_s = ns_tile(g, kind_, t);
+                        ns_sync<NSC_WORKERS>();
+                    }
+                    const NsTile &tl = nth < NSC_KEPT ? kept_s[kind_ == NS_APPLY][nth] : later_s;  // read where it is needed, not held
+                    const int kbs = tl.num_kb(kind_), kb0 = kbs * rank / C, kb1 = kbs * (rank + 1) / C;
+                    const int width = square ? tl.mp : tl.np, slot = square ? tl.slot_a : tl.slot_x;
+                    const float inv_r = kind == NS_POLY || kind == NS_LAST ? __ldcg(p.inv_r + tl.index) : 1.f;
+                    // this block finishes 64 / C columns of the tile; a thread takes GPT groups of eight, neighbours along the rows
+                    constexpr int GPR = 8 / C, GPT = C == 1 ? 2 : 1;  // groups per row, per thread (C = 4: half of the threads have none)
+                    float add[GPT][8];
+#pragma unroll
+                    for (int i = 0; i < GPT; ++i) {
+                        const int e = i * NSC_WORKERS + tid, row = tl.ti * 128 + e / GPR, col = tl.tj * NSC_BN + rank * (NSC_BN / C) + 8 * (e % GPR);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) add[i][j] = 0.f;
+                        if (e < 128 * GPR && row < tl.mp && col < width) {
+                            const size_t at = (size_t)(slot + row) * pitch + col;
+                            if (kind == NS_POLY) {
+                                ns_add8(__ldcg(reinterpret_cast<const uint4 *>(add_h + at)), add[i]);
+                                if (PARTS == 2) ns_add8(__ldcg(reinterpret_cast<const uint4 *>(add_h + p.lo_off_a + at)), add[i]);
+                            } else if (!square) {
+                                const float4 x = __ldcg(reinterpret_cast<const float4 *>(add_f + at)), y = __ldcg(reinterpret_cast<const float4 *>(add_f + at) + 1);
+                                add[i][0] = x.x; add[i][1] = x.y; add[i][2] = x.z; add[i][3] = x.w;
+                                add[i][4] = y.x; add[i][5] = y.y; add[i][6] = y.z; add[i][7] = y.w;
+                            }
+                        }
+                    }
+                    float v[16], lost[16];  // running sums and what their roundings lost
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] = lost[i] = 0.f;
+                    const int chunks = kb1 <= kb0 ? 0 : PARTS == 2 ? kb1 - kb0 : 1;
+                    bool failed = false;
+                    for (int c = 0; c < chunks; ++c, ++use) {
+                        const int b = use % NSC_ACCS;
+                        failed = !__all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_acc_full[b]), (use / NSC_ACCS) & 1, p.wait_ns));
+                        if (failed) {
+                            if (lane == 0) atomicExch(p.err, 3);
+                            break;
+                        }
+                        tc_fence_after();
+                        const uint32_t taddr = tmem + ((uint32_t)(q * 32) << 16) + b * NSC_ACC_COLS<PARTS> + quarter * 16;
+                        if (PARTS == 1) {  // one chunk
+                            tmem_ld_32x16(taddr, v);
+                        } else {
+#pragma unroll
+                            for (int o = 0; o < 16; o += 8) {  // eight columns at a time: nothing may spill (every barrier empties L1)
+                                float r[8], r2[8];
+                                tmem_ld_32x8_pair(taddr + o, taddr + NSC_BN + o, r, r2);
+                                if (c == 0) {
+#pragma unroll
+                                    for (int i = 0; i < 8; ++i) v[o + i] = r[i] + r2[i];
+                                } else {
+#pragma unroll
+                                    for (int i = 0; i < 8; ++i) ns_two_sum(v[o + i], lost[o + i], r[i] + r2[i]);
+                                }
+                            }
+                        }
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(smem_u32(&bar_acc_empty[b]));
+                    }
+                    if (PARTS == 2 && C > 1) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) v[i] += lost[i];
+                    }
+                    const float r2 = inv_r * inv_r;
+                    const float f = kind == NS_GRAM ? NS_A_SCALE / (NS_X_SCALE * NS_X_SCALE) : kind == NS_POLY ? p.c / NS_A_SCALE * r2 * r2 : 1.f / NS_A_SCALE;
+                    const float h = kind == NS_POLY ? p.b * r2 : p.a;
+                    // the sums go to shared memory, [block that finishes][row][64 / C] with the 16-byte pieces of a row permuted by the
+                    // row; every other block of the cluster gets its share by one bulk copy
+                    constexpr int SHARE = 128 * NSC_BN / C, PIECES = 16 / C;
+                    if (C > 1 && tiles_done > 0 && !mbar_wait_cluster(smem_u32(&bar_xfree), (tiles_done - 1) & 1, p.wait_ns)) { atomicExch(p.err, 7); failed = true; }
+                    const int row_t = q * 32 + lane;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int piece = quarter * 4 + i, to = piece / PIECES, within = piece % PIECES;
+                        *reinterpret_cast<float4 *>(mine + to * SHARE + row_t * (NSC_BN / C) + ((within ^ (row_t & (PIECES - 1))) << 2)) =
+                            make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                        if (PARTS == 2 && C == 1 && chunks > 1)  // what the sums lost goes along in the second area
+                            *reinterpret_cast<float4 *>(theirs + row_t * NSC_BN + ((within ^ (row_t & (PIECES - 1))) << 2)) =
+                                make_float4(lost[4 * i], lost[4 * i + 1], lost[4 * i + 2], lost[4 * i + 3]);
+                    }
+                    if (C > 1) fence_async_proxy();
+                    ok = !ns_any<NSC_WORKERS>(failed);  // all sixteen warps go on or all leave
+                    if (!ok) break;
+                    if (C > 1) {
+                        if (tid == 0) {
+                            mbar_expect_tx(smem_u32(&bar_xfull), (C - 1) * SHARE * 4);
+                            for (int o = 1; o < C; ++o) {
+                                const int to = (rank + o) % C;
+                                copy_to_cta(map_to_cta(smem_u32(theirs + rank * SHARE), to), smem_u32(mine + to * SHARE), SHARE * 4, map_to_cta(smem_u32(&bar_xfull), to));
+                            }
+                        }
+                        if (!mbar_wait_cluster(smem_u32(&bar_xfull), tiles_done & 1, p.wait_ns)) { atomicExch(p.err, 7); failed = true; }
+                    }
+#pragma unroll
+                    for (int i = 0; i < GPT; ++i) {
+                        const int e = i * NSC_WORKERS + tid;
+                        if (e >= 128 * GPR) break;
+                        const int r_t = e / GPR, piece = 2 * (e % GPR), row = tl.ti * 128 + r_t, col = tl.tj * NSC_BN + rank * (NSC_BN / C) + 4 * piece;
+                        float sum[8], off[8];
+#pragma unroll
+                        for (int other = 0; other < (C == 1 ? PARTS : C); ++other) {
+                            if (C == 1 && other == 1 && chunks <= 1) break;
+                            const float *row_p = (other == rank ? mine : theirs) + (C == 1 ? 0 : other * SHARE) + r_t * (NSC_BN / C);
+                            const float4 x = *reinterpret_cast<const float4 *>(row_p + ((piece ^ (r_t & (PIECES - 1))) << 2));
+                            const float4 y = *reinterpret_cast<const float4 *>(row_p + (((piece + 1) ^ (r_t & (PIECES - 1))) << 2));
+                            const float z[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) {
+                                if (other == 0) { sum[j] = z[j]; off[j] = 0.f; }
+                                else if (C == 1) off[j] = z[j];
+                                else ns_two_sum(sum[j], off[j], z[j]);
+                            }
+                        }
+                        if (row >= tl.mp || col >= width) continue;
+                        const size_t at = (size_t)(slot + row) * pitch + col;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) sum[j] = fmaf(f, off[j], fmaf(h, add[i][j], f * sum[j]));  // f is a power of two where precision counts
+                        if (kind != NS_LAST) {
+                            ns_store8<PARTS>(sum, out_h + at, out_lo);
+                            if (!square) {
+                                store_elems<float, 4>(next.full + at, sum);
+                                store_elems<float, 4>(next.full + at + 4, sum + 4);
+                            }
+                        } else if (row < tl.m && col < tl.n) {
+                            ns_result8(p, g.mat[tl.d], tl.rep, row, col, make_float4(sum[0], sum[1], sum[2], sum[3]), make_float4(sum[4], sum[5], sum[6], sum[7]),
+                                       inv_r / NS_X_SCALE);
+                        }
+                    }
+                    ok = !ns_any<NSC_WORKERS>(failed);  // and the sums may be overwritten
+                    if (!ok) break;
+                    if (C > 1 && tid < C) mbar_arrive_cluster(map_to_cta(smem_u32(&bar_xfree), tid));
+                    ++tiles_done;
+                }
+                if (ok && kind != NS_LAST) arrive(phase);
+            }
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (C > 1) cluster_barrier();  // nobody leaves while its sums may still be read
+    if (warp == 0) {
+        __syncwarp();
+        tmem_dealloc(tmem, NSC_ACCS * NSC_ACC_COLS<PARTS>);
     }
 }
 
 // ---------------------------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------------------------
+constexpr int NS_SMEM = 200 * 1024;
+
+template <int BN, int PARTS> constexpr int ns_tile_stages()
+{
+    return std::min(8, (NS_SMEM - 1024) / (PARTS * (128 + BN) * TC_BK * 2));
+}
+
+template <int PARTS> constexpr int NSC_SMEM = NSC_STAGES<PARTS> * NSC_STAGE_BYTES<PARTS> + 2 * NSC_SUM_BYTES + 1024;
+
+template <int PARTS, int C> static bool ns_chain_init()
+{
+    return cudaFuncSetAttribute(ns_chain_kernel<PARTS, C>, cudaFuncAttributeMaxDynamicSharedMemorySize, NSC_SMEM<PARTS>) == cudaSuccess;
+}
+
+template <int PARTS, int C> static cudaLaunchConfig_t ns_chain_config(int clusters, cudaStream_t st, cudaLaunchAttribute (&attr)[2])
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(clusters * C);
+    cfg.blockDim = dim3(NSC_THREADS);
+    cfg.dynamicSmemBytes = NSC_SMEM<PARTS>;
+    cfg.stream = st;
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = C;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeCooperative;
+    attr[1].val.cooperative = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cfg;
+}
+
+// clusters of C blocks that are resident at the same time
+template <int PARTS, int C> static int ns_chain_room()
+{
+    static int room = -1;
+    if (room < 0) {
+        cudaLaunchAttribute attr[2];
+        cudaLaunchConfig_t cfg = ns_chain_config<PARTS, C>(1, nullptr, attr);
+        cfg.numAttrs = 1;
+        if (cudaOccupancyMaxActiveClusters(&room, ns_chain_kernel<PARTS, C>, &cfg) != cudaSuccess) { cudaGetLastError(); room = 0; }
+    }
+    return room;
+}
+
 static bool ns_init(std::string &err)
 {
-    if (cudaFuncSetAttribute(ns_product_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024) != cudaSuccess) {
+    if (!ns_chain_init<1, 1>() || !ns_chain_init<1, 2>() || !ns_chain_init<1, 4>() || !ns_chain_init<2, 1>() || !ns_chain_init<2, 2>() || !ns_chain_init<2, 4>() ||
+        cudaFuncSetAttribute(ns_tile_kernel<128, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, NS_SMEM) != cudaSuccess ||
+        cudaFuncSetAttribute(ns_tile_kernel<128, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, NS_SMEM) != cudaSuccess) {
         err = "cannot raise the dynamic shared memory limit of the Newton-Schulz products";
         return false;
     }
@@ -469,43 +1262,60 @@ static bool ns_coefficients_ok(double a, double b, double c, int steps)
 }
 
 struct NsLayout {  // sizes of the arenas of a group
-    int rows_x = 0, rows_a = 0, pitch_x = 0, pitch_a = 0, norm_blocks = 0;
-    size_t x_elems() const { return (size_t)2 * NS_X_PARTS * rows_x * pitch_x; }
-    size_t a_elems(int parts) const { return (size_t)parts * rows_a * pitch_a; }
+    int rows_x = 0, rows_a = 0, pitch_x = 0, pitch_a = 0, norm_blocks = 0, conv_blocks = 0, matrices = 0;
+    size_t x_elems() const { return (size_t)rows_x * pitch_x; }
+    size_t a_elems() const { return (size_t)rows_a * pitch_a; }
     static size_t up(size_t b) { return (b + 1023) & ~(size_t)1023; }
-    size_t bytes(int parts) const { return up(2 * x_elems()) + 2 * up(2 * a_elems(parts)) + up(sizeof(double) * (size_t)std::max(norm_blocks, 1)); }
+    // two FP32 copies of X, two of its operands, A, B, the norm partials, 1 / r
+    size_t bytes(int parts) const
+    {
+        return 2 * up(4 * x_elems()) + up((size_t)4 * parts * x_elems()) + 2 * up((size_t)2 * parts * a_elems()) + up(sizeof(double) * (size_t)norm_blocks) +
+               up(sizeof(float) * (size_t)matrices);
+    }
 };
 
 // fills the derived fields of the descriptors (m, n, repeat, tall given)
 static NsLayout ns_layout(NsGroup &g)
 {
     NsLayout l;
-    int sym = 0, xt = 0, conv = 0;
     for (int d = 0; d < g.count; ++d) {
         NsMat &m = g.mat[d];
         m.mp = (m.m + 63) / 64 * 64;
         m.np = (m.n + 63) / 64 * 64;
         m.row_x = l.rows_x;
         m.row_a = l.rows_a;
+        m.index = l.matrices;
         l.rows_x += m.mp * m.repeat;
         l.rows_a += m.mp * m.repeat;
         l.pitch_x = std::max(l.pitch_x, m.np);
         l.pitch_a = std::max(l.pitch_a, m.mp);
-        const int T = (m.mp + 127) / 128;
-        m.tiles_sym = T * (T + 1) / 2;
-        m.tiles_x = T * ((m.np + 127) / 128);
-        m.first_sym = sym;
-        m.first_x = xt;
-        sym += m.tiles_sym * m.repeat;
-        xt += m.tiles_x * m.repeat;
-        m.norm_blocks = (int)ceil_div64((int64_t)m.m * m.n, NS_NORM_ELEMS);
+        const int64_t elems = (int64_t)m.m * m.n;
+        m.norm_elems = (int)std::max<int64_t>(NS_NORM_ELEMS, ceil_div64(ceil_div64(elems, NS_NORM_BLOCKS), NS_THREADS) * NS_THREADS);
+        m.norm_blocks = (int)ceil_div64(elems, m.norm_elems);
         m.conv_blocks = (m.mp / 64) * (m.np / 64);
         m.first_norm = l.norm_blocks;
-        m.first_conv = conv;
+        m.first_conv = l.conv_blocks;
         l.norm_blocks += m.norm_blocks * m.repeat;
-        conv += m.conv_blocks * m.repeat;
+        l.conv_blocks += m.conv_blocks * m.repeat;
+        l.matrices += m.repeat;
     }
     return l;
+}
+
+// tiles of the products for tiles of 128 x bn; returns the numbers of tiles of A and of X
+static void ns_tiles(NsGroup &g, int bn, int &tiles_a, int &tiles_x)
+{
+    tiles_a = tiles_x = 0;
+    for (int d = 0; d < g.count; ++d) {
+        NsMat &m = g.mat[d];
+        const int T = (m.mp + 127) / 128;
+        m.tiles_a = T * ((m.mp + bn - 1) / bn);
+        m.tiles_x = T * ((m.np + bn - 1) / bn);
+        m.first_a = tiles_a;
+        m.first_x = tiles_x;
+        tiles_a += m.tiles_a * m.repeat;
+        tiles_x += m.tiles_x * m.repeat;
+    }
 }
 
 struct NsTarget {
@@ -515,82 +1325,133 @@ struct NsTarget {
     float keep;
 };
 
-static bool ns_run(TcState &tc, Exec &ex, const NsSource &src, NsGroup &g, const NsLayout &l, int parts, int steps, double a, double b, double c, double eps,
-                   const NsTarget &out, uint8_t *ws, std::string &err)
+template <int BN, int PARTS>
+static void ns_launch_tile(Exec &ex, int tiles, const CUtensorMap &a, const CUtensorMap &b, NsPhase &p, const NsGroup &g)
 {
-    __half *X = (__half *)ws;
-    __half *A = (__half *)(ws + NsLayout::up(2 * l.x_elems()));
-    __half *B = (__half *)((uint8_t *)A + NsLayout::up(2 * l.a_elems(parts)));
-    double *partial = (double *)((uint8_t *)B + NsLayout::up(2 * l.a_elems(parts)));
-    const size_t lo_x = (size_t)l.rows_x * l.pitch_x, lo_a = (size_t)l.rows_a * l.pitch_a;
-    CUtensorMap xk, xmn, ak, bk;
-    if (!ns_make_map(tc, &xk, X, (int64_t)2 * NS_X_PARTS * l.rows_x, l.pitch_x, 128) || !ns_make_map(tc, &xmn, X, (int64_t)2 * NS_X_PARTS * l.rows_x, l.pitch_x, 64) ||
-        !ns_make_map(tc, &ak, A, (int64_t)parts * l.rows_a, l.pitch_a, 128) || !ns_make_map(tc, &bk, B, (int64_t)parts * l.rows_a, l.pitch_a, 128)) {
+    p.stages = ns_tile_stages<BN, PARTS>();
+    const size_t smem = (size_t)p.stages * PARTS * (128 + BN) * TC_BK * 2 + 1024;
+    launch_dep(ns_tile_kernel<BN, PARTS>, dim3(tiles), dim3(64 + 2 * BN), smem, ex.st, a, b, p, g);
+    ex.launches += 1;
+}
+
+// estimated microseconds of one step of the chain kernel with clusters of C blocks
+static double ns_chain_cost(const NsGroup &g, int parts, int c, int room, int tiles_a, int tiles_x)
+{
+    if (room <= 0) return 1e30;
+    int kb_m = 0, kb_n = 0;
+    for (int d = 0; d < g.count; ++d) { kb_m = std::max(kb_m, g.mat[d].mp / 64); kb_n = std::max(kb_n, g.mat[d].np / 64); }
+    const double kb_us = parts == 2 ? 0.7 : 0.45, tile_us = c > 1 ? 2.4 : 0.4, phase_us = 3.0;  // read off runs of 64 x 64, 256 x 256 and 1000 x 417
+    auto phase = [&](int tiles, int kb) { return phase_us + ((tiles + room - 1) / room) * (tile_us + kb_us * ((kb + c - 1) / c)); };
+    return phase(tiles_a, kb_n) + phase(tiles_a, kb_m) + phase(tiles_x, kb_m);
+}
+
+struct NsCounters {  // barrier counters of the chain kernel: two sets used in turn, each launch clears the other one
+    unsigned *dev = nullptr;
+    int turn = 0;
+};
+
+template <int PARTS>
+static bool ns_run(TcState &tc, Exec &ex, const NsSource &src, NsGroup &g, const NsLayout &l, const NsAdam &adam, NsCounters &counters, int steps, double a, double b,
+                   double c, double eps, const NsTarget &out, uint8_t *ws, std::string &err)
+{
+    const size_t nx = l.x_elems(), na = l.a_elems();
+    NsX X[2];
+    X[0].full = (float *)ws;
+    X[1].full = (float *)(ws + NsLayout::up(4 * nx));
+    __half *ops = (__half *)(ws + 2 * NsLayout::up(4 * nx));
+    for (int i = 0; i < 2; ++i) {
+        X[i].hi = ops + (size_t)i * PARTS * nx;
+        X[i].lo_off = nx;
+        X[i].pitch = l.pitch_x;
+    }
+    __half *A = (__half *)((uint8_t *)ops + NsLayout::up((size_t)4 * PARTS * nx));
+    __half *B = (__half *)((uint8_t *)A + NsLayout::up((size_t)2 * PARTS * na));
+    double *partial = (double *)((uint8_t *)B + NsLayout::up((size_t)2 * PARTS * na));
+    float *inv_r = (float *)((uint8_t *)partial + NsLayout::up(sizeof(double) * (size_t)l.norm_blocks));
+    const int adam_blocks = (int)ceil_div64(adam.spans.first[adam.spans.count], NS_ADAM_ELEMS);
+    CUtensorMap x128, x64, a128, a64, b128;
+    if (g.count > 0 && (!ns_make_map(tc, &x128, ops, (int64_t)2 * PARTS * l.rows_x, l.pitch_x, 128) || !ns_make_map(tc, &x64, ops, (int64_t)2 * PARTS * l.rows_x, l.pitch_x, 64) ||
+                        !ns_make_map(tc, &a128, A, (int64_t)PARTS * l.rows_a, l.pitch_a, 128) || !ns_make_map(tc, &a64, A, (int64_t)PARTS * l.rows_a, l.pitch_a, 64) ||
+                        !ns_make_map(tc, &b128, B, (int64_t)PARTS * l.rows_a, l.pitch_a, 128))) {
         err = "cuTensorMapEncodeTiled failed";
         return false;
     }
-    int sym = 0, xt = 0, conv = 0;
-    for (int d = 0; d < g.count; ++d) {
-        sym += g.mat[d].tiles_sym * g.mat[d].repeat;
-        xt += g.mat[d].tiles_x * g.mat[d].repeat;
-        conv += g.mat[d].conv_blocks * g.mat[d].repeat;
+    int tiles_a = 0, tiles_x = 0;
+    ns_tiles(g, NSC_BN, tiles_a, tiles_x);
+    const int rooms[3] = {ns_chain_room<PARTS, 1>(), ns_chain_room<PARTS, 2>(), ns_chain_room<PARTS, 4>()};
+    int best = -1;
+    double cost = 1e30;
+    for (int i = 0; i < 3; ++i) {
+        const double t = ns_chain_cost(g, PARTS, 1 << i, rooms[i], tiles_a, tiles_x);
+        if (t < cost) { cost = t; best = i; }
     }
-    launch_dep(ns_norm_kernel, dim3(l.norm_blocks), dim3(NS_THREADS), 0, ex.st, src, g, partial);
-    launch_dep(ns_convert_kernel, dim3(conv), dim3(NS_THREADS), 0, ex.st, src, g, partial, (float)eps, X, l.pitch_x, lo_x);
-    ex.launches += 2;
+    if (best >= 0 && g.count > 0 && std::max(tiles_a, tiles_x) <= 4 * tc_sm_count()) {
+        NsChain p{};
+        p.parts_rows_x = l.rows_x; p.parts_rows_a = l.rows_a;
+        p.steps = steps;
+        p.a = (float)a; p.b = (float)b; p.c = (float)c; p.eps = eps;
+        p.X[0] = X[0]; p.X[1] = X[1]; p.A = A; p.B = B;
+        p.pitch_a = l.pitch_a; p.lo_off_a = na;
+        p.partial = partial; p.inv_r = inv_r;
+        p.norm_blocks = l.norm_blocks; p.adam_blocks = adam_blocks; p.conv_blocks = l.conv_blocks; p.tiles_a = tiles_a; p.tiles_x = tiles_x;
+        p.dst = out.dst; p.bf16_dst = out.bf16_dst; p.params = out.params; p.keep = out.keep;
+        p.counters = counters.dev + counters.turn * NSC_BARRIERS;
+        p.next_counters = counters.dev + (counters.turn ^ 1) * NSC_BARRIERS;
+        p.err = tc.err_word; p.wait_ns = tc.wait_limit_ns; p.extra_tx = tc.overdeclare_tx;
+        tc.overdeclare_tx = 0;
+        const int cl = 1 << best;
+        const int clusters = std::min(rooms[best], std::max({tiles_a, tiles_x, (l.conv_blocks + cl - 1) / cl, (l.norm_blocks + adam_blocks + cl - 1) / cl}));
+        cudaLaunchAttribute attr[2];
+        cudaError_t e = cudaSuccess;
+#define LP_CHAIN(C_)                                                                                                                                 \
+    do {                                                                                                                                             \
+        cudaLaunchConfig_t cfg = ns_chain_config<PARTS, C_>(clusters, ex.st, attr);                                                                  \
+        e = cudaLaunchKernelEx(&cfg, ns_chain_kernel<PARTS, C_>, x128, x64, a128, a64, b128, src, g, adam, p);                                        \
+    } while (0)
+        if (best == 0) LP_CHAIN(1); else if (best == 1) LP_CHAIN(2); else LP_CHAIN(4);
+#undef LP_CHAIN
+        if (e != cudaSuccess) {
+            cudaGetLastError();
+            err = std::string("launch of the chain kernel: ") + cudaGetErrorString(e);
+            return false;
+        }
+        counters.turn ^= 1;
+        ex.launches += 1;
+        return true;
+    }
+    launch_dep(ns_norm_kernel, dim3(std::max(1, l.norm_blocks + adam_blocks)), dim3(NS_THREADS), 0, ex.st, src, g, adam, l.norm_blocks, partial);
+    ex.launches += 1;
+    if (g.count == 0) return true;
+    ns_tiles(g, 128, tiles_a, tiles_x);
+    launch_dep(ns_convert_kernel<PARTS>, dim3(l.conv_blocks), dim3(NS_THREADS), 0, ex.st, src, g, partial, eps, X[0], inv_r);
+    ex.launches += 1;
     NsPhase p{};
-    p.parts = parts;
     p.a = (float)a; p.b = (float)b; p.c = (float)c;
-    p.stages = parts == 2 ? 3 : 6;
     p.err = tc.err_word;
     p.wait_ns = tc.wait_limit_ns;
-    const size_t smem = (size_t)p.stages * 2 * parts * 128 * TC_BK * 2 + 1024;
-    for (int k = 0; k < steps; ++k) {
-        const int cur = k & 1;
-        p.row_off_b = cur * NS_X_PARTS * l.rows_x;
+    p.pitch_a = l.pitch_a;
+    p.lo_off_a = na;
+    p.inv_r = inv_r;
+    p.dst = out.dst; p.bf16_dst = out.bf16_dst; p.params = out.params; p.keep = out.keep;
+    auto product = [&](int kind, int tiles, const CUtensorMap &ma, const CUtensorMap &mb) {
+        p.kind = kind;
         p.extra_tx = tc.overdeclare_tx;
         tc.overdeclare_tx = 0;
-        p.kind = NS_GRAM;
-        p.part_rows_a = p.part_rows_b = l.rows_x;
-        p.addend = nullptr; p.out = A; p.pitch = l.pitch_a; p.lo_off = lo_a;
-        launch_dep(ns_product_kernel, dim3(sym), dim3(TC_THREADS), smem, ex.st, xk, xk, p, g);
-        p.extra_tx = 0;
-        p.kind = NS_POLY;
-        p.part_rows_a = p.part_rows_b = l.rows_a;
-        p.addend = A; p.out = B;
-        launch_dep(ns_product_kernel, dim3(sym), dim3(TC_THREADS), smem, ex.st, ak, ak, p, g);
-        p.kind = k + 1 == steps ? NS_LAST : NS_APPLY;
-        p.part_rows_b = l.rows_x;
-        p.addend = X + (size_t)cur * NS_X_PARTS * lo_x; p.out = X + (size_t)(cur ^ 1) * NS_X_PARTS * lo_x; p.pitch = l.pitch_x; p.lo_off = lo_x;
-        p.dst = out.dst; p.bf16_dst = out.bf16_dst; p.params = out.params; p.keep = out.keep;
-        launch_dep(ns_product_kernel, dim3(xt), dim3(TC_THREADS), smem, ex.st, bk, xmn, p, g);
-        ex.launches += 3;
+        ns_launch_tile<128, PARTS>(ex, tiles, ma, mb, p, g);
+    };
+    for (int k = 0; k < steps; ++k) {
+        const int cur = k & 1;
+        p.x_row0 = cur * PARTS * l.rows_x;
+        p.lo_rows_a = p.lo_rows_b = l.rows_x;
+        p.out = A;
+        p.next = X[cur ^ 1];
+        product(NS_GRAM, tiles_a, x128, x128);
+        p.lo_rows_a = p.lo_rows_b = l.rows_a;
+        p.A = A; p.out = B;
+        product(NS_POLY, tiles_a, a128, a128);
+        p.lo_rows_b = l.rows_x;
+        p.X = X[cur].full;
+        product(k + 1 == steps ? NS_LAST : NS_APPLY, tiles_x, b128, x64);
     }
     return true;
-}
-
-// ---------------------------------------------------------------------------------------------
-// weight update: every parameter that belongs to no matrix takes an Adam step
-// ---------------------------------------------------------------------------------------------
-struct NsSpans {  // the stretches of the flat vector between the matrices
-    int count;
-    long long begin[NS_MAX_MATS + 1], first[NS_MAX_MATS + 2];  // first element, and elements before the stretch; first[count] = all
-};
-__global__ void ns_adam_kernel(const float *__restrict__ p, const float *__restrict__ m, const float *__restrict__ v, const float *__restrict__ grad, const NsSpans spans,
-                               float scale, float lr, float b1, float one_minus_b1, float b2, float one_minus_b2, float eps, float inv_c1, float inv_c2,
-                               float *__restrict__ pn, float *__restrict__ mn, float *__restrict__ vn)
-{
-    LP_DEP_ENTER();
-    const long long e = (long long)blockIdx.x * blockDim.x + threadIdx.x;
-    if (e >= spans.first[spans.count]) return;
-    int s = 0;
-    while (e >= spans.first[s + 1]) ++s;
-    const long long i = spans.begin[s] + (e - spans.first[s]);
-    const float g = scale * grad[i];
-    const float mi = b1 * m[i] + one_minus_b1 * g;
-    const float vi = b2 * v[i] + one_minus_b2 * g * g;
-    const float pi = p[i] - lr * (mi * inv_c1) / (sqrtf(vi * inv_c2) + eps);
-    mn[i] = mi;
-    vn[i] = vi;
-    pn[i] = pi;
 }

@@ -256,7 +256,8 @@ def test_orthogonalize(ctx, dtype, batch, rows, cols):
     ctx.stats()
 
 
-@pytest.mark.parametrize("dtype,kind", [(BF16, "rank1"), (BF16, "rank3")] + [(d, k) for d in (F32, BF16) for k in ("decay", "zero_rows", "spike", "large", "tiny")])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("kind", ["rank1", "rank3", "decay", "zero_rows", "spike", "large", "tiny"])
 def test_orthogonalize_spectra(ctx, dtype, kind):
     g = gen(3)
     rows, cols = 192, 320
