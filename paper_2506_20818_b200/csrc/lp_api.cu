@@ -2188,26 +2188,35 @@ extern "C" lp_status lp_embed_grad(lp_ctx *ctx, int32_t dout_prec, const void *d
     lp_status s = check_table(ctx, "lp_embed_grad", dout_prec, grad_prec, rows, width, ld_grad, n_ids, ld_dout, scale);
     if (s != LP_OK) return s;
     if (dout_prec == LP_FP32 && grad_prec == LP_BF16) return fail(ctx, LP_EUNSUPPORTED, "lp_embed_grad: a BF16 gradient needs BF16 rows");
+    if (n_ids >= (int64_t)1 << 30) return fail(ctx, LP_EINVAL, "lp_embed_grad: number of ids must be below 2^30");
     if (!grad || (n_ids > 0 && (!ids || !dout))) return fail(ctx, LP_EINVAL, "lp_embed_grad: null array");
     if (misaligned(dout, dout_prec) || misaligned(ids, LP_FP32) || misaligned(grad, grad_prec))
         return fail(ctx, LP_EINVAL, "lp_embed_grad: an array is not aligned to its elements");
     if (n_ids == 0 && accumulate) return LP_OK;
     CK(cudaSetDevice(ctx->device));
-    // one workspace: keys and values (two sets each for the sort), bit per row, digit counts, partial rows of the chunks
+    // one workspace: keys and values (two sets each for the sort), flag per row, digit counts, tickets, tile counts, partial rows
     EmbedGradScratch sc;
+    EmbedSort &es = sc.sort;
+    const int key_bits = bits_for(rows + 1);
+    es.passes = (key_bits + 7) / 8;
+    es.bits = (key_bits + es.passes - 1) / es.passes;
+    es.tiles = (int)ceil_div64(n_ids, ES_TILE);
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) & ~(size_t)255; return here; };
-    const size_t n4 = sizeof(uint32_t) * (size_t)std::max<int64_t>(n_ids, 1), parts = sizeof(float) * (size_t)ceil_div64(std::max<int64_t>(n_ids, 1), EG_CHUNK) * width;
-    const size_t o_keys = take(n4), o_vals = take(n4), o_keys2 = take(n4), o_vals2 = take(n4), o_named = take(sizeof(uint32_t) * (size_t)ceil_div64(rows, 32));
-    const size_t o_hist = take(sizeof(int) * (size_t)SortScratch::hist_ints(n_ids)), o_scan = take(sizeof(int) * (size_t)SortScratch::scan_ints(n_ids));
+    const size_t n4 = sizeof(uint32_t) * (size_t)n_ids, parts = sizeof(float) * (size_t)ceil_div64(n_ids, EG_SPAN) * width;
+    const size_t o_named = take((size_t)rows), o_hist = take(sizeof(unsigned) * (size_t)es.passes * ES_DIGITS);
+    const size_t o_ticket = take(sizeof(unsigned) * (size_t)es.passes);
+    sc.clear_bytes = at;
+    const size_t o_keys = take(n4), o_vals = take(n4), o_keys2 = take(n4), o_vals2 = take(n4);
+    const size_t o_status = take(sizeof(unsigned) * (size_t)es.passes * es.tiles * ES_DIGITS);
     const size_t o_head = take(parts), o_tail = take(parts);
     uint8_t *ws = nullptr;
     s = op_workspace(ctx, at, &ws);
     if (s != LP_OK) return s;
-    sc.keys = (uint32_t *)(ws + o_keys); sc.vals = (uint32_t *)(ws + o_vals);
-    sc.sort.keys_alt = (uint32_t *)(ws + o_keys2); sc.sort.vals_alt = (uint32_t *)(ws + o_vals2);
-    sc.named = (uint32_t *)(ws + o_named);
-    sc.sort.hist = (int *)(ws + o_hist); sc.sort.scan_tmp = (int *)(ws + o_scan);
+    es.named = ws + o_named; es.hist = (unsigned *)(ws + o_hist); es.ticket = (unsigned *)(ws + o_ticket);
+    es.keys[0] = (uint32_t *)(ws + o_keys); es.vals[0] = (uint32_t *)(ws + o_vals);
+    es.keys[1] = (uint32_t *)(ws + o_keys2); es.vals[1] = (uint32_t *)(ws + o_vals2);
+    es.status = (unsigned *)(ws + o_status);
     sc.head = (float *)(ws + o_head); sc.tail = (float *)(ws + o_tail);
     const float f = (float)scale;
     if (dout_prec == LP_FP32) embed_grad_launch<float, float>(ctx->ex, (const float *)dout, ld_dout, ids, n_ids, padding_id, f, rows, width, (float *)grad, ld_grad, accumulate, sc, ctx->err_flag);
