@@ -307,7 +307,6 @@ struct NsPhase {
     int bf16_dst;
     const float *params;                 // weight update: dst = keep * params - update * result
     float keep;
-    int stages;
     int *err;
     unsigned long long wait_ns;
     int extra_tx;
@@ -350,253 +349,6 @@ template <int PARTS> LP_DEVINL void ns_store8(const float *v, __half *hi, size_t
     }
     *reinterpret_cast<uint4 *>(hi) = make_uint4(h[0], h[1], h[2], h[3]);
     if (PARTS == 2) *reinterpret_cast<uint4 *>(hi + lo_off) = make_uint4(l[0], l[1], l[2], l[3]);
-}
-
-// result columns col .. col + 63 of row `row` (oriented), already divided by the scale of X
-LP_DEVINL void ns_write_result(const NsPhase &p, const NsMat &mat, int rep, int row, int col, const float *v)
-{
-    const long long base = mat.dst + rep * mat.dst_stride;
-    if (mat.tall) {  // neighbouring lanes hold neighbouring rows, which are consecutive in the result
-#pragma unroll
-        for (int i = 0; i < 64; ++i) {
-            if (col + i >= mat.n) break;
-            const long long o = base + (long long)(col + i) * mat.ld_dst + row;
-            if (p.params) ((float *)p.dst)[o] = fmaf(-mat.update, v[i], p.keep * p.params[o]);
-            else if (p.bf16_dst) ((bf16 *)p.dst)[o] = __float2bfloat16_rn(v[i]);
-            else ((float *)p.dst)[o] = v[i];
-        }
-        return;
-    }
-    const long long o = base + (long long)row * mat.ld_dst + col;
-    const bool whole = col + 64 <= mat.n;
-    if (p.bf16_dst) {
-        bf16 *q = (bf16 *)p.dst + o;
-        if (whole && ((uintptr_t)q & 15) == 0) {
-#pragma unroll
-            for (int i = 0; i < 64; i += 8) store_elems<bf16, 8>(q + i, v + i);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 64; ++i)
-                if (col + i < mat.n) q[i] = __float2bfloat16_rn(v[i]);
-        }
-        return;
-    }
-    float *q = (float *)p.dst + o;
-    const float *w = p.params ? p.params + o : nullptr;
-    if (whole && (((uintptr_t)q | (uintptr_t)w) & 15) == 0) {
-#pragma unroll
-        for (int i = 0; i < 64; i += 4) {
-            float x[4] = {v[i], v[i + 1], v[i + 2], v[i + 3]};
-            if (w) {
-                float old[4];
-                load_elems<float, 4>(w + i, old);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) x[k] = fmaf(-mat.update, x[k], p.keep * old[k]);
-            }
-            store_elems<float, 4>(q + i, x);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 64; ++i)
-            if (col + i < mat.n) q[i] = w ? fmaf(-mat.update, v[i], p.keep * w[i]) : v[i];
-    }
-}
-
-// One CTA per 128 x BN tile of the result.  Warp 0 brings the operand tiles in by TMA (all parts of both), warp 1 issues the
-// matrix instructions, the other BN / 16 warps hold 64 columns of one row per thread and write the result.
-//   chunks: after every block of 64 terms (PARTS = 2) or at the end (PARTS = 1) the accumulator changes hands; two of them
-//           in tensor memory are used in turn, so the next block's products run while the last one is added up
-//   all tiles of A and B are computed although they are symmetric: these kernels run where there are fewer tiles than SMs,
-//           and writing mirrored tiles would only lengthen them
-//   the next kernel of the chain is let in at once (its blocks set themselves up on idle SMs and wait for this one to end)
-template <int BN, int PARTS>
-__global__ void __launch_bounds__(64 + 2 * BN) ns_tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const NsPhase p,
-                                                              const __grid_constant__ NsGroup g)
-{
-    extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t bar_full[8], bar_empty[8], bar_acc_full[2], bar_acc_empty[2];
-    __shared__ uint32_t tmem_base_s;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-    const bool square = p.kind == NS_GRAM || p.kind == NS_POLY;
-    const int t = blockIdx.x;
-    const int d = square ? ns_find(g, t, [](const NsMat &m) { return m.first_a; }) : ns_find(g, t, [](const NsMat &m) { return m.first_x; });
-    const NsMat &mat = g.mat[d];
-    const int per = square ? mat.tiles_a : mat.tiles_x, first = square ? mat.first_a : mat.first_x;
-    const int rep = (t - first) / per, tt = (t - first) % per;
-    const int T = (mat.mp + 127) / 128;
-    const int ti = tt % T, tj = tt / T;
-    const int K = p.kind == NS_GRAM ? mat.np : mat.mp;
-    const int num_kb = K / TC_BK;
-    const int slot_x = mat.row_x + rep * mat.mp, slot_a = mat.row_a + rep * mat.mp;
-    const bool b_mn = !square;
-    const int S = p.stages;
-    constexpr uint32_t a_bytes = 128 * TC_BK * 2, b_bytes = BN * TC_BK * 2, stage_bytes = PARTS * (a_bytes + b_bytes);
-
-    if (threadIdx.x == 0) {
-        for (int s = 0; s < S; ++s) {
-            mbar_init(smem_u32(&bar_full[s]), 1);
-            mbar_init(smem_u32(&bar_empty[s]), 1);
-        }
-        for (int b = 0; b < 2; ++b) {
-            mbar_init(smem_u32(&bar_acc_full[b]), 1);
-            mbar_init(smem_u32(&bar_acc_empty[b]), BN / 16);
-        }
-        fence_barrier_init();
-        fence_async_proxy();
-        tma_prefetch_desc(&mapA);
-        tma_prefetch_desc(&mapB);
-    }
-    if (warp == 0) {
-        __syncwarp();
-        tmem_alloc(smem_u32(&tmem_base_s), 2 * BN);
-    }
-    tc_fence_before();
-    __syncthreads();
-    tc_fence_after();
-    const uint32_t tmem = tmem_base_s;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    LP_DEP_ENTER();
-
-    if (warp == 0) {
-        if (lane == 0) {
-            const int row_a = (p.kind == NS_GRAM ? p.x_row0 + slot_x : slot_a) + ti * 128;
-            const int row_b = p.kind == NS_GRAM ? p.x_row0 + slot_x + tj * BN : p.kind == NS_POLY ? slot_a + tj * BN : p.x_row0 + slot_x;
-            for (int kb = 0; kb < num_kb; ++kb) {
-                const int s = kb % S;
-                if (kb >= S && !mbar_wait(smem_u32(&bar_empty[s]), ((kb / S) & 1) ^ 1, p.wait_ns)) {
-                    atomicExch(p.err, 1);
-                    break;
-                }
-                const uint32_t sa = smem_u32(smem + (size_t)s * stage_bytes), sb = sa + PARTS * a_bytes, bar = smem_u32(&bar_full[s]);
-                mbar_expect_tx(bar, stage_bytes + (kb == 0 && t == 0 ? (uint32_t)p.extra_tx : 0u));
-                const int kk = kb * TC_BK;
-#pragma unroll
-                for (int q = 0; q < PARTS; ++q) {
-                    tma_load_2d(sa + q * a_bytes, &mapA, bar, kk, row_a + q * p.lo_rows_a);
-                    if (!b_mn) {
-                        tma_load_2d(sb + q * b_bytes, &mapB, bar, kk, row_b + q * p.lo_rows_b);
-                    } else {  // X as the second operand: 64 rows of K, boxes of 64 columns
-#pragma unroll
-                        for (int c = 0; c < BN / 64; ++c) tma_load_2d(sb + q * b_bytes + c * 8192, &mapB, bar, tj * BN + c * 64, row_b + kk + q * p.lo_rows_b);
-                    }
-                }
-            }
-        }
-    } else if (warp == 1) {
-        if (lane == 0) {
-            const uint32_t idesc = make_idesc_f16(128, BN, b_mn);
-            bool ok = true;
-            for (int kb = 0; kb < num_kb && ok; ++kb) {
-                const int s = kb % S;
-                const int chunk = PARTS == 2 ? kb : 0, b = chunk & 1;
-                if (PARTS == 2 && kb >= 2 && !mbar_wait(smem_u32(&bar_acc_empty[b]), ((kb >> 1) & 1) ^ 1, p.wait_ns)) {
-                    atomicExch(p.err, 5);
-                    break;
-                }
-                if (!mbar_wait(smem_u32(&bar_full[s]), (kb / S) & 1, p.wait_ns)) {
-                    atomicExch(p.err, 2);
-                    break;
-                }
-                tc_fence_after();
-                const uint32_t sa = smem_u32(smem + (size_t)s * stage_bytes), sb = sa + PARTS * a_bytes;
-                const uint32_t acc = tmem + b * BN;
-                auto product = [&](uint32_t oa, uint32_t ob, int k, uint32_t add) {
-                    const uint64_t da = make_smem_desc(sa + oa + k * 32, 16, 1024);
-                    const uint64_t db = b_mn ? make_smem_desc(sb + ob + k * 2048, 8192, 1024) : make_smem_desc(sb + ob + k * 32, 16, 1024);
-                    umma_bf16(acc, da, db, idesc, add);
-                };
-                if (PARTS == 2) {  // the small terms first
-#pragma unroll
-                    for (int k = 0; k < TC_BK / TC_UMMA_K; ++k) {
-                        product(0, b_bytes, k, k != 0 ? 1u : 0u);
-                        product(a_bytes, 0, k, 1u);
-                    }
-                }
-#pragma unroll
-                for (int k = 0; k < TC_BK / TC_UMMA_K; ++k) product(0, 0, k, PARTS == 2 || (kb | k) != 0 ? 1u : 0u);
-                umma_commit(smem_u32(&bar_empty[s]));
-                if (PARTS == 2 || kb + 1 == num_kb) umma_commit(smem_u32(&bar_acc_full[b]));
-            }
-        }
-    } else {
-        const int q = warp & 3, half = (warp - 2) >> 2;
-        const int row = ti * 128 + q * 32 + lane, col = tj * BN + half * 64;
-        const bool live = row < mat.mp && col < (square ? mat.mp : mat.np);
-        // the addend is requested before the products are waited for
-        float v[64], add[64];
-        const size_t at_a = (size_t)(slot_a + row) * p.pitch_a + col, at_x = (size_t)(slot_x + row) * p.next.pitch + col;
-        float factor = NS_A_SCALE / (NS_X_SCALE * NS_X_SCALE), weight = 0.f;
-        const float inv_r = p.inv_r[mat.index + rep];
-#pragma unroll
-        for (int i = 0; i < 64; ++i) add[i] = 0.f;
-        if (p.kind == NS_POLY) {
-            factor = p.c / NS_A_SCALE * (inv_r * inv_r) * (inv_r * inv_r);
-            weight = p.b * (inv_r * inv_r);
-            if (live) {
-#pragma unroll
-                for (int i = 0; i < 64; i += 8) {
-                    ns_add8(*reinterpret_cast<const uint4 *>(p.A + at_a + i), add + i);
-                    if (PARTS == 2) ns_add8(*reinterpret_cast<const uint4 *>(p.A + p.lo_off_a + at_a + i), add + i);
-                }
-            }
-        } else if (!square) {
-            factor = 1.f / NS_A_SCALE;
-            weight = p.a;
-            if (live) {
-#pragma unroll
-                for (int i = 0; i < 64; i += 4) load_elems<float, 4>(p.X + at_x + i, add + i);
-            }
-        }
-        const int chunks = PARTS == 2 ? num_kb : 1;
-        bool ok = true;
-        for (int c = 0; c < chunks; ++c) {
-            const int b = c & 1;
-            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_acc_full[b]), (c >> 1) & 1, p.wait_ns));
-            if (!ok) {
-                if (lane == 0) atomicExch(p.err, 3);
-                break;
-            }
-            tc_fence_after();
-            const uint32_t taddr = tmem + ((uint32_t)(q * 32) << 16) + b * BN + half * 64;
-            uint32_t r[2][32];
-            tmem_ld_32x32_issue(taddr, r[0]);
-            tmem_ld_32x32_issue(taddr + 32, r[1]);
-            tmem_ld_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&bar_acc_empty[b]));
-#pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                v[i] = c == 0 ? __uint_as_float(r[0][i]) : v[i] + __uint_as_float(r[0][i]);
-                v[32 + i] = c == 0 ? __uint_as_float(r[1][i]) : v[32 + i] + __uint_as_float(r[1][i]);
-            }
-        }
-        if (ok && live) {
-#pragma unroll
-            for (int i = 0; i < 64; ++i) v[i] = fmaf(weight, add[i], factor * v[i]);
-            if (square) {
-#pragma unroll
-                for (int i = 0; i < 64; i += 8) ns_store8<PARTS>(v + i, p.out + at_a + i, p.lo_off_a);
-            } else if (p.kind == NS_APPLY) {
-#pragma unroll
-                for (int i = 0; i < 64; i += 4) store_elems<float, 4>(p.next.full + at_x + i, v + i);
-#pragma unroll
-                for (int i = 0; i < 64; i += 8) ns_store8<PARTS>(v + i, p.next.hi + at_x + i, p.next.lo_off);
-            } else if (row < mat.m && col < mat.n) {
-#pragma unroll
-                for (int i = 0; i < 64; ++i) v[i] *= inv_r / NS_X_SCALE;
-                ns_write_result(p, mat, rep, row, col, v);
-            }
-        }
-    }
-    __syncwarp();
-    tc_fence_before();
-    __syncthreads();
-    if (warp == 0) {
-        __syncwarp();
-        tmem_dealloc(tmem, 2 * BN);
-    }
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -1166,16 +918,333 @@ __global__ void __launch_bounds__(NSC_THREADS, 1) ns_chain_kernel(const __grid_c
     }
 }
 
+// The matrix instruction of a pair of SMs: 256 rows (128 per CTA), operands FP16
+LP_DEVINL void ns_result4(const NsPhase &p, const NsMat &mat, int rep, int row, int col, const float *v)  // columns col .. col + 3 of row `row`, not tall
+{
+    const long long o = mat.dst + rep * mat.dst_stride + (long long)row * mat.ld_dst + col;
+    if (col + 4 <= mat.n && p.bf16_dst && ((uintptr_t)((bf16 *)p.dst + o) & 7) == 0) {
+        store_elems<bf16, 4>((bf16 *)p.dst + o, v);
+        return;
+    }
+    if (col + 4 <= mat.n && !p.bf16_dst && (((uintptr_t)((float *)p.dst + o) | (uintptr_t)(p.params ? p.params + o : nullptr)) & 15) == 0) {
+        float x[4] = {v[0], v[1], v[2], v[3]};
+        if (p.params) {
+            float old[4];
+            load_elems<float, 4>(p.params + o, old);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = fmaf(-mat.update, v[i], p.keep * old[i]);
+        }
+        store_elems<float, 4>((float *)p.dst + o, x);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (col + i >= mat.n) break;
+        if (p.params) ((float *)p.dst)[o + i] = fmaf(-mat.update, v[i], p.keep * p.params[o + i]);
+        else if (p.bf16_dst) ((bf16 *)p.dst)[o + i] = __float2bfloat16_rn(v[i]);
+        else ((float *)p.dst)[o + i] = v[i];
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// products of large matrices: one launch per product, persistent pairs of SMs (clusters of two CTAs, cta_group::2)
+//
+// A pair multiplies tiles of 256 x 256 (PARTS = 2: 256 x 128): each CTA brings in 128 rows of the first operand and half of the
+// second, so a 64-term block costs 32 KiB per CTA for 512 cycles of products (48 KiB for 768).  PARTS = 1: two accumulators of
+// 256 columns fill tensor memory, and a tile's is drained while the next tile's products run.  PARTS = 2: the accumulators
+// change hands after every 64-term block and sixteen warps add the blocks up in registers (32 columns per thread; 64, for tiles of
+// 256 x 256, spill).
+// A and B are symmetric: only tiles on and above the diagonal are computed, the others are written turned.
+//   warp 0 operands, warp 1 matrix instructions (of the pair's first CTA), warps 2-17 results: 32 rows x 64 (32) columns each, turned
+//   through 4 KiB of shared memory per warp so that rows are written in pieces of 128 bytes
+// ---------------------------------------------------------------------------------------------
+constexpr int NSP_THREADS = 576;
+template <int PARTS> constexpr int NSP_BN = PARTS == 2 ? 128 : 256;
+template <int PARTS> constexpr int NSP_STAGES = PARTS == 2 ? 3 : 5;
+template <int PARTS> constexpr int NSP_STAGE_BYTES = PARTS * (128 + NSP_BN<PARTS> / 2) * TC_BK * 2;
+constexpr int NSP_TURN_BYTES = 16 * 4096;
+template <int PARTS> constexpr int NSP_SMEM = NSP_STAGES<PARTS> * NSP_STAGE_BYTES<PARTS> + NSP_TURN_BYTES + 1024;
+
+// tile t of the upper triangle (rows i <= columns j) of a T x T grid, row by row
+LP_DEVINL void ns_triangle(int t, int T, int &i, int &j)
+{
+    i = 0;
+    while (t >= T - i) { t -= T - i; ++i; }
+    j = i + t;
+}
+
+template <int PARTS>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NSP_THREADS, 1)
+    ns_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const __grid_constant__ NsPhase p, const __grid_constant__ NsGroup g, int tiles)
+{
+    LP_DEP_ENTER();
+    extern __shared__ uint8_t smem_raw[];
+    constexpr int S = NSP_STAGES<PARTS>;
+    __shared__ __align__(8) uint64_t bar_full[S], bar_empty[S], bar_acc_full[2], bar_acc_empty[2];
+    __shared__ uint32_t tmem_base_s;
+    constexpr int BN = NSP_BN<PARTS>, HALVES = BN / 128;  // HALVES: blocks of 32 columns per thread
+    constexpr uint32_t a_bytes = 128 * TC_BK * 2, b_bytes = BN / 2 * TC_BK * 2, stage_bytes = NSP_STAGE_BYTES<PARTS>;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    const int rank = (int)cluster_cta_rank();
+    const bool leader = rank == 0;
+    uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+    const bool square = p.kind == NS_GRAM || p.kind == NS_POLY;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S; ++s) {
+            mbar_init(smem_u32(&bar_full[s]), 2);   // one announcement per CTA of the pair (used in the leader only)
+            mbar_init(smem_u32(&bar_empty[s]), 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(smem_u32(&bar_acc_full[b]), 1);
+            mbar_init(smem_u32(&bar_acc_empty[b]), 32);  // sixteen warps in each CTA (used in the leader only)
+        }
+        fence_barrier_init();
+        fence_async_proxy();
+        tma_prefetch_desc(&mapA);
+        tma_prefetch_desc(&mapB);
+    }
+    if (warp == 0) {
+        __syncwarp();
+        tmem_alloc_pair(smem_u32(&tmem_base_s), 2 * BN);
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_barrier();  // both CTAs' barriers are initialised before either announces anything on them
+    tc_fence_after();
+    const uint32_t tmem = tmem_base_s;
+
+    // where tile t lies: descriptor, repetition, tile row and column, blocks of 64 terms
+    auto locate = [&](int t, int &rep, int &ti, int &tj) {
+        const int d = square ? ns_find(g, t, [](const NsMat &m) { return m.first_a; }) : ns_find(g, t, [](const NsMat &m) { return m.first_x; });
+        const NsMat &mat = g.mat[d];
+        const int per = square ? mat.tiles_a : mat.tiles_x, local = t - (square ? mat.first_a : mat.first_x);
+        rep = local / per;
+        const int tt = local - rep * per, T = (mat.mp + 255) / 256;
+        if (square) {  // blocks of 256 x 256 on and above the diagonal, 256 / BN tiles each
+            ns_triangle(tt / (256 / BN), T, ti, tj);
+            tj = tj * (256 / BN) + tt % (256 / BN);
+        }
+        else { ti = tt % T; tj = tt / T; }
+        return d;
+    };
+
+    if (warp == 0) {
+        if (elect_one()) {
+            // ---- operands: this CTA's 128 rows of the first and 128 rows (or columns) of the second
+            int s = 0, round = 0;
+            bool ok = true, first = true;
+            for (int t = pair; t < tiles && ok; t += n_pairs) {
+                int rep, ti, tj;
+                const NsMat &mat = g.mat[locate(t, rep, ti, tj)];
+                const int slot_x = mat.row_x + rep * mat.mp, slot_a = mat.row_a + rep * mat.mp;
+                const int kbs = (p.kind == NS_GRAM ? mat.np : mat.mp) / TC_BK;
+                const int row_a = (p.kind == NS_GRAM ? p.x_row0 + slot_x : slot_a) + ti * 256 + rank * 128;
+                const int at_b = tj * BN + rank * (BN / 2);
+                for (int kb = 0; kb < kbs; ++kb) {
+                    if (round > 0 && !mbar_wait(smem_u32(&bar_empty[s]), (round & 1) ^ 1, p.wait_ns)) { atomicExch(p.err, 1); ok = false; break; }
+                    const uint32_t sa = smem_u32(smem) + s * stage_bytes, sb = sa + PARTS * a_bytes, bar = map_to_cta(smem_u32(&bar_full[s]), 0);
+                    mbar_expect_tx_remote(bar, stage_bytes + (first && blockIdx.x == 0 ? (uint32_t)p.extra_tx : 0u));
+                    first = false;
+                    const int kk = kb * TC_BK;
+#pragma unroll
+                    for (int q = 0; q < PARTS; ++q) {
+                        tma_load_2d_pair(sa + q * a_bytes, &mapA, bar, kk, row_a + q * p.lo_rows_a);
+                        if (square) {
+                            tma_load_2d_pair(sb + q * b_bytes, &mapB, bar, kk, (p.kind == NS_GRAM ? p.x_row0 + slot_x : slot_a) + at_b + q * p.lo_rows_b);
+                        } else {  // X across: 64 rows of K, boxes of 64 columns
+                            const int row = p.x_row0 + slot_x + kk + q * p.lo_rows_b;
+#pragma unroll
+                            for (int c = 0; c < BN / 128; ++c) tma_load_2d_pair(sb + q * b_bytes + c * 8192, &mapB, bar, at_b + c * 64, row);
+                        }
+                    }
+                    if (++s == S) { s = 0; ++round; }
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (leader && elect_one()) {
+            // ---- products of the pair
+            int s = 0, round = 0, use = 0;
+            bool ok = true;
+            const uint32_t idesc = make_idesc_f16(256, BN, !square);
+            const uint64_t desc_a = make_smem_desc(smem_u32(smem), 16, 1024), desc_b = make_smem_desc(smem_u32(smem) + PARTS * a_bytes, square ? 16 : 8192, 1024);
+            const uint64_t step_b = square ? 32 >> 4 : 2048 >> 4;
+            for (int t = pair; t < tiles && ok; t += n_pairs) {
+                int rep, ti, tj;
+                const NsMat &mat = g.mat[locate(t, rep, ti, tj)];
+                const int kbs = (p.kind == NS_GRAM ? mat.np : mat.mp) / TC_BK;
+                for (int kb = 0; kb < kbs; ++kb) {
+                    const int b = use & 1;
+                    if ((PARTS == 2 || kb == 0) && use >= 2 && !mbar_wait(smem_u32(&bar_acc_empty[b]), ((use >> 1) & 1) ^ 1, p.wait_ns)) {
+                        atomicExch(p.err, 5);
+                        ok = false;
+                        break;
+                    }
+                    if (!mbar_wait(smem_u32(&bar_full[s]), round & 1, p.wait_ns)) { atomicExch(p.err, 2); ok = false; break; }
+                    tc_fence_after();
+                    const uint64_t da = desc_a + ((s * stage_bytes) >> 4), db = desc_b + ((s * stage_bytes) >> 4);
+                    const uint32_t acc = tmem + b * BN;
+                    if (PARTS == 2) {  // the small terms first, while the sums are small
+#pragma unroll
+                        for (int i = 0; i < TC_BK / TC_UMMA_K; ++i) {
+                            umma_bf16_pair(acc, da + i * 2, db + (b_bytes >> 4) + i * step_b, idesc, i != 0 ? 1u : 0u);
+                            umma_bf16_pair(acc, da + (a_bytes >> 4) + i * 2, db + i * step_b, idesc, 1u);
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < TC_BK / TC_UMMA_K; ++i) umma_bf16_pair(acc, da + i * 2, db + i * step_b, idesc, PARTS == 2 || kb != 0 || i != 0 ? 1u : 0u);
+                    umma_commit_pair(smem_u32(&bar_empty[s]));
+                    if (PARTS == 2 || kb + 1 == kbs) {
+                        umma_commit_pair(smem_u32(&bar_acc_full[b]));
+                        ++use;
+                    }
+                    if (++s == S) { s = 0; ++round; }
+                }
+            }
+        }
+    } else {
+        // ---- results: warp (q, cg) holds rows 32 q .. of this CTA's 128 and columns 64 cg .. of the tile's 256
+        const int q = warp & 3, cg = (warp - 2) >> 2;
+        float *turn = reinterpret_cast<float *>(smem + (size_t)S * stage_bytes) + (warp - 2) * 1024;
+        const int r_sub = lane >> 3, piece = lane & 7;  // after turning: rows 4 i + r_sub, columns 4 piece ..
+        int use = 0;
+        bool ok = true;
+        for (int t = pair; t < tiles && ok; t += n_pairs) {
+            int rep, ti, tj;
+            const int d = locate(t, rep, ti, tj);
+            const NsMat &mat = g.mat[d];
+            const int kbs = (p.kind == NS_GRAM ? mat.np : mat.mp) / TC_BK;
+            const int slot = square ? mat.row_a + rep * mat.mp : mat.row_x + rep * mat.mp;
+            const int width = square ? mat.mp : mat.np;
+            const int row0 = ti * 256 + rank * 128 + q * 32, col0 = tj * BN + cg * 32 * HALVES;
+            const bool live = row0 < mat.mp && col0 < width;  // whole blocks (sizes are padded to multiples of 64)
+            const float inv_r = p.inv_r[mat.index + rep], r2 = inv_r * inv_r;
+            const float f = p.kind == NS_GRAM ? NS_A_SCALE / (NS_X_SCALE * NS_X_SCALE) : p.kind == NS_POLY ? p.c / NS_A_SCALE * r2 * r2 : 1.f / NS_A_SCALE;
+            const float h = p.kind == NS_POLY ? p.b * r2 : p.a;
+            const int pitch = square ? p.pitch_a : p.next.pitch;
+            float v[32];
+            const int chunks = PARTS == 2 ? kbs : 1;
+            for (int c = 0; c < chunks; ++c, ++use) {
+                ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_acc_full[use & 1]), (use >> 1) & 1, p.wait_ns));
+                if (!ok) {
+                    if (lane == 0) atomicExch(p.err, 3);
+                    break;
+                }
+                tc_fence_after();
+                if (PARTS == 2) {
+                    const uint32_t taddr = tmem + ((uint32_t)(q * 32) << 16) + (use & 1) * BN + cg * 32;
+#pragma unroll
+                    for (int o = 0; o < 32; o += 16) {
+                        float r[16];
+                        tmem_ld_32x16(taddr + o, r);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) v[o + i] = c == 0 ? r[i] : v[o + i] + r[i];
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_remote(map_to_cta(smem_u32(&bar_acc_empty[use & 1]), 0));
+                }
+            }
+            if (!ok) break;
+#pragma unroll
+            for (int half = 0; half < HALVES; ++half) {
+                const int col = col0 + half * 32;
+                if (PARTS == 1) {
+                    tmem_ld_32x32(tmem + ((uint32_t)(q * 32) << 16) + ((use - 1) & 1) * BN + cg * 32 * HALVES + half * 32, v);
+                    if (half == HALVES - 1) {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_remote(map_to_cta(smem_u32(&bar_acc_empty[(use - 1) & 1]), 0));
+                    }
+                }
+                if (!live) continue;
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < 8; ++i)  // 16-byte piece i of row `lane` lies at i ^ (lane & 7)
+                    *reinterpret_cast<float4 *>(turn + lane * 32 + ((i ^ (lane & 7)) << 2)) = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                __syncwarp();
+                const bool mirror = square && ti != tj / (256 / BN), tall = p.kind == NS_LAST && mat.tall;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int r = 4 * i + r_sub, row = row0 + r, c = col + 4 * piece;
+                    float4 *place = reinterpret_cast<float4 *>(turn + r * 32 + ((piece ^ (r & 7)) << 2));
+                    const float4 x = *place;
+                    float y[4] = {f * x.x, f * x.y, f * x.z, f * x.w};
+                    const size_t at = (size_t)(slot + row) * pitch + c;
+                    if (p.kind == NS_POLY) {
+                        const __half2 *a2 = reinterpret_cast<const __half2 *>(p.A + at);
+                        float2 a0 = __half22float2(a2[0]), a1 = __half22float2(a2[1]);
+                        if (PARTS == 2) {
+                            const __half2 *l2 = reinterpret_cast<const __half2 *>(p.A + p.lo_off_a + at);
+                            const float2 l0 = __half22float2(l2[0]), l1 = __half22float2(l2[1]);
+                            a0.x += l0.x; a0.y += l0.y; a1.x += l1.x; a1.y += l1.y;
+                        }
+                        y[0] = fmaf(h, a0.x, y[0]); y[1] = fmaf(h, a0.y, y[1]); y[2] = fmaf(h, a1.x, y[2]); y[3] = fmaf(h, a1.y, y[3]);
+                    } else if (!square) {
+                        const float4 a = *reinterpret_cast<const float4 *>(p.X + at);
+                        y[0] = fmaf(h, a.x, y[0]); y[1] = fmaf(h, a.y, y[1]); y[2] = fmaf(h, a.z, y[2]); y[3] = fmaf(h, a.w, y[3]);
+                    }
+                    if (p.kind != NS_LAST) {
+                        if (!square) store_elems<float, 4>(p.next.full + at, y);
+                        __half *o = (square ? p.out : p.next.hi) + at;
+                        const size_t lo = square ? p.lo_off_a : p.next.lo_off;
+                        const __half2 h0 = __floats2half2_rn(y[0], y[1]), h1 = __floats2half2_rn(y[2], y[3]);
+                        *reinterpret_cast<uint2 *>(o) = make_uint2(*reinterpret_cast<const uint32_t *>(&h0), *reinterpret_cast<const uint32_t *>(&h1));
+                        if (PARTS == 2) {
+                            const float2 f0 = __half22float2(h0), f1 = __half22float2(h1);
+                            const __half2 l0 = __floats2half2_rn(y[0] - f0.x, y[1] - f0.y), l1 = __floats2half2_rn(y[2] - f1.x, y[3] - f1.y);
+                            *reinterpret_cast<uint2 *>(o + lo) = make_uint2(*reinterpret_cast<const uint32_t *>(&l0), *reinterpret_cast<const uint32_t *>(&l1));
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) y[j] *= inv_r / NS_X_SCALE;
+                        if (!tall && row < mat.m && c < mat.n) ns_result4(p, mat, rep, row, c, y);
+                    }
+                    if (mirror || tall) *place = make_float4(y[0], y[1], y[2], y[3]);
+                }
+                if (mirror || tall) {  // lane = row: 32 neighbouring elements of every turned row
+                    __syncwarp();
+                    const int row = row0 + lane;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float4 x = *reinterpret_cast<const float4 *>(turn + lane * 32 + ((i ^ (lane & 7)) << 2));
+                        const float y[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const int c = col + 4 * i + j;
+                            if (mirror) {
+                                __half *o = p.out + (size_t)(slot + c) * pitch + row;
+                                const __half hi = __float2half_rn(y[j]);
+                                *o = hi;
+                                if (PARTS == 2) o[p.lo_off_a] = __float2half_rn(y[j] - __half2float(hi));
+                            } else if (row < mat.m && c < mat.n) {
+                                const long long o = mat.dst + rep * mat.dst_stride + (long long)c * mat.ld_dst + row;
+                                if (p.params) ((float *)p.dst)[o] = fmaf(-mat.update, y[j], p.keep * p.params[o]);
+                                else if (p.bf16_dst) ((bf16 *)p.dst)[o] = __float2bfloat16_rn(y[j]);
+                                else ((float *)p.dst)[o] = y[j];
+                            }
+                        }
+                    }
+                }
+                __syncwarp();
+            }
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    cluster_barrier();  // neither CTA frees tensor memory, or leaves with barriers the other may still signal, before both are done
+    if (warp == 0) {
+        __syncwarp();
+        tmem_dealloc_pair(tmem, 2 * BN);
+    }
+}
+
 // ---------------------------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------------------------
-constexpr int NS_SMEM = 200 * 1024;
-
-template <int BN, int PARTS> constexpr int ns_tile_stages()
-{
-    return std::min(8, (NS_SMEM - 1024) / (PARTS * (128 + BN) * TC_BK * 2));
-}
-
 template <int PARTS> constexpr int NSC_SMEM = NSC_STAGES<PARTS> * NSC_STAGE_BYTES<PARTS> + 2 * NSC_SUM_BYTES + 1024;
 
 template <int PARTS, int C> static bool ns_chain_init()
@@ -1216,8 +1285,8 @@ template <int PARTS, int C> static int ns_chain_room()
 static bool ns_init(std::string &err)
 {
     if (!ns_chain_init<1, 1>() || !ns_chain_init<1, 2>() || !ns_chain_init<1, 4>() || !ns_chain_init<2, 1>() || !ns_chain_init<2, 2>() || !ns_chain_init<2, 4>() ||
-        cudaFuncSetAttribute(ns_tile_kernel<128, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, NS_SMEM) != cudaSuccess ||
-        cudaFuncSetAttribute(ns_tile_kernel<128, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, NS_SMEM) != cudaSuccess) {
+        cudaFuncSetAttribute(ns_pair_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, NSP_SMEM<1>) != cudaSuccess ||
+        cudaFuncSetAttribute(ns_pair_kernel<2>, cudaFuncAttributeMaxDynamicSharedMemorySize, NSP_SMEM<2>) != cudaSuccess) {
         err = "cannot raise the dynamic shared memory limit of the Newton-Schulz products";
         return false;
     }
@@ -1302,14 +1371,15 @@ static NsLayout ns_layout(NsGroup &g)
     return l;
 }
 
-// tiles of the products for tiles of 128 x bn; returns the numbers of tiles of A and of X
-static void ns_tiles(NsGroup &g, int bn, int &tiles_a, int &tiles_x)
+// tiles of the products for tiles of bm x bn; `half`: of A only those of the blocks of bm x bm on and above the diagonal.  Returns the
+// numbers of tiles of A and of X
+static void ns_tiles(NsGroup &g, int bm, int bn, bool half, int &tiles_a, int &tiles_x)
 {
     tiles_a = tiles_x = 0;
     for (int d = 0; d < g.count; ++d) {
         NsMat &m = g.mat[d];
-        const int T = (m.mp + 127) / 128;
-        m.tiles_a = T * ((m.mp + bn - 1) / bn);
+        const int T = (m.mp + bm - 1) / bm;
+        m.tiles_a = half ? T * (T + 1) / 2 * (bm / bn) : T * ((m.mp + bn - 1) / bn);
         m.tiles_x = T * ((m.np + bn - 1) / bn);
         m.first_a = tiles_a;
         m.first_x = tiles_x;
@@ -1324,15 +1394,6 @@ struct NsTarget {
     const float *params;
     float keep;
 };
-
-template <int BN, int PARTS>
-static void ns_launch_tile(Exec &ex, int tiles, const CUtensorMap &a, const CUtensorMap &b, NsPhase &p, const NsGroup &g)
-{
-    p.stages = ns_tile_stages<BN, PARTS>();
-    const size_t smem = (size_t)p.stages * PARTS * (128 + BN) * TC_BK * 2 + 1024;
-    launch_dep(ns_tile_kernel<BN, PARTS>, dim3(tiles), dim3(64 + 2 * BN), smem, ex.st, a, b, p, g);
-    ex.launches += 1;
-}
 
 // estimated microseconds of one step of the chain kernel with clusters of C blocks
 static double ns_chain_cost(const NsGroup &g, int parts, int c, int room, int tiles_a, int tiles_x)
@@ -1377,7 +1438,7 @@ static bool ns_run(TcState &tc, Exec &ex, const NsSource &src, NsGroup &g, const
         return false;
     }
     int tiles_a = 0, tiles_x = 0;
-    ns_tiles(g, NSC_BN, tiles_a, tiles_x);
+    ns_tiles(g, 128, NSC_BN, false, tiles_a, tiles_x);
     const int rooms[3] = {ns_chain_room<PARTS, 1>(), ns_chain_room<PARTS, 2>(), ns_chain_room<PARTS, 4>()};
     int best = -1;
     double cost = 1e30;
@@ -1385,7 +1446,7 @@ static bool ns_run(TcState &tc, Exec &ex, const NsSource &src, NsGroup &g, const
         const double t = ns_chain_cost(g, PARTS, 1 << i, rooms[i], tiles_a, tiles_x);
         if (t < cost) { cost = t; best = i; }
     }
-    if (best >= 0 && g.count > 0 && std::max(tiles_a, tiles_x) <= 4 * tc_sm_count()) {
+    if (best >= 0 && g.count > 0 && (getenv("NSC_ON") ? atoi(getenv("NSC_ON")) : std::max(tiles_a, tiles_x) <= 4 * tc_sm_count())) {
         NsChain p{};
         p.parts_rows_x = l.rows_x; p.parts_rows_a = l.rows_a;
         p.steps = steps;
@@ -1422,7 +1483,8 @@ static bool ns_run(TcState &tc, Exec &ex, const NsSource &src, NsGroup &g, const
     launch_dep(ns_norm_kernel, dim3(std::max(1, l.norm_blocks + adam_blocks)), dim3(NS_THREADS), 0, ex.st, src, g, adam, l.norm_blocks, partial);
     ex.launches += 1;
     if (g.count == 0) return true;
-    ns_tiles(g, 128, tiles_a, tiles_x);
+    ns_tiles(g, 256, NSP_BN<PARTS>, true, tiles_a, tiles_x);
+    const int pairs = std::max(1, tc_sm_count() / 2);
     launch_dep(ns_convert_kernel<PARTS>, dim3(l.conv_blocks), dim3(NS_THREADS), 0, ex.st, src, g, partial, eps, X[0], inv_r);
     ex.launches += 1;
     NsPhase p{};
@@ -1437,7 +1499,8 @@ static bool ns_run(TcState &tc, Exec &ex, const NsSource &src, NsGroup &g, const
         p.kind = kind;
         p.extra_tx = tc.overdeclare_tx;
         tc.overdeclare_tx = 0;
-        ns_launch_tile<128, PARTS>(ex, tiles, ma, mb, p, g);
+        launch_dep(ns_pair_kernel<PARTS>, dim3(2 * std::min(tiles, pairs)), dim3(NSP_THREADS), NSP_SMEM<PARTS>, ex.st, ma, mb, p, g, tiles);
+        ex.launches += 1;
     };
     for (int k = 0; k < steps; ++k) {
         const int cur = k & 1;
@@ -1445,10 +1508,10 @@ static bool ns_run(TcState &tc, Exec &ex, const NsSource &src, NsGroup &g, const
         p.lo_rows_a = p.lo_rows_b = l.rows_x;
         p.out = A;
         p.next = X[cur ^ 1];
-        product(NS_GRAM, tiles_a, x128, x128);
+        product(NS_GRAM, tiles_a, x128, PARTS == 2 ? x64 : x128);
         p.lo_rows_a = p.lo_rows_b = l.rows_a;
         p.A = A; p.out = B;
-        product(NS_POLY, tiles_a, a128, a128);
+        product(NS_POLY, tiles_a, a128, PARTS == 2 ? a64 : a128);
         p.lo_rows_b = l.rows_x;
         p.X = X[cur].full;
         product(k + 1 == steps ? NS_LAST : NS_APPLY, tiles_x, b128, x64);
