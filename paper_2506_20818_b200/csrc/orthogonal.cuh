@@ -153,7 +153,27 @@ template <int T> LP_DEVINL void ns_norm_block(const NsSource &s, const NsGroup &
     const long long e0 = (long long)blk * mat.norm_elems, e1 = min(e0 + mat.norm_elems, rows * cols);
     const long long base = mat.src + rep * mat.src_stride;
     double acc = 0.0;
-    constexpr int U = 4;  // elements in flight per thread
+    constexpr int U = 4;  // elements (or runs of four) in flight per thread
+    if (!s.grads && mat.ld_src == cols && ((base + e0) & 3) == 0 && ((uintptr_t)s.u & 15) == 0) {  // dense rows: four neighbours per load
+        for (long long e = e0 + 4 * tid; e < e1; e += U * 4 * T) {
+            float x[U][4];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const long long i = e + u * 4 * T;
+                if (i + 4 <= e1) {
+                    if (s.bf16_u) load_elems<bf16, 4>((const bf16 *)s.u + base + i, x[u]);
+                    else load_elems<float, 4>((const float *)s.u + base + i, x[u]);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) x[u][k] = i + k < e1 ? ns_source(s, base + i + k) : 0.f;
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) acc = fma((double)x[u][k], (double)x[u][k], acc);
+        }
+    } else
     for (long long e = e0 + tid; e < e1; e += U * T) {
         long long at[U];
         float x[U];
@@ -226,14 +246,23 @@ LP_DEVINL void ns_convert_block(const NsSource &s, const NsGroup &g, int t, int 
     const int cb = mat.np / 64;
     const int i0 = (blk / cb) * 64, j0 = (blk % cb) * 64;
     const long long base = mat.src + rep * mat.src_stride;
-    const int lx = tid & 63, ly = tid >> 6;
-    constexpr int R = 4096 / T, STEP = T / 64;  // elements per thread, rows of the tile between them
-    float u[R];
+    // a thread holds R runs of four neighbours in a row of U; tall: U is [n, m], and the tile is turned in shared memory
+    constexpr int R = 1024 / T, STEP = T / 16;
+    const int lx = (tid & 15) * 4, ly = tid >> 4;
+    float u[R][4];
+    const bool wide = !s.grads && (mat.ld_src & 3) == 0 && (base & 3) == 0 && ((uintptr_t)s.u & 15) == 0;
 #pragma unroll
-    for (int k = 0; k < R; ++k) {  // tall: U is [n, m]; its rows are read along i and the tile is turned in shared memory
-        const int y = ly + STEP * k;
-        const int i = mat.tall ? i0 + lx : i0 + y, j = mat.tall ? j0 + y : j0 + lx;
-        u[k] = i < mat.m && j < mat.n ? ns_source(s, base + (mat.tall ? (long long)j * mat.ld_src + i : (long long)i * mat.ld_src + j)) : 0.f;
+    for (int k = 0; k < R; ++k) {
+        const int row = (mat.tall ? j0 : i0) + ly + STEP * k, col = (mat.tall ? i0 : j0) + lx;
+        const int rows = mat.tall ? mat.n : mat.m, cols = mat.tall ? mat.m : mat.n;
+        const long long at = base + (long long)row * mat.ld_src + col;
+        if (wide && row < rows && col + 4 <= cols) {
+            if (s.bf16_u) load_elems<bf16, 4>((const bf16 *)s.u + at, u[k]);
+            else load_elems<float, 4>((const float *)s.u + at, u[k]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) u[k][j] = row < rows && col + j < cols ? ns_source(s, at + j) : 0.f;
+        }
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, o);
@@ -241,7 +270,10 @@ LP_DEVINL void ns_convert_block(const NsSource &s, const NsGroup &g, int t, int 
 #pragma unroll
     for (int k = 0; k < R; ++k) {
         const int y = ly + STEP * k;
-        if (mat.tall) tile[lx * 65 + y] = u[k]; else tile[y * 65 + lx] = u[k];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (mat.tall) tile[(lx + j) * 65 + y] = u[k][j]; else tile[y * 65 + lx + j] = u[k][j];
+        }
     }
     ns_sync<T>();
     acc = 0.0;
@@ -250,17 +282,20 @@ LP_DEVINL void ns_convert_block(const NsSource &s, const NsGroup &g, int t, int 
     double pow2;
     ns_start_scale(sqrt(acc) + eps, r, pow2);
     if (blk == 0 && tid == 0) inv_r[mat.index + rep] = 1.f / r;
-    const int px = (tid & 31) * 2;  // two columns per thread
 #pragma unroll
-    for (int y = tid >> 5; y < 64; y += T / 32) {
-        const float a = (float)(tile[y * 65 + px] * pow2), b = (float)(tile[y * 65 + px + 1] * pow2);
-        const size_t at = (size_t)(mat.row_x + rep * mat.mp + i0 + y) * X.pitch + j0 + px;
-        *reinterpret_cast<float2 *>(X.full + at) = make_float2(a, b);
-        const __half2 h = __floats2half2_rn(a, b);
-        *reinterpret_cast<__half2 *>(X.hi + at) = h;
+    for (int k = 0; k < R; ++k) {
+        const int y = ly + STEP * k;
+        float a[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) a[j] = (float)(tile[y * 65 + lx + j] * pow2);
+        const size_t at = (size_t)(mat.row_x + rep * mat.mp + i0 + y) * X.pitch + j0 + lx;
+        store_elems<float, 4>(X.full + at, a);
+        const __half2 h0 = __floats2half2_rn(a[0], a[1]), h1 = __floats2half2_rn(a[2], a[3]);
+        *reinterpret_cast<uint2 *>(X.hi + at) = make_uint2(*reinterpret_cast<const uint32_t *>(&h0), *reinterpret_cast<const uint32_t *>(&h1));
         if (PARTS == 2) {
-            const float2 f = __half22float2(h);
-            *reinterpret_cast<__half2 *>(X.hi + X.lo_off + at) = __floats2half2_rn(a - f.x, b - f.y);
+            const float2 f0 = __half22float2(h0), f1 = __half22float2(h1);
+            const __half2 l0 = __floats2half2_rn(a[0] - f0.x, a[1] - f0.y), l1 = __floats2half2_rn(a[2] - f1.x, a[3] - f1.y);
+            *reinterpret_cast<uint2 *>(X.hi + X.lo_off + at) = make_uint2(*reinterpret_cast<const uint32_t *>(&l0), *reinterpret_cast<const uint32_t *>(&l1));
         }
     }
     ns_sync<T>();
@@ -918,34 +953,6 @@ __global__ void __launch_bounds__(NSC_THREADS, 1) ns_chain_kernel(const __grid_c
     }
 }
 
-// The matrix instruction of a pair of SMs: 256 rows (128 per CTA), operands FP16
-LP_DEVINL void ns_result4(const NsPhase &p, const NsMat &mat, int rep, int row, int col, const float *v)  // columns col .. col + 3 of row `row`, not tall
-{
-    const long long o = mat.dst + rep * mat.dst_stride + (long long)row * mat.ld_dst + col;
-    if (col + 4 <= mat.n && p.bf16_dst && ((uintptr_t)((bf16 *)p.dst + o) & 7) == 0) {
-        store_elems<bf16, 4>((bf16 *)p.dst + o, v);
-        return;
-    }
-    if (col + 4 <= mat.n && !p.bf16_dst && (((uintptr_t)((float *)p.dst + o) | (uintptr_t)(p.params ? p.params + o : nullptr)) & 15) == 0) {
-        float x[4] = {v[0], v[1], v[2], v[3]};
-        if (p.params) {
-            float old[4];
-            load_elems<float, 4>(p.params + o, old);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = fmaf(-mat.update, v[i], p.keep * old[i]);
-        }
-        store_elems<float, 4>((float *)p.dst + o, x);
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (col + i >= mat.n) break;
-        if (p.params) ((float *)p.dst)[o + i] = fmaf(-mat.update, v[i], p.keep * p.params[o + i]);
-        else if (p.bf16_dst) ((bf16 *)p.dst)[o + i] = __float2bfloat16_rn(v[i]);
-        else ((float *)p.dst)[o + i] = v[i];
-    }
-}
-
 // ---------------------------------------------------------------------------------------------
 // products of large matrices: one launch per product, persistent pairs of SMs (clusters of two CTAs, cta_group::2)
 //
@@ -956,13 +963,13 @@ LP_DEVINL void ns_result4(const NsPhase &p, const NsMat &mat, int rep, int row, 
 // 256 x 256, spill).
 // A and B are symmetric: only tiles on and above the diagonal are computed, the others are written turned.
 //   warp 0 operands, warp 1 matrix instructions (of the pair's first CTA), warps 2-17 results: 32 rows x 64 (32) columns each, turned
-//   through 4 KiB of shared memory per warp so that rows are written in pieces of 128 bytes
+//   through 2 KiB of shared memory per warp, 16 columns at a time, so that rows are written in pieces of 64 bytes
 // ---------------------------------------------------------------------------------------------
 constexpr int NSP_THREADS = 576;
 template <int PARTS> constexpr int NSP_BN = PARTS == 2 ? 128 : 256;
-template <int PARTS> constexpr int NSP_STAGES = PARTS == 2 ? 3 : 5;
+template <int PARTS> constexpr int NSP_STAGES = PARTS == 2 ? 4 : 6;  // 192 KiB in flight (4096 x 4096 with 96, 128, 160 KiB: 1.48, 1.37, 1.32 ms)
 template <int PARTS> constexpr int NSP_STAGE_BYTES = PARTS * (128 + NSP_BN<PARTS> / 2) * TC_BK * 2;
-constexpr int NSP_TURN_BYTES = 16 * 4096;
+constexpr int NSP_TURN_BYTES = 16 * 2048;
 template <int PARTS> constexpr int NSP_SMEM = NSP_STAGES<PARTS> * NSP_STAGE_BYTES<PARTS> + NSP_TURN_BYTES + 1024;
 
 // tile t of the upper triangle (rows i <= columns j) of a T x T grid, row by row
@@ -971,6 +978,14 @@ LP_DEVINL void ns_triangle(int t, int T, int &i, int &j)
     i = 0;
     while (t >= T - i) { t -= T - i; ++i; }
     j = i + t;
+}
+
+// one element of the result
+LP_DEVINL void ns_result(const NsPhase &p, const NsMat &mat, long long o, float v)
+{
+    if (p.params) ((float *)p.dst)[o] = fmaf(-mat.update, v, p.keep * p.params[o]);
+    else if (p.bf16_dst) ((bf16 *)p.dst)[o] = __float2bfloat16_rn(v);
+    else ((float *)p.dst)[o] = v;
 }
 
 template <int PARTS>
@@ -982,7 +997,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NSP_THREADS, 1)
     constexpr int S = NSP_STAGES<PARTS>;
     __shared__ __align__(8) uint64_t bar_full[S], bar_empty[S], bar_acc_full[2], bar_acc_empty[2];
     __shared__ uint32_t tmem_base_s;
-    constexpr int BN = NSP_BN<PARTS>, HALVES = BN / 128;  // HALVES: blocks of 32 columns per thread
+    constexpr int BN = NSP_BN<PARTS>, COLS = BN / 4;  // COLS: columns of a warp
     constexpr uint32_t a_bytes = 128 * TC_BK * 2, b_bytes = BN / 2 * TC_BK * 2, stage_bytes = NSP_STAGE_BYTES<PARTS>;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const int rank = (int)cluster_cta_rank();
@@ -1107,8 +1122,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NSP_THREADS, 1)
     } else {
         // ---- results: warp (q, cg) holds rows 32 q .. of this CTA's 128 and columns 64 cg .. of the tile's 256
         const int q = warp & 3, cg = (warp - 2) >> 2;
-        float *turn = reinterpret_cast<float *>(smem + (size_t)S * stage_bytes) + (warp - 2) * 1024;
-        const int r_sub = lane >> 3, piece = lane & 7;  // after turning: rows 4 i + r_sub, columns 4 piece ..
+        float *turn = reinterpret_cast<float *>(smem + (size_t)S * stage_bytes) + (warp - 2) * 512;
+        const int r_sub = lane >> 2, piece = lane & 3;  // after turning: rows 8 i + r_sub, columns 4 piece ..
         int use = 0;
         bool ok = true;
         for (int t = pair; t < tiles && ok; t += n_pairs) {
@@ -1118,13 +1133,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NSP_THREADS, 1)
             const int kbs = (p.kind == NS_GRAM ? mat.np : mat.mp) / TC_BK;
             const int slot = square ? mat.row_a + rep * mat.mp : mat.row_x + rep * mat.mp;
             const int width = square ? mat.mp : mat.np;
-            const int row0 = ti * 256 + rank * 128 + q * 32, col0 = tj * BN + cg * 32 * HALVES;
+            const int row0 = ti * 256 + rank * 128 + q * 32, col0 = tj * BN + cg * COLS;
             const bool live = row0 < mat.mp && col0 < width;  // whole blocks (sizes are padded to multiples of 64)
             const float inv_r = p.inv_r[mat.index + rep], r2 = inv_r * inv_r;
             const float f = p.kind == NS_GRAM ? NS_A_SCALE / (NS_X_SCALE * NS_X_SCALE) : p.kind == NS_POLY ? p.c / NS_A_SCALE * r2 * r2 : 1.f / NS_A_SCALE;
             const float h = p.kind == NS_POLY ? p.b * r2 : p.a;
             const int pitch = square ? p.pitch_a : p.next.pitch;
-            float v[32];
+            float v[PARTS == 2 ? COLS : 16];
             const int chunks = PARTS == 2 ? kbs : 1;
             for (int c = 0; c < chunks; ++c, ++use) {
                 ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_acc_full[use & 1]), (use >> 1) & 1, p.wait_ns));
@@ -1148,12 +1163,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NSP_THREADS, 1)
                 }
             }
             if (!ok) break;
+            const bool mirror = square && ti != tj / (256 / BN), last = p.kind == NS_LAST;
 #pragma unroll
-            for (int half = 0; half < HALVES; ++half) {
-                const int col = col0 + half * 32;
+            for (int blk = 0; blk < COLS / 16; ++blk) {
+                const int col = col0 + blk * 16;
                 if (PARTS == 1) {
-                    tmem_ld_32x32(tmem + ((uint32_t)(q * 32) << 16) + ((use - 1) & 1) * BN + cg * 32 * HALVES + half * 32, v);
-                    if (half == HALVES - 1) {
+                    tmem_ld_32x16(tmem + ((uint32_t)(q * 32) << 16) + ((use - 1) & 1) * BN + cg * COLS + blk * 16, v);
+                    if (blk == COLS / 16 - 1) {
                         tc_fence_before();
                         __syncwarp();
                         if (lane == 0) mbar_arrive_remote(map_to_cta(smem_u32(&bar_acc_empty[(use - 1) & 1]), 0));
@@ -1161,15 +1177,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NSP_THREADS, 1)
                 }
                 if (!live) continue;
                 __syncwarp();
+                const float *w = v + (PARTS == 2 ? blk * 16 : 0);
 #pragma unroll
-                for (int i = 0; i < 8; ++i)  // 16-byte piece i of row `lane` lies at i ^ (lane & 7)
-                    *reinterpret_cast<float4 *>(turn + lane * 32 + ((i ^ (lane & 7)) << 2)) = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                for (int i = 0; i < 4; ++i)  // 16-byte piece i of row `lane` lies at i ^ (lane / 2 mod 4)
+                    *reinterpret_cast<float4 *>(turn + lane * 16 + ((i ^ ((lane >> 1) & 3)) << 2)) = make_float4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
                 __syncwarp();
-                const bool mirror = square && ti != tj / (256 / BN), tall = p.kind == NS_LAST && mat.tall;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int r = 4 * i + r_sub, row = row0 + r, c = col + 4 * piece;
-                    float4 *place = reinterpret_cast<float4 *>(turn + r * 32 + ((piece ^ (r & 7)) << 2));
+                for (int i = 0; i < 4; ++i) {
+                    const int r = 8 * i + r_sub, row = row0 + r, c = col + 4 * piece;
+                    float4 *place = reinterpret_cast<float4 *>(turn + r * 16 + ((piece ^ ((r >> 1) & 3)) << 2));
                     const float4 x = *place;
                     float y[4] = {f * x.x, f * x.y, f * x.z, f * x.w};
                     const size_t at = (size_t)(slot + row) * pitch + c;
@@ -1186,7 +1202,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NSP_THREADS, 1)
                         const float4 a = *reinterpret_cast<const float4 *>(p.X + at);
                         y[0] = fmaf(h, a.x, y[0]); y[1] = fmaf(h, a.y, y[1]); y[2] = fmaf(h, a.z, y[2]); y[3] = fmaf(h, a.w, y[3]);
                     }
-                    if (p.kind != NS_LAST) {
+                    if (!last) {
                         if (!square) store_elems<float, 4>(p.next.full + at, y);
                         __half *o = (square ? p.out : p.next.hi) + at;
                         const size_t lo = square ? p.lo_off_a : p.next.lo_off;
@@ -1197,19 +1213,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NSP_THREADS, 1)
                             const __half2 l0 = __floats2half2_rn(y[0] - f0.x, y[1] - f0.y), l1 = __floats2half2_rn(y[2] - f1.x, y[3] - f1.y);
                             *reinterpret_cast<uint2 *>(o + lo) = make_uint2(*reinterpret_cast<const uint32_t *>(&l0), *reinterpret_cast<const uint32_t *>(&l1));
                         }
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) y[j] *= inv_r / NS_X_SCALE;
-                        if (!tall && row < mat.m && c < mat.n) ns_result4(p, mat, rep, row, c, y);
                     }
-                    if (mirror || tall) *place = make_float4(y[0], y[1], y[2], y[3]);
+                    if (mirror || last) *place = make_float4(y[0], y[1], y[2], y[3]);
                 }
-                if (mirror || tall) {  // lane = row: 32 neighbouring elements of every turned row
+                if (mirror || (last && mat.tall)) {  // lane = row: 32 neighbouring elements of every turned row
                     __syncwarp();
                     const int row = row0 + lane;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float4 x = *reinterpret_cast<const float4 *>(turn + lane * 32 + ((i ^ (lane & 7)) << 2));
+                    for (int i = 0; i < 4; ++i) {
+                        const float4 x = *reinterpret_cast<const float4 *>(turn + lane * 16 + ((i ^ ((lane >> 1) & 3)) << 2));
                         const float y[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
@@ -1220,12 +1232,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NSP_THREADS, 1)
                                 *o = hi;
                                 if (PARTS == 2) o[p.lo_off_a] = __float2half_rn(y[j] - __half2float(hi));
                             } else if (row < mat.m && c < mat.n) {
-                                const long long o = mat.dst + rep * mat.dst_stride + (long long)c * mat.ld_dst + row;
-                                if (p.params) ((float *)p.dst)[o] = fmaf(-mat.update, y[j], p.keep * p.params[o]);
-                                else if (p.bf16_dst) ((bf16 *)p.dst)[o] = __float2bfloat16_rn(y[j]);
-                                else ((float *)p.dst)[o] = y[j];
+                                ns_result(p, mat, mat.dst + rep * mat.dst_stride + (long long)c * mat.ld_dst + row, y[j] * (inv_r / NS_X_SCALE));
                             }
                         }
+                    }
+                } else if (last) {  // lane = column, two rows at a time
+                    __syncwarp();
+                    const int c = col + (lane & 15);
+#pragma unroll 8
+                    for (int i = 0; i < 16; ++i) {
+                        const int r = 2 * i + (lane >> 4), row = row0 + r;
+                        const float y = turn[r * 16 + ((((lane & 15) >> 2) ^ ((r >> 1) & 3)) << 2) + (lane & 3)];
+                        if (row < mat.m && c < mat.n) ns_result(p, mat, mat.dst + rep * mat.dst_stride + (long long)row * mat.ld_dst + c, y * (inv_r / NS_X_SCALE));
                     }
                 }
                 __syncwarp();
