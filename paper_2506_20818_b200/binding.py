@@ -139,6 +139,8 @@ class Context:
         self.h = h
         self.n = self.nnz = self.f = 0
         self.n_params = 0
+        self._precs = {torch.float32: LP_FP32, torch.bfloat16: LP_BF16}
+        self._raw_stream = self.stream.cuda_stream
         self.desc: Optional[ModelDesc] = None
 
     def close(self):
@@ -285,36 +287,35 @@ class Context:
                                        C.c_int64(k), C.byref(out)))
         return float(out.value)
 
-    # ---- learned node features
+    # ---- learned node features (the checks are written for speed: a small call takes longer to make than to run)
     def _refuse(self, message: str):
         raise LpError(-1, message)
 
     def _prec(self, dtype, who: str) -> int:
-        if dtype == self._torch.float32:
-            return LP_FP32
-        if dtype == self._torch.bfloat16:
-            return LP_BF16
-        self._refuse(f"{who}: float32 or bfloat16 expected, got {dtype}")
+        p = self._precs.get(dtype)
+        if p is None:
+            self._refuse(f"{who}: float32 or bfloat16 expected, got {dtype}")
+        return p
 
     def _rows(self, x, who: str):
-        """Row pitch of a CUDA matrix whose rows are contiguous."""
-        if not x.is_cuda or x.device.index != self.device:
-            self._refuse(f"{who}: expected a tensor on cuda:{self.device}")
-        if x.dim() != 2:
-            self._refuse(f"{who}: expected a matrix, got {x.dim()} dimensions")
-        if x.shape[1] > 1 and x.stride(1) != 1:
+        """(rows, width, row pitch) of a CUDA matrix whose rows are contiguous."""
+        if x.get_device() != self.device or x.dim() != 2:
+            self._refuse(f"{who}: expected a matrix on cuda:{self.device}")
+        rows, width = x.shape
+        ld, step = x.stride()
+        if step != 1 and width > 1:
             self._refuse(f"{who}: the elements of a row must be contiguous")
-        return x.stride(0) if x.shape[0] > 1 else max(x.shape[1], x.stride(0))
+        return rows, width, ld if rows > 1 or ld > width else width
 
     def _ids(self, ids, who: str):
-        if not ids.is_cuda or ids.device.index != self.device or ids.dtype != self._torch.int32 or not ids.is_contiguous():
+        if ids.dtype is not self._torch.int32 or ids.get_device() != self.device or not ids.is_contiguous():
             self._refuse(f"{who}: ids must be a contiguous int32 tensor on cuda:{self.device}")
 
     def _enter(self, *tensors):
         """Work goes to the context's stream.  Called from another current stream, it waits for what that stream has
         enqueued so far, and the tensors are kept from reuse until it is done; returns the stream to hand back to."""
         t = self._torch
-        if t._C._cuda_getCurrentRawStream(self.device) == self.stream.cuda_stream:
+        if t._C._cuda_getCurrentRawStream(self.device) == self._raw_stream:
             return None
         cur = t.cuda.current_stream(self.device)
         self.stream.wait_stream(cur)
@@ -329,47 +330,49 @@ class Context:
 
     def embed(self, table, ids, scale: float = 1.0, padding_id: Optional[int] = None, out_dtype=None, out=None):
         """scale * table[ids] (ids int32, any shape; rows of zeros for padding_id); see lp_embed."""
-        t = self._torch
         self._ids(ids, "embed")
-        ldt = self._rows(table, "embed: table")
-        V, D = table.shape
+        V, D, ldt = self._rows(table, "embed: table")
         N = ids.numel()
         if out is None:
-            out = t.empty((*ids.shape, D), dtype=out_dtype or table.dtype, device=table.device)
+            shape = (N, D) if ids.dim() == 1 else (*ids.shape, D)
+            out = table.new_empty(shape) if out_dtype is None else table.new_empty(shape, dtype=out_dtype)
             ldo = D
         else:
-            if tuple(out.shape) != (N, D) or (out_dtype is not None and out.dtype != out_dtype):
+            n, d, ldo = self._rows(out, "embed: out")
+            if n != N or d != D or (out_dtype is not None and out.dtype != out_dtype):
                 self._refuse(f"embed: out must be [{N}, {D}] of the requested type")
-            ldo = self._rows(out, "embed: out")
         cur = self._enter(table, ids, out)
-        self._ck(self.lib.lp_embed(self.h, self._prec(table.dtype, "embed: table"), table.data_ptr(), V, D, ldt, ids.data_ptr(), N,
-                                   LP_NO_PADDING if padding_id is None else padding_id, scale, self._prec(out.dtype, "embed: out"), out.data_ptr(),
-                                   ldo))
-        self._leave(cur)
+        rc = self.lib.lp_embed(self.h, self._prec(table.dtype, "embed: table"), table.data_ptr(), V, D, ldt, ids.data_ptr(), N,
+                               LP_NO_PADDING if padding_id is None else padding_id, scale, self._prec(out.dtype, "embed: out"), out.data_ptr(), ldo)
+        if rc:
+            self._ck(rc)
+        if cur is not None:
+            self._leave(cur)
         return out
 
     def embed_grad(self, dout, ids, rows: int, scale: float = 1.0, padding_id: Optional[int] = None, grad=None, grad_dtype=None, accumulate: bool = False):
         """Gradient [rows, width] of the table of embed(); see lp_embed_grad.  accumulate adds to `grad`."""
-        t = self._torch
         self._ids(ids, "embed_grad")
-        ldd = self._rows(dout, "embed_grad: dout")
-        N, D = dout.shape
+        N, D, ldd = self._rows(dout, "embed_grad: dout")
         if ids.numel() != N:
             self._refuse(f"embed_grad: {ids.numel()} ids for {N} rows of dout")
         if grad is None:
             if accumulate:
                 self._refuse("embed_grad: accumulate needs a gradient to add to")
-            grad = t.empty((rows, D), dtype=grad_dtype or t.float32, device=dout.device)
+            grad = dout.new_empty((rows, D), dtype=grad_dtype or self._torch.float32)
             ldg = D
         else:
-            if tuple(grad.shape) != (rows, D) or (grad_dtype is not None and grad.dtype != grad_dtype):
+            n, d, ldg = self._rows(grad, "embed_grad: grad")
+            if n != rows or d != D or (grad_dtype is not None and grad.dtype != grad_dtype):
                 self._refuse(f"embed_grad: grad must be [{rows}, {D}] of the requested type")
-            ldg = self._rows(grad, "embed_grad: grad")
         cur = self._enter(dout, ids, grad)
-        self._ck(self.lib.lp_embed_grad(self.h, self._prec(dout.dtype, "embed_grad: dout"), dout.data_ptr(), ldd, ids.data_ptr(), N,
-                                        LP_NO_PADDING if padding_id is None else padding_id, scale, rows, D, self._prec(grad.dtype, "embed_grad: grad"),
-                                        grad.data_ptr(), ldg, int(accumulate)))
-        self._leave(cur)
+        rc = self.lib.lp_embed_grad(self.h, self._prec(dout.dtype, "embed_grad: dout"), dout.data_ptr(), ldd, ids.data_ptr(), N,
+                                    LP_NO_PADDING if padding_id is None else padding_id, scale, rows, D, self._prec(grad.dtype, "embed_grad: grad"),
+                                    grad.data_ptr(), ldg, accumulate)
+        if rc:
+            self._ck(rc)
+        if cur is not None:
+            self._leave(cur)
         return grad
 
     # ---- orthogonalised updates

@@ -407,15 +407,21 @@ template <int PARTS> constexpr int NSC_ACC_COLS = PARTS * NSC_BN;  // PARTS = 2:
 constexpr int NSC_SUM_BYTES = 128 * NSC_BN * 4;  // the sums of a tile
 constexpr int NSC_BARRIERS = 256;  // counters of one call: 2 + 3 * steps are used
 
+struct NsChainIo {       // of one kind of phase; the addend has the rows, columns and pitch of the output
+    const __half *add_h;   // B: A (parts out_lo apart)
+    const float *add_f;    // new X: X
+    __half *out_h;         // operands of a later phase
+    float *out_f;          // new X in FP32
+    long long out_lo;      // elements between the parts of out_h
+    int pitch;
+};
 struct NsChain {
+    NsChainIo io[2][3];                  // [step parity][kind], read from constant memory where needed: pointers held in registers spill
     int parts_rows_x, parts_rows_a;      // rows between the hi and lo parts of X and of A, B
     int steps;
     float a, b, c;
     double eps;
-    NsX X[2];
-    __half *A, *B;
-    int pitch_a;
-    size_t lo_off_a;
+    NsX X0;
     double *partial;
     float *inv_r;
     int norm_blocks, adam_blocks, conv_blocks, tiles_a, tiles_x;
@@ -613,7 +619,7 @@ LP_DEVINL void ns_chain_norm(const NsSource &src, const NsGroup &g, const NsAdam
 }
 template <int PARTS> LP_DEVINL void ns_chain_convert(const NsSource &src, const NsGroup &g, const NsChain &p, int tid, float *tile, double *sw)
 {
-    for (int t = blockIdx.x; t < p.conv_blocks; t += gridDim.x) ns_convert_block<PARTS, NSC_WORKERS>(src, g, t, tid, p.partial, p.eps, p.X[0], p.inv_r, tile, sw);
+    for (int t = blockIdx.x; t < p.conv_blocks; t += gridDim.x) ns_convert_block<PARTS, NSC_WORKERS>(src, g, t, tid, p.partial, p.eps, p.X0, p.inv_r, tile, sw);
 }
 
 template <int PARTS, int C>
@@ -788,19 +794,13 @@ __global__ void __launch_bounds__(NSC_THREADS, 1) ns_chain_kernel(const __grid_c
         const int q = warp & 3, quarter = (warp - 2) >> 2;  // the 32 rows that the warp may read from tensor memory, and its 16 columns
         int use = 0, tiles_done = 0;
         for (int k = 0; k < p.steps && ok; ++k) {
-            const NsX &cur = p.X[k & 1], &next = p.X[(k & 1) ^ 1];
             for (int kind_ = NS_GRAM; kind_ <= NS_APPLY && ok; ++kind_) {
                 const int phase = 2 + 3 * k + kind_;
                 const int kind = kind_ == NS_APPLY && k + 1 == p.steps ? NS_LAST : kind_;
                 const bool square = kind == NS_GRAM || kind == NS_POLY;
                 ok = await(phase - 1);
                 const int tiles = kind_ == NS_APPLY ? p.tiles_x : p.tiles_a;
-                // where the addend is read and the operands of the next phase are written: same rows, columns and pitch
-                const __half *add_h = p.A;
-                const float *add_f = cur.full;
-                __half *out_h = kind == NS_GRAM ? p.A : kind == NS_POLY ? p.B : next.hi;
-                const size_t out_lo = square ? p.lo_off_a : next.lo_off;
-                const int pitch = square ? p.pitch_a : next.pitch;
+                const NsChainIo &io = p.io[k & 1][kind_];
                 int nth = 0;
                 for (int t = cluster; t < tiles && ok; t += n_clusters, ++nth) {
                     if (nth >= NSC_KEPT) {
@@ -814,23 +814,29 @@ __global__ void __launch_bounds__(NSC_THREADS, 1) ns_chain_kernel(const __grid_c
                     // this block finishes 64 / C columns of the tile; a thread takes GPT groups of eight, neighbours along the rows
                     constexpr int GPR = 8 / C, GPT = C == 1 ? 2 : 1;  // groups per row, per thread (C = 4: half of the threads have none)
                     float add[GPT][8];
+                    auto fetch = [&]() {
 #pragma unroll
-                    for (int i = 0; i < GPT; ++i) {
-                        const int e = i * NSC_WORKERS + tid, row = tl.ti * 128 + e / GPR, col = tl.tj * NSC_BN + rank * (NSC_BN / C) + 8 * (e % GPR);
+                        for (int i = 0; i < GPT; ++i) {
+                            const int e = i * NSC_WORKERS + tid, row = tl.ti * 128 + e / GPR, col = tl.tj * NSC_BN + rank * (NSC_BN / C) + 8 * (e % GPR);
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) add[i][j] = 0.f;
-                        if (e < 128 * GPR && row < tl.mp && col < width) {
-                            const size_t at = (size_t)(slot + row) * pitch + col;
-                            if (kind == NS_POLY) {
-                                ns_add8(__ldcg(reinterpret_cast<const uint4 *>(add_h + at)), add[i]);
-                                if (PARTS == 2) ns_add8(__ldcg(reinterpret_cast<const uint4 *>(add_h + p.lo_off_a + at)), add[i]);
-                            } else if (!square) {
-                                const float4 x = __ldcg(reinterpret_cast<const float4 *>(add_f + at)), y = __ldcg(reinterpret_cast<const float4 *>(add_f + at) + 1);
-                                add[i][0] = x.x; add[i][1] = x.y; add[i][2] = x.z; add[i][3] = x.w;
-                                add[i][4] = y.x; add[i][5] = y.y; add[i][6] = y.z; add[i][7] = y.w;
+                            for (int j = 0; j < 8; ++j) add[i][j] = 0.f;
+                            if (e < 128 * GPR && row < tl.mp && col < width) {
+                                const size_t at = (size_t)(slot + row) * io.pitch + col;
+                                if (kind == NS_POLY) {
+                                    ns_add8(__ldcg(reinterpret_cast<const uint4 *>(io.add_h + at)), add[i]);
+                                    if (PARTS == 2) ns_add8(__ldcg(reinterpret_cast<const uint4 *>(io.add_h + io.out_lo + at)), add[i]);
+                                } else if (!square) {
+                                    const float4 x = __ldcg(reinterpret_cast<const float4 *>(io.add_f + at)), y = __ldcg(reinterpret_cast<const float4 *>(io.add_f + at) + 1);
+                                    add[i][0] = x.x; add[i][1] = x.y; add[i][2] = x.z; add[i][3] = x.w;
+                                    add[i][4] = y.x; add[i][5] = y.y; add[i][6] = y.z; add[i][7] = y.w;
+                                }
                             }
                         }
-                    }
+                    };
+                    // requested before the products are waited for, unless that makes registers spill: a spilled value costs more
+                    // than the wait, because every phase empties L1
+                    constexpr bool EARLY = PARTS == 1 || C == 4;
+                    if (EARLY) fetch();
                     float v[16], lost[16];  // running sums and what their roundings lost
 #pragma unroll
                     for (int i = 0; i < 16; ++i) v[i] = lost[i] = 0.f;
@@ -845,7 +851,8 @@ __global__ void __launch_bounds__(NSC_THREADS, 1) ns_chain_kernel(const __grid_c
                         }
                         tc_fence_after();
                         const uint32_t taddr = tmem + ((uint32_t)(q * 32) << 16) + b * NSC_ACC_COLS<PARTS> + quarter * 16;
-                        if (PARTS == 1) {  // one chunk
+                        if (tl.ti * 128 + q * 32 >= tl.mp) {  // rows behind the matrix
+                        } else if (PARTS == 1) {  // one chunk
                             tmem_ld_32x16(taddr, v);
                         } else {
 #pragma unroll
@@ -886,6 +893,7 @@ __global__ void __launch_bounds__(NSC_THREADS, 1) ns_chain_kernel(const __grid_c
                             *reinterpret_cast<float4 *>(theirs + row_t * NSC_BN + ((within ^ (row_t & (PIECES - 1))) << 2)) =
                                 make_float4(lost[4 * i], lost[4 * i + 1], lost[4 * i + 2], lost[4 * i + 3]);
                     }
+                    if (!EARLY) fetch();
                     if (C > 1) fence_async_proxy();
                     ok = !ns_any<NSC_WORKERS>(failed);  // all sixteen warps go on or all leave
                     if (!ok) break;
@@ -920,14 +928,14 @@ __global__ void __launch_bounds__(NSC_THREADS, 1) ns_chain_kernel(const __grid_c
                             }
                         }
                         if (row >= tl.mp || col >= width) continue;
-                        const size_t at = (size_t)(slot + row) * pitch + col;
+                        const size_t at = (size_t)(slot + row) * io.pitch + col;
 #pragma unroll
                         for (int j = 0; j < 8; ++j) sum[j] = fmaf(f, off[j], fmaf(h, add[i][j], f * sum[j]));  // f is a power of two where precision counts
                         if (kind != NS_LAST) {
-                            ns_store8<PARTS>(sum, out_h + at, out_lo);
+                            ns_store8<PARTS>(sum, io.out_h + at, io.out_lo);
                             if (!square) {
-                                store_elems<float, 4>(next.full + at, sum);
-                                store_elems<float, 4>(next.full + at + 4, sum + 4);
+                                store_elems<float, 4>(io.out_f + at, sum);
+                                store_elems<float, 4>(io.out_f + at + 4, sum + 4);
                             }
                         } else if (row < tl.m && col < tl.n) {
                             ns_result8(p, g.mat[tl.d], tl.rep, row, col, make_float4(sum[0], sum[1], sum[2], sum[3]), make_float4(sum[4], sum[5], sum[6], sum[7]),
@@ -1140,6 +1148,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NSP_THREADS, 1)
             const float h = p.kind == NS_POLY ? p.b * r2 : p.a;
             const int pitch = square ? p.pitch_a : p.next.pitch;
             float v[PARTS == 2 ? COLS : 16];
+            // the addends of 16 columns, as they lie in memory (POLY: 4 + 4 FP16, else 4 FP32), one block of columns ahead of their use
+            uint4 ahead[2][4];
+            auto fetch = [&](int blk) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const size_t at = (size_t)(slot + row0 + 8 * i + r_sub) * pitch + col0 + blk * 16 + 4 * piece;
+                    if (p.kind == NS_POLY) {
+                        const uint2 hi = *reinterpret_cast<const uint2 *>(p.A + at);
+                        const uint2 lo = PARTS == 2 ? *reinterpret_cast<const uint2 *>(p.A + p.lo_off_a + at) : make_uint2(0u, 0u);
+                        ahead[blk & 1][i] = make_uint4(hi.x, hi.y, lo.x, lo.y);
+                    } else if (!square) {
+                        ahead[blk & 1][i] = *reinterpret_cast<const uint4 *>(p.X + at);
+                    }
+                }
+            };
+            if (live && PARTS == 1) fetch(0);
             const int chunks = PARTS == 2 ? kbs : 1;
             for (int c = 0; c < chunks; ++c, ++use) {
                 ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_acc_full[use & 1]), (use >> 1) & 1, p.wait_ns));
@@ -1164,6 +1188,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NSP_THREADS, 1)
             }
             if (!ok) break;
             const bool mirror = square && ti != tj / (256 / BN), last = p.kind == NS_LAST;
+            if (live && PARTS == 2) fetch(0);
 #pragma unroll
             for (int blk = 0; blk < COLS / 16; ++blk) {
                 const int col = col0 + blk * 16;
@@ -1176,6 +1201,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NSP_THREADS, 1)
                     }
                 }
                 if (!live) continue;
+                if (blk + 1 < COLS / 16) fetch(blk + 1);
                 __syncwarp();
                 const float *w = v + (PARTS == 2 ? blk * 16 : 0);
 #pragma unroll
@@ -1189,18 +1215,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NSP_THREADS, 1)
                     const float4 x = *place;
                     float y[4] = {f * x.x, f * x.y, f * x.z, f * x.w};
                     const size_t at = (size_t)(slot + row) * pitch + c;
+                    const uint4 ad = ahead[blk & 1][i];
                     if (p.kind == NS_POLY) {
-                        const __half2 *a2 = reinterpret_cast<const __half2 *>(p.A + at);
-                        float2 a0 = __half22float2(a2[0]), a1 = __half22float2(a2[1]);
+                        float2 a0 = __half22float2(*reinterpret_cast<const __half2 *>(&ad.x)), a1 = __half22float2(*reinterpret_cast<const __half2 *>(&ad.y));
                         if (PARTS == 2) {
-                            const __half2 *l2 = reinterpret_cast<const __half2 *>(p.A + p.lo_off_a + at);
-                            const float2 l0 = __half22float2(l2[0]), l1 = __half22float2(l2[1]);
+                            const float2 l0 = __half22float2(*reinterpret_cast<const __half2 *>(&ad.z)), l1 = __half22float2(*reinterpret_cast<const __half2 *>(&ad.w));
                             a0.x += l0.x; a0.y += l0.y; a1.x += l1.x; a1.y += l1.y;
                         }
                         y[0] = fmaf(h, a0.x, y[0]); y[1] = fmaf(h, a0.y, y[1]); y[2] = fmaf(h, a1.x, y[2]); y[3] = fmaf(h, a1.y, y[3]);
                     } else if (!square) {
-                        const float4 a = *reinterpret_cast<const float4 *>(p.X + at);
-                        y[0] = fmaf(h, a.x, y[0]); y[1] = fmaf(h, a.y, y[1]); y[2] = fmaf(h, a.z, y[2]); y[3] = fmaf(h, a.w, y[3]);
+                        y[0] = fmaf(h, __uint_as_float(ad.x), y[0]); y[1] = fmaf(h, __uint_as_float(ad.y), y[1]);
+                        y[2] = fmaf(h, __uint_as_float(ad.z), y[2]); y[3] = fmaf(h, __uint_as_float(ad.w), y[3]);
                     }
                     if (!last) {
                         if (!square) store_elems<float, 4>(p.next.full + at, y);
@@ -1216,34 +1241,71 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NSP_THREADS, 1)
                     }
                     if (mirror || last) *place = make_float4(y[0], y[1], y[2], y[3]);
                 }
-                if (mirror || (last && mat.tall)) {  // lane = row: 32 neighbouring elements of every turned row
+                if (mirror) {  // lane = turned row and eight of its elements: stores of 16 bits cost as much as stores of 16 bytes
+                    __syncwarp();
+                    const int c = lane & 15;
+#pragma unroll
+                    for (int it = 0; it < 2; ++it) {
+                        const int r0 = 8 * ((lane >> 4) + 2 * it);
+                        float y[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) y[j] = turn[(r0 + j) * 16 + ((((c >> 2) ^ (j >> 1)) & 3) << 2) + (c & 3)];
+                        ns_store8<PARTS>(y, p.out + (size_t)(slot + col + c) * pitch + row0 + r0, p.lo_off_a);
+                    }
+                } else if (last && mat.tall) {  // lane = row: 32 neighbouring elements of every turned row
                     __syncwarp();
                     const int row = row0 + lane;
+                    const bool odd = (lane & 1) != 0;
+                    // BF16 in pairs where they are aligned: of two columns, the lane of the even row takes the first for both rows, the
+                    // lane of the odd row the second
+                    const bool pairs = p.bf16_dst && ((mat.dst + rep * mat.dst_stride) & 1) == 0 && (mat.ld_dst & 1) == 0 && ((uintptr_t)p.dst & 3) == 0;
+                    const float scale = inv_r / NS_X_SCALE;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const float4 x = *reinterpret_cast<const float4 *>(turn + lane * 16 + ((i ^ ((lane >> 1) & 3)) << 2));
-                        const float y[4] = {x.x, x.y, x.z, x.w};
+                        const float y[4] = {x.x * scale, x.y * scale, x.z * scale, x.w * scale};
+                        if (pairs) {
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const int c = col + 4 * i + j;
-                            if (mirror) {
-                                __half *o = p.out + (size_t)(slot + c) * pitch + row;
-                                const __half hi = __float2half_rn(y[j]);
-                                *o = hi;
-                                if (PARTS == 2) o[p.lo_off_a] = __float2half_rn(y[j] - __half2float(hi));
-                            } else if (row < mat.m && c < mat.n) {
-                                ns_result(p, mat, mat.dst + rep * mat.dst_stride + (long long)c * mat.ld_dst + row, y[j] * (inv_r / NS_X_SCALE));
+                            for (int j = 0; j < 4; j += 2) {
+                                const float got = __shfl_xor_sync(0xffffffffu, odd ? y[j] : y[j + 1], 1);
+                                const float lo = odd ? got : y[j], hi = odd ? y[j + 1] : got;  // rows row & ~1 and row | 1
+                                const int c = col + 4 * i + j + (odd ? 1 : 0), even = row & ~1;
+                                if (c < mat.n && even < mat.m) {
+                                    bf16 *o = (bf16 *)p.dst + mat.dst + rep * mat.dst_stride + (long long)c * mat.ld_dst + even;
+                                    if (even + 1 < mat.m) *reinterpret_cast<uint32_t *>(o) = pack_bf16(lo, hi);
+                                    else *o = __float2bfloat16_rn(lo);
+                                }
+                            }
+                        } else if (row < mat.m) {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const int c = col + 4 * i + j;
+                                if (c < mat.n) ns_result(p, mat, mat.dst + rep * mat.dst_stride + (long long)c * mat.ld_dst + row, y[j]);
                             }
                         }
                     }
-                } else if (last) {  // lane = column, two rows at a time
+                } else if (last) {
                     __syncwarp();
-                    const int c = col + (lane & 15);
+                    const long long base = mat.dst + rep * mat.dst_stride;
+                    const float scale = inv_r / NS_X_SCALE;
+                    if (p.bf16_dst && (base & 1) == 0 && (mat.ld_dst & 1) == 0 && ((uintptr_t)p.dst & 3) == 0) {  // two columns per lane, four rows at a time
+                        const int e = lane & 7, c = col + 2 * e;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const int r = 4 * i + (lane >> 3), row = row0 + r;
+                            const float2 y = *reinterpret_cast<const float2 *>(turn + r * 16 + (((e >> 1) ^ ((r >> 1) & 3)) << 2) + 2 * (e & 1));
+                            bf16 *o = (bf16 *)p.dst + base + (long long)row * mat.ld_dst + c;
+                            if (row < mat.m && c + 1 < mat.n) *reinterpret_cast<uint32_t *>(o) = pack_bf16(y.x * scale, y.y * scale);
+                            else if (row < mat.m && c < mat.n) *o = __float2bfloat16_rn(y.x * scale);
+                        }
+                    } else {  // lane = column, two rows at a time
+                        const int c = col + (lane & 15);
 #pragma unroll 8
-                    for (int i = 0; i < 16; ++i) {
-                        const int r = 2 * i + (lane >> 4), row = row0 + r;
-                        const float y = turn[r * 16 + ((((lane & 15) >> 2) ^ ((r >> 1) & 3)) << 2) + (lane & 3)];
-                        if (row < mat.m && c < mat.n) ns_result(p, mat, mat.dst + rep * mat.dst_stride + (long long)row * mat.ld_dst + c, y * (inv_r / NS_X_SCALE));
+                        for (int i = 0; i < 16; ++i) {
+                            const int r = 2 * i + (lane >> 4), row = row0 + r;
+                            const float y = turn[r * 16 + ((((lane & 15) >> 2) ^ ((r >> 1) & 3)) << 2) + (lane & 3)];
+                            if (row < mat.m && c < mat.n) ns_result(p, mat, base + (long long)row * mat.ld_dst + c, y * scale);
+                        }
                     }
                 }
                 __syncwarp();
@@ -1386,6 +1448,7 @@ static NsLayout ns_layout(NsGroup &g)
         l.conv_blocks += m.conv_blocks * m.repeat;
         l.matrices += m.repeat;
     }
+    if (getenv("NS_PAD")) { l.pitch_x += 64; l.pitch_a += 64; }
     return l;
 }
 
@@ -1464,13 +1527,18 @@ static bool ns_run(TcState &tc, Exec &ex, const NsSource &src, NsGroup &g, const
         const double t = ns_chain_cost(g, PARTS, 1 << i, rooms[i], tiles_a, tiles_x);
         if (t < cost) { cost = t; best = i; }
     }
+    if (getenv("NSC_C")) best = atoi(getenv("NSC_C"));
     if (best >= 0 && g.count > 0 && (getenv("NSC_ON") ? atoi(getenv("NSC_ON")) : std::max(tiles_a, tiles_x) <= 4 * tc_sm_count())) {
         NsChain p{};
+        for (int par = 0; par < 2; ++par) {
+            p.io[par][NS_GRAM] = {nullptr, nullptr, A, nullptr, (long long)na, l.pitch_a};
+            p.io[par][NS_POLY] = {A, nullptr, B, nullptr, (long long)na, l.pitch_a};
+            p.io[par][NS_APPLY] = {nullptr, X[par].full, X[par ^ 1].hi, X[par ^ 1].full, (long long)nx, l.pitch_x};
+        }
         p.parts_rows_x = l.rows_x; p.parts_rows_a = l.rows_a;
         p.steps = steps;
         p.a = (float)a; p.b = (float)b; p.c = (float)c; p.eps = eps;
-        p.X[0] = X[0]; p.X[1] = X[1]; p.A = A; p.B = B;
-        p.pitch_a = l.pitch_a; p.lo_off_a = na;
+        p.X0 = X[0];
         p.partial = partial; p.inv_r = inv_r;
         p.norm_blocks = l.norm_blocks; p.adam_blocks = adam_blocks; p.conv_blocks = l.conv_blocks; p.tiles_a = tiles_a; p.tiles_x = tiles_x;
         p.dst = out.dst; p.bf16_dst = out.bf16_dst; p.params = out.params; p.keep = out.keep;
