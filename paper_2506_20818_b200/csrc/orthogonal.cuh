@@ -1448,7 +1448,6 @@ static NsLayout ns_layout(NsGroup &g)
         l.conv_blocks += m.conv_blocks * m.repeat;
         l.matrices += m.repeat;
     }
-    if (getenv("NS_PAD")) { l.pitch_x += 64; l.pitch_a += 64; }
     return l;
 }
 
@@ -1476,16 +1475,31 @@ struct NsTarget {
     float keep;
 };
 
-// estimated microseconds of one step of the chain kernel with clusters of C blocks
-static double ns_chain_cost(const NsGroup &g, int parts, int c, int room, int tiles_a, int tiles_x)
+// Which kernel: estimated microseconds of one step, a fixed time per phase, a time per tile that a block (or pair) takes in turn and
+// one per 64 terms, fitted to runs of 64 x 64 to 2048 x 2048 and of batches.  Measured, BF16 (FP32), microseconds for five steps:
+//                     chain, C = 1     C = 2          C = 4          pair
+//   64 x 64           52 (69)          72 (82)        81 (87)        112 (113)
+//   64 x 1024         70 (121)         80 (107)       87 (101)       139 (150)
+//   768 x 768         103 (201)        101 (152)      199 (268)      235 (250)
+//   1024 x 1024       124 (248)        156 (286)      257 (381)      252 (278)
+//   2048 x 2048       549 (1497)       517 (1471)     1029 (2117)    350 (551)
+//   16 of 512 x 512   242 (552)        404 (645)      961 (1176)     241 (393)
+struct NsCost {
+    double phase, tile, kb;
+    double step(const NsGroup &g, int room, int tiles_a, int tiles_x, int split) const
+    {
+        int kb_m = 0, kb_n = 0;
+        for (int d = 0; d < g.count; ++d) { kb_m = std::max(kb_m, g.mat[d].mp / 64); kb_n = std::max(kb_n, g.mat[d].np / 64); }
+        auto one = [&](int tiles, int blocks) { return phase + ((tiles + room - 1) / room) * (tile + kb * ((blocks + split - 1) / split)); };
+        return one(tiles_a, kb_n) + one(tiles_a, kb_m) + one(tiles_x, kb_m);
+    }
+};
+static NsCost ns_chain_cost(int parts, int c)
 {
-    if (room <= 0) return 1e30;
-    int kb_m = 0, kb_n = 0;
-    for (int d = 0; d < g.count; ++d) { kb_m = std::max(kb_m, g.mat[d].mp / 64); kb_n = std::max(kb_n, g.mat[d].np / 64); }
-    const double kb_us = parts == 2 ? 0.7 : 0.45, tile_us = c > 1 ? 2.4 : 0.4, phase_us = 3.0;  // read off runs of 64 x 64, 256 x 256 and 1000 x 417
-    auto phase = [&](int tiles, int kb) { return phase_us + ((tiles + room - 1) / room) * (tile_us + kb_us * ((kb + c - 1) / c)); };
-    return phase(tiles_a, kb_n) + phase(tiles_a, kb_m) + phase(tiles_x, kb_m);
+    const double tile = c == 1 ? 1.0 : c == 2 ? 2.0 : 2.5;
+    return parts == 2 ? NsCost{2.9, tile, 0.75} : NsCost{2.4, tile, 0.26};
 }
+static NsCost ns_pair_cost(int parts) { return parts == 2 ? NsCost{8.0, 5.0, 0.42} : NsCost{13.0, 0.5, 0.29}; }
 
 struct NsCounters {  // barrier counters of the chain kernel: two sets used in turn, each launch clears the other one
     unsigned *dev = nullptr;
@@ -1518,17 +1532,18 @@ static bool ns_run(TcState &tc, Exec &ex, const NsSource &src, NsGroup &g, const
         err = "cuTensorMapEncodeTiled failed";
         return false;
     }
-    int tiles_a = 0, tiles_x = 0;
+    const int pairs = std::max(1, tc_sm_count() / 2);
+    int tiles_a = 0, tiles_x = 0, best = -1;  // best: log2 of the chain kernel's cluster size, -1 = pair kernel
+    ns_tiles(g, 256, NSP_BN<PARTS>, true, tiles_a, tiles_x);
+    double cost = ns_pair_cost(PARTS).step(g, pairs, tiles_a, tiles_x, 1);
     ns_tiles(g, 128, NSC_BN, false, tiles_a, tiles_x);
     const int rooms[3] = {ns_chain_room<PARTS, 1>(), ns_chain_room<PARTS, 2>(), ns_chain_room<PARTS, 4>()};
-    int best = -1;
-    double cost = 1e30;
     for (int i = 0; i < 3; ++i) {
-        const double t = ns_chain_cost(g, PARTS, 1 << i, rooms[i], tiles_a, tiles_x);
+        if (rooms[i] <= 0) continue;
+        const double t = ns_chain_cost(PARTS, 1 << i).step(g, rooms[i], tiles_a, tiles_x, 1 << i);
         if (t < cost) { cost = t; best = i; }
     }
-    if (getenv("NSC_C")) best = atoi(getenv("NSC_C"));
-    if (best >= 0 && g.count > 0 && (getenv("NSC_ON") ? atoi(getenv("NSC_ON")) : std::max(tiles_a, tiles_x) <= 4 * tc_sm_count())) {
+    if (best >= 0 && g.count > 0) {
         NsChain p{};
         for (int par = 0; par < 2; ++par) {
             p.io[par][NS_GRAM] = {nullptr, nullptr, A, nullptr, (long long)na, l.pitch_a};
@@ -1570,7 +1585,6 @@ static bool ns_run(TcState &tc, Exec &ex, const NsSource &src, NsGroup &g, const
     ex.launches += 1;
     if (g.count == 0) return true;
     ns_tiles(g, 256, NSP_BN<PARTS>, true, tiles_a, tiles_x);
-    const int pairs = std::max(1, tc_sm_count() / 2);
     launch_dep(ns_convert_kernel<PARTS>, dim3(l.conv_blocks), dim3(NS_THREADS), 0, ex.st, src, g, partial, eps, X[0], inv_r);
     ex.launches += 1;
     NsPhase p{};
