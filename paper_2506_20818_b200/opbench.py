@@ -14,7 +14,8 @@ captures of single kernels (few launches, small process).
     python -m paper_2506_20818_b200.opbench --op step --config c2_chunglu_sage2 --batch 10240 --fanout 25,10 --iters 5
 
 runs whole training steps (negatives, step, Adam) of one of the named workload configurations, optionally scaled
-down and over sampled blocks, and prints the time per step: a small process around any kernel of the step.
+down and over sampled blocks, and prints the time per step: a small process around any kernel of the step
+(`--optimizer muon`: the weight matrices take orthogonalised updates, lp_muon_step, in the place of Adam).
 """
 from __future__ import annotations
 
@@ -32,6 +33,7 @@ def main() -> None:
     ap.add_argument("--batch", type=int, default=65536, help="--op step: positives per step")
     ap.add_argument("--fanout", default="", help="--op step: comma-separated fan-outs (hop 1 first); empty = full-graph training")
     ap.add_argument("--prec", choices=["bf16", "fp32"], default="bf16")
+    ap.add_argument("--optimizer", choices=["adam", "muon"], default="adam", help="--op step: Adam, or orthogonalised updates of the weight matrices")
     ap.add_argument("--nodes", type=int, default=1_000_000)
     ap.add_argument("--mean-degree", type=float, default=16.0)
     ap.add_argument("--exponent", type=float, default=2.1)
@@ -67,13 +69,16 @@ def main() -> None:
             a.record()
             _, nd = ctx.sample_negatives(args.seed, i, 1, pu[lo:lo + B], edge_index_base=lo)
             ctx.train_step(p, pu[lo:lo + B], pv[lo:lo + B], None, nd, 1, loss, grads, seed=args.seed, step=i)
-            ctx.adam_step(p, m, v, grads, i + 1)
+            if args.optimizer == "muon":
+                ctx.muon_step(p, m, v, grads, t=i + 1)
+            else:
+                ctx.adam_step(p, m, v, grads, i + 1)
             b.record()
             torch.cuda.synchronize()
             if i >= args.warmup:
                 times.append(a.elapsed_time(b) * 1e3)
         print(json.dumps({"op": "step", "config": args.config, "scale": args.scale, "nodes": g.n, "entries": int(g.nnz), "batch_pos": B, "fanout": fanout,
-                          "dtype": args.prec, "us_per_step": round(float(np.median(times)), 1), "loss": float(loss.item()),
+                          "dtype": args.prec, "optimizer": args.optimizer, "us_per_step": round(float(np.median(times)), 1), "loss": float(loss.item()),
                           "launches_per_step": int(ctx.stats().kernel_launches // max(1, args.warmup + args.iters))}))
         ctx.close()
         return
