@@ -967,7 +967,7 @@ __global__ void __launch_bounds__(NSC_THREADS, 1) ns_chain_kernel(const __grid_c
 // A pair multiplies tiles of 256 x 256 (PARTS = 2: 256 x 128): each CTA brings in 128 rows of the first operand and half of the
 // second, so a 64-term block costs 32 KiB per CTA for 512 cycles of products (48 KiB for 768).  PARTS = 1: two accumulators of
 // 256 columns fill tensor memory, and a tile's is drained while the next tile's products run.  PARTS = 2: the accumulators
-// change hands after every 64-term block and sixteen warps add the blocks up in registers (32 columns per thread; 64, for tiles of
+// (four of 128 columns) change hands after every 64-term block and sixteen warps add the blocks up in registers (32 columns per thread; 64, for tiles of
 // 256 x 256, spill).
 // A and B are symmetric: only tiles on and above the diagonal are computed, the others are written turned.
 //   warp 0 operands, warp 1 matrix instructions (of the pair's first CTA), warps 2-17 results: 32 rows x 64 (32) columns each, turned
@@ -976,6 +976,7 @@ __global__ void __launch_bounds__(NSC_THREADS, 1) ns_chain_kernel(const __grid_c
 constexpr int NSP_THREADS = 576;
 template <int PARTS> constexpr int NSP_BN = PARTS == 2 ? 128 : 256;
 template <int PARTS> constexpr int NSP_STAGES = PARTS == 2 ? 4 : 6;  // 192 KiB in flight (4096 x 4096 with 96, 128, 160 KiB: 1.48, 1.37, 1.32 ms)
+template <int PARTS> constexpr int NSP_ACCS = PARTS == 2 ? 4 : 2;  // accumulators used in turn: all 512 columns of tensor memory
 template <int PARTS> constexpr int NSP_STAGE_BYTES = PARTS * (128 + NSP_BN<PARTS> / 2) * TC_BK * 2;
 constexpr int NSP_TURN_BYTES = 16 * 2048;
 template <int PARTS> constexpr int NSP_SMEM = NSP_STAGES<PARTS> * NSP_STAGE_BYTES<PARTS> + NSP_TURN_BYTES + 1024;
@@ -1002,8 +1003,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NSP_THREADS, 1)
 {
     LP_DEP_ENTER();
     extern __shared__ uint8_t smem_raw[];
-    constexpr int S = NSP_STAGES<PARTS>;
-    __shared__ __align__(8) uint64_t bar_full[S], bar_empty[S], bar_acc_full[2], bar_acc_empty[2];
+    constexpr int S = NSP_STAGES<PARTS>, ACCS = NSP_ACCS<PARTS>;
+    __shared__ __align__(8) uint64_t bar_full[S], bar_empty[S], bar_acc_full[ACCS], bar_acc_empty[ACCS];
     __shared__ uint32_t tmem_base_s;
     constexpr int BN = NSP_BN<PARTS>, COLS = BN / 4;  // COLS: columns of a warp
     constexpr uint32_t a_bytes = 128 * TC_BK * 2, b_bytes = BN / 2 * TC_BK * 2, stage_bytes = NSP_STAGE_BYTES<PARTS>;
@@ -1019,7 +1020,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NSP_THREADS, 1)
             mbar_init(smem_u32(&bar_full[s]), 2);   // one announcement per CTA of the pair (used in the leader only)
             mbar_init(smem_u32(&bar_empty[s]), 1);
         }
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < ACCS; ++b) {
             mbar_init(smem_u32(&bar_acc_full[b]), 1);
             mbar_init(smem_u32(&bar_acc_empty[b]), 32);  // sixteen warps in each CTA (used in the leader only)
         }
@@ -1030,7 +1031,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NSP_THREADS, 1)
     }
     if (warp == 0) {
         __syncwarp();
-        tmem_alloc_pair(smem_u32(&tmem_base_s), 2 * BN);
+        tmem_alloc_pair(smem_u32(&tmem_base_s), ACCS * BN);
     }
     tc_fence_before();
     __syncthreads();
@@ -1099,8 +1100,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NSP_THREADS, 1)
                 const NsMat &mat = g.mat[locate(t, rep, ti, tj)];
                 const int kbs = (p.kind == NS_GRAM ? mat.np : mat.mp) / TC_BK;
                 for (int kb = 0; kb < kbs; ++kb) {
-                    const int b = use & 1;
-                    if ((PARTS == 2 || kb == 0) && use >= 2 && !mbar_wait(smem_u32(&bar_acc_empty[b]), ((use >> 1) & 1) ^ 1, p.wait_ns)) {
+                    const int b = use % ACCS;
+                    if ((PARTS == 2 || kb == 0) && use >= ACCS && !mbar_wait(smem_u32(&bar_acc_empty[b]), ((use / ACCS) & 1) ^ 1, p.wait_ns)) {
                         atomicExch(p.err, 5);
                         ok = false;
                         break;
@@ -1166,14 +1167,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NSP_THREADS, 1)
             if (live && PARTS == 1) fetch(0);
             const int chunks = PARTS == 2 ? kbs : 1;
             for (int c = 0; c < chunks; ++c, ++use) {
-                ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_acc_full[use & 1]), (use >> 1) & 1, p.wait_ns));
+                ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_acc_full[use % ACCS]), (use / ACCS) & 1, p.wait_ns));
                 if (!ok) {
                     if (lane == 0) atomicExch(p.err, 3);
                     break;
                 }
                 tc_fence_after();
                 if (PARTS == 2) {
-                    const uint32_t taddr = tmem + ((uint32_t)(q * 32) << 16) + (use & 1) * BN + cg * 32;
+                    const uint32_t taddr = tmem + ((uint32_t)(q * 32) << 16) + (use % ACCS) * BN + cg * 32;
 #pragma unroll
                     for (int o = 0; o < 32; o += 16) {
                         float r[16];
@@ -1183,7 +1184,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NSP_THREADS, 1)
                     }
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive_remote(map_to_cta(smem_u32(&bar_acc_empty[use & 1]), 0));
+                    if (lane == 0) mbar_arrive_remote(map_to_cta(smem_u32(&bar_acc_empty[use % ACCS]), 0));
                 }
             }
             if (!ok) break;
@@ -1193,11 +1194,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NSP_THREADS, 1)
             for (int blk = 0; blk < COLS / 16; ++blk) {
                 const int col = col0 + blk * 16;
                 if (PARTS == 1) {
-                    tmem_ld_32x16(tmem + ((uint32_t)(q * 32) << 16) + ((use - 1) & 1) * BN + cg * COLS + blk * 16, v);
+                    tmem_ld_32x16(tmem + ((uint32_t)(q * 32) << 16) + ((use - 1) % ACCS) * BN + cg * COLS + blk * 16, v);
                     if (blk == COLS / 16 - 1) {
                         tc_fence_before();
                         __syncwarp();
-                        if (lane == 0) mbar_arrive_remote(map_to_cta(smem_u32(&bar_acc_empty[(use - 1) & 1]), 0));
+                        if (lane == 0) mbar_arrive_remote(map_to_cta(smem_u32(&bar_acc_empty[(use - 1) % ACCS]), 0));
                     }
                 }
                 if (!live) continue;
@@ -1318,7 +1319,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NSP_THREADS, 1)
     cluster_barrier();  // neither CTA frees tensor memory, or leaves with barriers the other may still signal, before both are done
     if (warp == 0) {
         __syncwarp();
-        tmem_dealloc_pair(tmem, 2 * BN);
+        tmem_dealloc_pair(tmem, ACCS * BN);
     }
 }
 
