@@ -85,6 +85,11 @@ static int elems_per_piece(const void *base, int64_t ld, int D, size_t elem, int
     return ve;
 }
 
+// Pieces of VE elements that a lane handles at a time, G * VE columns apart: four elements at least, so that rows whose width or
+// address only allows narrow pieces have as many loads in flight as the others (gradient from 200,000 rows of 257 floats: 220 us
+// with one piece, 180 so; of 101: 120 and 91)
+template <int VE> constexpr int PIECES_PER_LANE = VE >= 4 ? 1 : 4 / VE;
+
 // lanes that share a row: the smallest power of two in 8..32 that covers the row's pieces in one step
 static int lanes_per_row(int pieces) { return pieces <= 8 ? 8 : pieces <= 16 ? 16 : 32; }
 
@@ -94,7 +99,7 @@ static int lanes_per_row(int pieces) { return pieces <= 8 ? 8 : pieces <= 16 ? 1
 constexpr int EMB_THREADS = 256;
 constexpr int EMB_ROWS = 4;
 
-template <typename TT, typename TO, int VE>
+template <typename TT, typename TO, int VE, int U>
 __global__ void __launch_bounds__(EMB_THREADS) embed_kernel(const TT *__restrict__ table, int64_t V, int D, int64_t ldt, const int *__restrict__ ids,
                                                             int64_t N, int padding, float scale, TO *__restrict__ out, int64_t ldo, int G,
                                                             int *__restrict__ err)
@@ -111,25 +116,33 @@ __global__ void __launch_bounds__(EMB_THREADS) embed_kernel(const TT *__restrict
         live[r] = id[r] >= 0 && id[r] < V && id[r] != padding;
         if (i0 + r < N && !live[r] && gl == 0 && (id[r] != padding || padding == LP_NO_PADDING)) atomicOr(err, 1);
     }
-    for (int c = gl * VE; c < D; c += G * VE) {
-        float v[EMB_ROWS][VE];
+    for (int c0 = gl * VE; c0 < D; c0 += U * G * VE) {
+        float v[EMB_ROWS][U][VE];
 #pragma unroll
         for (int r = 0; r < EMB_ROWS; ++r) {
-            if (live[r]) {
-                load_elems<TT, VE>(table + (int64_t)id[r] * ldt + c, v[r]);
-            } else {
 #pragma unroll
-                for (int t = 0; t < VE; ++t) v[r][t] = 0.f;
+            for (int u = 0; u < U; ++u) {
+                const int c = c0 + u * G * VE;
+                if (live[r] && c < D) {
+                    load_elems<TT, VE>(table + (int64_t)id[r] * ldt + c, v[r][u]);
+                } else {
+#pragma unroll
+                    for (int t = 0; t < VE; ++t) v[r][u][t] = 0.f;
+                }
             }
         }
 #pragma unroll
         for (int r = 0; r < EMB_ROWS; ++r) {
-            if (i0 + r < N) {
+            if (i0 + r >= N) continue;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int c = c0 + u * G * VE;
+                if (c >= D) continue;
                 if (live[r]) {
 #pragma unroll
-                    for (int t = 0; t < VE; ++t) v[r][t] *= scale;
+                    for (int t = 0; t < VE; ++t) v[r][u][t] *= scale;
                 }
-                store_elems<TO, VE>(out + (i0 + r) * ldo + c, v[r]);
+                store_elems<TO, VE>(out + (i0 + r) * ldo + c, v[r][u]);
             }
         }
     }
@@ -143,11 +156,15 @@ static void embed_launch(Exec &ex, const TT *table, int64_t V, int D, int64_t ld
     const int ve = std::min(elems_per_piece(table, ldt, D, sizeof(TT), most), elems_per_piece(out, ldo, D, sizeof(TO), most));
     const int G = lanes_per_row((D + ve - 1) / ve);
     const dim3 grid((unsigned)ceil_div64(N, (int64_t)EMB_THREADS / G * EMB_ROWS)), block(EMB_THREADS);
-#define LP_EMBED(VE_) launch_dep(embed_kernel<TT, TO, VE_>, grid, block, 0, ex.st, table, V, D, ldt, ids, N, padding, scale, out, ldo, G, err)
-    if (ve == 8) { if constexpr (most == 8) LP_EMBED(8); }
-    else if (ve == 4) LP_EMBED(4);
-    else if (ve == 2) LP_EMBED(2);
-    else LP_EMBED(1);
+#define LP_EMBED(VE_, U_) launch_dep(embed_kernel<TT, TO, VE_, U_>, grid, block, 0, ex.st, table, V, D, ldt, ids, N, padding, scale, out, ldo, G, err)
+    // several pieces per lane pay for rows of floats wider than three pieces (200,000 rows of 257: 94 us with one, 76 with four; of
+    // 33: 21 and 27) and not for rows of BF16 (257: 68 and 107)
+    const bool several = sizeof(TT) == 4 && D >= 96;
+    if (ve == 8) { if constexpr (most == 8) LP_EMBED(8, 1); }
+    else if (ve == 4) LP_EMBED(4, 1);
+    else if (ve == 2) { if (several) LP_EMBED(2, 2); else LP_EMBED(2, 1); }
+    else if (several && sizeof(TO) == 4) LP_EMBED(1, 4);
+    else LP_EMBED(1, 1);
 #undef LP_EMBED
     ex.launches += 1;
 }
@@ -391,7 +408,8 @@ __global__ void __launch_bounds__(EG_THREADS, 3) embed_grad_sum_kernel(const uin
                                                                     int64_t ldg, int accumulate, float *__restrict__ head, float *__restrict__ tail, int G)
 {
     LP_DEP_ENTER();
-    __shared__ __align__(16) float head_s[EG_THREADS * VE], tail_s[EG_THREADS * VE];
+    constexpr int U = PIECES_PER_LANE<VE>, E = U * VE;
+    __shared__ __align__(16) float head_s[EG_THREADS * E], tail_s[EG_THREADS * E];
     __shared__ uint32_t key_s[EG_THREADS / 8 * EG_CHUNK], val_s[EG_THREADS / 8 * EG_CHUNK];  // the block's sorted ids
     const int gl = threadIdx.x & (G - 1), group = threadIdx.x / G, g = group % EG_PIECES;
     const int64_t span = (int64_t)blockIdx.x * (EG_THREADS / G / EG_PIECES) + group / EG_PIECES;
@@ -409,40 +427,64 @@ __global__ void __launch_bounds__(EG_THREADS, 3) embed_grad_sum_kernel(const uin
     __syncthreads();
     const uint32_t *ck = key_s + group * EG_CHUNK, *cv = val_s + group * EG_CHUNK;
     const uint32_t first = count > 0 ? ck[0] : none;
-    for (int c0 = 0; c0 < D; c0 += G * VE) {
+    // E sums of this lane to shared memory, to a row of FP32 partial sums, to the gradient
+    auto keep = [&](float *to, const float *acc) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) store_elems<float, VE>(to + threadIdx.x * E + u * VE, acc + u * VE);
+    };
+    for (int c0 = 0; c0 < D; c0 += U * G * VE) {
         const int c = c0 + gl * VE;
+        auto put = [&](float *row, const float *acc) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (c + u * G * VE < D) store_elems<float, VE>(row + c + u * G * VE, acc + u * VE);
+        };
+        auto finish = [&](uint32_t v, const float *acc) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (c + u * G * VE < D) embed_grad_store<TG, VE>(grad + (int64_t)v * ldg + c + u * G * VE, acc + u * VE, scale, accumulate != 0);
+        };
         uint32_t open = none;  // the run that begins in this chunk, or before the span, and goes on
         if (count > 0 && c < D) {
             uint32_t cur = first;
             bool from_before = before == first;
-            float acc[VE];
+            float acc[E];
 #pragma unroll
-            for (int t = 0; t < VE; ++t) acc[t] = 0.f;
+            for (int t = 0; t < E; ++t) acc[t] = 0.f;
             for (int b = 0; b < count; b += EG_BATCH) {
-                RawAligned<TD, VE> x[EG_BATCH];
+                RawAligned<TD, VE> x[EG_BATCH][U];
 #pragma unroll
                 for (int j = 0; j < EG_BATCH; ++j)
-                    if (b + j < count && ck[b + j] < (uint32_t)V) x[j].load(dout + (int64_t)cv[b + j] * ldd + c);
+                    if (b + j < count && ck[b + j] < (uint32_t)V) {
+                        const TD *row = dout + (int64_t)cv[b + j] * ldd + c;
+#pragma unroll
+                        for (int u = 0; u < U; ++u)
+                            if (c + u * G * VE < D) x[j][u].load(row + u * G * VE);
+                    }
 #pragma unroll
                 for (int j = 0; j < EG_BATCH; ++j) {
                     const uint32_t key = b + j < count ? ck[b + j] : (uint32_t)V;
                     if (key != cur) {
                         if (cur < (uint32_t)V) {
-                            if (from_before) store_elems<float, VE>(head_s + threadIdx.x * VE, acc);
-                            else embed_grad_store<TG, VE>(grad + (int64_t)cur * ldg + c, acc, scale, accumulate != 0);
+                            if (from_before) keep(head_s, acc);
+                            else finish(cur, acc);
                         }
                         from_before = false;
                         cur = key;
 #pragma unroll
-                        for (int t = 0; t < VE; ++t) acc[t] = 0.f;
+                        for (int t = 0; t < E; ++t) acc[t] = 0.f;
                     }
-                    if (key < (uint32_t)V) x[j].add_to(acc);
+                    if (key < (uint32_t)V) {
+#pragma unroll
+                        for (int u = 0; u < U; ++u)
+                            if (c + u * G * VE < D) x[j][u].add_to(acc + u * VE);
+                    }
                 }
             }
             if (cur < (uint32_t)V) {
-                if (from_before) store_elems<float, VE>(head_s + threadIdx.x * VE, acc);
-                else if (after == cur) { store_elems<float, VE>(tail_s + threadIdx.x * VE, acc); open = cur; }
-                else embed_grad_store<TG, VE>(grad + (int64_t)cur * ldg + c, acc, scale, accumulate != 0);
+                if (from_before) keep(head_s, acc);
+                else if (after == cur) { keep(tail_s, acc); open = cur; }
+                else finish(cur, acc);
             }
         }
         __syncthreads();
@@ -450,31 +492,25 @@ __global__ void __launch_bounds__(EG_THREADS, 3) embed_grad_sum_kernel(const uin
         const bool came_in = g == 0 && count > 0 && before == first && first < (uint32_t)V;
         if ((open != none || came_in) && c < D) {
             const uint32_t run = came_in ? first : open;
-            float acc[VE];
-            load_elems<float, VE>((came_in ? head_s : tail_s) + threadIdx.x * VE, acc);
-            int64_t q = p0 + EG_CHUNK;
-            for (int o = g + 1; q < span1 && keys[q] == run; ++o, q += EG_CHUNK) {
-                float x[VE];
-                load_elems<float, VE>(head_s + ((group - g + o) * G + gl) * VE, x);
+            float acc[E];
+            auto gather = [&](const float *own, uint32_t r) {  // this chunk's part and those of the chunks behind it that begin with the run
 #pragma unroll
-                for (int t = 0; t < VE; ++t) acc[t] += x[t];
-            }
-            const bool goes_on = span1 < N && keys[span1 - 1] == run && keys[span1] == run;
-            if (came_in) store_elems<float, VE>(head + span * D + c, acc);
-            else if (goes_on) store_elems<float, VE>(tail + span * D + c, acc);
-            else embed_grad_store<TG, VE>(grad + (int64_t)run * ldg + c, acc, scale, accumulate != 0);
-            // the first group may hold both: the run that came in and ended, and one that begins in its chunk and goes on
-            if (came_in && open != none) {
-                load_elems<float, VE>(tail_s + threadIdx.x * VE, acc);
-                q = p0 + EG_CHUNK;
-                for (int o = 1; q < span1 && keys[q] == open; ++o, q += EG_CHUNK) {
-                    float x[VE];
-                    load_elems<float, VE>(head_s + ((group - g + o) * G + gl) * VE, x);
+                for (int t = 0; t < E; ++t) acc[t] = own[threadIdx.x * E + t];
+                int64_t q = p0 + EG_CHUNK;
+                for (int o = g + 1; q < span1 && keys[q] == r; ++o, q += EG_CHUNK) {
 #pragma unroll
-                    for (int t = 0; t < VE; ++t) acc[t] += x[t];
+                    for (int t = 0; t < E; ++t) acc[t] += head_s[((group - g + o) * G + gl) * E + t];
                 }
-                if (span1 < N && keys[span1 - 1] == open && keys[span1] == open) store_elems<float, VE>(tail + span * D + c, acc);
-                else embed_grad_store<TG, VE>(grad + (int64_t)open * ldg + c, acc, scale, accumulate != 0);
+            };
+            auto goes_on = [&](uint32_t r) { return span1 < N && keys[span1 - 1] == r && keys[span1] == r; };
+            gather(came_in ? head_s : tail_s, run);
+            if (came_in) put(head + span * D, acc);
+            else if (goes_on(run)) put(tail + span * D, acc);
+            else finish(run, acc);
+            if (came_in && open != none) {  // the first group may hold both: the run that came in and ended, and one that begins in its chunk and goes on
+                gather(tail_s, open);
+                if (goes_on(open)) put(tail + span * D, acc);
+                else finish(open, acc);
             }
         }
         __syncthreads();
@@ -593,7 +629,8 @@ __global__ void __launch_bounds__(EG_THREADS) embed_grad_few_kernel(const int *_
     LP_DEP_ENTER();
     extern __shared__ uint32_t list[];                // (row - r0) << 13 | position
     __shared__ uint32_t named[EGS_MAX_ROWS / 32];
-    __shared__ __align__(16) float head[EG_THREADS * VE], tail[EG_THREADS * VE];
+    constexpr int PU = PIECES_PER_LANE<VE>, E = PU * VE;
+    __shared__ __align__(16) float head[EG_THREADS * E], tail[EG_THREADS * E];
     __shared__ int count_s;
     const int64_t r0 = (int64_t)blockIdx.x * R, r1 = min(r0 + R, V);
     for (int i = threadIdx.x; i < (R + 31) / 32; i += EG_THREADS) named[i] = 0;
@@ -650,54 +687,67 @@ __global__ void __launch_bounds__(EG_THREADS) embed_grad_few_kernel(const int *_
     const int per = (M + EG_PIECES - 1) / EG_PIECES, a0 = g < EG_PIECES ? min(M, g * per) : M, a1 = min(M, a0 + per);
     const uint32_t none = 0xFFFFFFFFu;
     const uint32_t before = a0 > 0 && a0 < a1 ? list[a0 - 1] >> 13 : none, after = a1 < M && a0 < a1 ? list[a1] >> 13 : none;
-    for (int c0 = 0; c0 < D; c0 += G * VE) {
+    auto keep = [&](float *to, const float *acc) {
+#pragma unroll
+        for (int t = 0; t < E; ++t) to[threadIdx.x * E + t] = acc[t];
+    };
+    for (int c0 = 0; c0 < D; c0 += PU * G * VE) {
         const int c = c0 + gl * VE;
+        auto finish = [&](uint32_t row, const float *acc) {
+#pragma unroll
+            for (int u = 0; u < PU; ++u)
+                if (c + u * G * VE < D) embed_grad_store<TG, VE>(grad + (r0 + row) * ldg + c + u * G * VE, acc + u * VE, scale, accumulate != 0);
+        };
         uint32_t open = none;  // the run that began here and goes on
         if (a0 < a1 && c < D) {
             uint32_t cur = list[a0] >> 13;
             bool from_before = before == cur;
-            float acc[VE];
+            float acc[E];
 #pragma unroll
-            for (int t = 0; t < VE; ++t) acc[t] = 0.f;
+            for (int t = 0; t < E; ++t) acc[t] = 0.f;
             for (int b = a0; b < a1; b += EG_BATCH) {
                 uint32_t k[EG_BATCH];
-                float x[EG_BATCH][VE];
+                RawAligned<TD, VE> x[EG_BATCH][PU];
 #pragma unroll
                 for (int j = 0; j < EG_BATCH; ++j) {
                     k[j] = b + j < a1 ? list[b + j] : none;
-                    if (b + j < a1) load_elems<TD, VE>(dout + (int64_t)(k[j] & 8191u) * ldd + c, x[j]);
+                    if (b + j < a1) {
+#pragma unroll
+                        for (int u = 0; u < PU; ++u)
+                            if (c + u * G * VE < D) x[j][u].load(dout + (int64_t)(k[j] & 8191u) * ldd + c + u * G * VE);
+                    }
                 }
 #pragma unroll
                 for (int j = 0; j < EG_BATCH; ++j) {
                     if (b + j < a1) {
                         if ((k[j] >> 13) != cur) {
-                            if (from_before) store_elems<float, VE>(head + threadIdx.x * VE, acc);
-                            else embed_grad_store<TG, VE>(grad + (r0 + cur) * ldg + c, acc, scale, accumulate != 0);
+                            if (from_before) keep(head, acc);
+                            else finish(cur, acc);
                             from_before = false;
                             cur = k[j] >> 13;
 #pragma unroll
-                            for (int t = 0; t < VE; ++t) acc[t] = 0.f;
+                            for (int t = 0; t < E; ++t) acc[t] = 0.f;
                         }
 #pragma unroll
-                        for (int t = 0; t < VE; ++t) acc[t] += x[j][t];
+                        for (int u = 0; u < PU; ++u)
+                            if (c + u * G * VE < D) x[j][u].add_to(acc + u * VE);
                     }
                 }
             }
-            if (from_before) store_elems<float, VE>(head + threadIdx.x * VE, acc);
-            else if (after == cur) { store_elems<float, VE>(tail + threadIdx.x * VE, acc); open = cur; }
-            else embed_grad_store<TG, VE>(grad + (r0 + cur) * ldg + c, acc, scale, accumulate != 0);
+            if (from_before) keep(head, acc);
+            else if (after == cur) { keep(tail, acc); open = cur; }
+            else finish(cur, acc);
         }
         __syncthreads();
         if (open != none) {
-            float acc[VE];
-            load_elems<float, VE>(tail + threadIdx.x * VE, acc);
-            for (int o = g + 1; o < EG_PIECES && o * per < M && (list[o * per] >> 13) == open; ++o) {
-                float x[VE];
-                load_elems<float, VE>(head + (o * G + gl) * VE, x);
+            float acc[E];
 #pragma unroll
-                for (int t = 0; t < VE; ++t) acc[t] += x[t];
+            for (int t = 0; t < E; ++t) acc[t] = tail[threadIdx.x * E + t];
+            for (int o = g + 1; o < EG_PIECES && o * per < M && (list[o * per] >> 13) == open; ++o) {
+#pragma unroll
+                for (int t = 0; t < E; ++t) acc[t] += head[(o * G + gl) * E + t];
             }
-            embed_grad_store<TG, VE>(grad + (r0 + open) * ldg + c, acc, scale, accumulate != 0);
+            finish(open, acc);
         }
         __syncthreads();
     }
