@@ -779,8 +779,8 @@ static void embed_grad_rows(Exec &ex, const TD *dout, int64_t ldd, const int *id
     // 2.9 M rows: 300 us against 150; 2,048: 137 against 150), so the limit is lower there.
     const int R = (int)std::min<int64_t>(EGS_MAX_ROWS, std::max<int64_t>(4, ceil_div64(V, 148 * 4)));
     if (N > 0 && N <= (R <= 1024 ? EGS_MAX_IDS : EGS_MAX_IDS / 4)) {
-        static const bool room = cudaFuncSetAttribute(embed_grad_few_kernel<TD, TG, VE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)few_bytes(EGS_MAX_IDS)) == cudaSuccess;
-        (void)room;  // without it the launch reports the error
+        if (few_bytes(N) > 8192)  // beside the static arrays it may pass the default limit; if refused, the launch reports the error
+            cudaFuncSetAttribute(embed_grad_few_kernel<TD, TG, VE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)few_bytes(EGS_MAX_IDS));
         launch_dep(embed_grad_few_kernel<TD, TG, VE>, dim3((unsigned)ceil_div64(V, R)), dim3(EG_THREADS), few_bytes(N), ex.st, ids, (int)N, V, padding, R, dout, ldd, D, scale, grad, ldg,
                    accumulate, G, err);
         ex.launches += 1;

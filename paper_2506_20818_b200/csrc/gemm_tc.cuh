@@ -1040,8 +1040,11 @@ static lp_status tc_check(TcState &tc, Exec &ex, bool synced, std::string &err)
 static lp_status tc_check_result(TcState &tc, Exec &ex, std::string &err)
 {
     if (*tc.host_err != 0) {
-        char buf[128];
-        snprintf(buf, sizeof buf, "tensor-core GEMM: bounded wait %d expired (1 = stage free, 2 = operands, 3 = accumulator, 4 = operands for the column sums)", *tc.host_err);
+        char buf[256];
+        snprintf(buf, sizeof buf,
+                 "tensor-core GEMM: bounded wait %d expired (1 = stage free, 2 = operands, 3 = accumulator, 4 = operands for the column sums, "
+                 "5 = accumulator free, 6 = phase of the chained products, 7 = exchange of sums)",
+                 *tc.host_err);
         err = buf;
         cudaMemsetAsync(tc.err_word, 0, sizeof(int), ex.st);
         return LP_ETIMEOUT;

@@ -503,6 +503,17 @@ LP_DEVINL void tmem_ld_32x16(uint32_t taddr, float *v)
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
+LP_DEVINL void tmem_ld_32x8(uint32_t a, float *v)
+{
+    uint32_t r[8];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(a)
+                 : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
+}
 LP_DEVINL void tmem_ld_32x8_pair(uint32_t a, uint32_t b, float *v, float *w)
 {
     uint32_t r[16];
@@ -558,23 +569,32 @@ LP_DEVINL NsTile ns_tile(const NsGroup &g, int kind, int t)
 __device__ __noinline__ void ns_result8(const NsChain &p, const NsMat &mat, int rep, int row, int col, const float4 lo, const float4 hi, float scale)
 {
     float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-    const long long base = mat.dst + rep * mat.dst_stride;
+    // read once: behind a store the compiler would fetch them again
+    const long long base = mat.dst + rep * mat.dst_stride, ld = mat.ld_dst;
+    const float *const params = p.params;
+    void *const dst = p.dst;
+    const bool to_bf16 = p.bf16_dst != 0, tall = mat.tall != 0;
+    const float update = mat.update, keep = p.keep;
+    const int n = mat.n;
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] *= scale;
-    if (mat.tall || col + 8 > mat.n) {
+    if (tall || col + 8 > n) {
+        const long long o = base + (tall ? (long long)col * ld + row : (long long)row * ld + col), step = tall ? ld : 1;
+        float old[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) old[i] = params && col + i < n ? params[o + i * step] : 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            if (col + i >= mat.n) break;
-            const long long o = base + (mat.tall ? (long long)(col + i) * mat.ld_dst + row : (long long)row * mat.ld_dst + col + i);
-            if (p.params) ((float *)p.dst)[o] = fmaf(-mat.update, v[i], p.keep * p.params[o]);
-            else if (p.bf16_dst) ((bf16 *)p.dst)[o] = __float2bfloat16_rn(v[i]);
-            else ((float *)p.dst)[o] = v[i];
+            if (col + i >= n) continue;
+            if (params) ((float *)dst)[o + i * step] = fmaf(-update, v[i], keep * old[i]);
+            else if (to_bf16) ((bf16 *)dst)[o + i * step] = __float2bfloat16_rn(v[i]);
+            else ((float *)dst)[o + i * step] = v[i];
         }
         return;
     }
-    const long long o = base + (long long)row * mat.ld_dst + col;
-    if (p.bf16_dst) {
-        bf16 *q = (bf16 *)p.dst + o;
+    const long long o = base + (long long)row * ld + col;
+    if (to_bf16) {
+        bf16 *q = (bf16 *)dst + o;
         if (((uintptr_t)q & 15) == 0) {
             store_elems<bf16, 8>(q, v);
         } else {
@@ -583,19 +603,19 @@ __device__ __noinline__ void ns_result8(const NsChain &p, const NsMat &mat, int 
         }
         return;
     }
-    float *q = (float *)p.dst + o;
-    const bool wide = (((uintptr_t)q | (uintptr_t)(p.params ? p.params + o : nullptr)) & 15) == 0;
-    if (p.params) {
+    float *q = (float *)dst + o;
+    const bool wide = (((uintptr_t)q | (uintptr_t)(params ? params + o : nullptr)) & 15) == 0;
+    if (params) {
         float old[8];
         if (wide) {
-            load_elems<float, 4>(p.params + o, old);
-            load_elems<float, 4>(p.params + o + 4, old + 4);
+            load_elems<float, 4>(params + o, old);
+            load_elems<float, 4>(params + o + 4, old + 4);
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) old[i] = p.params[o + i];
+            for (int i = 0; i < 8; ++i) old[i] = params[o + i];
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = fmaf(-mat.update, v[i], p.keep * old[i]);
+        for (int i = 0; i < 8; ++i) v[i] = fmaf(-update, v[i], keep * old[i]);
     }
     if (wide) {
         store_elems<float, 4>(q, v);
@@ -958,6 +978,291 @@ __global__ void __launch_bounds__(NSC_THREADS, 1) ns_chain_kernel(const __grid_c
     if (warp == 0) {
         __syncwarp();
         tmem_dealloc(tmem, NSC_ACCS * NSC_ACC_COLS<PARTS>);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// The whole iteration of a matrix of up to 128 x 128 in one block, for calls whose matrices are all of that size.
+//
+// Such a matrix needs 17 dependent steps of next to no work, so the time is the way from one product to the next.  Through
+// global memory and a counter (the chain kernel) that is 3.8 us; here X and A (then B, in its place) stay in shared memory as
+// operands of the matrix instructions, X also in FP32, and a product follows the one before it after one barrier of the block.  The same copy of X serves both products: its rows are the K-major
+// operands of X X^T, and read across, the MN-major second operand of B X.
+//   every warp sums and results: 32 rows x every fourth group of eight columns; warp 3 also the matrix instructions
+// PARTS = 2: every 32 terms have an accumulator of their own (four of 128 columns fill tensor memory).  Their four sums are added
+// in pairs; carrying the roundings along, as the chain kernel does for longer sums, took 54 us for 128 x 128 and changes the
+// error of a matrix of full rank from 6.4e-7 to 6.2e-7, of rank one from 2.3e-5 to 1.7e-5 (FP32 matrix products: 9.7e-5).
+// Blocks from `matrices` on take Adam steps.
+// Microseconds for five steps, FP32 (BF16), against the chain kernel: 64 x 64 24 (17) against 64 (47); 128 x 128 45 (27) against
+// 95 (60); 200 of 128 x 128 90 (52) against 243 (155); 1,000 of 64 x 64 157 (110) against 312 (228).  A 64 x 64 product takes 2,300
+// cycles: 930 for its twelve matrix instructions (50 each, the time in which shared memory delivers their operands) and their
+// completion, 1,250 to 1,600 for the sums, the next operands' rounding and their stores, the rest barriers.  Of 128 x 128 the sums
+// take most, and they are bound by instructions.
+// ---------------------------------------------------------------------------------------------
+constexpr int NSB_SIZE = 128;                // largest side
+constexpr int NSB_THREADS = 512;
+constexpr int NSB_COLS = NSB_SIZE * 64;      // elements of 64 columns of an operand
+constexpr int NSB_PART = 2 * NSB_COLS;       // elements of a part of an operand
+template <int PARTS> constexpr int NSB_SMEM = 2 * PARTS * NSB_PART * 2 + NSB_SIZE * NSB_SIZE * 4 + 1024;
+
+struct NsBlock {
+    int steps, matrices;
+    float a, b, c;
+    double eps;
+    void *dst;
+    int bf16_dst;
+    const float *params;
+    float keep;
+    int *err;
+    unsigned long long wait_ns;
+    int extra_tx;
+};
+
+template <int PARTS>
+__global__ void __launch_bounds__(NSB_THREADS, 1) ns_block_kernel(const __grid_constant__ NsSource src, const __grid_constant__ NsGroup g, const __grid_constant__ NsAdam adam,
+                                                                  const __grid_constant__ NsBlock p)
+{
+    LP_DEP_ENTER();
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t bar_acc;
+    __shared__ uint32_t tmem_base_s;
+    __shared__ double sw[NSB_THREADS / 32];
+    if ((int)blockIdx.x >= p.matrices) {
+        ns_adam_block<NSB_THREADS>(adam, blockIdx.x - p.matrices, threadIdx.x);
+        return;
+    }
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    const NsMat &mat = g.mat[ns_find(g, blockIdx.x, [](const NsMat &m) { return m.index; })];
+    const int rep = blockIdx.x - mat.index, mp = mat.mp, np = mat.np, m = mat.m, n = mat.n;
+    const bool tall = mat.tall != 0;
+    __half *Xs = reinterpret_cast<__half *>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023), *As = Xs + PARTS * NSB_PART;
+    float4 *Xf = reinterpret_cast<float4 *>(As + PARTS * NSB_PART);  // [four columns][row]
+    constexpr int TERMS = PARTS == 2 ? 32 : NSB_SIZE;                // terms of an accumulator
+    const uint32_t tmem_cols = (uint32_t)max((np + TERMS - 1) / TERMS * mp, (mp + TERMS - 1) / TERMS * np);  // a power of two, np >= mp
+    if (threadIdx.x == 0) {
+        mbar_init(smem_u32(&bar_acc), p.extra_tx != 0 && blockIdx.x == 0 ? 2 : 1);
+        fence_barrier_init();
+    }
+    if (warp == 0) {
+        __syncwarp();
+        tmem_alloc(smem_u32(&tmem_base_s), tmem_cols);
+    }
+    const int q = warp & 3, quarter = warp >> 2, row = q * 32 + lane;  // the rows that the warp may read from tensor memory
+    const bool rows_here = q * 32 < mp;
+    auto place = [&](__half *base, int group) {  // eight columns of this thread's row in an operand (128-byte swizzle)
+        return base + (group >> 3) * NSB_COLS + row * 64 + (((group & 7) ^ (row & 7)) << 3);
+    };
+    float r;
+    {
+        constexpr int GROUPS = NSB_SIZE / 32;
+        float x[GROUPS][8];
+        const long long base = mat.src + rep * mat.src_stride, ld = mat.ld_src;
+        const bool wide = !src.grads && !tall && (ld & 3) == 0 && (base & 3) == 0 && ((uintptr_t)src.u & 15) == 0;
+        double acc = 0.0;
+#pragma unroll
+        for (int i = 0; i < GROUPS; ++i) {
+            const int col = 8 * (quarter + 4 * i);
+            if (wide && row < m && col + 8 <= n) {
+                const long long at = base + row * ld + col;
+                if (src.bf16_u) {
+                    load_elems<bf16, 4>((const bf16 *)src.u + at, x[i]);
+                    load_elems<bf16, 4>((const bf16 *)src.u + at + 4, x[i] + 4);
+                } else {
+                    load_elems<float, 4>((const float *)src.u + at, x[i]);
+                    load_elems<float, 4>((const float *)src.u + at + 4, x[i] + 4);
+                }
+            } else if (!src.grads) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const long long at = base + (tall ? (col + j) * ld + row : row * ld + col + j);
+                    const bool in = row < m && col + j < n;
+                    x[i][j] = !in ? 0.f : src.bf16_u ? __bfloat162float(((const bf16 *)src.u)[at]) : ((const float *)src.u)[at];
+                }
+            } else {
+                float gr[8], av[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const long long at = base + (tall ? (col + j) * ld + row : row * ld + col + j);
+                    const bool in = row < m && col + j < n;
+                    gr[j] = in ? src.grad_scale * src.grads[at] : 0.f;
+                    x[i][j] = in ? src.momentum[at] : 0.f;
+                    if (src.new_adam_v) av[j] = in ? src.adam_v[at] : 0.f;
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const long long at = base + (tall ? (col + j) * ld + row : row * ld + col + j);
+                    const float mo = fmaf(src.mu, x[i][j], gr[j]);
+                    if (row < m && col + j < n) {
+                        src.new_momentum[at] = mo;
+                        if (src.new_adam_v) src.new_adam_v[at] = av[j];
+                    }
+                    x[i][j] = src.nesterov ? fmaf(src.mu, mo, gr[j]) : mo;
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < GROUPS; ++i)
+#pragma unroll
+            for (int j = 0; j < 8 && 32 * i < np; ++j) acc = fma((double)x[i][j], (double)x[i][j], acc);  // in double: no overflow for any FP32 input
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, o);
+        if (lane == 0) sw[warp] = acc;
+        __syncthreads();
+        acc = 0.0;
+        for (int w = 0; w < NSB_THREADS / 32; ++w) acc += sw[w];
+        double pow2;
+        ns_start_scale(sqrt(acc) + p.eps, r, pow2);
+#pragma unroll
+        for (int i = 0; i < GROUPS; ++i) {
+            const int group = quarter + 4 * i;
+            if (!rows_here || 32 * i >= np) break;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[i][j] = (float)(x[i][j] * pow2);
+            ns_store8<PARTS>(x[i], place(Xs, group), NSB_PART);
+            Xf[2 * group * NSB_SIZE + row] = make_float4(x[i][0], x[i][1], x[i][2], x[i][3]);
+            Xf[(2 * group + 1) * NSB_SIZE + row] = make_float4(x[i][4], x[i][5], x[i][6], x[i][7]);
+        }
+    }
+    const float inv_r = 1.f / r, r2 = inv_r * inv_r;
+    const float bf = p.b * r2, cf = p.c / NS_A_SCALE * r2 * r2, af = p.a;
+    fence_async_proxy();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_base_s, lanes = (uint32_t)(q * 32) << 16;
+
+    // one product: of the columns of this warp, the sums and what becomes of them
+    auto finish = [&](auto kind_) {
+        constexpr int kind = decltype(kind_)::value;
+        constexpr bool square = kind == NS_GRAM || kind == NS_POLY;
+        const int width = square ? mp : np, chunks = ((kind == NS_GRAM ? np : mp) + TERMS - 1) / TERMS;
+        // the last product: where it goes (held in registers: a store may not change it)
+        void *const dst = p.dst;
+        const float *const params = p.params;
+        const bool to_bf16 = p.bf16_dst != 0;
+        const long long base = mat.dst + rep * mat.dst_stride, step = tall ? mat.ld_dst : 1;
+        const float update = mat.update, keep = p.keep, unscale = inv_r / NS_X_SCALE;
+#pragma unroll 1
+        for (int group = quarter; 8 * group < width; group += 4) {
+            const uint32_t taddr = tmem + lanes + 8 * group;
+            float v[8], add[8];
+            if (PARTS == 2) {
+                float t[8], u[8];
+                tmem_ld_32x8_pair(taddr, taddr + width, v, t);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] += t[j];
+                if (chunks > 2) {
+                    tmem_ld_32x8_pair(taddr + 2 * width, taddr + 3 * width, t, u);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] += t[j] + u[j];
+                }
+            } else {
+                tmem_ld_32x8(taddr, v);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) add[j] = 0.f;
+            if (kind == NS_POLY) {
+                ns_add8(*reinterpret_cast<const uint4 *>(place(As, group)), add);
+                if (PARTS == 2) ns_add8(*reinterpret_cast<const uint4 *>(place(As, group) + NSB_PART), add);
+            } else if (!square) {
+                const float4 x0 = Xf[2 * group * NSB_SIZE + row], x1 = Xf[(2 * group + 1) * NSB_SIZE + row];
+                add[0] = x0.x; add[1] = x0.y; add[2] = x0.z; add[3] = x0.w;
+                add[4] = x1.x; add[5] = x1.y; add[6] = x1.z; add[7] = x1.w;
+            }
+            const float f = kind == NS_GRAM ? NS_A_SCALE / (NS_X_SCALE * NS_X_SCALE) : kind == NS_POLY ? cf : 1.f / NS_A_SCALE;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                v[j] *= f;  // a power of two where precision counts
+                if (kind != NS_GRAM) v[j] = fmaf(kind == NS_POLY ? bf : af, add[j], v[j]);
+            }
+            if (kind == NS_LAST) {
+                const long long o = base + (tall ? (long long)8 * group * step + row : (long long)row * mat.ld_dst + 8 * group);
+                const int live = row < m ? n - 8 * group : 0;  // columns inside the matrix
+                float old[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) old[j] = params && j < live ? params[o + j * step] : 0.f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    v[j] *= unscale;
+                    if (params) v[j] = fmaf(-update, v[j], keep * old[j]);
+                }
+                if (!tall && live >= 8 && !to_bf16 && ((uintptr_t)((float *)dst + o) & 15) == 0) {
+                    store_elems<float, 4>((float *)dst + o, v);
+                    store_elems<float, 4>((float *)dst + o + 4, v + 4);
+                } else if (!tall && live >= 8 && to_bf16 && ((uintptr_t)((bf16 *)dst + o) & 15) == 0) {
+                    store_elems<bf16, 8>((bf16 *)dst + o, v);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        if (j >= live) continue;
+                        if (to_bf16) ((bf16 *)dst)[o + j * step] = __float2bfloat16_rn(v[j]);
+                        else ((float *)dst)[o + j * step] = v[j];
+                    }
+                }
+            } else {
+                ns_store8<PARTS>(v, place(square ? As : Xs, group), NSB_PART);
+                if (!square) {
+                    Xf[2 * group * NSB_SIZE + row] = make_float4(v[0], v[1], v[2], v[3]);
+                    Xf[(2 * group + 1) * NSB_SIZE + row] = make_float4(v[4], v[5], v[6], v[7]);
+                }
+            }
+        }
+    };
+    int product = 0;
+    for (int k = 0; k < p.steps; ++k) {
+        bool failed = false;
+        for (int kind = NS_GRAM; kind <= NS_APPLY; ++kind, ++product) {
+            if (warp == 3) {  // without rows of its own where the matrix has 64
+                if (elect_one()) {
+                    const int terms = kind == NS_GRAM ? np : mp, width = kind == NS_APPLY ? np : mp;
+                    const uint32_t idesc = make_idesc_f16(NSB_SIZE, width, kind == NS_APPLY);
+                    const uint64_t da = make_smem_desc(smem_u32(kind == NS_GRAM ? Xs : As), 16, 1024);
+                    const uint64_t db = kind == NS_APPLY ? make_smem_desc(smem_u32(Xs), NSB_COLS * 2, 1024) : da;
+                    constexpr uint64_t lo = (NSB_PART * 2) >> 4;
+                    for (int s = 0; s < terms / TC_UMMA_K; s += 2) {  // 32 terms
+                        const uint64_t a0 = da + (s >> 2) * ((NSB_COLS * 2) >> 4) + (s & 3) * 2, a1 = a0 + 2;
+                        const uint64_t step = kind == NS_APPLY ? 2048 >> 4 : 2;
+                        const uint64_t b0 = kind == NS_APPLY ? db + s * step : a0, b1 = b0 + step;
+                        const uint32_t acc = tmem + (PARTS == 2 ? (s >> 1) * width : 0);
+                        if (PARTS == 2) {  // the small terms first, while the sums are small
+                            umma_bf16(acc, a0, b0 + lo, idesc, 0u);
+                            umma_bf16(acc, a0 + lo, b0, idesc, 1u);
+                            umma_bf16(acc, a1, b1 + lo, idesc, 1u);
+                            umma_bf16(acc, a1 + lo, b1, idesc, 1u);
+                        }
+                        umma_bf16(acc, a0, b0, idesc, PARTS == 2 || s != 0 ? 1u : 0u);
+                        umma_bf16(acc, a1, b1, idesc, 1u);
+                    }
+                    umma_commit(smem_u32(&bar_acc));
+                }
+                __syncwarp();
+            }
+            if (rows_here) {
+                failed = !__all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_acc), product & 1, p.wait_ns));
+                tc_fence_after();
+                if (failed) {
+                    if (lane == 0) atomicExch(p.err, 3);
+                } else if (kind == NS_GRAM) {
+                    finish(std::integral_constant<int, NS_GRAM>());
+                } else if (kind == NS_POLY) {
+                    finish(std::integral_constant<int, NS_POLY>());
+                } else if (k + 1 < p.steps) {
+                    finish(std::integral_constant<int, NS_APPLY>());
+                } else {
+                    finish(std::integral_constant<int, NS_LAST>());
+                }
+            }
+            fence_async_proxy();
+            tc_fence_before();
+            failed = __syncthreads_or(failed) != 0;  // all go on or all leave
+            tc_fence_after();
+            if (failed) break;
+        }
+        if (failed) break;
+    }
+    if (warp == 0) {
+        __syncwarp();
+        tmem_dealloc(tmem, tmem_cols);
     }
 }
 
@@ -1366,6 +1671,8 @@ template <int PARTS, int C> static int ns_chain_room()
 static bool ns_init(std::string &err)
 {
     if (!ns_chain_init<1, 1>() || !ns_chain_init<1, 2>() || !ns_chain_init<1, 4>() || !ns_chain_init<2, 1>() || !ns_chain_init<2, 2>() || !ns_chain_init<2, 4>() ||
+        cudaFuncSetAttribute(ns_block_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, NSB_SMEM<1>) != cudaSuccess ||
+        cudaFuncSetAttribute(ns_block_kernel<2>, cudaFuncAttributeMaxDynamicSharedMemorySize, NSB_SMEM<2>) != cudaSuccess ||
         cudaFuncSetAttribute(ns_pair_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, NSP_SMEM<1>) != cudaSuccess ||
         cudaFuncSetAttribute(ns_pair_kernel<2>, cudaFuncAttributeMaxDynamicSharedMemorySize, NSP_SMEM<2>) != cudaSuccess) {
         err = "cannot raise the dynamic shared memory limit of the Newton-Schulz products";
@@ -1526,6 +1833,19 @@ static bool ns_run(TcState &tc, Exec &ex, const NsSource &src, NsGroup &g, const
     double *partial = (double *)((uint8_t *)B + NsLayout::up((size_t)2 * PARTS * na));
     float *inv_r = (float *)((uint8_t *)partial + NsLayout::up(sizeof(double) * (size_t)l.norm_blocks));
     const int adam_blocks = (int)ceil_div64(adam.spans.first[adam.spans.count], NS_ADAM_ELEMS);
+    bool small = g.count > 0;  // faster wherever it applies (figures at the kernel)
+    for (int d = 0; d < g.count; ++d) small = small && g.mat[d].n <= NSB_SIZE;
+    if (small) {
+        NsBlock p{};
+        p.steps = steps; p.matrices = l.matrices;
+        p.a = (float)a; p.b = (float)b; p.c = (float)c; p.eps = eps;
+        p.dst = out.dst; p.bf16_dst = out.bf16_dst; p.params = out.params; p.keep = out.keep;
+        p.err = tc.err_word; p.wait_ns = tc.wait_limit_ns; p.extra_tx = tc.overdeclare_tx;
+        tc.overdeclare_tx = 0;
+        launch_dep(ns_block_kernel<PARTS>, dim3(l.matrices + adam_blocks), dim3(NSB_THREADS), NSB_SMEM<PARTS>, ex.st, src, g, adam, p);
+        ex.launches += 1;
+        return true;
+    }
     CUtensorMap x128, x64, a128, a64, b128;
     if (g.count > 0 && (!ns_make_map(tc, &x128, ops, (int64_t)2 * PARTS * l.rows_x, l.pitch_x, 128) || !ns_make_map(tc, &x64, ops, (int64_t)2 * PARTS * l.rows_x, l.pitch_x, 64) ||
                         !ns_make_map(tc, &a128, A, (int64_t)PARTS * l.rows_a, l.pitch_a, 128) || !ns_make_map(tc, &a64, A, (int64_t)PARTS * l.rows_a, l.pitch_a, 64) ||

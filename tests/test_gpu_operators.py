@@ -513,3 +513,94 @@ def test_bounded_wait_of_the_products(pkg):
     c.stats()
     assert torch.equal(c.orthogonalize(U), want)
     c.close()
+
+
+# ------------------------------------------------------------------------------------------ matrices of up to 128 x 128, one block each
+def fp32_orthogonalize(U):
+    """The iteration in FP32 matrix products."""
+    X = U if U.shape[0] <= U.shape[1] else U.T
+    X = X / (X.norm() + 1e-7)
+    a, b, c = COEFFS
+    for _ in range(5):
+        A = X @ X.T
+        X = a * X + (b * A + c * (A @ A)) @ X
+    return X if U.shape[0] <= U.shape[1] else X.T
+
+
+@pytest.mark.parametrize("kind", ["rank1", "rank3", "decay", "zero_rows", "spike", "large", "tiny"])
+@pytest.mark.parametrize("rows,cols", [(64, 64), (37, 128), (128, 128), (128, 50)])
+def test_small_orthogonalize_spectra(ctx, rows, cols, kind):
+    """No further from 64 bits than FP32 matrix products are where those miss the tolerance (directions that U lacks)."""
+    g = gen(rows + cols)
+    U = torch.randn(rows, cols, generator=g)
+    if kind in ("rank1", "rank3"):
+        r = int(kind[-1])
+        U = torch.randn(rows, r, generator=g) @ torch.randn(r, cols, generator=g)
+    elif kind == "decay":
+        P, S, Q = torch.linalg.svd(U, full_matrices=False)
+        U = (P * torch.logspace(0, -4, S.numel())) @ Q
+    elif kind == "zero_rows":
+        U[::2] = 0
+    elif kind == "spike":
+        U = torch.zeros(rows, cols)
+        U[17, 33] = 5.0
+    elif kind in ("large", "tiny"):
+        U *= 1e30 if kind == "large" else 1e-30
+    eps = 0.0 if kind == "tiny" else 1e-7
+    want = exact_orthogonalize(U, eps=eps)
+    tol = ORTH_TOL[F32]
+    if kind not in ("large", "tiny"):  # whose squares leave FP32
+        tol = max(tol, rel(fp32_orthogonalize(U), want))
+    assert rel(ctx.orthogonalize(U.to(DEV), eps=eps), want) <= tol
+    assert rel(ctx.orthogonalize(U.to(DEV).to(BF16), eps=eps), exact_orthogonalize(U.to(BF16), eps=eps)) <= ORTH_TOL[BF16]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,cols", [(5, 9), (9, 5), (1, 128), (128, 1), (64, 65), (100, 128), (128, 127)])
+def test_small_orthogonalize_many_strided(ctx, rows, cols, dtype):
+    """More matrices than SMs, rows apart, results into another layout: each the bits of the matrix alone."""
+    n = 300
+    U = torch.randn(n, rows, cols, generator=gen(rows * cols)).to(dtype).to(DEV)
+    want = ctx.orthogonalize(U)
+    assert (torch.stack([torch.as_tensor(rel(want[i], exact_orthogonalize(U[i].cpu()))) for i in range(0, n, 37)]) <= ORTH_TOL[dtype]).all()
+    assert torch.equal(ctx.orthogonalize(U[211]), want[211])
+    wide = torch.zeros(n, rows + 1, cols + 3, dtype=dtype, device=DEV)
+    wide[:, :rows, 1 : cols + 1] = U
+    out = torch.full((n, rows + 2, cols + 5), 7.0, dtype=dtype, device=DEV)
+    ctx.orthogonalize(wide[:, :rows, 1 : cols + 1], out=out[:, 1 : rows + 1, 2 : cols + 2])
+    assert torch.equal(out[:, 1 : rows + 1, 2 : cols + 2], want)
+    out[:, 1 : rows + 1, 2 : cols + 2] = 7.0
+    assert (out == 7.0).all()
+
+
+@pytest.mark.parametrize("shapes", [[(64, 128), (128, 64), (128, 128)], [(1, 1), (127, 3), (3, 127), (64, 64)], [(128, 129), (64, 64)]])
+def test_small_muon_step(ctx, shapes):
+    """All matrices small, and one that is not beside one that is; the stretches between them take Adam steps."""
+    mats, n = layout(shapes, 1500)
+    g = gen(n)
+    p, m, gr = 0.05 * torch.randn(n, generator=g), 1e-3 * torch.randn(n, generator=g), 1e-3 * torch.randn(n, generator=g)
+    v = 1e-6 * torch.rand(n, generator=g)
+    want = exact_muon(p, m, v, gr, mats, 4)
+    d = [x.to(DEV) for x in (p, m, v, gr)]
+    out = tuple(torch.full((n,), 5.0, device=DEV) for _ in range(3))
+    kw = dict(t=4, matrices=mats, weight_decay=0.01, grad_scale=0.5)
+    ctx.muon_step(*d, out=out, **kw)
+    for x, y in zip(out, want):
+        assert rel(x, y) <= 1e-6
+    ctx.muon_step(*d, **kw)
+    for x, y in zip(d[:3], out):
+        assert torch.equal(x, y)
+
+
+def test_bounded_wait_of_the_chained_products(pkg):
+    c = pkg.Context(0)
+    U = torch.randn(160, 160, device=DEV)
+    want = c.orthogonalize(U)
+    c.set_wait_limit(2_000_000, 16)
+    c.orthogonalize(U)
+    with pytest.raises(pkg.LpError) as ei:
+        c.stats()
+    assert ei.value.status == -6
+    c.set_wait_limit(2_000_000_000, 0)
+    assert torch.equal(c.orthogonalize(U), want)
+    c.close()
