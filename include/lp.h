@@ -397,6 +397,7 @@ lp_status lp_embed(lp_ctx *ctx, int32_t table_prec, const void *table, int64_t r
  * accumulate != 0 (grad[v] += ...).  The ids are sorted stably and a row's terms are added in the order of i in FP32, so
  * the result is the same bits in every run; a BF16 gradient is rounded once.
  *   dout[n_ids, width]   : DEVICE, row pitch ld_dout; dout_prec LP_FP32 or LP_BF16
+ *   ids[n_ids]           : DEVICE, fewer than 2^30
  *   grad[rows, width]    : DEVICE, row pitch ld_grad; grad_prec LP_FP32, or LP_BF16 when dout is LP_BF16
  * Takes workspace from the context (it grows to the largest call; growing synchronises).  Does not synchronise otherwise. */
 lp_status lp_embed_grad(lp_ctx *ctx, int32_t dout_prec, const void *dout, int64_t ld_dout, const int32_t *ids, int64_t n_ids, int32_t padding_id, double scale,

@@ -378,25 +378,25 @@ class Context:
     # ---- orthogonalised updates
     def orthogonalize(self, U, steps: int = 5, coeffs: Optional[Sequence[float]] = None, eps: float = 1e-7, out=None):
         """Newton-Schulz orthogonalisation of U [..., rows, cols] (float32 or bfloat16); see lp_orthogonalize."""
-        t = self._torch
         if U.dim() < 2:
             self._refuse("orthogonalize: expected matrices")
         shape = U.shape
-        U3 = U if U.dim() == 3 else U.unsqueeze(0) if U.dim() == 2 else U.reshape(-1, shape[-2], shape[-1])
-        if not U3.is_cuda or U3.device.index != self.device or (U3.shape[2] > 1 and U3.stride(2) != 1):
+        U3 = U if U.dim() <= 3 else U.reshape(-1, shape[-2], shape[-1])
+        if U3.get_device() != self.device or (shape[-1] > 1 and U3.stride(-1) != 1):
             self._refuse(f"orthogonalize: expected matrices with contiguous rows on cuda:{self.device}")
         if out is None:
-            out = t.empty(shape, dtype=U.dtype, device=U.device)
-        elif out.shape != shape or out.dtype != U.dtype or not out.is_cuda or out.dim() > 3 or (shape[-1] > 1 and out.stride(-1) != 1):
+            out = U.new_empty(shape)
+        elif out.shape != shape or out.dtype != U.dtype or out.get_device() != self.device or out.dim() > 3 or (shape[-1] > 1 and out.stride(-1) != 1):
             self._refuse("orthogonalize: out must have the shape, type and device of U, with contiguous rows, and at most three dimensions")
-        O3 = out if out.dim() == 3 else out.unsqueeze(0) if out.dim() == 2 else out.view(-1, shape[-2], shape[-1])
-        batch, rows, cols = U3.shape
-        lds = [x.stride(1) if rows > 1 else cols for x in (U3, O3)]
-        strides = [x.stride(0) if batch > 1 else rows * ld for x, ld in zip((U3, O3), lds)]
+        O3 = out if out.dim() <= 3 else out.view(-1, shape[-2], shape[-1])
+        rows, cols = shape[-2], shape[-1]
+        batch = U3.shape[0] if U3.dim() == 3 else 1
+        ld_u, ld_o = (U3.stride(-2), O3.stride(-2)) if rows > 1 else (cols, cols)
+        stride_u, stride_o = (U3.stride(0), O3.stride(0)) if batch > 1 else (rows * ld_u, rows * ld_o)
         c = (C.c_double * 3)(*coeffs) if coeffs is not None else None
         cur = self._enter(U, U3, out)
-        self._ck(self.lib.lp_orthogonalize(self.h, self._prec(U.dtype, "orthogonalize"), batch, rows, cols, U3.data_ptr(), lds[0], strides[0], steps, c, eps,
-                                           O3.data_ptr(), lds[1], strides[1]))
+        self._ck(self.lib.lp_orthogonalize(self.h, self._prec(U.dtype, "orthogonalize"), batch, rows, cols, U3.data_ptr(), ld_u, stride_u, steps, c, eps,
+                                           O3.data_ptr(), ld_o, stride_o))
         self._leave(cur)
         return out
 
