@@ -770,6 +770,8 @@ static size_t few_bytes(int64_t N)
     return n * sizeof(uint32_t);
 }
 
+constexpr int64_t EG_CLEAR_BYTES = (int64_t)64 << 20;
+
 struct EmbedGradScratch {
     EmbedSort sort;
     float *head = nullptr, *tail = nullptr;
@@ -787,11 +789,19 @@ static void embed_grad_rows(Exec &ex, const TD *dout, int64_t ldd, const int *id
     // against 27).  Where a block's range of rows is wide, ids that lie together land in few blocks (8,192 ids inside 5,000 of
     // 2.9 M rows: 300 us against 150; 2,048: 137 against 150), so the limit is lower there.
     const int R = (int)std::min<int64_t>(EGS_MAX_ROWS, std::max<int64_t>(4, ceil_div64(V, 148 * 4)));
-    if (N > 0 && N <= (R <= 1024 ? EGS_MAX_IDS : EGS_MAX_IDS / 4)) {
+    const bool few = N > 0 && N <= (R <= 1024 ? EGS_MAX_IDS : EGS_MAX_IDS / 4);
+    // A large dense gradient is cleared as a whole first where the rows without ids are nearly all of it and stores of a row are slow
+    // or all that there is to do.  Few ids: 937,500 x 320 floats, 550 ids 201 -> 178 us, 1,087,079 x 46 BF16, 819 ids 86 -> 25, but with
+    // a 53rd of 218,261 rows named 30 -> 35 and a 9th of 72,765 40 -> 57, since there the blocks' own sums hide the zeros.  Sorted ids,
+    // pieces of four bytes: 1,654,733 x 37 floats, 227,613 ids 147 -> 127, but pieces of 16 bytes: 701,850 x 64, 96,035 ids 71 -> 82.
+    const int64_t grad_bytes = V * D * (int64_t)sizeof(TG);
+    const bool clear = !accumulate && N > 0 && ldg == D && grad_bytes >= EG_CLEAR_BYTES && (few ? 64 * N <= V : VE * sizeof(TG) <= 4 && 4 * N <= V);
+    if (clear) cudaMemsetAsync(grad, 0, (size_t)grad_bytes, ex.st);
+    if (few) {
         if (few_bytes(N) > 8192)  // beside the static arrays it may pass the default limit; if refused, the launch reports the error
             cudaFuncSetAttribute(embed_grad_few_kernel<TD, TG, VE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)few_bytes(EGS_MAX_IDS));
         launch_dep(embed_grad_few_kernel<TD, TG, VE>, dim3((unsigned)ceil_div64(V, R)), dim3(EG_THREADS), few_bytes(N), ex.st, ids, (int)N, V, padding, R, dout, ldd, D, scale, grad, ldg,
-                   accumulate, G, err);
+                   accumulate || clear, G, err);
         ex.launches += 1;
         return;
     }
@@ -802,7 +812,7 @@ static void embed_grad_rows(Exec &ex, const TD *dout, int64_t ldd, const int *id
         return;
     }
     launch_dep(embed_hist_kernel, dim3(s.tiles), dim3(EG_THREADS), 0, ex.st, ids, N, V, padding, s, err);
-    const int zero_blocks = accumulate ? 0 : (int)std::min<int64_t>(ceil_div64(ceil_div64(V, s.passes), 256), 148 * 8);
+    const int zero_blocks = accumulate || clear ? 0 : (int)std::min<int64_t>(ceil_div64(ceil_div64(V, s.passes), 256), 148 * 8);
     for (int p = 0; p < s.passes; ++p)
         launch_dep(embed_sort_kernel<TG, VE>, dim3(s.tiles + zero_blocks), dim3(EG_THREADS), 0, ex.st, ids, N, V, padding, s, p, zero_blocks, D, grad, ldg, G, err);
     const uint32_t *keys = s.keys[(s.passes - 1) & 1], *vals = s.vals[(s.passes - 1) & 1];

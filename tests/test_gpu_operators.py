@@ -604,3 +604,26 @@ def test_bounded_wait_of_the_chained_products(pkg):
     c.set_wait_limit(2_000_000_000, 0)
     assert torch.equal(c.orthogonalize(U), want)
     c.close()
+
+
+@pytest.mark.parametrize("rows,width,n,dtype", [(300_000, 64, 40, F32), (1_200_000, 33, 700, BF16), (600_000, 37, 20_000, F32), (1_100_001, 31, 30_001, BF16)])
+def test_embed_grad_of_a_large_sparse_table(ctx, rows, width, n, dtype):
+    """Large gradients that few ids name: the bits of the same call with rows apart, which clears row by row; nothing stale stays."""
+    g = gen(n)
+    ids = torch.randint(0, rows, (n,), generator=g, dtype=torch.int32)
+    ids[: n // 3] = ids[0]
+    ids[-1] = rows - 1
+    dout = torch.randn(n, width, generator=g).to(dtype).to(DEV)
+    ids = ids.to(DEV)
+    grad = torch.full((rows, width), float("nan"), dtype=dtype, device=DEV)
+    ctx.embed_grad(dout, ids, rows, scale=2.0, grad=grad)
+    apart = torch.full((rows, width + 1), float("nan"), dtype=dtype, device=DEV)
+    ctx.embed_grad(dout, ids, rows, scale=2.0, grad=apart[:, :width])
+    assert torch.equal(grad, apart[:, :width])
+    named = torch.zeros(rows, dtype=torch.bool, device=DEV)
+    named[ids.long()] = True
+    assert (grad[~named] == 0).all()
+    want = torch.zeros(rows, width, dtype=torch.float64, device=DEV).index_add_(0, ids.long(), 2.0 * dout.double())[named]
+    size = torch.zeros(rows, width, dtype=torch.float64, device=DEV).index_add_(0, ids.long(), 2.0 * dout.double().abs())[named]
+    # FP32 sums of k terms: k 2^-24 of the sum of magnitudes, and one rounding to BF16
+    assert ((grad[named].double() - want).abs() <= n * 2.0**-24 * size + (2.0**-8 * want.abs() if dtype == BF16 else 0.0)).all()
