@@ -200,7 +200,7 @@ struct EmbedSort {
     int passes = 0, bits = 0;      // bits per pass
     int tiles = 0;
     uint32_t *keys[2] = {nullptr, nullptr}, *vals[2] = {nullptr, nullptr};
-    uint8_t *named = nullptr;      // [rows] row v receives a gradient      } cleared together before the call's first kernel
+    uint8_t *named = nullptr;      // [rows] row v receives a gradient, or null } cleared together before the call's first kernel
     unsigned *hist = nullptr;      // [passes][256] keys per digit        }
     unsigned *ticket = nullptr;    // [passes]                            }
     unsigned *status = nullptr;    // [passes][tiles][256], cleared by the first kernel
@@ -228,8 +228,9 @@ __global__ void __launch_bounds__(EG_THREADS) embed_hist_kernel(const int *__res
     for (int r = 0; r < ES_ITEMS; ++r) {
         if ((int64_t)blockIdx.x * ES_TILE + r * EG_THREADS + threadIdx.x < N) {
             const uint32_t key = embed_key(id[r], V, padding);
-            if (key < (uint32_t)V) s.named[key] = 1;
-            else if (id[r] != padding || padding == LP_NO_PADDING) atomicOr(err, 1);
+            if (key < (uint32_t)V) {
+                if (s.named) s.named[key] = 1;
+            } else if (id[r] != padding || padding == LP_NO_PADDING) atomicOr(err, 1);
             for (int p = 0; p < s.passes; ++p) atomicAdd(&h[p][(key >> (p * s.bits)) & mask], 1u);
         }
     }
@@ -441,7 +442,7 @@ __global__ void __launch_bounds__(EG_THREADS, 3) embed_grad_sum_kernel(const uin
 #pragma unroll
         for (int u = 0; u < U; ++u) store_elems<float, VE>(to + threadIdx.x * E + u * VE, acc + u * VE);
     };
-    for (int c0 = 0; c0 < D; c0 += U * G * VE) {
+    for (int c0 = blockIdx.y * U * G * VE; c0 < D; c0 += gridDim.y * U * G * VE) {
         const int c = c0 + gl * VE;
         auto put = [&](float *row, const float *acc) {
 #pragma unroll
@@ -563,7 +564,7 @@ __global__ void __launch_bounds__(EG_THREADS) embed_grad_join_kernel(const uint3
     for (int i = g; i < EG_JOIN; i += groups) {
         const int64_t span = first + i, last = last_s[i];
         if (last < 0 || last - span > EG_SHORT) continue;
-        for (int c = gl * VE; c < D; c += G * VE) {
+        for (int c = (blockIdx.y * G + gl) * VE; c < D; c += gridDim.y * G * VE) {
             float acc[VE];
             load_elems<float, VE>(tail + span * D + c, acc);
             for (int64_t q = span + 1; q <= last; ++q) {
@@ -579,7 +580,7 @@ __global__ void __launch_bounds__(EG_THREADS) embed_grad_join_kernel(const uint3
         const int64_t span = first + i, last = last_s[i];
         if (last < 0 || last - span <= EG_SHORT) continue;
         const int64_t share = (last - span + EG_PIECES - 1) / EG_PIECES, q0 = span + 1 + g * share, q1 = g < EG_PIECES ? min(last + 1, q0 + share) : q0;
-        for (int c0 = 0; c0 < D; c0 += G * VE) {
+        for (int c0 = blockIdx.y * G * VE; c0 < D; c0 += gridDim.y * G * VE) {
             const int c = c0 + gl * VE;
             float acc[VE];
 #pragma unroll
@@ -794,9 +795,13 @@ static void embed_grad_rows(Exec &ex, const TD *dout, int64_t ldd, const int *id
     // or all that there is to do.  Few ids: 937,500 x 320 floats, 550 ids 201 -> 178 us, 1,087,079 x 46 BF16, 819 ids 86 -> 25, but with
     // a 53rd of 218,261 rows named 30 -> 35 and a 9th of 72,765 40 -> 57, since there the blocks' own sums hide the zeros.  Sorted ids,
     // pieces of four bytes: 1,654,733 x 37 floats, 227,613 ids 147 -> 127, but pieces of 16 bytes: 701,850 x 64, 96,035 ids 71 -> 82.
+    // A gradient of far fewer rows than ids is cleared too: noting the named rows would take a store per id to a few hot lines
+    // (849,408 ids on 2,749 rows: counts and notes 96 us, counts alone 6; in all 229 us and 139).
     const int64_t grad_bytes = V * D * (int64_t)sizeof(TG);
-    const bool clear = !accumulate && N > 0 && ldg == D && grad_bytes >= EG_CLEAR_BYTES && (few ? 64 * N <= V : VE * sizeof(TG) <= 4 && 4 * N <= V);
-    if (clear) cudaMemsetAsync(grad, 0, (size_t)grad_bytes, ex.st);
+    const bool sparse = ldg == D && grad_bytes >= EG_CLEAR_BYTES && (few ? 64 * N <= V : VE * sizeof(TG) <= 4 && 4 * N <= V), dense = !few && 4 * V <= N;
+    const bool clear = !accumulate && N > 0 && (sparse || dense);
+    if (clear && ldg == D) cudaMemsetAsync(grad, 0, (size_t)grad_bytes, ex.st);
+    else if (clear) cudaMemset2DAsync(grad, (size_t)ldg * sizeof(TG), 0, (size_t)D * sizeof(TG), (size_t)V, ex.st);
     if (few) {
         if (few_bytes(N) > 8192)  // beside the static arrays it may pass the default limit; if refused, the launch reports the error
             cudaFuncSetAttribute(embed_grad_few_kernel<TD, TG, VE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)few_bytes(EGS_MAX_IDS));
@@ -811,15 +816,19 @@ static void embed_grad_rows(Exec &ex, const TD *dout, int64_t ldd, const int *id
         ex.launches += 1;
         return;
     }
-    launch_dep(embed_hist_kernel, dim3(s.tiles), dim3(EG_THREADS), 0, ex.st, ids, N, V, padding, s, err);
+    EmbedSort counts = s;
+    if (accumulate || clear) counts.named = nullptr;  // nobody asks
+    launch_dep(embed_hist_kernel, dim3(s.tiles), dim3(EG_THREADS), 0, ex.st, ids, N, V, padding, counts, err);
     const int zero_blocks = accumulate || clear ? 0 : (int)std::min<int64_t>(ceil_div64(ceil_div64(V, s.passes), 256), 148 * 8);
     for (int p = 0; p < s.passes; ++p)
         launch_dep(embed_sort_kernel<TG, VE>, dim3(s.tiles + zero_blocks), dim3(EG_THREADS), 0, ex.st, ids, N, V, padding, s, p, zero_blocks, D, grad, ldg, G, err);
     const uint32_t *keys = s.keys[(s.passes - 1) & 1], *vals = s.vals[(s.passes - 1) & 1];
-    const int64_t spans = ceil_div64(N, EG_SPAN);
-    launch_dep(embed_grad_sum_kernel<TD, TG, VE>, dim3((unsigned)ceil_div64(spans, groups / EG_PIECES)), dim3(EG_THREADS), 0, ex.st, keys, vals, N, V, dout, ldd, D, scale, grad,
+    const int64_t spans = ceil_div64(N, EG_SPAN), sums = ceil_div64(spans, groups / EG_PIECES), joins = ceil_div64(spans, EG_JOIN);
+    // few blocks share out the columns of wide rows as well (13,413 ids, rows of 450 floats: sums 40 -> 14 us, joins 16 -> 8)
+    auto split = [&](int64_t blocks, int columns) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div64(D, columns), 148 * 4 / blocks)); };
+    launch_dep(embed_grad_sum_kernel<TD, TG, VE>, dim3((unsigned)sums, split(sums, PIECES_PER_LANE<VE> * G * VE)), dim3(EG_THREADS), 0, ex.st, keys, vals, N, V, dout, ldd, D, scale, grad,
                ldg, accumulate, sc.head, sc.tail, G);
-    launch_dep(embed_grad_join_kernel<TG, VE>, dim3((unsigned)ceil_div64(spans, EG_JOIN)), dim3(EG_THREADS), 0, ex.st, keys, N, V, D, scale, grad, ldg, accumulate, sc.head,
+    launch_dep(embed_grad_join_kernel<TG, VE>, dim3((unsigned)joins, split(joins, G * VE)), dim3(EG_THREADS), 0, ex.st, keys, N, V, D, scale, grad, ldg, accumulate, sc.head,
                sc.tail, G);
     ex.launches += 3 + s.passes;
 }

@@ -627,3 +627,20 @@ def test_embed_grad_of_a_large_sparse_table(ctx, rows, width, n, dtype):
     size = torch.zeros(rows, width, dtype=torch.float64, device=DEV).index_add_(0, ids.long(), 2.0 * dout.double().abs())[named]
     # FP32 sums of k terms: k 2^-24 of the sum of magnitudes, and one rounding to BF16
     assert ((grad[named].double() - want).abs() <= n * 2.0**-24 * size + (2.0**-8 * want.abs() if dtype == BF16 else 0.0)).all()
+
+
+@pytest.mark.parametrize("rows,width,n,dtype", [(300, 33, 20_000, F32), (2000, 450, 9_001, BF16), (1, 700, 8_500, F32), (2200, 64, 8_800, BF16)])
+def test_embed_grad_of_a_small_dense_table(ctx, rows, width, n, dtype):
+    """Many more ids than rows, which clears everything first: stale rows go, what lies between the rows stays."""
+    g = gen(rows + n)
+    ids = torch.randint(0, max(1, rows - 7), (n,), generator=g, dtype=torch.int32).to(DEV)  # the last rows have no ids
+    dout = torch.randn(n, width, generator=g).to(dtype).to(DEV)
+    grad = torch.full((rows, width), float("nan"), dtype=dtype, device=DEV)
+    ctx.embed_grad(dout, ids, rows, scale=0.5, grad=grad)
+    apart = torch.full((rows, width + 5), 3.0, dtype=dtype, device=DEV)
+    ctx.embed_grad(dout, ids, rows, scale=0.5, grad=apart[:, 2 : width + 2])
+    assert torch.equal(apart[:, 2 : width + 2], grad)
+    assert (apart[:, :2] == 3.0).all() and (apart[:, width + 2 :] == 3.0).all()
+    want = torch.zeros(rows, width, dtype=torch.float64, device=DEV).index_add_(0, ids.long(), 0.5 * dout.double())
+    size = torch.zeros(rows, width, dtype=torch.float64, device=DEV).index_add_(0, ids.long(), 0.5 * dout.double().abs())
+    assert ((grad.double() - want).abs() <= n * 2.0**-24 * size + (2.0**-8 * want.abs() if dtype == BF16 else 0.0)).all()
