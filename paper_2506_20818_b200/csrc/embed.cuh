@@ -187,10 +187,13 @@ constexpr int EG_SHORT = 16;  // spans up to which a run is added up by one grou
 // Sorting.  Least significant digit first, up to eight bits a pass, one launch a pass: a block takes a tile of 2,048 pairs
 // (by ticket, so it only waits for tiles that are running), ranks them by digit, finds what earlier tiles hold of each digit by
 // looking back over their published counts (eight at a time; thread d looks for digit d), and writes its pairs in digit order.
-// The pass is bound by latency (1,966,080 pairs: 29 to 38 us, 200,000: 10 to 12), so the rows that no id names are set to zero by
-// further blocks of the same launches.  Tried and no faster for 1,966,080 ids (473 us): nine-bit digits (495 us, 200,000 ids 78
-// for 80), tiles of 4,096 pairs (481; 86 for 80), 148 to 592 blocks for the zeros in place of up to 1,184 (476 to 572), fewer and
-// longer blocks for the digit counts (474 to 476).
+// The pass is bound by latency (1,966,080 pairs: 29 to 38 us, 200,000: 10 to 12).  Tried and no faster: nine-bit digits (200,000 ids
+// 78 us for 80 in all, 1,966,080 ids 495 for 473), tiles of 4,096 pairs (86 for 80, 481 for 473).  The rows that no id
+// names were once set to zero by further blocks of these launches: with 1,966,080 ids that hides nothing (234 us together, 101 and
+// 110 alone), with fewer ids a part (96,035 ids, 701,850 rows of 64: 70 us so, 76 now), but noting the named rows before the sort
+// takes a store per id, and they queue up at the lines of the hubs (849,408 ids on 2,749 rows: 96 us with the counts, 6 without).
+// So the kernel that adds up the sorted rows notes them, once per run of equal ids, and the last launch sets the others to
+// zero (200,001 ids: 80 -> 76 us; 849,408 on 2,749 rows: 229 -> 139).
 constexpr int ES_ITEMS = 8;
 constexpr int ES_TILE = EG_THREADS * ES_ITEMS;
 constexpr int ES_DIGITS = 256;
@@ -200,7 +203,7 @@ struct EmbedSort {
     int passes = 0, bits = 0;      // bits per pass
     int tiles = 0;
     uint32_t *keys[2] = {nullptr, nullptr}, *vals[2] = {nullptr, nullptr};
-    uint8_t *named = nullptr;      // [rows] row v receives a gradient, or null } cleared together before the call's first kernel
+    uint8_t *named = nullptr;      // [rows] row v receives a gradient      } cleared together before the call's first kernel
     unsigned *hist = nullptr;      // [passes][256] keys per digit        }
     unsigned *ticket = nullptr;    // [passes]                            }
     unsigned *status = nullptr;    // [passes][tiles][256], cleared by the first kernel
@@ -228,9 +231,7 @@ __global__ void __launch_bounds__(EG_THREADS) embed_hist_kernel(const int *__res
     for (int r = 0; r < ES_ITEMS; ++r) {
         if ((int64_t)blockIdx.x * ES_TILE + r * EG_THREADS + threadIdx.x < N) {
             const uint32_t key = embed_key(id[r], V, padding);
-            if (key < (uint32_t)V) {
-                if (s.named) s.named[key] = 1;
-            } else if (id[r] != padding || padding == LP_NO_PADDING) atomicOr(err, 1);
+            if (key == (uint32_t)V && (id[r] != padding || padding == LP_NO_PADDING)) atomicOr(err, 1);
             for (int p = 0; p < s.passes; ++p) atomicAdd(&h[p][(key >> (p * s.bits)) & mask], 1u);
         }
     }
@@ -239,18 +240,18 @@ __global__ void __launch_bounds__(EG_THREADS) embed_hist_kernel(const int *__res
         if (h[p][threadIdx.x]) atomicAdd(s.hist + p * ES_DIGITS + threadIdx.x, h[p][threadIdx.x]);
 }
 
-// zero rows that no id names, of the groups of 32 rows [w0, w1); `blocks` blocks share the work.  A warp reads the flags of 32
+// sets the rows that no id names to zero; `blocks` blocks share the work.  A warp reads the flags of 32
 // rows at once and then only stores (a load per row: 218 us for 2.9 M rows of 512 bytes, this way 110 us)
 template <typename TG, int VE>
-LP_DEVINL void embed_zero_rows(const uint8_t *named, int64_t w0, int64_t w1, int64_t V, int D, TG *grad, int64_t ldg, int G, int block, int blocks)
+LP_DEVINL void embed_zero_rows(const uint8_t *named, int64_t V, int D, TG *grad, int64_t ldg, int G, int block, int blocks)
 {
     const int lane = threadIdx.x & 31, gl = lane & (G - 1), sub = lane / G, step = 32 / G;
-    const int64_t warps = (int64_t)blocks * (EG_THREADS / 32);
+    const int64_t warps = (int64_t)blocks * (EG_THREADS / 32), w1 = (V + 31) / 32;
     constexpr int ZE = VE * (int)sizeof(TG) > 16 ? 16 / (int)sizeof(TG) : VE;  // neighbouring lanes store neighbouring 16 bytes
     float z[ZE];
 #pragma unroll
     for (int t = 0; t < ZE; ++t) z[t] = 0.f;
-    int64_t w = w0 + (int64_t)block * (EG_THREADS / 32) + (threadIdx.x >> 5);
+    int64_t w = (int64_t)block * (EG_THREADS / 32) + (threadIdx.x >> 5);
     uint32_t flag = w < w1 && w * 32 + lane < V ? named[w * 32 + lane] : 0u;
     while (w < w1) {
         const uint32_t next = w + warps < w1 && (w + warps) * 32 + lane < V ? named[(w + warps) * 32 + lane] : 0u;
@@ -266,20 +267,9 @@ LP_DEVINL void embed_zero_rows(const uint8_t *named, int64_t w0, int64_t w1, int
     }
 }
 
-template <typename TG, int VE>
-__global__ void __launch_bounds__(EG_THREADS) embed_sort_kernel(const int *__restrict__ ids, int64_t N, int64_t V, int padding, const EmbedSort s, int pass, int zero_blocks,
-                                                                int D, TG *__restrict__ grad, int64_t ldg, int G, int *__restrict__ err)
+__global__ void __launch_bounds__(EG_THREADS) embed_sort_kernel(const int *__restrict__ ids, int64_t N, int64_t V, int padding, const EmbedSort s, int pass, int *__restrict__ err)
 {
     LP_DEP_ENTER();
-    // the two kinds of blocks alternate, so that every SM has both the latency of the sort and the bandwidth of the stores to fill
-    const int both = 2 * min(s.tiles, zero_blocks), b = blockIdx.x;
-    const bool zero = b < both ? (b & 1) != 0 : zero_blocks > s.tiles;
-    if (zero) {
-        const int64_t words = (V + 31) / 32;
-        embed_zero_rows<TG, VE>(s.named, words * pass / s.passes, words * (pass + 1) / s.passes, V, D, grad, ldg, G,
-                                b < both ? b >> 1 : b - both / 2, zero_blocks);
-        return;
-    }
     __shared__ int warp_count[EG_THREADS / 32][ES_DIGITS];
     __shared__ int start_s[ES_DIGITS];               // where a digit begins in the tile's own order
     __shared__ int out_s[ES_DIGITS];                 // ... and its first place in the output, less start_s
@@ -415,7 +405,7 @@ template <typename TG, int VE> LP_DEVINL void embed_grad_store(TG *p, const floa
 template <typename TD, typename TG, int VE>
 __global__ void __launch_bounds__(EG_THREADS, 3) embed_grad_sum_kernel(const uint32_t *__restrict__ keys, const uint32_t *__restrict__ vals, int64_t N, int64_t V,
                                                                     const TD *__restrict__ dout, int64_t ldd, int D, float scale, TG *__restrict__ grad,
-                                                                    int64_t ldg, int accumulate, float *__restrict__ head, float *__restrict__ tail, int G)
+                                                                    int64_t ldg, int accumulate, float *__restrict__ head, float *__restrict__ tail, uint8_t *__restrict__ named, int G)
 {
     LP_DEP_ENTER();
     constexpr int U = PIECES_PER_LANE<VE>, E = U * VE;
@@ -435,6 +425,11 @@ __global__ void __launch_bounds__(EG_THREADS, 3) embed_grad_sum_kernel(const uin
         val_s[i] = vals[b0 + i];
     }
     __syncthreads();
+    if (named && blockIdx.y == 0)  // rows with a gradient, at the first id of each
+        for (int i = threadIdx.x; i < ids; i += EG_THREADS) {
+            const uint32_t key = key_s[i];
+            if (key < (uint32_t)V && (i > 0 ? key_s[i - 1] != key : b0 == 0 || keys[b0 - 1] != key)) named[key] = 1;
+        }
     const uint32_t *ck = key_s + group * EG_CHUNK, *cv = val_s + group * EG_CHUNK;
     const uint32_t first = count > 0 ? ck[0] : none;
     // E sums of this lane to shared memory, to a row of FP32 partial sums, to the gradient
@@ -529,12 +524,17 @@ __global__ void __launch_bounds__(EG_THREADS, 3) embed_grad_sum_kernel(const uin
 
 // Runs that cross spans: for every span in which such a run begins, grad[run] = tail[span] + head[span + 1] + ...  A block
 // looks at EG_JOIN spans; runs over few spans are added up by a group of lanes each, the others by EG_PIECES groups that
-// take equal stretches.
+// take equal stretches.  Blocks from `joins` on set the rows that no id names to zero meanwhile: the joins are a chain of loads.
 template <typename TG, int VE>
 __global__ void __launch_bounds__(EG_THREADS) embed_grad_join_kernel(const uint32_t *__restrict__ keys, int64_t N, int64_t V, int D, float scale, TG *__restrict__ grad,
-                                                                     int64_t ldg, int accumulate, const float *__restrict__ head, const float *__restrict__ tail, int G)
+                                                                     int64_t ldg, int accumulate, const float *__restrict__ head, const float *__restrict__ tail, const uint8_t *__restrict__ named,
+                                                                     int joins, int G)
 {
     LP_DEP_ENTER();
+    if ((int)blockIdx.x >= joins) {
+        embed_zero_rows<TG, VE>(named, V, D, grad, ldg, G, (blockIdx.x - joins) * gridDim.y + blockIdx.y, (gridDim.x - joins) * gridDim.y);
+        return;
+    }
     __shared__ __align__(16) float part_s[EG_THREADS * VE];
     __shared__ uint32_t run_s[EG_JOIN];
     __shared__ int64_t last_s[EG_JOIN];  // last span of the run that begins in span i and goes on; -1: none
@@ -622,7 +622,7 @@ template <typename TG, int VE>
 __global__ void __launch_bounds__(EG_THREADS) embed_grad_zero_kernel(const uint8_t *__restrict__ named, int64_t V, int D, TG *__restrict__ grad, int64_t ldg, int G)
 {
     LP_DEP_ENTER();
-    embed_zero_rows<TG, VE>(named, 0, (V + 31) / 32, V, D, grad, ldg, G, blockIdx.x, gridDim.x);
+    embed_zero_rows<TG, VE>(named, V, D, grad, ldg, G, blockIdx.x, gridDim.x);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -795,13 +795,9 @@ static void embed_grad_rows(Exec &ex, const TD *dout, int64_t ldd, const int *id
     // or all that there is to do.  Few ids: 937,500 x 320 floats, 550 ids 201 -> 178 us, 1,087,079 x 46 BF16, 819 ids 86 -> 25, but with
     // a 53rd of 218,261 rows named 30 -> 35 and a 9th of 72,765 40 -> 57, since there the blocks' own sums hide the zeros.  Sorted ids,
     // pieces of four bytes: 1,654,733 x 37 floats, 227,613 ids 147 -> 127, but pieces of 16 bytes: 701,850 x 64, 96,035 ids 71 -> 82.
-    // A gradient of far fewer rows than ids is cleared too: noting the named rows would take a store per id to a few hot lines
-    // (849,408 ids on 2,749 rows: counts and notes 96 us, counts alone 6; in all 229 us and 139).
     const int64_t grad_bytes = V * D * (int64_t)sizeof(TG);
-    const bool sparse = ldg == D && grad_bytes >= EG_CLEAR_BYTES && (few ? 64 * N <= V : VE * sizeof(TG) <= 4 && 4 * N <= V), dense = !few && 4 * V <= N;
-    const bool clear = !accumulate && N > 0 && (sparse || dense);
-    if (clear && ldg == D) cudaMemsetAsync(grad, 0, (size_t)grad_bytes, ex.st);
-    else if (clear) cudaMemset2DAsync(grad, (size_t)ldg * sizeof(TG), 0, (size_t)D * sizeof(TG), (size_t)V, ex.st);
+    const bool clear = !accumulate && N > 0 && ldg == D && grad_bytes >= EG_CLEAR_BYTES && (few ? 64 * N <= V : VE * sizeof(TG) <= 4 && 4 * N <= V);
+    if (clear) cudaMemsetAsync(grad, 0, (size_t)grad_bytes, ex.st);
     if (few) {
         if (few_bytes(N) > 8192)  // beside the static arrays it may pass the default limit; if refused, the launch reports the error
             cudaFuncSetAttribute(embed_grad_few_kernel<TD, TG, VE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)few_bytes(EGS_MAX_IDS));
@@ -816,20 +812,20 @@ static void embed_grad_rows(Exec &ex, const TD *dout, int64_t ldd, const int *id
         ex.launches += 1;
         return;
     }
-    EmbedSort counts = s;
-    if (accumulate || clear) counts.named = nullptr;  // nobody asks
-    launch_dep(embed_hist_kernel, dim3(s.tiles), dim3(EG_THREADS), 0, ex.st, ids, N, V, padding, counts, err);
-    const int zero_blocks = accumulate || clear ? 0 : (int)std::min<int64_t>(ceil_div64(ceil_div64(V, s.passes), 256), 148 * 8);
+    launch_dep(embed_hist_kernel, dim3(s.tiles), dim3(EG_THREADS), 0, ex.st, ids, N, V, padding, s, err);
     for (int p = 0; p < s.passes; ++p)
-        launch_dep(embed_sort_kernel<TG, VE>, dim3(s.tiles + zero_blocks), dim3(EG_THREADS), 0, ex.st, ids, N, V, padding, s, p, zero_blocks, D, grad, ldg, G, err);
+        launch_dep(embed_sort_kernel, dim3(s.tiles), dim3(EG_THREADS), 0, ex.st, ids, N, V, padding, s, p, err);
+    uint8_t *named = accumulate || clear ? nullptr : s.named;
+    const int zero_blocks = named ? (int)std::min<int64_t>(ceil_div64(V, 256), 148 * 8) : 0;
     const uint32_t *keys = s.keys[(s.passes - 1) & 1], *vals = s.vals[(s.passes - 1) & 1];
     const int64_t spans = ceil_div64(N, EG_SPAN), sums = ceil_div64(spans, groups / EG_PIECES), joins = ceil_div64(spans, EG_JOIN);
     // few blocks share out the columns of wide rows as well (13,413 ids, rows of 450 floats: sums 40 -> 14 us, joins 16 -> 8)
     auto split = [&](int64_t blocks, int columns) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div64(D, columns), 148 * 4 / blocks)); };
     launch_dep(embed_grad_sum_kernel<TD, TG, VE>, dim3((unsigned)sums, split(sums, PIECES_PER_LANE<VE> * G * VE)), dim3(EG_THREADS), 0, ex.st, keys, vals, N, V, dout, ldd, D, scale, grad,
-               ldg, accumulate, sc.head, sc.tail, G);
-    launch_dep(embed_grad_join_kernel<TG, VE>, dim3((unsigned)joins, split(joins, G * VE)), dim3(EG_THREADS), 0, ex.st, keys, N, V, D, scale, grad, ldg, accumulate, sc.head,
-               sc.tail, G);
+               ldg, accumulate, sc.head, sc.tail, named, G);
+    const unsigned ways = split(joins, G * VE);
+    launch_dep(embed_grad_join_kernel<TG, VE>, dim3((unsigned)joins + ceil_div64(zero_blocks, ways), ways), dim3(EG_THREADS), 0, ex.st, keys, N, V, D, scale, grad, ldg, accumulate, sc.head,
+               sc.tail, named, (int)joins, G);
     ex.launches += 3 + s.passes;
 }
 
