@@ -304,7 +304,9 @@ lp_status lp_get_stats(lp_ctx *ctx, lp_stats *out);
  * usable.  limit_ns (default 2e9, allowed 1e3 .. 6e10) sets that bound for later launches of this context.
  * overdeclare_bytes (normally 0; a multiple of 16, at most 65536) is a self-test of that path: the NEXT tensor-core
  * launch announces that many bytes more than it copies on its first barrier, so every copy lands but the barrier
- * never completes and the waits run into the limit.  Nothing faults and nothing is left running. */
+ * never completes and the waits run into the limit.  Nothing faults and nothing is left running.
+ * The same limit bounds the waits of the sort inside lp_embed_grad (a tile of ids for the tiles before it), and a sort that is
+ * launched before the next tensor-core launch takes the self-test: its first tile publishes nothing. */
 lp_status lp_set_wait_limit(lp_ctx *ctx, uint64_t limit_ns, int32_t overdeclare_bytes);
 
 /* ---- per-kernel timing (roofline measurement) ------------------------------------------------ */

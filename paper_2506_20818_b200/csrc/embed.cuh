@@ -185,8 +185,9 @@ constexpr int EG_JOIN = 32;   // spans that one block looks at for runs to join
 constexpr int EG_SHORT = 16;  // spans up to which a run is added up by one group of lanes
 
 // Sorting.  Least significant digit first, up to eight bits a pass, one launch a pass: a block takes a tile of 2,048 pairs
-// (by ticket, so it only waits for tiles that are running), ranks them by digit, finds what earlier tiles hold of each digit by
-// looking back over their published counts (eight at a time; thread d looks for digit d), and writes its pairs in digit order.
+// (by ticket, so it only waits for tiles that are running, and not beyond the context's limit), ranks them by digit, finds what
+// earlier tiles hold of each digit by looking back over their published counts (eight at a time; thread d looks for digit d), and
+// writes its pairs in digit order.
 // The pass is bound by latency (1,966,080 pairs: 29 to 38 us, 200,000: 10 to 12).  Tried and no faster: nine-bit digits (200,000 ids
 // 78 us for 80 in all, 1,966,080 ids 495 for 473), tiles of 4,096 pairs (86 for 80, 481 for 473).  The rows that no id
 // names were once set to zero by further blocks of these launches: with 1,966,080 ids that hides nothing (234 us together, 101 and
@@ -207,6 +208,8 @@ struct EmbedSort {
     unsigned *hist = nullptr;      // [passes][256] keys per digit        }
     unsigned *ticket = nullptr;    // [passes]                            }
     unsigned *status = nullptr;    // [passes][tiles][256], cleared by the first kernel
+    unsigned long long wait_ns = 0;  // limit of a tile's wait for the tiles before it
+    int withhold = 0;              // self-test of that limit: the first tile of the first pass publishes nothing
 };
 
 // the key of an id: the id, or V (sorted behind every row) for the padding id and for ids outside the table
@@ -318,7 +321,8 @@ __global__ void __launch_bounds__(EG_THREADS) embed_sort_kernel(const int *__res
         total += c;
     }
     unsigned *mine = s.status + ((int64_t)pass * s.tiles + tile) * ES_DIGITS + d;
-    asm volatile("st.relaxed.gpu.global.u32 [%0], %1;" ::"l"(mine), "r"((tile == 0 ? ES_PREFIX : ES_SUM) | (unsigned)total) : "memory");
+    if (!s.withhold || tile > 0 || pass > 0)
+        asm volatile("st.relaxed.gpu.global.u32 [%0], %1;" ::"l"(mine), "r"((tile == 0 ? ES_PREFIX : ES_SUM) | (unsigned)total) : "memory");
     int sum;
     const int start = block_exclusive_scan_256(total, sw, &sum);
     const int digit_base = block_exclusive_scan_256((int)s.hist[pass * ES_DIGITS + d], sw, &sum);
@@ -351,7 +355,8 @@ __global__ void __launch_bounds__(EG_THREADS) embed_sort_kernel(const int *__res
                 unsigned long long now;
                 asm volatile("mov.u64 %0, %globaltimer;" : "=l"(now));
                 if (t0 == 0) t0 = now;
-                else if (now - t0 > 2000000000ull) {  // two seconds: give up, report, carry on (the places stay inside the arrays)
+                else if (now - t0 > s.wait_ns) {  // give up, report, carry on: places outside the arrays are not written, and places that
+                                                  // nobody writes hold anything, which the sums check before they use it
                     atomicOr(err, 2);
                     done = true;
                 }
@@ -421,8 +426,9 @@ __global__ void __launch_bounds__(EG_THREADS, 3) embed_grad_sum_kernel(const uin
     const int64_t b0 = (int64_t)blockIdx.x * (EG_THREADS / G) * EG_CHUNK;
     const int ids = (int)min((int64_t)(EG_THREADS / G) * EG_CHUNK, N - b0);
     for (int i = threadIdx.x; i < ids; i += EG_THREADS) {
-        key_s[i] = keys[b0 + i];
-        val_s[i] = vals[b0 + i];
+        const uint32_t val = vals[b0 + i];
+        key_s[i] = val < (uint32_t)N ? keys[b0 + i] : (uint32_t)V;  // no such position: the sort gave up a wait (reported), the pair was never written
+        val_s[i] = val;
     }
     __syncthreads();
     if (named && blockIdx.y == 0)  // rows with a gradient, at the first id of each
@@ -771,6 +777,12 @@ static size_t few_bytes(int64_t N)
     return n * sizeof(uint32_t);
 }
 
+// One launch for few ids (768 ids, 2,000 rows: 5.5 us against 31 for the sort; 8,192 ids: 15 against 31, all of one row 180
+// against 27).  Where a block's range of rows is wide, ids that lie together land in few blocks (8,192 ids inside 5,000 of
+// 2.9 M rows: 300 us against 150; 2,048: 137 against 150), so the limit is lower there.
+static int few_rows(int64_t V) { return (int)std::min<int64_t>(EGS_MAX_ROWS, std::max<int64_t>(4, ceil_div64(V, 148 * 4))); }
+static bool embed_grad_is_few(int64_t N, int64_t V) { return N <= (few_rows(V) <= 1024 ? EGS_MAX_IDS : EGS_MAX_IDS / 4); }
+
 constexpr int64_t EG_CLEAR_BYTES = (int64_t)64 << 20;
 
 struct EmbedGradScratch {
@@ -786,11 +798,8 @@ static void embed_grad_rows(Exec &ex, const TD *dout, int64_t ldd, const int *id
     const EmbedSort &s = sc.sort;
     const int G = lanes_per_row((D + VE - 1) / VE);
     const int64_t groups = EG_THREADS / G;
-    // One launch for few ids (768 ids, 2,000 rows: 5.5 us against 31 for the sort; 8,192 ids: 15 against 31, all of one row 180
-    // against 27).  Where a block's range of rows is wide, ids that lie together land in few blocks (8,192 ids inside 5,000 of
-    // 2.9 M rows: 300 us against 150; 2,048: 137 against 150), so the limit is lower there.
-    const int R = (int)std::min<int64_t>(EGS_MAX_ROWS, std::max<int64_t>(4, ceil_div64(V, 148 * 4)));
-    const bool few = N > 0 && N <= (R <= 1024 ? EGS_MAX_IDS : EGS_MAX_IDS / 4);
+    const int R = few_rows(V);
+    const bool few = N > 0 && embed_grad_is_few(N, V);
     // A large dense gradient is cleared as a whole first where the rows without ids are nearly all of it and stores of a row are slow
     // or all that there is to do.  Few ids: 937,500 x 320 floats, 550 ids 201 -> 178 us, 1,087,079 x 46 BF16, 819 ids 86 -> 25, but with
     // a 53rd of 218,261 rows named 30 -> 35 and a 9th of 72,765 40 -> 57, since there the blocks' own sums hide the zeros.  Sorted ids,

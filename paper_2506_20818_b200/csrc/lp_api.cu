@@ -2201,6 +2201,7 @@ extern "C" lp_status lp_embed_grad(lp_ctx *ctx, int32_t dout_prec, const void *d
     es.passes = (key_bits + 7) / 8;
     es.bits = (key_bits + es.passes - 1) / es.passes;
     es.tiles = (int)ceil_div64(n_ids, ES_TILE);
+    es.wait_ns = ctx->tc.wait_limit_ns;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) & ~(size_t)255; return here; };
     const size_t n4 = sizeof(uint32_t) * (size_t)n_ids, parts = sizeof(float) * (size_t)ceil_div64(n_ids, EG_SPAN) * width;
@@ -2218,6 +2219,10 @@ extern "C" lp_status lp_embed_grad(lp_ctx *ctx, int32_t dout_prec, const void *d
     es.keys[1] = (uint32_t *)(ws + o_keys2); es.vals[1] = (uint32_t *)(ws + o_vals2);
     es.status = (unsigned *)(ws + o_status);
     sc.head = (float *)(ws + o_head); sc.tail = (float *)(ws + o_tail);
+    if (n_ids > 0 && !embed_grad_is_few(n_ids, rows)) {
+        es.withhold = ctx->tc.overdeclare_tx != 0;
+        ctx->tc.overdeclare_tx = 0;
+    }
     const float f = (float)scale;
     if (dout_prec == LP_FP32) embed_grad_launch<float, float>(ctx->ex, (const float *)dout, ld_dout, ids, n_ids, padding_id, f, rows, width, (float *)grad, ld_grad, accumulate, sc, ctx->err_flag);
     else if (grad_prec == LP_FP32) embed_grad_launch<bf16, float>(ctx->ex, (const bf16 *)dout, ld_dout, ids, n_ids, padding_id, f, rows, width, (float *)grad, ld_grad, accumulate, sc, ctx->err_flag);

@@ -1,0 +1,58 @@
+"""Edges of the embedding and orthogonalisation operators: waits that run out, replayed graphs, zeros, layouts, error reports, and
+the kernel of the large products.
+
+Tolerances are those of test_gpu_operators.py unless a test derives its own.
+"""
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F32, BF16, F64 = torch.float32, torch.bfloat16, torch.float64
+COEFFS = (3.4445, -4.7750, 2.0315)
+ORTH_TOL = {F32: 2e-5, BF16: 1e-2}
+
+
+@pytest.fixture(scope="module")
+def pkg():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    import __graft_entry__ as ge
+    ge.build()
+    import paper_2506_20818_b200 as p
+    return p
+
+
+@pytest.fixture
+def ctx(pkg):
+    c = pkg.Context(0)
+    yield c
+    c.close()
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+# ------------------------------------------------------------------------------------------ waits that run out
+@pytest.mark.parametrize("n", [20_000, 300_000])
+def test_sort_that_gives_up_is_reported_and_reads_nothing_outside(pkg, ctx, n):
+    """The first tile of ids publishes nothing, so every other tile's wait runs out: reported once as LP_ETIMEOUT, and the context
+    stays usable.  Positions that no tile wrote hold the products of another operator here (any 32 bits), which must not be
+    followed into dout."""
+    rows, width = 5000, 40
+    ids = torch.randint(0, rows, (n,), generator=gen(n), dtype=torch.int32).to(DEV)
+    dout = torch.ones(n, width, device=DEV)
+    want = torch.bincount(ids, minlength=rows).float()[:, None].expand(rows, width)
+    assert torch.equal(ctx.embed_grad(dout, ids, rows), want)   # counts below 2^24: exact
+    ctx.orthogonalize(torch.randn(1024, 1200, generator=gen(0)).to(DEV))   # fills the workspace with numbers that are no positions
+    ctx.set_wait_limit(2_000_000, 16)
+    got = ctx.embed_grad(dout, ids, rows)
+    with pytest.raises(pkg.LpError) as ei:
+        ctx.stats()
+    assert ei.value.status == -6
+    assert got.shape == (rows, width)
+    ctx.stats()                              # reported once
+    ctx.set_wait_limit(2_000_000_000, 0)
+    assert torch.equal(ctx.embed_grad(dout, ids, rows), want)
+    ctx.stats()
