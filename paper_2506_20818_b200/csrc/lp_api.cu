@@ -133,7 +133,7 @@ struct lp_ctx {
     TcState tc;                         // tensor-core GEMM state (descriptor encoder, device error word)
     uint8_t *op_ws = nullptr;           // workspace of the embedding gradient and of the orthogonalisation: grows to the largest call
     size_t op_ws_bytes = 0;
-    NsCounters ns_counters;             // barrier counters of the orthogonalisation's chain kernel
+    unsigned *ns_counters = nullptr;    // barrier counters of the orthogonalisation's chain kernel, zero between its launches
     bf16 *w16 = nullptr, *w16t = nullptr;  // BF16 path: the parameter vector of the current call as BF16, as is and with every weight matrix transposed
     bf16 *w16s = nullptr;                  // ... and with the SAGE layers' [W_self ; W_neigh] stored side by side (see weights_cache_kernel)
     // One-pass SAGE layers l >= 1 on the tensor-core pair kernel take the input gradient as
@@ -297,16 +297,16 @@ extern "C" lp_status lp_create(lp_ctx **out, int32_t device, void *cuda_stream)
     ctx->ex.st = (cudaStream_t)cuda_stream;
     if (cudaMalloc((void **)&ctx->err_flag, 256) != cudaSuccess || cudaMalloc((void **)&ctx->exhausted_dev, 256) != cudaSuccess ||
         cudaMallocHost((void **)&ctx->host_counts, 64 * sizeof(int)) != cudaSuccess ||
-        cudaMalloc((void **)&ctx->ns_counters.dev, 2 * NSC_BARRIERS * sizeof(unsigned)) != cudaSuccess) {
+        cudaMalloc((void **)&ctx->ns_counters, NSC_BARRIERS * sizeof(unsigned)) != cudaSuccess) {
         delete ctx;
         return fail(nullptr, LP_ENOMEM, "lp_create: allocation failed");
     }
     cudaMemset(ctx->err_flag, 0, 256);
     cudaMemset(ctx->exhausted_dev, 0, 256);
-    cudaMemset(ctx->ns_counters.dev, 0, 2 * NSC_BARRIERS * sizeof(unsigned));
+    cudaMemset(ctx->ns_counters, 0, NSC_BARRIERS * sizeof(unsigned));
     std::string tc_err;
     if (!tc_init(ctx->tc, tc_err) || !ns_init(tc_err)) {
-        cudaFree(ctx->err_flag); cudaFree(ctx->exhausted_dev); cudaFreeHost(ctx->host_counts); cudaFree(ctx->ns_counters.dev);
+        cudaFree(ctx->err_flag); cudaFree(ctx->exhausted_dev); cudaFreeHost(ctx->host_counts); cudaFree(ctx->ns_counters);
         delete ctx;
         return fail(nullptr, LP_ECUDA, "lp_create: " + tc_err);
     }
@@ -325,7 +325,7 @@ extern "C" void lp_destroy(lp_ctx *ctx)
     free_list(ctx->graph_allocs);
     tc_destroy(ctx->tc);
     cudaFree(ctx->op_ws);
-    cudaFree(ctx->ns_counters.dev);
+    cudaFree(ctx->ns_counters);
     for (cudaEvent_t e : ctx->ex.prof.pool) cudaEventDestroy(e);
     cudaFree(ctx->err_flag);
     cudaFree(ctx->exhausted_dev);

@@ -405,7 +405,7 @@ constexpr int NSC_KEPT = 4;  // tiles of A and of X whose description a block ke
 constexpr int NSC_ACCS = 4;  // accumulators used in turn
 template <int PARTS> constexpr int NSC_ACC_COLS = PARTS * NSC_BN;  // PARTS = 2: the two halves of a 64-term block are added up apart
 constexpr int NSC_SUM_BYTES = 128 * NSC_BN * 4;  // the sums of a tile
-constexpr int NSC_BARRIERS = 256;  // counters of one call: 2 + 3 * steps are used
+constexpr int NSC_BARRIERS = 256;  // counters of one call: 2 + 3 * steps are used, the last one counts the blocks that leave
 
 struct NsChainIo {       // of one kind of phase; the addend has the rows, columns and pitch of the output
     const __half *add_h;   // B: A (parts out_lo apart)
@@ -429,7 +429,7 @@ struct NsChain {
     int bf16_dst;
     const float *params;
     float keep;
-    unsigned *counters, *next_counters;  // NSC_BARRIERS each: this call's (zero) and the next call's (cleared here)
+    unsigned *counters;  // NSC_BARRIERS of them, zero between launches
     int *err;
     unsigned long long wait_ns;
     int extra_tx;
@@ -686,7 +686,6 @@ __global__ void __launch_bounds__(NSC_THREADS, 1) ns_chain_kernel(const __grid_c
         __syncwarp();
         tmem_alloc(smem_u32(&tmem_base_s), NSC_ACCS * NSC_ACC_COLS<PARTS>);
     }
-    if (blockIdx.x == 0 && threadIdx.x < NSC_BARRIERS) p.next_counters[threadIdx.x] = 0;
     // every step visits the same tiles: the first ones of A, B and of X are looked up once
     if (threadIdx.x >= 64 && threadIdx.x < 64 + 2 * NSC_KEPT) {
         const int i = (threadIdx.x - 64) % NSC_KEPT, of_x = (threadIdx.x - 64) / NSC_KEPT, t = cluster + i * n_clusters;
@@ -978,6 +977,16 @@ __global__ void __launch_bounds__(NSC_THREADS, 1) ns_chain_kernel(const __grid_c
     if (warp == 0) {
         __syncwarp();
         tmem_dealloc(tmem, NSC_ACCS * NSC_ACC_COLS<PARTS>);
+    }
+    // Nothing in this block waits any more; the last block to get here puts the counters back to zero.  So a launch leaves them as it
+    // found them, also when it is one that a captured graph replays.
+    if (threadIdx.x == 0) {
+        __threadfence();
+        if (atomicAdd(p.counters + NSC_BARRIERS - 1, 1u) == everybody - 1) {
+            __threadfence();
+            for (int i = 0; i < 2 + 3 * p.steps; ++i) p.counters[i] = 0;
+            p.counters[NSC_BARRIERS - 1] = 0;
+        }
     }
 }
 
@@ -1809,13 +1818,8 @@ static NsCost ns_chain_cost(int parts, int c)
 }
 static NsCost ns_pair_cost(int parts) { return parts == 2 ? NsCost{8.0, 5.0, 0.42} : NsCost{13.0, 0.5, 0.29}; }
 
-struct NsCounters {  // barrier counters of the chain kernel: two sets used in turn, each launch clears the other one
-    unsigned *dev = nullptr;
-    int turn = 0;
-};
-
 template <int PARTS>
-static bool ns_run(TcState &tc, Exec &ex, const NsSource &src, NsGroup &g, const NsLayout &l, const NsAdam &adam, NsCounters &counters, int steps, double a, double b,
+static bool ns_run(TcState &tc, Exec &ex, const NsSource &src, NsGroup &g, const NsLayout &l, const NsAdam &adam, unsigned *counters, int steps, double a, double b,
                    double c, double eps, const NsTarget &out, uint8_t *ws, std::string &err)
 {
     const size_t nx = l.x_elems(), na = l.a_elems();
@@ -1878,8 +1882,7 @@ static bool ns_run(TcState &tc, Exec &ex, const NsSource &src, NsGroup &g, const
         p.partial = partial; p.inv_r = inv_r;
         p.norm_blocks = l.norm_blocks; p.adam_blocks = adam_blocks; p.conv_blocks = l.conv_blocks; p.tiles_a = tiles_a; p.tiles_x = tiles_x;
         p.dst = out.dst; p.bf16_dst = out.bf16_dst; p.params = out.params; p.keep = out.keep;
-        p.counters = counters.dev + counters.turn * NSC_BARRIERS;
-        p.next_counters = counters.dev + (counters.turn ^ 1) * NSC_BARRIERS;
+        p.counters = counters;
         p.err = tc.err_word; p.wait_ns = tc.wait_limit_ns; p.extra_tx = tc.overdeclare_tx;
         tc.overdeclare_tx = 0;
         const int cl = 1 << best;
@@ -1898,7 +1901,6 @@ static bool ns_run(TcState &tc, Exec &ex, const NsSource &src, NsGroup &g, const
             err = std::string("launch of the chain kernel: ") + cudaGetErrorString(e);
             return false;
         }
-        counters.turn ^= 1;
         ex.launches += 1;
         return true;
     }

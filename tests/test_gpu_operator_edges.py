@@ -56,3 +56,64 @@ def test_sort_that_gives_up_is_reported_and_reads_nothing_outside(pkg, ctx, n):
     ctx.set_wait_limit(2_000_000_000, 0)
     assert torch.equal(ctx.embed_grad(dout, ids, rows), want)
     ctx.stats()
+
+
+# ------------------------------------------------------------------------------------------ captured graphs
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,cols", [(64, 64), (160, 192), (512, 300)])
+def test_orthogonalize_in_a_replayed_graph(pkg, rows, cols, dtype):
+    """A captured call gives the bits of an eager one in every replay, and leaves an eager call after it right: (64, 64) is taken by the
+    one-block kernel, the others by the chain kernel, whose blocks wait for counters in global memory."""
+    side = torch.cuda.Stream()
+    c = pkg.Context(0, stream=side)
+    g = gen(rows)
+    U = torch.zeros(rows, cols, dtype=dtype, device=DEV)
+    O = torch.zeros_like(U)
+    inputs = [torch.randn(rows, cols, generator=g).to(dtype).to(DEV) for _ in range(5)]
+    torch.cuda.synchronize()
+    want = [c.orthogonalize(x) for x in inputs]   # also the workspace
+    torch.cuda.synchronize()
+    launches = c.stats().kernel_launches
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        c.orthogonalize(U, out=O)
+    assert c.stats().kernel_launches == launches + 1
+    for x, w in zip(inputs, want):
+        with torch.cuda.stream(side):
+            U.copy_(x)
+            O.fill_(float("nan"))
+            graph.replay()
+            graph.replay()
+        side.synchronize()
+        assert torch.equal(O, w)
+        assert torch.equal(c.orthogonalize(x), w)
+    c.stats()
+    del graph
+    c.close()
+
+
+def test_muon_step_in_a_replayed_graph(pkg):
+    side = torch.cuda.Stream()
+    c = pkg.Context(0, stream=side)
+    mats = [(0, 128, 256), (128 * 256 + 256, 256, 200)]
+    n = mats[1][0] + 256 * 200 + 77
+    g = gen(1)
+    start = [0.05 * torch.randn(n, generator=g), 1e-3 * torch.randn(n, generator=g), 1e-6 * torch.rand(n, generator=g), 1e-3 * torch.randn(n, generator=g)]
+    eager = [x.to(DEV) for x in start]
+    replayed = [x.to(DEV) for x in start]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        c.muon_step(*eager, t=2, matrices=mats)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        c.muon_step(*replayed, t=2, matrices=mats)
+    with torch.cuda.stream(side):
+        for _ in range(4):
+            graph.replay()
+    side.synchronize()
+    for x, y in zip(eager, replayed):
+        assert torch.equal(x, y)
+    c.stats()
+    del graph
+    c.close()
