@@ -378,6 +378,11 @@ lp_status lp_op_linear(lp_ctx *ctx, int32_t prec, int64_t M, int32_t N, int32_t 
 lp_status lp_op_weight_grad(lp_ctx *ctx, int32_t prec, int64_t M, int32_t N, int32_t K, const void *A, const void *dZ,
                             float *dW);
 
+/* The operators of this and the next section may be captured into a CUDA graph and replayed.  One that needs more workspace than
+ * earlier calls left is refused during a capture (LP_ESTATE): make it once before.  Workspace that a capture saw is kept until
+ * lp_destroy, so later, larger calls do not take it away from a graph; the graph must not be replayed after lp_destroy, nor at the
+ * same time as another call on the context. */
+
 /* ---- learned node features -------------------------------------------------------------------- */
 
 /* (No counterpart in the paper, whose nodes come with features; graphs without features learn a table.)

@@ -781,7 +781,7 @@ static size_t few_bytes(int64_t N)
 // against 27).  Where a block's range of rows is wide, ids that lie together land in few blocks (8,192 ids inside 5,000 of
 // 2.9 M rows: 300 us against 150; 2,048: 137 against 150), so the limit is lower there.
 static int few_rows(int64_t V) { return (int)std::min<int64_t>(EGS_MAX_ROWS, std::max<int64_t>(4, ceil_div64(V, 148 * 4))); }
-static bool embed_grad_is_few(int64_t N, int64_t V) { return N <= (few_rows(V) <= 1024 ? EGS_MAX_IDS : EGS_MAX_IDS / 4); }
+static bool embed_grad_is_few(int64_t N, int64_t V) { return N > 0 && N <= (few_rows(V) <= 1024 ? EGS_MAX_IDS : EGS_MAX_IDS / 4); }
 
 constexpr int64_t EG_CLEAR_BYTES = (int64_t)64 << 20;
 
@@ -799,7 +799,7 @@ static void embed_grad_rows(Exec &ex, const TD *dout, int64_t ldd, const int *id
     const int G = lanes_per_row((D + VE - 1) / VE);
     const int64_t groups = EG_THREADS / G;
     const int R = few_rows(V);
-    const bool few = N > 0 && embed_grad_is_few(N, V);
+    const bool few = embed_grad_is_few(N, V);
     // A large dense gradient is cleared as a whole first where the rows without ids are nearly all of it and stores of a row are slow
     // or all that there is to do.  Few ids: 937,500 x 320 floats, 550 ids 201 -> 178 us, 1,087,079 x 46 BF16, 819 ids 86 -> 25, but with
     // a 53rd of 218,261 rows named 30 -> 35 and a 9th of 72,765 40 -> 57, since there the blocks' own sums hide the zeros.  Sorted ids,

@@ -133,6 +133,9 @@ struct lp_ctx {
     TcState tc;                         // tensor-core GEMM state (descriptor encoder, device error word)
     uint8_t *op_ws = nullptr;           // workspace of the embedding gradient and of the orthogonalisation: grows to the largest call
     size_t op_ws_bytes = 0;
+    bool op_ws_captured = false;        // a captured launch uses the present one: it is kept when a larger one takes its place
+    std::vector<void *> op_ws_kept;
+    int64_t op_ws_kept_bytes = 0;
     unsigned *ns_counters = nullptr;    // barrier counters of the orthogonalisation's chain kernel, zero between its launches
     bf16 *w16 = nullptr, *w16t = nullptr;  // BF16 path: the parameter vector of the current call as BF16, as is and with every weight matrix transposed
     bf16 *w16s = nullptr;                  // ... and with the SAGE layers' [W_self ; W_neigh] stored side by side (see weights_cache_kernel)
@@ -325,6 +328,7 @@ extern "C" void lp_destroy(lp_ctx *ctx)
     free_list(ctx->graph_allocs);
     tc_destroy(ctx->tc);
     cudaFree(ctx->op_ws);
+    free_list(ctx->op_ws_kept);
     cudaFree(ctx->ns_counters);
     for (cudaEvent_t e : ctx->ex.prof.pool) cudaEventDestroy(e);
     cudaFree(ctx->err_flag);
@@ -1919,7 +1923,7 @@ extern "C" lp_status lp_get_stats(lp_ctx *ctx, lp_stats *out)
         for (int h = 0; h <= ctx->K; ++h) out->block_nodes[h] = ctx->hop[h].n_src;
         for (int h = 1; h <= ctx->K; ++h) out->block_edges[h - 1] = ctx->hop[h].entries;
     }
-    out->workspace_bytes = ctx->graph_bytes + ctx->model_bytes + (int64_t)ctx->op_ws_bytes;
+    out->workspace_bytes = ctx->graph_bytes + ctx->model_bytes + (int64_t)ctx->op_ws_bytes + ctx->op_ws_kept_bytes;
     out->kernel_launches = ctx->ex.launches;
     return tc_check(ctx->tc, ctx->ex, true, ctx->err);
 }
@@ -2133,17 +2137,33 @@ extern "C" lp_status lp_weight_grad_static(int32_t device, void *cuda_stream, in
 // ----------------------------------------------------------------------------------------------
 // learned node features
 // ----------------------------------------------------------------------------------------------
-// at least `bytes` of device memory that the next call on this context may overwrite
+// At least `bytes` of device memory that the next call on this context may overwrite.  A graph that was captured with the present
+// block may be replayed at any time, so that block stays until the context goes.
 static lp_status op_workspace(lp_ctx *ctx, size_t bytes, uint8_t **out)
 {
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    CK(cudaStreamIsCapturing(ctx->ex.st, &capture));
     if (bytes > ctx->op_ws_bytes) {
+        if (capture != cudaStreamCaptureStatusNone)
+            return fail(ctx, LP_ESTATE, "the call needs more workspace than the context has, and a stream capture cannot allocate it: make the call once before capturing");
         CK(cudaStreamSynchronize(ctx->ex.st));
-        cudaFree(ctx->op_ws);
+        if (ctx->op_ws_captured) {
+            try {
+                ctx->op_ws_kept.push_back(ctx->op_ws);
+            } catch (const std::bad_alloc &) {
+                return fail(ctx, LP_ENOMEM, "host allocation failed");
+            }
+            ctx->op_ws_kept_bytes += (int64_t)ctx->op_ws_bytes;
+        } else {
+            cudaFree(ctx->op_ws);
+        }
         ctx->op_ws = nullptr;
         ctx->op_ws_bytes = 0;
+        ctx->op_ws_captured = false;
         CK(cudaMalloc((void **)&ctx->op_ws, bytes));
         ctx->op_ws_bytes = bytes;
     }
+    ctx->op_ws_captured |= capture != cudaStreamCaptureStatusNone;
     *out = ctx->op_ws;
     return LP_OK;
 }
@@ -2194,7 +2214,9 @@ extern "C" lp_status lp_embed_grad(lp_ctx *ctx, int32_t dout_prec, const void *d
         return fail(ctx, LP_EINVAL, "lp_embed_grad: an array is not aligned to its elements");
     if (n_ids == 0 && accumulate) return LP_OK;
     CK(cudaSetDevice(ctx->device));
-    // one workspace: keys and values (two sets each for the sort), flag per row, digit counts, tickets, tile counts, partial rows
+    // one workspace: keys and values (two sets each for the sort), flag per row, digit counts, tickets, tile counts, partial rows; the
+    // one-launch form for few ids needs none
+    const bool few = embed_grad_is_few(n_ids, rows);
     EmbedGradScratch sc;
     EmbedSort &es = sc.sort;
     const int key_bits = bits_for(rows + 1);
@@ -2212,14 +2234,14 @@ extern "C" lp_status lp_embed_grad(lp_ctx *ctx, int32_t dout_prec, const void *d
     const size_t o_status = take(sizeof(unsigned) * (size_t)es.passes * es.tiles * ES_DIGITS);
     const size_t o_head = take(parts), o_tail = take(parts);
     uint8_t *ws = nullptr;
-    s = op_workspace(ctx, at, &ws);
+    if (!few) s = op_workspace(ctx, at, &ws);
     if (s != LP_OK) return s;
     es.named = ws + o_named; es.hist = (unsigned *)(ws + o_hist); es.ticket = (unsigned *)(ws + o_ticket);
     es.keys[0] = (uint32_t *)(ws + o_keys); es.vals[0] = (uint32_t *)(ws + o_vals);
     es.keys[1] = (uint32_t *)(ws + o_keys2); es.vals[1] = (uint32_t *)(ws + o_vals2);
     es.status = (unsigned *)(ws + o_status);
     sc.head = (float *)(ws + o_head); sc.tail = (float *)(ws + o_tail);
-    if (n_ids > 0 && !embed_grad_is_few(n_ids, rows)) {
+    if (!few && n_ids > 0) {
         es.withhold = ctx->tc.overdeclare_tx != 0;
         ctx->tc.overdeclare_tx = 0;
     }

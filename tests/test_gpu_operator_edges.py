@@ -117,3 +117,39 @@ def test_muon_step_in_a_replayed_graph(pkg):
     c.stats()
     del graph
     c.close()
+
+
+def test_workspace_of_a_captured_call_survives_larger_calls(pkg):
+    """The block that a graph was captured with stays where it is when a later call makes the workspace grow; a capture that would
+    have to allocate is refused and can go on."""
+    side = torch.cuda.Stream()
+    c = pkg.Context(0, stream=side)
+    rows, width, n = 3000, 48, 20_000
+    g = gen(8)
+    ids = torch.randint(0, rows, (n,), generator=g, dtype=torch.int32).to(DEV)
+    dout = torch.randn(n, width, generator=g).to(DEV)
+    U = torch.randn(200, 260, generator=g).to(DEV)
+    grad, O = torch.zeros(rows, width, device=DEV), torch.zeros_like(U)
+    big = torch.randn(1500, 1600, generator=g).to(DEV)
+    torch.cuda.synchronize()
+    want_grad, want_O = c.embed_grad(dout, ids, rows), c.orthogonalize(U)
+    torch.cuda.synchronize()
+    before = c.stats().workspace_bytes
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        c.embed_grad(dout, ids, rows, grad=grad)
+        c.orthogonalize(U, out=O)
+        with pytest.raises(pkg.LpError) as ei:
+            c.orthogonalize(big, out=big)
+    assert ei.value.status == -2   # LP_ESTATE
+    c.orthogonalize(big, out=big)      # grows
+    assert c.stats().workspace_bytes > 2 * before
+    reuse = [torch.full((before,), 255, dtype=torch.uint8, device=DEV) for _ in range(3)]   # whatever was given back is written over
+    with torch.cuda.stream(side):
+        graph.replay()
+    side.synchronize()
+    assert torch.equal(grad, want_grad) and torch.equal(O, want_O)
+    assert all((x == 255).all() for x in reuse)
+    c.stats()
+    del graph
+    c.close()
