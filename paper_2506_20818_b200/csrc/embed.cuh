@@ -286,7 +286,7 @@ __global__ void __launch_bounds__(EG_THREADS) embed_sort_kernel(const int *__res
     const int tile = tile_s, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int shift = pass * s.bits;
     const uint32_t mask = (1u << s.bits) - 1;
-    const uint32_t *keys = s.keys[(pass + 1) & 1], *vals = s.vals[(pass + 1) & 1];  // the first pass reads the ids and writes set 0
+    const uint32_t *keys = pass & 1 ? s.keys[0] : s.keys[1], *vals = pass & 1 ? s.vals[0] : s.vals[1];  // the first pass reads the ids and writes set 0
     uint32_t key[ES_ITEMS], val[ES_ITEMS];
     int rank[ES_ITEMS];
     const int64_t base = (int64_t)tile * ES_TILE + warp * (32 * ES_ITEMS) + lane;  // a warp's pairs are consecutive: ranks keep the order
@@ -376,7 +376,7 @@ __global__ void __launch_bounds__(EG_THREADS) embed_sort_kernel(const int *__res
     }
     __syncthreads();
     const int count = (int)min((int64_t)ES_TILE, N - (int64_t)tile * ES_TILE);
-    uint32_t *keys_out = s.keys[pass & 1], *vals_out = s.vals[pass & 1];
+    uint32_t *keys_out = pass & 1 ? s.keys[1] : s.keys[0], *vals_out = pass & 1 ? s.vals[1] : s.vals[0];
     for (int i = threadIdx.x; i < count; i += EG_THREADS) {
         const uint32_t k = key_s[i];
         const int64_t o = out_s[(k >> shift) & mask] + i;
