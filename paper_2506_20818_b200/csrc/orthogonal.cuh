@@ -405,7 +405,7 @@ constexpr int NSC_KEPT = 4;  // tiles of A and of X whose description a block ke
 constexpr int NSC_ACCS = 4;  // accumulators used in turn
 template <int PARTS> constexpr int NSC_ACC_COLS = PARTS * NSC_BN;  // PARTS = 2: the two halves of a 64-term block are added up apart
 constexpr int NSC_SUM_BYTES = 128 * NSC_BN * 4;  // the sums of a tile
-constexpr int NSC_BARRIERS = 256;  // counters of one call: 2 + 3 * steps are used, the last one counts the blocks that leave
+constexpr int NSC_BARRIERS = 256;  // counters of one call: 1 + 3 * steps are used, the last one counts the blocks that are done with them
 
 struct NsChainIo {       // of one kind of phase; the addend has the rows, columns and pitch of the output
     const __half *add_h;   // B: A (parts out_lo apart)
@@ -444,6 +444,17 @@ LP_DEVINL unsigned ld_acquire_gpu(const unsigned *p)
 LP_DEVINL void red_release_gpu(unsigned *p)
 {
     asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(p) : "memory");
+}
+// A block that will not wait for the counters again says so; the last one puts them back to zero, while the last products are still
+// under way.  So a launch leaves them as it found them, also one that a captured graph replays.
+LP_DEVINL void ns_leave(unsigned *counters, int used, int count)
+{
+    unsigned before;
+    asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(before) : "l"(counters + count) : "memory");
+    if (before != gridDim.x - 1) return;
+#pragma unroll 1
+    for (int i = 0; i < used; ++i) counters[i] = 0;
+    counters[count] = 0;
 }
 LP_DEVINL void fence_async_proxy_global() { asm volatile("fence.proxy.async.global;" ::: "memory"); }
 LP_DEVINL bool counter_wait(const unsigned *p, unsigned want, unsigned long long limit_ns)
@@ -642,6 +653,25 @@ template <int PARTS> LP_DEVINL void ns_chain_convert(const NsSource &src, const 
     for (int t = blockIdx.x; t < p.conv_blocks; t += gridDim.x) ns_convert_block<PARTS, NSC_WORKERS>(src, g, t, tid, p.partial, p.eps, p.X0, p.inv_r, tile, sw);
 }
 
+// After a wait that ran out somewhere in the block, copies into its shared memory and products may still be under way; both are waited
+// for (again not longer than the limit) before the block gives up its shared and tensor memory.  Without such a wait they have
+// long been used and nothing is waited for here.
+// copies: stages that the last S uses of the ring filled; `s`, `round`: where the ring would go on
+template <int S> LP_DEVINL void ns_drain_copies(const uint64_t *bar_full, int s, int round, unsigned long long limit_ns)
+{
+#pragma unroll 1
+    for (int i = 0; i < S; ++i) {
+        const int use = i < s ? round : round - 1;
+        if (use >= 0) mbar_wait(smem_u32(bar_full + i), use & 1, limit_ns);
+    }
+}
+// products: the last commit covers all of them
+template <int S> LP_DEVINL void ns_drain_products(const uint64_t *bar_empty, int s, int round, unsigned long long limit_ns)
+{
+    const int last = s > 0 ? s - 1 : S - 1, use = s > 0 ? round : round - 1;
+    if (use >= 0) mbar_wait(smem_u32(bar_empty + last), use & 1, limit_ns);
+}
+
 template <int PARTS, int C>
 __global__ void __launch_bounds__(NSC_THREADS, 1) ns_chain_kernel(const __grid_constant__ CUtensorMap mapX128, const __grid_constant__ CUtensorMap mapX64,
                                                                   const __grid_constant__ CUtensorMap mapA128, const __grid_constant__ CUtensorMap mapA64,
@@ -654,6 +684,7 @@ __global__ void __launch_bounds__(NSC_THREADS, 1) ns_chain_kernel(const __grid_c
     __shared__ uint32_t tmem_base_s;
     __shared__ double sw[NSC_WORKERS / 32];
     __shared__ NsTile kept_s[2][NSC_KEPT], later_s;
+    __shared__ int left_s, announced_s;  // the workers wait for no counter any more; the others' sums of this tile are announced and not yet here
     constexpr int S = NSC_STAGES<PARTS>;
     constexpr uint32_t a_bytes = 128 * TC_BK * 2, b_bytes = NSC_BN * TC_BK * 2, stage_bytes = NSC_STAGE_BYTES<PARTS>;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
@@ -674,6 +705,7 @@ __global__ void __launch_bounds__(NSC_THREADS, 1) ns_chain_kernel(const __grid_c
         }
         mbar_init(smem_u32(&bar_xfull), 1);
         mbar_init(smem_u32(&bar_xfree), C);
+        left_s = announced_s = 0;
         fence_barrier_init();
         fence_async_proxy();
         tma_prefetch_desc(&mapX128);
@@ -736,6 +768,14 @@ __global__ void __launch_bounds__(NSC_THREADS, 1) ns_chain_kernel(const __grid_c
                     }
                 }
             }
+            // the last operands are requested; the other thread of this block that waits for the counters is done with them, too, once it
+            // has seen the last one or given up, each of its waits being limited
+            const unsigned long long t0 = global_timer_ns();
+            bool others = *(volatile int *)&left_s != 0;
+            while (!others && global_timer_ns() - t0 <= 16 * p.wait_ns) others = *(volatile int *)&left_s != 0;
+            __threadfence_block();
+            if (others) ns_leave(p.counters, 1 + 3 * p.steps, NSC_BARRIERS - 1);
+            ns_drain_copies<S>(bar_full, s, round, p.wait_ns);
         }
     } else if (warp == 1) {
         if (elect_one()) {
@@ -788,6 +828,7 @@ __global__ void __launch_bounds__(NSC_THREADS, 1) ns_chain_kernel(const __grid_c
                     }
                 }
             }
+            ns_drain_products<S>(bar_empty, s, round, p.wait_ns);
         }
     } else {
         // ---- norm and conversion, then sums and results
@@ -818,6 +859,7 @@ __global__ void __launch_bounds__(NSC_THREADS, 1) ns_chain_kernel(const __grid_c
                 const int kind = kind_ == NS_APPLY && k + 1 == p.steps ? NS_LAST : kind_;
                 const bool square = kind == NS_GRAM || kind == NS_POLY;
                 ok = await(phase - 1);
+                if (kind == NS_LAST && tid == 0) *(volatile int *)&left_s = 1;
                 const int tiles = kind_ == NS_APPLY ? p.tiles_x : p.tiles_a;
                 const NsChainIo &io = p.io[k & 1][kind_];
                 int nth = 0;
@@ -919,6 +961,7 @@ __global__ void __launch_bounds__(NSC_THREADS, 1) ns_chain_kernel(const __grid_c
                     if (C > 1) {
                         if (tid == 0) {
                             mbar_expect_tx(smem_u32(&bar_xfull), (C - 1) * SHARE * 4);
+                            announced_s = 1;
                             for (int o = 1; o < C; ++o) {
                                 const int to = (rank + o) % C;
                                 copy_to_cta(map_to_cta(smem_u32(theirs + rank * SHARE), to), smem_u32(mine + to * SHARE), SHARE * 4, map_to_cta(smem_u32(&bar_xfull), to));
@@ -964,10 +1007,17 @@ __global__ void __launch_bounds__(NSC_THREADS, 1) ns_chain_kernel(const __grid_c
                     ok = !ns_any<NSC_WORKERS>(failed);  // and the sums may be overwritten
                     if (!ok) break;
                     if (C > 1 && tid < C) mbar_arrive_cluster(map_to_cta(smem_u32(&bar_xfree), tid));
+                    if (C > 1 && tid == 0) announced_s = 0;
                     ++tiles_done;
                 }
                 if (ok && kind != NS_LAST) arrive(phase);
             }
+        }
+        if (tid == 0) *(volatile int *)&left_s = 1;  // gave up before the last phase
+        // this block gave up: sums that others of its cluster may have sent it meanwhile land before its shared memory goes
+        if (C > 1 && !ok && tid == 0) {
+            if (!announced_s) mbar_expect_tx(smem_u32(&bar_xfull), (C - 1) * (128 * NSC_BN / C) * 4);
+            mbar_wait_cluster(smem_u32(&bar_xfull), tiles_done & 1, p.wait_ns);
         }
     }
     __syncwarp();
@@ -977,16 +1027,6 @@ __global__ void __launch_bounds__(NSC_THREADS, 1) ns_chain_kernel(const __grid_c
     if (warp == 0) {
         __syncwarp();
         tmem_dealloc(tmem, NSC_ACCS * NSC_ACC_COLS<PARTS>);
-    }
-    // Nothing in this block waits any more; the last block to get here puts the counters back to zero.  So a launch leaves them as it
-    // found them, also when it is one that a captured graph replays.
-    if (threadIdx.x == 0) {
-        __threadfence();
-        if (atomicAdd(p.counters + NSC_BARRIERS - 1, 1u) == everybody - 1) {
-            __threadfence();
-            for (int i = 0; i < 2 + 3 * p.steps; ++i) p.counters[i] = 0;
-            p.counters[NSC_BARRIERS - 1] = 0;
-        }
     }
 }
 
@@ -1400,6 +1440,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NSP_THREADS, 1)
                     if (++s == S) { s = 0; ++round; }
                 }
             }
+            if (leader) ns_drain_copies<S>(bar_full, s, round, p.wait_ns);  // both CTAs' copies count on the leader's barriers
         }
     } else if (warp == 1) {
         if (leader && elect_one()) {
@@ -1441,6 +1482,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NSP_THREADS, 1)
                     if (++s == S) { s = 0; ++round; }
                 }
             }
+            ns_drain_products<S>(bar_empty, s, round, p.wait_ns);
         }
     } else {
         // ---- results: warp (q, cg) holds rows 32 q .. of this CTA's 128 and columns 64 cg .. of the tile's 256
