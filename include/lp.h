@@ -415,7 +415,7 @@ lp_status lp_embed_grad(lp_ctx *ctx, int32_t dout_prec, const void *dout, int64_
 /* (No counterpart in the paper, which trains with Adam.)
  * Newton-Schulz orthogonalisation of `batch` matrices [rows, cols]:
  *   X_0 = U / (|U|_F + eps),  X <- a X + (b A + c A^2) X with A = X X^T, `steps` times (1..64); out = X.
- * A matrix with more rows than columns is iterated transposed.  A matrix of zeros gives zeros.
+ * A matrix with more rows than columns is iterated transposed.  A matrix of zeros gives zeros, also with eps = 0.
  *   prec     : LP_FP32 or LP_BF16, of U and out.  The products run on the tensor cores with FP32 accumulators: LP_BF16
  *              holds X, A and b A + c A^2 as FP16 numbers (11 bits), LP_FP32 as pairs of them (22 bits)
  *   U, out   : DEVICE, row pitch ld_*, matrices stride_* elements apart; out may be U itself

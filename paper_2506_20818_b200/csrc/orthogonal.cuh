@@ -225,9 +225,9 @@ LP_DEVINL void ns_start_scale(double norm, float &r, double &pow2)
 {
     int e = 0;
     const double f = frexp(norm, &e);  // norm = f 2^e, f in [1/2, 1)
-    if (norm == 0.0 || !isfinite(norm)) {  // zeros divided by eps = 0, or a norm of infinity or NaN: NaN or zero come out of the products
+    if (norm == 0.0 || !isfinite(norm)) {  // zeros with eps = 0 stay zeros; a norm of infinity or NaN makes the products NaN
         r = 1.f;
-        pow2 = (double)NS_X_SCALE / norm;
+        pow2 = norm == 0.0 ? 0.0 : (double)NS_X_SCALE / norm;
         return;
     }
     r = (float)f;

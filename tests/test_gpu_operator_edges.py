@@ -153,3 +153,31 @@ def test_workspace_of_a_captured_call_survives_larger_calls(pkg):
     c.stats()
     del graph
     c.close()
+
+
+# ------------------------------------------------------------------------------------------ zeros, infinities
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("batch,rows,cols", [(3, 64, 40), (3, 150, 200), (2, 2100, 2300)])   # one-block, chain and pair kernel
+def test_zeros_with_eps_zero_stay_zeros(ctx, dtype, batch, rows, cols):
+    U = torch.randn(batch, rows, cols, generator=gen(rows)).to(dtype).to(DEV)
+    U[1] = 0
+    launches = ctx.stats().kernel_launches
+    got = ctx.orthogonalize(U, eps=0.0)
+    assert ctx.stats().kernel_launches - launches == (1 if rows < 2000 else 2 + 3 * 5)   # which kernel it was
+    assert (got[1] == 0).all()
+    assert got.isfinite().all() and (got[0] != 0).any()
+    U[1, 3, 5] = float("inf")   # what is not finite is not hidden
+    got = ctx.orthogonalize(U, eps=0.0)
+    assert got[1].isnan().all() and got[0].isfinite().all()
+
+
+def test_muon_step_of_a_frozen_layer_with_eps_zero(ctx):
+    mats = [(0, 48, 96), (48 * 96, 256, 160)]
+    n = 48 * 96 + 256 * 160
+    g = gen(2)
+    p = torch.randn(n, generator=g).to(DEV)
+    m, gr = torch.zeros(n, device=DEV), torch.zeros(n, device=DEV)
+    gr[48 * 96:] = torch.randn(256 * 160, generator=g).to(DEV)   # the first matrix has no gradient and no momentum
+    new = ctx.muon_step(p, m, None, gr, t=1, matrices=mats, ns_eps=0.0, lr=0.5, weight_decay=0.25, out=(torch.empty_like(p), torch.empty_like(m), None))
+    assert torch.equal(new[0][:48 * 96], p[:48 * 96] * 0.875) and new[0].isfinite().all()
+    assert not torch.equal(new[0][48 * 96:], p[48 * 96:] * 0.875)
