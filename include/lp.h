@@ -293,8 +293,9 @@ lp_status lp_get_output_gradient(lp_ctx *ctx, float *out);
 lp_status lp_get_block(lp_ctx *ctx, int32_t hop, int32_t *frontier, int64_t *blk_ptr, int32_t *blk_col);
 
 /* Counters.  Synchronises the stream.  Returns LP_EINVAL (once) when an earlier step was
- * given a node id outside [0, n), and LP_ETIMEOUT (once) when a bounded wait inside a
- * tensor-core kernel of an earlier call expired. */
+ * given a node id outside [0, n) or an earlier lp_embed or lp_embed_grad an id outside its table, and
+ * LP_ETIMEOUT (once) when a bounded wait inside a tensor-core kernel or a sort of an earlier call expired.  Of several
+ * such reports each call returns one. */
 lp_status lp_get_stats(lp_ctx *ctx, lp_stats *out);
 
 /* (No counterpart in the paper: failure detection of the library itself.)
@@ -394,7 +395,7 @@ lp_status lp_op_weight_grad(lp_ctx *ctx, int32_t prec, int64_t M, int32_t N, int
  *   out[n_ids, width]    : DEVICE, row pitch ld_out elements; out_prec LP_FP32 or LP_BF16 (LP_BF16 when the table is)
  * Any width, pitch and alignment to the element is accepted; rows whose width, pitch and address are multiples of
  * 16 bytes are the fast ones.  An id outside [0, rows) that is not the padding id gives a row of zeros, and the next
- * synchronising call (lp_get_stats) returns LP_EINVAL once.  Does not synchronise. */
+ * lp_get_stats returns LP_EINVAL once (no other call reports it, takes it for its own, or forgets it).  Does not synchronise. */
 #define LP_NO_PADDING INT32_MIN
 lp_status lp_embed(lp_ctx *ctx, int32_t table_prec, const void *table, int64_t rows, int32_t width, int64_t ld_table, const int32_t *ids, int64_t n_ids,
                    int32_t padding_id, double scale, int32_t out_prec, void *out, int64_t ld_out);

@@ -81,7 +81,8 @@ struct lp_ctx {
     uint64_t neg_calls = 0;
     HeavyPlan plan_csr, plan_csc, plan_dyn;  // heavy-row plans: the loaded graph, its transpose, per-step structures
     float *heavy_partials = nullptr;
-    int *err_flag = nullptr;
+    int *err_flag = nullptr;            // of the steps, graph and candidate checks
+    int *embed_err = nullptr;           // of lp_embed and lp_embed_grad, in the same allocation: read and cleared by lp_get_stats alone
 
     // model
     bool model_set = false, sampled = false;
@@ -305,6 +306,7 @@ extern "C" lp_status lp_create(lp_ctx **out, int32_t device, void *cuda_stream)
         return fail(nullptr, LP_ENOMEM, "lp_create: allocation failed");
     }
     cudaMemset(ctx->err_flag, 0, 256);
+    ctx->embed_err = ctx->err_flag + 1;
     cudaMemset(ctx->exhausted_dev, 0, 256);
     cudaMemset(ctx->ns_counters, 0, NSC_BARRIERS * sizeof(unsigned));
     std::string tc_err;
@@ -1909,14 +1911,19 @@ extern "C" lp_status lp_get_stats(lp_ctx *ctx, lp_stats *out)
     CK(cudaSetDevice(ctx->device));
     memset(out, 0, sizeof *out);
     unsigned long long ex = 0;
-    int bad = 0;
+    int words[2] = {0, 0};  // err_flag, embed_err
     CK(cudaMemcpyAsync(&ex, ctx->exhausted_dev + (ctx->neg_calls + 15) % 16, sizeof ex, cudaMemcpyDeviceToHost, ctx->ex.st));  // the last call's counter
-    CK(cudaMemcpyAsync(&bad, ctx->err_flag, sizeof bad, cudaMemcpyDeviceToHost, ctx->ex.st));
+    CK(cudaMemcpyAsync(words, ctx->err_flag, sizeof words, cudaMemcpyDeviceToHost, ctx->ex.st));
     CK(cudaStreamSynchronize(ctx->ex.st));
-    if (bad) {
+    if (words[0]) {
         cudaMemsetAsync(ctx->err_flag, 0, sizeof(int), ctx->ex.st);
-        if (bad & 2) return fail(ctx, LP_ETIMEOUT, "a bounded wait inside the scan of an earlier step expired (results of that call are invalid)");
+        if (words[0] & 2) return fail(ctx, LP_ETIMEOUT, "a bounded wait inside the scan of an earlier step expired (results of that call are invalid)");
         return fail(ctx, LP_EINVAL, "a node id outside [0, n) was passed to an earlier call (it was clamped; results of that call are invalid)");
+    }
+    if (words[1]) {
+        cudaMemsetAsync(ctx->embed_err, 0, sizeof(int), ctx->ex.st);
+        if (words[1] & 2) return fail(ctx, LP_ETIMEOUT, "a bounded wait inside the sort of an earlier lp_embed_grad expired (its gradient is invalid)");
+        return fail(ctx, LP_EINVAL, "an id outside the table was passed to an earlier lp_embed (its row is zero) or lp_embed_grad (its row went nowhere)");
     }
     out->negatives_exhausted = (int64_t)ex;
     if (ctx->model_set && ctx->sampled) {
@@ -2194,9 +2201,9 @@ extern "C" lp_status lp_embed(lp_ctx *ctx, int32_t table_prec, const void *table
     if (n_ids == 0) return LP_OK;
     CK(cudaSetDevice(ctx->device));
     const float f = (float)scale;
-    if (table_prec == LP_BF16) embed_launch<bf16, bf16>(ctx->ex, (const bf16 *)table, rows, width, ld_table, ids, n_ids, padding_id, f, (bf16 *)out, ld_out, ctx->err_flag);
-    else if (out_prec == LP_BF16) embed_launch<float, bf16>(ctx->ex, (const float *)table, rows, width, ld_table, ids, n_ids, padding_id, f, (bf16 *)out, ld_out, ctx->err_flag);
-    else embed_launch<float, float>(ctx->ex, (const float *)table, rows, width, ld_table, ids, n_ids, padding_id, f, (float *)out, ld_out, ctx->err_flag);
+    if (table_prec == LP_BF16) embed_launch<bf16, bf16>(ctx->ex, (const bf16 *)table, rows, width, ld_table, ids, n_ids, padding_id, f, (bf16 *)out, ld_out, ctx->embed_err);
+    else if (out_prec == LP_BF16) embed_launch<float, bf16>(ctx->ex, (const float *)table, rows, width, ld_table, ids, n_ids, padding_id, f, (bf16 *)out, ld_out, ctx->embed_err);
+    else embed_launch<float, float>(ctx->ex, (const float *)table, rows, width, ld_table, ids, n_ids, padding_id, f, (float *)out, ld_out, ctx->embed_err);
     CK_LAUNCH();
     return LP_OK;
 }
@@ -2246,9 +2253,9 @@ extern "C" lp_status lp_embed_grad(lp_ctx *ctx, int32_t dout_prec, const void *d
         ctx->tc.overdeclare_tx = 0;
     }
     const float f = (float)scale;
-    if (dout_prec == LP_FP32) embed_grad_launch<float, float>(ctx->ex, (const float *)dout, ld_dout, ids, n_ids, padding_id, f, rows, width, (float *)grad, ld_grad, accumulate, sc, ctx->err_flag);
-    else if (grad_prec == LP_FP32) embed_grad_launch<bf16, float>(ctx->ex, (const bf16 *)dout, ld_dout, ids, n_ids, padding_id, f, rows, width, (float *)grad, ld_grad, accumulate, sc, ctx->err_flag);
-    else embed_grad_launch<bf16, bf16>(ctx->ex, (const bf16 *)dout, ld_dout, ids, n_ids, padding_id, f, rows, width, (bf16 *)grad, ld_grad, accumulate, sc, ctx->err_flag);
+    if (dout_prec == LP_FP32) embed_grad_launch<float, float>(ctx->ex, (const float *)dout, ld_dout, ids, n_ids, padding_id, f, rows, width, (float *)grad, ld_grad, accumulate, sc, ctx->embed_err);
+    else if (grad_prec == LP_FP32) embed_grad_launch<bf16, float>(ctx->ex, (const bf16 *)dout, ld_dout, ids, n_ids, padding_id, f, rows, width, (float *)grad, ld_grad, accumulate, sc, ctx->embed_err);
+    else embed_grad_launch<bf16, bf16>(ctx->ex, (const bf16 *)dout, ld_dout, ids, n_ids, padding_id, f, rows, width, (bf16 *)grad, ld_grad, accumulate, sc, ctx->embed_err);
     CK_LAUNCH();
     return LP_OK;
 }

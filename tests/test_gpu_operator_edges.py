@@ -181,3 +181,34 @@ def test_muon_step_of_a_frozen_layer_with_eps_zero(ctx):
     new = ctx.muon_step(p, m, None, gr, t=1, matrices=mats, ns_eps=0.0, lr=0.5, weight_decay=0.25, out=(torch.empty_like(p), torch.empty_like(m), None))
     assert torch.equal(new[0][:48 * 96], p[:48 * 96] * 0.875) and new[0].isfinite().all()
     assert not torch.equal(new[0][48 * 96:], p[48 * 96:] * 0.875)
+
+
+# ------------------------------------------------------------------------------------------ error reports
+def test_bad_embedding_ids_are_no_other_calls_error(pkg, ctx):
+    """An id outside the table is reported by the next stats() and by nothing else: candidates set meanwhile are not refused for it,
+    loading and sparsifying a graph do not forget it, and a step's own report does not swallow it."""
+    import workloads as wl
+    g = wl.erdos_renyi(200, 1500, seed=0)
+    table = torch.randn(10, 8, device=DEV)
+    bad = torch.tensor([1, 10, 2], dtype=torch.int32, device=DEV)
+
+    def report():
+        with pytest.raises(pkg.LpError) as ei:
+            ctx.stats()
+        assert ei.value.status == -1 and "table" in str(ei.value)
+        ctx.stats()   # once
+
+    ctx.embed(table, bad)
+    ctx.load_graph(g.n, g.rowptr, g.col, None, wl.node_features(g.n, 16, 0))
+    report()
+    ctx.embed_grad(torch.ones(3, 8, device=DEV), bad, 10)
+    candidates = torch.arange(50, dtype=torch.int32, device=DEV)
+    ctx.set_candidates(candidates)
+    report()
+    ctx.embed(table, bad)
+    ctx.sparsify(0.5, 1)
+    report()
+    ctx.embed(table, bad)
+    with pytest.raises(pkg.LpError):
+        ctx.set_candidates(torch.tensor([0, 200], dtype=torch.int32, device=DEV))   # a bad candidate is still one
+    report()
