@@ -419,7 +419,8 @@ lp_status lp_embed_grad(lp_ctx *ctx, int32_t dout_prec, const void *dout, int64_
  * A matrix with more rows than columns is iterated transposed.  A matrix of zeros gives zeros, also with eps = 0.
  *   prec     : LP_FP32 or LP_BF16, of U and out.  The products run on the tensor cores with FP32 accumulators: LP_BF16
  *              holds X, A and b A + c A^2 as FP16 numbers (11 bits), LP_FP32 as pairs of them (22 bits)
- *   U, out   : DEVICE, row pitch ld_*, matrices stride_* elements apart; out may be U itself
+ *   U, out   : DEVICE, row pitch ld_*, matrices stride_* elements apart; out may be U itself.  Matrices of out may lie behind one
+ *              another or between one another's rows (stride_out < ld_out); stride_u may also be 0
  *   coeffs   : HOST double[3] = {a, b, c}, or NULL for {3.4445, -4.7750, 2.0315}.  LP_EINVAL when singular values of
  *              [0, 1] could grow beyond 2 under them
  * Takes workspace from the context (growing synchronises).  Does not synchronise otherwise. */

@@ -2294,8 +2294,11 @@ extern "C" lp_status lp_orthogonalize(lp_ctx *ctx, int32_t prec, int64_t batch, 
     if (batch < 0 || rows < 0 || cols < 0) return fail(ctx, LP_EINVAL, "lp_orthogonalize: negative size");
     if (rows > NS_MAX_DIM || cols > NS_MAX_DIM) return fail(ctx, LP_EINVAL, "lp_orthogonalize: a matrix has at most 2^17 rows and columns");
     if (ld_u < cols || ld_out < cols) return fail(ctx, LP_EINVAL, "lp_orthogonalize: a row pitch is smaller than the number of columns");
-    if (batch > 1 && rows > 0 && (stride_u < 0 || stride_out < (rows - 1) * ld_out + cols))
-        return fail(ctx, LP_EINVAL, "lp_orthogonalize: matrices of the result overlap");
+    if (batch > 1 && rows > 0) {
+        // matrices of the result lie behind one another, or between one another's rows
+        const bool apart = stride_out >= (rows - 1) * ld_out + cols, between = stride_out >= cols && (ld_out - cols) / (batch - 1) >= stride_out;
+        if (stride_u < 0 || (!apart && !between)) return fail(ctx, LP_EINVAL, "lp_orthogonalize: matrices of the result overlap");
+    }
     double c[3];
     lp_status s = check_ns(ctx, "lp_orthogonalize", steps, coeffs, eps, c);
     if (s != LP_OK) return s;

@@ -212,3 +212,22 @@ def test_bad_embedding_ids_are_no_other_calls_error(pkg, ctx):
     with pytest.raises(pkg.LpError):
         ctx.set_candidates(torch.tensor([0, 200], dtype=torch.int32, device=DEV))   # a bad candidate is still one
     report()
+
+
+# ------------------------------------------------------------------------------------------ layouts
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("heads,rows,cols", [(3, 40, 64), (5, 90, 33), (3, 300, 160), (2, 2100, 2111)])
+def test_orthogonalize_of_interleaved_matrices(pkg, ctx, heads, rows, cols, dtype):
+    """Matrices whose rows lie between one another's ([heads, rows, cols] as a view of [rows, heads, cols]): out of place and in place."""
+    x = torch.randn(rows, heads, cols + 1, generator=gen(cols)).to(dtype).to(DEV)
+    view = x.transpose(0, 1)[:, :, :cols]
+    want = ctx.orthogonalize(view.contiguous())
+    assert torch.equal(ctx.orthogonalize(view), want)
+    last = x[:, :, cols].clone()
+    ctx.orthogonalize(view, out=view)
+    assert torch.equal(view, want) and torch.equal(x[:, :, cols], last)
+    lib = pkg.load_library()
+    prec = 0 if dtype == F32 else 1
+    assert pkg.LP_FP32 == 0 and pkg.LP_BF16 == 1
+    bad = lambda ld, stride: lib.lp_orthogonalize(ctx.h, prec, heads, rows, cols, x.data_ptr(), heads * (cols + 1), cols + 1, 5, None, 1e-7, x.data_ptr(), ld, stride)
+    assert bad(heads * (cols + 1), cols - 1) == -1 and bad(heads * (cols + 1) - 2, cols + 1) == -1 and bad(heads * (cols + 1), 0) == -1
