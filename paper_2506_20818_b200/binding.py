@@ -297,6 +297,18 @@ class Context:
             self._refuse(f"{who}: float32 or bfloat16 expected, got {dtype}")
         return p
 
+    def _padding(self, padding_id, who: str) -> int:
+        if padding_id is None:
+            return LP_NO_PADDING
+        if not -(1 << 31) <= padding_id < 1 << 31:  # ctypes would keep the low 32 bits, which are another id
+            self._refuse(f"{who}: padding_id {padding_id} is no 32-bit id")
+        return padding_id
+
+    def _steps(self, steps, who: str) -> int:
+        if not 1 <= steps <= 64:
+            self._refuse(f"{who}: steps must be in [1, 64]")
+        return steps
+
     def _rows(self, x, who: str):
         """(rows, width, row pitch) of a CUDA matrix whose rows are contiguous."""
         if x.get_device() != self.device or x.dim() != 2:
@@ -343,7 +355,7 @@ class Context:
                 self._refuse(f"embed: out must be [{N}, {D}] of the requested type")
         cur = self._enter(table, ids, out)
         rc = self.lib.lp_embed(self.h, self._prec(table.dtype, "embed: table"), table.data_ptr(), V, D, ldt, ids.data_ptr(), N,
-                               LP_NO_PADDING if padding_id is None else padding_id, scale, self._prec(out.dtype, "embed: out"), out.data_ptr(), ldo)
+                               self._padding(padding_id, "embed"), scale, self._prec(out.dtype, "embed: out"), out.data_ptr(), ldo)
         if rc:
             self._ck(rc)
         if cur is not None:
@@ -367,7 +379,7 @@ class Context:
                 self._refuse(f"embed_grad: grad must be [{rows}, {D}] of the requested type")
         cur = self._enter(dout, ids, grad)
         rc = self.lib.lp_embed_grad(self.h, self._prec(dout.dtype, "embed_grad: dout"), dout.data_ptr(), ldd, ids.data_ptr(), N,
-                                    LP_NO_PADDING if padding_id is None else padding_id, scale, rows, D, self._prec(grad.dtype, "embed_grad: grad"),
+                                    self._padding(padding_id, "embed_grad"), scale, rows, D, self._prec(grad.dtype, "embed_grad: grad"),
                                     grad.data_ptr(), ldg, accumulate)
         if rc:
             self._ck(rc)
@@ -395,8 +407,8 @@ class Context:
         stride_u, stride_o = (U3.stride(0), O3.stride(0)) if batch > 1 else (rows * ld_u, rows * ld_o)
         c = (C.c_double * 3)(*coeffs) if coeffs is not None else None
         cur = self._enter(U, U3, out)
-        self._ck(self.lib.lp_orthogonalize(self.h, self._prec(U.dtype, "orthogonalize"), batch, rows, cols, U3.data_ptr(), ld_u, stride_u, steps, c, eps,
-                                           O3.data_ptr(), ld_o, stride_o))
+        self._ck(self.lib.lp_orthogonalize(self.h, self._prec(U.dtype, "orthogonalize"), batch, rows, cols, U3.data_ptr(), ld_u, stride_u,
+                                           self._steps(steps, "orthogonalize"), c, eps, O3.data_ptr(), ld_o, stride_o))
         self._leave(cur)
         return out
 
@@ -412,9 +424,12 @@ class Context:
         for x in (params, momentum, adam_v, grads, *new):
             if x is not None and (not x.is_cuda or x.device.index != self.device or x.dtype != f32 or x.numel() != n or not x.is_contiguous()):
                 self._refuse(f"muon_step: expected contiguous float32 vectors of {n} elements on cuda:{self.device}")
-        d = MuonDesc(grad_scale, lr, mu, weight_decay, (C.c_double * 3)(*(coeffs or (0.0, 0.0, 0.0))), ns_eps, adam_lr, beta1, beta2, adam_eps, int(nesterov), steps)
+        d = MuonDesc(grad_scale, lr, mu, weight_decay, (C.c_double * 3)(*(coeffs or (0.0, 0.0, 0.0))), ns_eps, adam_lr, beta1, beta2, adam_eps, int(nesterov),
+                     self._steps(steps, "muon_step"))
         mats = None
         if matrices is not None:
+            if any(not -(1 << 31) <= size < 1 << 31 for mat in matrices if not isinstance(mat, Matrix) for size in mat[1:3]):
+                self._refuse("muon_step: a matrix has 1 to 2^17 rows and columns")
             mats = (Matrix * max(len(matrices), 1))(*matrices)
         p = [x.data_ptr() if x is not None else None for x in (params, momentum, adam_v, grads, *new)]
         cur = self._enter(params, momentum, adam_v, grads, *new)

@@ -231,3 +231,26 @@ def test_orthogonalize_of_interleaved_matrices(pkg, ctx, heads, rows, cols, dtyp
     assert pkg.LP_FP32 == 0 and pkg.LP_BF16 == 1
     bad = lambda ld, stride: lib.lp_orthogonalize(ctx.h, prec, heads, rows, cols, x.data_ptr(), heads * (cols + 1), cols + 1, 5, None, 1e-7, x.data_ptr(), ld, stride)
     assert bad(heads * (cols + 1), cols - 1) == -1 and bad(heads * (cols + 1) - 2, cols + 1) == -1 and bad(heads * (cols + 1), 0) == -1
+
+
+# ------------------------------------------------------------------------------------------ arguments beyond 32 bits
+def test_numbers_beyond_32_bits_are_refused_and_not_cut(pkg, ctx):
+    """2^32 is not id 0, 2^32 + 5 steps are not five, a matrix of 2^32 + 4 rows is not one of four."""
+    table = torch.randn(10, 8, device=DEV)
+    ids = torch.zeros(4, dtype=torch.int32, device=DEV)
+    U, vec = torch.randn(4, 4, device=DEV), torch.zeros(16, device=DEV)
+    for call in (lambda: ctx.embed(table, ids, padding_id=1 << 32), lambda: ctx.embed(table, ids, padding_id=-(1 << 32)),
+                 lambda: ctx.embed_grad(torch.ones(4, 8, device=DEV), ids, 10, padding_id=1 << 32), lambda: ctx.orthogonalize(U, steps=(1 << 32) + 5),
+                 lambda: ctx.muon_step(vec, vec, vec, vec, t=1, matrices=[(0, 4, 4)], steps=(1 << 32) + 5),
+                 lambda: ctx.muon_step(vec, vec, vec, vec, t=1, matrices=[(0, (1 << 32) + 4, 4)])):
+        with pytest.raises(pkg.LpError) as ei:
+            call()
+        assert ei.value.status == -1
+    assert (ctx.embed(table, ids, padding_id=0) == 0).all()
+    assert torch.equal(ctx.embed(table, ids, padding_id=pkg.LP_NO_PADDING), table[:1].expand(4, 8))
+    a, b = vec.clone(), vec.clone()
+    g = torch.randn(16, device=DEV)
+    ctx.muon_step(a, torch.zeros_like(a), None, g, t=1, matrices=[(0, 4, 4)])
+    ctx.muon_step(b, torch.zeros_like(b), None, g, t=1, matrices=[pkg.Matrix(0, 4, 4)])
+    assert torch.equal(a, b) and (a != 0).all()
+    ctx.stats()
