@@ -34,6 +34,10 @@ def gen(seed):
     return torch.Generator().manual_seed(seed)
 
 
+def rel(a, b):
+    return ((a.cpu().double() - b).norm() / b.norm()).item()
+
+
 # ------------------------------------------------------------------------------------------ waits that run out
 @pytest.mark.parametrize("n", [20_000, 300_000])
 def test_sort_that_gives_up_is_reported_and_reads_nothing_outside(pkg, ctx, n):
@@ -253,4 +257,28 @@ def test_numbers_beyond_32_bits_are_refused_and_not_cut(pkg, ctx):
     ctx.muon_step(a, torch.zeros_like(a), None, g, t=1, matrices=[(0, 4, 4)])
     ctx.muon_step(b, torch.zeros_like(b), None, g, t=1, matrices=[pkg.Matrix(0, 4, 4)])
     assert torch.equal(a, b) and (a != 0).all()
+    ctx.stats()
+
+
+# ------------------------------------------------------------------------------------------ workspace of an update
+def test_workspace_of_an_update_follows_its_matrices(ctx):
+    """One long matrix does not make the others' arenas as wide as itself: 100 x 100,000 takes about 0.2 GB and 2048 x 2048 0.1 GB, in
+    common arenas 3.5 GB.  The results are those of calls with one matrix each: the same bits for the one that shares no launch, and
+    within the tolerance of an update (1e-6) on both sides where the company decides which kernel multiplies."""
+    shapes = [(100, 100_000), (2048, 2048), (70, 64)]
+    mats, n = [], 0
+    for r, c in shapes:
+        mats.append((n, r, c))
+        n += r * c + 5
+    g = gen(4)
+    p, m, v, gr = (torch.randn(n, generator=g).to(DEV) for _ in range(4))
+    v.abs_()
+    base = ctx.stats().workspace_bytes
+    new = ctx.muon_step(p, m, v, gr, t=3, matrices=mats, out=tuple(torch.empty_like(p) for _ in range(3)))
+    assert ctx.stats().workspace_bytes - base < 400e6
+    for i, (at, r, c) in enumerate(mats):
+        end = at + r * c + 5   # the matrix and the five numbers behind it
+        alone = ctx.muon_step(p[at:end].clone(), m[at:end].clone(), v[at:end].clone(), gr[at:end].clone(), t=3, matrices=[(0, r, c)])
+        assert rel(new[0][at:end], alone[0].double().cpu()) <= (0.0 if i == 0 else 2e-6)
+        assert torch.equal(new[1][at:end], alone[1]) and torch.equal(new[2][at:end], alone[2])
     ctx.stats()
