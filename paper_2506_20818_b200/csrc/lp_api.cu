@@ -2167,7 +2167,11 @@ static lp_status op_workspace(lp_ctx *ctx, size_t bytes, uint8_t **out)
         ctx->op_ws = nullptr;
         ctx->op_ws_bytes = 0;
         ctx->op_ws_captured = false;
-        CK(cudaMalloc((void **)&ctx->op_ws, bytes));
+        if (cudaMalloc((void **)&ctx->op_ws, bytes) != cudaSuccess) {
+            cudaGetLastError();  // the refused allocation is no later call's error
+            ctx->op_ws = nullptr;
+            return fail(ctx, LP_ENOMEM, "no device memory for a workspace of " + std::to_string(bytes) + " bytes");
+        }
         ctx->op_ws_bytes = bytes;
     }
     ctx->op_ws_captured |= capture != cudaStreamCaptureStatusNone;

@@ -282,3 +282,24 @@ def test_workspace_of_an_update_follows_its_matrices(ctx):
         assert rel(new[0][at:end], alone[0].double().cpu()) <= (0.0 if i == 0 else 2e-6)
         assert torch.equal(new[1][at:end], alone[1]) and torch.equal(new[2][at:end], alone[2])
     ctx.stats()
+
+
+def test_workspace_that_cannot_be_had_fails_that_call_alone(pkg, ctx):
+    """LP_ENOMEM, nothing written, and the next call is as before."""
+    U = torch.randn(100, 140, generator=gen(6)).to(DEV)
+    want = ctx.orthogonalize(U)
+    n = 12_000   # 3.5 GB of workspace
+    p, m, g = (torch.ones(n * n, device=DEV) for _ in range(3))
+    torch.cuda.empty_cache()
+    free, _ = torch.cuda.mem_get_info()
+    taken = torch.empty(max(0, free - (2 << 30)), dtype=torch.uint8, device=DEV)   # 2 GB are left
+    try:
+        with pytest.raises(pkg.LpError) as ei:
+            ctx.muon_step(p, m, None, g, t=1, matrices=[(0, n, n)])
+        assert ei.value.status == -3
+        assert (p == 1.0).all() and (m == 1.0).all()
+        assert torch.equal(ctx.orthogonalize(U), want)
+        ctx.stats()
+    finally:
+        del taken
+        torch.cuda.empty_cache()
