@@ -303,3 +303,145 @@ def test_workspace_that_cannot_be_had_fails_that_call_alone(pkg, ctx):
     finally:
         del taken
         torch.cuda.empty_cache()
+
+
+# ------------------------------------------------------------------------------------------ the kernel of the large products
+# It is the only one that launches every product by itself, so the launches of a call tell that it was reached.
+def iterate(U, steps=5, eps=1e-7, dtype=F64):
+    """The iteration as it is written down, in `dtype`, on the GPU."""
+    tall = U.shape[-2] > U.shape[-1]
+    X = (U.mT if tall else U).to(dtype)
+    X = X / (torch.linalg.matrix_norm(X, keepdim=True) + eps)
+    a, b, c = COEFFS
+    for _ in range(steps):
+        A = X @ X.mT
+        X = a * X + (b * A + c * (A @ A)) @ X
+    return X.mT if tall else X
+
+
+def by_products(ctx, call, steps=5, groups=1):
+    before = ctx.stats().kernel_launches
+    got = call()
+    assert ctx.stats().kernel_launches - before == groups * (2 + 3 * steps)
+    return got
+
+
+def gpu_rel(a, b):
+    return ((a.double() - b).norm() / b.norm()).item()
+
+
+LARGE = [(F32, 1, 2049, 2111), (F32, 1, 2111, 2049), (F32, 1, 1090, 1025), (F32, 1, 1600, 1700), (F32, 6, 900, 1100), (F32, 5, 1100, 900), (F32, 16, 520, 530),
+         (BF16, 1, 2049, 2111), (BF16, 1, 2111, 2049), (BF16, 1, 1600, 1700), (BF16, 6, 900, 1100), (BF16, 5, 1100, 900), (BF16, 3, 1500, 1400), (BF16, 3, 1401, 1499)]
+
+
+@pytest.mark.parametrize("dtype,batch,rows,cols", LARGE)
+def test_large_orthogonalize(ctx, dtype, batch, rows, cols):
+    """Wide, tall, batches, odd sizes; into rows apart with even and odd pitch and base; in place."""
+    U = (1e-3 * torch.randn(batch, rows, cols, generator=gen(rows + cols))).to(dtype).to(DEV)
+    want = iterate(U)
+    got = by_products(ctx, lambda: ctx.orthogonalize(U))
+    for i in range(batch):
+        assert gpu_rel(got[i], want[i]) <= ORTH_TOL[dtype]
+    assert torch.equal(ctx.orthogonalize(U), got)
+    for extra, first in ((2, 0), (3, 1), (8, 8), (5, 2)):
+        wide = torch.full((batch, rows + 1, cols + extra + first), 7.0, dtype=dtype, device=DEV)
+        out = wide[:, :rows, first:first + cols]
+        ctx.orthogonalize(U, out=out)
+        assert torch.equal(out, got)
+        out.copy_(U)
+        ctx.orthogonalize(out, out=out)
+        assert torch.equal(out, got)
+        out.fill_(7.0)
+        assert (wide == 7.0).all()
+    ctx.stats()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,cols", [(1600, 1700), (1711, 1600)])
+@pytest.mark.parametrize("kind", ["rank1", "rank3", "zero_rows", "spike", "large", "tiny"])
+def test_large_orthogonalize_spectra(ctx, dtype, rows, cols, kind):
+    """No further from 64 bits than FP32 matrix products are where those miss the tolerance (directions that U lacks)."""
+    g = gen(rows)
+    U = torch.randn(rows, cols, generator=g)
+    if kind in ("rank1", "rank3"):
+        r = int(kind[-1])
+        U = torch.randn(rows, r, generator=g) @ torch.randn(r, cols, generator=g)
+    elif kind == "zero_rows":
+        U[::2] = 0
+        U[:, 5:9] = 0
+    elif kind == "spike":
+        U = torch.zeros(rows, cols)
+        U[17, 33] = 5.0
+    elif kind in ("large", "tiny"):
+        U *= 1e30 if kind == "large" else 1e-30
+    eps = 0.0 if kind == "tiny" else 1e-7
+    U = U.to(dtype).to(DEV)
+    want = iterate(U, eps=eps)
+    got = by_products(ctx, lambda: ctx.orthogonalize(U, eps=eps))
+    tol = ORTH_TOL[dtype]
+    if dtype == F32 and kind not in ("large", "tiny"):  # whose squares leave FP32
+        tol = max(tol, gpu_rel(iterate(U, dtype=F32), want))
+    assert gpu_rel(got, want) <= tol
+    if kind == "zero_rows":
+        assert (got[::2] == 0).all() and (got[:, 5:9] == 0).all()
+
+
+@pytest.mark.parametrize("steps", [1, 2, 7])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_large_orthogonalize_steps(ctx, dtype, steps):
+    U = torch.randn(2, 1700, 1500, generator=gen(steps)).to(dtype).to(DEV)
+    got = by_products(ctx, lambda: ctx.orthogonalize(U, steps=steps), steps)
+    want = iterate(U, steps)
+    assert max(gpu_rel(got[i], want[i]) for i in range(2)) <= ORTH_TOL[dtype]
+
+
+@pytest.mark.parametrize("shapes,gap", [([(1000, 1999), (1999, 1500), (1500, 417)], 333), ([(1600, 1600), (64, 1000), (1000, 30)], 0), ([(1801, 1799)], 5000)])
+@pytest.mark.parametrize("nesterov", [True, False])
+def test_large_muon_step(ctx, shapes, gap, nesterov):
+    """Several matrices in one launch, wide and tall, Adam steps between them; out of place and in place."""
+    mats, n = [], 0
+    for r, c in shapes:
+        n += gap
+        mats.append((n, r, c))
+        n += r * c
+    n += gap
+    g = gen(n)
+    p, m, gr = 0.05 * torch.randn(n, generator=g), 1e-3 * torch.randn(n, generator=g), 1e-3 * torch.randn(n, generator=g)
+    v = 1e-6 * torch.rand(n, generator=g)
+    d = [x.to(DEV) for x in (p, m, v, gr)]
+    P, M, V, G = (x.double() for x in d)
+    G = 0.5 * G
+    lr, mu, wd, b1, b2, t = 0.02, 0.95, 0.01, 0.9, 0.999, 3
+    nm, nv = b1 * M + (1 - b1) * G, b2 * V + (1 - b2) * G * G
+    new = P - 1e-3 * (nm / (1 - b1**t)) / ((nv / (1 - b2**t)).sqrt() + 1e-8)
+    for at, r, c in mats:
+        s = slice(at, at + r * c)
+        nm[s] = mu * M[s] + G[s]
+        nv[s] = V[s]
+        u = G[s] + mu * nm[s] if nesterov else nm[s]
+        new[s] = (1 - lr * wd) * P[s] - lr * max(1.0, c / r) ** 0.5 * iterate(u.view(r, c)).reshape(-1)
+    keep = [x.clone() for x in d]
+    out = tuple(torch.full((n,), 5.0, device=DEV) for _ in range(3))
+    kw = dict(t=t, matrices=mats, nesterov=nesterov, weight_decay=wd, grad_scale=0.5)
+    by_products(ctx, lambda: ctx.muon_step(*d, out=out, **kw))
+    assert all(torch.equal(x, y) for x, y in zip(d, keep))
+    for x, y in zip(out, (new, nm, nv)):
+        assert gpu_rel(x, y) <= 1e-6
+    ctx.muon_step(*d, **kw)
+    assert all(torch.equal(x, y) for x, y in zip(d[:3], out))
+    ctx.stats()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_bounded_wait_of_the_large_products(pkg, ctx, dtype):
+    U = torch.randn(1600, 1700, generator=gen(9)).to(dtype).to(DEV)
+    want = by_products(ctx, lambda: ctx.orthogonalize(U))
+    ctx.set_wait_limit(2_000_000, 16)
+    ctx.orthogonalize(U)
+    with pytest.raises(pkg.LpError) as ei:
+        ctx.stats()
+    assert ei.value.status == -6
+    ctx.set_wait_limit(2_000_000_000, 0)
+    ctx.stats()
+    assert torch.equal(ctx.orthogonalize(U), want)
+    ctx.stats()
