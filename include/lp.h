@@ -418,7 +418,9 @@ lp_status lp_embed_grad(lp_ctx *ctx, int32_t dout_prec, const void *dout, int64_
  *   X_0 = U / (|U|_F + eps),  X <- a X + (b A + c A^2) X with A = X X^T, `steps` times (1..64); out = X.
  * A matrix with more rows than columns is iterated transposed.  A matrix of zeros gives zeros, also with eps = 0.
  *   prec     : LP_FP32 or LP_BF16, of U and out.  The products run on the tensor cores with FP32 accumulators: LP_BF16
- *              holds X, A and b A + c A^2 as FP16 numbers (11 bits), LP_FP32 as pairs of them (22 bits)
+ *              holds X, A and b A + c A^2 as FP16 numbers (11 bits), LP_FP32 as pairs of them (22 bits).  FP16 has less range than FP32:
+ *              the error is about 1e-6 of the whole matrix, but rows or columns smaller than the others by more than about 1e-5
+ *              keep fewer bits of themselves (FP32 rows of 1e-6 of the others: up to 4e-5 off, relative to themselves)
  *   U, out   : DEVICE, row pitch ld_*, matrices stride_* elements apart; out may be U itself.  Matrices of out may lie behind one
  *              another or between one another's rows (stride_out < ld_out); stride_u may also be 0
  *   coeffs   : HOST double[3] = {a, b, c}, or NULL for {3.4445, -4.7750, 2.0315}.  LP_EINVAL when singular values of

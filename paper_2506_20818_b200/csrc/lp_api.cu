@@ -2270,14 +2270,13 @@ extern "C" lp_status lp_embed_grad(lp_ctx *ctx, int32_t dout_prec, const void *d
 constexpr int NS_MAX_DIM = 1 << 17;
 constexpr size_t NS_WORKSPACE = (size_t)4 << 30;  // repetitions are taken in groups that fit this (one matrix may need more)
 
-static lp_status check_ns(lp_ctx *ctx, const char *who, int32_t steps, const double *coeffs, double eps, double (&c)[3])
+static lp_status check_ns(lp_ctx *ctx, const char *who, int32_t steps, const double *coeffs, double eps, NsPoly &poly)
 {
     const std::string w(who);
-    c[0] = 3.4445; c[1] = -4.7750; c[2] = 2.0315;
-    if (coeffs) { c[0] = coeffs[0]; c[1] = coeffs[1]; c[2] = coeffs[2]; }
+    const double standard[3] = {3.4445, -4.7750, 2.0315}, *c = coeffs ? coeffs : standard;
     if (steps < 1 || steps > 64) return fail(ctx, LP_EINVAL, w + ": steps must be in [1, 64]");
     if (!(eps >= 0.0) || !std::isfinite(eps)) return fail(ctx, LP_EINVAL, w + ": eps must be finite and not negative");
-    if (!ns_coefficients_ok(c[0], c[1], c[2], steps))
+    if (!ns_coefficients_ok(c[0], c[1], c[2], steps, poly))
         return fail(ctx, LP_EINVAL, w + ": with these coefficients singular values in [0, 1] can grow beyond 2 (or b A + c A^2 beyond 200)");
     return LP_OK;
 }
@@ -2318,8 +2317,8 @@ extern "C" lp_status lp_orthogonalize(lp_ctx *ctx, int32_t prec, int64_t batch, 
         const bool apart = stride_out >= (rows - 1) * ld_out + cols, between = stride_out >= cols && (ld_out - cols) / (batch - 1) >= stride_out;
         if (stride_u < 0 || (!apart && !between)) return fail(ctx, LP_EINVAL, "lp_orthogonalize: matrices of the result overlap");
     }
-    double c[3];
-    lp_status s = check_ns(ctx, "lp_orthogonalize", steps, coeffs, eps, c);
+    NsPoly poly{};
+    lp_status s = check_ns(ctx, "lp_orthogonalize", steps, coeffs, eps, poly);
     if (s != LP_OK) return s;
     if (batch == 0 || rows == 0 || cols == 0) return LP_OK;
     if (!U || !out) return fail(ctx, LP_EINVAL, "lp_orthogonalize: null array");
@@ -2347,8 +2346,8 @@ extern "C" lp_status lp_orthogonalize(lp_ctx *ctx, int32_t prec, int64_t batch, 
         const NsTarget to{(uint8_t *)out + (size_t)(b0 * stride_out) * elem, prec == LP_BF16, nullptr, 0.f};
         std::string err;
         NsAdam none{};
-        const bool ok = parts == 2 ? ns_run<2>(ctx->tc, ctx->ex, src, g, l, none, ctx->ns_counters, steps, c[0], c[1], c[2], eps, to, ws, err)
-                                   : ns_run<1>(ctx->tc, ctx->ex, src, g, l, none, ctx->ns_counters, steps, c[0], c[1], c[2], eps, to, ws, err);
+        const bool ok = parts == 2 ? ns_run<2>(ctx->tc, ctx->ex, src, g, l, none, ctx->ns_counters, steps, poly, eps, to, ws, err)
+                                   : ns_run<1>(ctx->tc, ctx->ex, src, g, l, none, ctx->ns_counters, steps, poly, eps, to, ws, err);
         if (!ok) return fail(ctx, LP_ECUDA, "lp_orthogonalize: " + err);
     }
     CK_LAUNCH();
@@ -2388,9 +2387,9 @@ extern "C" lp_status lp_muon_step(lp_ctx *ctx, const lp_muon_desc *d, const lp_m
         end = m.offset + (int64_t)m.rows * m.cols;
     }
     vectors |= end < n_params;
-    double c[3];
+    NsPoly poly{};
     const bool default_coeffs = d->coeffs[0] == 0.0 && d->coeffs[1] == 0.0 && d->coeffs[2] == 0.0;
-    lp_status s = check_ns(ctx, "lp_muon_step", d->steps, default_coeffs ? nullptr : d->coeffs, d->eps, c);
+    lp_status s = check_ns(ctx, "lp_muon_step", d->steps, default_coeffs ? nullptr : d->coeffs, d->eps, poly);
     if (s != LP_OK) return s;
     for (double x : {d->grad_scale, d->lr, d->momentum, d->weight_decay, d->adam_lr, d->adam_beta1, d->adam_beta2, d->adam_eps})
         if (!std::isfinite(x)) return fail(ctx, LP_EINVAL, "lp_muon_step: a hyper-parameter is not finite");
@@ -2462,7 +2461,7 @@ extern "C" lp_status lp_muon_step(lp_ctx *ctx, const lp_muon_desc *d, const lp_m
         src.grad_scale = (float)d->grad_scale; src.mu = (float)d->momentum; src.nesterov = d->nesterov;
         const NsTarget to{new_params, 0, params, (float)(1.0 - d->lr * d->weight_decay)};
         std::string err;
-        if (!ns_run<2>(ctx->tc, ctx->ex, src, g, l, ad, ctx->ns_counters, d->steps, c[0], c[1], c[2], d->eps, to, ws, err)) return fail(ctx, LP_ECUDA, "lp_muon_step: " + err);
+        if (!ns_run<2>(ctx->tc, ctx->ex, src, g, l, ad, ctx->ns_counters, d->steps, poly, d->eps, to, ws, err)) return fail(ctx, LP_ECUDA, "lp_muon_step: " + err);
         i0 = i1;
     } while (i0 < mats.size());
     CK_LAUNCH();

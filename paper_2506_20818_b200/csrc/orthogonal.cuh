@@ -5,8 +5,11 @@
 // maps every singular value s of X_0 through the odd polynomial a s + b s^3 + c s^5 again and again and leaves the
 // singular vectors.  The products run on the tensor cores with FP16 operands and FP32 accumulators.  FP16 carries eleven
 // significant bits where BF16 carries eight, at the same rate, and the range it lacks is not needed here: the values
-// are bounded by the polynomial (the host refuses coefficients for which they are not), so X is held as 2^12 X and A and B
-// as 2^8 A, 2^8 B, which keeps the parts that matter inside the normal numbers of FP16.
+// are bounded by the polynomial (the host refuses coefficients for which they are not), so X is held as 2^14 X, A as 2^13 A and B as
+// 2^8 B to 2^13 B, as far as its coefficients' bound allows (2^12 B for the default): the largest values lie just below the end of FP16.
+// What a matrix holds far below its largest values ends at FP16's 2^-24: FP32 rows of 1e-5 of the others keep 4e-7 to 4e-6 of
+// themselves, rows of 1e-6 2e-6 to 4e-5 (64 x 64 to 800 x 900; with 2^12 X and 2^8 A, B it was 6e-6 to 1e-4 and 6e-5 to 1e-3), where
+// FP32 products keep 5e-7 at any size.  Of the whole matrix these errors are 1e-9.
 // X is kept twice: in FP32, from which the term a X of every step is taken, and as FP16 operands.
 //   BF16 results : X, A and B are one FP16 number per value in the products
 //   FP32 results : pairs of FP16 numbers hi + lo (22 bits), products hi*lo + lo*hi + hi*hi; the accumulator of the matrix
@@ -15,7 +18,7 @@
 // Why X keeps more bits than its operands: rounding X to eleven bits would add a matrix of full rank, and whatever lies
 // in directions that X hardly has is multiplied by a in every step (3.4^5 = 480 for five).  The errors of the products are
 // of the form dB X and B dX, which vanish in such directions, so they stay at their own size.  For the same reason X_0 is
-// U times a power of two 2^12 r / |U|, r in [1/2, 1), which is exact; b / r^2 and c / r^4 in the place of b and c keep r X
+// U times a power of two 2^14 r / |U|, r in [1/2, 1), which is exact; b / r^2 and c / r^4 in the place of b and c keep r X
 // going in the place of X, and the result is divided by r.
 // A matrix with more rows than columns is iterated transposed: m = min(rows, cols), n = max(rows, cols).
 //
@@ -33,8 +36,8 @@
 #include "gemm_tc.cuh"
 
 constexpr int NS_MAX_MATS = 16;       // descriptors in one launch group (they travel as kernel arguments, 4 KiB in all)
-constexpr float NS_X_SCALE = 4096.f;  // X is held as 2^12 X
-constexpr float NS_A_SCALE = 256.f;   // A and B as 2^8 A, 2^8 B
+constexpr float NS_X_SCALE = 16384.f;  // X is held as 2^14 X: |X| <= 2
+constexpr float NS_A_SCALE = 8192.f;   // A as 2^13 A: |A| <= 4
 
 struct NsMat {
     int m, n;              // oriented sizes, m <= n
@@ -55,6 +58,11 @@ struct NsMat {
 struct NsGroup {
     int count;
     NsMat mat[NS_MAX_MATS];
+};
+
+struct NsPoly {          // X <- a X + B X, B = b A + c A^2, in the scales that X, A and B are held in
+    float a, b, c;
+    float unscale;       // of B
 };
 
 struct NsX {             // one of the two buffers of X
@@ -220,7 +228,7 @@ template <int T> LP_DEVINL void ns_norm_block(const NsSource &s, const NsGroup &
     ns_sync<T>();
 }
 
-// |U| + eps = 2^e r with r in [1/2, 1): X_0 is held as 2^12 2^-e U, which is 2^12 r times U / (|U| + eps)
+// |U| + eps = 2^e r with r in [1/2, 1): X_0 is held as 2^14 2^-e U, which is 2^14 r times U / (|U| + eps)
 LP_DEVINL void ns_start_scale(double norm, float &r, double &pow2)
 {
     int e = 0;
@@ -327,7 +335,7 @@ enum { NS_GRAM = 0, NS_POLY = 1, NS_APPLY = 2, NS_LAST = 3 };
 
 struct NsPhase {
     int kind;
-    float a, b, c;
+    NsPoly poly;
     int lo_rows_a, lo_rows_b;            // rows between the hi and lo parts of the first and second operand's arena
     int x_row0;                          // first row of the X buffer that is read
     const __half *A;                     // POLY: the addend b A
@@ -419,7 +427,7 @@ struct NsChain {
     NsChainIo io[2][3];                  // [step parity][kind], read from constant memory where needed: pointers held in registers spill
     int parts_rows_x, parts_rows_a;      // rows between the hi and lo parts of X and of A, B
     int steps;
-    float a, b, c;
+    NsPoly poly;
     double eps;
     NsX X0;
     double *partial;
@@ -938,8 +946,8 @@ __global__ void __launch_bounds__(NSC_THREADS, 1) ns_chain_kernel(const __grid_c
                         for (int i = 0; i < 16; ++i) v[i] += lost[i];
                     }
                     const float r2 = inv_r * inv_r;
-                    const float f = kind == NS_GRAM ? NS_A_SCALE / (NS_X_SCALE * NS_X_SCALE) : kind == NS_POLY ? p.c / NS_A_SCALE * r2 * r2 : 1.f / NS_A_SCALE;
-                    const float h = kind == NS_POLY ? p.b * r2 : p.a;
+                    const float f = kind == NS_GRAM ? NS_A_SCALE / (NS_X_SCALE * NS_X_SCALE) : kind == NS_POLY ? p.poly.c * r2 * r2 : p.poly.unscale;
+                    const float h = kind == NS_POLY ? p.poly.b * r2 : p.poly.a;
                     // the sums go to shared memory, [block that finishes][row][64 / C] with the 16-byte pieces of a row permuted by the
                     // row; every other block of the cluster gets its share by one bulk copy
                     constexpr int SHARE = 128 * NSC_BN / C, PIECES = 16 / C;
@@ -1056,7 +1064,7 @@ template <int PARTS> constexpr int NSB_SMEM = 2 * PARTS * NSB_PART * 2 + NSB_SIZ
 
 struct NsBlock {
     int steps, matrices;
-    float a, b, c;
+    NsPoly poly;
     double eps;
     void *dst;
     int bf16_dst;
@@ -1173,7 +1181,7 @@ __global__ void __launch_bounds__(NSB_THREADS, 1) ns_block_kernel(const __grid_c
         }
     }
     const float inv_r = 1.f / r, r2 = inv_r * inv_r;
-    const float bf = p.b * r2, cf = p.c / NS_A_SCALE * r2 * r2, af = p.a;
+    const float bf = p.poly.b * r2, cf = p.poly.c * r2 * r2, af = p.poly.a;
     fence_async_proxy();
     tc_fence_before();
     __syncthreads();
@@ -1218,7 +1226,7 @@ __global__ void __launch_bounds__(NSB_THREADS, 1) ns_block_kernel(const __grid_c
                 add[0] = x0.x; add[1] = x0.y; add[2] = x0.z; add[3] = x0.w;
                 add[4] = x1.x; add[5] = x1.y; add[6] = x1.z; add[7] = x1.w;
             }
-            const float f = kind == NS_GRAM ? NS_A_SCALE / (NS_X_SCALE * NS_X_SCALE) : kind == NS_POLY ? cf : 1.f / NS_A_SCALE;
+            const float f = kind == NS_GRAM ? NS_A_SCALE / (NS_X_SCALE * NS_X_SCALE) : kind == NS_POLY ? cf : p.poly.unscale;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 v[j] *= f;  // a power of two where precision counts
@@ -1501,8 +1509,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NSP_THREADS, 1)
             const int row0 = ti * 256 + rank * 128 + q * 32, col0 = tj * BN + cg * COLS;
             const bool live = row0 < mat.mp && col0 < width;  // whole blocks (sizes are padded to multiples of 64)
             const float inv_r = p.inv_r[mat.index + rep], r2 = inv_r * inv_r;
-            const float f = p.kind == NS_GRAM ? NS_A_SCALE / (NS_X_SCALE * NS_X_SCALE) : p.kind == NS_POLY ? p.c / NS_A_SCALE * r2 * r2 : 1.f / NS_A_SCALE;
-            const float h = p.kind == NS_POLY ? p.b * r2 : p.a;
+            const float f = p.kind == NS_GRAM ? NS_A_SCALE / (NS_X_SCALE * NS_X_SCALE) : p.kind == NS_POLY ? p.poly.c * r2 * r2 : p.poly.unscale;
+            const float h = p.kind == NS_POLY ? p.poly.b * r2 : p.poly.a;
             const int pitch = square ? p.pitch_a : p.next.pitch;
             float v[PARTS == 2 ? COLS : 16];
             // the addends of 16 columns, as they lie in memory (POLY: 4 + 4 FP16, else 4 FP32), one block of columns ahead of their use
@@ -1743,14 +1751,15 @@ static bool ns_make_map(const TcState &tc, CUtensorMap *map, const __half *base,
                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Bounds of the iteration: with |X| <= 1 at the start, every later |X| must stay below 2 and |B| below 200 for the FP16
-// scales above.  The largest value of |a s + b s^3 + c s^5| on [0, top] is at an end or where its derivative vanishes.
-static bool ns_coefficients_ok(double a, double b, double c, int steps)
+// Bounds of the iteration: with |X| <= 1 at the start, every later |X| must stay below 2 and |B| below 200 for FP16 to
+// hold them.  The largest value of |a s + b s^3 + c s^5| on [0, top] is at an end or where its derivative vanishes.
+static bool ns_coefficients_ok(double a, double b, double c, int steps, NsPoly &poly)
 {
     if (!(std::isfinite(a) && std::isfinite(b) && std::isfinite(c))) return false;
-    double top = 1.0;
+    double top = 1.0, largest_b = 0.0;
     for (int k = 0; k < steps; ++k) {
-        if (std::fabs(b) * top * top + std::fabs(c) * top * top * top * top > 200.0) return false;
+        largest_b = std::max(largest_b, std::fabs(b) * top * top + std::fabs(c) * top * top * top * top);
+        if (largest_b > 200.0) return false;
         auto f = [&](double s) { return std::fabs(s * (a + s * s * (b + s * s * c))); };
         double best = f(top);
         const double disc = 9.0 * b * b - 20.0 * a * c;
@@ -1766,6 +1775,9 @@ static bool ns_coefficients_ok(double a, double b, double c, int steps)
         if (best > 2.0) return false;
         top = std::max(best, 1e-30);
     }
+    float b_scale = 256.f;  // the largest power of two for which B stays inside FP16 (65,504), the roundings of A and B included
+    while (b_scale < NS_A_SCALE && 2.0 * b_scale * largest_b <= 60000.0) b_scale *= 2.f;
+    poly = {(float)a, (float)b * (b_scale / NS_A_SCALE), (float)c * (b_scale / (NS_A_SCALE * NS_A_SCALE)), 1.f / b_scale};
     return true;
 }
 
@@ -1861,8 +1873,8 @@ static NsCost ns_chain_cost(int parts, int c)
 static NsCost ns_pair_cost(int parts) { return parts == 2 ? NsCost{8.0, 5.0, 0.42} : NsCost{13.0, 0.5, 0.29}; }
 
 template <int PARTS>
-static bool ns_run(TcState &tc, Exec &ex, const NsSource &src, NsGroup &g, const NsLayout &l, const NsAdam &adam, unsigned *counters, int steps, double a, double b,
-                   double c, double eps, const NsTarget &out, uint8_t *ws, std::string &err)
+static bool ns_run(TcState &tc, Exec &ex, const NsSource &src, NsGroup &g, const NsLayout &l, const NsAdam &adam, unsigned *counters, int steps,
+                   const NsPoly &poly, double eps, const NsTarget &out, uint8_t *ws, std::string &err)
 {
     const size_t nx = l.x_elems(), na = l.a_elems();
     NsX X[2];
@@ -1884,7 +1896,7 @@ static bool ns_run(TcState &tc, Exec &ex, const NsSource &src, NsGroup &g, const
     if (small) {
         NsBlock p{};
         p.steps = steps; p.matrices = l.matrices;
-        p.a = (float)a; p.b = (float)b; p.c = (float)c; p.eps = eps;
+        p.poly = poly; p.eps = eps;
         p.dst = out.dst; p.bf16_dst = out.bf16_dst; p.params = out.params; p.keep = out.keep;
         p.err = tc.err_word; p.wait_ns = tc.wait_limit_ns; p.extra_tx = tc.overdeclare_tx;
         tc.overdeclare_tx = 0;
@@ -1919,7 +1931,7 @@ static bool ns_run(TcState &tc, Exec &ex, const NsSource &src, NsGroup &g, const
         }
         p.parts_rows_x = l.rows_x; p.parts_rows_a = l.rows_a;
         p.steps = steps;
-        p.a = (float)a; p.b = (float)b; p.c = (float)c; p.eps = eps;
+        p.poly = poly; p.eps = eps;
         p.X0 = X[0];
         p.partial = partial; p.inv_r = inv_r;
         p.norm_blocks = l.norm_blocks; p.adam_blocks = adam_blocks; p.conv_blocks = l.conv_blocks; p.tiles_a = tiles_a; p.tiles_x = tiles_x;
@@ -1953,7 +1965,7 @@ static bool ns_run(TcState &tc, Exec &ex, const NsSource &src, NsGroup &g, const
     launch_dep(ns_convert_kernel<PARTS>, dim3(l.conv_blocks), dim3(NS_THREADS), 0, ex.st, src, g, partial, eps, X[0], inv_r);
     ex.launches += 1;
     NsPhase p{};
-    p.a = (float)a; p.b = (float)b; p.c = (float)c;
+    p.poly = poly;
     p.err = tc.err_word;
     p.wait_ns = tc.wait_limit_ns;
     p.pitch_a = l.pitch_a;

@@ -445,3 +445,19 @@ def test_bounded_wait_of_the_large_products(pkg, ctx, dtype):
     ctx.stats()
     assert torch.equal(ctx.orthogonalize(U), want)
     ctx.stats()
+
+
+# ------------------------------------------------------------------------------------------ rows far smaller than the others
+@pytest.mark.parametrize("rows,cols", [(64, 64), (128, 100), (256, 512), (1000, 300), (800, 900), (1600, 1700)])
+def test_small_rows_keep_their_own_digits(ctx, rows, cols):
+    """FP32: half of the rows are 1e-5 of the others.  They grow by the same factors as everything small does, and come out as near to
+    64 bits, relative to themselves, as the whole matrix (2e-5).  FP32 numbers keep 24 bits of them; pairs of FP16 do only as long as
+    the scales leave their low parts above 2^-24: with values of a 2048 x 2048 matrix of about 2^-11, rows of 2^-17 of that, held
+    as 2^14 X, a rounding of 2^-25 is 2^-11 of them, a half of the rows' directions at random, amplified like the rows themselves."""
+    U = torch.randn(rows, cols, generator=gen(rows * 5 + cols)).to(DEV)
+    U[::2] *= 1e-5
+    want = iterate(U)
+    got = ctx.orthogonalize(U)
+    assert gpu_rel(got, want) <= ORTH_TOL[F32]
+    assert gpu_rel(got[::2], want[::2]) <= ORTH_TOL[F32]
+    ctx.stats()
