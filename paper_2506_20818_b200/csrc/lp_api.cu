@@ -137,7 +137,7 @@ struct lp_ctx {
     bool op_ws_captured = false;        // a captured launch uses the present one: it is kept when a larger one takes its place
     std::vector<void *> op_ws_kept;
     int64_t op_ws_kept_bytes = 0;
-    unsigned *ns_counters = nullptr;    // barrier counters of the orthogonalisation's chain kernel, zero between its launches
+    NsState ns;                         // of the orthogonalisation's chain kernel
     bf16 *w16 = nullptr, *w16t = nullptr;  // BF16 path: the parameter vector of the current call as BF16, as is and with every weight matrix transposed
     bf16 *w16s = nullptr;                  // ... and with the SAGE layers' [W_self ; W_neigh] stored side by side (see weights_cache_kernel)
     // One-pass SAGE layers l >= 1 on the tensor-core pair kernel take the input gradient as
@@ -300,19 +300,18 @@ extern "C" lp_status lp_create(lp_ctx **out, int32_t device, void *cuda_stream)
     ctx->device = device;
     ctx->ex.st = (cudaStream_t)cuda_stream;
     if (cudaMalloc((void **)&ctx->err_flag, 256) != cudaSuccess || cudaMalloc((void **)&ctx->exhausted_dev, 256) != cudaSuccess ||
-        cudaMallocHost((void **)&ctx->host_counts, 64 * sizeof(int)) != cudaSuccess ||
-        cudaMalloc((void **)&ctx->ns_counters, NSC_BARRIERS * sizeof(unsigned)) != cudaSuccess) {
-        delete ctx;
+        cudaMallocHost((void **)&ctx->host_counts, 64 * sizeof(int)) != cudaSuccess) {
+        lp_destroy(ctx);  // what there is so far
+        cudaGetLastError();
         return fail(nullptr, LP_ENOMEM, "lp_create: allocation failed");
     }
     cudaMemset(ctx->err_flag, 0, 256);
     ctx->embed_err = ctx->err_flag + 1;
     cudaMemset(ctx->exhausted_dev, 0, 256);
-    cudaMemset(ctx->ns_counters, 0, NSC_BARRIERS * sizeof(unsigned));
     std::string tc_err;
-    if (!tc_init(ctx->tc, tc_err) || !ns_init(tc_err)) {
-        cudaFree(ctx->err_flag); cudaFree(ctx->exhausted_dev); cudaFreeHost(ctx->host_counts); cudaFree(ctx->ns_counters);
-        delete ctx;
+    if (!tc_init(ctx->tc, tc_err) || !ns_init(ctx->ns, tc_err)) {
+        lp_destroy(ctx);
+        cudaGetLastError();
         return fail(nullptr, LP_ECUDA, "lp_create: " + tc_err);
     }
     *out = ctx;
@@ -331,7 +330,7 @@ extern "C" void lp_destroy(lp_ctx *ctx)
     tc_destroy(ctx->tc);
     cudaFree(ctx->op_ws);
     free_list(ctx->op_ws_kept);
-    cudaFree(ctx->ns_counters);
+    cudaFree(ctx->ns.counters);
     for (cudaEvent_t e : ctx->ex.prof.pool) cudaEventDestroy(e);
     cudaFree(ctx->err_flag);
     cudaFree(ctx->exhausted_dev);
@@ -2346,8 +2345,8 @@ extern "C" lp_status lp_orthogonalize(lp_ctx *ctx, int32_t prec, int64_t batch, 
         const NsTarget to{(uint8_t *)out + (size_t)(b0 * stride_out) * elem, prec == LP_BF16, nullptr, 0.f};
         std::string err;
         NsAdam none{};
-        const bool ok = parts == 2 ? ns_run<2>(ctx->tc, ctx->ex, src, g, l, none, ctx->ns_counters, steps, poly, eps, to, ws, err)
-                                   : ns_run<1>(ctx->tc, ctx->ex, src, g, l, none, ctx->ns_counters, steps, poly, eps, to, ws, err);
+        const bool ok = parts == 2 ? ns_run<2>(ctx->tc, ctx->ex, src, g, l, none, ctx->ns, steps, poly, eps, to, ws, err)
+                                   : ns_run<1>(ctx->tc, ctx->ex, src, g, l, none, ctx->ns, steps, poly, eps, to, ws, err);
         if (!ok) return fail(ctx, LP_ECUDA, "lp_orthogonalize: " + err);
     }
     CK_LAUNCH();
@@ -2461,7 +2460,7 @@ extern "C" lp_status lp_muon_step(lp_ctx *ctx, const lp_muon_desc *d, const lp_m
         src.grad_scale = (float)d->grad_scale; src.mu = (float)d->momentum; src.nesterov = d->nesterov;
         const NsTarget to{new_params, 0, params, (float)(1.0 - d->lr * d->weight_decay)};
         std::string err;
-        if (!ns_run<2>(ctx->tc, ctx->ex, src, g, l, ad, ctx->ns_counters, d->steps, poly, d->eps, to, ws, err)) return fail(ctx, LP_ECUDA, "lp_muon_step: " + err);
+        if (!ns_run<2>(ctx->tc, ctx->ex, src, g, l, ad, ctx->ns, d->steps, poly, d->eps, to, ws, err)) return fail(ctx, LP_ECUDA, "lp_muon_step: " + err);
         i0 = i1;
     } while (i0 < mats.size());
     CK_LAUNCH();

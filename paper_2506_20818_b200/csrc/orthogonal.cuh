@@ -1714,20 +1714,23 @@ template <int PARTS, int C> static cudaLaunchConfig_t ns_chain_config(int cluste
     return cfg;
 }
 
-// clusters of C blocks that are resident at the same time
+// clusters of C blocks that are resident at the same time on the current device
 template <int PARTS, int C> static int ns_chain_room()
 {
-    static int room = -1;
-    if (room < 0) {
-        cudaLaunchAttribute attr[2];
-        cudaLaunchConfig_t cfg = ns_chain_config<PARTS, C>(1, nullptr, attr);
-        cfg.numAttrs = 1;
-        if (cudaOccupancyMaxActiveClusters(&room, ns_chain_kernel<PARTS, C>, &cfg) != cudaSuccess) { cudaGetLastError(); room = 0; }
-    }
+    int room = 0;
+    cudaLaunchAttribute attr[2];
+    cudaLaunchConfig_t cfg = ns_chain_config<PARTS, C>(1, nullptr, attr);
+    cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&room, ns_chain_kernel<PARTS, C>, &cfg) != cudaSuccess) { cudaGetLastError(); room = 0; }
     return room;
 }
 
-static bool ns_init(std::string &err)
+struct NsState {                  // of a context
+    unsigned *counters = nullptr; // barrier counters of the chain kernel, zero between its launches
+    int room[2][3] = {};          // [parts - 1][log2 of the cluster size]: ns_chain_room of the context's device
+};
+
+static bool ns_init(NsState &ns, std::string &err)
 {
     if (!ns_chain_init<1, 1>() || !ns_chain_init<1, 2>() || !ns_chain_init<1, 4>() || !ns_chain_init<2, 1>() || !ns_chain_init<2, 2>() || !ns_chain_init<2, 4>() ||
         cudaFuncSetAttribute(ns_block_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, NSB_SMEM<1>) != cudaSuccess ||
@@ -1737,6 +1740,12 @@ static bool ns_init(std::string &err)
         err = "cannot raise the dynamic shared memory limit of the Newton-Schulz products";
         return false;
     }
+    if (cudaMalloc((void **)&ns.counters, NSC_BARRIERS * sizeof(unsigned)) != cudaSuccess || cudaMemset(ns.counters, 0, NSC_BARRIERS * sizeof(unsigned)) != cudaSuccess) {
+        err = "allocation of the counters of the Newton-Schulz products failed";
+        return false;
+    }
+    ns.room[0][0] = ns_chain_room<1, 1>(); ns.room[0][1] = ns_chain_room<1, 2>(); ns.room[0][2] = ns_chain_room<1, 4>();
+    ns.room[1][0] = ns_chain_room<2, 1>(); ns.room[1][1] = ns_chain_room<2, 2>(); ns.room[1][2] = ns_chain_room<2, 4>();
     return true;
 }
 
@@ -1873,7 +1882,7 @@ static NsCost ns_chain_cost(int parts, int c)
 static NsCost ns_pair_cost(int parts) { return parts == 2 ? NsCost{8.0, 5.0, 0.42} : NsCost{13.0, 0.5, 0.29}; }
 
 template <int PARTS>
-static bool ns_run(TcState &tc, Exec &ex, const NsSource &src, NsGroup &g, const NsLayout &l, const NsAdam &adam, unsigned *counters, int steps,
+static bool ns_run(TcState &tc, Exec &ex, const NsSource &src, NsGroup &g, const NsLayout &l, const NsAdam &adam, const NsState &ns, int steps,
                    const NsPoly &poly, double eps, const NsTarget &out, uint8_t *ws, std::string &err)
 {
     const size_t nx = l.x_elems(), na = l.a_elems();
@@ -1916,7 +1925,7 @@ static bool ns_run(TcState &tc, Exec &ex, const NsSource &src, NsGroup &g, const
     ns_tiles(g, 256, NSP_BN<PARTS>, true, tiles_a, tiles_x);
     double cost = ns_pair_cost(PARTS).step(g, pairs, tiles_a, tiles_x, 1);
     ns_tiles(g, 128, NSC_BN, false, tiles_a, tiles_x);
-    const int rooms[3] = {ns_chain_room<PARTS, 1>(), ns_chain_room<PARTS, 2>(), ns_chain_room<PARTS, 4>()};
+    const int(&rooms)[3] = ns.room[PARTS - 1];
     for (int i = 0; i < 3; ++i) {
         if (rooms[i] <= 0) continue;
         const double t = ns_chain_cost(PARTS, 1 << i).step(g, rooms[i], tiles_a, tiles_x, 1 << i);
@@ -1936,7 +1945,7 @@ static bool ns_run(TcState &tc, Exec &ex, const NsSource &src, NsGroup &g, const
         p.partial = partial; p.inv_r = inv_r;
         p.norm_blocks = l.norm_blocks; p.adam_blocks = adam_blocks; p.conv_blocks = l.conv_blocks; p.tiles_a = tiles_a; p.tiles_x = tiles_x;
         p.dst = out.dst; p.bf16_dst = out.bf16_dst; p.params = out.params; p.keep = out.keep;
-        p.counters = counters;
+        p.counters = ns.counters;
         p.err = tc.err_word; p.wait_ns = tc.wait_limit_ns; p.extra_tx = tc.overdeclare_tx;
         tc.overdeclare_tx = 0;
         const int cl = 1 << best;
