@@ -2328,7 +2328,7 @@ extern "C" lp_status lp_orthogonalize(lp_ctx *ctx, int32_t prec, int64_t batch, 
     NsGroup g{};
     g.count = 1;
     ns_orient(g.mat[0], rows, cols);
-    const size_t one = ns_layout(g).bytes(parts);
+    const size_t one = std::max<size_t>(1, ns_workspace(g, ns_layout(g), parts));
     const int64_t at_once = std::max<int64_t>(1, std::min<int64_t>({batch, (int64_t)(NS_WORKSPACE / one), (int64_t)1 << 16}));
     for (int64_t b0 = 0; b0 < batch; b0 += at_once) {
         NsMat &m = g.mat[0];
@@ -2337,7 +2337,7 @@ extern "C" lp_status lp_orthogonalize(lp_ctx *ctx, int32_t prec, int64_t batch, 
         m.dst_stride = stride_out; m.ld_dst = ld_out;
         const NsLayout l = ns_layout(g);
         uint8_t *ws = nullptr;
-        s = op_workspace(ctx, l.bytes(parts), &ws);
+        s = op_workspace(ctx, ns_workspace(g, l, parts), &ws);
         if (s != LP_OK) return s;
         NsSource src{};
         src.u = (const uint8_t *)U + (size_t)(b0 * stride_u) * elem;
@@ -2417,7 +2417,7 @@ extern "C" lp_status lp_muon_step(lp_ctx *ctx, const lp_muon_desc *d, const lp_m
     for (size_t i0 = 0; i0 < mats.size();) {
         NsGroup g{};
         i0 = group(i0, g);
-        bytes = std::max(bytes, ns_layout(g).bytes(2));
+        bytes = std::max(bytes, ns_workspace(g, ns_layout(g), 2));
     }
     uint8_t *ws = nullptr;
     s = op_workspace(ctx, bytes, &ws);

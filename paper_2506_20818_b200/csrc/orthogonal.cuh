@@ -1848,6 +1848,15 @@ static void ns_tiles(NsGroup &g, int bm, int bn, bool half, int &tiles_a, int &t
     }
 }
 
+// all matrices go to the one-block kernel: faster wherever it applies (figures at the kernel), and it needs no workspace
+static bool ns_small(const NsGroup &g)
+{
+    for (int d = 0; d < g.count; ++d)
+        if (g.mat[d].n > NSB_SIZE) return false;
+    return g.count > 0;
+}
+static size_t ns_workspace(const NsGroup &g, const NsLayout &l, int parts) { return ns_small(g) ? 0 : l.bytes(parts); }
+
 struct NsTarget {
     void *dst;
     int bf16_dst;
@@ -1900,9 +1909,7 @@ static bool ns_run(TcState &tc, Exec &ex, const NsSource &src, NsGroup &g, const
     double *partial = (double *)((uint8_t *)B + NsLayout::up((size_t)2 * PARTS * na));
     float *inv_r = (float *)((uint8_t *)partial + NsLayout::up(sizeof(double) * (size_t)l.norm_blocks));
     const int adam_blocks = (int)ceil_div64(adam.spans.first[adam.spans.count], NS_ADAM_ELEMS);
-    bool small = g.count > 0;  // faster wherever it applies (figures at the kernel)
-    for (int d = 0; d < g.count; ++d) small = small && g.mat[d].n <= NSB_SIZE;
-    if (small) {
+    if (ns_small(g)) {
         NsBlock p{};
         p.steps = steps; p.matrices = l.matrices;
         p.poly = poly; p.eps = eps;

@@ -284,6 +284,24 @@ def test_workspace_of_an_update_follows_its_matrices(ctx):
     ctx.stats()
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_small_matrices_need_no_workspace(ctx, dtype):
+    """They stay on chip, so 70,000 of them (more than one launch takes) take no device memory beside themselves."""
+    U = torch.randn(70_000, 20, 33, generator=gen(3)).to(dtype).to(DEV)
+    base = ctx.stats().workspace_bytes
+    before = ctx.stats().kernel_launches
+    got = ctx.orthogonalize(U)
+    assert ctx.stats().kernel_launches - before == 2 and ctx.stats().workspace_bytes == base
+    want = iterate(U)
+    err = (got.double() - want).norm(dim=(-2, -1)) / want.norm(dim=(-2, -1))
+    assert (err <= ORTH_TOL[dtype]).all()
+    for i in (0, 65_535, 65_536, 69_999):
+        assert torch.equal(ctx.orthogonalize(U[i]), got[i])
+    p, m, g = (torch.randn(128 * 64 * 3, generator=gen(k)).to(DEV) for k in range(3))
+    ctx.muon_step(p, m, None, g, t=1, matrices=[(i * 128 * 64, 128, 64) for i in range(3)])
+    assert ctx.stats().workspace_bytes == base
+
+
 def test_workspace_that_cannot_be_had_fails_that_call_alone(pkg, ctx):
     """LP_ENOMEM, nothing written, and the next call is as before."""
     U = torch.randn(100, 140, generator=gen(6)).to(DEV)
