@@ -479,3 +479,33 @@ def test_small_rows_keep_their_own_digits(ctx, rows, cols):
     assert gpu_rel(got, want) <= ORTH_TOL[F32]
     assert gpu_rel(got[::2], want[::2]) <= ORTH_TOL[F32]
     ctx.stats()
+
+
+# ------------------------------------------------------------------------------------------ runs of the gradient that end at edges
+@pytest.mark.parametrize("width", [33, 64, 200])     # 8, 16, 32 lanes per row: other shares of a block
+@pytest.mark.parametrize("dout_t,grad_t", [(F32, F32), (BF16, F32), (BF16, BF16)])
+@pytest.mark.parametrize("shift", [0, 1, -1])
+def test_embed_grad_runs_that_end_at_edges(ctx, width, dout_t, grad_t, shift):
+    """Runs of equal ids that end at (or one beside) the edges of what a group of lanes (32 ids), a span (256), a block and a block of
+    joins (8,192) adds up, runs over many spans, rows named and not named on both sides of multiples of 32; into dense rows and rows
+    apart.  The bound is that of the gradient: (k + 2) 2^-24 of the sum of magnitudes, and 2^-8 for a BF16 result."""
+    runs = [32, 32, 192, 256, 256, 224, 1, 31, 512 - 32, 7, 249, 2048, 8192, 1, 1, 30, 224, 255, 1, 16 * 256, 17 * 256, 40 * 256, 5, 8192 - 5, 64, 3]
+    runs = [max(1, r + shift * (i % 3 == 0)) for i, r in enumerate(runs)]
+    named = [31, 32, 33, 63, 64, 95, 127, 128, 129, 130, 160, 191, 192, 193, 224, 255, 256, 287, 288, 319, 320, 351, 352, 383, 384, 415]
+    rows = 417
+    ids = torch.repeat_interleave(torch.tensor(named, dtype=torch.int32), torch.tensor(runs))
+    ids = ids[torch.randperm(len(ids), generator=gen(shift + 5))].to(DEV)
+    n = len(ids)
+    dout = torch.randn(n, width, generator=gen(width)).to(dout_t).to(DEV)
+    ref, mag = (torch.zeros(rows, width, dtype=F64, device=DEV).index_add_(0, ids.long(), 1.3 * x.double()) for x in (dout, dout.abs()))
+    count = torch.bincount(ids, minlength=rows)[:, None]
+    bound = (count + 2) * 2.0**-24 * mag + (ref.abs() * 2.0**-8 if grad_t == BF16 else 0.0)
+    grad = torch.full((rows, width), float("nan"), dtype=grad_t, device=DEV)
+    ctx.embed_grad(dout, ids, rows, scale=1.3, grad=grad)
+    assert ((grad.double() - ref).abs() <= bound).all()
+    assert (grad[count[:, 0] == 0] == 0).all()
+    apart = torch.full((rows, width + 3), 4.0, dtype=grad_t, device=DEV)
+    ctx.embed_grad(dout, ids, rows, scale=1.3, grad=apart[:, 1:width + 1])
+    assert torch.equal(apart[:, 1:width + 1], grad)
+    assert (apart[:, 0] == 4.0).all() and (apart[:, width + 1:] == 4.0).all()
+    ctx.stats()
