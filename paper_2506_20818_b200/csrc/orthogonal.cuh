@@ -925,7 +925,7 @@ __global__ void __launch_bounds__(NSC_THREADS, 1) ns_chain_kernel(const __grid_c
                             tmem_ld_32x16(taddr, v);
                         } else {
 #pragma unroll
-                            for (int o = 0; o < 16; o += 8) {  // eight columns at a time: nothing may spill (every barrier empties L1)
+                            for (int o = 0; o < 16; o += 8) {  // eight columns at a time: spills are dear, since every barrier empties L1 (one register does, C = 1 and 2)
                                 float r[8], r2[8];
                                 tmem_ld_32x8_pair(taddr + o, taddr + NSC_BN + o, r, r2);
                                 if (c == 0) {
@@ -1329,8 +1329,8 @@ __global__ void __launch_bounds__(NSB_THREADS, 1) ns_block_kernel(const __grid_c
 // A pair multiplies tiles of 256 x 256 (PARTS = 2: 256 x 128): each CTA brings in 128 rows of the first operand and half of the
 // second, so a 64-term block costs 32 KiB per CTA for 512 cycles of products (48 KiB for 768).  PARTS = 1: two accumulators of
 // 256 columns fill tensor memory, and a tile's is drained while the next tile's products run.  PARTS = 2: the accumulators
-// (four of 128 columns) change hands after every 64-term block and sixteen warps add the blocks up in registers (32 columns per thread; 64, for tiles of
-// 256 x 256, spill).
+// (four of 128 columns) change hands after every 64-term block and sixteen warps add the blocks up in registers (32
+// columns per thread, which spills 16 registers; 64, for tiles of 256 x 256, spilled far more).
 // A and B are symmetric: only tiles on and above the diagonal are computed, the others are written turned.
 //   warp 0 operands, warp 1 matrix instructions (of the pair's first CTA), warps 2-17 results: 32 rows x 64 (32) columns each, turned
 //   through 2 KiB of shared memory per warp, 16 columns at a time, so that rows are written in pieces of 64 bytes
