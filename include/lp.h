@@ -379,7 +379,8 @@ lp_status lp_op_linear(lp_ctx *ctx, int32_t prec, int64_t M, int32_t N, int32_t 
 lp_status lp_op_weight_grad(lp_ctx *ctx, int32_t prec, int64_t M, int32_t N, int32_t K, const void *A, const void *dZ,
                             float *dW);
 
-/* The operators of this and the next section may be captured into a CUDA graph and replayed.  One that needs more workspace than
+/* The operators of this and the next section may be captured into a CUDA graph and replayed, by a context whose stream can be
+ * captured (not the legacy default stream).  One that needs more workspace than
  * earlier calls left is refused during a capture (LP_ESTATE): make it once before.  Workspace that a capture saw is kept until
  * lp_destroy, so later, larger calls do not take it away from a graph; the graph must not be replayed after lp_destroy, nor at the
  * same time as another call on the context. */
@@ -420,7 +421,7 @@ lp_status lp_embed_grad(lp_ctx *ctx, int32_t dout_prec, const void *dout, int64_
  *   prec     : LP_FP32 or LP_BF16, of U and out.  The products run on the tensor cores with FP32 accumulators: LP_BF16
  *              holds X, A and b A + c A^2 as FP16 numbers (11 bits), LP_FP32 as pairs of them (22 bits).  FP16 has less range than FP32:
  *              the error is about 1e-6 of the whole matrix, but rows or columns smaller than the others by more than about 1e-5
- *              keep fewer bits of themselves (FP32 rows of 1e-6 of the others: up to 4e-5 off, relative to themselves)
+ *              keep fewer bits of themselves (FP32 rows of 1e-6 of the others: up to 9e-5 off, relative to themselves)
  *   U, out   : DEVICE, row pitch ld_*, matrices stride_* elements apart; out may be U itself.  Matrices of out may lie behind one
  *              another or between one another's rows (stride_out < ld_out); stride_u may also be 0
  *   coeffs   : HOST double[3] = {a, b, c}, or NULL for {3.4445, -4.7750, 2.0315}.  LP_EINVAL when singular values of

@@ -28,6 +28,8 @@ struct TcState {
     bf16 *wbuf = nullptr;     // device scratch: BF16 copy of one layer's weights
     int *host_err = nullptr;  // pinned
     unsigned long long wait_limit_ns = 2000000000ull;  // every mbarrier wait gives up after this long (default two seconds)
+    void *reset = nullptr;    // device memory that is cleared with the error word: blocks that gave up may have left it as it was
+    size_t reset_bytes = 0;
     int overdeclare_tx = 0;   // diagnostics: the next launch expects this many bytes more than it copies (consumed by that launch)
 };
 
@@ -1047,6 +1049,7 @@ static lp_status tc_check_result(TcState &tc, Exec &ex, std::string &err)
                  *tc.host_err);
         err = buf;
         cudaMemsetAsync(tc.err_word, 0, sizeof(int), ex.st);
+        if (tc.reset) cudaMemsetAsync(tc.reset, 0, tc.reset_bytes, ex.st);
         return LP_ETIMEOUT;
     }
     return LP_OK;

@@ -314,6 +314,8 @@ extern "C" lp_status lp_create(lp_ctx **out, int32_t device, void *cuda_stream)
         cudaGetLastError();
         return fail(nullptr, LP_ECUDA, "lp_create: " + tc_err);
     }
+    ctx->tc.reset = ctx->ns.counters;
+    ctx->tc.reset_bytes = NSC_BARRIERS * sizeof(unsigned);
     *out = ctx;
     return LP_OK;
 }

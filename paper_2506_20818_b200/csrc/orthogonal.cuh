@@ -7,9 +7,9 @@
 // significant bits where BF16 carries eight, at the same rate, and the range it lacks is not needed here: the values
 // are bounded by the polynomial (the host refuses coefficients for which they are not), so X is held as 2^14 X, A as 2^13 A and B as
 // 2^8 B to 2^13 B, as far as its coefficients' bound allows (2^12 B for the default): the largest values lie just below the end of FP16.
-// What a matrix holds far below its largest values ends at FP16's 2^-24: FP32 rows of 1e-5 of the others keep 4e-7 to 4e-6 of
-// themselves, rows of 1e-6 2e-6 to 4e-5 (64 x 64 to 800 x 900; with 2^12 X and 2^8 A, B it was 6e-6 to 1e-4 and 6e-5 to 1e-3), where
-// FP32 products keep 5e-7 at any size.  Of the whole matrix these errors are 1e-9.
+// What a matrix holds far below its largest values ends at FP16's 2^-24: FP32 rows of 1e-5 of the others are 3e-7 to 9e-6 off, relative
+// to themselves, rows of 1e-6 2e-6 to 9e-5 (64 x 64 to 2048 x 2048; with 2^12 X and 2^8 A, B thirty times that), where FP32 products
+// are 3e-7 to 2.5e-6 off for rows of any size.  Of the whole matrix these errors are 1e-9.
 // X is kept twice: in FP32, from which the term a X of every step is taken, and as FP16 operands.
 //   BF16 results : X, A and B are one FP16 number per value in the products
 //   FP32 results : pairs of FP16 numbers hi + lo (22 bits), products hi*lo + lo*hi + hi*hi; the accumulator of the matrix
@@ -925,7 +925,7 @@ __global__ void __launch_bounds__(NSC_THREADS, 1) ns_chain_kernel(const __grid_c
                             tmem_ld_32x16(taddr, v);
                         } else {
 #pragma unroll
-                            for (int o = 0; o < 16; o += 8) {  // eight columns at a time: spills are dear, since every barrier empties L1 (one register does, C = 1 and 2)
+                            for (int o = 0; o < 16; o += 8) {  // eight columns at a time: spills are dear, every barrier empties L1 (C = 1, 2: one register)
                                 float r[8], r2[8];
                                 tmem_ld_32x8_pair(taddr + o, taddr + NSC_BN + o, r, r2);
                                 if (c == 0) {
