@@ -379,7 +379,7 @@ lp_status lp_op_linear(lp_ctx *ctx, int32_t prec, int64_t M, int32_t N, int32_t 
 lp_status lp_op_weight_grad(lp_ctx *ctx, int32_t prec, int64_t M, int32_t N, int32_t K, const void *A, const void *dZ,
                             float *dW);
 
-/* The operators of this and the next section may be captured into a CUDA graph and replayed, by a context whose stream can be
+/* The operators of this and the following sections may be captured into a CUDA graph and replayed, by a context whose stream can be
  * captured (not the legacy default stream).  One that needs more workspace than
  * earlier calls left is refused during a capture (LP_ESTATE): make it once before.  Workspace that a capture saw is kept until
  * lp_destroy, so later, larger calls do not take it away from a graph; the graph must not be replayed after lp_destroy, nor at the
@@ -456,6 +456,67 @@ typedef struct {
  * Does not synchronise (except to grow the workspace). */
 lp_status lp_muon_step(lp_ctx *ctx, const lp_muon_desc *desc, const lp_matrix *matrices, int32_t n_matrices, int64_t n_params, const float *params,
                        const float *momentum, const float *adam_v, const float *grads, int64_t t, float *new_params, float *new_momentum, float *new_adam_v);
+
+/* ---- residual blocks ---------------------------------------------------------------------------- */
+
+/* (No counterpart in the paper, whose encoders have two or three layers and train without dropout.)
+ * Dropout with a mask that is never stored: out = in * 65536 / (65536 - t) where u >= t, else 0, with t = round(65536 p) and u,
+ * sixteen bits, a pure function of (seed, step, row_base + row, column): half (column % 2 = 0: the low one) of word
+ * (column % 8) / 2 of the Philox4x32-10 block with counter (row, row >> 32, lo32(step), 5 | (column / 8) << 8) and key = seed.
+ * The gradient is the same call on the gradient.  Results do not depend on how rows are split over calls (row_base), on pitches
+ * or on types.  Dropped elements are zero whatever they held, NaN included.
+ *   prec      : LP_FP32 or LP_BF16, of in and out
+ *   in, out   : DEVICE [rows, width], row pitch ld_*; out may be in itself.  width <= 2^20
+ *   p         : in [0, 1]
+ * Does not synchronise. */
+lp_status lp_dropout(lp_ctx *ctx, int32_t prec, int64_t rows, int32_t width, const void *in, int64_t ld_in, double p, uint64_t seed, uint64_t step, int64_t row_base,
+                     void *out, int64_t ld_out);
+
+enum { LP_NORM_NONE = 0, LP_NORM_RMS = 1, LP_NORM_LAYER = 2 };
+
+typedef struct {
+    int64_t rows;
+    int32_t width;               /* 1 .. 8192                                                               */
+    int32_t stream_prec;         /* of x, y, dy, dx; LP_BF16 only when prec is                              */
+    int32_t prec;                /* of h, n, a gate per element, and their gradients                        */
+    int32_t pre_norm, post_norm; /* LP_NORM_*                                                               */
+    double eps;                  /* > 0                                                                     */
+    double scale;                /* of the block's contribution                                             */
+    double p;                    /* dropout, as in lp_dropout                                               */
+    uint64_t seed, step;
+    int64_t row_base;
+    const float *pre, *pre_bias;   /* DEVICE [width], weight and bias of the norm before the next block; NULL = ones, zeros */
+    const float *post, *post_bias; /* ... of the norm after the block                                       */
+    const void *gate;            /* DEVICE; NULL = none; ld_gate = 0: float32 [width], else [rows, width] of `prec` */
+    int64_t ld_gate;
+} lp_residual_desc;
+
+/* The end of one residual block and the norm before the next, in one pass:
+ *     y = x + scale * gate * dropout(post(h)),     n = pre(y)
+ * RMS norm: v * weight / sqrt(mean(v^2) + eps) (+ bias); layer norm: the same of v - mean(v).  All arithmetic in FP32; y and n are
+ * rounded once (n is taken from the unrounded y).
+ *   x[rows, width] : DEVICE, row pitch ld_x
+ *   h[rows, width] : DEVICE; NULL: no block has run yet, y = x is not written and only n is
+ *   y[rows, width] : DEVICE, may be x itself; NULL = not wanted
+ *   n[rows, width] : DEVICE, may be h itself; NULL exactly when pre_norm is LP_NORM_NONE
+ * Any pitch and alignment to the element is accepted; rows that start on multiples of 16 bytes are the fast ones.
+ * Does not synchronise. */
+lp_status lp_residual_norm(lp_ctx *ctx, const lp_residual_desc *desc, const void *x, int64_t ld_x, const void *h, int64_t ld_h, void *y, int64_t ld_y, void *n,
+                           int64_t ld_n);
+
+/* Gradient of lp_residual_norm.  Nothing is kept from the forward pass but its h and y (x where h was NULL).
+ *   dy[rows, width] : DEVICE, gradient that reaches y past the next block; NULL = zero
+ *   dn[rows, width] : DEVICE, gradient of n; NULL exactly when pre_norm is LP_NORM_NONE
+ *   dx              : DEVICE, may be dy itself; NULL = not wanted, as for every result
+ *   dh              : DEVICE, may be dn or h itself
+ *   dgate           : DEVICE; float32 [width] for a gate per column (ld_dgate is not looked at), else [rows, width] of `prec`
+ *   dpre, dpre_bias, dpost, dpost_bias : DEVICE float32 [width]
+ *   accumulate != 0 : the results of [width] are added to
+ * Column sums are added in FP32 in a fixed order: the same bits in every run.  Takes workspace from the context (growing
+ * synchronises).  Does not synchronise otherwise. */
+lp_status lp_residual_norm_grad(lp_ctx *ctx, const lp_residual_desc *desc, const void *dy, int64_t ld_dy, const void *dn, int64_t ld_dn, const void *y, int64_t ld_y,
+                                const void *h, int64_t ld_h, void *dx, int64_t ld_dx, void *dh, int64_t ld_dh, void *dgate, int64_t ld_dgate, float *dpre,
+                                float *dpre_bias, float *dpost, float *dpost_bias, int32_t accumulate);
 
 /* ---- allocation-free variant ---------------------------------------------------------------- */
 

@@ -31,6 +31,7 @@ EXPORTS = [
     "lp_worker_view", "lp_get_worker_view", "lp_hits_at_k", "lp_get_predictor_activations",
     "lp_invalidate_embeddings", "lp_set_wait_limit",
     "lp_embed", "lp_embed_grad", "lp_orthogonalize", "lp_muon_step",
+    "lp_dropout", "lp_residual_norm", "lp_residual_norm_grad",
 ]
 
 PROF_CATEGORIES = ["agg_fwd", "agg_bwd", "gemm_fwd", "gemm_dgrad", "gemm_wgrad", "score", "incidence", "scatter",
@@ -74,7 +75,16 @@ class MuonDesc(C.Structure):
                 ("adam_beta2", C.c_double), ("adam_eps", C.c_double), ("nesterov", C.c_int32), ("steps", C.c_int32)]
 
 
+class ResidualDesc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("width", C.c_int32), ("stream_prec", C.c_int32), ("prec", C.c_int32), ("pre_norm", C.c_int32),
+                ("post_norm", C.c_int32), ("eps", C.c_double), ("scale", C.c_double), ("p", C.c_double), ("seed", C.c_uint64), ("step", C.c_uint64),
+                ("row_base", C.c_int64), ("pre", C.c_void_p), ("pre_bias", C.c_void_p), ("post", C.c_void_p), ("post_bias", C.c_void_p),
+                ("gate", C.c_void_p), ("ld_gate", C.c_int64)]
+
+
 LP_NO_PADDING = -(1 << 31)
+LP_NORM_NONE, LP_NORM_RMS, LP_NORM_LAYER = 0, 1, 2
+_NORMS = {None: LP_NORM_NONE, "rms": LP_NORM_RMS, "layer": LP_NORM_LAYER}
 
 # argument types of the calls whose latency counts: ctypes converts plain Python numbers by them
 _ARGTYPES = {
@@ -86,6 +96,9 @@ _ARGTYPES = {
                          C.c_void_p, C.c_int64, C.c_int64],
     "lp_muon_step": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p,
                      C.c_void_p, C.c_void_p],
+    "lp_dropout": [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_void_p, C.c_int64, C.c_double, C.c_uint64, C.c_uint64, C.c_int64, C.c_void_p, C.c_int64],
+    "lp_residual_norm": [C.c_void_p, C.c_void_p] + [C.c_void_p, C.c_int64] * 4,
+    "lp_residual_norm_grad": [C.c_void_p, C.c_void_p] + [C.c_void_p, C.c_int64] * 7 + [C.c_void_p] * 4 + [C.c_int32],
 }
 
 _lib = None
@@ -436,6 +449,134 @@ class Context:
         self._ck(self.lib.lp_muon_step(self.h, C.byref(d), mats, 0 if matrices is None else len(matrices), n, p[0], p[1], p[2], p[3], t, p[4], p[5], p[6]))
         self._leave(cur)
         return new
+
+    # ---- residual blocks
+    def _words(self, seed, step, row_base, who: str):
+        if not (0 <= seed < 1 << 64 and 0 <= step < 1 << 64 and 0 <= row_base < 1 << 62):
+            self._refuse(f"{who}: seed and step are 64-bit numbers, row_base a number of rows")
+
+    def dropout(self, x, p: float, seed: int, step: int, row_base: int = 0, out=None):
+        """Dropout of a matrix (float32 or bfloat16); the gradient is the same call on the gradient.  See lp_dropout."""
+        rows, width, ld = self._rows(x, "dropout")
+        prec = self._prec(x.dtype, "dropout")
+        self._words(seed, step, row_base, "dropout")
+        if out is None:
+            out, ldo = x.new_empty((rows, width)), width
+        else:
+            r, d, ldo = self._rows(out, "dropout: out")
+            if r != rows or d != width or out.dtype != x.dtype:
+                self._refuse(f"dropout: out must be [{rows}, {width}] of the type of x")
+        cur = self._enter(x, out)
+        rc = self.lib.lp_dropout(self.h, prec, rows, width, x.data_ptr(), ld, p, seed, step, row_base, out.data_ptr(), ldo)
+        if rc:
+            self._ck(rc)
+        if cur is not None:
+            self._leave(cur)
+        return out
+
+    def _column(self, v, width: int, who: str, name: str):
+        if v is None:
+            return None
+        if v.dtype is not self._torch.float32 or v.get_device() != self.device or v.numel() != width or not v.is_contiguous():
+            self._refuse(f"{who}: {name} must be a contiguous float32 vector of {width} elements on cuda:{self.device}")
+        return v.data_ptr()
+
+    def _matrix(self, v, rows: int, width: int, dtype, who: str, name: str):
+        """(address, row pitch) of a matrix that must have this shape and type."""
+        if v is None:
+            return None, width
+        r, d, ld = self._rows(v, who)
+        if r != rows or d != width or v.dtype != dtype:
+            self._refuse(f"{who}: {name} must be [{rows}, {width}] of {dtype}")
+        return v.data_ptr(), ld
+
+    def _residual(self, who, like, prec_dtype, pre_norm, pre, pre_bias, post_norm, post, post_bias, gate, scale, p, seed, step, row_base, eps):
+        if pre_norm not in _NORMS or post_norm not in _NORMS:
+            self._refuse(f"{who}: norms are 'rms', 'layer' or None")
+        rows, width, _ = self._rows(like, who)
+        self._words(seed, step, row_base, who)
+        g = ldg = None
+        if gate is not None:
+            if gate.dim() == 1:
+                g, ldg = self._column(gate, width, who, "gate"), 0
+            else:
+                g, ldg = self._matrix(gate, rows, width, prec_dtype, who, "gate")
+        return rows, width, ResidualDesc(rows, width, self._prec(like.dtype, who), self._prec(prec_dtype, who), _NORMS[pre_norm], _NORMS[post_norm], eps, scale, p, seed, step,
+                                         row_base, self._column(pre, width, who, "pre"), self._column(pre_bias, width, who, "pre_bias"),
+                                         self._column(post, width, who, "post"), self._column(post_bias, width, who, "post_bias"), g, ldg or 0)
+
+    def residual_norm(self, x, h=None, pre_norm: Optional[str] = "rms", pre=None, pre_bias=None, post_norm: Optional[str] = None, post=None, post_bias=None,
+                      gate=None, scale: float = 1.0, p: float = 0.0, seed: int = 0, step: int = 0, row_base: int = 0, eps: float = 1e-6, y=None, n=None, dtype=None):
+        """y = x + scale * gate * dropout(post(h)) and n = pre(y); returns (y, n).  Without h only the norm is taken and y is x;
+        without pre_norm n is None.  dtype: type of n where there is no h to say it.  See lp_residual_norm."""
+        if h is not None:
+            dtype = h.dtype
+        elif dtype is None:
+            dtype = n.dtype if n is not None else x.dtype
+        rows, width, d = self._residual("residual_norm", x, dtype, pre_norm, pre, pre_bias, post_norm, post, post_bias, gate, scale, p, seed, step, row_base, eps)
+        if h is None:
+            if y is not None and y is not x:
+                self._refuse("residual_norm: without h there is no y to write")
+            y = x
+        elif y is None:
+            y = x.new_empty((rows, width))
+        if pre_norm is None:
+            if n is not None:
+                self._refuse("residual_norm: without pre_norm there is no n to write")
+        elif n is None:
+            n = x.new_empty((rows, width), dtype=dtype)
+        a = self._matrix(x, rows, width, x.dtype, "residual_norm", "x") + self._matrix(h, rows, width, dtype, "residual_norm", "h") \
+            + self._matrix(y, rows, width, x.dtype, "residual_norm", "y") + self._matrix(n, rows, width, dtype, "residual_norm", "n")
+        cur = self._enter(x, h, y, n, pre, pre_bias, post, post_bias, gate)
+        rc = self.lib.lp_residual_norm(self.h, C.addressof(d), *a)
+        if rc:
+            self._ck(rc)
+        if cur is not None:
+            self._leave(cur)
+        return y, n
+
+    def residual_norm_grad(self, dy, dn, y, h=None, pre_norm: Optional[str] = "rms", pre=None, pre_bias=None, post_norm: Optional[str] = None, post=None,
+                           post_bias=None, gate=None, scale: float = 1.0, p: float = 0.0, seed: int = 0, step: int = 0, row_base: int = 0, eps: float = 1e-6,
+                           accumulate: bool = False, dx=None, dh=None, dgate=None, dpre=None, dpre_bias=None, dpost=None, dpost_bias=None):
+        """Gradients of residual_norm: dx, dh, dgate and those of the norms' parameters that were given, as a dict.  dy or dn may
+        be None (zero); results may be given (accumulate adds to the vectors among them).  See lp_residual_norm_grad."""
+        who = "residual_norm_grad"
+        like = y if y is not None else dy
+        if like is None:
+            self._refuse(f"{who}: neither y nor dy")
+        dtype = h.dtype if h is not None else dn.dtype if dn is not None else like.dtype
+        rows, width, d = self._residual(who, like, dtype, pre_norm, pre, pre_bias, post_norm, post, post_bias, gate, scale, p, seed, step, row_base, eps)
+        new = self._torch.float32
+        out = {"dx": dx if dx is not None else like.new_empty((rows, width))}
+        if h is not None:
+            out["dh"] = dh if dh is not None else like.new_empty((rows, width), dtype=dtype)
+        wanted = {"dpre": (pre, dpre), "dpre_bias": (pre_bias, dpre_bias), "dpost": (post, dpost), "dpost_bias": (post_bias, dpost_bias)}
+        if gate is not None and h is not None:
+            if gate.dim() == 1:
+                wanted["dgate"] = (gate, dgate)
+            else:
+                out["dgate"] = dgate if dgate is not None else like.new_empty((rows, width), dtype=dtype)
+        for name, (param, given) in wanted.items():
+            if given is not None:
+                out[name] = given
+            elif param is not None:
+                if accumulate:
+                    self._refuse(f"{who}: accumulate needs a {name} to add to")
+                out[name] = like.new_empty(width, dtype=new)
+        a = self._matrix(dy, rows, width, like.dtype, who, "dy") + self._matrix(dn, rows, width, dtype, who, "dn") + self._matrix(y, rows, width, like.dtype, who, "y") \
+            + self._matrix(h, rows, width, dtype, who, "h") + self._matrix(out["dx"], rows, width, like.dtype, who, "dx") + self._matrix(out.get("dh"), rows, width, dtype, who, "dh")
+        if "dgate" in wanted:
+            a += (self._column(out["dgate"], width, who, "dgate"), width)
+        else:
+            a += self._matrix(out.get("dgate"), rows, width, dtype, who, "dgate")
+        a += tuple(self._column(out.get(name), width, who, name) for name in ("dpre", "dpre_bias", "dpost", "dpost_bias"))
+        cur = self._enter(dy, dn, y, h, pre, pre_bias, post, post_bias, gate, *out.values())
+        rc = self.lib.lp_residual_norm_grad(self.h, C.addressof(d), *a, accumulate)
+        if rc:
+            self._ck(rc)
+        if cur is not None:
+            self._leave(cur)
+        return out
 
     # ---- inspection
     def stats(self) -> Stats:

@@ -1,0 +1,511 @@
+// Dropout from a counter-based generator, and the norms around a residual block fused with its dropout, gate and sum.
+//
+//   dropout         out = in * f where u >= t, else 0;  t = round(65536 p), f = 65536 / (65536 - t)
+//   residual norm   y = x + s gate * dropout(post(h)),  n = pre(y)
+//
+// The mask is never stored: u, sixteen bits per element, is a pure function of (seed, step, row, column), so the backward pass
+// draws it again.  Eight neighbouring columns share one Philox4x32-10 block with counter (row, row >> 32, step,
+// 5 | column / 8 << 8): with 32 bits per element the generator alone (about 85 instructions per block) would take as long as
+// HBM takes for BF16 rows.  f is computed from t, so the expectation is exact although p is rounded to sixteen bits.
+//
+// Norms of a row v of D columns, weight w, bias b (parameters FP32):
+//   RMS   : r = 1 / sqrt(mean(v^2) + eps),            out = w v r
+//   layer : c = v - mean(v), r = 1 / sqrt(mean(c^2) + eps), out = w c r + b
+// Backward, for a gradient q of out, u = w q, z = v r (c r):
+//   dv = r (u - z mean(u z) [- mean(u)]),  dw = sum over rows of q z,  db = sum of q
+// No statistics are kept from the forward pass: a row's sums come out of the same registers that its gradient needs anyway.
+//
+// A team of T threads (a power of two, eight columns each) holds a row in registers, so every array is read once and written
+// once: bound by HBM.  Teams of up to 32 threads are parts of warps, larger ones whole blocks.
+#pragma once
+#include "common.cuh"
+#include "sampler.cuh"
+
+enum : uint32_t { DRAW_DROPOUT = 5 };
+
+struct DropArgs {
+    uint2 key;
+    uint32_t step_lo;
+    uint32_t threshold;  // 0 = nothing is dropped, 65536 = everything
+    float factor;
+    int64_t row_base;
+};
+
+// bit i: element i of the eight of this row and group of columns stays
+LP_DEVINL uint32_t drop_keep8(const DropArgs &d, int64_t row, uint32_t group)
+{
+    const uint64_t r = (uint64_t)(d.row_base + row);
+    const uint4 x = philox4x32_10(make_uint4((uint32_t)r, (uint32_t)(r >> 32), d.step_lo, DRAW_DROPOUT | group << 8), d.key);
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    uint32_t keep = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        keep |= ((w[i] & 0xffffu) >= d.threshold ? 1u : 0u) << (2 * i);
+        keep |= ((w[i] >> 16) >= d.threshold ? 1u : 0u) << (2 * i + 1);
+    }
+    return keep;
+}
+
+// The eight columns of a thread.  VEC (rows start on 16 bytes): neighbouring ones.  Otherwise `step` = min(T, 32) columns apart, so
+// that a warp reads and writes runs of neighbouring elements.
+template <bool VEC> struct Cols {
+    int base, step, width;
+    // t: thread of the team
+    LP_DEVINL Cols(int t, int T, int width_) : width(width_)
+    {
+        if (VEC) { base = 8 * t; step = 1; }
+        else { step = min(T, 32); base = (t / 32) * 256 + (t & (step - 1)); }
+    }
+    LP_DEVINL int at(int j) const { return base + j * step; }
+    LP_DEVINL bool has(int j) const { return at(j) < width; }
+    LP_DEVINL bool full() const { return VEC && base + 8 <= width; }
+    // keep bits in the order of the thread's columns
+    LP_DEVINL uint32_t keep(const DropArgs &d, int64_t row, int lane) const
+    {
+        if (VEC) return drop_keep8(d, row, (uint32_t)(base >> 3));
+        // the thread draws the bits of the eight neighbouring columns that it would own under VEC and hands them round its team
+        const int lane_t = lane & (step - 1), first = base - lane_t;
+        const uint32_t mine = drop_keep8(d, row, (uint32_t)(first / 8 + lane_t));
+        uint32_t keep = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int c = lane_t + j * step;
+            keep |= ((__shfl_sync(0xffffffffu, mine, c >> 3, step) >> (c & 7)) & 1u) << j;
+        }
+        return keep;
+    }
+};
+
+template <typename T, bool VEC> LP_DEVINL void load8(const T *row, const Cols<VEC> &c, float *v)
+{
+    if (c.full()) {
+        constexpr int VN = Vec16<T>::N;
+#pragma unroll
+        for (int k = 0; k < 8 / VN; ++k) {
+            Vec16<T> x;
+            x.load_once(row + c.base + k * VN);
+            x.to_float(v + k * VN);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = c.has(j) ? to_f<T>(row[c.at(j)]) : 0.f;
+    }
+}
+template <typename T, bool VEC> LP_DEVINL void store8(T *row, const Cols<VEC> &c, const float *v)
+{
+    if (c.full()) {
+        constexpr int VN = Vec16<T>::N;
+#pragma unroll
+        for (int k = 0; k < 8 / VN; ++k) {
+            Vec16<T> x;
+            x.from_float(v + k * VN);
+            x.store(row + c.base + k * VN);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (c.has(j)) row[c.at(j)] = from_f<T>(v[j]);
+    }
+}
+// per-column parameter, `other` where there is none
+template <bool VEC> LP_DEVINL void load_param8(const float *p, const Cols<VEC> &c, float other, float *v)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = p && c.has(j) ? __ldg(p + c.at(j)) : other;
+}
+
+// ---------------------------------------------------------------------------------------------
+// dropout
+// ---------------------------------------------------------------------------------------------
+constexpr int DROP_THREADS = 256;
+
+struct DropoutParams {
+    const void *in;
+    void *out;
+    int64_t rows, ld_in, ld_out;
+    int width;
+    int team;            // threads per row (a power of two, at most 256); wider rows are taken in pieces of 8 team columns
+    DropArgs drop;
+};
+
+template <typename T, bool VEC> __global__ void __launch_bounds__(DROP_THREADS) dropout_kernel(const DropoutParams p)
+{
+    LP_DEP_ENTER();
+    const int t = threadIdx.x & (p.team - 1), lane = threadIdx.x & 31;
+    const int64_t stride = (int64_t)gridDim.x * (DROP_THREADS / p.team);
+    const int64_t rounds = (p.rows + stride - 1) / stride;
+    int64_t row = (int64_t)blockIdx.x * (DROP_THREADS / p.team) + threadIdx.x / p.team;
+    for (int64_t i = 0; i < rounds; ++i, row += stride) {
+        for (int c0 = 0; c0 < p.width; c0 += 8 * p.team) {
+            Cols<VEC> c(t, p.team, p.width);
+            c.base += c0;
+            // the whole warp takes part in handing the bits round, rows that are not there too
+            const uint32_t keep = c.keep(p.drop, row, lane);
+            if (row < p.rows) {
+                float v[8];
+                load8<T, VEC>((const T *)p.in + row * p.ld_in, c, v);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = (keep >> j) & 1u ? v[j] * p.drop.factor : 0.f;
+                store8<T, VEC>((T *)p.out + row * p.ld_out, c, v);
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// residual norm
+// ---------------------------------------------------------------------------------------------
+constexpr int RN_MAX_WIDTH = 8192;  // eight columns for each of 1024 threads
+constexpr int RN_SUMS = 5;          // column sums of the backward pass: dpre, dpost, dgate, dpre_bias, dpost_bias
+
+struct ResidualParams {
+    int64_t rows;
+    int width, team;
+    int pre_norm, post_norm;   // lp_norm
+    float eps, inv_width, scale;
+    DropArgs drop;
+    const float *pre, *pre_bias, *post, *post_bias, *gate_vec;
+    const void *gate;          // [rows, width], or null
+    int64_t ld_gate;
+    // forward: x, h in, y, n out (null: not wanted); backward: dy, dn, y, h in, dx, dh, dgate out
+    const void *x, *h, *dy, *dn;
+    void *y, *n, *dx, *dh, *dgate;
+    int64_t ld_x, ld_h, ld_y, ld_n, ld_dy, ld_dn, ld_dx, ld_dh, ld_dgate;
+    float *partial;            // [gridDim.x][RN_SUMS][width] column sums of each block
+};
+
+// Sums of K values over a team, in every one of its threads.  A fixed tree, so the same bits in every run.
+template <int K, bool BLOCK> LP_DEVINL void team_sum(float (&v)[K], int T, float *scratch, int &turn)
+{
+    if (!BLOCK) {
+        for (int o = T >> 1; o > 0; o >>= 1)
+#pragma unroll
+            for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+        return;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+        for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = T >> 5;
+    float *s = scratch + (turn & 1) * 32 * 4;  // two areas in turn: one barrier per sum
+    ++turn;
+    if (lane == 0)
+#pragma unroll
+        for (int k = 0; k < K; ++k) s[k * 32 + warp] = v[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < K; ++k) v[k] = lane < warps ? s[k * 32 + lane] : 0.f;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+        for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+}
+
+// v becomes z (the normalised row); returns r
+template <bool VEC, bool BLOCK> LP_DEVINL float normalise(float *v, int kind, float eps, float inv_width, const Cols<VEC> &c, int T, float *scratch, int &turn)
+{
+    if (kind == LP_NORM_LAYER) {
+        float s[1] = {0.f};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[0] += v[j];
+        team_sum<1, BLOCK>(s, T, scratch, turn);
+        const float mean = s[0] * inv_width;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = c.has(j) ? v[j] - mean : 0.f;
+    }
+    float q[1] = {0.f};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) q[0] = fmaf(v[j], v[j], q[0]);
+    team_sum<1, BLOCK>(q, T, scratch, turn);
+    const float r = 1.f / sqrtf(fmaf(q[0], inv_width, eps));
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] *= r;
+    return r;
+}
+
+// MAXT: the largest team of the variant, 32 (parts of warps) or 1024 (whole blocks)
+template <typename TS, typename TD, bool VEC, int MAXT> __global__ void __launch_bounds__(MAXT < 256 ? 256 : MAXT) residual_norm_kernel(const __grid_constant__ ResidualParams p)
+{
+    LP_DEP_ENTER();
+    constexpr bool BLOCK = MAXT > 32;
+    __shared__ float scratch[2 * 32 * 4];
+    int turn = 0;
+    const int T = p.team, t = threadIdx.x & (T - 1), lane = threadIdx.x & 31, teams = BLOCK ? 1 : blockDim.x / T;
+    const Cols<VEC> c(t, T, p.width);
+    float pre[8], pre_bias[8], post[8], post_bias[8], gate_vec[8];
+    load_param8(p.pre, c, 1.f, pre);
+    load_param8(p.pre_bias, c, 0.f, pre_bias);
+    load_param8(p.post, c, 1.f, post);
+    load_param8(p.post_bias, c, 0.f, post_bias);
+    load_param8(p.gate_vec, c, 1.f, gate_vec);
+    const int64_t stride = (int64_t)gridDim.x * teams, rounds = (p.rows + stride - 1) / stride;
+    int64_t row = (int64_t)blockIdx.x * teams + (BLOCK ? 0 : threadIdx.x / T);
+    for (int64_t i = 0; i < rounds; ++i, row += stride) {
+        const bool live = row < p.rows;  // of a warp's teams some may be past the last row; they take part in the sums of the others
+        float y[8], b[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = b[j] = 0.f;
+        if (live) load8<TS, VEC>((const TS *)p.x + row * p.ld_x, c, y);
+        if (p.h) {
+            if (live) load8<TD, VEC>((const TD *)p.h + row * p.ld_h, c, b);
+            if (p.post_norm) {
+                normalise<VEC, BLOCK>(b, p.post_norm, p.eps, p.inv_width, c, T, scratch, turn);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) b[j] = fmaf(b[j], post[j], post_bias[j]);
+            }
+            if (p.drop.threshold) {
+                const uint32_t keep = c.keep(p.drop, row, lane);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) b[j] = (keep >> j) & 1u ? b[j] * p.drop.factor : 0.f;
+            }
+            if (p.gate) {
+                float g[8] = {};
+                if (live) load8<TD, VEC>((const TD *)p.gate + row * p.ld_gate, c, g);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) b[j] *= g[j];
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = fmaf(p.scale * gate_vec[j], b[j], y[j]);
+            if (live && p.y) store8<TS, VEC>((TS *)p.y + row * p.ld_y, c, y);
+        }
+        if (p.pre_norm) {
+            normalise<VEC, BLOCK>(y, p.pre_norm, p.eps, p.inv_width, c, T, scratch, turn);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = fmaf(y[j], pre[j], pre_bias[j]);
+            if (live) store8<TD, VEC>((TD *)p.n + row * p.ld_n, c, y);
+        }
+    }
+}
+
+// v: the row, becomes z.  q: gradient of the norm's output, becomes that of its input.  dw, db: column sums.
+template <bool VEC, bool BLOCK, bool BIAS>
+LP_DEVINL void norm_backward(float *v, float *q, const float *w, int kind, float eps, float inv_width, const Cols<VEC> &c, int T, float *scratch, int &turn, float *dw, float *db)
+{
+    const bool layer = kind == LP_NORM_LAYER;
+    if (layer) {
+        float s[1] = {0.f};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[0] += v[j];
+        team_sum<1, BLOCK>(s, T, scratch, turn);
+        const float mean = s[0] * inv_width;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = c.has(j) ? v[j] - mean : 0.f;
+    }
+    float s[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float u = w[j] * q[j];
+        s[0] = fmaf(v[j], v[j], s[0]);
+        s[1] = fmaf(u, v[j], s[1]);
+        s[2] += u;
+    }
+    team_sum<3, BLOCK>(s, T, scratch, turn);
+    const float r = 1.f / sqrtf(fmaf(s[0], inv_width, eps));
+    const float along = s[1] * inv_width * r, mean_u = layer ? s[2] * inv_width : 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        v[j] *= r;
+        dw[j] = fmaf(q[j], v[j], dw[j]);
+        if (BIAS) db[j] += q[j];
+        q[j] = r * (fmaf(-v[j], along, w[j] * q[j]) - mean_u);
+    }
+}
+
+// BIAS: column sums of the biases too (sixteen more registers).  MAXT as above, and 256: blocks of 1024 threads leave 64 registers
+// for each, which the column sums do not fit into.
+template <typename TS, typename TD, bool VEC, int MAXT, bool BIAS>
+__global__ void __launch_bounds__(MAXT < 256 ? 256 : MAXT) residual_norm_grad_kernel(const __grid_constant__ ResidualParams p)
+{
+    LP_DEP_ENTER();
+    constexpr bool BLOCK = MAXT > 32;
+    __shared__ float scratch[2 * 32 * 4];
+    __shared__ float sums[BLOCK ? 1 : 8 * 256];
+    int turn = 0;
+    const int T = p.team, t = threadIdx.x & (T - 1), lane = threadIdx.x & 31, teams = BLOCK ? 1 : blockDim.x / T;
+    const Cols<VEC> c(t, T, p.width);
+    float pre[8], post[8], post_bias[8], gate_vec[8];
+    load_param8(p.pre, c, 1.f, pre);
+    load_param8(p.post, c, 1.f, post);
+    load_param8(p.post_bias, c, 0.f, post_bias);
+    load_param8(p.gate_vec, c, 1.f, gate_vec);
+    float acc[RN_SUMS][8];
+#pragma unroll
+    for (int k = 0; k < RN_SUMS; ++k)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[k][j] = 0.f;
+    const int64_t stride = (int64_t)gridDim.x * teams, rounds = (p.rows + stride - 1) / stride;
+    int64_t row = (int64_t)blockIdx.x * teams + (BLOCK ? 0 : threadIdx.x / T);
+    for (int64_t i = 0; i < rounds; ++i, row += stride) {
+        const bool live = row < p.rows;
+        float g[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) g[j] = 0.f;
+        if (p.pre_norm) {
+            float y[8] = {};
+            if (live) {
+                load8<TD, VEC>((const TD *)p.dn + row * p.ld_dn, c, g);
+                load8<TS, VEC>((const TS *)p.y + row * p.ld_y, c, y);
+            }
+            norm_backward<VEC, BLOCK, BIAS>(y, g, pre, p.pre_norm, p.eps, p.inv_width, c, T, scratch, turn, acc[0], acc[3]);
+        }
+        if (p.dy && live) {
+            float d[8];
+            load8<TS, VEC>((const TS *)p.dy + row * p.ld_dy, c, d);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) g[j] += d[j];
+        }
+        if (p.dx && live) store8<TS, VEC>((TS *)p.dx + row * p.ld_dx, c, g);
+        if (!p.h) continue;
+        // the branch: g -> gradient of h
+        float h[8] = {}, m[8] = {}, z[8];
+        if (live) load8<TD, VEC>((const TD *)p.h + row * p.ld_h, c, h);
+        if (p.gate && live) load8<TD, VEC>((const TD *)p.gate + row * p.ld_gate, c, m);
+        const uint32_t keep = p.drop.threshold ? c.keep(p.drop, row, lane) : 0xffu;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            g[j] = (keep >> j) & 1u ? p.scale * p.drop.factor * g[j] : 0.f;   // times gate: gradient of post(h)
+            z[j] = h[j];
+        }
+        float q[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) q[j] = g[j] * gate_vec[j] * (p.gate ? m[j] : 1.f);
+        if (p.post_norm) norm_backward<VEC, BLOCK, BIAS>(z, q, post, p.post_norm, p.eps, p.inv_width, c, T, scratch, turn, acc[1], acc[4]);
+        if (p.dh && live) store8<TD, VEC>((TD *)p.dh + row * p.ld_dh, c, q);
+        if (p.dgate && live) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) m[j] = (keep >> j) & 1u ? g[j] * fmaf(z[j], post[j], post_bias[j]) : 0.f;
+            store8<TD, VEC>((TD *)p.dgate + row * p.ld_dgate, c, m);
+        }
+        if (p.gate_vec)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[2][j] += (keep >> j) & 1u ? g[j] * fmaf(z[j], post[j], post_bias[j]) : 0.f;
+    }
+    // column sums of the block: its teams' added in order
+#pragma unroll
+    for (int k = 0; k < (BIAS ? 5 : 3); ++k) {
+        float *dst = p.partial + ((size_t)blockIdx.x * RN_SUMS + k) * p.width;
+        if (BLOCK) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (c.has(j)) dst[c.at(j)] = acc[k][j];
+        } else {
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sums[(threadIdx.x / T) * 8 * T + c.at(j)] = acc[k][j];
+            __syncthreads();
+            for (int col = threadIdx.x; col < p.width; col += blockDim.x) {
+                float s = 0.f;
+                for (int q = 0; q < teams; ++q) s += sums[q * 8 * T + col];
+                dst[col] = s;
+            }
+        }
+    }
+}
+
+// out[k][col] (+)= sum over the blocks, in a fixed order: 32 columns per block, 32 threads share the blocks of a column
+struct ResidualSums {
+    float *out[RN_SUMS];
+};
+__global__ void __launch_bounds__(1024) residual_sums_kernel(const float *partial, int blocks, int width, const ResidualSums o, int accumulate)
+{
+    LP_DEP_ENTER();
+    __shared__ float s[32][33];
+    float *out = o.out[blockIdx.y];
+    if (!out) return;
+    const int col = blockIdx.x * 32 + threadIdx.x;
+    float v = 0.f;
+    if (col < width)
+        for (int b = threadIdx.y; b < blocks; b += 32) v += partial[((size_t)b * RN_SUMS + blockIdx.y) * width + col];
+    s[threadIdx.y][threadIdx.x] = v;
+    __syncthreads();
+    v = s[threadIdx.x][threadIdx.y];  // a warp holds the 32 shares of one column
+#pragma unroll
+    for (int i = 16; i > 0; i >>= 1) v += __shfl_xor_sync(0xffffffffu, v, i);
+    const int c = blockIdx.x * 32 + threadIdx.y;
+    if (threadIdx.x == 0 && c < width) out[c] = accumulate ? out[c] + v : v;
+}
+
+// ---------------------------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------------------------
+static int pow2_at_least(int64_t n)
+{
+    int t = 1;
+    while (t < n) t <<= 1;
+    return t;
+}
+template <typename T> static bool on_16_bytes(const void *p, int64_t ld) { return !p || (((uintptr_t)p & 15) == 0 && ld * (int64_t)sizeof(T) % 16 == 0); }
+
+template <typename T> static void dropout_launch(Exec &ex, DropoutParams &p)
+{
+    p.team = std::min(DROP_THREADS, pow2_at_least(ceil_div64(p.width, 8)));
+    const int64_t blocks = std::min<int64_t>(ceil_div64(p.rows, DROP_THREADS / p.team), (int64_t)tc_sm_count() * 8);
+    const bool vec = on_16_bytes<T>(p.in, p.ld_in) && on_16_bytes<T>(p.out, p.ld_out);
+    if (vec) launch_dep(dropout_kernel<T, true>, dim3((unsigned)blocks), dim3(DROP_THREADS), 0, ex.st, p);
+    else launch_dep(dropout_kernel<T, false>, dim3((unsigned)blocks), dim3(DROP_THREADS), 0, ex.st, p);
+    ex.launches += 1;
+}
+
+struct ResidualGrid {
+    int team, threads, blocks;
+    bool block;
+};
+static ResidualGrid residual_grid(int64_t rows, int width, int threads_per_sm)
+{
+    ResidualGrid g;
+    g.team = pow2_at_least(ceil_div64(width, 8));
+    g.block = g.team > 32;
+    g.threads = g.block ? g.team : 256;
+    const int64_t per_sm = std::max(1, threads_per_sm / g.threads);
+    g.blocks = (int)std::min<int64_t>(ceil_div64(rows, g.threads / g.team), (int64_t)tc_sm_count() * per_sm);
+    return g;
+}
+
+template <typename TS, typename TD> static bool residual_vec(const ResidualParams &p)
+{
+    return on_16_bytes<TS>(p.x, p.ld_x) && on_16_bytes<TD>(p.h, p.ld_h) && on_16_bytes<TS>(p.y, p.ld_y) && on_16_bytes<TD>(p.n, p.ld_n) &&
+           on_16_bytes<TS>(p.dy, p.ld_dy) && on_16_bytes<TD>(p.dn, p.ld_dn) && on_16_bytes<TS>(p.dx, p.ld_dx) && on_16_bytes<TD>(p.dh, p.ld_dh) &&
+           on_16_bytes<TD>(p.gate, p.ld_gate) && on_16_bytes<TD>(p.dgate, p.ld_dgate);
+}
+
+template <typename TS, typename TD> static void residual_launch(Exec &ex, ResidualParams &p)
+{
+    const ResidualGrid g = residual_grid(p.rows, p.width, 1024);
+    p.team = g.team;
+    const dim3 grid(g.blocks), block(g.threads);
+    if (residual_vec<TS, TD>(p)) {
+        if (g.block) launch_dep(residual_norm_kernel<TS, TD, true, 1024>, grid, block, 0, ex.st, p);
+        else launch_dep(residual_norm_kernel<TS, TD, true, 32>, grid, block, 0, ex.st, p);
+    } else {
+        if (g.block) launch_dep(residual_norm_kernel<TS, TD, false, 1024>, grid, block, 0, ex.st, p);
+        else launch_dep(residual_norm_kernel<TS, TD, false, 32>, grid, block, 0, ex.st, p);
+    }
+    ex.launches += 1;
+}
+
+template <typename TS, typename TD, bool VEC, bool BIAS> static void residual_grad_dispatch(Exec &ex, const ResidualParams &p, const ResidualGrid &g)
+{
+    if (g.threads > 256) launch_dep(residual_norm_grad_kernel<TS, TD, VEC, 1024, BIAS>, dim3(g.blocks), dim3(g.threads), 0, ex.st, p);
+    else if (g.block) launch_dep(residual_norm_grad_kernel<TS, TD, VEC, 256, BIAS>, dim3(g.blocks), dim3(g.threads), 0, ex.st, p);
+    else launch_dep(residual_norm_grad_kernel<TS, TD, VEC, 32, BIAS>, dim3(g.blocks), dim3(g.threads), 0, ex.st, p);
+}
+template <typename TS, typename TD> static void residual_grad_launch(Exec &ex, ResidualParams &p, const ResidualGrid &g, const ResidualSums &o, int accumulate)
+{
+    p.team = g.team;
+    const bool bias = o.out[3] || o.out[4];
+    if (residual_vec<TS, TD>(p)) {
+        if (bias) residual_grad_dispatch<TS, TD, true, true>(ex, p, g);
+        else residual_grad_dispatch<TS, TD, true, false>(ex, p, g);
+    } else {
+        if (bias) residual_grad_dispatch<TS, TD, false, true>(ex, p, g);
+        else residual_grad_dispatch<TS, TD, false, false>(ex, p, g);
+    }
+    ex.launches += 1;
+    int last = -1;
+    for (int k = 0; k < RN_SUMS; ++k)
+        if (o.out[k]) last = k;
+    if (last < 0) return;
+    launch_dep(residual_sums_kernel, dim3((unsigned)ceil_div64(p.width, 32), (unsigned)(last + 1)), dim3(32, 32), 0, ex.st, p.partial, g.blocks, p.width, o, accumulate);
+    ex.launches += 1;
+}

@@ -19,6 +19,7 @@
 #include "probe.cuh"
 #include "embed.cuh"
 #include "orthogonal.cuh"
+#include "block.cuh"
 
 // ----------------------------------------------------------------------------------------------
 // context
@@ -2465,6 +2466,159 @@ extern "C" lp_status lp_muon_step(lp_ctx *ctx, const lp_muon_desc *d, const lp_m
         if (!ns_run<2>(ctx->tc, ctx->ex, src, g, l, ad, ctx->ns, d->steps, poly, d->eps, to, ws, err)) return fail(ctx, LP_ECUDA, "lp_muon_step: " + err);
         i0 = i1;
     } while (i0 < mats.size());
+    CK_LAUNCH();
+    return LP_OK;
+}
+
+// ----------------------------------------------------------------------------------------------
+// residual blocks
+// ----------------------------------------------------------------------------------------------
+static bool drop_args(double p, uint64_t seed, uint64_t step, int64_t row_base, DropArgs &d)
+{
+    if (!(p >= 0.0 && p <= 1.0) || row_base < 0) return false;
+    d.key = make_uint2((uint32_t)seed, (uint32_t)(seed >> 32));
+    d.step_lo = (uint32_t)step;
+    d.threshold = (uint32_t)std::llround(65536.0 * p);
+    d.factor = d.threshold < 65536u ? (float)(65536.0 / (65536.0 - d.threshold)) : 0.f;
+    d.row_base = row_base;
+    return true;
+}
+
+static bool prec_ok(int32_t prec) { return prec == LP_FP32 || prec == LP_BF16; }
+
+extern "C" lp_status lp_dropout(lp_ctx *ctx, int32_t prec, int64_t rows, int32_t width, const void *in, int64_t ld_in, double p, uint64_t seed, uint64_t step,
+                                int64_t row_base, void *out, int64_t ld_out)
+{
+    if (!ctx) return LP_EINVAL;
+    if (!prec_ok(prec)) return fail(ctx, LP_EINVAL, "lp_dropout: unknown precision");
+    if (rows < 0) return fail(ctx, LP_EINVAL, "lp_dropout: negative number of rows");
+    if (width < 1 || width > (1 << 20)) return fail(ctx, LP_EINVAL, "lp_dropout: width must be in [1, 2^20]");
+    if (ld_in < width || ld_out < width) return fail(ctx, LP_EINVAL, "lp_dropout: a row pitch is smaller than the width");
+    DropoutParams k{};
+    if (!drop_args(p, seed, step, row_base, k.drop)) return fail(ctx, LP_EINVAL, "lp_dropout: p must be in [0, 1] and row_base not negative");
+    if (rows == 0) return LP_OK;
+    if (!in || !out) return fail(ctx, LP_EINVAL, "lp_dropout: null array");
+    if (misaligned(in, prec) || misaligned(out, prec)) return fail(ctx, LP_EINVAL, "lp_dropout: an array is not aligned to its elements");
+    CK(cudaSetDevice(ctx->device));
+    k.in = in; k.out = out; k.rows = rows; k.width = width; k.ld_in = ld_in; k.ld_out = ld_out;
+    if (prec == LP_FP32) dropout_launch<float>(ctx->ex, k);
+    else dropout_launch<bf16>(ctx->ex, k);
+    CK_LAUNCH();
+    return LP_OK;
+}
+
+// what the forward and the backward call have in common; `branch`: there is an h
+static lp_status residual_params(lp_ctx *ctx, const std::string &who, const lp_residual_desc *d, bool branch, ResidualParams &k)
+{
+    if (!d) return fail(ctx, LP_EINVAL, who + ": null descriptor");
+    if (!prec_ok(d->prec) || !prec_ok(d->stream_prec)) return fail(ctx, LP_EINVAL, who + ": unknown precision");
+    if (d->stream_prec == LP_BF16 && d->prec == LP_FP32) return fail(ctx, LP_EUNSUPPORTED, who + ": a BF16 residual sum takes BF16 blocks");
+    if (d->rows < 0) return fail(ctx, LP_EINVAL, who + ": negative number of rows");
+    if (d->width < 1 || d->width > RN_MAX_WIDTH) return fail(ctx, LP_EINVAL, who + ": width must be in [1, 8192]");
+    for (int32_t kind : {d->pre_norm, d->post_norm})
+        if (kind != LP_NORM_NONE && kind != LP_NORM_RMS && kind != LP_NORM_LAYER) return fail(ctx, LP_EINVAL, who + ": unknown norm");
+    if (!(d->eps > 0.0) || !std::isfinite(d->eps) || !((float)d->eps > 0.f)) return fail(ctx, LP_EINVAL, who + ": eps must be positive and finite");
+    if (!std::isfinite(d->scale)) return fail(ctx, LP_EINVAL, who + ": scale is not finite");
+    if (!drop_args(d->p, d->seed, d->step, d->row_base, k.drop)) return fail(ctx, LP_EINVAL, who + ": p must be in [0, 1] and row_base not negative");
+    if (d->gate && d->ld_gate != 0 && d->ld_gate < d->width) return fail(ctx, LP_EINVAL, who + ": a row pitch is smaller than the width");
+    if (!branch && d->pre_norm == LP_NORM_NONE) return fail(ctx, LP_EINVAL, who + ": neither a block nor a norm");
+    for (const float *v : {d->pre, d->pre_bias, d->post, d->post_bias})
+        if (misaligned(v, LP_FP32)) return fail(ctx, LP_EINVAL, who + ": an array is not aligned to its elements");
+    if (d->gate && misaligned(d->gate, d->ld_gate == 0 ? LP_FP32 : d->prec)) return fail(ctx, LP_EINVAL, who + ": an array is not aligned to its elements");
+    k.rows = d->rows;
+    k.width = d->width;
+    k.pre_norm = d->pre_norm;
+    k.post_norm = branch ? d->post_norm : LP_NORM_NONE;
+    k.eps = (float)d->eps;
+    k.inv_width = 1.f / (float)d->width;
+    k.scale = (float)d->scale;
+    if (k.pre_norm) { k.pre = d->pre; k.pre_bias = d->pre_bias; }
+    if (k.post_norm) { k.post = d->post; k.post_bias = d->post_bias; }
+    if (d->gate && branch) {
+        if (d->ld_gate == 0) k.gate_vec = (const float *)d->gate;
+        else { k.gate = d->gate; k.ld_gate = d->ld_gate; }
+    }
+    return LP_OK;
+}
+
+struct ResidualArray {
+    const void *p;
+    int64_t ld;
+    int32_t prec;
+};
+static lp_status residual_arrays(lp_ctx *ctx, const std::string &who, int width, std::initializer_list<ResidualArray> arrays)
+{
+    for (const ResidualArray &a : arrays) {
+        if (!a.p) continue;
+        if (a.ld < width) return fail(ctx, LP_EINVAL, who + ": a row pitch is smaller than the width");
+        if (misaligned(a.p, a.prec)) return fail(ctx, LP_EINVAL, who + ": an array is not aligned to its elements");
+    }
+    return LP_OK;
+}
+
+extern "C" lp_status lp_residual_norm(lp_ctx *ctx, const lp_residual_desc *desc, const void *x, int64_t ld_x, const void *h, int64_t ld_h, void *y, int64_t ld_y, void *n,
+                                      int64_t ld_n)
+{
+    if (!ctx) return LP_EINVAL;
+    ResidualParams k{};
+    lp_status s = residual_params(ctx, "lp_residual_norm", desc, h != nullptr, k);
+    if (s != LP_OK) return s;
+    const int32_t ps = desc->stream_prec, pd = desc->prec;
+    s = residual_arrays(ctx, "lp_residual_norm", desc->width, {{x, ld_x, ps}, {h, ld_h, pd}, {y, ld_y, ps}, {n, ld_n, pd}});
+    if (s != LP_OK) return s;
+    if (desc->rows == 0) return LP_OK;
+    if (!x || (n == nullptr) != (k.pre_norm == LP_NORM_NONE)) return fail(ctx, LP_EINVAL, "lp_residual_norm: x is missing, or n and pre_norm do not go together");
+    if (!y && !n) return fail(ctx, LP_EINVAL, "lp_residual_norm: no result is wanted");
+    CK(cudaSetDevice(ctx->device));
+    k.x = x; k.ld_x = ld_x; k.h = h; k.ld_h = ld_h; k.y = h ? y : nullptr; k.ld_y = ld_y; k.n = n; k.ld_n = ld_n;
+    if (ps == LP_BF16) residual_launch<bf16, bf16>(ctx->ex, k);
+    else if (pd == LP_BF16) residual_launch<float, bf16>(ctx->ex, k);
+    else residual_launch<float, float>(ctx->ex, k);
+    CK_LAUNCH();
+    return LP_OK;
+}
+
+extern "C" lp_status lp_residual_norm_grad(lp_ctx *ctx, const lp_residual_desc *desc, const void *dy, int64_t ld_dy, const void *dn, int64_t ld_dn, const void *y,
+                                           int64_t ld_y, const void *h, int64_t ld_h, void *dx, int64_t ld_dx, void *dh, int64_t ld_dh, void *dgate, int64_t ld_dgate,
+                                           float *dpre, float *dpre_bias, float *dpost, float *dpost_bias, int32_t accumulate)
+{
+    if (!ctx) return LP_EINVAL;
+    const std::string who = "lp_residual_norm_grad";
+    ResidualParams k{};
+    // without rows there may be no arrays: the results of [width] are those that the descriptor allows
+    const bool branch = h != nullptr || (desc && desc->rows == 0 && (dh || dgate || dpost || dpost_bias));
+    lp_status s = residual_params(ctx, who, desc, branch, k);
+    if (s != LP_OK) return s;
+    const int32_t ps = desc->stream_prec, pd = desc->prec;
+    const bool gate_sum = k.gate_vec != nullptr;
+    if (dgate && !k.gate && !gate_sum) return fail(ctx, LP_EINVAL, who + ": a gradient of the gate is wanted and there is no gate");
+    if ((dpre || dpre_bias) && !k.pre_norm) return fail(ctx, LP_EINVAL, who + ": gradients of a norm are wanted and there is none");
+    if ((dpost || dpost_bias) && !k.post_norm) return fail(ctx, LP_EINVAL, who + ": gradients of a norm are wanted and there is none");
+    if (dh && !branch) return fail(ctx, LP_EINVAL, who + ": a gradient of h is wanted and there is no h");
+    s = residual_arrays(ctx, who, desc->width, {{dy, ld_dy, ps}, {dn, ld_dn, pd}, {y, ld_y, ps}, {h, ld_h, pd}, {dx, ld_dx, ps}, {dh, ld_dh, pd},
+                                                {gate_sum ? nullptr : dgate, ld_dgate, pd}});
+    if (s != LP_OK) return s;
+    for (const void *v : {(const void *)dpre, (const void *)dpre_bias, (const void *)dpost, (const void *)dpost_bias, gate_sum ? (const void *)dgate : nullptr})
+        if (misaligned(v, LP_FP32)) return fail(ctx, LP_EINVAL, who + ": an array is not aligned to its elements");
+    ResidualSums o{{dpre, dpost, gate_sum ? (float *)dgate : nullptr, dpre_bias, dpost_bias}};
+    CK(cudaSetDevice(ctx->device));
+    if (desc->rows == 0) {
+        for (float *v : o.out)
+            if (v && !accumulate) CK(cudaMemsetAsync(v, 0, sizeof(float) * (size_t)desc->width, ctx->ex.st));
+        return LP_OK;
+    }
+    if (k.pre_norm ? !dn || !y : dn != nullptr) return fail(ctx, LP_EINVAL, who + ": dn and y are needed with a norm before the next block, and dn only then");
+    if (!dy && !dn) return fail(ctx, LP_EINVAL, who + ": neither dy nor dn");
+    const ResidualGrid g = residual_grid(desc->rows, desc->width, 512);
+    uint8_t *ws = nullptr;
+    s = op_workspace(ctx, sizeof(float) * (size_t)g.blocks * RN_SUMS * desc->width, &ws);
+    if (s != LP_OK) return s;
+    k.dy = dy; k.ld_dy = ld_dy; k.dn = dn; k.ld_dn = ld_dn; k.y = (void *)y; k.ld_y = ld_y; k.h = h; k.ld_h = ld_h;
+    k.dx = dx; k.ld_dx = ld_dx; k.dh = dh; k.ld_dh = ld_dh; k.partial = (float *)ws;
+    if (!gate_sum) { k.dgate = dgate; k.ld_dgate = ld_dgate; }
+    if (ps == LP_BF16) residual_grad_launch<bf16, bf16>(ctx->ex, k, g, o, accumulate);
+    else if (pd == LP_BF16) residual_grad_launch<float, bf16>(ctx->ex, k, g, o, accumulate);
+    else residual_grad_launch<float, float>(ctx->ex, k, g, o, accumulate);
     CK_LAUNCH();
     return LP_OK;
 }
