@@ -518,6 +518,33 @@ lp_status lp_residual_norm_grad(lp_ctx *ctx, const lp_residual_desc *desc, const
                                 const void *h, int64_t ld_h, void *dx, int64_t ld_dx, void *dh, int64_t ld_dh, void *dgate, int64_t ld_dgate, float *dpre,
                                 float *dpre_bias, float *dpost, float *dpost_bias, int32_t accumulate);
 
+/* ---- products by group ---------------------------------------------------------------------------- */
+
+/* (No counterpart in the paper, whose nodes are of one type.)
+ * Dense transform with one weight matrix per group of neighbouring rows (nodes sorted by type, by partition, by expert):
+ *     C[r] = act(A[r] B[g] + bias[g])    for offsets[g] <= r < offsets[g + 1]
+ * B[g] is [K, N] row-major (trans_b = 0) or [N, K] (trans_b = 1: with A = dZ and the forward B, the input gradient).
+ *   prec       : LP_FP32 or LP_BF16, of A, B and C; sums are FP32, C is rounded once.  The products run on the tensor cores: LP_FP32
+ *                operands as three BF16 numbers each (24 bits; an infinity gives NaN)
+ *   offsets    : DEVICE int32 [groups + 1], not decreasing, in [0, M].  Others are clamped to the nearest that are, and the next
+ *                lp_get_stats returns LP_EINVAL once.  Rows before offsets[0] and from offsets[groups] on are neither read into any
+ *                result nor written
+ *   A[M, K]    : DEVICE, row pitch ld_a;  C[M, N]: DEVICE, row pitch ld_c, does not overlap the inputs
+ *   B          : DEVICE [groups, K, N] or [groups, N, K], matrices behind one another
+ *   bias       : DEVICE float32 [groups, N] or NULL
+ * Any width, pitch and alignment to the element is accepted; BF16 rows of A and B that start on multiples of 16 bytes are the fast
+ * ones.  Does not synchronise. */
+lp_status lp_grouped_linear(lp_ctx *ctx, int32_t prec, int64_t M, int32_t N, int32_t K, int64_t groups, const int32_t *offsets, const void *A, int64_t ld_a,
+                            const void *B, int32_t trans_b, const float *bias, int32_t relu, void *C, int64_t ld_c);
+
+/* Weight gradients of lp_grouped_linear: dW[g] = A_g^T dZ_g and dbias[g] = column sums of dZ_g over the rows of group g, zeros for a
+ * group without rows.  FP32 sums in a fixed order: the same bits in every run.
+ *   A[M, K], dZ[M, N] : DEVICE, row pitches ld_*, of `prec`
+ *   dW[groups, K, N], dbias[groups, N] : DEVICE float32; dbias may be NULL.  accumulate != 0 adds to both
+ * Takes workspace from the context (at most 40 MB; growing synchronises).  Does not synchronise otherwise. */
+lp_status lp_grouped_weight_grad(lp_ctx *ctx, int32_t prec, int64_t M, int32_t N, int32_t K, int64_t groups, const int32_t *offsets, const void *A, int64_t ld_a,
+                                 const void *dZ, int64_t ld_dz, int32_t accumulate, float *dW, float *dbias);
+
 /* ---- allocation-free variant ---------------------------------------------------------------- */
 
 /* (No counterpart in the paper: this entry point exists for the callers described below.)

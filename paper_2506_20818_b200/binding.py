@@ -31,7 +31,7 @@ EXPORTS = [
     "lp_worker_view", "lp_get_worker_view", "lp_hits_at_k", "lp_get_predictor_activations",
     "lp_invalidate_embeddings", "lp_set_wait_limit",
     "lp_embed", "lp_embed_grad", "lp_orthogonalize", "lp_muon_step",
-    "lp_dropout", "lp_residual_norm", "lp_residual_norm_grad",
+    "lp_dropout", "lp_residual_norm", "lp_residual_norm_grad", "lp_grouped_linear", "lp_grouped_weight_grad",
 ]
 
 PROF_CATEGORIES = ["agg_fwd", "agg_bwd", "gemm_fwd", "gemm_dgrad", "gemm_wgrad", "score", "incidence", "scatter",
@@ -98,6 +98,10 @@ _ARGTYPES = {
                      C.c_void_p, C.c_void_p],
     "lp_dropout": [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_void_p, C.c_int64, C.c_double, C.c_uint64, C.c_uint64, C.c_int64, C.c_void_p, C.c_int64],
     "lp_residual_norm": [C.c_void_p, C.c_void_p] + [C.c_void_p, C.c_int64] * 4,
+    "lp_grouped_linear": [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_void_p,
+                          C.c_int32, C.c_void_p, C.c_int64],
+    "lp_grouped_weight_grad": [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int32,
+                               C.c_void_p, C.c_void_p],
     "lp_residual_norm_grad": [C.c_void_p, C.c_void_p] + [C.c_void_p, C.c_int64] * 7 + [C.c_void_p] * 4 + [C.c_int32],
 }
 
@@ -577,6 +581,70 @@ class Context:
         if cur is not None:
             self._leave(cur)
         return out
+
+    # ---- products by group
+    def _offsets(self, offsets, who: str) -> int:
+        self._ids(offsets, who)
+        if offsets.dim() != 1 or offsets.numel() < 1:
+            self._refuse(f"{who}: offsets must be a vector of one more element than there are groups")
+        return offsets.numel() - 1
+
+    def grouped_linear(self, A, offsets, B, bias=None, relu: bool = False, trans_b: bool = False, out=None):
+        """act(A[r] B[g] + bias[g]) for the rows offsets[g] <= r < offsets[g + 1]; B [groups, K, N], or [groups, N, K] with trans_b.
+        Rows outside the groups are left as they are in `out`.  See lp_grouped_linear."""
+        who = "grouped_linear"
+        M, K, lda = self._rows(A, who)
+        groups = self._offsets(offsets, who)
+        if B.dim() != 3 or B.get_device() != self.device or B.dtype != A.dtype or not B.is_contiguous() or B.shape[0] != groups or B.shape[2 if trans_b else 1] != K:
+            self._refuse(f"{who}: B must be {f'[{groups}, N, {K}]' if trans_b else f'[{groups}, {K}, N]'}, contiguous, of the type of A and on its device")
+        N = B.shape[1 if trans_b else 2]
+        if bias is not None and (bias.dtype is not self._torch.float32 or bias.get_device() != self.device or bias.shape != (groups, N) or not bias.is_contiguous()):
+            self._refuse(f"{who}: bias must be a contiguous float32 matrix [{groups}, {N}] on cuda:{self.device}")
+        prec = self._prec(A.dtype, who)
+        if out is None:
+            out, ldc = A.new_empty((M, N)), N
+        else:
+            r, d, ldc = self._rows(out, who)
+            if r != M or d != N or out.dtype != A.dtype:
+                self._refuse(f"{who}: out must be [{M}, {N}] of the type of A")
+        cur = self._enter(A, offsets, B, bias, out)
+        rc = self.lib.lp_grouped_linear(self.h, prec, M, N, K, groups, offsets.data_ptr(), A.data_ptr(), lda, B.data_ptr(), trans_b,
+                                        None if bias is None else bias.data_ptr(), relu, out.data_ptr(), ldc)
+        if rc:
+            self._ck(rc)
+        if cur is not None:
+            self._leave(cur)
+        return out
+
+    def grouped_weight_grad(self, A, dZ, offsets, bias: bool = False, accumulate: bool = False, dW=None, dbias=None):
+        """Weight gradients of grouped_linear: dW[g] = A_g^T dZ_g, [groups, K, N] float32, and with bias=True (or a given dbias)
+        (dW, column sums of dZ_g).  See lp_grouped_weight_grad."""
+        who = "grouped_weight_grad"
+        M, K, lda = self._rows(A, who)
+        m, N, ldz = self._rows(dZ, who)
+        groups = self._offsets(offsets, who)
+        if m != M or dZ.dtype != A.dtype:
+            self._refuse(f"{who}: dZ must have {M} rows of the type of A")
+        f32 = self._torch.float32
+        bias = bias or dbias is not None
+        if accumulate and (dW is None or (bias and dbias is None)):
+            self._refuse(f"{who}: accumulate needs gradients to add to")
+        for x, shape in ((dW, (groups, K, N)), (dbias, (groups, N))):
+            if x is not None and (x.dtype is not f32 or x.get_device() != self.device or x.shape != shape or not x.is_contiguous()):
+                self._refuse(f"{who}: gradients must be contiguous float32 tensors {(groups, K, N)} and {(groups, N)} on cuda:{self.device}")
+        prec = self._prec(A.dtype, who)
+        if dW is None:
+            dW = A.new_empty((groups, K, N), dtype=f32)
+        if bias and dbias is None:
+            dbias = A.new_empty((groups, N), dtype=f32)
+        cur = self._enter(A, dZ, offsets, dW, dbias)
+        rc = self.lib.lp_grouped_weight_grad(self.h, prec, M, N, K, groups, offsets.data_ptr(), A.data_ptr(), lda, dZ.data_ptr(), ldz, accumulate, dW.data_ptr(),
+                                             None if dbias is None else dbias.data_ptr())
+        if rc:
+            self._ck(rc)
+        if cur is not None:
+            self._leave(cur)
+        return (dW, dbias) if bias else dW
 
     # ---- inspection
     def stats(self) -> Stats:

@@ -20,6 +20,7 @@
 #include "embed.cuh"
 #include "orthogonal.cuh"
 #include "block.cuh"
+#include "grouped.cuh"
 
 // ----------------------------------------------------------------------------------------------
 // context
@@ -310,7 +311,7 @@ extern "C" lp_status lp_create(lp_ctx **out, int32_t device, void *cuda_stream)
     ctx->embed_err = ctx->err_flag + 1;
     cudaMemset(ctx->exhausted_dev, 0, 256);
     std::string tc_err;
-    if (!tc_init(ctx->tc, tc_err) || !ns_init(ctx->ns, tc_err)) {
+    if (!tc_init(ctx->tc, tc_err) || !ns_init(ctx->ns, tc_err) || !grouped_init(tc_err)) {
         lp_destroy(ctx);
         cudaGetLastError();
         return fail(nullptr, LP_ECUDA, "lp_create: " + tc_err);
@@ -1925,6 +1926,7 @@ extern "C" lp_status lp_get_stats(lp_ctx *ctx, lp_stats *out)
     if (words[1]) {
         cudaMemsetAsync(ctx->embed_err, 0, sizeof(int), ctx->ex.st);
         if (words[1] & 2) return fail(ctx, LP_ETIMEOUT, "a bounded wait inside the sort of an earlier lp_embed_grad expired (its gradient is invalid)");
+        if (words[1] & 4) return fail(ctx, LP_EINVAL, "decreasing offsets, or offsets outside the rows, were passed to an earlier lp_grouped_linear or lp_grouped_weight_grad (they were clamped)");
         return fail(ctx, LP_EINVAL, "an id outside the table was passed to an earlier lp_embed (its row is zero) or lp_embed_grad (its row went nowhere)");
     }
     out->negatives_exhausted = (int64_t)ex;
@@ -2619,6 +2621,94 @@ extern "C" lp_status lp_residual_norm_grad(lp_ctx *ctx, const lp_residual_desc *
     if (ps == LP_BF16) residual_grad_launch<bf16, bf16>(ctx->ex, k, g, o, accumulate);
     else if (pd == LP_BF16) residual_grad_launch<float, bf16>(ctx->ex, k, g, o, accumulate);
     else residual_grad_launch<float, float>(ctx->ex, k, g, o, accumulate);
+    CK_LAUNCH();
+    return LP_OK;
+}
+
+// ----------------------------------------------------------------------------------------------
+// products by group
+// ----------------------------------------------------------------------------------------------
+static lp_status grouped_check(lp_ctx *ctx, const std::string &who, int32_t prec, int64_t M, int32_t N, int32_t K, int64_t groups, const int32_t *offsets)
+{
+    if (!prec_ok(prec)) return fail(ctx, LP_EINVAL, who + ": unknown precision");
+    if (M < 0 || M >= ((int64_t)1 << 31) - 256) return fail(ctx, LP_EINVAL, who + ": number of rows must be in [0, 2^31 - 257]");
+    if (N < 1 || K < 1 || N > (1 << 20) || K > (1 << 20)) return fail(ctx, LP_EINVAL, who + ": widths must be in [1, 2^20]");
+    if (groups < 0 || groups > GP_MAX_GROUPS) return fail(ctx, LP_EINVAL, who + ": number of groups must be in [0, 2^20]");
+    if (groups > 0 && !offsets) return fail(ctx, LP_EINVAL, who + ": null array");
+    if (misaligned(offsets, LP_FP32)) return fail(ctx, LP_EINVAL, who + ": an array is not aligned to its elements");
+    return LP_OK;
+}
+
+extern "C" lp_status lp_grouped_linear(lp_ctx *ctx, int32_t prec, int64_t M, int32_t N, int32_t K, int64_t groups, const int32_t *offsets, const void *A, int64_t ld_a,
+                                       const void *B, int32_t trans_b, const float *bias, int32_t relu, void *C, int64_t ld_c)
+{
+    if (!ctx) return LP_EINVAL;
+    const std::string who = "lp_grouped_linear";
+    lp_status s = grouped_check(ctx, who, prec, M, N, K, groups, offsets);
+    if (s != LP_OK) return s;
+    if (ld_a < K || ld_c < N) return fail(ctx, LP_EINVAL, who + ": a row pitch is smaller than the width");
+    if (M == 0 || groups == 0) return LP_OK;
+    if (!A || !B || !C) return fail(ctx, LP_EINVAL, who + ": null array");
+    if (misaligned(A, prec) || misaligned(B, prec) || misaligned(C, prec) || misaligned(bias, LP_FP32)) return fail(ctx, LP_EINVAL, who + ": an array is not aligned to its elements");
+    CK(cudaSetDevice(ctx->device));
+    GroupedParams p{};
+    p.offsets = offsets; p.groups = (int)groups; p.rows = (int)M; p.N = N; p.K = K;
+    p.A = A; p.lda = ld_a; p.B = B; p.ldb = trans_b ? K : N; p.stride_b = (int64_t)N * K;
+    p.bias = bias; p.relu = relu != 0; p.C = C; p.ldc = ld_c;
+    p.offsets_err = ctx->embed_err;
+    std::string err;
+    bool ok;
+    if (prec == LP_FP32) {
+        p.flush = 1;
+        p.vec_c = on_16_bytes<float>(C, ld_c) && N % 4 == 0;
+        const GroupedPlan g = grouped_plan(false, false, M, groups, N, K);
+        ok = trans_b ? grouped_launch<GP_NT, float>(ctx->tc, ctx->ex, p, g, err) : grouped_launch<GP_NN, float>(ctx->tc, ctx->ex, p, g, err);
+    } else {
+        p.flush = (K + 63) / 64;
+        p.vec_c = on_16_bytes<bf16>(C, ld_c) && N % 8 == 0;
+        const GroupedPlan g = grouped_plan(grouped_tma<bf16>(A, ld_a, B, p.ldb), false, M, groups, N, K);
+        ok = trans_b ? grouped_launch<GP_NT, bf16>(ctx->tc, ctx->ex, p, g, err) : grouped_launch<GP_NN, bf16>(ctx->tc, ctx->ex, p, g, err);
+    }
+    if (!ok) return fail(ctx, LP_ECUDA, who + ": " + err);
+    CK_LAUNCH();
+    return LP_OK;
+}
+
+extern "C" lp_status lp_grouped_weight_grad(lp_ctx *ctx, int32_t prec, int64_t M, int32_t N, int32_t K, int64_t groups, const int32_t *offsets, const void *A, int64_t ld_a,
+                                            const void *dZ, int64_t ld_dz, int32_t accumulate, float *dW, float *dbias)
+{
+    if (!ctx) return LP_EINVAL;
+    const std::string who = "lp_grouped_weight_grad";
+    lp_status s = grouped_check(ctx, who, prec, M, N, K, groups, offsets);
+    if (s != LP_OK) return s;
+    if (ld_a < K || ld_dz < N) return fail(ctx, LP_EINVAL, who + ": a row pitch is smaller than the width");
+    if (groups == 0) return LP_OK;
+    if (!dW || (M > 0 && (!A || !dZ))) return fail(ctx, LP_EINVAL, who + ": null array");
+    if (misaligned(A, prec) || misaligned(dZ, prec) || misaligned(dW, LP_FP32) || misaligned(dbias, LP_FP32))
+        return fail(ctx, LP_EINVAL, who + ": an array is not aligned to its elements");
+    CK(cudaSetDevice(ctx->device));
+    if (M == 0) {
+        if (!accumulate) {
+            CK(cudaMemsetAsync(dW, 0, sizeof(float) * (size_t)groups * K * N, ctx->ex.st));
+            if (dbias) CK(cudaMemsetAsync(dbias, 0, sizeof(float) * (size_t)groups * N, ctx->ex.st));
+        }
+        return LP_OK;
+    }
+    const GroupedPlan g = grouped_plan(prec == LP_BF16 && grouped_tma<bf16>(A, ld_a, dZ, ld_dz), true, M, groups, N, K);
+    uint8_t *ws = nullptr;
+    s = op_workspace(ctx, g.slots_bytes + sizeof(GroupedSplit) * (size_t)g.blocks, &ws);
+    if (s != LP_OK) return s;
+    GroupedParams p{};
+    p.offsets = offsets; p.groups = (int)groups; p.rows = (int)M; p.N = N; p.K = K;
+    p.A = A; p.lda = ld_a; p.B = dZ; p.ldb = ld_dz; p.stride_b = 0;
+    p.vec_c = on_16_bytes<float>(dW, N) && N % 4 == 0;
+    p.dW = dW; p.dbias = dbias; p.accumulate = accumulate != 0;
+    p.slots = (float *)ws; p.splits = (GroupedSplit *)(ws + g.slots_bytes);
+    p.offsets_err = ctx->embed_err;
+    p.flush = prec == LP_FP32 ? 1 : 8;
+    std::string err;
+    const bool ok = prec == LP_FP32 ? grouped_launch<GP_WGRAD, float>(ctx->tc, ctx->ex, p, g, err) : grouped_launch<GP_WGRAD, bf16>(ctx->tc, ctx->ex, p, g, err);
+    if (!ok) return fail(ctx, LP_ECUDA, who + ": " + err);
     CK_LAUNCH();
     return LP_OK;
 }

@@ -6,7 +6,7 @@ import re
 import pytest
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
-NAMES = ("lp_dropout", "lp_residual_norm", "lp_residual_norm_grad")
+NAMES = ("lp_dropout", "lp_residual_norm", "lp_residual_norm_grad", "lp_grouped_linear", "lp_grouped_weight_grad")
 
 
 @pytest.fixture(scope="module")
