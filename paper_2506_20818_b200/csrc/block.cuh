@@ -27,21 +27,40 @@ struct DropArgs {
     uint2 key;
     uint32_t step_lo;
     uint32_t threshold;  // 0 = nothing is dropped, 65536 = everything
+    uint32_t below2;     // threshold - 1 in both halves: the largest u that is dropped
     float factor;
     int64_t row_base;
 };
 
-// bit i: element i of the eight of this row and group of columns stays
-LP_DEVINL uint32_t drop_keep8(const DropArgs &d, int64_t row, uint32_t group)
+// the bits of the eight elements of this row and group of columns, two per word
+LP_DEVINL uint4 drop_words(const DropArgs &d, int64_t row, uint32_t group)
 {
     const uint64_t r = (uint64_t)(d.row_base + row);
-    const uint4 x = philox4x32_10(make_uint4((uint32_t)r, (uint32_t)(r >> 32), d.step_lo, DRAW_DROPOUT | group << 8), d.key);
+    return philox4x32_10(make_uint4((uint32_t)r, (uint32_t)(r >> 32), d.step_lo, DRAW_DROPOUT | group << 8), d.key);
+}
+// zero in the place of the elements of v that are dropped (not for threshold 0)
+LP_DEVINL void drop8(const DropArgs &d, const uint4 &x, float *v)
+{
     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-    uint32_t keep = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        keep |= ((w[i] & 0xffffu) >= d.threshold ? 1u : 0u) << (2 * i);
-        keep |= ((w[i] >> 16) >= d.threshold ? 1u : 0u) << (2 * i + 1);
+        bool hi, lo;  // one instruction compares both halves of a word
+        (void)__vibmin_u16x2(w[i], d.below2, &hi, &lo);
+        v[2 * i] = lo ? 0.f : v[2 * i];
+        v[2 * i + 1] = hi ? 0.f : v[2 * i + 1];
+    }
+}
+// bit i: element i stays (not for threshold 0)
+LP_DEVINL uint32_t drop_keep8(const DropArgs &d, const uint4 &x)
+{
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    uint32_t keep = 0xffu;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        bool hi, lo;
+        (void)__vibmin_u16x2(w[i], d.below2, &hi, &lo);
+        keep ^= lo ? 1u << (2 * i) : 0u;
+        keep ^= hi ? 2u << (2 * i) : 0u;
     }
     return keep;
 }
@@ -62,10 +81,10 @@ template <bool VEC> struct Cols {
     // keep bits in the order of the thread's columns
     LP_DEVINL uint32_t keep(const DropArgs &d, int64_t row, int lane) const
     {
-        if (VEC) return drop_keep8(d, row, (uint32_t)(base >> 3));
+        if (VEC) return drop_keep8(d, drop_words(d, row, (uint32_t)(base >> 3)));
         // the thread draws the bits of the eight neighbouring columns that it would own under VEC and hands them round its team
         const int lane_t = lane & (step - 1), first = base - lane_t;
-        const uint32_t mine = drop_keep8(d, row, (uint32_t)(first / 8 + lane_t));
+        const uint32_t mine = drop_keep8(d, drop_words(d, row, (uint32_t)(first / 8 + lane_t)));
         uint32_t keep = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -135,15 +154,39 @@ template <typename T, bool VEC> __global__ void __launch_bounds__(DROP_THREADS) 
     const int64_t stride = (int64_t)gridDim.x * (DROP_THREADS / p.team);
     const int64_t rounds = (p.rows + stride - 1) / stride;
     int64_t row = (int64_t)blockIdx.x * (DROP_THREADS / p.team) + threadIdx.x / p.team;
+    if (VEC) {
+        // two rows at a time: four to eight loads are under way while the bits are drawn
+        for (; row < p.rows; row += 2 * stride) {
+            const bool two = row + stride < p.rows;
+            for (int c0 = 8 * t; c0 < p.width; c0 += 8 * p.team) {
+                Cols<VEC> c(0, 1, p.width);
+                c.base = c0;
+                float v[8], w[8];
+                load8<T, VEC>((const T *)p.in + row * p.ld_in, c, v);
+                if (two) load8<T, VEC>((const T *)p.in + (row + stride) * p.ld_in, c, w);
+                if (p.drop.threshold) drop8(p.drop, drop_words(p.drop, row, (uint32_t)c0 >> 3), v);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] *= p.drop.factor;
+                store8<T, VEC>((T *)p.out + row * p.ld_out, c, v);
+                if (two) {
+                    if (p.drop.threshold) drop8(p.drop, drop_words(p.drop, row + stride, (uint32_t)c0 >> 3), w);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) w[j] *= p.drop.factor;
+                    store8<T, VEC>((T *)p.out + (row + stride) * p.ld_out, c, w);
+                }
+            }
+        }
+        return;
+    }
     for (int64_t i = 0; i < rounds; ++i, row += stride) {
         for (int c0 = 0; c0 < p.width; c0 += 8 * p.team) {
             Cols<VEC> c(t, p.team, p.width);
             c.base += c0;
+            float v[8];
+            if (row < p.rows) load8<T, VEC>((const T *)p.in + row * p.ld_in, c, v);
             // the whole warp takes part in handing the bits round, rows that are not there too
-            const uint32_t keep = c.keep(p.drop, row, lane);
+            const uint32_t keep = p.drop.threshold ? c.keep(p.drop, row, lane) : 0xffu;
             if (row < p.rows) {
-                float v[8];
-                load8<T, VEC>((const T *)p.in + row * p.ld_in, c, v);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] = (keep >> j) & 1u ? v[j] * p.drop.factor : 0.f;
                 store8<T, VEC>((T *)p.out + row * p.ld_out, c, v);
@@ -172,6 +215,80 @@ struct ResidualParams {
     void *y, *n, *dx, *dh, *dgate;
     int64_t ld_x, ld_h, ld_y, ld_n, ld_dy, ld_dn, ld_dx, ld_dh, ld_dgate;
     float *partial;            // [gridDim.x][RN_SUMS][width] column sums of each block
+    int pieces, stages;        // of the rows under way: 16-byte pieces per thread and row, rows
+    int at_x, at_h, at_gate, at_y, at_dn, at_dy;  // first piece of each array
+};
+
+// Rows on their way into shared memory: each thread copies its own eight columns of the arrays a row needs (16 bytes at a time;
+// FP32 rows of any alignment 4 bytes at a time) several rows ahead and reads back only what it copied itself, so no barrier is
+// needed, and what is under way takes no registers.  What lies beyond the row or the last row arrives as zeros.
+// BF16 rows that do not start on 16 bytes cannot be copied this way and are loaded when they are needed.
+template <typename T> constexpr int PIPE_PIECES = sizeof(T) == 4 ? 2 : 1;  // of 16 bytes
+LP_DEVINL void copy_async_16(uint32_t dst, const void *src, int bytes)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+LP_DEVINL void copy_async_4(uint32_t dst, const void *src, int bytes)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+template <bool VEC> struct RowPipe {
+    uint32_t base;       // of this thread's pieces
+    uint32_t piece, stage_bytes;
+    int stages, head;    // the stage that is read next
+    LP_DEVINL RowPipe(uint8_t *smem, int pieces, int stages_)
+        : base(smem_u32(smem) + threadIdx.x * 16), piece(blockDim.x * 16), stage_bytes(pieces * blockDim.x * 16), stages(stages_), head(0) {}
+    LP_DEVINL uint32_t stage(int ahead) const
+    {
+        int s = head + ahead;
+        if (s >= stages) s -= stages;
+        return base + s * stage_bytes;
+    }
+    // `at`: first piece of the array in the stage
+    template <typename T> LP_DEVINL void copy(uint32_t st, int at, const void *array, int64_t ld, int64_t row, bool live, const Cols<VEC> &c) const
+    {
+        if (!VEC && sizeof(T) == 2) return;
+        const T *src = (const T *)array + (live ? row * ld : 0);
+        if (VEC) {
+#pragma unroll
+            for (int k = 0; k < PIPE_PIECES<T>; ++k) {
+                const int col = c.base + k * (16 / (int)sizeof(T)), have = live ? min(max(c.width - col, 0) * (int)sizeof(T), 16) : 0;
+                copy_async_16(st + (at + k) * piece, src + (have ? col : 0), have);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const bool has = live && c.has(j);
+                copy_async_4(st + (at + (j >> 2)) * piece + (j & 3) * 4, src + (has ? c.at(j) : 0), has ? 4 : 0);
+            }
+        }
+    }
+    template <typename T> LP_DEVINL void read(uint32_t st, int at, const void *array, int64_t ld, int64_t row, bool live, const Cols<VEC> &c, float *v) const
+    {
+        if (!VEC && sizeof(T) == 2) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = live && c.has(j) ? to_f<T>(((const T *)array)[row * ld + c.at(j)]) : 0.f;
+            return;
+        }
+#pragma unroll
+        for (int k = 0; k < PIPE_PIECES<T>; ++k) {
+            Vec16<T> x;
+            uint32_t w[4];
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(st + (at + k) * piece));
+            memcpy(&x.v, w, 16);
+            x.to_float(v + k * Vec16<T>::N);
+        }
+    }
+    LP_DEVINL void commit() const { asm volatile("cp.async.commit_group;" ::: "memory"); }
+    // the oldest row has arrived
+    LP_DEVINL void wait() const
+    {
+        if (stages == 1) asm volatile("cp.async.wait_group 0;" ::: "memory");
+        else if (stages == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+        else if (stages == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
+        else asm volatile("cp.async.wait_group 3;" ::: "memory");
+    }
+    LP_DEVINL void next() { head = head + 1 == stages ? 0 : head + 1; }
 };
 
 // Sums of K values over a team, in every one of its threads.  A fixed tree, so the same bits in every run.
@@ -224,44 +341,66 @@ template <bool VEC, bool BLOCK> LP_DEVINL float normalise(float *v, int kind, fl
     return r;
 }
 
-// MAXT: the largest team of the variant, 32 (parts of warps) or 1024 (whole blocks)
-template <typename TS, typename TD, bool VEC, int MAXT> __global__ void __launch_bounds__(MAXT < 256 ? 256 : MAXT) residual_norm_kernel(const __grid_constant__ ResidualParams p)
+// MAXT: the largest team of the variant, 32 (parts of warps), 256 or 1024 (whole blocks).  BIAS: norms with a bias
+template <typename TS, typename TD, bool VEC, int MAXT, bool BIAS> __global__ void __launch_bounds__(MAXT < 256 ? 256 : MAXT) residual_norm_kernel(const __grid_constant__ ResidualParams p)
 {
     LP_DEP_ENTER();
     constexpr bool BLOCK = MAXT > 32;
     __shared__ float scratch[2 * 32 * 4];
+    extern __shared__ __align__(16) uint8_t pipe_smem[];
     int turn = 0;
     const int T = p.team, t = threadIdx.x & (T - 1), lane = threadIdx.x & 31, teams = BLOCK ? 1 : blockDim.x / T;
     const Cols<VEC> c(t, T, p.width);
     float pre[8], pre_bias[8], post[8], post_bias[8], gate_vec[8];
     load_param8(p.pre, c, 1.f, pre);
-    load_param8(p.pre_bias, c, 0.f, pre_bias);
     load_param8(p.post, c, 1.f, post);
-    load_param8(p.post_bias, c, 0.f, post_bias);
     load_param8(p.gate_vec, c, 1.f, gate_vec);
+    if (BIAS) {
+        load_param8(p.pre_bias, c, 0.f, pre_bias);
+        load_param8(p.post_bias, c, 0.f, post_bias);
+    }
     const int64_t stride = (int64_t)gridDim.x * teams, rounds = (p.rows + stride - 1) / stride;
     int64_t row = (int64_t)blockIdx.x * teams + (BLOCK ? 0 : threadIdx.x / T);
-    for (int64_t i = 0; i < rounds; ++i, row += stride) {
+    RowPipe<VEC> pipe(pipe_smem, p.pieces, p.stages);
+    auto fetch = [&](int64_t r, int ahead) {
+        const uint32_t st = pipe.stage(ahead);
+        const bool live = r < p.rows;
+        pipe.template copy<TS>(st, p.at_x, p.x, p.ld_x, r, live, c);
+        if (p.h) pipe.template copy<TD>(st, p.at_h, p.h, p.ld_h, r, live, c);
+        if (p.gate) pipe.template copy<TD>(st, p.at_gate, p.gate, p.ld_gate, r, live, c);
+        pipe.commit();
+    };
+    for (int i = 0; i < p.stages - 1; ++i) fetch(row + i * stride, i);
+    for (int64_t i = 0; i < rounds; ++i, row += stride, pipe.next()) {
         const bool live = row < p.rows;  // of a warp's teams some may be past the last row; they take part in the sums of the others
+        fetch(row + (p.stages - 1) * stride, p.stages - 1);
+        uint4 bits;
+        if (VEC && p.drop.threshold) bits = drop_words(p.drop, row, (uint32_t)c.base >> 3);
+        pipe.wait();
+        const uint32_t st = pipe.stage(0);
         float y[8], b[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = b[j] = 0.f;
-        if (live) load8<TS, VEC>((const TS *)p.x + row * p.ld_x, c, y);
+        pipe.template read<TS>(st, p.at_x, p.x, p.ld_x, row, live, c, y);
         if (p.h) {
-            if (live) load8<TD, VEC>((const TD *)p.h + row * p.ld_h, c, b);
+            pipe.template read<TD>(st, p.at_h, p.h, p.ld_h, row, live, c, b);
             if (p.post_norm) {
                 normalise<VEC, BLOCK>(b, p.post_norm, p.eps, p.inv_width, c, T, scratch, turn);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) b[j] = fmaf(b[j], post[j], post_bias[j]);
+                for (int j = 0; j < 8; ++j) b[j] = BIAS ? fmaf(b[j], post[j], post_bias[j]) : b[j] * post[j];
             }
             if (p.drop.threshold) {
-                const uint32_t keep = c.keep(p.drop, row, lane);
+                if (VEC) {
+                    drop8(p.drop, bits, b);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) b[j] = (keep >> j) & 1u ? b[j] * p.drop.factor : 0.f;
+                    for (int j = 0; j < 8; ++j) b[j] *= p.drop.factor;
+                } else {
+                    const uint32_t keep = c.keep(p.drop, row, lane);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) b[j] = (keep >> j) & 1u ? b[j] * p.drop.factor : 0.f;
+                }
             }
             if (p.gate) {
-                float g[8] = {};
-                if (live) load8<TD, VEC>((const TD *)p.gate + row * p.ld_gate, c, g);
+                float g[8];
+                pipe.template read<TD>(st, p.at_gate, p.gate, p.ld_gate, row, live, c, g);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) b[j] *= g[j];
             }
@@ -272,7 +411,7 @@ template <typename TS, typename TD, bool VEC, int MAXT> __global__ void __launch
         if (p.pre_norm) {
             normalise<VEC, BLOCK>(y, p.pre_norm, p.eps, p.inv_width, c, T, scratch, turn);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = fmaf(y[j], pre[j], pre_bias[j]);
+            for (int j = 0; j < 8; ++j) y[j] = BIAS ? fmaf(y[j], pre[j], pre_bias[j]) : y[j] * pre[j];
             if (live) store8<TD, VEC>((TD *)p.n + row * p.ld_n, c, y);
         }
     }
@@ -321,14 +460,15 @@ __global__ void __launch_bounds__(MAXT < 256 ? 256 : MAXT) residual_norm_grad_ke
     constexpr bool BLOCK = MAXT > 32;
     __shared__ float scratch[2 * 32 * 4];
     __shared__ float sums[BLOCK ? 1 : 8 * 256];
+    extern __shared__ __align__(16) uint8_t pipe_smem[];
     int turn = 0;
     const int T = p.team, t = threadIdx.x & (T - 1), lane = threadIdx.x & 31, teams = BLOCK ? 1 : blockDim.x / T;
     const Cols<VEC> c(t, T, p.width);
     float pre[8], post[8], post_bias[8], gate_vec[8];
     load_param8(p.pre, c, 1.f, pre);
     load_param8(p.post, c, 1.f, post);
-    load_param8(p.post_bias, c, 0.f, post_bias);
     load_param8(p.gate_vec, c, 1.f, gate_vec);
+    if (BIAS) load_param8(p.post_bias, c, 0.f, post_bias);
     float acc[RN_SUMS][8];
 #pragma unroll
     for (int k = 0; k < RN_SUMS; ++k)
@@ -336,50 +476,68 @@ __global__ void __launch_bounds__(MAXT < 256 ? 256 : MAXT) residual_norm_grad_ke
         for (int j = 0; j < 8; ++j) acc[k][j] = 0.f;
     const int64_t stride = (int64_t)gridDim.x * teams, rounds = (p.rows + stride - 1) / stride;
     int64_t row = (int64_t)blockIdx.x * teams + (BLOCK ? 0 : threadIdx.x / T);
-    for (int64_t i = 0; i < rounds; ++i, row += stride) {
+    RowPipe<VEC> pipe(pipe_smem, p.pieces, p.stages);
+    auto fetch = [&](int64_t r, int ahead) {
+        const uint32_t st = pipe.stage(ahead);
+        const bool live = r < p.rows;
+        if (p.pre_norm) {
+            pipe.template copy<TD>(st, p.at_dn, p.dn, p.ld_dn, r, live, c);
+            pipe.template copy<TS>(st, p.at_y, p.y, p.ld_y, r, live, c);
+        }
+        if (p.dy) pipe.template copy<TS>(st, p.at_dy, p.dy, p.ld_dy, r, live, c);
+        if (p.h) pipe.template copy<TD>(st, p.at_h, p.h, p.ld_h, r, live, c);
+        if (p.gate) pipe.template copy<TD>(st, p.at_gate, p.gate, p.ld_gate, r, live, c);
+        pipe.commit();
+    };
+    for (int i = 0; i < p.stages - 1; ++i) fetch(row + i * stride, i);
+    for (int64_t i = 0; i < rounds; ++i, row += stride, pipe.next()) {
         const bool live = row < p.rows;
+        fetch(row + (p.stages - 1) * stride, p.stages - 1);
+        const uint32_t keep = p.drop.threshold ? c.keep(p.drop, row, lane) : 0xffu;
+        pipe.wait();
+        const uint32_t st = pipe.stage(0);
         float g[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) g[j] = 0.f;
         if (p.pre_norm) {
-            float y[8] = {};
-            if (live) {
-                load8<TD, VEC>((const TD *)p.dn + row * p.ld_dn, c, g);
-                load8<TS, VEC>((const TS *)p.y + row * p.ld_y, c, y);
-            }
+            float y[8];
+            pipe.template read<TD>(st, p.at_dn, p.dn, p.ld_dn, row, live, c, g);
+            pipe.template read<TS>(st, p.at_y, p.y, p.ld_y, row, live, c, y);
             norm_backward<VEC, BLOCK, BIAS>(y, g, pre, p.pre_norm, p.eps, p.inv_width, c, T, scratch, turn, acc[0], acc[3]);
         }
-        if (p.dy && live) {
+        if (p.dy) {
             float d[8];
-            load8<TS, VEC>((const TS *)p.dy + row * p.ld_dy, c, d);
+            pipe.template read<TS>(st, p.at_dy, p.dy, p.ld_dy, row, live, c, d);
 #pragma unroll
             for (int j = 0; j < 8; ++j) g[j] += d[j];
         }
         if (p.dx && live) store8<TS, VEC>((TS *)p.dx + row * p.ld_dx, c, g);
         if (!p.h) continue;
         // the branch: g -> gradient of h
-        float h[8] = {}, m[8] = {}, z[8];
-        if (live) load8<TD, VEC>((const TD *)p.h + row * p.ld_h, c, h);
-        if (p.gate && live) load8<TD, VEC>((const TD *)p.gate + row * p.ld_gate, c, m);
-        const uint32_t keep = p.drop.threshold ? c.keep(p.drop, row, lane) : 0xffu;
+        float m[8], z[8], q[8];
+        pipe.template read<TD>(st, p.at_h, p.h, p.ld_h, row, live, c, z);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             g[j] = (keep >> j) & 1u ? p.scale * p.drop.factor * g[j] : 0.f;   // times gate: gradient of post(h)
-            z[j] = h[j];
+            q[j] = g[j] * gate_vec[j];
         }
-        float q[8];
+        if (p.gate) {
+            pipe.template read<TD>(st, p.at_gate, p.gate, p.ld_gate, row, live, c, m);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) q[j] = g[j] * gate_vec[j] * (p.gate ? m[j] : 1.f);
+            for (int j = 0; j < 8; ++j) q[j] *= m[j];
+        }
         if (p.post_norm) norm_backward<VEC, BLOCK, BIAS>(z, q, post, p.post_norm, p.eps, p.inv_width, c, T, scratch, turn, acc[1], acc[4]);
         if (p.dh && live) store8<TD, VEC>((TD *)p.dh + row * p.ld_dh, c, q);
-        if (p.dgate && live) {
+        if (p.dgate || p.gate_vec) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) m[j] = (keep >> j) & 1u ? g[j] * fmaf(z[j], post[j], post_bias[j]) : 0.f;
-            store8<TD, VEC>((TD *)p.dgate + row * p.ld_dgate, c, m);
+            for (int j = 0; j < 8; ++j) m[j] = (keep >> j) & 1u ? g[j] * (BIAS ? fmaf(z[j], post[j], post_bias[j]) : z[j] * post[j]) : 0.f;
+            if (p.gate_vec) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[2][j] += m[j];
+            } else if (live) {
+                store8<TD, VEC>((TD *)p.dgate + row * p.ld_dgate, c, m);
+            }
         }
-        if (p.gate_vec)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) acc[2][j] += (keep >> j) & 1u ? g[j] * fmaf(z[j], post[j], post_bias[j]) : 0.f;
     }
     // column sums of the block: its teams' added in order
 #pragma unroll
@@ -469,37 +627,70 @@ template <typename TS, typename TD> static bool residual_vec(const ResidualParam
            on_16_bytes<TD>(p.gate, p.ld_gate) && on_16_bytes<TD>(p.dgate, p.ld_dgate);
 }
 
+// pieces of the rows under way and how many rows: `room` bytes of shared memory per thread keep as many blocks resident as registers do
+template <typename TS, typename TD> static size_t residual_pipe(ResidualParams &p, const ResidualGrid &g, int room)
+{
+    const int s = PIPE_PIECES<TS>, d = PIPE_PIECES<TD>;
+    int at = 0;
+    auto place = [&](const void *array, int pieces) { const int here = at; if (array) at += pieces; return here; };
+    p.at_x = place(p.x, s);
+    p.at_dn = place(p.dn, d);
+    p.at_y = place(p.dn ? p.y : nullptr, s);
+    p.at_dy = place(p.dy, s);
+    p.at_h = place(p.h, d);
+    p.at_gate = place(p.gate, d);
+    p.pieces = at;
+    p.stages = std::max(2, std::min(4, room / (16 * at)));
+    while (p.stages * at * 16 * g.threads > 216 * 1024) --p.stages;  // blocks of 1024 threads: down to one, nothing under way
+    return (size_t)p.stages * at * 16 * g.threads;
+}
+template <typename... A, typename... P> static void launch_large(void (*kernel)(A...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, P &&...args)
+{
+    if (smem > 40 * 1024) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    launch_dep(kernel, grid, block, smem, st, args...);
+}
+
+template <typename TS, typename TD, bool VEC, bool BIAS> static void residual_dispatch(Exec &ex, const ResidualParams &p, const ResidualGrid &g, size_t smem)
+{
+    const dim3 grid(g.blocks), block(g.threads);
+    if (g.threads > 256) launch_large(residual_norm_kernel<TS, TD, VEC, 1024, BIAS>, grid, block, smem, ex.st, p);
+    else if (g.block) launch_large(residual_norm_kernel<TS, TD, VEC, 256, BIAS>, grid, block, smem, ex.st, p);
+    else launch_large(residual_norm_kernel<TS, TD, VEC, 32, BIAS>, grid, block, smem, ex.st, p);
+}
 template <typename TS, typename TD> static void residual_launch(Exec &ex, ResidualParams &p)
 {
-    const ResidualGrid g = residual_grid(p.rows, p.width, 1024);
+    const ResidualGrid g = residual_grid(p.rows, p.width, 768);
     p.team = g.team;
-    const dim3 grid(g.blocks), block(g.threads);
+    const size_t smem = residual_pipe<TS, TD>(p, g, 256);
+    const bool bias = p.pre_bias || p.post_bias;
     if (residual_vec<TS, TD>(p)) {
-        if (g.block) launch_dep(residual_norm_kernel<TS, TD, true, 1024>, grid, block, 0, ex.st, p);
-        else launch_dep(residual_norm_kernel<TS, TD, true, 32>, grid, block, 0, ex.st, p);
+        if (bias) residual_dispatch<TS, TD, true, true>(ex, p, g, smem);
+        else residual_dispatch<TS, TD, true, false>(ex, p, g, smem);
     } else {
-        if (g.block) launch_dep(residual_norm_kernel<TS, TD, false, 1024>, grid, block, 0, ex.st, p);
-        else launch_dep(residual_norm_kernel<TS, TD, false, 32>, grid, block, 0, ex.st, p);
+        if (bias) residual_dispatch<TS, TD, false, true>(ex, p, g, smem);
+        else residual_dispatch<TS, TD, false, false>(ex, p, g, smem);
     }
     ex.launches += 1;
 }
 
-template <typename TS, typename TD, bool VEC, bool BIAS> static void residual_grad_dispatch(Exec &ex, const ResidualParams &p, const ResidualGrid &g)
+template <typename TS, typename TD, bool VEC, bool BIAS> static void residual_grad_dispatch(Exec &ex, const ResidualParams &p, const ResidualGrid &g, size_t smem)
 {
-    if (g.threads > 256) launch_dep(residual_norm_grad_kernel<TS, TD, VEC, 1024, BIAS>, dim3(g.blocks), dim3(g.threads), 0, ex.st, p);
-    else if (g.block) launch_dep(residual_norm_grad_kernel<TS, TD, VEC, 256, BIAS>, dim3(g.blocks), dim3(g.threads), 0, ex.st, p);
-    else launch_dep(residual_norm_grad_kernel<TS, TD, VEC, 32, BIAS>, dim3(g.blocks), dim3(g.threads), 0, ex.st, p);
+    const dim3 grid(g.blocks), block(g.threads);
+    if (g.threads > 256) launch_large(residual_norm_grad_kernel<TS, TD, VEC, 1024, BIAS>, grid, block, smem, ex.st, p);
+    else if (g.block) launch_large(residual_norm_grad_kernel<TS, TD, VEC, 256, BIAS>, grid, block, smem, ex.st, p);
+    else launch_large(residual_norm_grad_kernel<TS, TD, VEC, 32, BIAS>, grid, block, smem, ex.st, p);
 }
 template <typename TS, typename TD> static void residual_grad_launch(Exec &ex, ResidualParams &p, const ResidualGrid &g, const ResidualSums &o, int accumulate)
 {
     p.team = g.team;
-    const bool bias = o.out[3] || o.out[4];
+    const size_t smem = residual_pipe<TS, TD>(p, g, 380);
+    const bool bias = o.out[3] || o.out[4] || p.post_bias;
     if (residual_vec<TS, TD>(p)) {
-        if (bias) residual_grad_dispatch<TS, TD, true, true>(ex, p, g);
-        else residual_grad_dispatch<TS, TD, true, false>(ex, p, g);
+        if (bias) residual_grad_dispatch<TS, TD, true, true>(ex, p, g, smem);
+        else residual_grad_dispatch<TS, TD, true, false>(ex, p, g, smem);
     } else {
-        if (bias) residual_grad_dispatch<TS, TD, false, true>(ex, p, g);
-        else residual_grad_dispatch<TS, TD, false, false>(ex, p, g);
+        if (bias) residual_grad_dispatch<TS, TD, false, true>(ex, p, g, smem);
+        else residual_grad_dispatch<TS, TD, false, false>(ex, p, g, smem);
     }
     ex.launches += 1;
     int last = -1;

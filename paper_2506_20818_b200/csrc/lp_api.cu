@@ -2482,6 +2482,7 @@ static bool drop_args(double p, uint64_t seed, uint64_t step, int64_t row_base, 
     d.step_lo = (uint32_t)step;
     d.threshold = (uint32_t)std::llround(65536.0 * p);
     d.factor = d.threshold < 65536u ? (float)(65536.0 / (65536.0 - d.threshold)) : 0.f;
+    d.below2 = (d.threshold - 1u) * 0x10001u;
     d.row_base = row_base;
     return true;
 }
