@@ -24,7 +24,7 @@
 enum : uint32_t { DRAW_DROPOUT = 5 };
 
 struct DropArgs {
-    uint2 key;
+    uint32_t key[20];    // of the ten rounds: constants beside the instructions that use them
     uint32_t step_lo;
     uint32_t threshold;  // 0 = nothing is dropped, 65536 = everything
     uint32_t below2;     // threshold - 1 in both halves: the largest u that is dropped
@@ -36,7 +36,13 @@ struct DropArgs {
 LP_DEVINL uint4 drop_words(const DropArgs &d, int64_t row, uint32_t group)
 {
     const uint64_t r = (uint64_t)(d.row_base + row);
-    return philox4x32_10(make_uint4((uint32_t)r, (uint32_t)(r >> 32), d.step_lo, DRAW_DROPOUT | group << 8), d.key);
+    uint4 c = make_uint4((uint32_t)r, (uint32_t)(r >> 32), d.step_lo, DRAW_DROPOUT | group << 8);
+#pragma unroll
+    for (int i = 0; i < 10; ++i) {
+        const uint64_t a = (uint64_t)0xD2511F53u * c.x, b = (uint64_t)0xCD9E8D57u * c.z;
+        c = make_uint4((uint32_t)(b >> 32) ^ c.y ^ d.key[2 * i], (uint32_t)b, (uint32_t)(a >> 32) ^ c.w ^ d.key[2 * i + 1], (uint32_t)a);
+    }
+    return c;
 }
 // zero in the place of the elements of v that are dropped (not for threshold 0)
 LP_DEVINL void drop8(const DropArgs &d, const uint4 &x, float *v)
@@ -141,51 +147,69 @@ constexpr int DROP_THREADS = 256;
 struct DropoutParams {
     const void *in;
     void *out;
-    int64_t rows, ld_in, ld_out;
-    int width;
+    int rows, width;
+    int64_t ld_in, ld_out;
     int team;            // threads per row (a power of two, at most 256); wider rows are taken in pieces of 8 team columns
     DropArgs drop;
 };
 
+// A block takes DROP_ROWS rows per team, one after the other; the loads of all of them are under way while the bits are drawn.
+constexpr int DROP_ROWS = 4;
 template <typename T, bool VEC> __global__ void __launch_bounds__(DROP_THREADS) dropout_kernel(const DropoutParams p)
 {
     LP_DEP_ENTER();
-    const int t = threadIdx.x & (p.team - 1), lane = threadIdx.x & 31;
-    const int64_t stride = (int64_t)gridDim.x * (DROP_THREADS / p.team);
-    const int64_t rounds = (p.rows + stride - 1) / stride;
-    int64_t row = (int64_t)blockIdx.x * (DROP_THREADS / p.team) + threadIdx.x / p.team;
+    const int t = threadIdx.x & (p.team - 1), lane = threadIdx.x & 31, teams = DROP_THREADS / p.team;
+    const int64_t row0 = (int64_t)blockIdx.x * teams * DROP_ROWS + threadIdx.x / p.team;
+    const bool drops = p.drop.threshold != 0;
     if (VEC) {
-        // two rows at a time: four to eight loads are under way while the bits are drawn
-        for (; row < p.rows; row += 2 * stride) {
-            const bool two = row + stride < p.rows;
-            for (int c0 = 8 * t; c0 < p.width; c0 += 8 * p.team) {
-                Cols<VEC> c(0, 1, p.width);
-                c.base = c0;
-                float v[8], w[8];
-                load8<T, VEC>((const T *)p.in + row * p.ld_in, c, v);
-                if (two) load8<T, VEC>((const T *)p.in + (row + stride) * p.ld_in, c, w);
-                if (p.drop.threshold) drop8(p.drop, drop_words(p.drop, row, (uint32_t)c0 >> 3), v);
+        constexpr int VN = Vec16<T>::N, NV = 8 / VN;
+        for (int c0 = 8 * t; c0 < p.width; c0 += 8 * p.team) {
+            const T *in = (const T *)p.in + row0 * p.ld_in + c0;
+            T *out = (T *)p.out + row0 * p.ld_out + c0;
+            if (c0 + 8 <= p.width) {
+                Vec16<T> x[DROP_ROWS][NV];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] *= p.drop.factor;
-                store8<T, VEC>((T *)p.out + row * p.ld_out, c, v);
-                if (two) {
-                    if (p.drop.threshold) drop8(p.drop, drop_words(p.drop, row + stride, (uint32_t)c0 >> 3), w);
+                for (int i = 0; i < DROP_ROWS; ++i)
+                    if (row0 + i * teams < p.rows)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) w[j] *= p.drop.factor;
-                    store8<T, VEC>((T *)p.out + (row + stride) * p.ld_out, c, w);
+                        for (int k = 0; k < NV; ++k) x[i][k].load_once(in + (int64_t)i * teams * p.ld_in + k * VN);
+#pragma unroll
+                for (int i = 0; i < DROP_ROWS; ++i) {
+                    const int64_t row = row0 + i * teams;
+                    if (row >= p.rows) break;
+                    float v[8];
+#pragma unroll
+                    for (int k = 0; k < NV; ++k) x[i][k].to_float(v + k * VN);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] *= p.drop.factor;
+                    if (drops) drop8(p.drop, drop_words(p.drop, row, (uint32_t)c0 >> 3), v);
+#pragma unroll
+                    for (int k = 0; k < NV; ++k) {
+                        x[i][k].from_float(v + k * VN);
+                        x[i][k].store(out + (int64_t)i * teams * p.ld_out + k * VN);
+                    }
+                }
+            } else {  // the end of a row whose width is no multiple of eight
+                for (int i = 0; i < DROP_ROWS && row0 + i * teams < p.rows; ++i) {
+                    const uint32_t keep = drops ? drop_keep8(p.drop, drop_words(p.drop, row0 + i * teams, (uint32_t)c0 >> 3)) : 0xffu;
+                    for (int j = 0; c0 + j < p.width; ++j) {
+                        const float x = to_f<T>(in[(int64_t)i * teams * p.ld_in + j]);
+                        out[(int64_t)i * teams * p.ld_out + j] = from_f<T>((keep >> j) & 1u ? x * p.drop.factor : 0.f);
+                    }
                 }
             }
         }
         return;
     }
-    for (int64_t i = 0; i < rounds; ++i, row += stride) {
+    for (int i = 0; i < DROP_ROWS; ++i) {
+        const int64_t row = row0 + i * teams;
         for (int c0 = 0; c0 < p.width; c0 += 8 * p.team) {
             Cols<VEC> c(t, p.team, p.width);
             c.base += c0;
             float v[8];
             if (row < p.rows) load8<T, VEC>((const T *)p.in + row * p.ld_in, c, v);
             // the whole warp takes part in handing the bits round, rows that are not there too
-            const uint32_t keep = p.drop.threshold ? c.keep(p.drop, row, lane) : 0xffu;
+            const uint32_t keep = drops ? c.keep(p.drop, row, lane) : 0xffu;
             if (row < p.rows) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] = (keep >> j) & 1u ? v[j] * p.drop.factor : 0.f;
@@ -199,24 +223,26 @@ template <typename T, bool VEC> __global__ void __launch_bounds__(DROP_THREADS) 
 // residual norm
 // ---------------------------------------------------------------------------------------------
 constexpr int RN_MAX_WIDTH = 8192;  // eight columns for each of 1024 threads
+constexpr int64_t RN_MAX_PITCH = (int64_t)1 << 29;  // elements: a pitch in bytes fits 32 bits, and a row's offset is one multiplication
 constexpr int RN_SUMS = 5;          // column sums of the backward pass: dpre, dpost, dgate, dpre_bias, dpost_bias
 
 struct ResidualParams {
-    int64_t rows;
+    int rows;
     int width, team;
     int pre_norm, post_norm;   // lp_norm
     float eps, inv_width, scale;
     DropArgs drop;
     const float *pre, *pre_bias, *post, *post_bias, *gate_vec;
     const void *gate;          // [rows, width], or null
-    int64_t ld_gate;
+    // pitches in bytes
+    uint32_t ld_gate;
     // forward: x, h in, y, n out (null: not wanted); backward: dy, dn, y, h in, dx, dh, dgate out
     const void *x, *h, *dy, *dn;
     void *y, *n, *dx, *dh, *dgate;
-    int64_t ld_x, ld_h, ld_y, ld_n, ld_dy, ld_dn, ld_dx, ld_dh, ld_dgate;
+    uint32_t ld_x, ld_h, ld_y, ld_n, ld_dy, ld_dn, ld_dx, ld_dh, ld_dgate;
     float *partial;            // [gridDim.x][RN_SUMS][width] column sums of each block
     int pieces, stages;        // of the rows under way: 16-byte pieces per thread and row, rows
-    int at_x, at_h, at_gate, at_y, at_dn, at_dy;  // first piece of each array
+    uint32_t at_x, at_h, at_gate, at_y, at_dn, at_dy;  // bytes to each array's pieces
 };
 
 // Rows on their way into shared memory: each thread copies its own eight columns of the arrays a row needs (16 bytes at a time;
@@ -244,37 +270,38 @@ template <bool VEC> struct RowPipe {
         if (s >= stages) s -= stages;
         return base + s * stage_bytes;
     }
-    // `at`: first piece of the array in the stage
-    template <typename T> LP_DEVINL void copy(uint32_t st, int at, const void *array, int64_t ld, int64_t row, bool live, const Cols<VEC> &c) const
+    // `at`: bytes from the start of a stage to the array's pieces; `ld`: bytes between rows.  row: of an array's row that is there, live: false for zeros
+    template <typename T> LP_DEVINL void copy(uint32_t st, uint32_t at, const void *array, uint32_t ld, uint32_t row, bool live, const Cols<VEC> &c) const
     {
         if (!VEC && sizeof(T) == 2) return;
-        const T *src = (const T *)array + (live ? row * ld : 0);
+        const char *src = (const char *)array + (uint64_t)row * ld;
         if (VEC) {
 #pragma unroll
             for (int k = 0; k < PIPE_PIECES<T>; ++k) {
-                const int col = c.base + k * (16 / (int)sizeof(T)), have = live ? min(max(c.width - col, 0) * (int)sizeof(T), 16) : 0;
-                copy_async_16(st + (at + k) * piece, src + (have ? col : 0), have);
+                const int col = c.base + k * (16 / (int)sizeof(T)), have = min(max(c.width - col, 0) * (int)sizeof(T), 16);
+                copy_async_16(st + at + k * piece, src + (have ? col * (int)sizeof(T) : 0), live ? have : 0);
             }
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const bool has = live && c.has(j);
-                copy_async_4(st + (at + (j >> 2)) * piece + (j & 3) * 4, src + (has ? c.at(j) : 0), has ? 4 : 0);
+                const bool has = c.has(j);
+                copy_async_4(st + at + (j >> 2) * piece + (j & 3) * 4, src + (has ? c.at(j) * (int)sizeof(T) : 0), live && has ? 4 : 0);
             }
         }
     }
-    template <typename T> LP_DEVINL void read(uint32_t st, int at, const void *array, int64_t ld, int64_t row, bool live, const Cols<VEC> &c, float *v) const
+    template <typename T> LP_DEVINL void read(uint32_t st, uint32_t at, const void *array, uint32_t ld, uint32_t row, bool live, const Cols<VEC> &c, float *v) const
     {
         if (!VEC && sizeof(T) == 2) {
+            const T *src = (const T *)((const char *)array + (uint64_t)row * ld);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = live && c.has(j) ? to_f<T>(((const T *)array)[row * ld + c.at(j)]) : 0.f;
+            for (int j = 0; j < 8; ++j) v[j] = live && c.has(j) ? to_f<T>(src[c.at(j)]) : 0.f;
             return;
         }
 #pragma unroll
         for (int k = 0; k < PIPE_PIECES<T>; ++k) {
             Vec16<T> x;
             uint32_t w[4];
-            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(st + (at + k) * piece));
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(st + at + k * piece) : "memory");
             memcpy(&x.v, w, 16);
             x.to_float(v + k * Vec16<T>::N);
         }
@@ -291,10 +318,27 @@ template <bool VEC> struct RowPipe {
     LP_DEVINL void next() { head = head + 1 == stages ? 0 : head + 1; }
 };
 
+template <typename T> LP_DEVINL T *row_at(void *array, uint32_t row, uint32_t ld) { return (T *)((char *)array + (uint64_t)row * ld); }
+
+// 1 / sqrt(x) of a positive x: the hardware's estimate and one Newton step, off by about 1.5 2^-24 (the correctly rounded square root and
+// division took 35 instructions)
+LP_DEVINL float inv_sqrt(float x)
+{
+    const float r = rsqrtf(x);
+    return fmaf(r * fmaf(-x * r, r, 1.f), 0.5f, r);
+}
+
 // Sums of K values over a team, in every one of its threads.  A fixed tree, so the same bits in every run.
 template <int K, bool BLOCK> LP_DEVINL void team_sum(float (&v)[K], int T, float *scratch, int &turn)
 {
     if (!BLOCK) {
+        if (T == 32) {
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+                for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+            return;
+        }
         for (int o = T >> 1; o > 0; o >>= 1)
 #pragma unroll
             for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
@@ -335,7 +379,7 @@ template <bool VEC, bool BLOCK> LP_DEVINL float normalise(float *v, int kind, fl
 #pragma unroll
     for (int j = 0; j < 8; ++j) q[0] = fmaf(v[j], v[j], q[0]);
     team_sum<1, BLOCK>(q, T, scratch, turn);
-    const float r = 1.f / sqrtf(fmaf(q[0], inv_width, eps));
+    const float r = inv_sqrt(fmaf(q[0], inv_width, eps));
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] *= r;
     return r;
@@ -355,33 +399,38 @@ template <typename TS, typename TD, bool VEC, int MAXT, bool BIAS> __global__ vo
     load_param8(p.pre, c, 1.f, pre);
     load_param8(p.post, c, 1.f, post);
     load_param8(p.gate_vec, c, 1.f, gate_vec);
+    const float factor = p.h && p.drop.threshold ? p.scale * p.drop.factor : p.scale;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) gate_vec[j] *= factor;
     if (BIAS) {
         load_param8(p.pre_bias, c, 0.f, pre_bias);
         load_param8(p.post_bias, c, 0.f, post_bias);
     }
-    const int64_t stride = (int64_t)gridDim.x * teams, rounds = (p.rows + stride - 1) / stride;
+    const int stride = (int)gridDim.x * teams, rounds = (int)((p.rows + (int64_t)stride - 1) / stride);
     int64_t row = (int64_t)blockIdx.x * teams + (BLOCK ? 0 : threadIdx.x / T);
     RowPipe<VEC> pipe(pipe_smem, p.pieces, p.stages);
-    auto fetch = [&](int64_t r, int ahead) {
+    auto fetch = [&](int64_t at, int ahead) {
         const uint32_t st = pipe.stage(ahead);
-        const bool live = r < p.rows;
+        const bool live = at < p.rows;
+        const uint32_t r = live ? (uint32_t)at : 0u;
         pipe.template copy<TS>(st, p.at_x, p.x, p.ld_x, r, live, c);
         if (p.h) pipe.template copy<TD>(st, p.at_h, p.h, p.ld_h, r, live, c);
         if (p.gate) pipe.template copy<TD>(st, p.at_gate, p.gate, p.ld_gate, r, live, c);
         pipe.commit();
     };
-    for (int i = 0; i < p.stages - 1; ++i) fetch(row + i * stride, i);
-    for (int64_t i = 0; i < rounds; ++i, row += stride, pipe.next()) {
+    for (int i = 0; i < p.stages - 1; ++i) fetch(row + (int64_t)i * stride, i);
+    for (int i = 0; i < rounds; ++i, row += stride, pipe.next()) {
         const bool live = row < p.rows;  // of a warp's teams some may be past the last row; they take part in the sums of the others
-        fetch(row + (p.stages - 1) * stride, p.stages - 1);
+        fetch(row + (int64_t)(p.stages - 1) * stride, p.stages - 1);
+        const uint32_t r = live ? (uint32_t)row : 0u;
         uint4 bits;
         if (VEC && p.drop.threshold) bits = drop_words(p.drop, row, (uint32_t)c.base >> 3);
         pipe.wait();
         const uint32_t st = pipe.stage(0);
         float y[8], b[8];
-        pipe.template read<TS>(st, p.at_x, p.x, p.ld_x, row, live, c, y);
+        pipe.template read<TS>(st, p.at_x, p.x, p.ld_x, r, live, c, y);
         if (p.h) {
-            pipe.template read<TD>(st, p.at_h, p.h, p.ld_h, row, live, c, b);
+            pipe.template read<TD>(st, p.at_h, p.h, p.ld_h, r, live, c, b);
             if (p.post_norm) {
                 normalise<VEC, BLOCK>(b, p.post_norm, p.eps, p.inv_width, c, T, scratch, turn);
 #pragma unroll
@@ -390,29 +439,27 @@ template <typename TS, typename TD, bool VEC, int MAXT, bool BIAS> __global__ vo
             if (p.drop.threshold) {
                 if (VEC) {
                     drop8(p.drop, bits, b);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) b[j] *= p.drop.factor;
                 } else {
                     const uint32_t keep = c.keep(p.drop, row, lane);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) b[j] = (keep >> j) & 1u ? b[j] * p.drop.factor : 0.f;
+                    for (int j = 0; j < 8; ++j) b[j] = (keep >> j) & 1u ? b[j] : 0.f;
                 }
             }
             if (p.gate) {
                 float g[8];
-                pipe.template read<TD>(st, p.at_gate, p.gate, p.ld_gate, row, live, c, g);
+                pipe.template read<TD>(st, p.at_gate, p.gate, p.ld_gate, r, live, c, g);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) b[j] *= g[j];
             }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = fmaf(p.scale * gate_vec[j], b[j], y[j]);
-            if (live && p.y) store8<TS, VEC>((TS *)p.y + row * p.ld_y, c, y);
+            for (int j = 0; j < 8; ++j) y[j] = fmaf(gate_vec[j], b[j], y[j]);  // with scale and dropout factor in it
+            if (live && p.y) store8<TS, VEC>(row_at<TS>(p.y, r, p.ld_y), c, y);
         }
         if (p.pre_norm) {
             normalise<VEC, BLOCK>(y, p.pre_norm, p.eps, p.inv_width, c, T, scratch, turn);
 #pragma unroll
             for (int j = 0; j < 8; ++j) y[j] = BIAS ? fmaf(y[j], pre[j], pre_bias[j]) : y[j] * pre[j];
-            if (live) store8<TD, VEC>((TD *)p.n + row * p.ld_n, c, y);
+            if (live) store8<TD, VEC>(row_at<TD>(p.n, r, p.ld_n), c, y);
         }
     }
 }
@@ -431,17 +478,30 @@ LP_DEVINL void norm_backward(float *v, float *q, const float *w, int kind, float
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = c.has(j) ? v[j] - mean : 0.f;
     }
-    float s[3] = {0.f, 0.f, 0.f};
+    float s[2] = {0.f, 0.f}, mean_u = 0.f;
+    if (layer) {
+        float x[3] = {0.f, 0.f, 0.f};
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const float u = w[j] * q[j];
-        s[0] = fmaf(v[j], v[j], s[0]);
-        s[1] = fmaf(u, v[j], s[1]);
-        s[2] += u;
+        for (int j = 0; j < 8; ++j) {
+            const float u = w[j] * q[j];
+            x[0] = fmaf(v[j], v[j], x[0]);
+            x[1] = fmaf(u, v[j], x[1]);
+            x[2] += u;
+        }
+        team_sum<3, BLOCK>(x, T, scratch, turn);
+        s[0] = x[0];
+        s[1] = x[1];
+        mean_u = x[2] * inv_width;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            s[0] = fmaf(v[j], v[j], s[0]);
+            s[1] = fmaf(w[j] * q[j], v[j], s[1]);
+        }
+        team_sum<2, BLOCK>(s, T, scratch, turn);
     }
-    team_sum<3, BLOCK>(s, T, scratch, turn);
-    const float r = 1.f / sqrtf(fmaf(s[0], inv_width, eps));
-    const float along = s[1] * inv_width * r, mean_u = layer ? s[2] * inv_width : 0.f;
+    const float r = inv_sqrt(fmaf(s[0], inv_width, eps));
+    const float along = s[1] * inv_width * r;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         v[j] *= r;
@@ -469,17 +529,19 @@ __global__ void __launch_bounds__(MAXT < 256 ? 256 : MAXT) residual_norm_grad_ke
     load_param8(p.post, c, 1.f, post);
     load_param8(p.gate_vec, c, 1.f, gate_vec);
     if (BIAS) load_param8(p.post_bias, c, 0.f, post_bias);
+    const float factor = p.scale * p.drop.factor;  // the factor is 1 where nothing is dropped
     float acc[RN_SUMS][8];
 #pragma unroll
     for (int k = 0; k < RN_SUMS; ++k)
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[k][j] = 0.f;
-    const int64_t stride = (int64_t)gridDim.x * teams, rounds = (p.rows + stride - 1) / stride;
+    const int stride = (int)gridDim.x * teams, rounds = (int)((p.rows + (int64_t)stride - 1) / stride);
     int64_t row = (int64_t)blockIdx.x * teams + (BLOCK ? 0 : threadIdx.x / T);
     RowPipe<VEC> pipe(pipe_smem, p.pieces, p.stages);
-    auto fetch = [&](int64_t r, int ahead) {
+    auto fetch = [&](int64_t at, int ahead) {
         const uint32_t st = pipe.stage(ahead);
-        const bool live = r < p.rows;
+        const bool live = at < p.rows;
+        const uint32_t r = live ? (uint32_t)at : 0u;
         if (p.pre_norm) {
             pipe.template copy<TD>(st, p.at_dn, p.dn, p.ld_dn, r, live, c);
             pipe.template copy<TS>(st, p.at_y, p.y, p.ld_y, r, live, c);
@@ -489,10 +551,11 @@ __global__ void __launch_bounds__(MAXT < 256 ? 256 : MAXT) residual_norm_grad_ke
         if (p.gate) pipe.template copy<TD>(st, p.at_gate, p.gate, p.ld_gate, r, live, c);
         pipe.commit();
     };
-    for (int i = 0; i < p.stages - 1; ++i) fetch(row + i * stride, i);
-    for (int64_t i = 0; i < rounds; ++i, row += stride, pipe.next()) {
+    for (int i = 0; i < p.stages - 1; ++i) fetch(row + (int64_t)i * stride, i);
+    for (int i = 0; i < rounds; ++i, row += stride, pipe.next()) {
         const bool live = row < p.rows;
-        fetch(row + (p.stages - 1) * stride, p.stages - 1);
+        fetch(row + (int64_t)(p.stages - 1) * stride, p.stages - 1);
+        const uint32_t r = live ? (uint32_t)row : 0u;
         const uint32_t keep = p.drop.threshold ? c.keep(p.drop, row, lane) : 0xffu;
         pipe.wait();
         const uint32_t st = pipe.stage(0);
@@ -501,33 +564,33 @@ __global__ void __launch_bounds__(MAXT < 256 ? 256 : MAXT) residual_norm_grad_ke
         for (int j = 0; j < 8; ++j) g[j] = 0.f;
         if (p.pre_norm) {
             float y[8];
-            pipe.template read<TD>(st, p.at_dn, p.dn, p.ld_dn, row, live, c, g);
-            pipe.template read<TS>(st, p.at_y, p.y, p.ld_y, row, live, c, y);
+            pipe.template read<TD>(st, p.at_dn, p.dn, p.ld_dn, r, live, c, g);
+            pipe.template read<TS>(st, p.at_y, p.y, p.ld_y, r, live, c, y);
             norm_backward<VEC, BLOCK, BIAS>(y, g, pre, p.pre_norm, p.eps, p.inv_width, c, T, scratch, turn, acc[0], acc[3]);
         }
         if (p.dy) {
             float d[8];
-            pipe.template read<TS>(st, p.at_dy, p.dy, p.ld_dy, row, live, c, d);
+            pipe.template read<TS>(st, p.at_dy, p.dy, p.ld_dy, r, live, c, d);
 #pragma unroll
             for (int j = 0; j < 8; ++j) g[j] += d[j];
         }
-        if (p.dx && live) store8<TS, VEC>((TS *)p.dx + row * p.ld_dx, c, g);
+        if (p.dx && live) store8<TS, VEC>(row_at<TS>(p.dx, r, p.ld_dx), c, g);
         if (!p.h) continue;
         // the branch: g -> gradient of h
         float m[8], z[8], q[8];
-        pipe.template read<TD>(st, p.at_h, p.h, p.ld_h, row, live, c, z);
+        pipe.template read<TD>(st, p.at_h, p.h, p.ld_h, r, live, c, z);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            g[j] = (keep >> j) & 1u ? p.scale * p.drop.factor * g[j] : 0.f;   // times gate: gradient of post(h)
+            g[j] = (keep >> j) & 1u ? factor * g[j] : 0.f;   // times gate: gradient of post(h)
             q[j] = g[j] * gate_vec[j];
         }
         if (p.gate) {
-            pipe.template read<TD>(st, p.at_gate, p.gate, p.ld_gate, row, live, c, m);
+            pipe.template read<TD>(st, p.at_gate, p.gate, p.ld_gate, r, live, c, m);
 #pragma unroll
             for (int j = 0; j < 8; ++j) q[j] *= m[j];
         }
         if (p.post_norm) norm_backward<VEC, BLOCK, BIAS>(z, q, post, p.post_norm, p.eps, p.inv_width, c, T, scratch, turn, acc[1], acc[4]);
-        if (p.dh && live) store8<TD, VEC>((TD *)p.dh + row * p.ld_dh, c, q);
+        if (p.dh && live) store8<TD, VEC>(row_at<TD>(p.dh, r, p.ld_dh), c, q);
         if (p.dgate || p.gate_vec) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) m[j] = (keep >> j) & 1u ? g[j] * (BIAS ? fmaf(z[j], post[j], post_bias[j]) : z[j] * post[j]) : 0.f;
@@ -535,7 +598,7 @@ __global__ void __launch_bounds__(MAXT < 256 ? 256 : MAXT) residual_norm_grad_ke
 #pragma unroll
                 for (int j = 0; j < 8; ++j) acc[2][j] += m[j];
             } else if (live) {
-                store8<TD, VEC>((TD *)p.dgate + row * p.ld_dgate, c, m);
+                store8<TD, VEC>(row_at<TD>(p.dgate, r, p.ld_dgate), c, m);
             }
         }
     }
@@ -598,7 +661,7 @@ template <typename T> static bool on_16_bytes(const void *p, int64_t ld) { retur
 template <typename T> static void dropout_launch(Exec &ex, DropoutParams &p)
 {
     p.team = std::min(DROP_THREADS, pow2_at_least(ceil_div64(p.width, 8)));
-    const int64_t blocks = std::min<int64_t>(ceil_div64(p.rows, DROP_THREADS / p.team), (int64_t)tc_sm_count() * 8);
+    const int64_t blocks = ceil_div64(p.rows, DROP_THREADS / p.team * DROP_ROWS);
     const bool vec = on_16_bytes<T>(p.in, p.ld_in) && on_16_bytes<T>(p.out, p.ld_out);
     if (vec) launch_dep(dropout_kernel<T, true>, dim3((unsigned)blocks), dim3(DROP_THREADS), 0, ex.st, p);
     else launch_dep(dropout_kernel<T, false>, dim3((unsigned)blocks), dim3(DROP_THREADS), 0, ex.st, p);
@@ -620,11 +683,11 @@ static ResidualGrid residual_grid(int64_t rows, int width, int threads_per_sm)
     return g;
 }
 
-template <typename TS, typename TD> static bool residual_vec(const ResidualParams &p)
+static bool residual_vec(const ResidualParams &p)
 {
-    return on_16_bytes<TS>(p.x, p.ld_x) && on_16_bytes<TD>(p.h, p.ld_h) && on_16_bytes<TS>(p.y, p.ld_y) && on_16_bytes<TD>(p.n, p.ld_n) &&
-           on_16_bytes<TS>(p.dy, p.ld_dy) && on_16_bytes<TD>(p.dn, p.ld_dn) && on_16_bytes<TS>(p.dx, p.ld_dx) && on_16_bytes<TD>(p.dh, p.ld_dh) &&
-           on_16_bytes<TD>(p.gate, p.ld_gate) && on_16_bytes<TD>(p.dgate, p.ld_dgate);
+    auto ok = [](const void *array, uint32_t ld) { return !array || (((uintptr_t)array | ld) & 15) == 0; };
+    return ok(p.x, p.ld_x) && ok(p.h, p.ld_h) && ok(p.y, p.ld_y) && ok(p.n, p.ld_n) && ok(p.dy, p.ld_dy) && ok(p.dn, p.ld_dn) && ok(p.dx, p.ld_dx) && ok(p.dh, p.ld_dh) &&
+           ok(p.gate, p.ld_gate) && ok(p.dgate, p.ld_dgate);
 }
 
 // pieces of the rows under way and how many rows: `room` bytes of shared memory per thread keep as many blocks resident as registers do
@@ -632,7 +695,7 @@ template <typename TS, typename TD> static size_t residual_pipe(ResidualParams &
 {
     const int s = PIPE_PIECES<TS>, d = PIPE_PIECES<TD>;
     int at = 0;
-    auto place = [&](const void *array, int pieces) { const int here = at; if (array) at += pieces; return here; };
+    auto place = [&](const void *array, int pieces) { const uint32_t here = (uint32_t)at * 16 * g.threads; if (array) at += pieces; return here; };
     p.at_x = place(p.x, s);
     p.at_dn = place(p.dn, d);
     p.at_y = place(p.dn ? p.y : nullptr, s);
@@ -663,7 +726,7 @@ template <typename TS, typename TD> static void residual_launch(Exec &ex, Residu
     p.team = g.team;
     const size_t smem = residual_pipe<TS, TD>(p, g, 256);
     const bool bias = p.pre_bias || p.post_bias;
-    if (residual_vec<TS, TD>(p)) {
+    if (residual_vec(p)) {
         if (bias) residual_dispatch<TS, TD, true, true>(ex, p, g, smem);
         else residual_dispatch<TS, TD, true, false>(ex, p, g, smem);
     } else {
@@ -685,7 +748,7 @@ template <typename TS, typename TD> static void residual_grad_launch(Exec &ex, R
     p.team = g.team;
     const size_t smem = residual_pipe<TS, TD>(p, g, 380);
     const bool bias = o.out[3] || o.out[4] || p.post_bias;
-    if (residual_vec<TS, TD>(p)) {
+    if (residual_vec(p)) {
         if (bias) residual_grad_dispatch<TS, TD, true, true>(ex, p, g, smem);
         else residual_grad_dispatch<TS, TD, true, false>(ex, p, g, smem);
     } else {

@@ -2478,7 +2478,10 @@ extern "C" lp_status lp_muon_step(lp_ctx *ctx, const lp_muon_desc *d, const lp_m
 static bool drop_args(double p, uint64_t seed, uint64_t step, int64_t row_base, DropArgs &d)
 {
     if (!(p >= 0.0 && p <= 1.0) || row_base < 0) return false;
-    d.key = make_uint2((uint32_t)seed, (uint32_t)(seed >> 32));
+    for (uint32_t i = 0; i < 10; ++i) {
+        d.key[2 * i] = (uint32_t)seed + i * 0x9E3779B9u;
+        d.key[2 * i + 1] = (uint32_t)(seed >> 32) + i * 0xBB67AE85u;
+    }
     d.step_lo = (uint32_t)step;
     d.threshold = (uint32_t)std::llround(65536.0 * p);
     d.factor = d.threshold < 65536u ? (float)(65536.0 / (65536.0 - d.threshold)) : 0.f;
@@ -2494,7 +2497,7 @@ extern "C" lp_status lp_dropout(lp_ctx *ctx, int32_t prec, int64_t rows, int32_t
 {
     if (!ctx) return LP_EINVAL;
     if (!prec_ok(prec)) return fail(ctx, LP_EINVAL, "lp_dropout: unknown precision");
-    if (rows < 0) return fail(ctx, LP_EINVAL, "lp_dropout: negative number of rows");
+    if (rows < 0 || rows >= (int64_t)1 << 31) return fail(ctx, LP_EINVAL, "lp_dropout: number of rows must be in [0, 2^31)");
     if (width < 1 || width > (1 << 20)) return fail(ctx, LP_EINVAL, "lp_dropout: width must be in [1, 2^20]");
     if (ld_in < width || ld_out < width) return fail(ctx, LP_EINVAL, "lp_dropout: a row pitch is smaller than the width");
     DropoutParams k{};
@@ -2503,7 +2506,7 @@ extern "C" lp_status lp_dropout(lp_ctx *ctx, int32_t prec, int64_t rows, int32_t
     if (!in || !out) return fail(ctx, LP_EINVAL, "lp_dropout: null array");
     if (misaligned(in, prec) || misaligned(out, prec)) return fail(ctx, LP_EINVAL, "lp_dropout: an array is not aligned to its elements");
     CK(cudaSetDevice(ctx->device));
-    k.in = in; k.out = out; k.rows = rows; k.width = width; k.ld_in = ld_in; k.ld_out = ld_out;
+    k.in = in; k.out = out; k.rows = (int)rows; k.width = width; k.ld_in = ld_in; k.ld_out = ld_out;
     if (prec == LP_FP32) dropout_launch<float>(ctx->ex, k);
     else dropout_launch<bf16>(ctx->ex, k);
     CK_LAUNCH();
@@ -2516,19 +2519,20 @@ static lp_status residual_params(lp_ctx *ctx, const std::string &who, const lp_r
     if (!d) return fail(ctx, LP_EINVAL, who + ": null descriptor");
     if (!prec_ok(d->prec) || !prec_ok(d->stream_prec)) return fail(ctx, LP_EINVAL, who + ": unknown precision");
     if (d->stream_prec == LP_BF16 && d->prec == LP_FP32) return fail(ctx, LP_EUNSUPPORTED, who + ": a BF16 residual sum takes BF16 blocks");
-    if (d->rows < 0) return fail(ctx, LP_EINVAL, who + ": negative number of rows");
+    if (d->rows < 0 || d->rows >= (int64_t)1 << 31) return fail(ctx, LP_EINVAL, who + ": number of rows must be in [0, 2^31)");
     if (d->width < 1 || d->width > RN_MAX_WIDTH) return fail(ctx, LP_EINVAL, who + ": width must be in [1, 8192]");
     for (int32_t kind : {d->pre_norm, d->post_norm})
         if (kind != LP_NORM_NONE && kind != LP_NORM_RMS && kind != LP_NORM_LAYER) return fail(ctx, LP_EINVAL, who + ": unknown norm");
     if (!(d->eps > 0.0) || !std::isfinite(d->eps) || !((float)d->eps > 0.f)) return fail(ctx, LP_EINVAL, who + ": eps must be positive and finite");
     if (!std::isfinite(d->scale)) return fail(ctx, LP_EINVAL, who + ": scale is not finite");
     if (!drop_args(d->p, d->seed, d->step, d->row_base, k.drop)) return fail(ctx, LP_EINVAL, who + ": p must be in [0, 1] and row_base not negative");
+    if (d->gate && d->ld_gate >= RN_MAX_PITCH) return fail(ctx, LP_EINVAL, who + ": a row pitch is 2^29 elements or more");
     if (d->gate && d->ld_gate != 0 && d->ld_gate < d->width) return fail(ctx, LP_EINVAL, who + ": a row pitch is smaller than the width");
     if (!branch && d->pre_norm == LP_NORM_NONE) return fail(ctx, LP_EINVAL, who + ": neither a block nor a norm");
     for (const float *v : {d->pre, d->pre_bias, d->post, d->post_bias})
         if (misaligned(v, LP_FP32)) return fail(ctx, LP_EINVAL, who + ": an array is not aligned to its elements");
     if (d->gate && misaligned(d->gate, d->ld_gate == 0 ? LP_FP32 : d->prec)) return fail(ctx, LP_EINVAL, who + ": an array is not aligned to its elements");
-    k.rows = d->rows;
+    k.rows = (int)d->rows;
     k.width = d->width;
     k.pre_norm = d->pre_norm;
     k.post_norm = branch ? d->post_norm : LP_NORM_NONE;
@@ -2539,7 +2543,7 @@ static lp_status residual_params(lp_ctx *ctx, const std::string &who, const lp_r
     if (k.post_norm) { k.post = d->post; k.post_bias = d->post_bias; }
     if (d->gate && branch) {
         if (d->ld_gate == 0) k.gate_vec = (const float *)d->gate;
-        else { k.gate = d->gate; k.ld_gate = d->ld_gate; }
+        else { k.gate = d->gate; k.ld_gate = (uint32_t)(d->ld_gate * (d->prec == LP_FP32 ? 4 : 2)); }
     }
     return LP_OK;
 }
@@ -2554,6 +2558,7 @@ static lp_status residual_arrays(lp_ctx *ctx, const std::string &who, int width,
     for (const ResidualArray &a : arrays) {
         if (!a.p) continue;
         if (a.ld < width) return fail(ctx, LP_EINVAL, who + ": a row pitch is smaller than the width");
+        if (a.ld >= RN_MAX_PITCH) return fail(ctx, LP_EINVAL, who + ": a row pitch is 2^29 elements or more");
         if (misaligned(a.p, a.prec)) return fail(ctx, LP_EINVAL, who + ": an array is not aligned to its elements");
     }
     return LP_OK;
@@ -2573,7 +2578,8 @@ extern "C" lp_status lp_residual_norm(lp_ctx *ctx, const lp_residual_desc *desc,
     if (!x || (n == nullptr) != (k.pre_norm == LP_NORM_NONE)) return fail(ctx, LP_EINVAL, "lp_residual_norm: x is missing, or n and pre_norm do not go together");
     if (!y && !n) return fail(ctx, LP_EINVAL, "lp_residual_norm: no result is wanted");
     CK(cudaSetDevice(ctx->device));
-    k.x = x; k.ld_x = ld_x; k.h = h; k.ld_h = ld_h; k.y = h ? y : nullptr; k.ld_y = ld_y; k.n = n; k.ld_n = ld_n;
+    const uint32_t bs = ps == LP_FP32 ? 4 : 2, bd = pd == LP_FP32 ? 4 : 2;
+    k.x = x; k.ld_x = (uint32_t)ld_x * bs; k.h = h; k.ld_h = (uint32_t)ld_h * bd; k.y = h ? y : nullptr; k.ld_y = (uint32_t)ld_y * bs; k.n = n; k.ld_n = (uint32_t)ld_n * bd;
     if (ps == LP_BF16) residual_launch<bf16, bf16>(ctx->ex, k);
     else if (pd == LP_BF16) residual_launch<float, bf16>(ctx->ex, k);
     else residual_launch<float, float>(ctx->ex, k);
@@ -2616,9 +2622,10 @@ extern "C" lp_status lp_residual_norm_grad(lp_ctx *ctx, const lp_residual_desc *
     uint8_t *ws = nullptr;
     s = op_workspace(ctx, sizeof(float) * (size_t)g.blocks * RN_SUMS * desc->width, &ws);
     if (s != LP_OK) return s;
-    k.dy = dy; k.ld_dy = ld_dy; k.dn = dn; k.ld_dn = ld_dn; k.y = (void *)y; k.ld_y = ld_y; k.h = h; k.ld_h = ld_h;
-    k.dx = dx; k.ld_dx = ld_dx; k.dh = dh; k.ld_dh = ld_dh; k.partial = (float *)ws;
-    if (!gate_sum) { k.dgate = dgate; k.ld_dgate = ld_dgate; }
+    const uint32_t bs = ps == LP_FP32 ? 4 : 2, bd = pd == LP_FP32 ? 4 : 2;
+    k.dy = dy; k.ld_dy = (uint32_t)ld_dy * bs; k.dn = dn; k.ld_dn = (uint32_t)ld_dn * bd; k.y = (void *)y; k.ld_y = (uint32_t)ld_y * bs; k.h = h; k.ld_h = (uint32_t)ld_h * bd;
+    k.dx = dx; k.ld_dx = (uint32_t)ld_dx * bs; k.dh = dh; k.ld_dh = (uint32_t)ld_dh * bd; k.partial = (float *)ws;
+    if (!gate_sum) { k.dgate = dgate; k.ld_dgate = (uint32_t)ld_dgate * bd; }
     if (ps == LP_BF16) residual_grad_launch<bf16, bf16>(ctx->ex, k, g, o, accumulate);
     else if (pd == LP_BF16) residual_grad_launch<float, bf16>(ctx->ex, k, g, o, accumulate);
     else residual_grad_launch<float, float>(ctx->ex, k, g, o, accumulate);
