@@ -466,7 +466,7 @@ lp_status lp_muon_step(lp_ctx *ctx, const lp_muon_desc *desc, const lp_matrix *m
  * The gradient is the same call on the gradient.  Results do not depend on how rows are split over calls (row_base), on pitches
  * or on types.  Dropped elements are zero whatever they held, NaN included.
  *   prec      : LP_FP32 or LP_BF16, of in and out
- *   in, out   : DEVICE [rows, width], row pitch ld_*; out may be in itself.  rows < 2^31, width <= 2^20
+ *   in, out   : DEVICE [rows, width], row pitch ld_*; out may be in itself.  rows < 2^31, width <= 2^20, pitches < 2^29
  *   p         : in [0, 1]
  * Does not synchronise. */
 lp_status lp_dropout(lp_ctx *ctx, int32_t prec, int64_t rows, int32_t width, const void *in, int64_t ld_in, double p, uint64_t seed, uint64_t step, int64_t row_base,
@@ -480,7 +480,7 @@ typedef struct {
     int32_t stream_prec;         /* of x, y, dy, dx; LP_BF16 only when prec is                              */
     int32_t prec;                /* of h, n, a gate per element, and their gradients                        */
     int32_t pre_norm, post_norm; /* LP_NORM_*                                                               */
-    double eps;                  /* > 0                                                                     */
+    double eps;                  /* >= 1e-37                                                                */
     double scale;                /* of the block's contribution                                             */
     double p;                    /* dropout, as in lp_dropout                                               */
     uint64_t seed, step;

@@ -119,6 +119,12 @@ template <typename T, bool VEC> LP_DEVINL void load8(const T *row, const Cols<VE
 template <typename T, bool VEC> LP_DEVINL void store8(T *row, const Cols<VEC> &c, const float *v)
 {
     if (c.full()) {
+        if (sizeof(T) == 4 && ((uintptr_t)row & 31) == 0) {  // a whole sector in one instruction
+            asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(row + c.base), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]),
+                         "f"(v[6]), "f"(v[7])
+                         : "memory");
+            return;
+        }
         constexpr int VN = Vec16<T>::N;
 #pragma unroll
         for (int k = 0; k < 8 / VN; ++k) {
@@ -132,11 +138,52 @@ template <typename T, bool VEC> LP_DEVINL void store8(T *row, const Cols<VEC> &c
             if (c.has(j)) row[c.at(j)] = from_f<T>(v[j]);
     }
 }
-// per-column parameter, `other` where there is none
+// Eight columns at once, two per instruction (sm_100 has FP32 multiplications and additions on pairs; one instruction per element made
+// these kernels wait for the scheduler rather than for HBM).
+LP_DEVINL float2 pair(const float *v, int k) { return make_float2(v[2 * k], v[2 * k + 1]); }
+LP_DEVINL void set_pair(float *v, int k, float2 x) { v[2 * k] = x.x; v[2 * k + 1] = x.y; }
+LP_DEVINL void mul8(float *v, const float *w)
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k) set_pair(v, k, __fmul2_rn(pair(v, k), pair(w, k)));
+}
+LP_DEVINL void scale8(float *v, float f)
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k) set_pair(v, k, __fmul2_rn(pair(v, k), make_float2(f, f)));
+}
+LP_DEVINL void add8(float *v, const float *w)
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k) set_pair(v, k, __fadd2_rn(pair(v, k), pair(w, k)));
+}
+LP_DEVINL void shift8(float *v, float f)
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k) set_pair(v, k, __fadd2_rn(pair(v, k), make_float2(f, f)));
+}
+LP_DEVINL void fma8(const float *a, const float *b, float *acc)  // acc += a b
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k) set_pair(acc, k, __ffma2_rn(pair(a, k), pair(b, k), pair(acc, k)));
+}
+LP_DEVINL float sum8(const float *v)
+{
+    const float2 a = __fadd2_rn(__fadd2_rn(pair(v, 0), pair(v, 1)), __fadd2_rn(pair(v, 2), pair(v, 3)));
+    return a.x + a.y;
+}
+LP_DEVINL float dot8(const float *a, const float *b)
+{
+    float2 x = __fmul2_rn(pair(a, 0), pair(b, 0));
+#pragma unroll
+    for (int k = 1; k < 4; ++k) x = __ffma2_rn(pair(a, k), pair(b, k), x);
+    return x.x + x.y;
+}
+// per-column parameter, `other` where there is none; zeros beyond the row, so that nothing there enters a sum
 template <bool VEC> LP_DEVINL void load_param8(const float *p, const Cols<VEC> &c, float other, float *v)
 {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = p && c.has(j) ? __ldg(p + c.at(j)) : other;
+    for (int j = 0; j < 8; ++j) v[j] = !c.has(j) ? 0.f : p ? __ldg(p + c.at(j)) : other;
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -148,53 +195,52 @@ struct DropoutParams {
     const void *in;
     void *out;
     int rows, width;
-    int64_t ld_in, ld_out;
-    int team;            // threads per row (a power of two, at most 256); wider rows are taken in pieces of 8 team columns
+    uint32_t ld_in, ld_out;  // bytes
+    int shift;               // 2^shift threads per row, at most 256; wider rows are taken in pieces of eight times as many columns
     DropArgs drop;
 };
 
 // A block takes DROP_ROWS rows per team, one after the other; the loads of all of them are under way while the bits are drawn.
 constexpr int DROP_ROWS = 4;
-template <typename T, bool VEC> __global__ void __launch_bounds__(DROP_THREADS) dropout_kernel(const DropoutParams p)
+template <typename T, bool VEC> __global__ void __launch_bounds__(DROP_THREADS, 4) dropout_kernel(const __grid_constant__ DropoutParams p)
 {
     LP_DEP_ENTER();
-    const int t = threadIdx.x & (p.team - 1), lane = threadIdx.x & 31, teams = DROP_THREADS / p.team;
-    const int64_t row0 = (int64_t)blockIdx.x * teams * DROP_ROWS + threadIdx.x / p.team;
+    const int team = 1 << p.shift, teams = DROP_THREADS >> p.shift, t = threadIdx.x & (team - 1), lane = threadIdx.x & 31;
+    const uint32_t row0 = blockIdx.x * (uint32_t)(teams * DROP_ROWS) + (threadIdx.x >> p.shift);  // rows < 2^31: no overflow
     const bool drops = p.drop.threshold != 0;
     if (VEC) {
         constexpr int VN = Vec16<T>::N, NV = 8 / VN;
-        for (int c0 = 8 * t; c0 < p.width; c0 += 8 * p.team) {
-            const T *in = (const T *)p.in + row0 * p.ld_in + c0;
-            T *out = (T *)p.out + row0 * p.ld_out + c0;
+        for (int c0 = 8 * t; c0 < p.width; c0 += 8 * team) {
+            const char *in = (const char *)p.in + c0 * sizeof(T);
+            char *out = (char *)p.out + c0 * sizeof(T);
             if (c0 + 8 <= p.width) {
                 Vec16<T> x[DROP_ROWS][NV];
 #pragma unroll
                 for (int i = 0; i < DROP_ROWS; ++i)
-                    if (row0 + i * teams < p.rows)
+                    if (row0 + i * teams < (uint32_t)p.rows)
 #pragma unroll
-                        for (int k = 0; k < NV; ++k) x[i][k].load_once(in + (int64_t)i * teams * p.ld_in + k * VN);
+                        for (int k = 0; k < NV; ++k) x[i][k].load_once((const T *)(in + (uint64_t)(row0 + i * teams) * p.ld_in) + k * VN);
 #pragma unroll
                 for (int i = 0; i < DROP_ROWS; ++i) {
-                    const int64_t row = row0 + i * teams;
-                    if (row >= p.rows) break;
+                    const uint32_t row = row0 + i * teams;
+                    if (row >= (uint32_t)p.rows) break;
                     float v[8];
 #pragma unroll
                     for (int k = 0; k < NV; ++k) x[i][k].to_float(v + k * VN);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] *= p.drop.factor;
+                    scale8(v, p.drop.factor);
                     if (drops) drop8(p.drop, drop_words(p.drop, row, (uint32_t)c0 >> 3), v);
 #pragma unroll
                     for (int k = 0; k < NV; ++k) {
                         x[i][k].from_float(v + k * VN);
-                        x[i][k].store(out + (int64_t)i * teams * p.ld_out + k * VN);
+                        x[i][k].store((T *)(out + (uint64_t)row * p.ld_out) + k * VN);
                     }
                 }
             } else {  // the end of a row whose width is no multiple of eight
-                for (int i = 0; i < DROP_ROWS && row0 + i * teams < p.rows; ++i) {
-                    const uint32_t keep = drops ? drop_keep8(p.drop, drop_words(p.drop, row0 + i * teams, (uint32_t)c0 >> 3)) : 0xffu;
+                for (int i = 0; i < DROP_ROWS && row0 + i * teams < (uint32_t)p.rows; ++i) {
+                    const uint32_t row = row0 + i * teams, keep = drops ? drop_keep8(p.drop, drop_words(p.drop, row, (uint32_t)c0 >> 3)) : 0xffu;
                     for (int j = 0; c0 + j < p.width; ++j) {
-                        const float x = to_f<T>(in[(int64_t)i * teams * p.ld_in + j]);
-                        out[(int64_t)i * teams * p.ld_out + j] = from_f<T>((keep >> j) & 1u ? x * p.drop.factor : 0.f);
+                        const float x = to_f<T>(((const T *)(in + (uint64_t)row * p.ld_in))[j]);
+                        ((T *)(out + (uint64_t)row * p.ld_out))[j] = from_f<T>((keep >> j) & 1u ? x * p.drop.factor : 0.f);
                     }
                 }
             }
@@ -202,18 +248,18 @@ template <typename T, bool VEC> __global__ void __launch_bounds__(DROP_THREADS) 
         return;
     }
     for (int i = 0; i < DROP_ROWS; ++i) {
-        const int64_t row = row0 + i * teams;
-        for (int c0 = 0; c0 < p.width; c0 += 8 * p.team) {
-            Cols<VEC> c(t, p.team, p.width);
+        const uint32_t row = row0 + i * teams;
+        for (int c0 = 0; c0 < p.width; c0 += 8 * team) {
+            Cols<VEC> c(t, team, p.width);
             c.base += c0;
             float v[8];
-            if (row < p.rows) load8<T, VEC>((const T *)p.in + row * p.ld_in, c, v);
+            if (row < (uint32_t)p.rows) load8<T, VEC>((const T *)((const char *)p.in + (uint64_t)row * p.ld_in), c, v);
             // the whole warp takes part in handing the bits round, rows that are not there too
             const uint32_t keep = drops ? c.keep(p.drop, row, lane) : 0xffu;
-            if (row < p.rows) {
+            if (row < (uint32_t)p.rows) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] = (keep >> j) & 1u ? v[j] * p.drop.factor : 0.f;
-                store8<T, VEC>((T *)p.out + row * p.ld_out, c, v);
+                store8<T, VEC>((T *)((char *)p.out + (uint64_t)row * p.ld_out), c, v);
             }
         }
     }
@@ -225,6 +271,13 @@ template <typename T, bool VEC> __global__ void __launch_bounds__(DROP_THREADS) 
 constexpr int RN_MAX_WIDTH = 8192;  // eight columns for each of 1024 threads
 constexpr int64_t RN_MAX_PITCH = (int64_t)1 << 29;  // elements: a pitch in bytes fits 32 bits, and a row's offset is one multiplication
 constexpr int RN_SUMS = 5;          // column sums of the backward pass: dpre, dpost, dgate, dpre_bias, dpost_bias
+
+struct PipeArray {        // of a kernel's arrays
+    const char *at;
+    uint32_t ld;          // bytes between rows
+    uint32_t row_bytes;   // VEC: of a row
+    uint32_t offset;      // in a stage
+};
 
 struct ResidualParams {
     int rows;
@@ -241,81 +294,147 @@ struct ResidualParams {
     void *y, *n, *dx, *dh, *dgate;
     uint32_t ld_x, ld_h, ld_y, ld_n, ld_dy, ld_dn, ld_dx, ld_dh, ld_dgate;
     float *partial;            // [gridDim.x][RN_SUMS][width] column sums of each block
-    int pieces, stages;        // of the rows under way: 16-byte pieces per thread and row, rows
-    uint32_t at_x, at_h, at_gate, at_y, at_dn, at_dy;  // bytes to each array's pieces
+    // rows under way: how many, bytes of a unit's row of all arrays (VEC) or between rows of all threads' pieces
+    int stages;
+    uint32_t stage_bytes;
+    uint32_t copy_bytes;       // VEC: of one row of all arrays
+    int unit_teams;            // teams of a unit
+    PipeArray pipe[5];         // forward: x, h, gate; backward: dn, y, dy, h, gate
+    int *err;
+    unsigned long long wait_ns;
 };
 
-// Rows on their way into shared memory: each thread copies its own eight columns of the arrays a row needs (16 bytes at a time;
-// FP32 rows of any alignment 4 bytes at a time) several rows ahead and reads back only what it copied itself, so no barrier is
-// needed, and what is under way takes no registers.  What lies beyond the row or the last row arrives as zeros.
-// BF16 rows that do not start on 16 bytes cannot be copied this way and are loaded when they are needed.
-template <typename T> constexpr int PIPE_PIECES = sizeof(T) == 4 ? 2 : 1;  // of 16 bytes
-LP_DEVINL void copy_async_16(uint32_t dst, const void *src, int bytes)
+
+// Rows on their way into shared memory, several ahead of the one that is worked on, so that what is under way takes no registers.
+//   VEC        one bulk copy per row and array, counted on a barrier of the unit (the warp, or the block of a large team) and row: two
+//              instructions per row where copies by every thread took about 150 and, of FP32, asked for every sector twice
+//   otherwise  each thread copies its own eight FP32 columns, 4 bytes at a time, and reads back only what it copied itself;
+//              BF16 rows that do not start on 16 bytes cannot be copied this way and are loaded when they are needed
+LP_DEVINL void copy_row(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
 {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 LP_DEVINL void copy_async_4(uint32_t dst, const void *src, int bytes)
 {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
-template <bool VEC> struct RowPipe {
-    uint32_t base;       // of this thread's pieces
-    uint32_t piece, stage_bytes;
-    int stages, head;    // the stage that is read next
-    LP_DEVINL RowPipe(uint8_t *smem, int pieces, int stages_)
-        : base(smem_u32(smem) + threadIdx.x * 16), piece(blockDim.x * 16), stage_bytes(pieces * blockDim.x * 16), stages(stages_), head(0) {}
-    LP_DEVINL uint32_t stage(int ahead) const
+template <bool VEC, bool BLOCK> struct RowPipe {
+    const ResidualParams &p;
+    uint32_t first, in, out, end;   // of the unit (VEC) or thread: where the next row goes, where the oldest lies
+    uint32_t bar_in, bar_out, bars; // VEC: the same of the barriers
+    uint32_t piece, parity;
+    bool ok;
+    LP_DEVINL RowPipe(const ResidualParams &p_, uint8_t *smem) : p(p_), parity(0), ok(true)
     {
-        int s = head + ahead;
-        if (s >= stages) s -= stages;
-        return base + s * stage_bytes;
-    }
-    // `at`: bytes from the start of a stage to the array's pieces; `ld`: bytes between rows.  row: of an array's row that is there, live: false for zeros
-    template <typename T> LP_DEVINL void copy(uint32_t st, uint32_t at, const void *array, uint32_t ld, uint32_t row, bool live, const Cols<VEC> &c) const
-    {
-        if (!VEC && sizeof(T) == 2) return;
-        const char *src = (const char *)array + (uint64_t)row * ld;
         if (VEC) {
-#pragma unroll
-            for (int k = 0; k < PIPE_PIECES<T>; ++k) {
-                const int col = c.base + k * (16 / (int)sizeof(T)), have = min(max(c.width - col, 0) * (int)sizeof(T), 16);
-                copy_async_16(st + at + k * piece, src + (have ? col * (int)sizeof(T) : 0), live ? have : 0);
+            const uint32_t unit = BLOCK ? 0 : threadIdx.x >> 5, units = BLOCK ? 1 : blockDim.x >> 5;
+            first = smem_u32(smem) + unit * p.stages * p.stage_bytes;
+            bars = smem_u32(smem) + units * p.stages * p.stage_bytes + unit * p.stages * 8;
+            bar_in = bar_out = bars;
+            if (BLOCK ? threadIdx.x == 0 : (threadIdx.x & 31) == 0) {
+                for (int i = 0; i < p.stages; ++i) mbar_init(bars + 8 * i, 1);
+                fence_barrier_init();
+                fence_async_proxy();
             }
+            sync();
+        } else {
+            first = smem_u32(smem) + threadIdx.x * 16;
+            piece = blockDim.x * 16;
+        }
+        in = out = first;
+        end = first + p.stages * p.stage_bytes;
+    }
+    // the threads that share the rows of a stage
+    LP_DEVINL void sync() const
+    {
+        if (BLOCK) __syncthreads();
+        else __syncwarp();
+    }
+    // rows first_row .. of the unit's teams (this thread's is `row`), where they are below p.rows
+    template <int N> LP_DEVINL void fetch(const PipeArray (&arrays)[N], int64_t row, int t, int team, const Cols<VEC> &c)
+    {
+        const bool live = row < p.rows;
+        if (VEC) {
+            if (t == 0) {
+                // the unit's first thread says how much is on its way, the first of every team sends its row's share
+                if (team == 0) mbar_expect_tx(bar_in, p.copy_bytes * (uint32_t)min(max((int64_t)p.rows - row, (int64_t)0), (int64_t)p.unit_teams));
+                if (live)
+#pragma unroll
+                    for (int k = 0; k < N; ++k)
+                        if (arrays[k].at) copy_row(in + arrays[k].offset + team * arrays[k].row_bytes, arrays[k].at + (uint64_t)(uint32_t)row * arrays[k].ld, arrays[k].row_bytes, bar_in);
+            }
+            bar_in += 8;
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const bool has = c.has(j);
-                copy_async_4(st + at + (j >> 2) * piece + (j & 3) * 4, src + (has ? c.at(j) * (int)sizeof(T) : 0), live && has ? 4 : 0);
-            }
+            for (int k = 0; k < N; ++k)
+                if (arrays[k].at && arrays[k].row_bytes) {
+                    const char *src = arrays[k].at + (uint64_t)(live ? (uint32_t)row : 0u) * arrays[k].ld;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const bool has = c.has(j);
+                        copy_async_4(in + arrays[k].offset + (j >> 2) * piece + (j & 3) * 4, src + (has ? c.at(j) * 4 : 0), live && has ? 4 : 0);
+                    }
+                }
+            asm volatile("cp.async.commit_group;" ::: "memory");
         }
+        in += p.stage_bytes;
+        if (in == end) { in = first; bar_in = bars; }
     }
-    template <typename T> LP_DEVINL void read(uint32_t st, uint32_t at, const void *array, uint32_t ld, uint32_t row, bool live, const Cols<VEC> &c, float *v) const
+    template <typename T> LP_DEVINL void read(const PipeArray &a, int64_t row, int team, const Cols<VEC> &c, float *v) const
     {
+        const bool live = row < p.rows;
+        constexpr int VN = Vec16<T>::N;
         if (!VEC && sizeof(T) == 2) {
-            const T *src = (const T *)((const char *)array + (uint64_t)row * ld);
+            const T *src = (const T *)(a.at + (uint64_t)(live ? (uint32_t)row : 0u) * a.ld);
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = live && c.has(j) ? to_f<T>(src[c.at(j)]) : 0.f;
             return;
         }
 #pragma unroll
-        for (int k = 0; k < PIPE_PIECES<T>; ++k) {
+        for (int k = 0; k < 8 / VN; ++k) {
             Vec16<T> x;
-            uint32_t w[4];
-            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(st + at + k * piece) : "memory");
-            memcpy(&x.v, w, 16);
-            x.to_float(v + k * Vec16<T>::N);
+            x.zero();
+            if (!VEC || (live && c.base + k * VN < c.width)) {
+                uint32_t w[4];
+                const uint32_t src = out + a.offset + (VEC ? team * a.row_bytes + (c.base + k * VN) * (uint32_t)sizeof(T) : k * piece);
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(src) : "memory");
+                memcpy(&x.v, w, 16);
+            }
+            x.to_float(v + k * VN);
         }
     }
-    LP_DEVINL void commit() const { asm volatile("cp.async.commit_group;" ::: "memory"); }
-    // the oldest row has arrived
-    LP_DEVINL void wait() const
+    // the oldest row has arrived; false when the wait ran out (in all threads of the unit)
+    LP_DEVINL bool wait()
     {
-        if (stages == 1) asm volatile("cp.async.wait_group 0;" ::: "memory");
-        else if (stages == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
-        else if (stages == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
+        if (VEC) {
+            ok = mbar_wait(bar_out, parity, p.wait_ns);
+            ok = BLOCK ? __syncthreads_and(ok) != 0 : __all_sync(0xffffffffu, ok) != 0;
+            return ok;
+        }
+        if (p.stages == 1) asm volatile("cp.async.wait_group 0;" ::: "memory");
+        else if (p.stages == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+        else if (p.stages == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
         else asm volatile("cp.async.wait_group 3;" ::: "memory");
+        return true;
     }
-    LP_DEVINL void next() { head = head + 1 == stages ? 0 : head + 1; }
+    // the oldest row's place is free again
+    LP_DEVINL void next()
+    {
+        if (VEC) sync();
+        out += p.stage_bytes;
+        bar_out += 8;
+        if (out == end) { out = first; bar_out = bars; parity ^= 1; }
+    }
+    // after a wait that ran out: what is under way lands before the block goes (rows that were waited for have)
+    LP_DEVINL void drain(int ahead)
+    {
+        if (VEC) {
+            for (int i = 0; i < ahead; ++i) {
+                mbar_wait(bar_out, parity, p.wait_ns);
+                next();
+            }
+        }
+    }
 };
 
 template <typename T> LP_DEVINL T *row_at(void *array, uint32_t row, uint32_t ld) { return (T *)((char *)array + (uint64_t)row * ld); }
@@ -324,7 +443,8 @@ template <typename T> LP_DEVINL T *row_at(void *array, uint32_t row, uint32_t ld
 // division took 35 instructions)
 LP_DEVINL float inv_sqrt(float x)
 {
-    const float r = rsqrtf(x);
+    float r;
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return fmaf(r * fmaf(-x * r, r, 1.f), 0.5f, r);
 }
 
@@ -363,26 +483,26 @@ template <int K, bool BLOCK> LP_DEVINL void team_sum(float (&v)[K], int T, float
         for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
 }
 
-// v becomes z (the normalised row); returns r
-template <bool VEC, bool BLOCK> LP_DEVINL float normalise(float *v, int kind, float eps, float inv_width, const Cols<VEC> &c, int T, float *scratch, int &turn)
+// v less its mean over the row
+template <bool VEC, bool BLOCK> LP_DEVINL void centre(float *v, float inv_width, const Cols<VEC> &c, int T, float *scratch, int &turn)
 {
-    if (kind == LP_NORM_LAYER) {
-        float s[1] = {0.f};
+    float s[1] = {sum8(v)};
+    team_sum<1, BLOCK>(s, T, scratch, turn);
+    shift8(v, -s[0] * inv_width);
+    if (!c.full())
 #pragma unroll
-        for (int j = 0; j < 8; ++j) s[0] += v[j];
-        team_sum<1, BLOCK>(s, T, scratch, turn);
-        const float mean = s[0] * inv_width;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = c.has(j) ? v[j] - mean : 0.f;
-    }
-    float q[1] = {0.f};
-#pragma unroll
-    for (int j = 0; j < 8; ++j) q[0] = fmaf(v[j], v[j], q[0]);
+        for (int j = 0; j < 8; ++j) v[j] = c.has(j) ? v[j] : 0.f;
+}
+
+// v becomes w times the normalised row (w: the weight)
+template <bool VEC, bool BLOCK>
+LP_DEVINL void normalise(float *v, const float *w, int kind, float eps, float inv_width, const Cols<VEC> &c, int T, float *scratch, int &turn)
+{
+    if (kind == LP_NORM_LAYER) centre<VEC, BLOCK>(v, inv_width, c, T, scratch, turn);
+    float q[1] = {dot8(v, v)};
     team_sum<1, BLOCK>(q, T, scratch, turn);
-    const float r = inv_sqrt(fmaf(q[0], inv_width, eps));
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] *= r;
-    return r;
+    scale8(v, inv_sqrt(fmaf(q[0], inv_width, eps)));
+    mul8(v, w);
 }
 
 // MAXT: the largest team of the variant, 32 (parts of warps), 256 or 1024 (whole blocks).  BIAS: norms with a bias
@@ -408,33 +528,23 @@ template <typename TS, typename TD, bool VEC, int MAXT, bool BIAS> __global__ vo
     }
     const int stride = (int)gridDim.x * teams, rounds = (int)((p.rows + (int64_t)stride - 1) / stride);
     int64_t row = (int64_t)blockIdx.x * teams + (BLOCK ? 0 : threadIdx.x / T);
-    RowPipe<VEC> pipe(pipe_smem, p.pieces, p.stages);
-    auto fetch = [&](int64_t at, int ahead) {
-        const uint32_t st = pipe.stage(ahead);
-        const bool live = at < p.rows;
-        const uint32_t r = live ? (uint32_t)at : 0u;
-        pipe.template copy<TS>(st, p.at_x, p.x, p.ld_x, r, live, c);
-        if (p.h) pipe.template copy<TD>(st, p.at_h, p.h, p.ld_h, r, live, c);
-        if (p.gate) pipe.template copy<TD>(st, p.at_gate, p.gate, p.ld_gate, r, live, c);
-        pipe.commit();
-    };
-    for (int i = 0; i < p.stages - 1; ++i) fetch(row + (int64_t)i * stride, i);
-    for (int i = 0; i < rounds; ++i, row += stride, pipe.next()) {
+    RowPipe<VEC, BLOCK> pipe(p, pipe_smem);
+    const PipeArray arrays[3] = {p.pipe[0], p.pipe[1], p.pipe[2]};
+    const int team = BLOCK ? 0 : lane / T;
+    for (int i = 0; i < p.stages; ++i) pipe.fetch(arrays, row + (int64_t)i * stride, t, team, c);
+    for (int i = 0; i < rounds; ++i, row += stride) {
         const bool live = row < p.rows;  // of a warp's teams some may be past the last row; they take part in the sums of the others
-        fetch(row + (int64_t)(p.stages - 1) * stride, p.stages - 1);
         const uint32_t r = live ? (uint32_t)row : 0u;
         uint4 bits;
         if (VEC && p.drop.threshold) bits = drop_words(p.drop, row, (uint32_t)c.base >> 3);
-        pipe.wait();
-        const uint32_t st = pipe.stage(0);
+        if (!pipe.wait()) break;
         float y[8], b[8];
-        pipe.template read<TS>(st, p.at_x, p.x, p.ld_x, r, live, c, y);
+        pipe.template read<TS>(arrays[0], row, team, c, y);
         if (p.h) {
-            pipe.template read<TD>(st, p.at_h, p.h, p.ld_h, r, live, c, b);
+            pipe.template read<TD>(arrays[1], row, team, c, b);
             if (p.post_norm) {
-                normalise<VEC, BLOCK>(b, p.post_norm, p.eps, p.inv_width, c, T, scratch, turn);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) b[j] = BIAS ? fmaf(b[j], post[j], post_bias[j]) : b[j] * post[j];
+                normalise<VEC, BLOCK>(b, post, p.post_norm, p.eps, p.inv_width, c, T, scratch, turn);
+                if (BIAS) add8(b, post_bias);
             }
             if (p.drop.threshold) {
                 if (VEC) {
@@ -447,74 +557,59 @@ template <typename TS, typename TD, bool VEC, int MAXT, bool BIAS> __global__ vo
             }
             if (p.gate) {
                 float g[8];
-                pipe.template read<TD>(st, p.at_gate, p.gate, p.ld_gate, r, live, c, g);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) b[j] *= g[j];
+                pipe.template read<TD>(arrays[2], row, team, c, g);
+                mul8(b, g);
             }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = fmaf(gate_vec[j], b[j], y[j]);  // with scale and dropout factor in it
+            fma8(gate_vec, b, y);  // scale and dropout factor are in it
             if (live && p.y) store8<TS, VEC>(row_at<TS>(p.y, r, p.ld_y), c, y);
         }
         if (p.pre_norm) {
-            normalise<VEC, BLOCK>(y, p.pre_norm, p.eps, p.inv_width, c, T, scratch, turn);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = BIAS ? fmaf(y[j], pre[j], pre_bias[j]) : y[j] * pre[j];
+            normalise<VEC, BLOCK>(y, pre, p.pre_norm, p.eps, p.inv_width, c, T, scratch, turn);
+            if (BIAS) add8(y, pre_bias);
             if (live) store8<TD, VEC>(row_at<TD>(p.n, r, p.ld_n), c, y);
         }
+        pipe.next();
+        pipe.fetch(arrays, row + (int64_t)p.stages * stride, t, team, c);
     }
+    if (!pipe.ok && threadIdx.x % 32 == 0) atomicExch(p.err, 8);
+    pipe.drain(p.stages);
 }
 
 // v: the row, becomes z.  q: gradient of the norm's output, becomes that of its input.  dw, db: column sums.
 template <bool VEC, bool BLOCK, bool BIAS>
 LP_DEVINL void norm_backward(float *v, float *q, const float *w, int kind, float eps, float inv_width, const Cols<VEC> &c, int T, float *scratch, int &turn, float *dw, float *db)
 {
-    const bool layer = kind == LP_NORM_LAYER;
-    if (layer) {
-        float s[1] = {0.f};
+    float u[8], r, along, mean_u = 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) s[0] += v[j];
-        team_sum<1, BLOCK>(s, T, scratch, turn);
-        const float mean = s[0] * inv_width;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = c.has(j) ? v[j] - mean : 0.f;
-    }
-    float s[2] = {0.f, 0.f}, mean_u = 0.f;
-    if (layer) {
-        float x[3] = {0.f, 0.f, 0.f};
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float u = w[j] * q[j];
-            x[0] = fmaf(v[j], v[j], x[0]);
-            x[1] = fmaf(u, v[j], x[1]);
-            x[2] += u;
-        }
-        team_sum<3, BLOCK>(x, T, scratch, turn);
-        s[0] = x[0];
-        s[1] = x[1];
-        mean_u = x[2] * inv_width;
+    for (int j = 0; j < 8; ++j) u[j] = w[j];
+    mul8(u, q);
+    if (kind == LP_NORM_LAYER) {
+        centre<VEC, BLOCK>(v, inv_width, c, T, scratch, turn);
+        float s[3] = {dot8(v, v), dot8(u, v), sum8(u)};
+        team_sum<3, BLOCK>(s, T, scratch, turn);
+        r = inv_sqrt(fmaf(s[0], inv_width, eps));
+        along = s[1] * inv_width * r;
+        mean_u = s[2] * inv_width;
     } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            s[0] = fmaf(v[j], v[j], s[0]);
-            s[1] = fmaf(w[j] * q[j], v[j], s[1]);
-        }
+        float s[2] = {dot8(v, v), dot8(u, v)};
         team_sum<2, BLOCK>(s, T, scratch, turn);
+        r = inv_sqrt(fmaf(s[0], inv_width, eps));
+        along = s[1] * inv_width * r;
     }
-    const float r = inv_sqrt(fmaf(s[0], inv_width, eps));
-    const float along = s[1] * inv_width * r;
+    scale8(v, r);
+    fma8(q, v, dw);
+    if (BIAS) add8(db, q);
+    // r (u - z along - mean(u))
+    const float2 minus = make_float2(-along * r, -along * r), rr = make_float2(r, r);
+    const float off = -mean_u * r;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        v[j] *= r;
-        dw[j] = fmaf(q[j], v[j], dw[j]);
-        if (BIAS) db[j] += q[j];
-        q[j] = r * (fmaf(-v[j], along, w[j] * q[j]) - mean_u);
-    }
+    for (int k = 0; k < 4; ++k) set_pair(q, k, __ffma2_rn(pair(v, k), minus, __ffma2_rn(pair(u, k), rr, make_float2(off, off))));
 }
 
 // BIAS: column sums of the biases too (sixteen more registers).  MAXT as above, and 256: blocks of 1024 threads leave 64 registers
 // for each, which the column sums do not fit into.
 template <typename TS, typename TD, bool VEC, int MAXT, bool BIAS>
-__global__ void __launch_bounds__(MAXT < 256 ? 256 : MAXT) residual_norm_grad_kernel(const __grid_constant__ ResidualParams p)
+__global__ void __launch_bounds__(MAXT < 256 ? 256 : MAXT, MAXT > 256 ? 1 : 2) residual_norm_grad_kernel(const __grid_constant__ ResidualParams p)
 {
     LP_DEP_ENTER();
     constexpr bool BLOCK = MAXT > 32;
@@ -537,71 +632,70 @@ __global__ void __launch_bounds__(MAXT < 256 ? 256 : MAXT) residual_norm_grad_ke
         for (int j = 0; j < 8; ++j) acc[k][j] = 0.f;
     const int stride = (int)gridDim.x * teams, rounds = (int)((p.rows + (int64_t)stride - 1) / stride);
     int64_t row = (int64_t)blockIdx.x * teams + (BLOCK ? 0 : threadIdx.x / T);
-    RowPipe<VEC> pipe(pipe_smem, p.pieces, p.stages);
-    auto fetch = [&](int64_t at, int ahead) {
-        const uint32_t st = pipe.stage(ahead);
-        const bool live = at < p.rows;
-        const uint32_t r = live ? (uint32_t)at : 0u;
-        if (p.pre_norm) {
-            pipe.template copy<TD>(st, p.at_dn, p.dn, p.ld_dn, r, live, c);
-            pipe.template copy<TS>(st, p.at_y, p.y, p.ld_y, r, live, c);
-        }
-        if (p.dy) pipe.template copy<TS>(st, p.at_dy, p.dy, p.ld_dy, r, live, c);
-        if (p.h) pipe.template copy<TD>(st, p.at_h, p.h, p.ld_h, r, live, c);
-        if (p.gate) pipe.template copy<TD>(st, p.at_gate, p.gate, p.ld_gate, r, live, c);
-        pipe.commit();
-    };
-    for (int i = 0; i < p.stages - 1; ++i) fetch(row + (int64_t)i * stride, i);
-    for (int i = 0; i < rounds; ++i, row += stride, pipe.next()) {
+    RowPipe<VEC, BLOCK> pipe(p, pipe_smem);
+    const PipeArray arrays[5] = {p.pipe[0], p.pipe[1], p.pipe[2], p.pipe[3], p.pipe[4]};
+    const int team = BLOCK ? 0 : lane / T;
+    for (int i = 0; i < p.stages; ++i) pipe.fetch(arrays, row + (int64_t)i * stride, t, team, c);
+    for (int i = 0; i < rounds; ++i, row += stride) {
         const bool live = row < p.rows;
-        fetch(row + (int64_t)(p.stages - 1) * stride, p.stages - 1);
         const uint32_t r = live ? (uint32_t)row : 0u;
         const uint32_t keep = p.drop.threshold ? c.keep(p.drop, row, lane) : 0xffu;
-        pipe.wait();
-        const uint32_t st = pipe.stage(0);
+        if (!pipe.wait()) break;
         float g[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) g[j] = 0.f;
         if (p.pre_norm) {
             float y[8];
-            pipe.template read<TD>(st, p.at_dn, p.dn, p.ld_dn, r, live, c, g);
-            pipe.template read<TS>(st, p.at_y, p.y, p.ld_y, r, live, c, y);
+            pipe.template read<TD>(arrays[0], row, team, c, g);
+            pipe.template read<TS>(arrays[1], row, team, c, y);
             norm_backward<VEC, BLOCK, BIAS>(y, g, pre, p.pre_norm, p.eps, p.inv_width, c, T, scratch, turn, acc[0], acc[3]);
         }
         if (p.dy) {
             float d[8];
-            pipe.template read<TS>(st, p.at_dy, p.dy, p.ld_dy, r, live, c, d);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) g[j] += d[j];
+            pipe.template read<TS>(arrays[2], row, team, c, d);
+            add8(g, d);
         }
         if (p.dx && live) store8<TS, VEC>(row_at<TS>(p.dx, r, p.ld_dx), c, g);
-        if (!p.h) continue;
-        // the branch: g -> gradient of h
-        float m[8], z[8], q[8];
-        pipe.template read<TD>(st, p.at_h, p.h, p.ld_h, r, live, c, z);
+        if (p.h) {  // the branch: g -> gradient of h
+            float m[8], z[8], q[8];
+            pipe.template read<TD>(arrays[3], row, team, c, z);
+            scale8(g, factor);
+            if (p.drop.threshold)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            g[j] = (keep >> j) & 1u ? factor * g[j] : 0.f;   // times gate: gradient of post(h)
-            q[j] = g[j] * gate_vec[j];
-        }
-        if (p.gate) {
-            pipe.template read<TD>(st, p.at_gate, p.gate, p.ld_gate, r, live, c, m);
+                for (int j = 0; j < 8; ++j) g[j] = (keep >> j) & 1u ? g[j] : 0.f;   // times gate: gradient of post(h)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) q[j] *= m[j];
-        }
-        if (p.post_norm) norm_backward<VEC, BLOCK, BIAS>(z, q, post, p.post_norm, p.eps, p.inv_width, c, T, scratch, turn, acc[1], acc[4]);
-        if (p.dh && live) store8<TD, VEC>(row_at<TD>(p.dh, r, p.ld_dh), c, q);
-        if (p.dgate || p.gate_vec) {
+            for (int j = 0; j < 8; ++j) q[j] = g[j];
+            mul8(q, gate_vec);
+            if (p.gate) {
+                pipe.template read<TD>(arrays[4], row, team, c, m);
+                mul8(q, m);
+            }
+            if (p.post_norm) norm_backward<VEC, BLOCK, BIAS>(z, q, post, p.post_norm, p.eps, p.inv_width, c, T, scratch, turn, acc[1], acc[4]);
+            if (p.dh && live) store8<TD, VEC>(row_at<TD>(p.dh, r, p.ld_dh), c, q);
+            if (p.dgate || p.gate_vec) {
+                // gradient of the gate: g post(h), where nothing was dropped
+                if (BIAS) {
+                    mul8(z, post);
+                    add8(z, post_bias);
+                }
+                if (p.drop.threshold)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) m[j] = (keep >> j) & 1u ? g[j] * (BIAS ? fmaf(z[j], post[j], post_bias[j]) : z[j] * post[j]) : 0.f;
-            if (p.gate_vec) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) acc[2][j] += m[j];
-            } else if (live) {
-                store8<TD, VEC>(row_at<TD>(p.dgate, r, p.ld_dgate), c, m);
+                    for (int j = 0; j < 8; ++j) z[j] = (keep >> j) & 1u ? z[j] : 0.f;
+                if (p.gate_vec) {
+                    fma8(g, z, acc[2]);  // without a bias the weight is the same for all rows and comes in at the end
+                } else {
+                    if (!BIAS) mul8(z, post);
+                    mul8(z, g);
+                    if (live) store8<TD, VEC>(row_at<TD>(p.dgate, r, p.ld_dgate), c, z);
+                }
             }
         }
+        pipe.next();
+        pipe.fetch(arrays, row + (int64_t)p.stages * stride, t, team, c);
     }
+    if (!pipe.ok && lane == 0) atomicExch(p.err, 8);
+    pipe.drain(p.stages);
+    if (!BIAS) mul8(acc[2], post);
     // column sums of the block: its teams' added in order
 #pragma unroll
     for (int k = 0; k < (BIAS ? 5 : 3); ++k) {
@@ -660,9 +754,10 @@ template <typename T> static bool on_16_bytes(const void *p, int64_t ld) { retur
 
 template <typename T> static void dropout_launch(Exec &ex, DropoutParams &p)
 {
-    p.team = std::min(DROP_THREADS, pow2_at_least(ceil_div64(p.width, 8)));
-    const int64_t blocks = ceil_div64(p.rows, DROP_THREADS / p.team * DROP_ROWS);
-    const bool vec = on_16_bytes<T>(p.in, p.ld_in) && on_16_bytes<T>(p.out, p.ld_out);
+    p.shift = 0;
+    while ((8 << p.shift) < p.width && p.shift < 8) ++p.shift;
+    const int64_t blocks = ceil_div64(p.rows, (DROP_THREADS >> p.shift) * DROP_ROWS);
+    const bool vec = (((uintptr_t)p.in | (uintptr_t)p.out | p.ld_in | p.ld_out) & 15) == 0;
     if (vec) launch_dep(dropout_kernel<T, true>, dim3((unsigned)blocks), dim3(DROP_THREADS), 0, ex.st, p);
     else launch_dep(dropout_kernel<T, false>, dim3((unsigned)blocks), dim3(DROP_THREADS), 0, ex.st, p);
     ex.launches += 1;
@@ -683,29 +778,45 @@ static ResidualGrid residual_grid(int64_t rows, int width, int threads_per_sm)
     return g;
 }
 
-static bool residual_vec(const ResidualParams &p)
+// every row of every array starts on 16 bytes and is made of pieces of 16
+static bool residual_vec(const ResidualParams &p, int size_s, int size_d)
 {
+    const bool only_d = !p.x && !p.dy && !(p.pre_norm && p.y);
+    if (p.width * size_d % 16 != 0 || (!only_d && p.width * size_s % 16 != 0)) return false;
     auto ok = [](const void *array, uint32_t ld) { return !array || (((uintptr_t)array | ld) & 15) == 0; };
     return ok(p.x, p.ld_x) && ok(p.h, p.ld_h) && ok(p.y, p.ld_y) && ok(p.n, p.ld_n) && ok(p.dy, p.ld_dy) && ok(p.dn, p.ld_dn) && ok(p.dx, p.ld_dx) && ok(p.dh, p.ld_dh) &&
            ok(p.gate, p.ld_gate) && ok(p.dgate, p.ld_dgate);
 }
 
-// pieces of the rows under way and how many rows: `room` bytes of shared memory per thread keep as many blocks resident as registers do
-template <typename TS, typename TD> static size_t residual_pipe(ResidualParams &p, const ResidualGrid &g, int room)
+// Places of the arrays in the ring of rows and how many rows it holds: `room` bytes of shared memory per thread keep as many blocks
+// resident as registers do.  Returns the bytes of shared memory of a block.
+static size_t residual_pipe(ResidualParams &p, const ResidualGrid &g, bool vec, bool forward, int size_s, int size_d, int room)
 {
-    const int s = PIPE_PIECES<TS>, d = PIPE_PIECES<TD>;
-    int at = 0;
-    auto place = [&](const void *array, int pieces) { const uint32_t here = (uint32_t)at * 16 * g.threads; if (array) at += pieces; return here; };
-    p.at_x = place(p.x, s);
-    p.at_dn = place(p.dn, d);
-    p.at_y = place(p.dn ? p.y : nullptr, s);
-    p.at_dy = place(p.dy, s);
-    p.at_h = place(p.h, d);
-    p.at_gate = place(p.gate, d);
-    p.pieces = at;
-    p.stages = std::max(2, std::min(4, room / (16 * at)));
-    while (p.stages * at * 16 * g.threads > 216 * 1024) --p.stages;  // blocks of 1024 threads: down to one, nothing under way
-    return (size_t)p.stages * at * 16 * g.threads;
+    const int units = g.block ? 1 : g.threads / 32, teams = g.block ? 1 : 32 / g.team;
+    uint32_t at = 0;
+    auto place = [&](PipeArray &a, const void *array, uint32_t ld, int size) {
+        a = PipeArray{(const char *)array, ld, 0, at};
+        if (!array || (!vec && size == 2)) return;
+        a.row_bytes = (uint32_t)p.width * size;
+        at += vec ? teams * a.row_bytes : 2u * 16 * g.threads;
+    };
+    int k = 0;
+    if (forward) {
+        place(p.pipe[k++], p.x, p.ld_x, size_s);
+    } else {
+        place(p.pipe[k++], p.pre_norm ? p.dn : nullptr, p.ld_dn, size_d);
+        place(p.pipe[k++], p.pre_norm ? p.y : nullptr, p.ld_y, size_s);
+        place(p.pipe[k++], p.dy, p.ld_dy, size_s);
+    }
+    place(p.pipe[k++], p.h, p.ld_h, size_d);
+    place(p.pipe[k++], p.gate, p.ld_gate, size_d);
+    p.copy_bytes = vec ? at / teams : 0;
+    p.unit_teams = teams;
+    p.stage_bytes = std::max(at, 16u);
+    const int64_t all = (int64_t)p.stage_bytes * (vec ? units : 1);
+    p.stages = (int)std::max<int64_t>(2, std::min<int64_t>(vec ? 8 : 4, (int64_t)room * g.threads / all));
+    while (p.stages > 1 && p.stages * all > 208 * 1024) --p.stages;  // blocks of 1024 threads: down to one, nothing under way
+    return (size_t)(p.stages * (all + (vec ? 8 * units : 0)));
 }
 template <typename... A, typename... P> static void launch_large(void (*kernel)(A...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, P &&...args)
 {
@@ -724,9 +835,9 @@ template <typename TS, typename TD> static void residual_launch(Exec &ex, Residu
 {
     const ResidualGrid g = residual_grid(p.rows, p.width, 768);
     p.team = g.team;
-    const size_t smem = residual_pipe<TS, TD>(p, g, 256);
-    const bool bias = p.pre_bias || p.post_bias;
-    if (residual_vec(p)) {
+    const bool bias = p.pre_bias || p.post_bias, vec = residual_vec(p, sizeof(TS), sizeof(TD));
+    const size_t smem = residual_pipe(p, g, vec, true, sizeof(TS), sizeof(TD), 256);
+    if (vec) {
         if (bias) residual_dispatch<TS, TD, true, true>(ex, p, g, smem);
         else residual_dispatch<TS, TD, true, false>(ex, p, g, smem);
     } else {
@@ -746,9 +857,9 @@ template <typename TS, typename TD, bool VEC, bool BIAS> static void residual_gr
 template <typename TS, typename TD> static void residual_grad_launch(Exec &ex, ResidualParams &p, const ResidualGrid &g, const ResidualSums &o, int accumulate)
 {
     p.team = g.team;
-    const size_t smem = residual_pipe<TS, TD>(p, g, 380);
-    const bool bias = o.out[3] || o.out[4] || p.post_bias;
-    if (residual_vec(p)) {
+    const bool bias = o.out[3] || o.out[4] || p.post_bias, vec = residual_vec(p, sizeof(TS), sizeof(TD));
+    const size_t smem = residual_pipe(p, g, vec, false, sizeof(TS), sizeof(TD), 380);
+    if (vec) {
         if (bias) residual_grad_dispatch<TS, TD, true, true>(ex, p, g, smem);
         else residual_grad_dispatch<TS, TD, true, false>(ex, p, g, smem);
     } else {

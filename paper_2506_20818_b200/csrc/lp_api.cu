@@ -2500,13 +2500,14 @@ extern "C" lp_status lp_dropout(lp_ctx *ctx, int32_t prec, int64_t rows, int32_t
     if (rows < 0 || rows >= (int64_t)1 << 31) return fail(ctx, LP_EINVAL, "lp_dropout: number of rows must be in [0, 2^31)");
     if (width < 1 || width > (1 << 20)) return fail(ctx, LP_EINVAL, "lp_dropout: width must be in [1, 2^20]");
     if (ld_in < width || ld_out < width) return fail(ctx, LP_EINVAL, "lp_dropout: a row pitch is smaller than the width");
+    if (ld_in >= RN_MAX_PITCH || ld_out >= RN_MAX_PITCH) return fail(ctx, LP_EINVAL, "lp_dropout: a row pitch is 2^29 elements or more");
     DropoutParams k{};
     if (!drop_args(p, seed, step, row_base, k.drop)) return fail(ctx, LP_EINVAL, "lp_dropout: p must be in [0, 1] and row_base not negative");
     if (rows == 0) return LP_OK;
     if (!in || !out) return fail(ctx, LP_EINVAL, "lp_dropout: null array");
     if (misaligned(in, prec) || misaligned(out, prec)) return fail(ctx, LP_EINVAL, "lp_dropout: an array is not aligned to its elements");
     CK(cudaSetDevice(ctx->device));
-    k.in = in; k.out = out; k.rows = (int)rows; k.width = width; k.ld_in = ld_in; k.ld_out = ld_out;
+    k.in = in; k.out = out; k.rows = (int)rows; k.width = width; k.ld_in = (uint32_t)(ld_in * (prec == LP_FP32 ? 4 : 2)); k.ld_out = (uint32_t)(ld_out * (prec == LP_FP32 ? 4 : 2));
     if (prec == LP_FP32) dropout_launch<float>(ctx->ex, k);
     else dropout_launch<bf16>(ctx->ex, k);
     CK_LAUNCH();
@@ -2523,7 +2524,7 @@ static lp_status residual_params(lp_ctx *ctx, const std::string &who, const lp_r
     if (d->width < 1 || d->width > RN_MAX_WIDTH) return fail(ctx, LP_EINVAL, who + ": width must be in [1, 8192]");
     for (int32_t kind : {d->pre_norm, d->post_norm})
         if (kind != LP_NORM_NONE && kind != LP_NORM_RMS && kind != LP_NORM_LAYER) return fail(ctx, LP_EINVAL, who + ": unknown norm");
-    if (!(d->eps > 0.0) || !std::isfinite(d->eps) || !((float)d->eps > 0.f)) return fail(ctx, LP_EINVAL, who + ": eps must be positive and finite");
+    if (!(d->eps >= 1e-37) || !std::isfinite((float)d->eps)) return fail(ctx, LP_EINVAL, who + ": eps must be at least 1e-37 and finite");
     if (!std::isfinite(d->scale)) return fail(ctx, LP_EINVAL, who + ": scale is not finite");
     if (!drop_args(d->p, d->seed, d->step, d->row_base, k.drop)) return fail(ctx, LP_EINVAL, who + ": p must be in [0, 1] and row_base not negative");
     if (d->gate && d->ld_gate >= RN_MAX_PITCH) return fail(ctx, LP_EINVAL, who + ": a row pitch is 2^29 elements or more");
@@ -2538,6 +2539,8 @@ static lp_status residual_params(lp_ctx *ctx, const std::string &who, const lp_r
     k.post_norm = branch ? d->post_norm : LP_NORM_NONE;
     k.eps = (float)d->eps;
     k.inv_width = 1.f / (float)d->width;
+    k.err = ctx->tc.err_word;
+    k.wait_ns = ctx->tc.wait_limit_ns;
     k.scale = (float)d->scale;
     if (k.pre_norm) { k.pre = d->pre; k.pre_bias = d->pre_bias; }
     if (k.post_norm) { k.post = d->post; k.post_bias = d->post_bias; }

@@ -193,7 +193,7 @@ def close(got, want, mag, ulps, dtype):
 
 WIDTHS = [(1, 1), (3, 7), (65, 64), (33, 100), (257, 417), (50, 256), (64, 1000), (130, 2048), (3, 5000), (2, 8192)]
 KINDS = [("rms", None, "none", 0.0), ("rms", "rms", "vector", 0.1), ("layer", "layer", "matrix", 0.25), (None, "rms", "none", 0.5), ("layer", None, "vector", 0.0),
-         (None, None, "matrix", 0.3)]
+         (None, None, "matrix", 0.3), ("layer", "layer", "vector", 0.0), ("layer", "layer", "none", 0.1)]
 
 
 @pytest.mark.parametrize("rows,width", WIDTHS)
