@@ -275,8 +275,9 @@ constexpr int RN_SUMS = 5;          // column sums of the backward pass: dpre, d
 struct PipeArray {        // of a kernel's arrays
     const char *at;
     uint32_t ld;          // bytes between rows
-    uint32_t row_bytes;   // VEC: of a row
-    uint32_t offset;      // in a stage
+    uint32_t row_bytes;   // of a row
+    uint32_t slot_bytes;  // of its place in a stage
+    uint32_t offset;      // of the first team's place
 };
 
 struct ResidualParams {
@@ -294,7 +295,7 @@ struct ResidualParams {
     void *y, *n, *dx, *dh, *dgate;
     uint32_t ld_x, ld_h, ld_y, ld_n, ld_dy, ld_dn, ld_dx, ld_dh, ld_dgate;
     float *partial;            // [gridDim.x][RN_SUMS][width] column sums of each block
-    // rows under way: how many, bytes of a unit's row of all arrays (VEC) or between rows of all threads' pieces
+    // rows under way: how many, bytes of a unit's rows of all arrays
     int stages;
     uint32_t stage_bytes;
     uint32_t copy_bytes;       // VEC: of one row of all arrays
@@ -305,44 +306,34 @@ struct ResidualParams {
 };
 
 
-// Rows on their way into shared memory, several ahead of the one that is worked on, so that what is under way takes no registers.
-//   VEC        one bulk copy per row and array, counted on a barrier of the unit (the warp, or the block of a large team) and row: two
-//              instructions per row where copies by every thread took about 150 and, of FP32, asked for every sector twice
-//   otherwise  each thread copies its own eight FP32 columns, 4 bytes at a time, and reads back only what it copied itself;
-//              BF16 rows that do not start on 16 bytes cannot be copied this way and are loaded when they are needed
+// Rows on their way into shared memory, several ahead of the one that is worked on, so that what is under way takes no registers: one
+// bulk copy per row and array, counted on a barrier of the unit (the warp, or the block of a large team) and row.  (Copies by every
+// thread took about 150 instructions per row and, of FP32, asked for every sector twice.)  Bulk copies are made of aligned pieces of
+// 16 bytes.  Rows that are not come with the bytes beside them in their first and last piece, which nobody looks at; a piece with a
+// byte of the row lies in the row's page.
 LP_DEVINL void copy_row(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
 {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
-LP_DEVINL void copy_async_4(uint32_t dst, const void *src, int bytes)
-{
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-}
+LP_DEVINL void mbar_expect_more(uint32_t bar, uint32_t bytes) { asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory"); }
 template <bool VEC, bool BLOCK> struct RowPipe {
     const ResidualParams &p;
-    uint32_t first, in, out, end;   // of the unit (VEC) or thread: where the next row goes, where the oldest lies
-    uint32_t bar_in, bar_out, bars; // VEC: the same of the barriers
-    uint32_t piece, parity;
+    uint32_t first, in, out, end;   // of the unit: where the next row goes, where the oldest lies
+    uint32_t bar_in, bar_out, bars; // the same of the barriers
+    uint32_t parity;
     bool ok;
     LP_DEVINL RowPipe(const ResidualParams &p_, uint8_t *smem) : p(p_), parity(0), ok(true)
     {
-        if (VEC) {
-            const uint32_t unit = BLOCK ? 0 : threadIdx.x >> 5, units = BLOCK ? 1 : blockDim.x >> 5;
-            first = smem_u32(smem) + unit * p.stages * p.stage_bytes;
-            bars = smem_u32(smem) + units * p.stages * p.stage_bytes + unit * p.stages * 8;
-            bar_in = bar_out = bars;
-            if (BLOCK ? threadIdx.x == 0 : (threadIdx.x & 31) == 0) {
-                for (int i = 0; i < p.stages; ++i) mbar_init(bars + 8 * i, 1);
-                fence_barrier_init();
-                fence_async_proxy();
-            }
-            sync();
-        } else {
-            first = smem_u32(smem) + threadIdx.x * 16;
-            piece = blockDim.x * 16;
-        }
-        in = out = first;
+        const uint32_t unit = BLOCK ? 0 : threadIdx.x >> 5, units = BLOCK ? 1 : blockDim.x >> 5;
+        first = in = out = smem_u32(smem) + unit * p.stages * p.stage_bytes;
         end = first + p.stages * p.stage_bytes;
+        bars = bar_in = bar_out = smem_u32(smem) + units * p.stages * p.stage_bytes + unit * p.stages * 8;
+        if (BLOCK ? threadIdx.x == 0 : (threadIdx.x & 31) == 0) {
+            for (int i = 0; i < p.stages; ++i) mbar_init(bars + 8 * i, 1);
+            fence_barrier_init();
+            fence_async_proxy();
+        }
+        sync();
     }
     // the threads that share the rows of a stage
     LP_DEVINL void sync() const
@@ -350,89 +341,95 @@ template <bool VEC, bool BLOCK> struct RowPipe {
         if (BLOCK) __syncthreads();
         else __syncwarp();
     }
-    // rows first_row .. of the unit's teams (this thread's is `row`), where they are below p.rows
-    template <int N> LP_DEVINL void fetch(const PipeArray (&arrays)[N], int64_t row, int t, int team, const Cols<VEC> &c)
+    // the next row of every team of the unit; `row` is this thread's
+    template <int N> LP_DEVINL void fetch(const PipeArray (&arrays)[N], int64_t row, int t, int team)
     {
-        const bool live = row < p.rows;
+        const bool sends = t == 0 && row < p.rows;
         if (VEC) {
-            if (t == 0) {
-                // the unit's first thread says how much is on its way, the first of every team sends its row's share
-                if (team == 0) mbar_expect_tx(bar_in, p.copy_bytes * (uint32_t)min(max((int64_t)p.rows - row, (int64_t)0), (int64_t)p.unit_teams));
-                if (live)
-#pragma unroll
-                    for (int k = 0; k < N; ++k)
-                        if (arrays[k].at) copy_row(in + arrays[k].offset + team * arrays[k].row_bytes, arrays[k].at + (uint64_t)(uint32_t)row * arrays[k].ld, arrays[k].row_bytes, bar_in);
-            }
-            bar_in += 8;
+            // the unit's first thread says how much is on its way
+            if (t == 0 && team == 0) mbar_expect_tx(bar_in, p.copy_bytes * (uint32_t)min(max((int64_t)p.rows - row, (int64_t)0), (int64_t)p.unit_teams));
         } else {
+            if (sends) {
+                uint32_t bytes = 0;
+#pragma unroll
+                for (int k = 0; k < N; ++k)
+                    if (arrays[k].at) {
+                        const uint32_t at = (uint32_t)(uintptr_t)arrays[k].at + (uint32_t)row * arrays[k].ld;  // the low bits of the address
+                        bytes += ((at & 15) + arrays[k].row_bytes + 15) & ~15u;
+                    }
+                mbar_expect_more(bar_in, bytes);
+            }
+            if (!BLOCK) __syncwarp();
+            if (t == 0 && team == 0) mbar_arrive(bar_in);
+        }
+        if (sends)
 #pragma unroll
             for (int k = 0; k < N; ++k)
-                if (arrays[k].at && arrays[k].row_bytes) {
-                    const char *src = arrays[k].at + (uint64_t)(live ? (uint32_t)row : 0u) * arrays[k].ld;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const bool has = c.has(j);
-                        copy_async_4(in + arrays[k].offset + (j >> 2) * piece + (j & 3) * 4, src + (has ? c.at(j) * 4 : 0), live && has ? 4 : 0);
-                    }
+                if (arrays[k].at) {
+                    const uint64_t at = (uint64_t)arrays[k].at + (uint64_t)(uint32_t)row * arrays[k].ld;
+                    copy_row(in + arrays[k].offset + team * arrays[k].slot_bytes, (const void *)(VEC ? at : at & ~(uint64_t)15),
+                             VEC ? arrays[k].row_bytes : (((uint32_t)at & 15) + arrays[k].row_bytes + 15) & ~15u, bar_in);
                 }
-            asm volatile("cp.async.commit_group;" ::: "memory");
-        }
         in += p.stage_bytes;
+        bar_in += 8;
         if (in == end) { in = first; bar_in = bars; }
     }
     template <typename T> LP_DEVINL void read(const PipeArray &a, int64_t row, int team, const Cols<VEC> &c, float *v) const
     {
         const bool live = row < p.rows;
-        constexpr int VN = Vec16<T>::N;
-        if (!VEC && sizeof(T) == 2) {
-            const T *src = (const T *)(a.at + (uint64_t)(live ? (uint32_t)row : 0u) * a.ld);
+        uint32_t src = out + a.offset + team * a.slot_bytes;
+        if (VEC) {
+            constexpr int VN = Vec16<T>::N;
+            src += c.base * (uint32_t)sizeof(T);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = live && c.has(j) ? to_f<T>(src[c.at(j)]) : 0.f;
-            return;
-        }
-#pragma unroll
-        for (int k = 0; k < 8 / VN; ++k) {
-            Vec16<T> x;
-            x.zero();
-            if (!VEC || (live && c.base + k * VN < c.width)) {
-                uint32_t w[4];
-                const uint32_t src = out + a.offset + (VEC ? team * a.row_bytes + (c.base + k * VN) * (uint32_t)sizeof(T) : k * piece);
-                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(src) : "memory");
-                memcpy(&x.v, w, 16);
+            for (int k = 0; k < 8 / VN; ++k) {
+                Vec16<T> x;
+                x.zero();
+                if (live && c.base + k * VN < c.width) {
+                    uint32_t w[4];
+                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(src + 16 * k) : "memory");
+                    memcpy(&x.v, w, 16);
+                }
+                x.to_float(v + k * VN);
             }
-            x.to_float(v + k * VN);
+        } else {
+            src += (((uint32_t)(uintptr_t)a.at + (uint32_t)row * a.ld) & 15) + c.base * (uint32_t)sizeof(T);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                v[j] = 0.f;
+                if (live && c.has(j)) {
+                    if (sizeof(T) == 4) {
+                        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v[j]) : "r"(src + j * c.step * 4) : "memory");
+                    } else {
+                        uint16_t h;
+                        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(src + j * c.step * 2) : "memory");
+                        v[j] = __uint_as_float((uint32_t)h << 16);
+                    }
+                }
+            }
         }
     }
     // the oldest row has arrived; false when the wait ran out (in all threads of the unit)
     LP_DEVINL bool wait()
     {
-        if (VEC) {
-            ok = mbar_wait(bar_out, parity, p.wait_ns);
-            ok = BLOCK ? __syncthreads_and(ok) != 0 : __all_sync(0xffffffffu, ok) != 0;
-            return ok;
-        }
-        if (p.stages == 1) asm volatile("cp.async.wait_group 0;" ::: "memory");
-        else if (p.stages == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
-        else if (p.stages == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
-        else asm volatile("cp.async.wait_group 3;" ::: "memory");
-        return true;
+        ok = mbar_wait(bar_out, parity, p.wait_ns);
+        ok = BLOCK ? __syncthreads_and(ok) != 0 : __all_sync(0xffffffffu, ok) != 0;
+        return ok;
     }
     // the oldest row's place is free again
     LP_DEVINL void next()
     {
-        if (VEC) sync();
+        sync();
         out += p.stage_bytes;
         bar_out += 8;
         if (out == end) { out = first; bar_out = bars; parity ^= 1; }
     }
-    // after a wait that ran out: what is under way lands before the block goes (rows that were waited for have)
-    LP_DEVINL void drain(int ahead)
+    // what is under way lands before the block goes (after a wait that ran out; else nothing is)
+    LP_DEVINL void drain()
     {
-        if (VEC) {
-            for (int i = 0; i < ahead; ++i) {
-                mbar_wait(bar_out, parity, p.wait_ns);
-                next();
-            }
+        for (int i = 0; i < p.stages; ++i) {
+            mbar_wait(bar_out, parity, p.wait_ns);
+            next();
         }
     }
 };
@@ -506,7 +503,7 @@ LP_DEVINL void normalise(float *v, const float *w, int kind, float eps, float in
 }
 
 // MAXT: the largest team of the variant, 32 (parts of warps), 256 or 1024 (whole blocks).  BIAS: norms with a bias
-template <typename TS, typename TD, bool VEC, int MAXT, bool BIAS> __global__ void __launch_bounds__(MAXT < 256 ? 256 : MAXT) residual_norm_kernel(const __grid_constant__ ResidualParams p)
+template <typename TS, typename TD, bool VEC, int MAXT, bool BIAS> __global__ void __launch_bounds__(MAXT < 256 ? 256 : MAXT, MAXT > 256 ? 1 : 3) residual_norm_kernel(const __grid_constant__ ResidualParams p)
 {
     LP_DEP_ENTER();
     constexpr bool BLOCK = MAXT > 32;
@@ -531,7 +528,7 @@ template <typename TS, typename TD, bool VEC, int MAXT, bool BIAS> __global__ vo
     RowPipe<VEC, BLOCK> pipe(p, pipe_smem);
     const PipeArray arrays[3] = {p.pipe[0], p.pipe[1], p.pipe[2]};
     const int team = BLOCK ? 0 : lane / T;
-    for (int i = 0; i < p.stages; ++i) pipe.fetch(arrays, row + (int64_t)i * stride, t, team, c);
+    for (int i = 0; i < p.stages; ++i) pipe.fetch(arrays, row + (int64_t)i * stride, t, team);
     for (int i = 0; i < rounds; ++i, row += stride) {
         const bool live = row < p.rows;  // of a warp's teams some may be past the last row; they take part in the sums of the others
         const uint32_t r = live ? (uint32_t)row : 0u;
@@ -569,10 +566,10 @@ template <typename TS, typename TD, bool VEC, int MAXT, bool BIAS> __global__ vo
             if (live) store8<TD, VEC>(row_at<TD>(p.n, r, p.ld_n), c, y);
         }
         pipe.next();
-        pipe.fetch(arrays, row + (int64_t)p.stages * stride, t, team, c);
+        pipe.fetch(arrays, row + (int64_t)p.stages * stride, t, team);
     }
     if (!pipe.ok && threadIdx.x % 32 == 0) atomicExch(p.err, 8);
-    pipe.drain(p.stages);
+    pipe.drain();
 }
 
 // v: the row, becomes z.  q: gradient of the norm's output, becomes that of its input.  dw, db: column sums.
@@ -606,15 +603,17 @@ LP_DEVINL void norm_backward(float *v, float *q, const float *w, int kind, float
     for (int k = 0; k < 4; ++k) set_pair(q, k, __ffma2_rn(pair(v, k), minus, __ffma2_rn(pair(u, k), rr, make_float2(off, off))));
 }
 
-// BIAS: column sums of the biases too (sixteen more registers).  MAXT as above, and 256: blocks of 1024 threads leave 64 registers
-// for each, which the column sums do not fit into.
+// BIAS: column sums of the biases too (sixteen more registers: 384 threads per SM instead of 512).  MAXT as above, and 128 and 256:
+// blocks of 1024 threads leave 64 registers for each, which the column sums do not fit into.
+template <int MAXT, bool BIAS> constexpr int RN_GRAD_THREADS = MAXT > 32 ? MAXT : BIAS ? 128 : 256;
+template <bool BIAS> constexpr int RN_GRAD_RESIDENT = BIAS ? 384 : 512;
 template <typename TS, typename TD, bool VEC, int MAXT, bool BIAS>
-__global__ void __launch_bounds__(MAXT < 256 ? 256 : MAXT, MAXT > 256 ? 1 : 2) residual_norm_grad_kernel(const __grid_constant__ ResidualParams p)
+__global__ void __launch_bounds__(RN_GRAD_THREADS<MAXT, BIAS>, MAXT > 256 ? 1 : RN_GRAD_RESIDENT<BIAS> / RN_GRAD_THREADS<MAXT, BIAS>) residual_norm_grad_kernel(const __grid_constant__ ResidualParams p)
 {
     LP_DEP_ENTER();
     constexpr bool BLOCK = MAXT > 32;
     __shared__ float scratch[2 * 32 * 4];
-    __shared__ float sums[BLOCK ? 1 : 8 * 256];
+    __shared__ float sums[BLOCK ? 1 : 8 * RN_GRAD_THREADS<MAXT, BIAS>];
     extern __shared__ __align__(16) uint8_t pipe_smem[];
     int turn = 0;
     const int T = p.team, t = threadIdx.x & (T - 1), lane = threadIdx.x & 31, teams = BLOCK ? 1 : blockDim.x / T;
@@ -635,7 +634,7 @@ __global__ void __launch_bounds__(MAXT < 256 ? 256 : MAXT, MAXT > 256 ? 1 : 2) r
     RowPipe<VEC, BLOCK> pipe(p, pipe_smem);
     const PipeArray arrays[5] = {p.pipe[0], p.pipe[1], p.pipe[2], p.pipe[3], p.pipe[4]};
     const int team = BLOCK ? 0 : lane / T;
-    for (int i = 0; i < p.stages; ++i) pipe.fetch(arrays, row + (int64_t)i * stride, t, team, c);
+    for (int i = 0; i < p.stages; ++i) pipe.fetch(arrays, row + (int64_t)i * stride, t, team);
     for (int i = 0; i < rounds; ++i, row += stride) {
         const bool live = row < p.rows;
         const uint32_t r = live ? (uint32_t)row : 0u;
@@ -691,10 +690,10 @@ __global__ void __launch_bounds__(MAXT < 256 ? 256 : MAXT, MAXT > 256 ? 1 : 2) r
             }
         }
         pipe.next();
-        pipe.fetch(arrays, row + (int64_t)p.stages * stride, t, team, c);
+        pipe.fetch(arrays, row + (int64_t)p.stages * stride, t, team);
     }
     if (!pipe.ok && lane == 0) atomicExch(p.err, 8);
-    pipe.drain(p.stages);
+    pipe.drain();
     if (!BIAS) mul8(acc[2], post);
     // column sums of the block: its teams' added in order
 #pragma unroll
@@ -767,15 +766,19 @@ struct ResidualGrid {
     int team, threads, blocks;
     bool block;
 };
-static ResidualGrid residual_grid(int64_t rows, int width, int threads_per_sm)
+// `threads` per block where the teams are parts of warps, `resident` per SM
+static ResidualGrid residual_grid(int64_t rows, int width, int threads, int resident)
 {
     ResidualGrid g;
     g.team = pow2_at_least(ceil_div64(width, 8));
     g.block = g.team > 32;
-    g.threads = g.block ? g.team : 256;
-    const int64_t per_sm = std::max(1, threads_per_sm / g.threads);
-    g.blocks = (int)std::min<int64_t>(ceil_div64(rows, g.threads / g.team), (int64_t)tc_sm_count() * per_sm);
+    g.threads = g.block ? g.team : threads;
+    g.blocks = (int)std::min<int64_t>(ceil_div64(rows, g.threads / g.team), (int64_t)tc_sm_count() * std::max(1, resident / g.threads));
     return g;
+}
+static ResidualGrid residual_grad_grid(int64_t rows, int width, bool bias)
+{
+    return bias ? residual_grid(rows, width, RN_GRAD_THREADS<32, true>, RN_GRAD_RESIDENT<true>) : residual_grid(rows, width, RN_GRAD_THREADS<32, false>, RN_GRAD_RESIDENT<false>);
 }
 
 // every row of every array starts on 16 bytes and is made of pieces of 16
@@ -795,10 +798,9 @@ static size_t residual_pipe(ResidualParams &p, const ResidualGrid &g, bool vec, 
     const int units = g.block ? 1 : g.threads / 32, teams = g.block ? 1 : 32 / g.team;
     uint32_t at = 0;
     auto place = [&](PipeArray &a, const void *array, uint32_t ld, int size) {
-        a = PipeArray{(const char *)array, ld, 0, at};
-        if (!array || (!vec && size == 2)) return;
-        a.row_bytes = (uint32_t)p.width * size;
-        at += vec ? teams * a.row_bytes : 2u * 16 * g.threads;
+        const uint32_t row = (uint32_t)p.width * size;
+        a = PipeArray{(const char *)array, ld, row, vec ? row : (row + 30) & ~15u, at};
+        if (array) at += teams * a.slot_bytes;
     };
     int k = 0;
     if (forward) {
@@ -813,10 +815,10 @@ static size_t residual_pipe(ResidualParams &p, const ResidualGrid &g, bool vec, 
     p.copy_bytes = vec ? at / teams : 0;
     p.unit_teams = teams;
     p.stage_bytes = std::max(at, 16u);
-    const int64_t all = (int64_t)p.stage_bytes * (vec ? units : 1);
-    p.stages = (int)std::max<int64_t>(2, std::min<int64_t>(vec ? 8 : 4, (int64_t)room * g.threads / all));
+    const int64_t all = (int64_t)p.stage_bytes * units;
+    p.stages = (int)std::max<int64_t>(2, std::min<int64_t>(8, (int64_t)room * g.threads / all));
     while (p.stages > 1 && p.stages * all > 208 * 1024) --p.stages;  // blocks of 1024 threads: down to one, nothing under way
-    return (size_t)(p.stages * (all + (vec ? 8 * units : 0)));
+    return (size_t)(p.stages * (all + 8 * units));
 }
 template <typename... A, typename... P> static void launch_large(void (*kernel)(A...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, P &&...args)
 {
@@ -833,7 +835,7 @@ template <typename TS, typename TD, bool VEC, bool BIAS> static void residual_di
 }
 template <typename TS, typename TD> static void residual_launch(Exec &ex, ResidualParams &p)
 {
-    const ResidualGrid g = residual_grid(p.rows, p.width, 768);
+    const ResidualGrid g = residual_grid(p.rows, p.width, 256, 768);
     p.team = g.team;
     const bool bias = p.pre_bias || p.post_bias, vec = residual_vec(p, sizeof(TS), sizeof(TD));
     const size_t smem = residual_pipe(p, g, vec, true, sizeof(TS), sizeof(TD), 256);
@@ -851,14 +853,15 @@ template <typename TS, typename TD, bool VEC, bool BIAS> static void residual_gr
 {
     const dim3 grid(g.blocks), block(g.threads);
     if (g.threads > 256) launch_large(residual_norm_grad_kernel<TS, TD, VEC, 1024, BIAS>, grid, block, smem, ex.st, p);
-    else if (g.block) launch_large(residual_norm_grad_kernel<TS, TD, VEC, 256, BIAS>, grid, block, smem, ex.st, p);
+    else if (g.threads > 128 && g.block) launch_large(residual_norm_grad_kernel<TS, TD, VEC, 256, BIAS>, grid, block, smem, ex.st, p);
+    else if (g.block) launch_large(residual_norm_grad_kernel<TS, TD, VEC, 128, BIAS>, grid, block, smem, ex.st, p);
     else launch_large(residual_norm_grad_kernel<TS, TD, VEC, 32, BIAS>, grid, block, smem, ex.st, p);
 }
-template <typename TS, typename TD> static void residual_grad_launch(Exec &ex, ResidualParams &p, const ResidualGrid &g, const ResidualSums &o, int accumulate)
+template <typename TS, typename TD> static void residual_grad_launch(Exec &ex, ResidualParams &p, const ResidualGrid &g, const ResidualSums &o, bool bias, int accumulate)
 {
     p.team = g.team;
-    const bool bias = o.out[3] || o.out[4] || p.post_bias, vec = residual_vec(p, sizeof(TS), sizeof(TD));
-    const size_t smem = residual_pipe(p, g, vec, false, sizeof(TS), sizeof(TD), 380);
+    const bool vec = residual_vec(p, sizeof(TS), sizeof(TD));
+    const size_t smem = residual_pipe(p, g, vec, false, sizeof(TS), sizeof(TD), 190 * 1024 / (bias ? RN_GRAD_RESIDENT<true> : RN_GRAD_RESIDENT<false>));
     if (vec) {
         if (bias) residual_grad_dispatch<TS, TD, true, true>(ex, p, g, smem);
         else residual_grad_dispatch<TS, TD, true, false>(ex, p, g, smem);
