@@ -8,10 +8,14 @@
 // larger ones are taken, so that a product is off by about 2^-23; the accumulator of the matrix instructions rounds towards
 // zero, so it adds up 64 terms, small products first, and those sums are added in FP32 registers.
 //
-// One persistent block per SM, 18 warps.  Sizes of the groups are on the device: every role walks the offsets itself, 32 groups at a
-// time, and finds its tiles (linear) or its share of the 64-row blocks of all tiles (weight gradient) without any plan or host read.
-//   warp 0    operands by TMA (BF16, rows on 16 bytes)         warp 1   matrix instructions
-//   others    sums and results; without TMA the last eight bring in the operands through registers
+// Persistent blocks of 18 warps, one per SM.  Sizes of the groups are on the device: every role walks the offsets itself, 32 groups at
+// a time, and finds its tiles (linear) or its share of the 64-row blocks of all tiles (weight gradient) without any plan or host read.
+//   warp 0    operands by TMA         warp 1   matrix instructions
+//   others    sums and results; FP32: the last eight bring in the operands that have to be split, through registers
+// Large BF16 products take pairs of SMs (cta_group::2) and tiles of 256 x 256: a 64-term block then costs 32 KiB of operands per SM for
+// 512 cycles of products, where a block of its own with 128 x 256 would need 48 KiB.
+// BF16 operands whose rows do not start on 16 bytes are copied to rows that do (TMA takes no others), FP32 ones, too, so that they can be
+// read 16 bytes at a time; the FP32 matrices B are split into their parts once per call.
 // The weight gradient deals out equal shares of 64-row blocks: a tile that lies in several shares is written as partial tiles,
 // added in a fixed order by a second kernel.  Bits do not depend on anything but the sizes.
 #pragma once
@@ -35,9 +39,8 @@ struct GroupedParams {
     int rows;                // of A; offsets are clamped to [0, rows]
     int N, K;                // linear: columns of C, of A; weight gradient: columns of dZ, of A
     int tiles_n, tiles_k;    // tiles_k: weight gradient only
-    const void *A, *B;       // register loads only (B: dZ of the weight gradient)
-    int64_t lda, ldb, stride_b;
-    int vec_a, vec_b;        // rows on 16 bytes
+    const void *A, *B;       // operands that come through registers (B: dZ of the weight gradient); rows on 16 bytes
+    int64_t lda, ldb;
     int stages, flush;       // blocks of 64 terms that an accumulator adds up
     // linear
     const float *bias;
@@ -61,12 +64,12 @@ struct GroupedParams {
 // ---------------------------------------------------------------------------------------------
 // A warp's window of 32 groups.  Offsets that decrease or leave [0, rows] count as the nearest ones that do not, so that no tile can
 // leave the arrays and no two groups share a row.
-template <bool WGRAD> struct GroupWalk {
+template <bool WGRAD, int ROWS> struct GroupWalk {  // ROWS: of a tile (linear)
     const int *off;
     int groups, rows;
     int g0, before, last;        // first group of the window, tiles before it, end of the group before it
     int begin, end, incl, total; // of this lane's group; tiles up to and with it; tiles of the window
-    LP_DEVINL int count(int size) const { return WGRAD ? max(1, (size + 63) >> 6) : (size + 127) >> 7; }
+    LP_DEVINL int count(int size) const { return WGRAD ? max(1, (size + 63) >> 6) : (size + ROWS - 1) / ROWS; }
     LP_DEVINL void window()
     {
         const int lane = threadIdx.x & 31, g = g0 + lane;
@@ -122,17 +125,20 @@ template <bool WGRAD> struct GroupWalk {
 struct GroupedJob {
     int g, row0, row_end;  // linear: rows of the tile; weight gradient: rows of the share
     int kt, nt, kbs;       // tile, blocks of 64 terms
-    int slot;              // weight gradient: partial tile, or -1: the whole tile is in this share
+    int slot;              // weight gradient: partial tile of the worker, or -1: the whole tile is in this share
     bool begins;           // ... the share begins the tile, which ends before block tile_end of all
     int64_t tile_end;
 };
 
-template <int MODE> struct GroupedJobs {
-    GroupWalk<MODE == GP_WGRAD> walk;
+// `worker` of `workers`: block or pair of blocks
+template <int MODE, int ROWS> struct GroupedJobs {
+    GroupWalk<MODE == GP_WGRAD, ROWS> walk;
     const GroupedParams &p;
-    int64_t t;           // linear: next tile of this block
+    int worker, workers;
+    int64_t t;           // linear: next tile
     int64_t u, lo, hi;   // weight gradient: 64-row blocks of this share
-    LP_DEVINL GroupedJobs(const GroupedParams &p_, int64_t lo_, int64_t hi_) : walk(p_), p(p_), t(blockIdx.x), u(lo_), lo(lo_), hi(hi_) {}
+    LP_DEVINL GroupedJobs(const GroupedParams &p_, int worker_, int workers_, int64_t lo_, int64_t hi_)
+        : walk(p_), p(p_), worker(worker_), workers(workers_), t(worker_), u(lo_), lo(lo_), hi(hi_) {}
     LP_DEVINL bool next(GroupedJob &j)
     {
         int b, e, pre;
@@ -140,12 +146,12 @@ template <int MODE> struct GroupedJobs {
             const int mt = (int)(t / p.tiles_n);
             j.nt = (int)(t - (int64_t)mt * p.tiles_n);
             if (!walk.seek(mt, j.g, b, e, pre)) return false;
-            j.row0 = b + (mt - pre) * 128;
-            j.row_end = min(e, j.row0 + 128);
+            j.row0 = b + (mt - pre) * ROWS;
+            j.row_end = min(e, j.row0 + ROWS);
             j.kt = 0;
             j.kbs = (p.K + 63) >> 6;
             j.slot = -1;
-            t += gridDim.x;
+            t += workers;
             return true;
         }
         if (u >= hi) return false;
@@ -159,7 +165,7 @@ template <int MODE> struct GroupedJobs {
         j.nt = tile - j.kt * p.tiles_n;
         j.row0 = b + kb0 * 64;
         j.row_end = min(e, j.row0 + j.kbs * 64);
-        j.slot = kb0 == 0 && j.kbs == blocks ? -1 : 2 * (int)blockIdx.x + (u == lo ? 0 : 1);
+        j.slot = kb0 == 0 && j.kbs == blocks ? -1 : 2 * worker + (u == lo ? 0 : 1);
         j.begins = kb0 == 0;
         j.tile_end = u - kb0 + blocks;
         u += j.kbs;
@@ -170,41 +176,13 @@ template <int MODE> struct GroupedJobs {
 // ---------------------------------------------------------------------------------------------
 // operands through registers
 // ---------------------------------------------------------------------------------------------
-// eight neighbouring elements of a row, zeros beyond its end
-template <typename T> struct Piece8;
-template <> struct Piece8<bf16> {
-    uint4 w;
-    LP_DEVINL void load(const bf16 *row, int col, int limit, int vec)
-    {
-        const int n = limit - col;
-        if (vec && n >= 8) {
-            w = __ldg(reinterpret_cast<const uint4 *>(row + col));
-        } else {
-            uint32_t x[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < n) x[i >> 1] |= (uint32_t)__ldg(reinterpret_cast<const unsigned short *>(row + col) + i) << (16 * (i & 1));
-            w = make_uint4(x[0], x[1], x[2], x[3]);
-        }
-    }
-    LP_DEVINL void zero() { w = make_uint4(0u, 0u, 0u, 0u); }
-    LP_DEVINL void store(uint8_t *s, uint32_t) const { *reinterpret_cast<uint4 *>(s) = w; }
-    LP_DEVINL void add_to(float *acc) const
-    {
-        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            acc[2 * i] += __uint_as_float(x[i] << 16);
-            acc[2 * i + 1] += __uint_as_float(x[i] & 0xffff0000u);
-        }
-    }
-};
-template <> struct Piece8<float> {
+// eight neighbouring elements of an FP32 row on 16 bytes, zeros beyond its end
+struct Piece8 {
     float v[8];
-    LP_DEVINL void load(const float *row, int col, int limit, int vec)
+    LP_DEVINL void load(const float *row, int col, int limit)
     {
         const int n = limit - col;
-        if (vec && n >= 8) {
+        if (n >= 8) {
             const float4 a = __ldg(reinterpret_cast<const float4 *>(row + col)), b = __ldg(reinterpret_cast<const float4 *>(row + col) + 1);
             v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
         } else {
@@ -217,8 +195,8 @@ template <> struct Piece8<float> {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = 0.f;
     }
-    // the three parts lie `part` bytes apart
-    LP_DEVINL void store(uint8_t *s, uint32_t part) const
+    // part q of the values goes to put(q, 16 bytes)
+    template <typename F> LP_DEVINL void parts(F put) const
     {
         float r[8];
 #pragma unroll
@@ -228,98 +206,164 @@ template <> struct Piece8<float> {
             uint32_t x[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) x[i] = __byte_perm(__float_as_uint(r[2 * i]), __float_as_uint(r[2 * i + 1]), 0x7632);  // the upper halves
-            *reinterpret_cast<uint4 *>(s + q * part) = make_uint4(x[0], x[1], x[2], x[3]);
+            put(q, make_uint4(x[0], x[1], x[2], x[3]));
             if (q < 2)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) r[i] -= __uint_as_float(__float_as_uint(r[i]) & 0xffff0000u);  // exact
         }
     }
-    LP_DEVINL void add_to(float *acc) const
-    {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) acc[i] += v[i];
-    }
 };
+
+// A matrix copied to rows that start on 16 bytes: `width` elements in rows of `ld_out`, 16 bytes per thread out of aligned words
+template <typename T> __global__ void __launch_bounds__(256) grouped_align_kernel(const T *in, int64_t rows, int width, int64_t ld_in, T *out, int64_t ld_out)
+{
+    LP_DEP_ENTER();
+    constexpr int E = 16 / sizeof(T);
+    const int64_t per = ld_out / E, i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / per;
+    if (row >= rows) return;
+    const int col = (int)(i - row * per) * E, n = min(E, width - col);
+    const T *src = in + row * ld_in + col;
+    uint32_t w[5] = {0u, 0u, 0u, 0u, 0u};
+    const uint32_t *words = reinterpret_cast<const uint32_t *>((uintptr_t)src & ~(uintptr_t)3);
+    const int odd = ((uintptr_t)src & 3) != 0;  // BF16: the first element is the upper half of a word
+    const int count = (n * (int)sizeof(T) + 2 * odd + 3) / 4;
+#pragma unroll
+    for (int k = 0; k < 5; ++k)
+        if (k < count) w[k] = __ldg(words + k);
+    if (odd)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = __funnelshift_r(w[k], w[k + 1], 16);
+    *reinterpret_cast<uint4 *>(out + row * ld_out + col) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// An FP32 matrix as its three parts, each in rows of `ld_out` BF16 numbers, `part` elements apart
+__global__ void __launch_bounds__(256) grouped_split_kernel(const float *in, int64_t rows, int width, int vec, bf16 *out, int64_t ld_out, int64_t part)
+{
+    LP_DEP_ENTER();
+    const int64_t per = ld_out / 8, i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / per;
+    if (row >= rows) return;
+    const int col = (int)(i - row * per) * 8;
+    Piece8 x;
+    if (vec) {
+        x.load(in + row * width, col, width);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x.v[k] = col + k < width ? __ldg(in + row * width + col + k) : 0.f;
+    }
+    x.parts([&](int q, const uint4 &w) { *reinterpret_cast<uint4 *>(out + q * part + row * ld_out + col) = w; });
+}
 
 // ---------------------------------------------------------------------------------------------
 // results
 // ---------------------------------------------------------------------------------------------
-// sixteen neighbouring columns of a warp's 32 rows, a row per lane: rows below `rows`, columns below `cols`
-template <typename T> LP_DEVINL void put16(T *dst, int64_t ld, int rows, int cols, const float *v, int vec, float *stage, bool accumulate)
+// Neighbouring columns of a warp's 32 rows, a row per lane (64 bytes of it, so 16 FP32 or 32 BF16 columns): rows below `rows`, columns
+// below `cols`.  They go through 2 KiB of shared memory, so that a store instruction writes whole runs of a few rows: 64 bytes of eight
+// rows, or sixteen elements of two rows where the rows of the result do not start on 16 bytes.
+template <typename T> constexpr int PUT_COLS = 64 / sizeof(T);
+template <typename T> LP_DEVINL void put_columns(T *dst, int64_t ld, int rows, int cols, const float *v, int vec, uint8_t *stage, bool accumulate)
 {
     const int lane = threadIdx.x & 31;
+    constexpr int VN = Vec16<T>::N;
     if (vec) {
-        if (lane < rows) {
-            T *d = dst + (int64_t)lane * ld;
-            constexpr int VN = Vec16<T>::N;
+        __syncwarp();
 #pragma unroll
-            for (int c = 0; c < 16; c += VN)
-                if (c < cols) {
-                    Vec16<T> o;
-                    float w[VN];
-#pragma unroll
-                    for (int i = 0; i < VN; ++i) w[i] = v[c + i];
-                    if (accumulate) {
-                        o.v = *reinterpret_cast<decltype(o.v) *>(d + c);
-                        float x[VN];
-                        o.to_float(x);
-#pragma unroll
-                        for (int i = 0; i < VN; ++i) w[i] += x[i];
-                    }
-                    o.from_float(w);
-                    o.store(d + c);
-                }
+        for (int q = 0; q < 4; ++q) {
+            Vec16<T> o;
+            o.from_float(v + q * VN);
+            *reinterpret_cast<decltype(o.v) *>(stage + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4)) = o.v;
         }
+        __syncwarp();
+        const int q = lane & 3;
+        if (q * VN < cols)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = 8 * i + (lane >> 2);
+                if (r < rows) {
+                    Vec16<T> o;
+                    o.v = *reinterpret_cast<const decltype(o.v) *>(stage + r * 64 + ((q ^ ((r >> 1) & 3)) << 4));
+                    T *d = dst + (int64_t)r * ld + q * VN;
+                    if (accumulate) {
+                        Vec16<T> old;
+                        old.v = *reinterpret_cast<const decltype(o.v) *>(d);
+                        float x[VN], y[VN];
+                        old.to_float(x);
+                        o.to_float(y);
+#pragma unroll
+                        for (int k = 0; k < VN; ++k) y[k] += x[k];
+                        o.from_float(y);
+                    }
+                    o.store(d);
+                }
+            }
         return;
     }
-    // through shared memory, so that a store instruction writes runs of sixteen elements of two rows
-    __syncwarp();
+    float *s = reinterpret_cast<float *>(stage);
 #pragma unroll
-    for (int c = 0; c < 16; ++c) stage[lane * 16 + (c ^ (lane & 15))] = v[c];
-    __syncwarp();
-    const int c = lane & 15;
-    if (c < cols)
+    for (int half = 0; half < PUT_COLS<T> / 16; ++half) {
+        __syncwarp();
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int r = 2 * i + (lane >> 4);
-            if (r < rows) {
-                T *d = dst + (int64_t)r * ld + c;
-                const float x = stage[r * 16 + (c ^ (r & 15))];
-                *d = from_f<T>(accumulate ? to_f<T>(*d) + x : x);
+        for (int c = 0; c < 16; ++c) s[lane * 16 + (c ^ (lane & 15))] = v[half * 16 + c];
+        __syncwarp();
+        const int c = lane & 15;
+        if (half * 16 + c < cols)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int r = 2 * i + (lane >> 4);
+                if (r < rows) {
+                    T *d = dst + (int64_t)r * ld + half * 16 + c;
+                    const float x = s[r * 16 + (c ^ (r & 15))];
+                    *d = from_f<T>(accumulate ? to_f<T>(*d) + x : x);
+                }
             }
-        }
+    }
 }
 
 // ---------------------------------------------------------------------------------------------
 // kernel
 // ---------------------------------------------------------------------------------------------
-LP_DEVINL void tma_load_3d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int y, int z)
+// copies into this block's shared memory, counted on a barrier of this block or (PAIR) of the pair's first
+template <bool PAIR> LP_DEVINL void tile_2d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int y)
 {
-    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst), "l"(map),
-                 "r"(bar), "r"(x), "r"(y), "r"(z)
-                 : "memory");
+    if (PAIR) tma_load_2d_pair(dst, map, bar, x, y);
+    else tma_load_2d(dst, map, bar, x, y);
+}
+template <bool PAIR> LP_DEVINL void tile_3d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int y, int z)
+{
+    if (PAIR)
+        asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst), "l"(map),
+                     "r"(bar), "r"(x), "r"(y), "r"(z)
+                     : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst), "l"(map),
+                     "r"(bar), "r"(x), "r"(y), "r"(z)
+                     : "memory");
 }
 
+// A worker (a block, or a pair of blocks) multiplies tiles of ROWS x BN.  BH: columns of B that a block brings in.
 template <typename T> constexpr int GP_PARTS = sizeof(T) == 4 ? 3 : 1;
-template <typename T, int BN> constexpr int GP_STAGE_BYTES = GP_PARTS<T> * (128 + BN) * 128;
+template <bool PAIR> constexpr int GP_BN = PAIR ? 256 : 128;
+template <typename T> constexpr int GP_STAGE_BYTES = GP_PARTS<T> * (128 + 128) * 128;
 
-template <int MODE, typename T, int BN, bool TMA>
+template <int MODE, typename T, bool PAIR>
 __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
                                                                  const __grid_constant__ GroupedParams p)
 {
     LP_DEP_ENTER();
-    constexpr int PARTS = GP_PARTS<T>;
-    constexpr bool WGRAD = MODE == GP_WGRAD;
+    constexpr int PARTS = GP_PARTS<T>, BN = GP_BN<PAIR>, BH = 128, ROWS = PAIR ? 256 : 128;
+    constexpr bool WGRAD = MODE == GP_WGRAD, TMA_A = PARTS == 1, TMA_B = PARTS == 1 || !WGRAD;
     constexpr bool A_MN = WGRAD, B_MN = MODE != GP_NT;
-    constexpr int EPI = TMA ? 16 : 8, COLS = BN * 4 / EPI;  // warps of sums and results, columns of each
-    constexpr int LOADERS = TMA ? 0 : 8;
-    constexpr uint32_t a_bytes = 128 * 128, b_bytes = BN * 128, stage_bytes = GP_STAGE_BYTES<T, BN>;
-    static_assert(TMA ? PARTS == 1 : BN == 128, "TMA brings in BF16 operands, registers tiles of 128 columns");
+    constexpr int EPI = TMA_A ? 16 : 8, COLS = BN * 4 / EPI;  // warps of sums and results, columns of each
+    constexpr int LOADERS = TMA_A ? 0 : 8;
+    constexpr uint32_t a_bytes = 128 * 128, b_bytes = BH * 128, stage_bytes = GP_STAGE_BYTES<T>, tma_bytes = (TMA_A ? a_bytes : 0) + (TMA_B ? PARTS * b_bytes : 0);
+    static_assert(!PAIR || PARTS == 1, "pairs take BF16 operands");
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t bar_full[GP_MAX_STAGES], bar_empty[GP_MAX_STAGES], bar_acc_full[2], bar_acc_empty[2], bar_sum_full, bar_sum_empty, bar_done;
+    __shared__ __align__(8) uint64_t bar_full[GP_MAX_STAGES], bar_empty[GP_MAX_STAGES], bar_read[GP_MAX_STAGES], bar_acc_full[2], bar_acc_empty[2], bar_sum_full, bar_sum_empty,
+        bar_done, bar_tail;
     __shared__ uint32_t tmem_base_s;
     __shared__ int blocks_s;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    const int rank = PAIR ? (int)cluster_cta_rank() : 0, worker = PAIR ? blockIdx.x >> 1 : blockIdx.x, workers = PAIR ? gridDim.x >> 1 : gridDim.x;
+    const bool leader = rank == 0;  // of a pair: issues its matrix instructions
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     const int S = p.stages;
     uint8_t *extra = smem + (size_t)S * stage_bytes;
@@ -327,29 +371,30 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < S; ++s) {
-            mbar_init(smem_u32(&bar_full[s]), TMA ? 1 : LOADERS);
-            mbar_init(smem_u32(&bar_empty[s]), TMA && sums ? 1 + EPI : 1);
+            mbar_init(smem_u32(&bar_full[s]), (PAIR ? 2 : TMA_A || TMA_B ? 1 : 0) + LOADERS);
+            mbar_init(smem_u32(&bar_empty[s]), 1);
+            mbar_init(smem_u32(&bar_read[s]), EPI);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(smem_u32(&bar_acc_full[b]), 1);
-            mbar_init(smem_u32(&bar_acc_empty[b]), EPI);
+            mbar_init(smem_u32(&bar_acc_empty[b]), PAIR ? 2 * EPI : EPI);
         }
-        mbar_init(smem_u32(&bar_sum_full), TMA ? EPI : LOADERS);
-        mbar_init(smem_u32(&bar_sum_empty), BN / 32);
+        mbar_init(smem_u32(&bar_sum_full), TMA_A ? EPI : LOADERS);
+        mbar_init(smem_u32(&bar_sum_empty), BH / 32);
         mbar_init(smem_u32(&bar_done), 1);
+        mbar_init(smem_u32(&bar_tail), 1);
         fence_barrier_init();
         fence_async_proxy();
-        if (TMA) {
-            tma_prefetch_desc(&mapA);
-            tma_prefetch_desc(&mapB);
-        }
+        if (TMA_A) tma_prefetch_desc(&mapA);
+        if (TMA_B) tma_prefetch_desc(&mapB);
     }
     if (warp == 0) {
         __syncwarp();
-        tmem_alloc(smem_u32(&tmem_base_s), 2 * BN);
+        if (PAIR) tmem_alloc_pair(smem_u32(&tmem_base_s), 2 * BN);
+        else tmem_alloc(smem_u32(&tmem_base_s), 2 * BN);
     } else if (warp == 1) {
         if (WGRAD) {
-            GroupWalk<true> w(p);
+            GroupWalk<true, ROWS> w(p);
             const int n = w.all();
             if (lane == 0) blocks_s = n;
         }
@@ -360,56 +405,88 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
     }
     tc_fence_before();
     __syncthreads();
+    if (PAIR) cluster_barrier();  // both blocks' barriers are there before either uses the other's
     tc_fence_after();
     const uint32_t tmem = tmem_base_s;
     int64_t lo = 0, hi = 0, all = 0;
     if (WGRAD) {
         all = (int64_t)blocks_s * p.tiles_k * p.tiles_n;
-        lo = all * blockIdx.x / gridDim.x;
-        hi = all * (blockIdx.x + 1) / gridDim.x;
+        lo = all * worker / workers;
+        hi = all * (worker + 1) / workers;
     }
-    GroupedJobs<MODE> jobs(p, lo, hi);
+    GroupedJobs<MODE, ROWS> jobs(p, worker, workers, lo, hi);
     GroupedJob j;
 
     if (warp == 0) {
-        if (TMA) {
-            // ---- operands
-            int s = 0, round = 0;
+        if (TMA_A || TMA_B) {
+            // ---- operands by TMA: this block's 128 rows (weight gradient: columns) of A and its BH columns of B
+            int s = 0, round = 0, tails = 0;
             bool ok = true, first = blockIdx.x == (WGRAD ? gridDim.x - 1 : 0);  // a block that has work in any case
-            const bool chosen = elect_one();
-            const int chosen_lane = __ffs(__ballot_sync(0xffffffffu, chosen)) - 1;
             while (ok && jobs.next(j)) {
-                if (chosen) {
-                    for (int kb = 0; kb < j.kbs; ++kb) {
-                        if (round > 0 && !mbar_wait(smem_u32(&bar_empty[s]), (round & 1) ^ 1, p.wait_ns)) { atomicExch(p.err, 1); ok = false; break; }
-                        const uint32_t sa = smem_u32(smem) + s * stage_bytes, sb = sa + a_bytes, bar = smem_u32(&bar_full[s]);
-                        mbar_expect_tx(bar, stage_bytes + (first ? (uint32_t)p.extra_tx : 0u));
-                        first = false;
+                for (int kb = 0; kb < j.kbs && ok; ++kb) {
+                    if (round > 0) {
+                        ok = mbar_wait(smem_u32(&bar_empty[s]), (round & 1) ^ 1, p.wait_ns) && (!(TMA_A && sums) || mbar_wait(smem_u32(&bar_read[s]), (round & 1) ^ 1, p.wait_ns));
+                        ok = __all_sync(0xffffffffu, ok);
+                        if (!ok) { if (lane == 0) atomicExch(p.err, 1); break; }
+                    }
+                    const uint32_t sa = smem_u32(smem) + s * stage_bytes, sb = sa + PARTS * a_bytes;
+                    uint32_t bar = smem_u32(&bar_full[s]);
+                    const int have = j.row_end - (j.row0 + kb * 64);
+                    const bool tail = WGRAD && have < 64;  // the last rows of a group: they arrive here first
+                    if (elect_one()) {
+                        const uint32_t more = first ? (uint32_t)p.extra_tx : 0u;
+                        if (tail) {
+                            mbar_expect_tx(smem_u32(&bar_tail), tma_bytes + more);
+                            bar = smem_u32(&bar_tail);
+                            if (PAIR) bar = map_to_cta(bar, rank);
+                        } else if (PAIR) {
+                            bar = map_to_cta(bar, 0);
+                            mbar_expect_tx_remote(bar, tma_bytes + more);
+                        } else {
+                            mbar_expect_tx(bar, tma_bytes + more);
+                        }
                         if (WGRAD) {
                             const int row = j.row0 + kb * 64;
 #pragma unroll
-                            for (int c = 0; c < 2; ++c) tma_load_2d(sa + c * 8192, &mapA, bar, j.kt * 128 + c * 64, row);
+                            for (int c = 0; c < 2; ++c) tile_2d<PAIR>(sa + c * 8192, &mapA, bar, j.kt * ROWS + rank * 128 + c * 64, row);
 #pragma unroll
-                            for (int c = 0; c < BN / 64; ++c) tma_load_2d(sb + c * 8192, &mapB, bar, j.nt * BN + c * 64, row);
+                            for (int c = 0; c < 2; ++c) tile_2d<PAIR>(sb + c * 8192, &mapB, bar, j.nt * BN + rank * BH + c * 64, row);
                         } else {
-                            tma_load_2d(sa, &mapA, bar, kb * 64, j.row0);
-                            if (B_MN) {
+                            if (TMA_A) tile_2d<PAIR>(sa, &mapA, bar, kb * 64, j.row0 + rank * 128);
 #pragma unroll
-                                for (int c = 0; c < BN / 64; ++c) tma_load_3d(sb + c * 8192, &mapB, bar, j.nt * BN + c * 64, kb * 64, j.g);
-                            } else {
-                                tma_load_3d(sb, &mapB, bar, kb * 64, j.nt * BN, j.g);
+                            for (int q = 0; q < PARTS; ++q) {
+                                if (B_MN) {
+#pragma unroll
+                                    for (int c = 0; c < 2; ++c) tile_3d<PAIR>(sb + q * b_bytes + c * 8192, &mapB, bar, j.nt * BN + rank * BH + c * 64, kb * 64, q * p.groups + j.g);
+                                } else {
+                                    tile_3d<PAIR>(sb + q * b_bytes, &mapB, bar, kb * 64, j.nt * BN + rank * BH, q * p.groups + j.g);
+                                }
                             }
                         }
-                        if (++s == S) { s = 0; ++round; }
                     }
+                    __syncwarp();
+                    first = false;
+                    if (tail) {
+                        // rows behind the group belong to the next one (or to nobody): zeros in both operands, whatever they hold
+                        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_tail), tails & 1, p.wait_ns));
+                        if (!ok) { if (lane == 0) atomicExch(p.err, 2); break; }
+                        ++tails;
+                        uint8_t *st = smem + (size_t)s * stage_bytes + max(have, 0) * 128;
+                        for (int i = lane; i < (64 - max(have, 0)) * 8; i += 32)
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) *reinterpret_cast<uint4 *>(st + c * 8192 + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+                        fence_async_proxy();
+                        __syncwarp();
+                        if (lane == 0) {
+                            if (PAIR) mbar_arrive_remote(map_to_cta(smem_u32(&bar_full[s]), 0));
+                            else mbar_arrive(smem_u32(&bar_full[s]));
+                        }
+                    }
+                    if (++s == S) { s = 0; ++round; }
                 }
-                __syncwarp();
-                ok = __all_sync(0xffffffffu, ok);
             }
-            s = __shfl_sync(0xffffffffu, s, chosen_lane);
-            round = __shfl_sync(0xffffffffu, round, chosen_lane);
             // copies under way land before the block gives up its shared memory (after a wait that ran out; else they long have)
-            if (lane == 0)
+            if (lane == 0 && leader)
                 for (int i = 0; i < S; ++i) {
                     const int at = s - 1 - i < 0 ? s - 1 - i + S : s - 1 - i, r = s - 1 - i < 0 ? round - 1 : round;
                     if (r >= 0) mbar_wait(smem_u32(&bar_full[at]), r & 1, p.wait_ns);
@@ -420,13 +497,21 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
         // ---- products
         int s = 0, round = 0, use = 0;
         bool ok = true;
-        constexpr uint32_t idesc_mn = (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u);
-        const uint32_t idesc = make_idesc_bf16(BN, false, false) | idesc_mn;
+        const uint32_t idesc = (PAIR ? make_idesc_bf16_pair(BN) : make_idesc_bf16(BN, false, false)) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u);
         const uint64_t desc_a = make_smem_desc(smem_u32(smem), A_MN ? 8192 : 16, 1024), desc_b = make_smem_desc(smem_u32(smem) + PARTS * a_bytes, B_MN ? 8192 : 16, 1024);
         constexpr uint64_t step_a = (A_MN ? 2048 : 32) >> 4, step_b = (B_MN ? 2048 : 32) >> 4;
-        while (ok && jobs.next(j)) {
+        auto product = [&](uint32_t acc, uint64_t da, uint64_t db, bool more) {
+            if (PAIR) umma_bf16_pair(acc, da, db, idesc, more ? 1u : 0u);
+            else umma_bf16(acc, da, db, idesc, more ? 1u : 0u);
+        };
+        auto commit = [&](uint64_t &bar) {
+            if (PAIR) umma_commit_pair(smem_u32(&bar));
+            else umma_commit(smem_u32(&bar));
+        };
+        while (leader && ok && jobs.next(j)) {
+            int in_flush = 0;
             for (int kb = 0; kb < j.kbs && ok; ++kb) {
-                const int b = use & 1, in_flush = kb % p.flush;
+                const int b = use & 1;
                 if (in_flush == 0 && use >= 2 && !mbar_wait(smem_u32(&bar_acc_empty[b]), ((use >> 1) & 1) ^ 1, p.wait_ns)) {
                     if (lane == 0) atomicExch(p.err, 5);
                     ok = false;
@@ -438,90 +523,131 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_fence_after();
-                if (WGRAD && TMA) {
-                    // rows behind the group belong to the next one (or to nobody): zeros in both operands, whatever they hold
-                    const int have = j.row_end - (j.row0 + kb * 64);
-                    if (have < 64) {
-                        uint8_t *st = smem + (size_t)s * stage_bytes;
-                        for (int i = lane; i < (64 - max(have, 0)) * 8; i += 32)
-#pragma unroll
-                            for (int c = 0; c < 2 + BN / 64; ++c) *reinterpret_cast<uint4 *>(st + c * 8192 + max(have, 0) * 128 + i * 16) = make_uint4(0u, 0u, 0u, 0u);
-                        fence_async_proxy();
-                        __syncwarp();
-                    }
-                }
                 const bool done = in_flush == p.flush - 1 || kb == j.kbs - 1;
                 if (elect_one()) {
                     const uint64_t da = desc_a + ((s * stage_bytes) >> 4), db = desc_b + ((s * stage_bytes) >> 4);
                     const uint32_t acc = tmem + b * BN;
                     if (PARTS == 1) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) umma_bf16(acc, da + i * step_a, db + i * step_b, idesc, in_flush != 0 || i != 0 ? 1u : 0u);
+                        for (int i = 0; i < 4; ++i) product(acc, da + i * step_a, db + i * step_b, in_flush != 0 || i != 0);
                     } else {
                         constexpr int first[6] = {0, 2, 1, 0, 1, 0}, second[6] = {2, 0, 1, 1, 0, 0};  // the small products first, while the sums are small
 #pragma unroll
                         for (int q = 0; q < 6; ++q)
 #pragma unroll
                             for (int i = 0; i < 4; ++i)
-                                umma_bf16(acc, da + first[q] * (a_bytes >> 4) + i * step_a, db + second[q] * (b_bytes >> 4) + i * step_b, idesc,
-                                          in_flush != 0 || q != 0 || i != 0 ? 1u : 0u);
+                                product(acc, da + first[q] * (a_bytes >> 4) + i * step_a, db + second[q] * (b_bytes >> 4) + i * step_b, in_flush != 0 || q != 0 || i != 0);
                     }
-                    umma_commit(smem_u32(&bar_empty[s]));
-                    if (done) umma_commit(smem_u32(&bar_acc_full[b]));
+                    commit(bar_empty[s]);
+                    if (done) commit(bar_acc_full[b]);
                 }
                 __syncwarp();
+                in_flush = done ? 0 : in_flush + 1;
                 if (done) ++use;
                 if (++s == S) { s = 0; ++round; }
             }
         }
-        // products under way are done with the block's memory before it goes, also after a wait that ran out
-        if (elect_one()) umma_commit(smem_u32(&bar_done));
-        __syncwarp();
-        mbar_wait(smem_u32(&bar_done), 0, p.wait_ns);
+        // products under way are done with the memory of both blocks before they go, also after a wait that ran out
+        if (leader) {
+            if (elect_one()) commit(bar_done);
+            __syncwarp();
+            mbar_wait(smem_u32(&bar_done), 0, p.wait_ns);
+        }
         __syncwarp();
     } else if (warp < 2 + EPI) {
         // ---- sums and results: 32 rows x COLS columns per warp
         const int quarter = warp & 3, part = (warp - 2) >> 2;
         const int epi_thread = threadIdx.x - 64;
-        float *stage = reinterpret_cast<float *>(extra) + (warp - 2) * 512;
+        uint8_t *stage = extra + (warp - 2) * 2048;
+        const uint32_t acc_free = PAIR ? map_to_cta(smem_u32(&bar_acc_empty[0]), 0) : smem_u32(&bar_acc_empty[0]);
         int use = 0, s = 0, round = 0, summed = 0;
         bool ok = true;
         GroupedSplit split{0, 0, 0, -1, 0, 0};
+        // the accumulator that holds the next sums; false when the wait ran out
+        auto take = [&](uint32_t &at) {
+            const int b = use & 1;
+            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_acc_full[b]), (use >> 1) & 1, p.wait_ns));
+            if (!ok) { if (lane == 0) atomicExch(p.err, 3); return false; }
+            tc_fence_after();
+            at = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(b * BN + part * COLS);
+            return true;
+        };
+        auto give_back = [&]() {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if (PAIR) mbar_arrive_remote(acc_free + (use & 1) * 8);
+                else mbar_arrive(acc_free + (use & 1) * 8);
+            }
+            ++use;
+        };
         while (ok && jobs.next(j)) {
+            const int c0 = j.nt * BN + part * COLS;  // first column of this warp
+            if (!WGRAD && PARTS == 1) {
+                // one accumulator holds all terms: from tensor memory straight to the result
+                const int row = j.row0 + rank * 128 + quarter * 32;
+                T *dst = (T *)p.C + (int64_t)row * p.ldc + c0;
+                const float *bias = p.bias ? p.bias + (int64_t)j.g * p.N + c0 : nullptr;
+                uint32_t at;
+                if (!take(at)) break;
+                constexpr int PC = PUT_COLS<T>;
+#pragma unroll
+                for (int c = 0; c < COLS; c += PC) {
+                    float v[PC];
+#pragma unroll
+                    for (int i = 0; i < PC; i += 16) tmem_ld_32x16(at + c + i, v + i);
+                    tmem_ld_wait();
+                    if (c + PC >= COLS) give_back();  // read, if not written yet
+                    if (c0 + c >= p.N) continue;
+                    if (bias) {
+                        // a column per lane, handed round
+                        const float mine = PC == 32 || lane < 16 ? (c0 + c + lane < p.N ? __ldg(bias + c + lane) : 0.f) : 0.f;
+#pragma unroll
+                        for (int i = 0; i < PC; ++i) v[i] += __shfl_sync(0xffffffffu, mine, i);
+                    }
+                    if (p.relu)
+#pragma unroll
+                        for (int i = 0; i < PC; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];  // NaN stays
+                    put_columns<T>(dst + c, p.ldc, j.row_end - row, p.N - (c0 + c), v, p.vec_c, stage, false);
+                }
+                continue;
+            }
             float v[COLS];
 #pragma unroll
             for (int c = 0; c < COLS; ++c) v[c] = 0.f;
             float col[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            const bool adds = sums && TMA && j.kt == 0;
+            const bool adds = sums && TMA_A && j.kt == 0;
+            int in_flush = 0;
             for (int kb = 0; kb < j.kbs && ok; ++kb) {
-                if (TMA && sums) {
-                    // column sums of dZ out of the staged tiles: eight columns (piece of 16 bytes) of a few rows per thread
-                    constexpr int PIECES = BN / 8, ROWS = 64 * PIECES / (EPI * 32);
-                    ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_full[s]), round & 1, p.wait_ns));
+                if (TMA_A && sums) {
+                    // column sums of dZ out of the staged tiles, once their products are done: eight columns (a piece of 16 bytes) of two rows per thread
+                    constexpr int PIECES = BH / 8, RPT = 64 * PIECES / (EPI * 32);
+                    ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_empty[s]), round & 1, p.wait_ns));
                     if (!ok) { if (lane == 0) atomicExch(p.err, 4); break; }
                     if (adds) {
-                        const int piece = epi_thread % PIECES, r0 = epi_thread / PIECES * ROWS, have = j.row_end - (j.row0 + kb * 64);
+                        const int piece = epi_thread % PIECES, r0 = epi_thread / PIECES * RPT, have = j.row_end - (j.row0 + kb * 64);
                         const uint8_t *sb = smem + (size_t)s * stage_bytes + a_bytes + (piece >> 3) * 8192;
 #pragma unroll
-                        for (int i = 0; i < ROWS; ++i) {
+                        for (int i = 0; i < RPT; ++i) {
                             const int r = r0 + i;
                             if (r < have) {
-                                Piece8<bf16> x;
-                                x.w = *reinterpret_cast<const uint4 *>(sb + r * 128 + (((piece & 7) ^ (r & 7)) << 4));
-                                x.add_to(col);
+                                Vec16<bf16> x;
+                                x.v = *reinterpret_cast<const uint4 *>(sb + r * 128 + (((piece & 7) ^ (r & 7)) << 4));
+                                float f[8];
+                                x.to_float(f);
+                                add8(col, f);
                             }
                         }
                         __syncwarp();
                     }
-                    if (lane == 0) mbar_arrive(smem_u32(&bar_empty[s]));
+                    if (lane == 0) mbar_arrive(smem_u32(&bar_read[s]));
                     if (++s == S) { s = 0; ++round; }
                 }
-                if (kb % p.flush != p.flush - 1 && kb != j.kbs - 1) continue;
-                const int b = use & 1;
-                ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_acc_full[b]), (use >> 1) & 1, p.wait_ns));
-                if (!ok) { if (lane == 0) atomicExch(p.err, 3); break; }
-                tc_fence_after();
-                const uint32_t at = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(b * BN + part * COLS);
+                const bool done = in_flush == p.flush - 1 || kb == j.kbs - 1;
+                in_flush = done ? 0 : in_flush + 1;
+                if (!done) continue;
+                uint32_t at;
+                if (!take(at)) break;
 #pragma unroll
                 for (int c = 0; c < COLS; c += 16) {
                     float x[16];
@@ -530,53 +656,53 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
 #pragma unroll
                     for (int i = 0; i < 16; ++i) v[c + i] += x[i];
                 }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&bar_acc_empty[b]));
-                ++use;
+                give_back();
             }
             if (!ok) break;
             if (summed > 0) {  // the column sums of the job before have been read
                 ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_sum_empty), (summed - 1) & 1, p.wait_ns));
                 if (!ok) { if (lane == 0) atomicExch(p.err, 7); break; }
             }
-            const int c0 = j.nt * BN + part * COLS;  // first column of this warp
             if (!WGRAD) {
                 const int row = j.row0 + quarter * 32;
                 T *dst = (T *)p.C + (int64_t)row * p.ldc + c0;
                 const float *bias = p.bias ? p.bias + (int64_t)j.g * p.N + c0 : nullptr;
+                constexpr int PC = PUT_COLS<T>;
 #pragma unroll
-                for (int c = 0; c < COLS; c += 16) {
+                for (int c = 0; c < COLS; c += PC) {
                     if (c0 + c >= p.N) break;
-                    if (bias)
+                    if (bias) {
+                        const float mine = lane < PC && c0 + c + lane < p.N ? __ldg(bias + c + lane) : 0.f;
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) v[c + i] += c0 + c + i < p.N ? __ldg(bias + c + i) : 0.f;
+                        for (int i = 0; i < PC; ++i) v[c + i] += __shfl_sync(0xffffffffu, mine, i);
+                    }
                     if (p.relu)
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) v[c + i] = v[c + i] > 0.f || v[c + i] != v[c + i] ? v[c + i] : 0.f;  // NaN stays
-                    put16<T>(dst + c, p.ldc, j.row_end - row, p.N - (c0 + c), v + c, p.vec_c, stage, false);
+                        for (int i = 0; i < PC; ++i) v[c + i] = v[c + i] < 0.f ? 0.f : v[c + i];
+                    put_columns<T>(dst + c, p.ldc, j.row_end - row, p.N - (c0 + c), v + c, p.vec_c, stage, false);
                 }
             } else if (j.slot < 0) {
-                const int row = j.kt * 128 + quarter * 32;
+                const int row = j.kt * ROWS + rank * 128 + quarter * 32;
                 float *dst = p.dW + ((int64_t)j.g * p.K + row) * p.N + c0;
 #pragma unroll
                 for (int c = 0; c < COLS; c += 16)
-                    if (c0 + c < p.N) put16<float>(dst + c, p.N, p.K - row, p.N - (c0 + c), v + c, p.vec_c, stage, p.accumulate != 0);
+                    if (c0 + c < p.N) put_columns<float>(dst + c, p.N, p.K - row, p.N - (c0 + c), v + c, p.vec_c, stage, p.accumulate != 0);
             } else {
-                float *dst = p.slots + ((size_t)j.slot * 129 + quarter * 32 + lane) * BN + part * COLS;
+                float *dst = p.slots + (((size_t)j.slot * (ROWS / 128) + rank) * 129 + quarter * 32) * BN + part * COLS;
 #pragma unroll
-                for (int c = 0; c < COLS; c += 4) *reinterpret_cast<float4 *>(dst + c) = make_float4(v[c], v[c + 1], v[c + 2], v[c + 3]);
+                for (int c = 0; c < COLS; c += 16) put_columns<float>(dst + c, BN, 32, 16, v + c, 1, stage, false);
             }
             if (adds) {
-                // every warp leaves its sums of a few rows in its own part of the area; the first BN threads add them up in order
-                constexpr int PIECES = BN / 8, SHARES = EPI * 32 / PIECES;
-                float *area = reinterpret_cast<float *>(extra);
+                // every warp leaves its sums of a few rows in its own part of the area; the first BH threads add them up in order
+                constexpr int PIECES = BH / 8, SHARES = EPI * 32 / PIECES;
+                const float *area = reinterpret_cast<const float *>(extra);
+                float *own = reinterpret_cast<float *>(stage);
                 __syncwarp();
 #pragma unroll
-                for (int i = 0; i < 8; ++i) stage[lane * 8 + i] = col[i];
+                for (int i = 0; i < 8; ++i) own[lane * 8 + i] = col[i];
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&bar_sum_full));
-                if (epi_thread < BN) {
+                if (epi_thread < BH) {
                     ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_sum_full), summed & 1, p.wait_ns));
                     if (!ok) { if (lane == 0) atomicExch(p.err, 7); break; }
                     float x = 0.f;
@@ -585,8 +711,8 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
                         const int writer = i * PIECES + epi_thread / 8;  // thread that has these columns of share i
                         x += area[(writer >> 5) * 512 + (writer & 31) * 8 + (epi_thread & 7)];
                     }
-                    const int c = j.nt * BN + epi_thread;
-                    if (j.slot >= 0) p.slots[((size_t)j.slot * 129 + 128) * BN + epi_thread] = x;
+                    const int in_tile = rank * BH + epi_thread, c = j.nt * BN + in_tile;
+                    if (j.slot >= 0) p.slots[(((size_t)j.slot * (ROWS / 128) + rank) * 129 + 128) * BN + in_tile] = x;
                     else if (c < p.N) {
                         float *d = p.dbias + (int64_t)j.g * p.N + c;
                         *d = p.accumulate ? *d + x : x;
@@ -596,97 +722,118 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
                 }
                 ++summed;
             }
-            // of the shares of a block only the last can begin a tile that others go on with
+            // of the shares of a worker only the last can begin a tile that others go on with
             if (WGRAD && j.slot >= 0 && j.begins)
-                split = GroupedSplit{j.g, j.kt, j.nt, j.slot, (int)((j.tile_end * gridDim.x - 1) / all), all};
+                split = GroupedSplit{j.g, j.kt, j.nt, j.slot, (int)((j.tile_end * workers - 1) / all), all};
         }
         if (WGRAD && warp == 2 && lane == 0) p.splits[blockIdx.x] = split;
-    } else if (!TMA) {
-        // ---- operands through registers: four pieces of each operand per thread and block of 64 terms.  The pieces of the second
-        // operand are under way while those of the first are put down, and the first's next ones while those of the second are.
+    } else if (!TMA_A) {
+        // ---- FP32 operands through registers, a block of 64 terms in two halves (of A alone, or A and dZ): while the pieces of one are
+        // put down, those of the next are under way
+        constexpr bool BOTH = !TMA_B;
         const int lt = threadIdx.x - (2 + EPI) * 32;
         int s = 0, round = 0, summed = 0;
         bool ok = true;
-        Piece8<T> a[4], bq[4];
+        Piece8 x[4], y[4];
         float col[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        auto load = [&](Piece8<T> (&x)[4], const T *base, int64_t ld, int row, int row_end, int col0, int limit, int vec, bool mn) {
+        auto load = [&](Piece8 (&d)[4], const float *base, int64_t ld, int row, int row_end, int col0, int limit, bool mn) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int q = lt + 256 * i, r = row + (mn ? q >> 4 : q >> 3), c = col0 + 8 * (mn ? q & 15 : q & 7);
-                if (r < row_end && c < limit) x[i].load(base + (int64_t)r * ld, c, limit, vec);
-                else x[i].zero();
+                if (r < row_end && c < limit) d[i].load(base + (int64_t)r * ld, c, limit);
+                else d[i].zero();
             }
         };
-        auto load_a = [&](const GroupedJob &w, int kb) {
-            if (WGRAD) load(a, (const T *)p.A, p.lda, w.row0 + kb * 64, w.row_end, w.kt * 128, p.K, p.vec_a, true);
-            else load(a, (const T *)p.A, p.lda, w.row0, w.row_end, kb * 64, p.K, p.vec_a, false);
+        auto load_a = [&](Piece8 (&d)[4], const GroupedJob &w, int kb) {
+            if (WGRAD) load(d, (const float *)p.A, p.lda, w.row0 + kb * 64, w.row_end, w.kt * 128, p.K, true);
+            else load(d, (const float *)p.A, p.lda, w.row0, w.row_end, kb * 64, p.K, false);
         };
-        auto load_b = [&](const GroupedJob &w, int kb) {
-            const T *b = (const T *)p.B + (WGRAD ? 0 : (int64_t)w.g * p.stride_b);
-            if (WGRAD) load(bq, b, p.ldb, w.row0 + kb * 64, w.row_end, w.nt * 128, p.N, p.vec_b, true);
-            else if (MODE == GP_NN) load(bq, b, p.ldb, kb * 64, p.K, w.nt * 128, p.N, p.vec_b, true);
-            else load(bq, b, p.ldb, w.nt * 128, p.N, kb * 64, p.K, p.vec_b, false);
-        };
-        auto put = [&](const Piece8<T> (&x)[4], uint8_t *dst, uint32_t part, bool mn) {
+        auto put = [&](const Piece8 (&d)[4], uint8_t *dst, uint32_t part, bool mn) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int q = lt + 256 * i, r = mn ? q >> 4 : q >> 3, c = mn ? q & 15 : q & 7;
-                x[i].store(dst + (c >> 3) * 8192 + r * 128 + (((c & 7) ^ (r & 7)) << 4), part);
+                uint8_t *at = dst + (c >> 3) * 8192 + r * 128 + (((c & 7) ^ (r & 7)) << 4);
+                d[i].parts([&](int k, const uint4 &w) { *reinterpret_cast<uint4 *>(at + k * part) = w; });
             }
         };
-        int kb = 0;
-        bool more = jobs.next(j);
-        if (more) load_a(j, 0);
-        while (more && ok) {
-            load_b(j, kb);
+        auto free_stage = [&]() {
             if (round > 0) {
                 ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_empty[s]), (round & 1) ^ 1, p.wait_ns));
-                if (!ok) { if (lane == 0) atomicExch(p.err, 1); break; }
+                if (!ok && lane == 0) atomicExch(p.err, 1);
             }
-            uint8_t *st = smem + (size_t)s * stage_bytes;
-            put(a, st, a_bytes, A_MN);
-            const GroupedJob cur = j;
-            const bool last = ++kb == j.kbs;
-            if (last) {
-                kb = 0;
-                more = jobs.next(j);
-            }
-            if (more) load_a(j, kb);
-            put(bq, st + PARTS * a_bytes, b_bytes, B_MN);
+            return ok;
+        };
+        auto full_stage = [&]() {
             fence_async_proxy();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&bar_full[s]));
             if (++s == S) { s = 0; ++round; }
-            if (sums && cur.kt == 0) {
+        };
+        int kb = 0;
+        bool more = jobs.next(j);
+        auto advance = [&]() {  // true: that was the job's last block
+            if (++kb < j.kbs) return false;
+            kb = 0;
+            more = jobs.next(j);
+            return true;
+        };
+        if (more) load_a(x, j, 0);
+        if (!BOTH) {
+            while (more) {
+                advance();
+                if (more) load_a(y, j, kb);
+                if (!free_stage()) break;
+                put(x, smem + (size_t)s * stage_bytes, a_bytes, A_MN);
+                full_stage();
+                if (!more) break;
+                advance();
+                if (more) load_a(x, j, kb);
+                if (!free_stage()) break;
+                put(y, smem + (size_t)s * stage_bytes, a_bytes, A_MN);
+                full_stage();
+            }
+        } else {
+            while (more) {
+                load(y, (const float *)p.B, p.ldb, j.row0 + kb * 64, j.row_end, j.nt * 128, p.N, true);
+                if (!free_stage()) break;
+                uint8_t *st = smem + (size_t)s * stage_bytes;
+                put(x, st, a_bytes, A_MN);
+                const GroupedJob cur = j;
+                const bool last = advance();
+                if (more) load_a(x, j, kb);
+                put(y, st + PARTS * a_bytes, b_bytes, B_MN);
+                full_stage();
+                if (sums && cur.kt == 0) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) bq[i].add_to(col);
-                if (last) {
-                    // a thread has the rows 16 i + lt / 16 of its eight columns: sixteen sums per column, added up in order
-                    float *area = reinterpret_cast<float *>(extra) + EPI * 512;
-                    if (summed > 0) {
-                        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_sum_empty), (summed - 1) & 1, p.wait_ns));
-                        if (!ok) { if (lane == 0) atomicExch(p.err, 7); break; }
-                    }
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) { area[(lt >> 4) * 128 + (lt & 15) * 8 + i] = col[i]; col[i] = 0.f; }
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(smem_u32(&bar_sum_full));
-                    if (lt < 128) {
-                        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_sum_full), summed & 1, p.wait_ns));
-                        if (!ok) { if (lane == 0) atomicExch(p.err, 7); break; }
-                        float x = 0.f;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) x += area[i * 128 + lt];
-                        const int c = cur.nt * 128 + lt;
-                        if (cur.slot >= 0) p.slots[((size_t)cur.slot * 129 + 128) * BN + lt] = x;
-                        else if (c < p.N) {
-                            float *d = p.dbias + (int64_t)cur.g * p.N + c;
-                            *d = p.accumulate ? *d + x : x;
+                    for (int i = 0; i < 4; ++i) add8(col, y[i].v);
+                    if (last) {
+                        // a thread has the rows 16 i + lt / 16 of its eight columns: sixteen sums per column, added up in order
+                        float *area = reinterpret_cast<float *>(extra) + EPI * 512;
+                        if (summed > 0) {
+                            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_sum_empty), (summed - 1) & 1, p.wait_ns));
+                            if (!ok) { if (lane == 0) atomicExch(p.err, 7); break; }
                         }
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) { area[(lt >> 4) * 128 + (lt & 15) * 8 + i] = col[i]; col[i] = 0.f; }
                         __syncwarp();
-                        if (lane == 0) mbar_arrive(smem_u32(&bar_sum_empty));
+                        if (lane == 0) mbar_arrive(smem_u32(&bar_sum_full));
+                        if (lt < 128) {
+                            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_sum_full), summed & 1, p.wait_ns));
+                            if (!ok) { if (lane == 0) atomicExch(p.err, 7); break; }
+                            float v = 0.f;
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) v += area[i * 128 + lt];
+                            const int c = cur.nt * 128 + lt;
+                            if (cur.slot >= 0) p.slots[((size_t)cur.slot * 129 + 128) * BN + lt] = v;
+                            else if (c < p.N) {
+                                float *d = p.dbias + (int64_t)cur.g * p.N + c;
+                                *d = p.accumulate ? *d + v : v;
+                            }
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(smem_u32(&bar_sum_empty));
+                        }
+                        ++summed;
                     }
-                    ++summed;
                 }
             }
         }
@@ -694,39 +841,42 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
     __syncwarp();
     tc_fence_before();
     __syncthreads();
+    if (PAIR) cluster_barrier();  // neither block frees tensor memory, or leaves with barriers the other may still signal, before both are done
     if (warp == 0) {
         __syncwarp();
-        tmem_dealloc(tmem, 2 * BN);
+        if (PAIR) tmem_dealloc_pair(tmem, 2 * BN);
+        else tmem_dealloc(tmem, 2 * BN);
     }
 }
 
-// tiles that several blocks share: their partial tiles added in the order of the blocks.  gridDim.x = blocks of the product
-template <int BN> __global__ void __launch_bounds__(256) grouped_splits_kernel(const __grid_constant__ GroupedParams p)
+// tiles that several workers share: their partial tiles added in the order of the workers.  gridDim.x = blocks of the product
+template <bool PAIR> __global__ void __launch_bounds__(256) grouped_splits_kernel(const __grid_constant__ GroupedParams p)
 {
     LP_DEP_ENTER();
     const GroupedSplit sp = p.splits[blockIdx.x];
     if (sp.first_slot < 0) return;
-    constexpr int EACH = 4;
+    constexpr int EACH = 4, BN = GP_BN<PAIR>, BLOCKS = PAIR ? 2 : 1;  // blocks of a worker
+    const int worker = blockIdx.x / BLOCKS, rank = blockIdx.x % BLOCKS, workers = gridDim.x / BLOCKS;
     float v[EACH];
     const int at = blockIdx.y * 256 * EACH + threadIdx.x, size = 129 * BN;
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) v[i] = at + 256 * i < size ? p.slots[(size_t)sp.first_slot * size + at + 256 * i] : 0.f;
-    for (int c = (int)blockIdx.x + 1; c <= sp.last_block; ++c) {
-        if (sp.blocks * c / gridDim.x == sp.blocks * (c + 1) / gridDim.x) continue;  // a block without a share
+    for (int i = 0; i < EACH; ++i) v[i] = at + 256 * i < size ? p.slots[((size_t)sp.first_slot * BLOCKS + rank) * size + at + 256 * i] : 0.f;
+    for (int c = worker + 1; c <= sp.last_block; ++c) {
+        if (sp.blocks * c / workers == sp.blocks * (c + 1) / workers) continue;  // a worker without a share
 #pragma unroll
         for (int i = 0; i < EACH; ++i)
-            if (at + 256 * i < size) v[i] += p.slots[(size_t)(2 * c) * size + at + 256 * i];
+            if (at + 256 * i < size) v[i] += p.slots[((size_t)(2 * c) * BLOCKS + rank) * size + at + 256 * i];
     }
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-        const int row = (at + 256 * i) / BN, col = sp.nt * BN + (at + 256 * i) % BN, k = sp.kt * 128 + row;
+        const int row = (at + 256 * i) / BN, in_tile = (at + 256 * i) % BN, col = sp.nt * BN + in_tile, k = (sp.kt * BLOCKS + rank) * 128 + row;
         if (row > 128 || col >= p.N) continue;
         float *d;
         if (row < 128) {
             if (k >= p.K) continue;
             d = p.dW + ((int64_t)sp.group * p.K + k) * p.N + col;
         } else {
-            if (!p.dbias || sp.kt != 0) continue;
+            if (!p.dbias || sp.kt != 0 || in_tile / 128 != rank) continue;  // a block adds up the 128 columns it brings in
             d = p.dbias + (int64_t)sp.group * p.N + col;
         }
         *d = p.accumulate ? *d + v[i] : v[i];
@@ -736,24 +886,23 @@ template <int BN> __global__ void __launch_bounds__(256) grouped_splits_kernel(c
 // ---------------------------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------------------------
-template <int MODE, typename T, int BN, bool TMA> static bool grouped_init_one(std::string &err)
+template <int MODE, typename T, bool PAIR> static bool grouped_init_one(std::string &err)
 {
-    if (cudaFuncSetAttribute(grouped_kernel<MODE, T, BN, TMA>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024 - 1024) == cudaSuccess) return true;
+    if (cudaFuncSetAttribute(grouped_kernel<MODE, T, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024 - 1024) == cudaSuccess) return true;
     err = "cannot raise the dynamic shared memory limit of the grouped products";
     return false;
 }
 template <int MODE> static bool grouped_init_mode(std::string &err)
 {
-    return grouped_init_one<MODE, bf16, 128, true>(err) && grouped_init_one<MODE, bf16, 256, true>(err) && grouped_init_one<MODE, bf16, 128, false>(err) &&
-           grouped_init_one<MODE, float, 128, false>(err);
+    return grouped_init_one<MODE, bf16, false>(err) && grouped_init_one<MODE, bf16, true>(err) && grouped_init_one<MODE, float, false>(err);
 }
 static bool grouped_init(std::string &err) { return grouped_init_mode<GP_NN>(err) && grouped_init_mode<GP_NT>(err) && grouped_init_mode<GP_WGRAD>(err); }
 
-// tensor map over [groups][rows][cols] BF16 matrices behind one another
-static bool grouped_map_3d(const TcState &tc, CUtensorMap *map, const bf16 *base, int64_t groups, int64_t rows, int64_t cols, int box_rows, std::string &err)
+// tensor map over [matrices][rows][cols] BF16 matrices behind one another in rows of ld
+static bool grouped_map_3d(const TcState &tc, CUtensorMap *map, const bf16 *base, int64_t matrices, int64_t rows, int64_t cols, int64_t ld, int box_rows, std::string &err)
 {
-    cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)groups};
-    cuuint64_t strides[2] = {(cuuint64_t)cols * 2, (cuuint64_t)cols * (cuuint64_t)rows * 2};
+    cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)matrices};
+    cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)ld * (cuuint64_t)rows * 2};
     cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1}, estr[3] = {1, 1, 1};
     if (tc.encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, (void *)base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS)
@@ -762,61 +911,130 @@ static bool grouped_map_3d(const TcState &tc, CUtensorMap *map, const bf16 *base
     return false;
 }
 
-template <int MODE, typename T, int BN, bool TMA> static void grouped_launch_one(Exec &ex, const CUtensorMap &a, const CUtensorMap &b, GroupedParams &p, int blocks)
+template <int MODE, typename T, bool PAIR> static void grouped_launch_one(Exec &ex, const CUtensorMap &a, const CUtensorMap &b, GroupedParams &p, int blocks)
 {
-    constexpr int stage = GP_STAGE_BYTES<T, BN>;
+    constexpr int stage = GP_STAGE_BYTES<T>;
     p.stages = std::min(GP_MAX_STAGES, (227 * 1024 - 1024 - 1024 - GP_EXTRA_SMEM) / stage);
     const size_t smem = (size_t)p.stages * stage + GP_EXTRA_SMEM + 1024;
-    launch_dep(grouped_kernel<MODE, T, BN, TMA>, dim3((unsigned)blocks), dim3(GP_THREADS), smem, ex.st, a, b, p);
+    if (PAIR) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)blocks);
+        cfg.blockDim = dim3(GP_THREADS);
+        cfg.dynamicSmemBytes = smem;
+        cfg.stream = ex.st;
+        cudaLaunchAttribute attr[2];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = 2;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[1].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 2;
+        cudaLaunchKernelEx(&cfg, grouped_kernel<MODE, T, PAIR>, a, b, p);
+    } else {
+        launch_dep(grouped_kernel<MODE, T, PAIR>, dim3((unsigned)blocks), dim3(GP_THREADS), smem, ex.st, a, b, p);
+    }
     ex.launches += 1;
     if (MODE == GP_WGRAD) {
-        launch_dep(grouped_splits_kernel<BN>, dim3((unsigned)blocks, (unsigned)ceil_div64(129 * BN, 1024)), dim3(256), 0, ex.st, p);
+        launch_dep(grouped_splits_kernel<PAIR>, dim3((unsigned)blocks, (unsigned)ceil_div64(129 * GP_BN<PAIR>, 1024)), dim3(256), 0, ex.st, p);
         ex.launches += 1;
     }
 }
 
-struct GroupedPlan {
-    bool tma;
-    int bn, blocks;
-    size_t slots_bytes;  // weight gradient; the notes on shared tiles follow
+// an operand and, where its rows have to be copied or split first, its place in the workspace
+struct GroupedOperand {
+    const void *at;
+    int64_t matrices, rows;    // rows: of a matrix
+    int cols;
+    int64_t ld;
+    bool split;                // FP32 into three BF16 parts
+    bool copied = false;
+    size_t bytes = 0, offset = 0;
 };
-template <typename T> static bool grouped_tma(const void *A, int64_t lda, const void *B, int64_t ldb)
+template <typename T> static GroupedOperand grouped_operand(const void *at, int64_t matrices, int64_t rows, int cols, int64_t ld, bool split, size_t &ws)
 {
-    return sizeof(T) == 2 && on_16_bytes<T>(A, lda) && on_16_bytes<T>(B, ldb);
+    GroupedOperand o{at, matrices, rows, cols, ld, split};
+    o.copied = split || !on_16_bytes<T>(at, ld);
+    if (o.copied) {
+        const int64_t step = split ? 8 : 16 / (int64_t)sizeof(T);
+        o.ld = ceil_div64(cols, step) * step;
+        o.bytes = (size_t)(o.ld * rows * matrices) * (split ? 6 : sizeof(T));
+        o.offset = ws;
+        ws += (o.bytes + 255) & ~(size_t)255;
+    }
+    return o;
 }
-// tiles of 256 columns where they keep every SM busy, of 128 elsewhere and for operands through registers
-static GroupedPlan grouped_plan(bool tma, bool wgrad, int64_t rows, int64_t groups, int N, int K)
+// makes the copy; the operand is then where `at` says
+template <typename T> static void grouped_prepare(Exec &ex, GroupedOperand &o, int64_t ld_in, uint8_t *ws)
 {
+    if (!o.copied) return;
+    const int64_t rows = o.matrices * o.rows;
+    void *out = ws + o.offset;
+    if (o.split) {
+        launch_dep(grouped_split_kernel, dim3((unsigned)ceil_div64(rows * (o.ld / 8), 256)), dim3(256), 0, ex.st, (const float *)o.at, rows, o.cols,
+                   (int)(on_16_bytes<float>(o.at, ld_in)), (bf16 *)out, o.ld, o.ld * rows);
+    } else {
+        constexpr int E = 16 / sizeof(T);
+        launch_dep(grouped_align_kernel<T>, dim3((unsigned)ceil_div64(rows * (o.ld / E), 256)), dim3(256), 0, ex.st, (const T *)o.at, rows, o.cols, ld_in, (T *)out, o.ld);
+    }
+    ex.launches += 1;
+    o.at = out;
+}
+
+struct GroupedPlan {
+    bool pair;
+    int blocks;
+    GroupedOperand a, b;
+    size_t slots, splits, bytes;  // places in the workspace and its size
+};
+// Pairs of SMs and tiles of 256 x 256 where those keep most SMs busy (weight gradient: where the matrix fills such a tile), blocks of their
+// own and tiles of 128 x 128 elsewhere and for FP32
+template <int MODE, typename T> static GroupedPlan grouped_plan(int64_t rows, int64_t groups, int N, int K, const void *A, int64_t lda, const void *B, int64_t ldb)
+{
+    constexpr bool WGRAD = MODE == GP_WGRAD;
     GroupedPlan g{};
+    g.a = grouped_operand<T>(A, 1, rows, K, lda, false, g.bytes);
+    g.b = WGRAD ? grouped_operand<T>(B, 1, rows, N, ldb, false, g.bytes)
+                : grouped_operand<T>(B, groups, MODE == GP_NN ? K : N, MODE == GP_NN ? N : K, ldb, sizeof(T) == 4, g.bytes);
     const int64_t sms = tc_sm_count(), busy = std::min(rows, groups);
-    g.tma = tma;
-    auto tiles = [&](int bn) { return (wgrad ? (ceil_div64(rows, 64) + groups) * ceil_div64(K, 128) : ceil_div64(rows, 128) + busy) * ceil_div64(N, bn); };
-    g.bn = tma && N > 128 && (wgrad || tiles(256) >= sms) ? 256 : 128;
-    g.blocks = (int)std::min<int64_t>(sms, std::max<int64_t>(1, tiles(g.bn)));
-    g.slots_bytes = wgrad ? sizeof(float) * (size_t)2 * g.blocks * 129 * g.bn : 0;
+    auto tiles = [&](int side) { return (WGRAD ? (ceil_div64(rows, 64) + groups) * ceil_div64(K, side) : ceil_div64(rows, side) + busy) * ceil_div64(N, side); };
+    g.pair = sizeof(T) == 2 && N > 128 && (WGRAD ? K > 128 && rows >= 2048 : ceil_div64(rows, 256) * ceil_div64(N, 256) * 4 >= sms);
+    g.blocks = g.pair ? 2 * (int)std::min<int64_t>(sms / 2, std::max<int64_t>(1, tiles(256))) : (int)std::min<int64_t>(sms, std::max<int64_t>(1, tiles(128)));
+    if (WGRAD) {
+        g.slots = g.bytes;
+        g.splits = g.slots + sizeof(float) * (size_t)2 * g.blocks * 129 * (g.pair ? 256 : 128);
+        g.bytes = g.splits + sizeof(GroupedSplit) * (size_t)g.blocks;
+    }
     return g;
 }
-template <int MODE, typename T> static bool grouped_launch(TcState &tc, Exec &ex, GroupedParams &p, const GroupedPlan &g, std::string &err)
+template <int MODE, typename T> static bool grouped_launch(TcState &tc, Exec &ex, GroupedParams &p, GroupedPlan &g, int64_t lda, int64_t ldb, uint8_t *ws, std::string &err)
 {
     CUtensorMap a{}, b{};
-    p.tiles_n = (int)ceil_div64(p.N, g.bn);
-    p.tiles_k = (int)ceil_div64(p.K, 128);
-    p.vec_a = on_16_bytes<T>(p.A, p.lda);
-    p.vec_b = on_16_bytes<T>(p.B, p.ldb) && on_16_bytes<T>(p.B, p.stride_b);
+    constexpr bool WGRAD = MODE == GP_WGRAD;
+    const int side = g.pair ? 256 : 128;
+    p.tiles_n = (int)ceil_div64(p.N, side);
+    p.tiles_k = (int)ceil_div64(p.K, side);
     p.err = tc.err_word;
     p.wait_ns = tc.wait_limit_ns;
-    p.extra_tx = g.tma ? tc.overdeclare_tx : 0;
-    if (g.tma) {
-        tc.overdeclare_tx = 0;
-        const bf16 *A = (const bf16 *)p.A, *B = (const bf16 *)p.B;
-        if (!tc_make_map(tc, &a, A, p.rows, p.K, p.lda, 64, MODE == GP_WGRAD ? 64 : 128, err)) return false;
-        if (MODE == GP_WGRAD ? !tc_make_map(tc, &b, B, p.rows, p.N, p.ldb, 64, 64, err)
-                             : !grouped_map_3d(tc, &b, B, p.groups, MODE == GP_NN ? p.K : p.N, MODE == GP_NN ? p.N : p.K, MODE == GP_NN ? 64 : g.bn, err))
-            return false;
+    p.extra_tx = sizeof(T) == 2 || !WGRAD ? tc.overdeclare_tx : 0;
+    grouped_prepare<T>(ex, g.a, lda, ws);
+    grouped_prepare<T>(ex, g.b, ldb, ws);
+    p.A = g.a.at; p.lda = g.a.ld; p.B = g.b.at; p.ldb = g.b.ld;
+    p.slots = (float *)(ws + g.slots);
+    p.splits = (GroupedSplit *)(ws + g.splits);
+    if (sizeof(T) == 2 && !tc_make_map(tc, &a, (const bf16 *)p.A, p.rows, p.K, p.lda, 64, WGRAD ? 64 : 128, err)) return false;
+    if (WGRAD) {
+        if (sizeof(T) == 2 && !tc_make_map(tc, &b, (const bf16 *)p.B, p.rows, p.N, p.ldb, 64, 64, err)) return false;
+    } else if (!grouped_map_3d(tc, &b, (const bf16 *)p.B, p.groups * (int64_t)GP_PARTS<T>, g.b.rows, g.b.cols, p.ldb, MODE == GP_NN ? 64 : 128, err)) {
+        return false;
     }
-    if (sizeof(T) == 4) grouped_launch_one<MODE, float, 128, false>(ex, a, b, p, g.blocks);
-    else if (!g.tma) grouped_launch_one<MODE, bf16, 128, false>(ex, a, b, p, g.blocks);
-    else if (g.bn == 256) grouped_launch_one<MODE, bf16, 256, true>(ex, a, b, p, g.blocks);
-    else grouped_launch_one<MODE, bf16, 128, true>(ex, a, b, p, g.blocks);
+    if (p.extra_tx) tc.overdeclare_tx = 0;
+    if constexpr (sizeof(T) == 2) {
+        if (g.pair) {
+            grouped_launch_one<MODE, T, true>(ex, a, b, p, g.blocks);
+            return true;
+        }
+    }
+    grouped_launch_one<MODE, T, false>(ex, a, b, p, g.blocks);
     return true;
 }

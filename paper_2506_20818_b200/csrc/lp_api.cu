@@ -4,6 +4,7 @@
 #include <cmath>
 #include <memory>
 #include <new>
+#include <type_traits>
 
 #include "common.cuh"
 #include "scan_sort.cuh"
@@ -2665,23 +2666,28 @@ extern "C" lp_status lp_grouped_linear(lp_ctx *ctx, int32_t prec, int64_t M, int
     CK(cudaSetDevice(ctx->device));
     GroupedParams p{};
     p.offsets = offsets; p.groups = (int)groups; p.rows = (int)M; p.N = N; p.K = K;
-    p.A = A; p.lda = ld_a; p.B = B; p.ldb = trans_b ? K : N; p.stride_b = (int64_t)N * K;
     p.bias = bias; p.relu = relu != 0; p.C = C; p.ldc = ld_c;
     p.offsets_err = ctx->embed_err;
-    std::string err;
-    bool ok;
-    if (prec == LP_FP32) {
-        p.flush = 1;
-        p.vec_c = on_16_bytes<float>(C, ld_c) && N % 4 == 0;
-        const GroupedPlan g = grouped_plan(false, false, M, groups, N, K);
-        ok = trans_b ? grouped_launch<GP_NT, float>(ctx->tc, ctx->ex, p, g, err) : grouped_launch<GP_NN, float>(ctx->tc, ctx->ex, p, g, err);
-    } else {
-        p.flush = (K + 63) / 64;
-        p.vec_c = on_16_bytes<bf16>(C, ld_c) && N % 8 == 0;
-        const GroupedPlan g = grouped_plan(grouped_tma<bf16>(A, ld_a, B, p.ldb), false, M, groups, N, K);
-        ok = trans_b ? grouped_launch<GP_NT, bf16>(ctx->tc, ctx->ex, p, g, err) : grouped_launch<GP_NN, bf16>(ctx->tc, ctx->ex, p, g, err);
-    }
-    if (!ok) return fail(ctx, LP_ECUDA, who + ": " + err);
+    const int64_t ldb = trans_b ? K : N;
+    auto run = [&](auto mode, auto elem) -> lp_status {
+        constexpr int MODE = decltype(mode)::value;
+        using T = decltype(elem);
+        p.flush = sizeof(T) == 4 ? 1 : (K + 63) / 64;
+        p.vec_c = on_16_bytes<T>(C, ld_c) && N % (16 / (int)sizeof(T)) == 0;
+        GroupedPlan g = grouped_plan<MODE, T>(M, groups, N, K, A, ld_a, B, ldb);
+        uint8_t *ws = nullptr;
+        if (g.bytes) {
+            const lp_status st = op_workspace(ctx, g.bytes, &ws);
+            if (st != LP_OK) return st;
+        }
+        std::string err;
+        return grouped_launch<MODE, T>(ctx->tc, ctx->ex, p, g, ld_a, ldb, ws, err) ? LP_OK : fail(ctx, LP_ECUDA, who + ": " + err);
+    };
+    const std::integral_constant<int, GP_NN> nn{};
+    const std::integral_constant<int, GP_NT> nt{};
+    if (prec == LP_FP32) s = trans_b ? run(nt, float()) : run(nn, float());
+    else s = trans_b ? run(nt, bf16()) : run(nn, bf16());
+    if (s != LP_OK) return s;
     CK_LAUNCH();
     return LP_OK;
 }
@@ -2706,21 +2712,23 @@ extern "C" lp_status lp_grouped_weight_grad(lp_ctx *ctx, int32_t prec, int64_t M
         }
         return LP_OK;
     }
-    const GroupedPlan g = grouped_plan(prec == LP_BF16 && grouped_tma<bf16>(A, ld_a, dZ, ld_dz), true, M, groups, N, K);
-    uint8_t *ws = nullptr;
-    s = op_workspace(ctx, g.slots_bytes + sizeof(GroupedSplit) * (size_t)g.blocks, &ws);
-    if (s != LP_OK) return s;
     GroupedParams p{};
     p.offsets = offsets; p.groups = (int)groups; p.rows = (int)M; p.N = N; p.K = K;
-    p.A = A; p.lda = ld_a; p.B = dZ; p.ldb = ld_dz; p.stride_b = 0;
     p.vec_c = on_16_bytes<float>(dW, N) && N % 4 == 0;
     p.dW = dW; p.dbias = dbias; p.accumulate = accumulate != 0;
-    p.slots = (float *)ws; p.splits = (GroupedSplit *)(ws + g.slots_bytes);
     p.offsets_err = ctx->embed_err;
-    p.flush = prec == LP_FP32 ? 1 : 8;
-    std::string err;
-    const bool ok = prec == LP_FP32 ? grouped_launch<GP_WGRAD, float>(ctx->tc, ctx->ex, p, g, err) : grouped_launch<GP_WGRAD, bf16>(ctx->tc, ctx->ex, p, g, err);
-    if (!ok) return fail(ctx, LP_ECUDA, who + ": " + err);
+    auto run = [&](auto elem) -> lp_status {
+        using T = decltype(elem);
+        p.flush = sizeof(T) == 4 ? 1 : 8;
+        GroupedPlan g = grouped_plan<GP_WGRAD, T>(M, groups, N, K, A, ld_a, dZ, ld_dz);
+        uint8_t *ws = nullptr;
+        const lp_status st = op_workspace(ctx, g.bytes, &ws);
+        if (st != LP_OK) return st;
+        std::string err;
+        return grouped_launch<GP_WGRAD, T>(ctx->tc, ctx->ex, p, g, ld_a, ld_dz, ws, err) ? LP_OK : fail(ctx, LP_ECUDA, who + ": " + err);
+    };
+    s = prec == LP_FP32 ? run(float()) : run(bf16());
+    if (s != LP_OK) return s;
     CK_LAUNCH();
     return LP_OK;
 }
