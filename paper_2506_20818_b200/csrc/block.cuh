@@ -412,7 +412,9 @@ template <bool VEC, bool BLOCK> struct RowPipe {
     // the oldest row has arrived; false when the wait ran out (in all threads of the unit)
     LP_DEVINL bool wait()
     {
-        ok = mbar_wait(bar_out, parity, p.wait_ns);
+        ok = false;
+        for (int i = 0; i < 256 && !ok; ++i) ok = mbar_try_wait(bar_out, parity);  // reading the time takes longer than most waits do
+        if (!ok) ok = mbar_wait(bar_out, parity, p.wait_ns);
         ok = BLOCK ? __syncthreads_and(ok) != 0 : __all_sync(0xffffffffu, ok) != 0;
         return ok;
     }

@@ -1045,7 +1045,7 @@ static lp_status tc_check_result(TcState &tc, Exec &ex, std::string &err)
         char buf[256];
         snprintf(buf, sizeof buf,
                  "tensor-core GEMM: bounded wait %d expired (1 = stage free, 2 = operands, 3 = accumulator, 4 = operands for the column sums, "
-                 "5 = accumulator free, 6 = phase of the chained products, 7 = exchange of sums, 8 = rows of a residual norm)",
+                 "5 = accumulator free, 6 = phase of the chained products, 7 = exchange of sums, 8 = rows of a residual norm, 9 = tiles by group)",
                  *tc.host_err);
         err = buf;
         cudaMemsetAsync(tc.err_word, 0, sizeof(int), ex.st);

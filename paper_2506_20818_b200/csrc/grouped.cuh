@@ -8,9 +8,11 @@
 // larger ones are taken, so that a product is off by about 2^-23; the accumulator of the matrix instructions rounds towards
 // zero, so it adds up 64 terms, small products first, and those sums are added in FP32 registers.
 //
-// Persistent blocks of 18 warps, one per SM.  Sizes of the groups are on the device: every role walks the offsets itself, 32 groups at
-// a time, and finds its tiles (linear) or its share of the 64-row blocks of all tiles (weight gradient) without any plan or host read.
-//   warp 0    operands by TMA         warp 1   matrix instructions
+// Persistent blocks of 19 warps, one per SM.  Sizes of the groups are on the device: one warp walks the offsets, 32 groups at a time,
+// and finds the block's tiles (linear) or its share of the 64-row blocks of all tiles (weight gradient) without any plan or host read.
+// It runs a few tiles ahead of the others, who read where they lie from shared memory (every role walking for itself took 2,500 cycles
+// a tile, four times what a block of 64 terms takes).
+//   warp 0    operands by TMA         warp 1   matrix instructions        warp 18  where the tiles lie
 //   others    sums and results; FP32: the last eight bring in the operands that have to be split, through registers
 // Large BF16 products take pairs of SMs (cta_group::2) and tiles of 256 x 256: a 64-term block then costs 32 KiB of operands per SM for
 // 512 cycles of products, where a block of its own with 128 x 256 would need 48 KiB.
@@ -23,8 +25,9 @@
 #include "orthogonal.cuh"
 
 enum { GP_NN = 0, GP_NT = 1, GP_WGRAD = 2 };
-constexpr int GP_THREADS = 576;
-constexpr int GP_EXTRA_SMEM = 32768;  // results that are written element by element, sums of columns
+constexpr int GP_THREADS = 608;
+template <bool WIDE> constexpr int GP_EXTRA_SMEM = WIDE ? 65536 : 32768;  // results on their way out (WIDE: 128 bytes of a row at a time), sums of columns
+constexpr int GP_JOBS = 4;  // tiles that are known ahead
 constexpr int GP_MAX_STAGES = 8;
 constexpr int GP_MAX_GROUPS = 1 << 20;
 
@@ -123,11 +126,10 @@ template <bool WGRAD, int ROWS> struct GroupWalk {  // ROWS: of a tile (linear)
 };
 
 struct GroupedJob {
-    int g, row0, row_end;  // linear: rows of the tile; weight gradient: rows of the share
+    int g, row0, row_end;  // linear: rows of the tile; weight gradient: rows of the share.  g < 0: no more
     int kt, nt, kbs;       // tile, blocks of 64 terms
     int slot;              // weight gradient: partial tile of the worker, or -1: the whole tile is in this share
-    bool begins;           // ... the share begins the tile, which ends before block tile_end of all
-    int64_t tile_end;
+    int unused;
 };
 
 // `worker` of `workers`: block or pair of blocks
@@ -135,23 +137,36 @@ template <int MODE, int ROWS> struct GroupedJobs {
     GroupWalk<MODE == GP_WGRAD, ROWS> walk;
     const GroupedParams &p;
     int worker, workers;
-    int64_t t;           // linear: next tile
-    int64_t u, lo, hi;   // weight gradient: 64-row blocks of this share
-    LP_DEVINL GroupedJobs(const GroupedParams &p_, int worker_, int workers_, int64_t lo_, int64_t hi_)
-        : walk(p_), p(p_), worker(worker_), workers(workers_), t(worker_), u(lo_), lo(lo_), hi(hi_) {}
+    int mt, nt;              // linear: next tile
+    int64_t u, lo, hi, all;  // weight gradient: 64-row blocks of this share and of all
+    GroupedSplit split;      // ... the tile that this worker begins and others go on with
+    LP_DEVINL GroupedJobs(const GroupedParams &p_, int worker_, int workers_) : walk(p_), p(p_), worker(worker_), workers(workers_), split{0, 0, 0, -1, 0, 0}
+    {
+        if (MODE == GP_WGRAD) {
+            GroupWalk<MODE == GP_WGRAD, ROWS> w(walk);
+            all = (int64_t)w.all() * p.tiles_k * p.tiles_n;
+            u = lo = all * worker / workers;
+            hi = all * (worker + 1) / workers;
+        } else {
+            mt = worker / p.tiles_n;
+            nt = worker - mt * p.tiles_n;
+        }
+    }
     LP_DEVINL bool next(GroupedJob &j)
     {
         int b, e, pre;
         if (MODE != GP_WGRAD) {
-            const int mt = (int)(t / p.tiles_n);
-            j.nt = (int)(t - (int64_t)mt * p.tiles_n);
             if (!walk.seek(mt, j.g, b, e, pre)) return false;
+            j.nt = nt;
             j.row0 = b + (mt - pre) * ROWS;
             j.row_end = min(e, j.row0 + ROWS);
             j.kt = 0;
             j.kbs = (p.K + 63) >> 6;
             j.slot = -1;
-            t += workers;
+            const int step = workers / p.tiles_n;
+            mt += step;
+            nt += workers - step * p.tiles_n;
+            if (nt >= p.tiles_n) { nt -= p.tiles_n; ++mt; }
             return true;
         }
         if (u >= hi) return false;
@@ -166,12 +181,20 @@ template <int MODE, int ROWS> struct GroupedJobs {
         j.row0 = b + kb0 * 64;
         j.row_end = min(e, j.row0 + j.kbs * 64);
         j.slot = kb0 == 0 && j.kbs == blocks ? -1 : 2 * worker + (u == lo ? 0 : 1);
-        j.begins = kb0 == 0;
-        j.tile_end = u - kb0 + blocks;
+        // only the last share of a worker can begin a tile that others go on with: up to the one that has its last block
+        if (kb0 == 0 && j.slot >= 0) split = GroupedSplit{j.g, j.kt, j.nt, j.slot, (int)(((u + blocks) * workers - 1) / all), all};
         u += j.kbs;
         return true;
     }
 };
+
+// Bounded wait that looks at the time only after some thousand cycles: reading it takes longer than most waits do.
+LP_DEVINL bool wait_bar(uint32_t bar, uint32_t parity, unsigned long long limit_ns)
+{
+    for (int i = 0; i < 512; ++i)
+        if (mbar_try_wait(bar, parity)) return true;
+    return mbar_wait(bar, parity, limit_ns);
+}
 
 // ---------------------------------------------------------------------------------------------
 // operands through registers
@@ -256,32 +279,33 @@ __global__ void __launch_bounds__(256) grouped_split_kernel(const float *in, int
 // ---------------------------------------------------------------------------------------------
 // results
 // ---------------------------------------------------------------------------------------------
-// Neighbouring columns of a warp's 32 rows, a row per lane (64 bytes of it, so 16 FP32 or 32 BF16 columns): rows below `rows`, columns
-// below `cols`.  They go through 2 KiB of shared memory, so that a store instruction writes whole runs of a few rows: 64 bytes of eight
-// rows, or sixteen elements of two rows where the rows of the result do not start on 16 bytes.
-template <typename T> constexpr int PUT_COLS = 64 / sizeof(T);
-template <typename T> LP_DEVINL void put_columns(T *dst, int64_t ld, int rows, int cols, const float *v, int vec, uint8_t *stage, bool accumulate)
+// Neighbouring columns of a warp's 32 rows, a row per lane (RB bytes of it: 64 or 128): rows below `rows`, columns below `cols`.  They go
+// through shared memory (32 RB bytes), so that a store instruction writes whole runs of a few rows: 512 bytes, or sixteen elements of
+// two rows where the rows of the result do not start on 16 bytes.
+template <typename T, int RB> constexpr int PUT_COLS = RB / sizeof(T);
+template <typename T, int RB> LP_DEVINL void put_columns(T *dst, int64_t ld, int rows, int cols, const float *v, int vec, uint8_t *stage, bool accumulate)
 {
     const int lane = threadIdx.x & 31;
-    constexpr int VN = Vec16<T>::N;
+    constexpr int VN = Vec16<T>::N, PIECES = RB / 16, AT_ONCE = 32 / PIECES;  // rows of a store instruction
+    auto place = [](int r, int q) { return r * RB + ((q ^ (RB == 128 ? r & 7 : (r >> 1) & 3)) << 4); };  // no two of eight lanes in the same banks
     if (vec) {
         __syncwarp();
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
+        for (int q = 0; q < PIECES; ++q) {
             Vec16<T> o;
             o.from_float(v + q * VN);
-            *reinterpret_cast<decltype(o.v) *>(stage + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4)) = o.v;
+            *reinterpret_cast<decltype(o.v) *>(stage + place(lane, q)) = o.v;
         }
         __syncwarp();
-        const int q = lane & 3;
+        const int q = lane & (PIECES - 1);
+        T *d = dst + (int64_t)(lane / PIECES) * ld + q * VN;
         if (q * VN < cols)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int r = 8 * i + (lane >> 2);
+            for (int i = 0; i < PIECES; ++i, d += AT_ONCE * ld) {
+                const int r = AT_ONCE * i + lane / PIECES;
                 if (r < rows) {
                     Vec16<T> o;
-                    o.v = *reinterpret_cast<const decltype(o.v) *>(stage + r * 64 + ((q ^ ((r >> 1) & 3)) << 4));
-                    T *d = dst + (int64_t)r * ld + q * VN;
+                    o.v = *reinterpret_cast<const decltype(o.v) *>(stage + place(r, q));
                     if (accumulate) {
                         Vec16<T> old;
                         old.v = *reinterpret_cast<const decltype(o.v) *>(d);
@@ -299,7 +323,7 @@ template <typename T> LP_DEVINL void put_columns(T *dst, int64_t ld, int rows, i
     }
     float *s = reinterpret_cast<float *>(stage);
 #pragma unroll
-    for (int half = 0; half < PUT_COLS<T> / 16; ++half) {
+    for (int half = 0; half < PUT_COLS<T, RB> / 16; ++half) {
         __syncwarp();
 #pragma unroll
         for (int c = 0; c < 16; ++c) s[lane * 16 + (c ^ (lane & 15))] = v[half * 16 + c];
@@ -344,6 +368,8 @@ template <typename T> constexpr int GP_PARTS = sizeof(T) == 4 ? 3 : 1;
 template <bool PAIR> constexpr int GP_BN = PAIR ? 256 : 128;
 template <typename T> constexpr int GP_STAGE_BYTES = GP_PARTS<T> * (128 + 128) * 128;
 
+template <int MODE, bool PAIR> constexpr bool GP_WIDE = MODE != GP_WGRAD && PAIR;
+
 template <int MODE, typename T, bool PAIR>
 __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
                                                                  const __grid_constant__ GroupedParams p)
@@ -359,8 +385,9 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bar_full[GP_MAX_STAGES], bar_empty[GP_MAX_STAGES], bar_read[GP_MAX_STAGES], bar_acc_full[2], bar_acc_empty[2], bar_sum_full, bar_sum_empty,
         bar_done, bar_tail;
+    __shared__ __align__(8) uint64_t bar_job_full[GP_JOBS], bar_job_empty[GP_JOBS];
+    __shared__ __align__(16) GroupedJob jobs_s[GP_JOBS];
     __shared__ uint32_t tmem_base_s;
-    __shared__ int blocks_s;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const int rank = PAIR ? (int)cluster_cta_rank() : 0, worker = PAIR ? blockIdx.x >> 1 : blockIdx.x, workers = PAIR ? gridDim.x >> 1 : gridDim.x;
     const bool leader = rank == 0;  // of a pair: issues its matrix instructions
@@ -369,6 +396,40 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
     uint8_t *extra = smem + (size_t)S * stage_bytes;
     const bool sums = WGRAD && p.dbias != nullptr;
 
+    if (warp == GP_THREADS / 32 - 1) {
+        // ---- where the tiles lie (the first is found while the others set the block up)
+        GroupedJobs<MODE, ROWS> jobs(p, worker, workers);
+        GroupedJob w{};
+        bool more = jobs.next(w), ok = true;
+        if (blockIdx.x == 0) {
+            bool bad = false;
+            for (int g = lane; g <= p.groups; g += 32) bad |= p.offsets[g] < (g ? p.offsets[g - 1] : 0) || p.offsets[g] > p.rows;
+            if (__any_sync(0xffffffffu, bad) && lane == 0) atomicOr(p.offsets_err, 4);
+        }
+        tc_fence_before();
+        __syncthreads();
+        if (PAIR) cluster_barrier();
+        for (int at = 0, round = 0; ok;) {
+            if (round > 0) {
+                ok = __all_sync(0xffffffffu, wait_bar(smem_u32(&bar_job_empty[at]), (round & 1) ^ 1, p.wait_ns));
+                if (!ok) { if (lane == 0) atomicExch(p.err, 9); break; }
+            }
+            if (!more) w.g = -1;
+            if (lane == 0) {
+                jobs_s[at] = w;
+                mbar_arrive(smem_u32(&bar_job_full[at]));
+            }
+            __syncwarp();
+            if (!more) break;
+            more = jobs.next(w);
+            if (++at == GP_JOBS) { at = 0; ++round; }
+        }
+        if (WGRAD && lane == 0) p.splits[blockIdx.x] = jobs.split;
+        __syncwarp();
+        __syncthreads();
+        if (PAIR) cluster_barrier();
+        return;
+    }
     if (threadIdx.x == 0) {
         for (int s = 0; s < S; ++s) {
             mbar_init(smem_u32(&bar_full[s]), (PAIR ? 2 : TMA_A || TMA_B ? 1 : 0) + LOADERS);
@@ -381,6 +442,10 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
         }
         mbar_init(smem_u32(&bar_sum_full), TMA_A ? EPI : LOADERS);
         mbar_init(smem_u32(&bar_sum_empty), BH / 32);
+        for (int i = 0; i < GP_JOBS; ++i) {
+            mbar_init(smem_u32(&bar_job_full[i]), 1);
+            mbar_init(smem_u32(&bar_job_empty[i]), (TMA_A || TMA_B ? 1 : 0) + (leader ? 1 : 0) + EPI + LOADERS);
+        }
         mbar_init(smem_u32(&bar_done), 1);
         mbar_init(smem_u32(&bar_tail), 1);
         fence_barrier_init();
@@ -392,40 +457,38 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
         __syncwarp();
         if (PAIR) tmem_alloc_pair(smem_u32(&tmem_base_s), 2 * BN);
         else tmem_alloc(smem_u32(&tmem_base_s), 2 * BN);
-    } else if (warp == 1) {
-        if (WGRAD) {
-            GroupWalk<true, ROWS> w(p);
-            const int n = w.all();
-            if (lane == 0) blocks_s = n;
-        }
-    } else if (warp == 2 && blockIdx.x == 0) {
-        bool bad = false;
-        for (int g = lane; g <= p.groups; g += 32) bad |= p.offsets[g] < (g ? p.offsets[g - 1] : 0) || p.offsets[g] > p.rows;
-        if (__any_sync(0xffffffffu, bad) && lane == 0) atomicOr(p.offsets_err, 4);
     }
     tc_fence_before();
     __syncthreads();
     if (PAIR) cluster_barrier();  // both blocks' barriers are there before either uses the other's
     tc_fence_after();
     const uint32_t tmem = tmem_base_s;
-    int64_t lo = 0, hi = 0, all = 0;
-    if (WGRAD) {
-        all = (int64_t)blocks_s * p.tiles_k * p.tiles_n;
-        lo = all * worker / workers;
-        hi = all * (worker + 1) / workers;
-    }
-    GroupedJobs<MODE, ROWS> jobs(p, worker, workers, lo, hi);
     GroupedJob j;
+    int job_at = 0, job_round = 0;
+    // this warp's next tile; false: there is none, or the wait ran out
+    auto next_job = [&]() {
+        bool there = wait_bar(smem_u32(&bar_job_full[job_at]), job_round & 1, p.wait_ns);
+        there = __all_sync(0xffffffffu, there);
+        if (!there) {
+            if (lane == 0) atomicExch(p.err, 9);
+            return false;
+        }
+        j = jobs_s[job_at];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bar_job_empty[job_at]));
+        if (++job_at == GP_JOBS) { job_at = 0; ++job_round; }
+        return j.g >= 0;
+    };
 
     if (warp == 0) {
         if (TMA_A || TMA_B) {
             // ---- operands by TMA: this block's 128 rows (weight gradient: columns) of A and its BH columns of B
             int s = 0, round = 0, tails = 0;
             bool ok = true, first = blockIdx.x == (WGRAD ? gridDim.x - 1 : 0);  // a block that has work in any case
-            while (ok && jobs.next(j)) {
+            while (ok && next_job()) {
                 for (int kb = 0; kb < j.kbs && ok; ++kb) {
                     if (round > 0) {
-                        ok = mbar_wait(smem_u32(&bar_empty[s]), (round & 1) ^ 1, p.wait_ns) && (!(TMA_A && sums) || mbar_wait(smem_u32(&bar_read[s]), (round & 1) ^ 1, p.wait_ns));
+                        ok = wait_bar(smem_u32(&bar_empty[s]), (round & 1) ^ 1, p.wait_ns) && (!(TMA_A && sums) || wait_bar(smem_u32(&bar_read[s]), (round & 1) ^ 1, p.wait_ns));
                         ok = __all_sync(0xffffffffu, ok);
                         if (!ok) { if (lane == 0) atomicExch(p.err, 1); break; }
                     }
@@ -468,7 +531,7 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
                     first = false;
                     if (tail) {
                         // rows behind the group belong to the next one (or to nobody): zeros in both operands, whatever they hold
-                        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_tail), tails & 1, p.wait_ns));
+                        ok = __all_sync(0xffffffffu, wait_bar(smem_u32(&bar_tail), tails & 1, p.wait_ns));
                         if (!ok) { if (lane == 0) atomicExch(p.err, 2); break; }
                         ++tails;
                         uint8_t *st = smem + (size_t)s * stage_bytes + max(have, 0) * 128;
@@ -489,7 +552,7 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
             if (lane == 0 && leader)
                 for (int i = 0; i < S; ++i) {
                     const int at = s - 1 - i < 0 ? s - 1 - i + S : s - 1 - i, r = s - 1 - i < 0 ? round - 1 : round;
-                    if (r >= 0) mbar_wait(smem_u32(&bar_full[at]), r & 1, p.wait_ns);
+                    if (r >= 0) wait_bar(smem_u32(&bar_full[at]), r & 1, p.wait_ns);
                 }
             __syncwarp();
         }
@@ -508,15 +571,15 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
             if (PAIR) umma_commit_pair(smem_u32(&bar));
             else umma_commit(smem_u32(&bar));
         };
-        while (leader && ok && jobs.next(j)) {
+        while (leader && ok && next_job()) {
             int in_flush = 0;
             for (int kb = 0; kb < j.kbs && ok; ++kb) {
                 const int b = use & 1;
-                if (in_flush == 0 && use >= 2 && !mbar_wait(smem_u32(&bar_acc_empty[b]), ((use >> 1) & 1) ^ 1, p.wait_ns)) {
+                if (in_flush == 0 && use >= 2 && !wait_bar(smem_u32(&bar_acc_empty[b]), ((use >> 1) & 1) ^ 1, p.wait_ns)) {
                     if (lane == 0) atomicExch(p.err, 5);
                     ok = false;
                 }
-                if (ok && !mbar_wait(smem_u32(&bar_full[s]), round & 1, p.wait_ns)) {
+                if (ok && !wait_bar(smem_u32(&bar_full[s]), round & 1, p.wait_ns)) {
                     if (lane == 0) atomicExch(p.err, 2);
                     ok = false;
                 }
@@ -551,22 +614,22 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
         if (leader) {
             if (elect_one()) commit(bar_done);
             __syncwarp();
-            mbar_wait(smem_u32(&bar_done), 0, p.wait_ns);
+            wait_bar(smem_u32(&bar_done), 0, p.wait_ns);
         }
         __syncwarp();
     } else if (warp < 2 + EPI) {
         // ---- sums and results: 32 rows x COLS columns per warp
         const int quarter = warp & 3, part = (warp - 2) >> 2;
         const int epi_thread = threadIdx.x - 64;
-        uint8_t *stage = extra + (warp - 2) * 2048;
+        constexpr int OUT = GP_WIDE<MODE, PAIR> ? 4096 : 2048;  // bytes of a warp's results on their way
+        uint8_t *stage = extra + (warp - 2) * OUT;
         const uint32_t acc_free = PAIR ? map_to_cta(smem_u32(&bar_acc_empty[0]), 0) : smem_u32(&bar_acc_empty[0]);
         int use = 0, s = 0, round = 0, summed = 0;
         bool ok = true;
-        GroupedSplit split{0, 0, 0, -1, 0, 0};
         // the accumulator that holds the next sums; false when the wait ran out
         auto take = [&](uint32_t &at) {
             const int b = use & 1;
-            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_acc_full[b]), (use >> 1) & 1, p.wait_ns));
+            ok = __all_sync(0xffffffffu, wait_bar(smem_u32(&bar_acc_full[b]), (use >> 1) & 1, p.wait_ns));
             if (!ok) { if (lane == 0) atomicExch(p.err, 3); return false; }
             tc_fence_after();
             at = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(b * BN + part * COLS);
@@ -581,35 +644,41 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
             }
             ++use;
         };
-        while (ok && jobs.next(j)) {
+        while (ok && next_job()) {
             const int c0 = j.nt * BN + part * COLS;  // first column of this warp
             if (!WGRAD && PARTS == 1) {
                 // one accumulator holds all terms: from tensor memory straight to the result
                 const int row = j.row0 + rank * 128 + quarter * 32;
                 T *dst = (T *)p.C + (int64_t)row * p.ldc + c0;
                 const float *bias = p.bias ? p.bias + (int64_t)j.g * p.N + c0 : nullptr;
+                // the bias of the warp's columns, on its way while the products run, then to every lane out of shared memory
+                float mine[(COLS + 31) / 32];
+#pragma unroll
+                for (int i = 0; i < (COLS + 31) / 32; ++i) mine[i] = bias && c0 + 32 * i + lane < p.N ? __ldg(bias + 32 * i + lane) : 0.f;
                 uint32_t at;
                 if (!take(at)) break;
-                constexpr int PC = PUT_COLS<T>;
+                float v[COLS];
 #pragma unroll
-                for (int c = 0; c < COLS; c += PC) {
-                    float v[PC];
+                for (int i = 0; i < COLS; i += 16) tmem_ld_32x16(at + i, v + i);
+                tmem_ld_wait();
+                give_back();
+                if (c0 >= p.N) continue;
+                if (bias) {
+                    float *b = reinterpret_cast<float *>(stage);
+                    __syncwarp();
 #pragma unroll
-                    for (int i = 0; i < PC; i += 16) tmem_ld_32x16(at + c + i, v + i);
-                    tmem_ld_wait();
-                    if (c + PC >= COLS) give_back();  // read, if not written yet
-                    if (c0 + c >= p.N) continue;
-                    if (bias) {
-                        // a column per lane, handed round
-                        const float mine = PC == 32 || lane < 16 ? (c0 + c + lane < p.N ? __ldg(bias + c + lane) : 0.f) : 0.f;
+                    for (int i = 0; i < (COLS + 31) / 32; ++i) b[32 * i + lane] = mine[i];
+                    __syncwarp();
 #pragma unroll
-                        for (int i = 0; i < PC; ++i) v[i] += __shfl_sync(0xffffffffu, mine, i);
+                    for (int i = 0; i < COLS; i += 4) {
+                        const float4 x = *reinterpret_cast<const float4 *>(b + i);
+                        v[i] += x.x; v[i + 1] += x.y; v[i + 2] += x.z; v[i + 3] += x.w;
                     }
-                    if (p.relu)
-#pragma unroll
-                        for (int i = 0; i < PC; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];  // NaN stays
-                    put_columns<T>(dst + c, p.ldc, j.row_end - row, p.N - (c0 + c), v, p.vec_c, stage, false);
                 }
+                if (p.relu)
+#pragma unroll
+                    for (int i = 0; i < COLS; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];  // NaN stays
+                put_columns<T, COLS * 2>(dst, p.ldc, j.row_end - row, p.N - c0, v, p.vec_c, stage, false);
                 continue;
             }
             float v[COLS];
@@ -622,7 +691,7 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
                 if (TMA_A && sums) {
                     // column sums of dZ out of the staged tiles, once their products are done: eight columns (a piece of 16 bytes) of two rows per thread
                     constexpr int PIECES = BH / 8, RPT = 64 * PIECES / (EPI * 32);
-                    ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_empty[s]), round & 1, p.wait_ns));
+                    ok = __all_sync(0xffffffffu, wait_bar(smem_u32(&bar_empty[s]), round & 1, p.wait_ns));
                     if (!ok) { if (lane == 0) atomicExch(p.err, 4); break; }
                     if (adds) {
                         const int piece = epi_thread % PIECES, r0 = epi_thread / PIECES * RPT, have = j.row_end - (j.row0 + kb * 64);
@@ -660,14 +729,14 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
             }
             if (!ok) break;
             if (summed > 0) {  // the column sums of the job before have been read
-                ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_sum_empty), (summed - 1) & 1, p.wait_ns));
+                ok = __all_sync(0xffffffffu, wait_bar(smem_u32(&bar_sum_empty), (summed - 1) & 1, p.wait_ns));
                 if (!ok) { if (lane == 0) atomicExch(p.err, 7); break; }
             }
             if (!WGRAD) {
                 const int row = j.row0 + quarter * 32;
                 T *dst = (T *)p.C + (int64_t)row * p.ldc + c0;
                 const float *bias = p.bias ? p.bias + (int64_t)j.g * p.N + c0 : nullptr;
-                constexpr int PC = PUT_COLS<T>;
+                constexpr int PC = PUT_COLS<T, 64>;
 #pragma unroll
                 for (int c = 0; c < COLS; c += PC) {
                     if (c0 + c >= p.N) break;
@@ -679,18 +748,18 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
                     if (p.relu)
 #pragma unroll
                         for (int i = 0; i < PC; ++i) v[c + i] = v[c + i] < 0.f ? 0.f : v[c + i];
-                    put_columns<T>(dst + c, p.ldc, j.row_end - row, p.N - (c0 + c), v + c, p.vec_c, stage, false);
+                    put_columns<T, 64>(dst + c, p.ldc, j.row_end - row, p.N - (c0 + c), v + c, p.vec_c, stage, false);
                 }
             } else if (j.slot < 0) {
                 const int row = j.kt * ROWS + rank * 128 + quarter * 32;
                 float *dst = p.dW + ((int64_t)j.g * p.K + row) * p.N + c0;
 #pragma unroll
                 for (int c = 0; c < COLS; c += 16)
-                    if (c0 + c < p.N) put_columns<float>(dst + c, p.N, p.K - row, p.N - (c0 + c), v + c, p.vec_c, stage, p.accumulate != 0);
+                    if (c0 + c < p.N) put_columns<float, 64>(dst + c, p.N, p.K - row, p.N - (c0 + c), v + c, p.vec_c, stage, p.accumulate != 0);
             } else {
                 float *dst = p.slots + (((size_t)j.slot * (ROWS / 128) + rank) * 129 + quarter * 32) * BN + part * COLS;
 #pragma unroll
-                for (int c = 0; c < COLS; c += 16) put_columns<float>(dst + c, BN, 32, 16, v + c, 1, stage, false);
+                for (int c = 0; c < COLS; c += 16) put_columns<float, 64>(dst + c, BN, 32, 16, v + c, 1, stage, false);
             }
             if (adds) {
                 // every warp leaves its sums of a few rows in its own part of the area; the first BH threads add them up in order
@@ -703,13 +772,13 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&bar_sum_full));
                 if (epi_thread < BH) {
-                    ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_sum_full), summed & 1, p.wait_ns));
+                    ok = __all_sync(0xffffffffu, wait_bar(smem_u32(&bar_sum_full), summed & 1, p.wait_ns));
                     if (!ok) { if (lane == 0) atomicExch(p.err, 7); break; }
                     float x = 0.f;
 #pragma unroll
                     for (int i = 0; i < SHARES; ++i) {
                         const int writer = i * PIECES + epi_thread / 8;  // thread that has these columns of share i
-                        x += area[(writer >> 5) * 512 + (writer & 31) * 8 + (epi_thread & 7)];
+                        x += area[(writer >> 5) * (OUT / 4) + (writer & 31) * 8 + (epi_thread & 7)];
                     }
                     const int in_tile = rank * BH + epi_thread, c = j.nt * BN + in_tile;
                     if (j.slot >= 0) p.slots[(((size_t)j.slot * (ROWS / 128) + rank) * 129 + 128) * BN + in_tile] = x;
@@ -722,11 +791,7 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
                 }
                 ++summed;
             }
-            // of the shares of a worker only the last can begin a tile that others go on with
-            if (WGRAD && j.slot >= 0 && j.begins)
-                split = GroupedSplit{j.g, j.kt, j.nt, j.slot, (int)((j.tile_end * workers - 1) / all), all};
         }
-        if (WGRAD && warp == 2 && lane == 0) p.splits[blockIdx.x] = split;
     } else if (!TMA_A) {
         // ---- FP32 operands through registers, a block of 64 terms in two halves (of A alone, or A and dZ): while the pieces of one are
         // put down, those of the next are under way
@@ -758,7 +823,7 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
         };
         auto free_stage = [&]() {
             if (round > 0) {
-                ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_empty[s]), (round & 1) ^ 1, p.wait_ns));
+                ok = __all_sync(0xffffffffu, wait_bar(smem_u32(&bar_empty[s]), (round & 1) ^ 1, p.wait_ns));
                 if (!ok && lane == 0) atomicExch(p.err, 1);
             }
             return ok;
@@ -770,11 +835,11 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
             if (++s == S) { s = 0; ++round; }
         };
         int kb = 0;
-        bool more = jobs.next(j);
+        bool more = next_job();
         auto advance = [&]() {  // true: that was the job's last block
             if (++kb < j.kbs) return false;
             kb = 0;
-            more = jobs.next(j);
+            more = next_job();
             return true;
         };
         if (more) load_a(x, j, 0);
@@ -808,9 +873,9 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
                     for (int i = 0; i < 4; ++i) add8(col, y[i].v);
                     if (last) {
                         // a thread has the rows 16 i + lt / 16 of its eight columns: sixteen sums per column, added up in order
-                        float *area = reinterpret_cast<float *>(extra) + EPI * 512;
+                        float *area = reinterpret_cast<float *>(extra + EPI * 2048);
                         if (summed > 0) {
-                            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_sum_empty), (summed - 1) & 1, p.wait_ns));
+                            ok = __all_sync(0xffffffffu, wait_bar(smem_u32(&bar_sum_empty), (summed - 1) & 1, p.wait_ns));
                             if (!ok) { if (lane == 0) atomicExch(p.err, 7); break; }
                         }
 #pragma unroll
@@ -818,7 +883,7 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
                         __syncwarp();
                         if (lane == 0) mbar_arrive(smem_u32(&bar_sum_full));
                         if (lt < 128) {
-                            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_sum_full), summed & 1, p.wait_ns));
+                            ok = __all_sync(0xffffffffu, wait_bar(smem_u32(&bar_sum_full), summed & 1, p.wait_ns));
                             if (!ok) { if (lane == 0) atomicExch(p.err, 7); break; }
                             float v = 0.f;
 #pragma unroll
@@ -888,7 +953,7 @@ template <bool PAIR> __global__ void __launch_bounds__(256) grouped_splits_kerne
 // ---------------------------------------------------------------------------------------------
 template <int MODE, typename T, bool PAIR> static bool grouped_init_one(std::string &err)
 {
-    if (cudaFuncSetAttribute(grouped_kernel<MODE, T, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024 - 1024) == cudaSuccess) return true;
+    if (cudaFuncSetAttribute(grouped_kernel<MODE, T, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024 - 1536) == cudaSuccess) return true;
     err = "cannot raise the dynamic shared memory limit of the grouped products";
     return false;
 }
@@ -914,8 +979,9 @@ static bool grouped_map_3d(const TcState &tc, CUtensorMap *map, const bf16 *base
 template <int MODE, typename T, bool PAIR> static void grouped_launch_one(Exec &ex, const CUtensorMap &a, const CUtensorMap &b, GroupedParams &p, int blocks)
 {
     constexpr int stage = GP_STAGE_BYTES<T>;
-    p.stages = std::min(GP_MAX_STAGES, (227 * 1024 - 1024 - 1024 - GP_EXTRA_SMEM) / stage);
-    const size_t smem = (size_t)p.stages * stage + GP_EXTRA_SMEM + 1024;
+    constexpr int extra = GP_EXTRA_SMEM<GP_WIDE<MODE, PAIR>>;
+    p.stages = std::min(GP_MAX_STAGES, (227 * 1024 - 1536 - 1024 - extra) / stage);
+    const size_t smem = (size_t)p.stages * stage + extra + 1024;
     if (PAIR) {
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)blocks);
