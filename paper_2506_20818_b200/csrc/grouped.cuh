@@ -8,11 +8,11 @@
 // larger ones are taken, so that a product is off by about 2^-23; the accumulator of the matrix instructions rounds towards
 // zero, so it adds up 64 terms, small products first, and those sums are added in FP32 registers.
 //
-// Persistent blocks of 19 warps, one per SM.  Sizes of the groups are on the device: one warp walks the offsets, 32 groups at a time,
+// Persistent blocks of 20 warps, one per SM.  Sizes of the groups are on the device: one warp walks the offsets, 32 groups at a time,
 // and finds the block's tiles (linear) or its share of the 64-row blocks of all tiles (weight gradient) without any plan or host read.
 // It runs a few tiles ahead of the others, who read where they lie from shared memory (every role walking for itself took 2,500 cycles
 // a tile, four times what a block of 64 terms takes).
-//   warp 0    operands by TMA         warp 1   matrix instructions        warp 18  where the tiles lie
+//   warp 0    operands by TMA         warp 1   matrix instructions        warp 2   where the tiles lie
 //   others    sums and results; FP32: the last eight bring in the operands that have to be split, through registers
 // Large BF16 products take pairs of SMs (cta_group::2) and tiles of 256 x 256: a 64-term block then costs 32 KiB of operands per SM for
 // 512 cycles of products, where a block of its own with 128 x 256 would need 48 KiB.
@@ -25,7 +25,12 @@
 #include "orthogonal.cuh"
 
 enum { GP_NN = 0, GP_NT = 1, GP_WGRAD = 2 };
-constexpr int GP_THREADS = 608;
+constexpr int GP_THREADS = 640;
+// Registers of the warpgroups: 5 x 96 at the launch, moved to those that hold sums and pieces of operands
+constexpr int GP_REGS_CONTROL = 48, GP_REGS_SUMS = 104, GP_REGS_LOADS = 112;
+static_assert(GP_REGS_CONTROL + 2 * GP_REGS_SUMS + 2 * GP_REGS_LOADS <= 5 * 96 && GP_REGS_CONTROL + 4 * GP_REGS_SUMS <= 5 * 96, "the block was launched with fewer");
+template <int N> LP_DEVINL void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> LP_DEVINL void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <bool WIDE> constexpr int GP_EXTRA_SMEM = WIDE ? 65536 : 32768;  // results on their way out (WIDE: 128 bytes of a row at a time), sums of columns
 constexpr int GP_JOBS = 4;  // tiles that are known ahead
 constexpr int GP_MAX_STAGES = 8;
@@ -50,7 +55,7 @@ struct GroupedParams {
     int relu;
     void *C;
     int64_t ldc;
-    int vec_c;
+    int vec_c, vec_bias;     // rows on 16 bytes
     // weight gradient
     float *dW, *dbias;
     int accumulate;
@@ -283,42 +288,52 @@ __global__ void __launch_bounds__(256) grouped_split_kernel(const float *in, int
 // through shared memory (32 RB bytes), so that a store instruction writes whole runs of a few rows: 512 bytes, or sixteen elements of
 // two rows where the rows of the result do not start on 16 bytes.
 template <typename T, int RB> constexpr int PUT_COLS = RB / sizeof(T);
+template <int RB> LP_DEVINL int stage_place(int r, int q) { return r * RB + ((q ^ (RB == 128 ? r & 7 : (r >> 1) & 3)) << 4); }  // no two of eight lanes in the same banks
+// N columns of the lane's row, from column c on
+template <typename T, int RB, int N> LP_DEVINL void stage_columns(int c, const float *v, uint8_t *stage)
+{
+    constexpr int VN = Vec16<T>::N;
+#pragma unroll
+    for (int q = 0; q < N / VN; ++q) {
+        Vec16<T> o;
+        o.from_float(v + q * VN);
+        *reinterpret_cast<decltype(o.v) *>(stage + stage_place<RB>(threadIdx.x & 31, c / VN + q)) = o.v;
+    }
+}
+template <typename T, int RB> LP_DEVINL void put_staged(T *dst, int64_t ld, int rows, int cols, const uint8_t *stage, bool accumulate)
+{
+    constexpr int VN = Vec16<T>::N, PIECES = RB / 16, AT_ONCE = 32 / PIECES;  // rows of a store instruction
+    const int lane = threadIdx.x & 31, q = lane & (PIECES - 1);
+    T *d = dst + (int64_t)(lane / PIECES) * ld + q * VN;
+    if (q * VN < cols)
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i, d += AT_ONCE * ld) {
+            const int r = AT_ONCE * i + lane / PIECES;
+            if (r < rows) {
+                Vec16<T> o;
+                o.v = *reinterpret_cast<const decltype(o.v) *>(stage + stage_place<RB>(r, q));
+                if (accumulate) {
+                    Vec16<T> old;
+                    old.v = *reinterpret_cast<const decltype(o.v) *>(d);
+                    float x[VN], y[VN];
+                    old.to_float(x);
+                    o.to_float(y);
+#pragma unroll
+                    for (int k = 0; k < VN; ++k) y[k] += x[k];
+                    o.from_float(y);
+                }
+                o.store(d);
+            }
+        }
+}
 template <typename T, int RB> LP_DEVINL void put_columns(T *dst, int64_t ld, int rows, int cols, const float *v, int vec, uint8_t *stage, bool accumulate)
 {
     const int lane = threadIdx.x & 31;
-    constexpr int VN = Vec16<T>::N, PIECES = RB / 16, AT_ONCE = 32 / PIECES;  // rows of a store instruction
-    auto place = [](int r, int q) { return r * RB + ((q ^ (RB == 128 ? r & 7 : (r >> 1) & 3)) << 4); };  // no two of eight lanes in the same banks
     if (vec) {
         __syncwarp();
-#pragma unroll
-        for (int q = 0; q < PIECES; ++q) {
-            Vec16<T> o;
-            o.from_float(v + q * VN);
-            *reinterpret_cast<decltype(o.v) *>(stage + place(lane, q)) = o.v;
-        }
+        stage_columns<T, RB, PUT_COLS<T, RB>>(0, v, stage);
         __syncwarp();
-        const int q = lane & (PIECES - 1);
-        T *d = dst + (int64_t)(lane / PIECES) * ld + q * VN;
-        if (q * VN < cols)
-#pragma unroll
-            for (int i = 0; i < PIECES; ++i, d += AT_ONCE * ld) {
-                const int r = AT_ONCE * i + lane / PIECES;
-                if (r < rows) {
-                    Vec16<T> o;
-                    o.v = *reinterpret_cast<const decltype(o.v) *>(stage + place(r, q));
-                    if (accumulate) {
-                        Vec16<T> old;
-                        old.v = *reinterpret_cast<const decltype(o.v) *>(d);
-                        float x[VN], y[VN];
-                        old.to_float(x);
-                        o.to_float(y);
-#pragma unroll
-                        for (int k = 0; k < VN; ++k) y[k] += x[k];
-                        o.from_float(y);
-                    }
-                    o.store(d);
-                }
-            }
+        put_staged<T, RB>(dst, ld, rows, cols, stage, accumulate);
         return;
     }
     float *s = reinterpret_cast<float *>(stage);
@@ -396,7 +411,7 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
     uint8_t *extra = smem + (size_t)S * stage_bytes;
     const bool sums = WGRAD && p.dbias != nullptr;
 
-    if (warp == GP_THREADS / 32 - 1) {
+    if (warp == 2) {
         // ---- where the tiles lie (the first is found while the others set the block up)
         GroupedJobs<MODE, ROWS> jobs(p, worker, workers);
         GroupedJob w{};
@@ -409,6 +424,7 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
         tc_fence_before();
         __syncthreads();
         if (PAIR) cluster_barrier();
+        fewer_registers<GP_REGS_CONTROL>();
         for (int at = 0, round = 0; ok;) {
             if (round > 0) {
                 ok = __all_sync(0xffffffffu, wait_bar(smem_u32(&bar_job_empty[at]), (round & 1) ^ 1, p.wait_ns));
@@ -481,6 +497,7 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
     };
 
     if (warp == 0) {
+        fewer_registers<GP_REGS_CONTROL>();
         if (TMA_A || TMA_B) {
             // ---- operands by TMA: this block's 128 rows (weight gradient: columns) of A and its BH columns of B
             int s = 0, round = 0, tails = 0;
@@ -557,6 +574,7 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
             __syncwarp();
         }
     } else if (warp == 1) {
+        fewer_registers<GP_REGS_CONTROL>();
         // ---- products
         int s = 0, round = 0, use = 0;
         bool ok = true;
@@ -617,12 +635,15 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
             wait_bar(smem_u32(&bar_done), 0, p.wait_ns);
         }
         __syncwarp();
-    } else if (warp < 2 + EPI) {
+    } else if (warp == 3) {
+        fewer_registers<GP_REGS_CONTROL>();
+    } else if (warp < 4 + EPI) {
+        more_registers<GP_REGS_SUMS>();
         // ---- sums and results: 32 rows x COLS columns per warp
-        const int quarter = warp & 3, part = (warp - 2) >> 2;
-        const int epi_thread = threadIdx.x - 64;
+        const int quarter = warp & 3, part = (warp - 4) >> 2;
+        const int epi_thread = threadIdx.x - 128;
         constexpr int OUT = GP_WIDE<MODE, PAIR> ? 4096 : 2048;  // bytes of a warp's results on their way
-        uint8_t *stage = extra + (warp - 2) * OUT;
+        uint8_t *stage = extra + (warp - 4) * OUT;
         const uint32_t acc_free = PAIR ? map_to_cta(smem_u32(&bar_acc_empty[0]), 0) : smem_u32(&bar_acc_empty[0]);
         int use = 0, s = 0, round = 0, summed = 0;
         bool ok = true;
@@ -651,34 +672,42 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
                 const int row = j.row0 + rank * 128 + quarter * 32;
                 T *dst = (T *)p.C + (int64_t)row * p.ldc + c0;
                 const float *bias = p.bias ? p.bias + (int64_t)j.g * p.N + c0 : nullptr;
-                // the bias of the warp's columns, on its way while the products run, then to every lane out of shared memory
-                float mine[(COLS + 31) / 32];
-#pragma unroll
-                for (int i = 0; i < (COLS + 31) / 32; ++i) mine[i] = bias && c0 + 32 * i + lane < p.N ? __ldg(bias + 32 * i + lane) : 0.f;
                 uint32_t at;
                 if (!take(at)) break;
-                float v[COLS];
 #pragma unroll
-                for (int i = 0; i < COLS; i += 16) tmem_ld_32x16(at + i, v + i);
-                tmem_ld_wait();
-                give_back();
-                if (c0 >= p.N) continue;
-                if (bias) {
-                    float *b = reinterpret_cast<float *>(stage);
-                    __syncwarp();
+                for (int c = 0; c < COLS; c += 32) {
+                    float v[32];
+                    tmem_ld_32x16(at + c, v);
+                    tmem_ld_32x16(at + c + 16, v + 16);
+                    tmem_ld_wait();
+                    if (c + 32 >= COLS) give_back();
+                    if (c0 + c >= p.N) continue;
+                    if (bias) {
+                        if (p.vec_bias && c0 + c + 32 <= p.N) {
 #pragma unroll
-                    for (int i = 0; i < (COLS + 31) / 32; ++i) b[32 * i + lane] = mine[i];
-                    __syncwarp();
+                            for (int i = 0; i < 32; i += 4) {
+                                const float4 x = __ldg(reinterpret_cast<const float4 *>(bias + c + i));
+                                v[i] += x.x; v[i + 1] += x.y; v[i + 2] += x.z; v[i + 3] += x.w;
+                            }
+                        } else {
 #pragma unroll
-                    for (int i = 0; i < COLS; i += 4) {
-                        const float4 x = *reinterpret_cast<const float4 *>(b + i);
-                        v[i] += x.x; v[i + 1] += x.y; v[i + 2] += x.z; v[i + 3] += x.w;
+                            for (int i = 0; i < 32; ++i) v[i] += c0 + c + i < p.N ? __ldg(bias + c + i) : 0.f;
+                        }
+                    }
+                    if (p.relu)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];  // NaN stays
+                    if (p.vec_c) {
+                        if (c == 0) __syncwarp();
+                        stage_columns<T, COLS * 2, 32>(c, v, stage);
+                    } else {
+                        put_columns<T, 64>(dst + c, p.ldc, j.row_end - row, p.N - (c0 + c), v, 0, stage, false);
                     }
                 }
-                if (p.relu)
-#pragma unroll
-                    for (int i = 0; i < COLS; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];  // NaN stays
-                put_columns<T, COLS * 2>(dst, p.ldc, j.row_end - row, p.N - c0, v, p.vec_c, stage, false);
+                if (p.vec_c && c0 < p.N) {
+                    __syncwarp();
+                    put_staged<T, COLS * 2>(dst, p.ldc, j.row_end - row, p.N - c0, stage, false);
+                }
                 continue;
             }
             float v[COLS];
@@ -793,10 +822,11 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
             }
         }
     } else if (!TMA_A) {
+        more_registers<GP_REGS_LOADS>();
         // ---- FP32 operands through registers, a block of 64 terms in two halves (of A alone, or A and dZ): while the pieces of one are
         // put down, those of the next are under way
         constexpr bool BOTH = !TMA_B;
-        const int lt = threadIdx.x - (2 + EPI) * 32;
+        const int lt = threadIdx.x - (4 + EPI) * 32;
         int s = 0, round = 0, summed = 0;
         bool ok = true;
         Piece8 x[4], y[4];

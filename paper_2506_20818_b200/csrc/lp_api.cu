@@ -2666,7 +2666,7 @@ extern "C" lp_status lp_grouped_linear(lp_ctx *ctx, int32_t prec, int64_t M, int
     CK(cudaSetDevice(ctx->device));
     GroupedParams p{};
     p.offsets = offsets; p.groups = (int)groups; p.rows = (int)M; p.N = N; p.K = K;
-    p.bias = bias; p.relu = relu != 0; p.C = C; p.ldc = ld_c;
+    p.bias = bias; p.vec_bias = on_16_bytes<float>(bias, N); p.relu = relu != 0; p.C = C; p.ldc = ld_c;
     p.offsets_err = ctx->embed_err;
     const int64_t ldb = trans_b ? K : N;
     auto run = [&](auto mode, auto elem) -> lp_status {
