@@ -16,8 +16,9 @@
 //   others    sums and results; FP32: the last eight bring in the operands that have to be split, through registers
 // Large BF16 products take pairs of SMs (cta_group::2) and tiles of 256 x 256: a 64-term block then costs 32 KiB of operands per SM for
 // 512 cycles of products, where a block of its own with 128 x 256 would need 48 KiB.
-// BF16 operands whose rows do not start on 16 bytes are copied to rows that do (TMA takes no others), FP32 ones, too, so that they can be
-// read 16 bytes at a time; the FP32 matrices B are split into their parts once per call.
+// Of FP32 operands one is split into its parts before (the matrices B; A of the weight gradient) and comes by TMA, the other is split on
+// its way through registers.  BF16 operands whose rows do not start on 16 bytes are copied to rows that do (TMA takes no others), FP32
+// ones, too, so that they can be read 16 bytes at a time.
 // The weight gradient deals out equal shares of 64-row blocks: a tile that lies in several shares is written as partial tiles,
 // added in a fixed order by a second kernel.  Bits do not depend on anything but the sizes.
 #pragma once
@@ -47,8 +48,8 @@ struct GroupedParams {
     int rows;                // of A; offsets are clamped to [0, rows]
     int N, K;                // linear: columns of C, of A; weight gradient: columns of dZ, of A
     int tiles_n, tiles_k;    // tiles_k: weight gradient only
-    const void *A, *B;       // operands that come through registers (B: dZ of the weight gradient); rows on 16 bytes
-    int64_t lda, ldb;
+    const float *reg;        // FP32: the operand that comes through registers (A; dZ of the weight gradient), rows on 16 bytes
+    int64_t ld_reg;
     int stages, flush;       // blocks of 64 terms that an accumulator adds up
     // linear
     const float *bias;
@@ -56,6 +57,7 @@ struct GroupedParams {
     void *C;
     int64_t ldc;
     int vec_c, vec_bias;     // rows on 16 bytes
+    int tma_c;               // whole tiles of rows leave by TMA
     // weight gradient
     float *dW, *dbias;
     int accumulate;
@@ -265,7 +267,7 @@ template <typename T> __global__ void __launch_bounds__(256) grouped_align_kerne
 }
 
 // An FP32 matrix as its three parts, each in rows of `ld_out` BF16 numbers, `part` elements apart
-__global__ void __launch_bounds__(256) grouped_split_kernel(const float *in, int64_t rows, int width, int vec, bf16 *out, int64_t ld_out, int64_t part)
+__global__ void __launch_bounds__(256) grouped_split_kernel(const float *in, int64_t rows, int width, int64_t ld_in, int vec, bf16 *out, int64_t ld_out, int64_t part)
 {
     LP_DEP_ENTER();
     const int64_t per = ld_out / 8, i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / per;
@@ -273,10 +275,10 @@ __global__ void __launch_bounds__(256) grouped_split_kernel(const float *in, int
     const int col = (int)(i - row * per) * 8;
     Piece8 x;
     if (vec) {
-        x.load(in + row * width, col, width);
+        x.load(in + row * ld_in, col, width);
     } else {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x.v[k] = col + k < width ? __ldg(in + row * width + col + k) : 0.f;
+        for (int k = 0; k < 8; ++k) x.v[k] = col + k < width ? __ldg(in + row * ld_in + col + k) : 0.f;
     }
     x.parts([&](int q, const uint4 &w) { *reinterpret_cast<uint4 *>(out + q * part + row * ld_out + col) = w; });
 }
@@ -325,6 +327,28 @@ template <typename T, int RB> LP_DEVINL void put_staged(T *dst, int64_t ld, int 
                 o.store(d);
             }
         }
+}
+// The staged rows leave by one TMA store of the warp, or, at the end of a group, whose next rows are not this tile's, row by row.
+template <int N> LP_DEVINL void stage_free()  // all stores but the last N of the warp have read their rows
+{
+    if ((threadIdx.x & 31) == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");
+    __syncwarp();
+}
+template <typename T, int RB>
+LP_DEVINL void put_rows(const CUtensorMap *map, int col, int row, T *dst, int64_t ld, int rows, int cols, const uint8_t *stage)
+{
+    if (map && rows >= 32) {
+        fence_async_proxy();
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) {
+            tma_store_2d(map, smem_u32(stage), col, row);
+            tma_store_commit();
+        }
+    } else {
+        __syncwarp();
+        put_staged<T, RB>(dst, ld, rows, cols, stage, false);
+        __syncwarp();
+    }
 }
 template <typename T, int RB> LP_DEVINL void put_columns(T *dst, int64_t ld, int rows, int cols, const float *v, int vec, uint8_t *stage, bool accumulate)
 {
@@ -387,15 +411,15 @@ template <int MODE, bool PAIR> constexpr bool GP_WIDE = MODE != GP_WGRAD && PAIR
 
 template <int MODE, typename T, bool PAIR>
 __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
-                                                                 const __grid_constant__ GroupedParams p)
+                                                                 const __grid_constant__ CUtensorMap mapC, const __grid_constant__ GroupedParams p)
 {
     LP_DEP_ENTER();
     constexpr int PARTS = GP_PARTS<T>, BN = GP_BN<PAIR>, BH = 128, ROWS = PAIR ? 256 : 128;
-    constexpr bool WGRAD = MODE == GP_WGRAD, TMA_A = PARTS == 1, TMA_B = PARTS == 1 || !WGRAD;
+    constexpr bool WGRAD = MODE == GP_WGRAD, SPLIT = PARTS == 3, TMA_A = !SPLIT || WGRAD, TMA_B = !SPLIT || !WGRAD;
     constexpr bool A_MN = WGRAD, B_MN = MODE != GP_NT;
-    constexpr int EPI = TMA_A ? 16 : 8, COLS = BN * 4 / EPI;  // warps of sums and results, columns of each
-    constexpr int LOADERS = TMA_A ? 0 : 8;
-    constexpr uint32_t a_bytes = 128 * 128, b_bytes = BH * 128, stage_bytes = GP_STAGE_BYTES<T>, tma_bytes = (TMA_A ? a_bytes : 0) + (TMA_B ? PARTS * b_bytes : 0);
+    constexpr int EPI = SPLIT ? 8 : 16, COLS = BN * 4 / EPI;  // warps of sums and results, columns of each
+    constexpr int LOADERS = SPLIT ? 8 : 0;
+    constexpr uint32_t a_bytes = 128 * 128, b_bytes = BH * 128, stage_bytes = GP_STAGE_BYTES<T>, tma_bytes = (TMA_A ? PARTS * a_bytes : 0) + (TMA_B ? PARTS * b_bytes : 0);
     static_assert(!PAIR || PARTS == 1, "pairs take BF16 operands");
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bar_full[GP_MAX_STAGES], bar_empty[GP_MAX_STAGES], bar_read[GP_MAX_STAGES], bar_acc_full[2], bar_acc_empty[2], bar_sum_full, bar_sum_empty,
@@ -448,7 +472,7 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
     }
     if (threadIdx.x == 0) {
         for (int s = 0; s < S; ++s) {
-            mbar_init(smem_u32(&bar_full[s]), (PAIR ? 2 : TMA_A || TMA_B ? 1 : 0) + LOADERS);
+            mbar_init(smem_u32(&bar_full[s]), (PAIR ? 2 : 1) + LOADERS);
             mbar_init(smem_u32(&bar_empty[s]), 1);
             mbar_init(smem_u32(&bar_read[s]), EPI);
         }
@@ -456,11 +480,11 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
             mbar_init(smem_u32(&bar_acc_full[b]), 1);
             mbar_init(smem_u32(&bar_acc_empty[b]), PAIR ? 2 * EPI : EPI);
         }
-        mbar_init(smem_u32(&bar_sum_full), TMA_A ? EPI : LOADERS);
+        mbar_init(smem_u32(&bar_sum_full), SPLIT ? LOADERS : EPI);
         mbar_init(smem_u32(&bar_sum_empty), BH / 32);
         for (int i = 0; i < GP_JOBS; ++i) {
             mbar_init(smem_u32(&bar_job_full[i]), 1);
-            mbar_init(smem_u32(&bar_job_empty[i]), (TMA_A || TMA_B ? 1 : 0) + (leader ? 1 : 0) + EPI + LOADERS);
+            mbar_init(smem_u32(&bar_job_empty[i]), 1 + (leader ? 1 : 0) + EPI + LOADERS);
         }
         mbar_init(smem_u32(&bar_done), 1);
         mbar_init(smem_u32(&bar_tail), 1);
@@ -468,6 +492,7 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
         fence_async_proxy();
         if (TMA_A) tma_prefetch_desc(&mapA);
         if (TMA_B) tma_prefetch_desc(&mapB);
+        if (!WGRAD && p.tma_c) tma_prefetch_desc(&mapC);
     }
     if (warp == 0) {
         __syncwarp();
@@ -498,14 +523,14 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
 
     if (warp == 0) {
         fewer_registers<GP_REGS_CONTROL>();
-        if (TMA_A || TMA_B) {
+        {
             // ---- operands by TMA: this block's 128 rows (weight gradient: columns) of A and its BH columns of B
             int s = 0, round = 0, tails = 0;
             bool ok = true, first = blockIdx.x == (WGRAD ? gridDim.x - 1 : 0);  // a block that has work in any case
             while (ok && next_job()) {
                 for (int kb = 0; kb < j.kbs && ok; ++kb) {
                     if (round > 0) {
-                        ok = wait_bar(smem_u32(&bar_empty[s]), (round & 1) ^ 1, p.wait_ns) && (!(TMA_A && sums) || wait_bar(smem_u32(&bar_read[s]), (round & 1) ^ 1, p.wait_ns));
+                        ok = wait_bar(smem_u32(&bar_empty[s]), (round & 1) ^ 1, p.wait_ns) && (SPLIT || !sums || wait_bar(smem_u32(&bar_read[s]), (round & 1) ^ 1, p.wait_ns));
                         ok = __all_sync(0xffffffffu, ok);
                         if (!ok) { if (lane == 0) atomicExch(p.err, 1); break; }
                     }
@@ -528,9 +553,12 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
                         if (WGRAD) {
                             const int row = j.row0 + kb * 64;
 #pragma unroll
-                            for (int c = 0; c < 2; ++c) tile_2d<PAIR>(sa + c * 8192, &mapA, bar, j.kt * ROWS + rank * 128 + c * 64, row);
+                            for (int q = 0; q < PARTS; ++q)
 #pragma unroll
-                            for (int c = 0; c < 2; ++c) tile_2d<PAIR>(sb + c * 8192, &mapB, bar, j.nt * BN + rank * BH + c * 64, row);
+                                for (int c = 0; c < 2; ++c) tile_3d<PAIR>(sa + q * a_bytes + c * 8192, &mapA, bar, j.kt * ROWS + rank * 128 + c * 64, row, q);
+                            if (TMA_B)
+#pragma unroll
+                                for (int c = 0; c < 2; ++c) tile_2d<PAIR>(sb + c * 8192, &mapB, bar, j.nt * BN + rank * BH + c * 64, row);
                         } else {
                             if (TMA_A) tile_2d<PAIR>(sa, &mapA, bar, kb * 64, j.row0 + rank * 128);
 #pragma unroll
@@ -547,14 +575,14 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
                     __syncwarp();
                     first = false;
                     if (tail) {
-                        // rows behind the group belong to the next one (or to nobody): zeros in both operands, whatever they hold
+                        // rows behind the group belong to the next one (or to nobody): zeros, whatever they hold
                         ok = __all_sync(0xffffffffu, wait_bar(smem_u32(&bar_tail), tails & 1, p.wait_ns));
                         if (!ok) { if (lane == 0) atomicExch(p.err, 2); break; }
                         ++tails;
                         uint8_t *st = smem + (size_t)s * stage_bytes + max(have, 0) * 128;
                         for (int i = lane; i < (64 - max(have, 0)) * 8; i += 32)
 #pragma unroll
-                            for (int c = 0; c < 4; ++c) *reinterpret_cast<uint4 *>(st + c * 8192 + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+                            for (int c = 0; c < (SPLIT ? 6 : 4); ++c) *reinterpret_cast<uint4 *>(st + c * 8192 + i * 16) = make_uint4(0u, 0u, 0u, 0u);
                         fence_async_proxy();
                         __syncwarp();
                         if (lane == 0) {
@@ -642,7 +670,7 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
         // ---- sums and results: 32 rows x COLS columns per warp
         const int quarter = warp & 3, part = (warp - 4) >> 2;
         const int epi_thread = threadIdx.x - 128;
-        constexpr int OUT = GP_WIDE<MODE, PAIR> ? 4096 : 2048;  // bytes of a warp's results on their way
+        constexpr int OUT = GP_WIDE<MODE, PAIR> || (SPLIT && !WGRAD) ? 4096 : 2048;  // bytes of a warp's results on their way
         uint8_t *stage = extra + (warp - 4) * OUT;
         const uint32_t acc_free = PAIR ? map_to_cta(smem_u32(&bar_acc_empty[0]), 0) : smem_u32(&bar_acc_empty[0]);
         int use = 0, s = 0, round = 0, summed = 0;
@@ -698,26 +726,23 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
 #pragma unroll
                         for (int i = 0; i < 32; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];  // NaN stays
                     if (p.vec_c) {
-                        if (c == 0) __syncwarp();
+                        if (c == 0) stage_free<0>();
                         stage_columns<T, COLS * 2, 32>(c, v, stage);
                     } else {
                         put_columns<T, 64>(dst + c, p.ldc, j.row_end - row, p.N - (c0 + c), v, 0, stage, false);
                     }
                 }
-                if (p.vec_c && c0 < p.N) {
-                    __syncwarp();
-                    put_staged<T, COLS * 2>(dst, p.ldc, j.row_end - row, p.N - c0, stage, false);
-                }
+                if (p.vec_c && c0 < p.N) put_rows<T, COLS * 2>(p.tma_c ? &mapC : nullptr, c0, row, dst, p.ldc, j.row_end - row, p.N - c0, stage);
                 continue;
             }
             float v[COLS];
 #pragma unroll
             for (int c = 0; c < COLS; ++c) v[c] = 0.f;
             float col[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            const bool adds = sums && TMA_A && j.kt == 0;
+            const bool adds = sums && !SPLIT && j.kt == 0;
             int in_flush = 0;
             for (int kb = 0; kb < j.kbs && ok; ++kb) {
-                if (TMA_A && sums) {
+                if (!SPLIT && sums) {
                     // column sums of dZ out of the staged tiles, once their products are done: eight columns (a piece of 16 bytes) of two rows per thread
                     constexpr int PIECES = BH / 8, RPT = 64 * PIECES / (EPI * 32);
                     ok = __all_sync(0xffffffffu, wait_bar(smem_u32(&bar_empty[s]), round & 1, p.wait_ns));
@@ -770,14 +795,28 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
                 for (int c = 0; c < COLS; c += PC) {
                     if (c0 + c >= p.N) break;
                     if (bias) {
-                        const float mine = lane < PC && c0 + c + lane < p.N ? __ldg(bias + c + lane) : 0.f;
+                        if (p.vec_bias && c0 + c + PC <= p.N) {
 #pragma unroll
-                        for (int i = 0; i < PC; ++i) v[c + i] += __shfl_sync(0xffffffffu, mine, i);
+                            for (int i = 0; i < PC; i += 4) {
+                                const float4 x = __ldg(reinterpret_cast<const float4 *>(bias + c + i));
+                                v[c + i] += x.x; v[c + i + 1] += x.y; v[c + i + 2] += x.z; v[c + i + 3] += x.w;
+                            }
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < PC; ++i) v[c + i] += c0 + c + i < p.N ? __ldg(bias + c + i) : 0.f;
+                        }
                     }
                     if (p.relu)
 #pragma unroll
                         for (int i = 0; i < PC; ++i) v[c + i] = v[c + i] < 0.f ? 0.f : v[c + i];
-                    put_columns<T, 64>(dst + c, p.ldc, j.row_end - row, p.N - (c0 + c), v + c, p.vec_c, stage, false);
+                    if (p.vec_c) {
+                        uint8_t *half = stage + (c / PC & 1) * 2048;  // the store before may still read the other half
+                        stage_free<1>();
+                        stage_columns<T, 64, PC>(0, v + c, half);
+                        put_rows<T, 64>(p.tma_c ? &mapC : nullptr, c0 + c, row, dst + c, p.ldc, j.row_end - row, p.N - (c0 + c), half);
+                    } else {
+                        put_columns<T, 64>(dst + c, p.ldc, j.row_end - row, p.N - (c0 + c), v + c, 0, stage, false);
+                    }
                 }
             } else if (j.slot < 0) {
                 const int row = j.kt * ROWS + rank * 128 + quarter * 32;
@@ -821,116 +860,109 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
                 ++summed;
             }
         }
-    } else if (!TMA_A) {
+        if (!WGRAD && lane == 0) tma_store_wait_all();
+    } else if (SPLIT) {
         more_registers<GP_REGS_LOADS>();
-        // ---- FP32 operands through registers, a block of 64 terms in two halves (of A alone, or A and dZ): while the pieces of one are
-        // put down, those of the next are under way
-        constexpr bool BOTH = !TMA_B;
+        // ---- the FP32 operand that is split on its way: four pieces per thread and block of 64 terms.  While those of one block are put
+        // down, those of the next are under way, and what comes after them is asked into L2.
+        constexpr bool MN = WGRAD;
+        constexpr uint32_t part = WGRAD ? b_bytes : a_bytes;
         const int lt = threadIdx.x - (4 + EPI) * 32;
+        uint8_t *const first = smem + (WGRAD ? PARTS * a_bytes : 0);
         int s = 0, round = 0, summed = 0;
         bool ok = true;
         Piece8 x[4], y[4];
         float col[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        auto load = [&](Piece8 (&d)[4], const float *base, int64_t ld, int row, int row_end, int col0, int limit, bool mn) {
+        auto load = [&](Piece8 (&d)[4], int kb) {
+            const int row = MN ? j.row0 + kb * 64 + (lt >> 4) : j.row0 + (lt >> 3), c = MN ? j.nt * 128 + 8 * (lt & 15) : kb * 64 + 8 * (lt & 7), limit = MN ? p.N : p.K;
+            const float *at = p.reg + (int64_t)row * p.ld_reg;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int q = lt + 256 * i, r = row + (mn ? q >> 4 : q >> 3), c = col0 + 8 * (mn ? q & 15 : q & 7);
-                if (r < row_end && c < limit) d[i].load(base + (int64_t)r * ld, c, limit);
+                const int r = (MN ? 16 : 32) * i;
+                if (row + r < j.row_end && c < limit) d[i].load(at + (int64_t)r * p.ld_reg, c, limit);
                 else d[i].zero();
             }
         };
-        auto load_a = [&](Piece8 (&d)[4], const GroupedJob &w, int kb) {
-            if (WGRAD) load(d, (const float *)p.A, p.lda, w.row0 + kb * 64, w.row_end, w.kt * 128, p.K, true);
-            else load(d, (const float *)p.A, p.lda, w.row0, w.row_end, kb * 64, p.K, false);
+        auto ahead = [&](int kb) {  // into L2: 32 columns (a line) of one row per thread
+            const int row = MN ? j.row0 + kb * 64 + (lt >> 2) : j.row0 + (lt >> 1), c = MN ? j.nt * 128 + 32 * (lt & 3) : kb * 64 + 32 * (lt & 1);
+            if (row < j.row_end && c < (MN ? p.N : p.K)) asm volatile("prefetch.global.L2 [%0];" ::"l"(p.reg + (int64_t)row * p.ld_reg + c));
         };
-        auto put = [&](const Piece8 (&d)[4], uint8_t *dst, uint32_t part, bool mn) {
+        auto put = [&](const Piece8 (&d)[4]) {
+            uint8_t *dst = first + (size_t)s * stage_bytes;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int q = lt + 256 * i, r = mn ? q >> 4 : q >> 3, c = mn ? q & 15 : q & 7;
+                const int q = lt + 256 * i, r = MN ? q >> 4 : q >> 3, c = MN ? q & 15 : q & 7;
                 uint8_t *at = dst + (c >> 3) * 8192 + r * 128 + (((c & 7) ^ (r & 7)) << 4);
                 d[i].parts([&](int k, const uint4 &w) { *reinterpret_cast<uint4 *>(at + k * part) = w; });
             }
         };
-        auto free_stage = [&]() {
+        int kb = 0, done_kt = 0, done_nt = 0, done_g = 0, done_slot = 0;
+        bool more = next_job(), last = false;
+        constexpr int AHEAD = 6;  // blocks that are asked into L2
+        auto open_job = [&]() {
+            for (int i = 0; i < AHEAD && i < j.kbs; ++i) ahead(i);
+        };
+        if (more) {
+            open_job();
+            load(x, 0);
+        }
+        // one block: the pieces in `cur` go into the stage, the next block's into `nxt`
+        auto step = [&](Piece8 (&cur)[4], Piece8 (&nxt)[4]) {
+            done_kt = j.kt; done_nt = j.nt; done_g = j.g; done_slot = j.slot;
+            last = ++kb == j.kbs;
+            if (last) {
+                kb = 0;
+                more = next_job();
+                if (more) open_job();
+            } else if (kb + AHEAD - 1 < j.kbs) {
+                ahead(kb + AHEAD - 1);
+            }
+            if (more) load(nxt, kb);
             if (round > 0) {
                 ok = __all_sync(0xffffffffu, wait_bar(smem_u32(&bar_empty[s]), (round & 1) ^ 1, p.wait_ns));
-                if (!ok && lane == 0) atomicExch(p.err, 1);
+                if (!ok) { if (lane == 0) atomicExch(p.err, 1); return; }
             }
-            return ok;
-        };
-        auto full_stage = [&]() {
+            put(cur);
             fence_async_proxy();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&bar_full[s]));
             if (++s == S) { s = 0; ++round; }
-        };
-        int kb = 0;
-        bool more = next_job();
-        auto advance = [&]() {  // true: that was the job's last block
-            if (++kb < j.kbs) return false;
-            kb = 0;
-            more = next_job();
-            return true;
-        };
-        if (more) load_a(x, j, 0);
-        if (!BOTH) {
-            while (more) {
-                advance();
-                if (more) load_a(y, j, kb);
-                if (!free_stage()) break;
-                put(x, smem + (size_t)s * stage_bytes, a_bytes, A_MN);
-                full_stage();
-                if (!more) break;
-                advance();
-                if (more) load_a(x, j, kb);
-                if (!free_stage()) break;
-                put(y, smem + (size_t)s * stage_bytes, a_bytes, A_MN);
-                full_stage();
-            }
-        } else {
-            while (more) {
-                load(y, (const float *)p.B, p.ldb, j.row0 + kb * 64, j.row_end, j.nt * 128, p.N, true);
-                if (!free_stage()) break;
-                uint8_t *st = smem + (size_t)s * stage_bytes;
-                put(x, st, a_bytes, A_MN);
-                const GroupedJob cur = j;
-                const bool last = advance();
-                if (more) load_a(x, j, kb);
-                put(y, st + PARTS * a_bytes, b_bytes, B_MN);
-                full_stage();
-                if (sums && cur.kt == 0) {
+            if (!sums || done_kt != 0) return;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) add8(col, y[i].v);
-                    if (last) {
-                        // a thread has the rows 16 i + lt / 16 of its eight columns: sixteen sums per column, added up in order
-                        float *area = reinterpret_cast<float *>(extra + EPI * 2048);
-                        if (summed > 0) {
-                            ok = __all_sync(0xffffffffu, wait_bar(smem_u32(&bar_sum_empty), (summed - 1) & 1, p.wait_ns));
-                            if (!ok) { if (lane == 0) atomicExch(p.err, 7); break; }
+            for (int i = 0; i < 4; ++i) add8(col, cur[i].v);
+            if (!last) return;
+            // a thread has the rows 16 i + lt / 16 of its eight columns: sixteen sums per column, added up in order
+            float *area = reinterpret_cast<float *>(extra + EPI * 2048);
+            if (summed > 0) ok = __all_sync(0xffffffffu, wait_bar(smem_u32(&bar_sum_empty), (summed - 1) & 1, p.wait_ns));
+            if (ok) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) { area[(lt >> 4) * 128 + (lt & 15) * 8 + i] = col[i]; col[i] = 0.f; }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&bar_sum_full));
+                if (lt < 128) {
+                    ok = __all_sync(0xffffffffu, wait_bar(smem_u32(&bar_sum_full), summed & 1, p.wait_ns));
+                    if (ok) {
+                        float v = 0.f;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) v += area[i * 128 + lt];
+                        const int c = done_nt * 128 + lt;
+                        if (done_slot >= 0) p.slots[((size_t)done_slot * 129 + 128) * BN + lt] = v;
+                        else if (c < p.N) {
+                            float *d = p.dbias + (int64_t)done_g * p.N + c;
+                            *d = p.accumulate ? *d + v : v;
                         }
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) { area[(lt >> 4) * 128 + (lt & 15) * 8 + i] = col[i]; col[i] = 0.f; }
                         __syncwarp();
-                        if (lane == 0) mbar_arrive(smem_u32(&bar_sum_full));
-                        if (lt < 128) {
-                            ok = __all_sync(0xffffffffu, wait_bar(smem_u32(&bar_sum_full), summed & 1, p.wait_ns));
-                            if (!ok) { if (lane == 0) atomicExch(p.err, 7); break; }
-                            float v = 0.f;
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) v += area[i * 128 + lt];
-                            const int c = cur.nt * 128 + lt;
-                            if (cur.slot >= 0) p.slots[((size_t)cur.slot * 129 + 128) * BN + lt] = v;
-                            else if (c < p.N) {
-                                float *d = p.dbias + (int64_t)cur.g * p.N + c;
-                                *d = p.accumulate ? *d + v : v;
-                            }
-                            __syncwarp();
-                            if (lane == 0) mbar_arrive(smem_u32(&bar_sum_empty));
-                        }
-                        ++summed;
+                        if (lane == 0) mbar_arrive(smem_u32(&bar_sum_empty));
                     }
                 }
             }
+            if (!ok && lane == 0) atomicExch(p.err, 7);
+            ++summed;
+        };
+        while (more && ok) {
+            step(x, y);
+            if (!more || !ok) break;
+            step(y, x);
         }
     }
     __syncwarp();
@@ -950,17 +982,25 @@ template <bool PAIR> __global__ void __launch_bounds__(256) grouped_splits_kerne
     LP_DEP_ENTER();
     const GroupedSplit sp = p.splits[blockIdx.x];
     if (sp.first_slot < 0) return;
-    constexpr int EACH = 4, BN = GP_BN<PAIR>, BLOCKS = PAIR ? 2 : 1;  // blocks of a worker
+    constexpr int EACH = 2, BN = GP_BN<PAIR>, BLOCKS = PAIR ? 2 : 1, AT_ONCE = 8;  // BLOCKS: of a worker
     const int worker = blockIdx.x / BLOCKS, rank = blockIdx.x % BLOCKS, workers = gridDim.x / BLOCKS;
     float v[EACH];
     const int at = blockIdx.y * 256 * EACH + threadIdx.x, size = 129 * BN;
+    const bool gaps = sp.blocks < workers;  // some workers have no share
 #pragma unroll
     for (int i = 0; i < EACH; ++i) v[i] = at + 256 * i < size ? p.slots[((size_t)sp.first_slot * BLOCKS + rank) * size + at + 256 * i] : 0.f;
-    for (int c = worker + 1; c <= sp.last_block; ++c) {
-        if (sp.blocks * c / workers == sp.blocks * (c + 1) / workers) continue;  // a worker without a share
+    for (int c = worker + 1; c <= sp.last_block; c += AT_ONCE) {
+        float x[AT_ONCE][EACH];
 #pragma unroll
-        for (int i = 0; i < EACH; ++i)
-            if (at + 256 * i < size) v[i] += p.slots[((size_t)(2 * c) * BLOCKS + rank) * size + at + 256 * i];
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const bool there = c + k <= sp.last_block && !(gaps && sp.blocks * (c + k) / workers == sp.blocks * (c + k + 1) / workers);
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) x[k][i] = there && at + 256 * i < size ? p.slots[((size_t)(2 * (c + k)) * BLOCKS + rank) * size + at + 256 * i] : 0.f;
+        }
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k)
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) v[i] += x[k][i];
     }
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
@@ -1006,7 +1046,7 @@ static bool grouped_map_3d(const TcState &tc, CUtensorMap *map, const bf16 *base
     return false;
 }
 
-template <int MODE, typename T, bool PAIR> static void grouped_launch_one(Exec &ex, const CUtensorMap &a, const CUtensorMap &b, GroupedParams &p, int blocks)
+template <int MODE, typename T, bool PAIR> static void grouped_launch_one(Exec &ex, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &c, GroupedParams &p, int blocks)
 {
     constexpr int stage = GP_STAGE_BYTES<T>;
     constexpr int extra = GP_EXTRA_SMEM<GP_WIDE<MODE, PAIR>>;
@@ -1026,13 +1066,13 @@ template <int MODE, typename T, bool PAIR> static void grouped_launch_one(Exec &
         attr[1].val.programmaticStreamSerializationAllowed = 1;
         cfg.attrs = attr;
         cfg.numAttrs = 2;
-        cudaLaunchKernelEx(&cfg, grouped_kernel<MODE, T, PAIR>, a, b, p);
+        cudaLaunchKernelEx(&cfg, grouped_kernel<MODE, T, PAIR>, a, b, c, p);
     } else {
-        launch_dep(grouped_kernel<MODE, T, PAIR>, dim3((unsigned)blocks), dim3(GP_THREADS), smem, ex.st, a, b, p);
+        launch_dep(grouped_kernel<MODE, T, PAIR>, dim3((unsigned)blocks), dim3(GP_THREADS), smem, ex.st, a, b, c, p);
     }
     ex.launches += 1;
     if (MODE == GP_WGRAD) {
-        launch_dep(grouped_splits_kernel<PAIR>, dim3((unsigned)blocks, (unsigned)ceil_div64(129 * GP_BN<PAIR>, 1024)), dim3(256), 0, ex.st, p);
+        launch_dep(grouped_splits_kernel<PAIR>, dim3((unsigned)blocks, (unsigned)ceil_div64(129 * GP_BN<PAIR>, 512)), dim3(256), 0, ex.st, p);
         ex.launches += 1;
     }
 }
@@ -1067,7 +1107,7 @@ template <typename T> static void grouped_prepare(Exec &ex, GroupedOperand &o, i
     const int64_t rows = o.matrices * o.rows;
     void *out = ws + o.offset;
     if (o.split) {
-        launch_dep(grouped_split_kernel, dim3((unsigned)ceil_div64(rows * (o.ld / 8), 256)), dim3(256), 0, ex.st, (const float *)o.at, rows, o.cols,
+        launch_dep(grouped_split_kernel, dim3((unsigned)ceil_div64(rows * (o.ld / 8), 256)), dim3(256), 0, ex.st, (const float *)o.at, rows, o.cols, ld_in,
                    (int)(on_16_bytes<float>(o.at, ld_in)), (bf16 *)out, o.ld, o.ld * rows);
     } else {
         constexpr int E = 16 / sizeof(T);
@@ -1089,7 +1129,7 @@ template <int MODE, typename T> static GroupedPlan grouped_plan(int64_t rows, in
 {
     constexpr bool WGRAD = MODE == GP_WGRAD;
     GroupedPlan g{};
-    g.a = grouped_operand<T>(A, 1, rows, K, lda, false, g.bytes);
+    g.a = grouped_operand<T>(A, 1, rows, K, lda, sizeof(T) == 4 && WGRAD, g.bytes);
     g.b = WGRAD ? grouped_operand<T>(B, 1, rows, N, ldb, false, g.bytes)
                 : grouped_operand<T>(B, groups, MODE == GP_NN ? K : N, MODE == GP_NN ? N : K, ldb, sizeof(T) == 4, g.bytes);
     const int64_t sms = tc_sm_count(), busy = std::min(rows, groups);
@@ -1105,32 +1145,44 @@ template <int MODE, typename T> static GroupedPlan grouped_plan(int64_t rows, in
 }
 template <int MODE, typename T> static bool grouped_launch(TcState &tc, Exec &ex, GroupedParams &p, GroupedPlan &g, int64_t lda, int64_t ldb, uint8_t *ws, std::string &err)
 {
-    CUtensorMap a{}, b{};
-    constexpr bool WGRAD = MODE == GP_WGRAD;
+    CUtensorMap a{}, b{}, c{};
+    constexpr bool WGRAD = MODE == GP_WGRAD, SPLIT = sizeof(T) == 4;
     const int side = g.pair ? 256 : 128;
     p.tiles_n = (int)ceil_div64(p.N, side);
     p.tiles_k = (int)ceil_div64(p.K, side);
     p.err = tc.err_word;
     p.wait_ns = tc.wait_limit_ns;
-    p.extra_tx = sizeof(T) == 2 || !WGRAD ? tc.overdeclare_tx : 0;
+    p.extra_tx = tc.overdeclare_tx;
     grouped_prepare<T>(ex, g.a, lda, ws);
     grouped_prepare<T>(ex, g.b, ldb, ws);
-    p.A = g.a.at; p.lda = g.a.ld; p.B = g.b.at; p.ldb = g.b.ld;
     p.slots = (float *)(ws + g.slots);
     p.splits = (GroupedSplit *)(ws + g.splits);
-    if (sizeof(T) == 2 && !tc_make_map(tc, &a, (const bf16 *)p.A, p.rows, p.K, p.lda, 64, WGRAD ? 64 : 128, err)) return false;
+    const GroupedOperand &reg = WGRAD ? g.b : g.a;
+    if (SPLIT) { p.reg = (const float *)reg.at; p.ld_reg = reg.ld; }
+    // operands that come by TMA
     if (WGRAD) {
-        if (sizeof(T) == 2 && !tc_make_map(tc, &b, (const bf16 *)p.B, p.rows, p.N, p.ldb, 64, 64, err)) return false;
-    } else if (!grouped_map_3d(tc, &b, (const bf16 *)p.B, p.groups * (int64_t)GP_PARTS<T>, g.b.rows, g.b.cols, p.ldb, MODE == GP_NN ? 64 : 128, err)) {
-        return false;
+        if (!grouped_map_3d(tc, &a, (const bf16 *)g.a.at, GP_PARTS<T>, p.rows, p.K, g.a.ld, 64, err)) return false;
+        if (!SPLIT && !tc_make_map(tc, &b, (const bf16 *)g.b.at, p.rows, p.N, g.b.ld, 64, 64, err)) return false;
+    } else {
+        if (!SPLIT && !tc_make_map(tc, &a, (const bf16 *)g.a.at, p.rows, p.K, g.a.ld, 64, 128, err)) return false;
+        if (!grouped_map_3d(tc, &b, (const bf16 *)g.b.at, p.groups * (int64_t)GP_PARTS<T>, g.b.rows, g.b.cols, g.b.ld, MODE == GP_NN ? 64 : 128, err)) return false;
+    }
+    p.tma_c = !WGRAD && p.vec_c;
+    if (p.tma_c) {  // boxes of a warp: 32 rows, 64 or 128 bytes wide, laid out as they are staged
+        const bool wide = g.pair;
+        cuuint64_t dims[2] = {(cuuint64_t)p.N, (cuuint64_t)p.rows}, strides[1] = {(cuuint64_t)p.ldc * sizeof(T)};
+        cuuint32_t box[2] = {(cuuint32_t)((wide ? 128 : 64) / sizeof(T)), 32}, estr[2] = {1, 1};
+        if (tc.encode(&c, SPLIT ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p.C, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                      wide ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+            p.tma_c = 0;  // a pitch that no tensor map takes: rows leave one by one
     }
     if (p.extra_tx) tc.overdeclare_tx = 0;
     if constexpr (sizeof(T) == 2) {
         if (g.pair) {
-            grouped_launch_one<MODE, T, true>(ex, a, b, p, g.blocks);
+            grouped_launch_one<MODE, T, true>(ex, a, b, c, p, g.blocks);
             return true;
         }
     }
-    grouped_launch_one<MODE, T, false>(ex, a, b, p, g.blocks);
+    grouped_launch_one<MODE, T, false>(ex, a, b, c, p, g.blocks);
     return true;
 }
