@@ -211,14 +211,13 @@ struct Piece8 {
     float v[8];
     LP_DEVINL void load(const float *row, int col, int limit)
     {
-        const int n = limit - col;
-        if (n >= 8) {
-            const float4 a = __ldg(reinterpret_cast<const float4 *>(row + col)), b = __ldg(reinterpret_cast<const float4 *>(row + col) + 1);
-            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-        } else {
+        const int n = limit - col;  // > 0
+        const float4 a = __ldg(reinterpret_cast<const float4 *>(row + col));
+        const float4 b = n > 4 ? __ldg(reinterpret_cast<const float4 *>(row + col) + 1) : make_float4(0.f, 0.f, 0.f, 0.f);
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        if (n < 8)  // of the last 16 bytes, which lie on one page, some may not be the row's
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = i < n ? __ldg(row + col + i) : 0.f;
-        }
+            for (int i = 1; i < 8; ++i) v[i] = i < n ? v[i] : 0.f;
     }
     LP_DEVINL void zero()
     {
@@ -286,9 +285,11 @@ __global__ void __launch_bounds__(256) grouped_split_kernel(const float *in, int
 // ---------------------------------------------------------------------------------------------
 // results
 // ---------------------------------------------------------------------------------------------
-// Neighbouring columns of a warp's 32 rows, a row per lane (RB bytes of it: 64 or 128): rows below `rows`, columns below `cols`.  They go
-// through shared memory (32 RB bytes), so that a store instruction writes whole runs of a few rows: 512 bytes, or sixteen elements of
-// two rows where the rows of the result do not start on 16 bytes.
+// A warp's results leave through shared memory, 32 rows of RB (64 or 128) bytes at a time: a lane puts its row there, and then the
+// whole runs of a few rows are written: by one TMA store, or 512 bytes per store instruction where only some of the rows are the
+// tile's (the end of a group) or the old values are added, or element by element where the rows of the result do not start on 16 bytes.
+// The code is kept short: the roles of a block run different parts of it, and when these did not fit into the instruction cache together
+// the results of an FP32 tile took 18,000 cycles.
 template <typename T, int RB> constexpr int PUT_COLS = RB / sizeof(T);
 template <int RB> LP_DEVINL int stage_place(int r, int q) { return r * RB + ((q ^ (RB == 128 ? r & 7 : (r >> 1) & 3)) << 4); }  // no two of eight lanes in the same banks
 // N columns of the lane's row, from column c on
@@ -302,40 +303,54 @@ template <typename T, int RB, int N> LP_DEVINL void stage_columns(int c, const f
         *reinterpret_cast<decltype(o.v) *>(stage + stage_place<RB>(threadIdx.x & 31, c / VN + q)) = o.v;
     }
 }
-template <typename T, int RB> LP_DEVINL void put_staged(T *dst, int64_t ld, int rows, int cols, const uint8_t *stage, bool accumulate)
+// the staged rows below `rows` and columns below `cols`
+template <typename T, int RB> LP_DEVINL void put_staged(T *dst, int64_t ld, int rows, int cols, int vec, const uint8_t *stage, bool accumulate)
 {
     constexpr int VN = Vec16<T>::N, PIECES = RB / 16, AT_ONCE = 32 / PIECES;  // rows of a store instruction
-    const int lane = threadIdx.x & 31, q = lane & (PIECES - 1);
-    T *d = dst + (int64_t)(lane / PIECES) * ld + q * VN;
-    if (q * VN < cols)
+    const int lane = threadIdx.x & 31;
+    __syncwarp();
+    if (vec) {
+        const int q = lane & (PIECES - 1);
+        T *d = dst + (int64_t)(lane / PIECES) * ld + q * VN;
+#pragma unroll 4
+        for (int r = lane / PIECES; r < (q * VN < cols ? rows : 0) && r < 32; r += AT_ONCE, d += AT_ONCE * ld) {
+            Vec16<T> o;
+            o.v = *reinterpret_cast<const decltype(o.v) *>(stage + stage_place<RB>(r, q));
+            if (accumulate) {
+                Vec16<T> old;
+                old.v = *reinterpret_cast<const decltype(o.v) *>(d);
+                float x[VN], y[VN];
+                old.to_float(x);
+                o.to_float(y);
 #pragma unroll
-        for (int i = 0; i < PIECES; ++i, d += AT_ONCE * ld) {
-            const int r = AT_ONCE * i + lane / PIECES;
-            if (r < rows) {
-                Vec16<T> o;
-                o.v = *reinterpret_cast<const decltype(o.v) *>(stage + stage_place<RB>(r, q));
-                if (accumulate) {
-                    Vec16<T> old;
-                    old.v = *reinterpret_cast<const decltype(o.v) *>(d);
-                    float x[VN], y[VN];
-                    old.to_float(x);
-                    o.to_float(y);
-#pragma unroll
-                    for (int k = 0; k < VN; ++k) y[k] += x[k];
-                    o.from_float(y);
-                }
-                o.store(d);
+                for (int k = 0; k < VN; ++k) y[k] += x[k];
+                o.from_float(y);
+            }
+            o.store(d);
+        }
+    } else {
+        const int count = min(rows, 32) * PUT_COLS<T, RB>;
+#pragma unroll 4
+        for (int i = lane; i < count; i += 32) {
+            const int r = i / PUT_COLS<T, RB>, c = i % PUT_COLS<T, RB>;
+            if (c < cols) {
+                const float x = to_f<T>(*reinterpret_cast<const T *>(stage + stage_place<RB>(r, c / VN) + c % VN * (int)sizeof(T)));
+                T *d = dst + (int64_t)r * ld + c;
+                *d = from_f<T>(accumulate ? to_f<T>(*d) + x : x);
             }
         }
+    }
+    __syncwarp();
 }
-// The staged rows leave by one TMA store of the warp, or, at the end of a group, whose next rows are not this tile's, row by row.
-template <int N> LP_DEVINL void stage_free()  // all stores but the last N of the warp have read their rows
+// all TMA stores of the warp but the last N have read their rows
+template <int N> LP_DEVINL void stage_free()
 {
     if ((threadIdx.x & 31) == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");
     __syncwarp();
 }
+// ... by TMA where `map` says so and all 32 rows are the tile's
 template <typename T, int RB>
-LP_DEVINL void put_rows(const CUtensorMap *map, int col, int row, T *dst, int64_t ld, int rows, int cols, const uint8_t *stage)
+LP_DEVINL void put_rows(const CUtensorMap *map, int col, int row, T *dst, int64_t ld, int rows, int cols, int vec, const uint8_t *stage)
 {
     if (map && rows >= 32) {
         fence_async_proxy();
@@ -345,40 +360,27 @@ LP_DEVINL void put_rows(const CUtensorMap *map, int col, int row, T *dst, int64_
             tma_store_commit();
         }
     } else {
-        __syncwarp();
-        put_staged<T, RB>(dst, ld, rows, cols, stage, false);
-        __syncwarp();
+        put_staged<T, RB>(dst, ld, rows, cols, vec, stage, false);
     }
 }
-template <typename T, int RB> LP_DEVINL void put_columns(T *dst, int64_t ld, int rows, int cols, const float *v, int vec, uint8_t *stage, bool accumulate)
+// bias and ReLU of N columns
+template <int N> LP_DEVINL void finish_columns(float *v, const float *bias, int vec, int cols, int relu)
 {
-    const int lane = threadIdx.x & 31;
-    if (vec) {
-        __syncwarp();
-        stage_columns<T, RB, PUT_COLS<T, RB>>(0, v, stage);
-        __syncwarp();
-        put_staged<T, RB>(dst, ld, rows, cols, stage, accumulate);
-        return;
-    }
-    float *s = reinterpret_cast<float *>(stage);
+    if (bias) {
+        if (vec && cols >= N) {
 #pragma unroll
-    for (int half = 0; half < PUT_COLS<T, RB> / 16; ++half) {
-        __syncwarp();
-#pragma unroll
-        for (int c = 0; c < 16; ++c) s[lane * 16 + (c ^ (lane & 15))] = v[half * 16 + c];
-        __syncwarp();
-        const int c = lane & 15;
-        if (half * 16 + c < cols)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int r = 2 * i + (lane >> 4);
-                if (r < rows) {
-                    T *d = dst + (int64_t)r * ld + half * 16 + c;
-                    const float x = s[r * 16 + (c ^ (r & 15))];
-                    *d = from_f<T>(accumulate ? to_f<T>(*d) + x : x);
-                }
+            for (int i = 0; i < N; i += 4) {
+                const float4 x = __ldg(reinterpret_cast<const float4 *>(bias + i));
+                v[i] += x.x; v[i + 1] += x.y; v[i + 2] += x.z; v[i + 3] += x.w;
             }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] += i < cols ? __ldg(bias + i) : 0.f;
+        }
     }
+    if (relu)
+#pragma unroll
+        for (int i = 0; i < N; ++i) asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(v[i]));  // NaN stays
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -640,12 +642,13 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
 #pragma unroll
                         for (int i = 0; i < 4; ++i) product(acc, da + i * step_a, db + i * step_b, in_flush != 0 || i != 0);
                     } else {
-                        constexpr int first[6] = {0, 2, 1, 0, 1, 0}, second[6] = {2, 0, 1, 1, 0, 0};  // the small products first, while the sums are small
+                        // parts 0 2, 2 0, 1 1, 0 1, 1 0, 0 0: the small products first, while the sums are small
+#pragma unroll 1
+                        for (int q = 0; q < 6; ++q) {
+                            const uint64_t qa = da + ((0x021010u >> 4 * (5 - q)) & 3u) * (a_bytes >> 4), qb = db + ((0x201100u >> 4 * (5 - q)) & 3u) * (b_bytes >> 4);
 #pragma unroll
-                        for (int q = 0; q < 6; ++q)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                product(acc, da + first[q] * (a_bytes >> 4) + i * step_a, db + second[q] * (b_bytes >> 4) + i * step_b, in_flush != 0 || q != 0 || i != 0);
+                            for (int i = 0; i < 4; ++i) product(acc, qa + i * step_a, qb + i * step_b, in_flush != 0 || q != 0 || i != 0);
+                        }
                     }
                     commit(bar_empty[s]);
                     if (done) commit(bar_acc_full[b]);
@@ -702,37 +705,18 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
                 const float *bias = p.bias ? p.bias + (int64_t)j.g * p.N + c0 : nullptr;
                 uint32_t at;
                 if (!take(at)) break;
-#pragma unroll
+                if (p.tma_c) stage_free<0>();
+#pragma unroll 1
                 for (int c = 0; c < COLS; c += 32) {
                     float v[32];
                     tmem_ld_32x16(at + c, v);
                     tmem_ld_32x16(at + c + 16, v + 16);
                     tmem_ld_wait();
                     if (c + 32 >= COLS) give_back();
-                    if (c0 + c >= p.N) continue;
-                    if (bias) {
-                        if (p.vec_bias && c0 + c + 32 <= p.N) {
-#pragma unroll
-                            for (int i = 0; i < 32; i += 4) {
-                                const float4 x = __ldg(reinterpret_cast<const float4 *>(bias + c + i));
-                                v[i] += x.x; v[i + 1] += x.y; v[i + 2] += x.z; v[i + 3] += x.w;
-                            }
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) v[i] += c0 + c + i < p.N ? __ldg(bias + c + i) : 0.f;
-                        }
-                    }
-                    if (p.relu)
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];  // NaN stays
-                    if (p.vec_c) {
-                        if (c == 0) stage_free<0>();
-                        stage_columns<T, COLS * 2, 32>(c, v, stage);
-                    } else {
-                        put_columns<T, 64>(dst + c, p.ldc, j.row_end - row, p.N - (c0 + c), v, 0, stage, false);
-                    }
+                    finish_columns<32>(v, bias ? bias + c : nullptr, p.vec_bias, p.N - (c0 + c), p.relu);
+                    stage_columns<T, COLS * 2, 32>(c, v, stage);
                 }
-                if (p.vec_c && c0 < p.N) put_rows<T, COLS * 2>(p.tma_c ? &mapC : nullptr, c0, row, dst, p.ldc, j.row_end - row, p.N - c0, stage);
+                if (c0 < p.N) put_rows<T, COLS * 2>(p.tma_c ? &mapC : nullptr, c0, row, dst, p.ldc, j.row_end - row, p.N - c0, p.vec_c, stage);
                 continue;
             }
             float v[COLS];
@@ -789,45 +773,30 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
             if (!WGRAD) {
                 const int row = j.row0 + quarter * 32;
                 T *dst = (T *)p.C + (int64_t)row * p.ldc + c0;
-                const float *bias = p.bias ? p.bias + (int64_t)j.g * p.N + c0 : nullptr;
                 constexpr int PC = PUT_COLS<T, 64>;
+                finish_columns<COLS>(v, p.bias ? p.bias + (int64_t)j.g * p.N + c0 : nullptr, p.vec_bias, p.N - c0, p.relu);
 #pragma unroll
                 for (int c = 0; c < COLS; c += PC) {
-                    if (c0 + c >= p.N) break;
-                    if (bias) {
-                        if (p.vec_bias && c0 + c + PC <= p.N) {
-#pragma unroll
-                            for (int i = 0; i < PC; i += 4) {
-                                const float4 x = __ldg(reinterpret_cast<const float4 *>(bias + c + i));
-                                v[c + i] += x.x; v[c + i + 1] += x.y; v[c + i + 2] += x.z; v[c + i + 3] += x.w;
-                            }
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < PC; ++i) v[c + i] += c0 + c + i < p.N ? __ldg(bias + c + i) : 0.f;
-                        }
-                    }
-                    if (p.relu)
-#pragma unroll
-                        for (int i = 0; i < PC; ++i) v[c + i] = v[c + i] < 0.f ? 0.f : v[c + i];
-                    if (p.vec_c) {
+                    if (c0 + c < p.N) {
                         uint8_t *half = stage + (c / PC & 1) * 2048;  // the store before may still read the other half
-                        stage_free<1>();
+                        if (p.tma_c) stage_free<1>();
                         stage_columns<T, 64, PC>(0, v + c, half);
-                        put_rows<T, 64>(p.tma_c ? &mapC : nullptr, c0 + c, row, dst + c, p.ldc, j.row_end - row, p.N - (c0 + c), half);
-                    } else {
-                        put_columns<T, 64>(dst + c, p.ldc, j.row_end - row, p.N - (c0 + c), v + c, 0, stage, false);
+                        put_rows<T, 64>(p.tma_c ? &mapC : nullptr, c0 + c, row, dst + c, p.ldc, j.row_end - row, p.N - (c0 + c), p.vec_c, half);
                     }
                 }
-            } else if (j.slot < 0) {
+            } else {
+                // the whole tile is this share's, or a partial tile of it
+                const bool whole = j.slot < 0;
                 const int row = j.kt * ROWS + rank * 128 + quarter * 32;
-                float *dst = p.dW + ((int64_t)j.g * p.K + row) * p.N + c0;
+                float *dst = whole ? p.dW + ((int64_t)j.g * p.K + row) * p.N + c0
+                                   : p.slots + (((size_t)j.slot * (ROWS / 128) + rank) * 129 + quarter * 32) * BN + part * COLS;
+                const int ld = whole ? p.N : BN, rows = whole ? p.K - row : 32, cols = whole ? p.N - c0 : COLS, vec = whole ? p.vec_c : 1;
 #pragma unroll
                 for (int c = 0; c < COLS; c += 16)
-                    if (c0 + c < p.N) put_columns<float, 64>(dst + c, p.N, p.K - row, p.N - (c0 + c), v + c, p.vec_c, stage, p.accumulate != 0);
-            } else {
-                float *dst = p.slots + (((size_t)j.slot * (ROWS / 128) + rank) * 129 + quarter * 32) * BN + part * COLS;
-#pragma unroll
-                for (int c = 0; c < COLS; c += 16) put_columns<float, 64>(dst + c, BN, 32, 16, v + c, 1, stage, false);
+                    if (c < cols) {
+                        stage_columns<float, 64, 16>(0, v + c, stage);
+                        put_staged<float, 64>(dst + c, ld, rows, cols - c, vec, stage, whole && p.accumulate != 0);
+                    }
             }
             if (adds) {
                 // every warp leaves its sums of a few rows in its own part of the area; the first BH threads add them up in order
