@@ -416,7 +416,7 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
                                                                  const __grid_constant__ CUtensorMap mapC, const __grid_constant__ GroupedParams p)
 {
     LP_DEP_ENTER();
-    constexpr int PARTS = GP_PARTS<T>, BN = GP_BN<PAIR>, BH = 128, ROWS = PAIR ? 256 : 128;
+    constexpr int PARTS = GP_PARTS<T>, BN = GP_BN<PAIR>, BH = 128, ROWS = PAIR ? 256 : 128, ACCS = 512 / BN;  // accumulators used in turn: all of tensor memory
     constexpr bool WGRAD = MODE == GP_WGRAD, SPLIT = PARTS == 3, TMA_A = !SPLIT || WGRAD, TMA_B = !SPLIT || !WGRAD;
     constexpr bool A_MN = WGRAD, B_MN = MODE != GP_NT;
     constexpr int EPI = SPLIT ? 8 : 16, COLS = BN * 4 / EPI;  // warps of sums and results, columns of each
@@ -424,7 +424,7 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
     constexpr uint32_t a_bytes = 128 * 128, b_bytes = BH * 128, stage_bytes = GP_STAGE_BYTES<T>, tma_bytes = (TMA_A ? PARTS * a_bytes : 0) + (TMA_B ? PARTS * b_bytes : 0);
     static_assert(!PAIR || PARTS == 1, "pairs take BF16 operands");
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t bar_full[GP_MAX_STAGES], bar_empty[GP_MAX_STAGES], bar_read[GP_MAX_STAGES], bar_acc_full[2], bar_acc_empty[2], bar_sum_full, bar_sum_empty,
+    __shared__ __align__(8) uint64_t bar_full[GP_MAX_STAGES], bar_empty[GP_MAX_STAGES], bar_read[GP_MAX_STAGES], bar_acc_full[ACCS], bar_acc_empty[ACCS], bar_sum_full, bar_sum_empty,
         bar_done, bar_tail;
     __shared__ __align__(8) uint64_t bar_job_full[GP_JOBS], bar_job_empty[GP_JOBS];
     __shared__ __align__(16) GroupedJob jobs_s[GP_JOBS];
@@ -478,7 +478,7 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
             mbar_init(smem_u32(&bar_empty[s]), 1);
             mbar_init(smem_u32(&bar_read[s]), EPI);
         }
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < ACCS; ++b) {
             mbar_init(smem_u32(&bar_acc_full[b]), 1);
             mbar_init(smem_u32(&bar_acc_empty[b]), PAIR ? 2 * EPI : EPI);
         }
@@ -498,8 +498,8 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
     }
     if (warp == 0) {
         __syncwarp();
-        if (PAIR) tmem_alloc_pair(smem_u32(&tmem_base_s), 2 * BN);
-        else tmem_alloc(smem_u32(&tmem_base_s), 2 * BN);
+        if (PAIR) tmem_alloc_pair(smem_u32(&tmem_base_s), ACCS * BN);
+        else tmem_alloc(smem_u32(&tmem_base_s), ACCS * BN);
     }
     tc_fence_before();
     __syncthreads();
@@ -622,8 +622,8 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
         while (leader && ok && next_job()) {
             int in_flush = 0;
             for (int kb = 0; kb < j.kbs && ok; ++kb) {
-                const int b = use & 1;
-                if (in_flush == 0 && use >= 2 && !wait_bar(smem_u32(&bar_acc_empty[b]), ((use >> 1) & 1) ^ 1, p.wait_ns)) {
+                const int b = use % ACCS;
+                if (in_flush == 0 && use >= ACCS && !wait_bar(smem_u32(&bar_acc_empty[b]), ((use / ACCS) & 1) ^ 1, p.wait_ns)) {
                     if (lane == 0) atomicExch(p.err, 5);
                     ok = false;
                 }
@@ -680,8 +680,8 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
         bool ok = true;
         // the accumulator that holds the next sums; false when the wait ran out
         auto take = [&](uint32_t &at) {
-            const int b = use & 1;
-            ok = __all_sync(0xffffffffu, wait_bar(smem_u32(&bar_acc_full[b]), (use >> 1) & 1, p.wait_ns));
+            const int b = use % ACCS;
+            ok = __all_sync(0xffffffffu, wait_bar(smem_u32(&bar_acc_full[b]), (use / ACCS) & 1, p.wait_ns));
             if (!ok) { if (lane == 0) atomicExch(p.err, 3); return false; }
             tc_fence_after();
             at = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(b * BN + part * COLS);
@@ -691,8 +691,8 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
             tc_fence_before();
             __syncwarp();
             if (lane == 0) {
-                if (PAIR) mbar_arrive_remote(acc_free + (use & 1) * 8);
-                else mbar_arrive(acc_free + (use & 1) * 8);
+                if (PAIR) mbar_arrive_remote(acc_free + (use % ACCS) * 8);
+                else mbar_arrive(acc_free + (use % ACCS) * 8);
             }
             ++use;
         };
@@ -940,8 +940,8 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
     if (PAIR) cluster_barrier();  // neither block frees tensor memory, or leaves with barriers the other may still signal, before both are done
     if (warp == 0) {
         __syncwarp();
-        if (PAIR) tmem_dealloc_pair(tmem, 2 * BN);
-        else tmem_dealloc(tmem, 2 * BN);
+        if (PAIR) tmem_dealloc_pair(tmem, ACCS * BN);
+        else tmem_dealloc(tmem, ACCS * BN);
     }
 }
 
