@@ -425,7 +425,7 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
     static_assert(!PAIR || PARTS == 1, "pairs take BF16 operands");
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bar_full[GP_MAX_STAGES], bar_empty[GP_MAX_STAGES], bar_read[GP_MAX_STAGES], bar_acc_full[ACCS], bar_acc_empty[ACCS], bar_sum_full, bar_sum_empty,
-        bar_done, bar_tail;
+        bar_done, bar_tail[GP_MAX_STAGES];
     __shared__ __align__(8) uint64_t bar_job_full[GP_JOBS], bar_job_empty[GP_JOBS];
     __shared__ __align__(16) GroupedJob jobs_s[GP_JOBS];
     __shared__ uint32_t tmem_base_s;
@@ -477,6 +477,7 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
             mbar_init(smem_u32(&bar_full[s]), (PAIR ? 2 : 1) + LOADERS);
             mbar_init(smem_u32(&bar_empty[s]), 1);
             mbar_init(smem_u32(&bar_read[s]), EPI);
+            mbar_init(smem_u32(&bar_tail[s]), 1);
         }
         for (int b = 0; b < ACCS; ++b) {
             mbar_init(smem_u32(&bar_acc_full[b]), 1);
@@ -486,10 +487,9 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
         mbar_init(smem_u32(&bar_sum_empty), BH / 32);
         for (int i = 0; i < GP_JOBS; ++i) {
             mbar_init(smem_u32(&bar_job_full[i]), 1);
-            mbar_init(smem_u32(&bar_job_empty[i]), 1 + (leader ? 1 : 0) + EPI + LOADERS);
+            mbar_init(smem_u32(&bar_job_empty[i]), 1 + (leader ? 1 : 0) + (WGRAD ? 1 : 0) + EPI + LOADERS);
         }
         mbar_init(smem_u32(&bar_done), 1);
-        mbar_init(smem_u32(&bar_tail), 1);
         fence_barrier_init();
         fence_async_proxy();
         if (TMA_A) tma_prefetch_desc(&mapA);
@@ -527,7 +527,7 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
         fewer_registers<GP_REGS_CONTROL>();
         {
             // ---- operands by TMA: this block's 128 rows (weight gradient: columns) of A and its BH columns of B
-            int s = 0, round = 0, tails = 0;
+            int s = 0, round = 0;
             bool ok = true, first = blockIdx.x == (WGRAD ? gridDim.x - 1 : 0);  // a block that has work in any case
             while (ok && next_job()) {
                 for (int kb = 0; kb < j.kbs && ok; ++kb) {
@@ -539,12 +539,12 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
                     const uint32_t sa = smem_u32(smem) + s * stage_bytes, sb = sa + PARTS * a_bytes;
                     uint32_t bar = smem_u32(&bar_full[s]);
                     const int have = j.row_end - (j.row0 + kb * 64);
-                    const bool tail = WGRAD && have < 64;  // the last rows of a group: they arrive here first
+                    const bool tail = WGRAD && have < 64;  // the last rows of a group: warp 3 gets them first
                     if (elect_one()) {
                         const uint32_t more = first ? (uint32_t)p.extra_tx : 0u;
                         if (tail) {
-                            mbar_expect_tx(smem_u32(&bar_tail), tma_bytes + more);
-                            bar = smem_u32(&bar_tail);
+                            mbar_expect_tx(smem_u32(&bar_tail[s]), tma_bytes + more);
+                            bar = smem_u32(&bar_tail[s]);
                             if (PAIR) bar = map_to_cta(bar, rank);
                         } else if (PAIR) {
                             bar = map_to_cta(bar, 0);
@@ -576,26 +576,11 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
                     }
                     __syncwarp();
                     first = false;
-                    if (tail) {
-                        // rows behind the group belong to the next one (or to nobody): zeros, whatever they hold
-                        ok = __all_sync(0xffffffffu, wait_bar(smem_u32(&bar_tail), tails & 1, p.wait_ns));
-                        if (!ok) { if (lane == 0) atomicExch(p.err, 2); break; }
-                        ++tails;
-                        uint8_t *st = smem + (size_t)s * stage_bytes + max(have, 0) * 128;
-                        for (int i = lane; i < (64 - max(have, 0)) * 8; i += 32)
-#pragma unroll
-                            for (int c = 0; c < (SPLIT ? 6 : 4); ++c) *reinterpret_cast<uint4 *>(st + c * 8192 + i * 16) = make_uint4(0u, 0u, 0u, 0u);
-                        fence_async_proxy();
-                        __syncwarp();
-                        if (lane == 0) {
-                            if (PAIR) mbar_arrive_remote(map_to_cta(smem_u32(&bar_full[s]), 0));
-                            else mbar_arrive(smem_u32(&bar_full[s]));
-                        }
-                    }
                     if (++s == S) { s = 0; ++round; }
                 }
             }
-            // copies under way land before the block gives up its shared memory (after a wait that ran out; else they long have)
+            // copies under way land before the block gives up its shared memory (after a wait that ran out; else they long have; those of
+            // a group's last block warp 3 waits for)
             if (lane == 0 && leader)
                 for (int i = 0; i < S; ++i) {
                     const int at = s - 1 - i < 0 ? s - 1 - i + S : s - 1 - i, r = s - 1 - i < 0 ? round - 1 : round;
@@ -668,6 +653,32 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
         __syncwarp();
     } else if (warp == 3) {
         fewer_registers<GP_REGS_CONTROL>();
+        if (WGRAD) {
+            // ---- the last block of a group, before it is multiplied: rows behind the group belong to the next one (or to nobody): zeros in what TMA
+            // brought, whatever they hold
+            int at = 0;
+            uint32_t phase = 0;  // of each stage's barrier
+            bool ok = true;
+            while (ok && next_job()) {
+                const int kb = j.kbs - 1, have = j.row_end - (j.row0 + kb * 64);
+                at += j.kbs;
+                if (have >= 64) continue;
+                const int s = (at - 1) % S;
+                ok = __all_sync(0xffffffffu, wait_bar(smem_u32(&bar_tail[s]), phase >> s & 1, p.wait_ns));
+                if (!ok) { if (lane == 0) atomicExch(p.err, 2); break; }
+                phase ^= 1u << s;
+                uint8_t *st = smem + (size_t)s * stage_bytes + max(have, 0) * 128;
+                for (int i = lane; i < (64 - max(have, 0)) * 8; i += 32)
+#pragma unroll
+                    for (int c = 0; c < (SPLIT ? 6 : 4); ++c) *reinterpret_cast<uint4 *>(st + c * 8192 + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+                fence_async_proxy();
+                __syncwarp();
+                if (lane == 0) {
+                    if (PAIR) mbar_arrive_remote(map_to_cta(smem_u32(&bar_full[s]), 0));
+                    else mbar_arrive(smem_u32(&bar_full[s]));
+                }
+            }
+        }
     } else if (warp < 4 + EPI) {
         more_registers<GP_REGS_SUMS>();
         // ---- sums and results: 32 rows x COLS columns per warp
@@ -951,40 +962,36 @@ template <bool PAIR> __global__ void __launch_bounds__(256) grouped_splits_kerne
     LP_DEP_ENTER();
     const GroupedSplit sp = p.splits[blockIdx.x];
     if (sp.first_slot < 0) return;
-    constexpr int EACH = 2, BN = GP_BN<PAIR>, BLOCKS = PAIR ? 2 : 1, AT_ONCE = 8;  // BLOCKS: of a worker
+    constexpr int BN = GP_BN<PAIR>, BLOCKS = PAIR ? 2 : 1, AT_ONCE = 8, size = 129 * BN / 4;  // BLOCKS: of a worker; sizes in float4
     const int worker = blockIdx.x / BLOCKS, rank = blockIdx.x % BLOCKS, workers = gridDim.x / BLOCKS;
-    float v[EACH];
-    const int at = blockIdx.y * 256 * EACH + threadIdx.x, size = 129 * BN;
+    const int at = blockIdx.y * 256 + threadIdx.x;
+    if (at >= size) return;
+    const float4 *slots = reinterpret_cast<const float4 *>(p.slots);
     const bool gaps = sp.blocks < workers;  // some workers have no share
-#pragma unroll
-    for (int i = 0; i < EACH; ++i) v[i] = at + 256 * i < size ? p.slots[((size_t)sp.first_slot * BLOCKS + rank) * size + at + 256 * i] : 0.f;
+    float4 v = slots[((size_t)sp.first_slot * BLOCKS + rank) * size + at];
     for (int c = worker + 1; c <= sp.last_block; c += AT_ONCE) {
-        float x[AT_ONCE][EACH];
+        float4 x[AT_ONCE];
 #pragma unroll
         for (int k = 0; k < AT_ONCE; ++k) {
             const bool there = c + k <= sp.last_block && !(gaps && sp.blocks * (c + k) / workers == sp.blocks * (c + k + 1) / workers);
-#pragma unroll
-            for (int i = 0; i < EACH; ++i) x[k][i] = there && at + 256 * i < size ? p.slots[((size_t)(2 * (c + k)) * BLOCKS + rank) * size + at + 256 * i] : 0.f;
+            x[k] = there ? slots[((size_t)(2 * (c + k)) * BLOCKS + rank) * size + at] : make_float4(0.f, 0.f, 0.f, 0.f);
         }
 #pragma unroll
-        for (int k = 0; k < AT_ONCE; ++k)
-#pragma unroll
-            for (int i = 0; i < EACH; ++i) v[i] += x[k][i];
+        for (int k = 0; k < AT_ONCE; ++k) { v.x += x[k].x; v.y += x[k].y; v.z += x[k].z; v.w += x[k].w; }
     }
-#pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-        const int row = (at + 256 * i) / BN, in_tile = (at + 256 * i) % BN, col = sp.nt * BN + in_tile, k = (sp.kt * BLOCKS + rank) * 128 + row;
-        if (row > 128 || col >= p.N) continue;
-        float *d;
-        if (row < 128) {
-            if (k >= p.K) continue;
-            d = p.dW + ((int64_t)sp.group * p.K + k) * p.N + col;
-        } else {
-            if (!p.dbias || sp.kt != 0 || in_tile / 128 != rank) continue;  // a block adds up the 128 columns it brings in
-            d = p.dbias + (int64_t)sp.group * p.N + col;
-        }
-        *d = p.accumulate ? *d + v[i] : v[i];
+    const int row = at * 4 / BN, in_tile = at * 4 % BN, col = sp.nt * BN + in_tile, k = (sp.kt * BLOCKS + rank) * 128 + row;
+    float *d;
+    if (row < 128) {
+        if (k >= p.K) return;
+        d = p.dW + ((int64_t)sp.group * p.K + k) * p.N + col;
+    } else {
+        if (!p.dbias || sp.kt != 0 || in_tile / 128 != rank) return;  // a block adds up the 128 columns it brings in
+        d = p.dbias + (int64_t)sp.group * p.N + col;
     }
+    const float w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (col + i < p.N) d[i] = p.accumulate ? d[i] + w[i] : w[i];
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -1041,7 +1048,7 @@ template <int MODE, typename T, bool PAIR> static void grouped_launch_one(Exec &
     }
     ex.launches += 1;
     if (MODE == GP_WGRAD) {
-        launch_dep(grouped_splits_kernel<PAIR>, dim3((unsigned)blocks, (unsigned)ceil_div64(129 * GP_BN<PAIR>, 512)), dim3(256), 0, ex.st, p);
+        launch_dep(grouped_splits_kernel<PAIR>, dim3((unsigned)blocks, (unsigned)ceil_div64(129 * GP_BN<PAIR>, 1024)), dim3(256), 0, ex.st, p);
         ex.launches += 1;
     }
 }
