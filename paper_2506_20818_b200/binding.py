@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional, Sequence
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -85,6 +86,7 @@ class ResidualDesc(C.Structure):
 LP_NO_PADDING = -(1 << 31)
 LP_NORM_NONE, LP_NORM_RMS, LP_NORM_LAYER = 0, 1, 2
 _NORMS = {None: LP_NORM_NONE, "rms": LP_NORM_RMS, "layer": LP_NORM_LAYER}
+_RESIDUAL = struct.Struct("qiiiii4xdddQQqQQQQQq")  # ResidualDesc, packed in one go: the fields of a Structure one by one take longer than the kernel
 
 # argument types of the calls whose latency counts: ctypes converts plain Python numbers by them
 _ARGTYPES = {
@@ -157,6 +159,7 @@ class Context:
         self.n = self.nnz = self.f = 0
         self.n_params = 0
         self._precs = {torch.float32: LP_FP32, torch.bfloat16: LP_BF16}
+        self._f32, self._empty_like = torch.float32, torch.empty_like
         self._raw_stream = self.stream.cuda_stream
         self.desc: Optional[ModelDesc] = None
 
@@ -455,59 +458,74 @@ class Context:
         return new
 
     # ---- residual blocks
-    def _words(self, seed, step, row_base, who: str):
-        if not (0 <= seed < 1 << 64 and 0 <= step < 1 << 64 and 0 <= row_base < 1 << 62):
-            self._refuse(f"{who}: seed and step are 64-bit numbers, row_base a number of rows")
-
     def dropout(self, x, p: float, seed: int, step: int, row_base: int = 0, out=None):
         """Dropout of a matrix (float32 or bfloat16); the gradient is the same call on the gradient.  See lp_dropout."""
-        rows, width, ld = self._rows(x, "dropout")
-        prec = self._prec(x.dtype, "dropout")
-        self._words(seed, step, row_base, "dropout")
+        shape = x.shape
+        prec = self._precs.get(x.dtype)
+        if len(shape) != 2 or prec is None:
+            self._refuse(f"dropout: expected a float32 or bfloat16 matrix on cuda:{self.device}")
+        if not (0 <= seed < 1 << 64 and 0 <= step < 1 << 64 and 0 <= row_base < 1 << 62):
+            self._refuse("dropout: seed and step are 64-bit numbers, row_base a number of rows")
+        if shape[1] >= 1 << 31:
+            self._refuse("dropout: width must be in [1, 2^20]")
         if out is None:
-            out, ldo = x.new_empty((rows, width)), width
-        else:
-            r, d, ldo = self._rows(out, "dropout: out")
-            if r != rows or d != width or out.dtype != x.dtype:
-                self._refuse(f"dropout: out must be [{rows}, {width}] of the type of x")
-        cur = self._enter(x, out)
-        rc = self.lib.lp_dropout(self.h, prec, rows, width, x.data_ptr(), ld, p, seed, step, row_base, out.data_ptr(), ldo)
+            out = self._empty_like(x)
+        a, lda = self._matrix(x, shape, x.dtype, "dropout", "x")
+        b, ldb = self._matrix(out, shape, x.dtype, "dropout", "out")
+        cur = None
+        if self._torch._C._cuda_getCurrentRawStream(self.device) != self._raw_stream:
+            cur = self._enter(x, out)
+        rc = self.lib.lp_dropout(self.h, prec, shape[0], shape[1], a, lda, p, seed, step, row_base, b, ldb)
         if rc:
             self._ck(rc)
         if cur is not None:
             self._leave(cur)
         return out
 
-    def _column(self, v, width: int, who: str, name: str):
+    def _column(self, v, width: int, who: str, name: str) -> int:
+        """Address of a vector of the columns, 0 for None."""
         if v is None:
-            return None
-        if v.dtype is not self._torch.float32 or v.get_device() != self.device or v.numel() != width or not v.is_contiguous():
+            return 0
+        if v.dtype is not self._f32 or v.get_device() != self.device or v.numel() != width or not v.is_contiguous():
             self._refuse(f"{who}: {name} must be a contiguous float32 vector of {width} elements on cuda:{self.device}")
         return v.data_ptr()
 
-    def _matrix(self, v, rows: int, width: int, dtype, who: str, name: str):
-        """(address, row pitch) of a matrix that must have this shape and type."""
+    def _matrix(self, v, shape, dtype, who: str, name: str):
+        """(address, row pitch) of a matrix that must have this shape and type; (None, width) for None."""
         if v is None:
-            return None, width
-        r, d, ld = self._rows(v, who)
-        if r != rows or d != width or v.dtype != dtype:
-            self._refuse(f"{who}: {name} must be [{rows}, {width}] of {dtype}")
-        return v.data_ptr(), ld
+            return None, shape[1]
+        if v.shape != shape or v.dtype is not dtype or v.get_device() != self.device:
+            self._refuse(f"{who}: {name} must be [{shape[0]}, {shape[1]}] of {dtype} on cuda:{self.device}")
+        ld, step = v.stride()
+        if step != 1 and shape[1] > 1:
+            self._refuse(f"{who}: the elements of a row must be contiguous")
+        return v.data_ptr(), ld if shape[0] > 1 or ld > shape[1] else shape[1]
 
-    def _residual(self, who, like, prec_dtype, pre_norm, pre, pre_bias, post_norm, post, post_bias, gate, scale, p, seed, step, row_base, eps):
+    def _residual(self, who, like, dtype, pre_norm, pre, pre_bias, post_norm, post, post_bias, gate, scale, p, seed, step, row_base, eps):
+        """The descriptor (lp_residual_desc as bytes) and the shape of the call's matrices."""
+        shape = like.shape
+        if len(shape) != 2 or like.get_device() != self.device:
+            self._refuse(f"{who}: expected a matrix on cuda:{self.device}")
         if pre_norm not in _NORMS or post_norm not in _NORMS:
             self._refuse(f"{who}: norms are 'rms', 'layer' or None")
-        rows, width, _ = self._rows(like, who)
-        self._words(seed, step, row_base, who)
-        g = ldg = None
+        if not (0 <= seed < 1 << 64 and 0 <= step < 1 << 64 and 0 <= row_base < 1 << 62):
+            self._refuse(f"{who}: seed and step are 64-bit numbers, row_base a number of rows")
+        rows, width = shape
+        if width >= 1 << 31:
+            self._refuse(f"{who}: width must be in [1, 8192]")
+        g = ldg = 0
         if gate is not None:
             if gate.dim() == 1:
-                g, ldg = self._column(gate, width, who, "gate"), 0
+                g = self._column(gate, width, who, "gate")
             else:
-                g, ldg = self._matrix(gate, rows, width, prec_dtype, who, "gate")
-        return rows, width, ResidualDesc(rows, width, self._prec(like.dtype, who), self._prec(prec_dtype, who), _NORMS[pre_norm], _NORMS[post_norm], eps, scale, p, seed, step,
-                                         row_base, self._column(pre, width, who, "pre"), self._column(pre_bias, width, who, "pre_bias"),
-                                         self._column(post, width, who, "post"), self._column(post_bias, width, who, "post_bias"), g, ldg or 0)
+                g, ldg = self._matrix(gate, shape, dtype, who, "gate")
+        prec_s, prec_d = self._precs.get(like.dtype), self._precs.get(dtype)
+        if prec_s is None or prec_d is None:
+            self._refuse(f"{who}: float32 or bfloat16 expected, got {like.dtype} and {dtype}")
+        return shape, _RESIDUAL.pack(rows, width, prec_s, prec_d, _NORMS[pre_norm], _NORMS[post_norm], eps, scale, p, seed, step, row_base,
+                                     pre is not None and self._column(pre, width, who, "pre"), pre_bias is not None and self._column(pre_bias, width, who, "pre_bias"),
+                                     post is not None and self._column(post, width, who, "post"), post_bias is not None and self._column(post_bias, width, who, "post_bias"),
+                                     g, ldg)
 
     def residual_norm(self, x, h=None, pre_norm: Optional[str] = "rms", pre=None, pre_bias=None, post_norm: Optional[str] = None, post=None, post_bias=None,
                       gate=None, scale: float = 1.0, p: float = 0.0, seed: int = 0, step: int = 0, row_base: int = 0, eps: float = 1e-6, y=None, n=None, dtype=None):
@@ -517,22 +535,26 @@ class Context:
             dtype = h.dtype
         elif dtype is None:
             dtype = n.dtype if n is not None else x.dtype
-        rows, width, d = self._residual("residual_norm", x, dtype, pre_norm, pre, pre_bias, post_norm, post, post_bias, gate, scale, p, seed, step, row_base, eps)
+        shape, desc = self._residual("residual_norm", x, dtype, pre_norm, pre, pre_bias, post_norm, post, post_bias, gate, scale, p, seed, step, row_base, eps)
         if h is None:
             if y is not None and y is not x:
                 self._refuse("residual_norm: without h there is no y to write")
             y = x
         elif y is None:
-            y = x.new_empty((rows, width))
+            y = self._empty_like(x)
         if pre_norm is None:
             if n is not None:
                 self._refuse("residual_norm: without pre_norm there is no n to write")
         elif n is None:
-            n = x.new_empty((rows, width), dtype=dtype)
-        a = self._matrix(x, rows, width, x.dtype, "residual_norm", "x") + self._matrix(h, rows, width, dtype, "residual_norm", "h") \
-            + self._matrix(y, rows, width, x.dtype, "residual_norm", "y") + self._matrix(n, rows, width, dtype, "residual_norm", "n")
-        cur = self._enter(x, h, y, n, pre, pre_bias, post, post_bias, gate)
-        rc = self.lib.lp_residual_norm(self.h, C.addressof(d), *a)
+            n = self._empty_like(x if h is None else h, dtype=dtype)
+        a, lda = self._matrix(x, shape, x.dtype, "residual_norm", "x")
+        b, ldb = self._matrix(h, shape, dtype, "residual_norm", "h")
+        c, ldc = self._matrix(y, shape, x.dtype, "residual_norm", "y")
+        d, ldd = self._matrix(n, shape, dtype, "residual_norm", "n")
+        cur = None
+        if self._torch._C._cuda_getCurrentRawStream(self.device) != self._raw_stream:
+            cur = self._enter(x, h, y, n, pre, pre_bias, post, post_bias, gate)
+        rc = self.lib.lp_residual_norm(self.h, desc, a, lda, b, ldb, c, ldc, d, ldd)
         if rc:
             self._ck(rc)
         if cur is not None:
@@ -549,33 +571,38 @@ class Context:
         if like is None:
             self._refuse(f"{who}: neither y nor dy")
         dtype = h.dtype if h is not None else dn.dtype if dn is not None else like.dtype
-        rows, width, d = self._residual(who, like, dtype, pre_norm, pre, pre_bias, post_norm, post, post_bias, gate, scale, p, seed, step, row_base, eps)
-        new = self._torch.float32
-        out = {"dx": dx if dx is not None else like.new_empty((rows, width))}
+        shape, desc = self._residual(who, like, dtype, pre_norm, pre, pre_bias, post_norm, post, post_bias, gate, scale, p, seed, step, row_base, eps)
+        width = shape[1]
+        out = {"dx": dx if dx is not None else self._empty_like(like)}
         if h is not None:
-            out["dh"] = dh if dh is not None else like.new_empty((rows, width), dtype=dtype)
-        wanted = {"dpre": (pre, dpre), "dpre_bias": (pre_bias, dpre_bias), "dpost": (post, dpost), "dpost_bias": (post_bias, dpost_bias)}
+            out["dh"] = dh if dh is not None else self._empty_like(like, dtype=dtype)
+        elif dh is not None:
+            self._refuse(f"{who}: a gradient of h is wanted and there is no h")
+        gate_column = False
         if gate is not None and h is not None:
-            if gate.dim() == 1:
-                wanted["dgate"] = (gate, dgate)
-            else:
-                out["dgate"] = dgate if dgate is not None else like.new_empty((rows, width), dtype=dtype)
-        for name, (param, given) in wanted.items():
-            if given is not None:
-                out[name] = given
-            elif param is not None:
+            gate_column = gate.dim() == 1
+            if not gate_column:
+                out["dgate"] = dgate if dgate is not None else self._empty_like(like, dtype=dtype)
+        elif dgate is not None:
+            self._refuse(f"{who}: a gradient of the gate is wanted and there is no gate")
+        columns = [0, 0, 0, 0, 0]
+        for i, (name, param, given) in enumerate((("dpre", pre, dpre), ("dpre_bias", pre_bias, dpre_bias), ("dpost", post, dpost), ("dpost_bias", post_bias, dpost_bias),
+                                                  ("dgate", gate if gate_column else None, dgate if gate_column else None))):
+            if given is None:
+                if param is None:
+                    continue
                 if accumulate:
                     self._refuse(f"{who}: accumulate needs a {name} to add to")
-                out[name] = like.new_empty(width, dtype=new)
-        a = self._matrix(dy, rows, width, like.dtype, who, "dy") + self._matrix(dn, rows, width, dtype, who, "dn") + self._matrix(y, rows, width, like.dtype, who, "y") \
-            + self._matrix(h, rows, width, dtype, who, "h") + self._matrix(out["dx"], rows, width, like.dtype, who, "dx") + self._matrix(out.get("dh"), rows, width, dtype, who, "dh")
-        if "dgate" in wanted:
-            a += (self._column(out["dgate"], width, who, "dgate"), width)
-        else:
-            a += self._matrix(out.get("dgate"), rows, width, dtype, who, "dgate")
-        a += tuple(self._column(out.get(name), width, who, name) for name in ("dpre", "dpre_bias", "dpost", "dpost_bias"))
-        cur = self._enter(dy, dn, y, h, pre, pre_bias, post, post_bias, gate, *out.values())
-        rc = self.lib.lp_residual_norm_grad(self.h, C.addressof(d), *a, accumulate)
+                given = like.new_empty(width, dtype=self._f32)
+            out[name] = given
+            columns[i] = self._column(given, width, who, name)
+        a = (*self._matrix(dy, shape, like.dtype, who, "dy"), *self._matrix(dn, shape, dtype, who, "dn"), *self._matrix(y, shape, like.dtype, who, "y"),
+             *self._matrix(h, shape, dtype, who, "h"), *self._matrix(out["dx"], shape, like.dtype, who, "dx"), *self._matrix(out.get("dh"), shape, dtype, who, "dh"))
+        a += (columns[4], width) if gate_column else self._matrix(out.get("dgate"), shape, dtype, who, "dgate")
+        cur = None
+        if self._torch._C._cuda_getCurrentRawStream(self.device) != self._raw_stream:
+            cur = self._enter(dy, dn, y, h, pre, pre_bias, post, post_bias, gate, *out.values())
+        rc = self.lib.lp_residual_norm_grad(self.h, desc, *a, *columns[:4], accumulate)
         if rc:
             self._ck(rc)
         if cur is not None:
@@ -598,6 +625,8 @@ class Context:
         if B.dim() != 3 or B.get_device() != self.device or B.dtype != A.dtype or not B.is_contiguous() or B.shape[0] != groups or B.shape[2 if trans_b else 1] != K:
             self._refuse(f"{who}: B must be {f'[{groups}, N, {K}]' if trans_b else f'[{groups}, {K}, N]'}, contiguous, of the type of A and on its device")
         N = B.shape[1 if trans_b else 2]
+        if K >= 1 << 31 or N >= 1 << 31:
+            self._refuse(f"{who}: widths must be in [1, 2^20]")
         if bias is not None and (bias.dtype is not self._torch.float32 or bias.get_device() != self.device or bias.shape != (groups, N) or not bias.is_contiguous()):
             self._refuse(f"{who}: bias must be a contiguous float32 matrix [{groups}, {N}] on cuda:{self.device}")
         prec = self._prec(A.dtype, who)
@@ -607,7 +636,9 @@ class Context:
             r, d, ldc = self._rows(out, who)
             if r != M or d != N or out.dtype != A.dtype:
                 self._refuse(f"{who}: out must be [{M}, {N}] of the type of A")
-        cur = self._enter(A, offsets, B, bias, out)
+        cur = None
+        if self._torch._C._cuda_getCurrentRawStream(self.device) != self._raw_stream:
+            cur = self._enter(A, offsets, B, bias, out)
         rc = self.lib.lp_grouped_linear(self.h, prec, M, N, K, groups, offsets.data_ptr(), A.data_ptr(), lda, B.data_ptr(), trans_b,
                                         None if bias is None else bias.data_ptr(), relu, out.data_ptr(), ldc)
         if rc:
@@ -623,7 +654,7 @@ class Context:
         M, K, lda = self._rows(A, who)
         m, N, ldz = self._rows(dZ, who)
         groups = self._offsets(offsets, who)
-        if m != M or dZ.dtype != A.dtype:
+        if m != M or dZ.dtype != A.dtype or K >= 1 << 31 or N >= 1 << 31:
             self._refuse(f"{who}: dZ must have {M} rows of the type of A")
         f32 = self._torch.float32
         bias = bias or dbias is not None
@@ -637,7 +668,9 @@ class Context:
             dW = A.new_empty((groups, K, N), dtype=f32)
         if bias and dbias is None:
             dbias = A.new_empty((groups, N), dtype=f32)
-        cur = self._enter(A, dZ, offsets, dW, dbias)
+        cur = None
+        if self._torch._C._cuda_getCurrentRawStream(self.device) != self._raw_stream:
+            cur = self._enter(A, dZ, offsets, dW, dbias)
         rc = self.lib.lp_grouped_weight_grad(self.h, prec, M, N, K, groups, offsets.data_ptr(), A.data_ptr(), lda, dZ.data_ptr(), ldz, accumulate, dW.data_ptr(),
                                              None if dbias is None else dbias.data_ptr())
         if rc:

@@ -828,10 +828,14 @@ template <typename... A, typename... P> static void launch_large(void (*kernel)(
     launch_dep(kernel, grid, block, smem, st, args...);
 }
 
+// Which variant: the biases' registers are spared where rows are on 16 bytes and of at most 2,048 columns; the others (half as many
+// variants to build) are bound by other things.
+static bool residual_bias(bool wanted, bool vec, int width) { return wanted || !vec || width > 8 * 256; }
+
 template <typename TS, typename TD, bool VEC, bool BIAS> static void residual_dispatch(Exec &ex, const ResidualParams &p, const ResidualGrid &g, size_t smem)
 {
     const dim3 grid(g.blocks), block(g.threads);
-    if (g.threads > 256) launch_large(residual_norm_kernel<TS, TD, VEC, 1024, BIAS>, grid, block, smem, ex.st, p);
+    if (g.threads > 256) launch_large(residual_norm_kernel<TS, TD, VEC, 1024, true>, grid, block, smem, ex.st, p);
     else if (g.block) launch_large(residual_norm_kernel<TS, TD, VEC, 256, BIAS>, grid, block, smem, ex.st, p);
     else launch_large(residual_norm_kernel<TS, TD, VEC, 32, BIAS>, grid, block, smem, ex.st, p);
 }
@@ -839,38 +843,30 @@ template <typename TS, typename TD> static void residual_launch(Exec &ex, Residu
 {
     const ResidualGrid g = residual_grid(p.rows, p.width, 256, 768);
     p.team = g.team;
-    const bool bias = p.pre_bias || p.post_bias, vec = residual_vec(p, sizeof(TS), sizeof(TD));
+    const bool vec = residual_vec(p, sizeof(TS), sizeof(TD)), bias = residual_bias(p.pre_bias || p.post_bias, vec, p.width);
     const size_t smem = residual_pipe(p, g, vec, true, sizeof(TS), sizeof(TD), 256);
-    if (vec) {
-        if (bias) residual_dispatch<TS, TD, true, true>(ex, p, g, smem);
-        else residual_dispatch<TS, TD, true, false>(ex, p, g, smem);
-    } else {
-        if (bias) residual_dispatch<TS, TD, false, true>(ex, p, g, smem);
-        else residual_dispatch<TS, TD, false, false>(ex, p, g, smem);
-    }
+    if (!vec) residual_dispatch<TS, TD, false, true>(ex, p, g, smem);
+    else if (bias) residual_dispatch<TS, TD, true, true>(ex, p, g, smem);
+    else residual_dispatch<TS, TD, true, false>(ex, p, g, smem);
     ex.launches += 1;
 }
 
 template <typename TS, typename TD, bool VEC, bool BIAS> static void residual_grad_dispatch(Exec &ex, const ResidualParams &p, const ResidualGrid &g, size_t smem)
 {
     const dim3 grid(g.blocks), block(g.threads);
-    if (g.threads > 256) launch_large(residual_norm_grad_kernel<TS, TD, VEC, 1024, BIAS>, grid, block, smem, ex.st, p);
+    if (g.threads > 256) launch_large(residual_norm_grad_kernel<TS, TD, VEC, 1024, true>, grid, block, smem, ex.st, p);
     else if (g.threads > 128 && g.block) launch_large(residual_norm_grad_kernel<TS, TD, VEC, 256, BIAS>, grid, block, smem, ex.st, p);
     else if (g.block) launch_large(residual_norm_grad_kernel<TS, TD, VEC, 128, BIAS>, grid, block, smem, ex.st, p);
     else launch_large(residual_norm_grad_kernel<TS, TD, VEC, 32, BIAS>, grid, block, smem, ex.st, p);
 }
-template <typename TS, typename TD> static void residual_grad_launch(Exec &ex, ResidualParams &p, const ResidualGrid &g, const ResidualSums &o, bool bias, int accumulate)
+// vec, bias: residual_vec, residual_bias of this call
+template <typename TS, typename TD> static void residual_grad_launch(Exec &ex, ResidualParams &p, const ResidualGrid &g, const ResidualSums &o, bool vec, bool bias, int accumulate)
 {
     p.team = g.team;
-    const bool vec = residual_vec(p, sizeof(TS), sizeof(TD));
     const size_t smem = residual_pipe(p, g, vec, false, sizeof(TS), sizeof(TD), 190 * 1024 / (bias ? RN_GRAD_RESIDENT<true> : RN_GRAD_RESIDENT<false>));
-    if (vec) {
-        if (bias) residual_grad_dispatch<TS, TD, true, true>(ex, p, g, smem);
-        else residual_grad_dispatch<TS, TD, true, false>(ex, p, g, smem);
-    } else {
-        if (bias) residual_grad_dispatch<TS, TD, false, true>(ex, p, g, smem);
-        else residual_grad_dispatch<TS, TD, false, false>(ex, p, g, smem);
-    }
+    if (!vec) residual_grad_dispatch<TS, TD, false, true>(ex, p, g, smem);
+    else if (bias) residual_grad_dispatch<TS, TD, true, true>(ex, p, g, smem);
+    else residual_grad_dispatch<TS, TD, true, false>(ex, p, g, smem);
     ex.launches += 1;
     int last = -1;
     for (int k = 0; k < RN_SUMS; ++k)

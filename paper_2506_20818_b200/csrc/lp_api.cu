@@ -2622,18 +2622,19 @@ extern "C" lp_status lp_residual_norm_grad(lp_ctx *ctx, const lp_residual_desc *
     }
     if (k.pre_norm ? !dn || !y : dn != nullptr) return fail(ctx, LP_EINVAL, who + ": dn and y are needed with a norm before the next block, and dn only then");
     if (!dy && !dn) return fail(ctx, LP_EINVAL, who + ": neither dy nor dn");
-    const bool bias = o.out[3] || o.out[4] || k.post_bias;
+    const uint32_t bs = ps == LP_FP32 ? 4 : 2, bd = pd == LP_FP32 ? 4 : 2;
+    k.dy = dy; k.ld_dy = (uint32_t)ld_dy * bs; k.dn = dn; k.ld_dn = (uint32_t)ld_dn * bd; k.y = (void *)y; k.ld_y = (uint32_t)ld_y * bs; k.h = h; k.ld_h = (uint32_t)ld_h * bd;
+    k.dx = dx; k.ld_dx = (uint32_t)ld_dx * bs; k.dh = dh; k.ld_dh = (uint32_t)ld_dh * bd;
+    if (!gate_sum) { k.dgate = dgate; k.ld_dgate = (uint32_t)ld_dgate * bd; }
+    const bool vec = residual_vec(k, (int)bs, (int)bd), bias = residual_bias(o.out[3] || o.out[4] || k.post_bias, vec, desc->width);
     const ResidualGrid g = residual_grad_grid(desc->rows, desc->width, bias);
     uint8_t *ws = nullptr;
     s = op_workspace(ctx, sizeof(float) * (size_t)g.blocks * RN_SUMS * desc->width, &ws);
     if (s != LP_OK) return s;
-    const uint32_t bs = ps == LP_FP32 ? 4 : 2, bd = pd == LP_FP32 ? 4 : 2;
-    k.dy = dy; k.ld_dy = (uint32_t)ld_dy * bs; k.dn = dn; k.ld_dn = (uint32_t)ld_dn * bd; k.y = (void *)y; k.ld_y = (uint32_t)ld_y * bs; k.h = h; k.ld_h = (uint32_t)ld_h * bd;
-    k.dx = dx; k.ld_dx = (uint32_t)ld_dx * bs; k.dh = dh; k.ld_dh = (uint32_t)ld_dh * bd; k.partial = (float *)ws;
-    if (!gate_sum) { k.dgate = dgate; k.ld_dgate = (uint32_t)ld_dgate * bd; }
-    if (ps == LP_BF16) residual_grad_launch<bf16, bf16>(ctx->ex, k, g, o, bias, accumulate);
-    else if (pd == LP_BF16) residual_grad_launch<float, bf16>(ctx->ex, k, g, o, bias, accumulate);
-    else residual_grad_launch<float, float>(ctx->ex, k, g, o, bias, accumulate);
+    k.partial = (float *)ws;
+    if (ps == LP_BF16) residual_grad_launch<bf16, bf16>(ctx->ex, k, g, o, vec, bias, accumulate);
+    else if (pd == LP_BF16) residual_grad_launch<float, bf16>(ctx->ex, k, g, o, vec, bias, accumulate);
+    else residual_grad_launch<float, float>(ctx->ex, k, g, o, vec, bias, accumulate);
     CK_LAUNCH();
     return LP_OK;
 }

@@ -48,3 +48,12 @@ def test_descriptor_follows_the_header(pkg):
                 kind = C.c_void_p if ptr else {"int64_t": C.c_int64, "int32_t": C.c_int32, "uint64_t": C.c_uint64, "double": C.c_double}[m.group(1)]
                 want.append((name.strip().lstrip("*"), kind))
     assert [tuple(f) for f in pkg.ResidualDesc._fields_] == want
+
+
+def test_packed_descriptor_is_the_structure(pkg):
+    from paper_2506_20818_b200 import binding
+    values = (5, 6, 1, 0, 2, 1, 1e-5, 0.5, 0.25, 2**64 - 1, 3, 9, 11, 12, 13, 14, 15, 16)
+    packed = binding._RESIDUAL.pack(*values)
+    assert len(packed) == C.sizeof(pkg.ResidualDesc)
+    d = pkg.ResidualDesc.from_buffer_copy(packed)
+    assert tuple(getattr(d, name) for name, _ in pkg.ResidualDesc._fields_) == values
