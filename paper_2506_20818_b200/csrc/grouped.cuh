@@ -243,7 +243,9 @@ struct Piece8 {
     }
 };
 
-// A matrix copied to rows that start on 16 bytes: `width` elements in rows of `ld_out`, 16 bytes per thread out of aligned words
+// A matrix copied to rows that start on 16 bytes: `width` elements in rows of `ld_out`, 16 bytes per thread out of the one or two aligned
+// pieces of 16 bytes that hold them (word by word the loads took a third longer than HBM does).  A piece with a byte of the row lies in
+// the row's page.
 template <typename T> __global__ void __launch_bounds__(256) grouped_align_kernel(const T *in, int64_t rows, int width, int64_t ld_in, T *out, int64_t ld_out)
 {
     LP_DEP_ENTER();
@@ -251,17 +253,17 @@ template <typename T> __global__ void __launch_bounds__(256) grouped_align_kerne
     const int64_t per = ld_out / E, i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / per;
     if (row >= rows) return;
     const int col = (int)(i - row * per) * E, n = min(E, width - col);
-    const T *src = in + row * ld_in + col;
-    uint32_t w[5] = {0u, 0u, 0u, 0u, 0u};
-    const uint32_t *words = reinterpret_cast<const uint32_t *>((uintptr_t)src & ~(uintptr_t)3);
-    const int odd = ((uintptr_t)src & 3) != 0;  // BF16: the first element is the upper half of a word
-    const int count = (n * (int)sizeof(T) + 2 * odd + 3) / 4;
+    const uintptr_t src = (uintptr_t)(in + row * ld_in + col);
+    const int m = (int)(src & 15);
+    const uint4 *piece = reinterpret_cast<const uint4 *>(src & ~(uintptr_t)15);
+    const uint4 a = __ldg(piece), b = m + n * (int)sizeof(T) > 16 ? __ldg(piece + 1) : make_uint4(0u, 0u, 0u, 0u);
+    uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
-    for (int k = 0; k < 5; ++k)
-        if (k < count) w[k] = __ldg(words + k);
-    if (odd)
+    for (int k = 0; k < 6; ++k) w[k] = m & 8 ? w[k + 2] : w[k];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) w[k] = __funnelshift_r(w[k], w[k + 1], 16);
+    for (int k = 0; k < 5; ++k) w[k] = m & 4 ? w[k + 1] : w[k];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = __funnelshift_r(w[k], w[k + 1], 8 * (m & 3));
     *reinterpret_cast<uint4 *>(out + row * ld_out + col) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
