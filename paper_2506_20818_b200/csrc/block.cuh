@@ -17,9 +17,17 @@
 //
 // A team of T threads (a power of two, eight columns each) holds a row in registers, so every array is read once and written
 // once: bound by HBM.  Teams of up to 32 threads are parts of warps, larger ones whole blocks.
+//
+// Measured on the device (the copy rate is 6.55 TB/s):
+//   dropout, 1,000,000 x 256 BF16                                    179 us, 5.7 TB/s: 64 of 112 instructions per eight elements are the
+//                                                                    generator's, whose multiplications keep their pipe busy
+//   residual norm, 196,608 x 256, FP32 sums, BF16 blocks, both norms, dropout, gate per column    104 us, 5.8 TB/s
+//   its gradient                                                     177 us, 5.1 TB/s, and 5 us for the column sums of the blocks: 580
+//                                                                    instructions per row of a warp at 16 warps per SM (128 registers)
+//   gradient, 50,001 x 417 FP32, layer norms, gate per element       186 us, 3.6 TB/s, and 8 us: 53 of a team's 64 threads have columns,
+//                                                                    single elements loaded from shared memory and stored, four barriers a row
 #pragma once
-#include "common.cuh"
-#include "sampler.cuh"
+#include "gemm_tc.cuh"
 
 enum : uint32_t { DRAW_DROPOUT = 5 };
 
@@ -439,12 +447,12 @@ template <bool VEC, bool BLOCK> struct RowPipe {
 template <typename T> LP_DEVINL T *row_at(void *array, uint32_t row, uint32_t ld) { return (T *)((char *)array + (uint64_t)row * ld); }
 
 // 1 / sqrt(x) of a positive x: the hardware's estimate and one Newton step, off by about 1.5 2^-24 (the correctly rounded square root and
-// division took 35 instructions)
+// division took 35 instructions); 0 for a sum that is infinite
 LP_DEVINL float inv_sqrt(float x)
 {
     float r;
     asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return fmaf(r * fmaf(-x * r, r, 1.f), 0.5f, r);
+    return r == 0.f ? 0.f : fmaf(r * fmaf(-x * r, r, 1.f), 0.5f, r);
 }
 
 // Sums of K values over a team, in every one of its threads.  A fixed tree, so the same bits in every run.

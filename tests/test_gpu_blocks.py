@@ -326,6 +326,18 @@ def test_residual_norm_rows_without_content(ctx):
     assert (keep == 3.0).all()
 
 
+@pytest.mark.parametrize("width", [64, 417])
+def test_residual_norm_of_rows_too_large_to_square(ctx, width):
+    """A row whose squares pass the end of FP32 comes out as zeros, as it does when x is divided by an infinite norm."""
+    x = torch.randn(5, width, generator=gen(12)).to(DEV)
+    x[2] = 1e25
+    x[3, 7] = float("inf")
+    _, n = ctx.residual_norm(x)
+    want = x.float() / torch.sqrt(x.square().mean(1, keepdim=True) + 1e-6)
+    assert (n[2] == 0).all() and (n[3].isnan() == want[3].isnan()).all() and (n[3].nan_to_num(0.0) == 0).all()
+    assert (n[[0, 1, 4]] - want[[0, 1, 4]]).abs().max() <= 64 * U * 8
+
+
 def test_residual_norm_grad_against_differences(ctx):
     """Directional differences of the forward call in FP32: sum(dy y) + sum(dn n) along a random direction of every input."""
     g = gen(11)
