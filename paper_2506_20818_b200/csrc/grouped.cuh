@@ -33,8 +33,9 @@
 //                                                          stores either 141, with one of the six products 200: the ways through shared memory
 //                                                          (320 KB a block by count) and two stages share the time
 //   weight gradient, FP32, 30,011 rows, 417 x 1,000, 40 groups    405 us, and 30 us before and after it
-// Tried for FP32 and slower: blocks of 32 terms with four stages (249 and 558 us where 64 terms with two took 218 and 433), the next
-// tile's rows asked into L2 while the present one is multiplied (237 and 469 us).
+// Tried for FP32 and not faster (product, weight gradient; 64 terms with two stages and all loaders on one block: 210 to 218, 425 to 433 us):
+// blocks of 32 terms with four stages 249, 558, and with four groups of loaders that take blocks in turn 235, 495; two such groups with
+// blocks of 64 terms 222, 413 (and 17 instead of 15 us for 768 rows); the next tile's rows asked into L2 one tile earlier 237, 469.
 #pragma once
 #include "gemm_tc.cuh"
 #include "orthogonal.cuh"
