@@ -346,14 +346,17 @@ template <typename T, int RB> LP_DEVINL void put_staged(T *dst, int64_t ld, int 
             o.store(d);
         }
     } else {
-        const int count = min(rows, 32) * PUT_COLS<T, RB>;
-#pragma unroll 4
-        for (int i = lane; i < count; i += 32) {
-            const int r = i / PUT_COLS<T, RB>, c = i % PUT_COLS<T, RB>;
-            if (c < cols) {
-                const float x = to_f<T>(*reinterpret_cast<const T *>(stage + stage_place<RB>(r, c / VN) + c % VN * (int)sizeof(T)));
-                T *d = dst + (int64_t)r * ld + c;
-                *d = from_f<T>(accumulate ? to_f<T>(*d) + x : x);
+        // a lane stays in its column
+        constexpr int W = PUT_COLS<T, RB> < 32 ? PUT_COLS<T, RB> : 32, STEP = 32 / W;
+#pragma unroll
+        for (int first = 0; first < PUT_COLS<T, RB>; first += W) {
+            const int c = first + lane % W, n = c < cols ? min(rows, 32) : 0;
+            const uint8_t *src = stage + c % VN * (int)sizeof(T);
+            T *d = dst + (int64_t)(lane / W) * ld + c;
+#pragma unroll 8
+            for (int r = lane / W; r < n; r += STEP, d += STEP * ld) {
+                const T x = *reinterpret_cast<const T *>(src + stage_place<RB>(r, c / VN));
+                *d = accumulate ? from_f<T>(to_f<T>(*d) + to_f<T>(x)) : x;
             }
         }
     }
