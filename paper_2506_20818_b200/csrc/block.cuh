@@ -311,6 +311,7 @@ struct ResidualParams {
     PipeArray pipe[5];         // forward: x, h, gate; backward: dn, y, dy, h, gate
     int *err;
     unsigned long long wait_ns;
+    uint32_t extra_tx;         // diagnostics: the first row's wait expires
 };
 
 
@@ -349,16 +350,16 @@ template <bool VEC, bool BLOCK> struct RowPipe {
         if (BLOCK) __syncthreads();
         else __syncwarp();
     }
-    // the next row of every team of the unit; `row` is this thread's
-    template <int N> LP_DEVINL void fetch(const PipeArray (&arrays)[N], int64_t row, int t, int team)
+    // the next row of every team of the unit; `row` is this thread's.  extra: bytes that are announced and never come (diagnostics)
+    template <int N> LP_DEVINL void fetch(const PipeArray (&arrays)[N], int64_t row, int t, int team, uint32_t extra = 0)
     {
         const bool sends = t == 0 && row < p.rows;
         if (VEC) {
             // the unit's first thread says how much is on its way
-            if (t == 0 && team == 0) mbar_expect_tx(bar_in, p.copy_bytes * (uint32_t)min(max((int64_t)p.rows - row, (int64_t)0), (int64_t)p.unit_teams));
+            if (t == 0 && team == 0) mbar_expect_tx(bar_in, p.copy_bytes * (uint32_t)min(max((int64_t)p.rows - row, (int64_t)0), (int64_t)p.unit_teams) + extra);
         } else {
             if (sends) {
-                uint32_t bytes = 0;
+                uint32_t bytes = extra;
 #pragma unroll
                 for (int k = 0; k < N; ++k)
                     if (arrays[k].at) {
@@ -538,7 +539,7 @@ template <typename TS, typename TD, bool VEC, int MAXT, bool BIAS> __global__ vo
     RowPipe<VEC, BLOCK> pipe(p, pipe_smem);
     const PipeArray arrays[3] = {p.pipe[0], p.pipe[1], p.pipe[2]};
     const int team = BLOCK ? 0 : lane / T;
-    for (int i = 0; i < p.stages; ++i) pipe.fetch(arrays, row + (int64_t)i * stride, t, team);
+    for (int i = 0; i < p.stages; ++i) pipe.fetch(arrays, row + (int64_t)i * stride, t, team, i == 0 && blockIdx.x == 0 ? p.extra_tx : 0u);
     for (int i = 0; i < rounds; ++i, row += stride) {
         const bool live = row < p.rows;  // of a warp's teams some may be past the last row; they take part in the sums of the others
         const uint32_t r = live ? (uint32_t)row : 0u;
@@ -644,7 +645,7 @@ __global__ void __launch_bounds__(RN_GRAD_THREADS<MAXT, BIAS>, MAXT > 256 ? 1 : 
     RowPipe<VEC, BLOCK> pipe(p, pipe_smem);
     const PipeArray arrays[5] = {p.pipe[0], p.pipe[1], p.pipe[2], p.pipe[3], p.pipe[4]};
     const int team = BLOCK ? 0 : lane / T;
-    for (int i = 0; i < p.stages; ++i) pipe.fetch(arrays, row + (int64_t)i * stride, t, team);
+    for (int i = 0; i < p.stages; ++i) pipe.fetch(arrays, row + (int64_t)i * stride, t, team, i == 0 && blockIdx.x == 0 ? p.extra_tx : 0u);
     for (int i = 0; i < rounds; ++i, row += stride) {
         const bool live = row < p.rows;
         const uint32_t r = live ? (uint32_t)row : 0u;

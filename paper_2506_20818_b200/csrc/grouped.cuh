@@ -28,11 +28,11 @@
 //                                                          products), after 87 us that copy both operands to aligned rows at 6.4 TB/s
 //   weight gradient, BF16, 196,608 rows, 256 x 256, 8 groups   63 us and 12 us for shared tiles: 1,200 cycles per block of 64 rows where HBM
 //                                                          allows 1,400 at best, then 3 us to start, 7 us to write 19 MB of partial tiles
-//   linear, FP32, 100,003 rows, 256 -> 512, 16 groups      221 us: 711 TFLOP/s of BF16 products, tensor pipe 34 % busy.  A block of 64 terms
+//   linear, FP32, 100,003 rows, 256 -> 512, 16 groups      212 us: 742 TFLOP/s of BF16 products, tensor pipe 35 % busy.  A block of 64 terms
 //                                                          takes 2,500 cycles, 1,536 of them products.  Without the loads of A 157 us, without its
 //                                                          stores either 141, with one of the six products 200: the ways through shared memory
 //                                                          (320 KB a block by count) and two stages share the time
-//   weight gradient, FP32, 30,011 rows, 417 x 1,000, 40 groups    405 us, and 30 us before and after it
+//   weight gradient, FP32, 30,011 rows, 417 x 1,000, 40 groups    360 us, and 30 us before and after it
 // Tried for FP32 and not faster (product, weight gradient; 64 terms with two stages and all loaders on one block: 210 to 218, 425 to 433 us):
 // blocks of 32 terms with four stages 249, 558, and with four groups of loaders that take blocks in turn 235, 495; two such groups with
 // blocks of 64 terms 222, 413 (and 17 instead of 15 us for 768 rows); the next tile's rows asked into L2 one tile earlier 237, 469.

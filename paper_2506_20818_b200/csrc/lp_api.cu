@@ -2583,6 +2583,8 @@ extern "C" lp_status lp_residual_norm(lp_ctx *ctx, const lp_residual_desc *desc,
     if (!y && !n) return fail(ctx, LP_EINVAL, "lp_residual_norm: no result is wanted");
     CK(cudaSetDevice(ctx->device));
     const uint32_t bs = ps == LP_FP32 ? 4 : 2, bd = pd == LP_FP32 ? 4 : 2;
+    k.extra_tx = (uint32_t)ctx->tc.overdeclare_tx;
+    ctx->tc.overdeclare_tx = 0;
     k.x = x; k.ld_x = (uint32_t)ld_x * bs; k.h = h; k.ld_h = (uint32_t)ld_h * bd; k.y = h ? y : nullptr; k.ld_y = (uint32_t)ld_y * bs; k.n = n; k.ld_n = (uint32_t)ld_n * bd;
     if (ps == LP_BF16) residual_launch<bf16, bf16>(ctx->ex, k);
     else if (pd == LP_BF16) residual_launch<float, bf16>(ctx->ex, k);
@@ -2632,6 +2634,8 @@ extern "C" lp_status lp_residual_norm_grad(lp_ctx *ctx, const lp_residual_desc *
     s = op_workspace(ctx, sizeof(float) * (size_t)g.blocks * RN_SUMS * desc->width, &ws);
     if (s != LP_OK) return s;
     k.partial = (float *)ws;
+    k.extra_tx = (uint32_t)ctx->tc.overdeclare_tx;
+    ctx->tc.overdeclare_tx = 0;
     if (ps == LP_BF16) residual_grad_launch<bf16, bf16>(ctx->ex, k, g, o, vec, bias, accumulate);
     else if (pd == LP_BF16) residual_grad_launch<float, bf16>(ctx->ex, k, g, o, vec, bias, accumulate);
     else residual_grad_launch<float, float>(ctx->ex, k, g, o, vec, bias, accumulate);

@@ -391,6 +391,29 @@ def test_residual_norm_repeats_and_replays(pkg):
     c.close()
 
 
+@pytest.mark.parametrize("width", [64, 100, 417, 1000])
+def test_residual_norm_wait_that_runs_out(pkg, width):
+    """The first row's wait expires (16 bytes more are announced than come): reported once, and the context goes on."""
+    c = pkg.Context(0)
+    x = torch.randn(300, width, generator=gen(13)).to(DEV)
+    w = torch.ones(width, device=DEV)
+    y, n = c.residual_norm(x, x, pre=w)
+    got = c.residual_norm_grad(x, x, y, x, pre=w)
+    c.stats()
+    for call in (lambda: c.residual_norm(x, x, pre=w), lambda: c.residual_norm_grad(x, x, y, x, pre=w)):
+        c.set_wait_limit(2_000_000, 16)
+        call()
+        with pytest.raises(pkg.LpError) as e:
+            c.stats()
+        assert e.value.status == -6
+        c.set_wait_limit(2_000_000_000, 0)
+        c.stats()
+        assert torch.equal(c.residual_norm(x, x, pre=w)[1], n)
+        again = c.residual_norm_grad(x, x, y, x, pre=w)
+        assert all(torch.equal(again[k], got[k]) for k in got)
+    c.close()
+
+
 def test_block_refusals(pkg, ctx):
     x = torch.zeros(4, 16, device=DEV)
     w = torch.ones(16, device=DEV)
