@@ -809,8 +809,14 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
 #pragma unroll
                 for (int c = 0; c < COLS; c += PC) {
                     if (c0 + c < p.N) {
-                        uint8_t *half = stage + (c / PC & 1) * 2048;  // the store before may still read the other half
-                        if (p.tma_c) stage_free<1>();
+                        // Two halves in turn.  Before a half is written, the TMA stores that read it are done: at the first piece none of the tile before
+                        // is left (whose last store may have read either half, or come before rows that left without TMA), and within a tile either every
+                        // piece is a store, so that the one that may still be reading has the other half, or (fewer than 32 rows) none is.
+                        uint8_t *half = stage + (c / PC & 1) * 2048;
+                        if (p.tma_c) {
+                            if (c == 0) stage_free<0>();
+                            else stage_free<1>();
+                        }
                         stage_columns<T, 64, PC>(0, v + c, half);
                         put_rows<T, 64>(p.tma_c ? &mapC : nullptr, c0 + c, row, dst + c, p.ldc, j.row_end - row, p.N - (c0 + c), p.vec_c, half);
                     }

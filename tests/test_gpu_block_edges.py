@@ -1,0 +1,54 @@
+"""Edges of the residual-block operators and the products by group: what a call may meet beside the cases of their own tests.
+
+Tolerances of the products are derived in the docstring of test_gpu_grouped, those of the norms in test_gpu_blocks.
+"""
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F32, BF16, I32 = torch.float32, torch.bfloat16, torch.int32
+
+
+@pytest.fixture(scope="module")
+def pkg():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    import __graft_entry__ as ge
+    ge.build()
+    import paper_2506_20818_b200 as p
+    return p
+
+
+@pytest.fixture(scope="module")
+def ctx(pkg):
+    c = pkg.Context(0)
+    yield c
+    c.close()
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+@pytest.mark.parametrize("n", [16, 48, 100, 112, 1000])
+def test_fp32_results_of_whole_and_short_tiles(ctx, n):
+    """Results leave by TMA where a warp has all 32 rows and row by row where it does not, sixteen columns at a time out of two areas
+    in turn: odd numbers of such pieces, and short tiles after whole ones.  One block of terms, so that tiles follow one another fast."""
+    g = gen(n)
+    sizes = [256, 130, 1, 128, 300, 127, 64, 128, 31, 200, 33] * 300
+    rows, groups, k = sum(sizes), len(sizes), 64
+    offsets = torch.tensor([0] + sizes).cumsum(0)
+    a = torch.randn(rows, k, generator=g).to(DEV)
+    b = torch.randn(3, k, n, generator=g).to(DEV)[torch.arange(groups, device=DEV) % 3]
+    group = torch.repeat_interleave(torch.arange(groups), torch.tensor(sizes)).to(DEV) % 3
+    want, mag = torch.empty(rows, n, dtype=torch.float64, device=DEV), torch.empty(rows, n, dtype=torch.float64, device=DEV)
+    for i in range(3):
+        pick = group == i
+        want[pick], mag[pick] = a[pick].double() @ b[i].double(), a[pick].double().abs() @ b[i].double().abs()
+    off = offsets.to(I32).to(DEV)
+    first = ctx.grouped_linear(a, off, b)
+    per = 2.0 ** -21 + 5 * 2.0 ** -22 + (k / 64 + 3) * 2.0 ** -24
+    assert ((first.double() - want).abs() <= per * mag + 2.0 ** -24 * want.abs()).all()
+    for _ in range(20):
+        assert torch.equal(ctx.grouped_linear(a, off, b, out=torch.zeros_like(first)), first)
