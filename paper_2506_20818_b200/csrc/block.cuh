@@ -802,6 +802,9 @@ static bool residual_vec(const ResidualParams &p, int size_s, int size_d)
            ok(p.gate, p.ld_gate) && ok(p.dgate, p.ld_dgate);
 }
 
+// Rows under way (one row of all arrays is at most 160 KiB and 80 bytes) and their barriers, up to eight of eight units
+constexpr int RN_MAX_ROWS_SMEM = 208 * 1024, RN_MAX_SMEM = RN_MAX_ROWS_SMEM + 8 * 8 * 8;
+
 // Places of the arrays in the ring of rows and how many rows it holds: `room` bytes of shared memory per thread keep as many blocks
 // resident as registers do.  Returns the bytes of shared memory of a block.
 static size_t residual_pipe(ResidualParams &p, const ResidualGrid &g, bool vec, bool forward, int size_s, int size_d, int room)
@@ -828,25 +831,24 @@ static size_t residual_pipe(ResidualParams &p, const ResidualGrid &g, bool vec, 
     p.stage_bytes = std::max(at, 16u);
     const int64_t all = (int64_t)p.stage_bytes * units;
     p.stages = (int)std::max<int64_t>(2, std::min<int64_t>(8, (int64_t)room * g.threads / all));
-    while (p.stages > 1 && p.stages * all > 208 * 1024) --p.stages;  // blocks of 1024 threads: down to one, nothing under way
+    while (p.stages > 1 && p.stages * all > RN_MAX_ROWS_SMEM) --p.stages;  // blocks of 1024 threads: down to one, nothing under way
     return (size_t)(p.stages * (all + 8 * units));
-}
-template <typename... A, typename... P> static void launch_large(void (*kernel)(A...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, P &&...args)
-{
-    if (smem > 40 * 1024) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    launch_dep(kernel, grid, block, smem, st, args...);
 }
 
 // Which variant: the biases' registers are spared where rows are on 16 bytes and of at most 2,048 columns; the others (half as many
 // variants to build) are bound by other things.
 static bool residual_bias(bool wanted, bool vec, int width) { return wanted || !vec || width > 8 * 256; }
 
-template <typename TS, typename TD, bool VEC, bool BIAS> static void residual_dispatch(Exec &ex, const ResidualParams &p, const ResidualGrid &g, size_t smem)
+typedef void (*ResidualKernel)(ResidualParams);
+template <typename TS, typename TD, bool VEC, bool BIAS> static ResidualKernel residual_kernel(int threads, bool block)
 {
-    const dim3 grid(g.blocks), block(g.threads);
-    if (g.threads > 256) launch_large(residual_norm_kernel<TS, TD, VEC, 1024, true>, grid, block, smem, ex.st, p);
-    else if (g.block) launch_large(residual_norm_kernel<TS, TD, VEC, 256, BIAS>, grid, block, smem, ex.st, p);
-    else launch_large(residual_norm_kernel<TS, TD, VEC, 32, BIAS>, grid, block, smem, ex.st, p);
+    if (threads > 256) return residual_norm_kernel<TS, TD, VEC, 1024, true>;
+    return block ? residual_norm_kernel<TS, TD, VEC, 256, BIAS> : residual_norm_kernel<TS, TD, VEC, 32, BIAS>;
+}
+template <typename TS, typename TD> static ResidualKernel residual_kernel(bool vec, bool bias, int threads, bool block)
+{
+    if (!vec) return residual_kernel<TS, TD, false, true>(threads, block);
+    return bias ? residual_kernel<TS, TD, true, true>(threads, block) : residual_kernel<TS, TD, true, false>(threads, block);
 }
 template <typename TS, typename TD> static void residual_launch(Exec &ex, ResidualParams &p)
 {
@@ -854,28 +856,27 @@ template <typename TS, typename TD> static void residual_launch(Exec &ex, Residu
     p.team = g.team;
     const bool vec = residual_vec(p, sizeof(TS), sizeof(TD)), bias = residual_bias(p.pre_bias || p.post_bias, vec, p.width);
     const size_t smem = residual_pipe(p, g, vec, true, sizeof(TS), sizeof(TD), 256);
-    if (!vec) residual_dispatch<TS, TD, false, true>(ex, p, g, smem);
-    else if (bias) residual_dispatch<TS, TD, true, true>(ex, p, g, smem);
-    else residual_dispatch<TS, TD, true, false>(ex, p, g, smem);
+    launch_dep(residual_kernel<TS, TD>(vec, bias, g.threads, g.block), dim3(g.blocks), dim3(g.threads), smem, ex.st, p);
     ex.launches += 1;
 }
 
-template <typename TS, typename TD, bool VEC, bool BIAS> static void residual_grad_dispatch(Exec &ex, const ResidualParams &p, const ResidualGrid &g, size_t smem)
+template <typename TS, typename TD, bool VEC, bool BIAS> static ResidualKernel residual_grad_kernel(int threads, bool block)
 {
-    const dim3 grid(g.blocks), block(g.threads);
-    if (g.threads > 256) launch_large(residual_norm_grad_kernel<TS, TD, VEC, 1024, true>, grid, block, smem, ex.st, p);
-    else if (g.threads > 128 && g.block) launch_large(residual_norm_grad_kernel<TS, TD, VEC, 256, BIAS>, grid, block, smem, ex.st, p);
-    else if (g.block) launch_large(residual_norm_grad_kernel<TS, TD, VEC, 128, BIAS>, grid, block, smem, ex.st, p);
-    else launch_large(residual_norm_grad_kernel<TS, TD, VEC, 32, BIAS>, grid, block, smem, ex.st, p);
+    if (threads > 256) return residual_norm_grad_kernel<TS, TD, VEC, 1024, true>;
+    if (!block) return residual_norm_grad_kernel<TS, TD, VEC, 32, BIAS>;
+    return threads > 128 ? residual_norm_grad_kernel<TS, TD, VEC, 256, BIAS> : residual_norm_grad_kernel<TS, TD, VEC, 128, BIAS>;
+}
+template <typename TS, typename TD> static ResidualKernel residual_grad_kernel(bool vec, bool bias, int threads, bool block)
+{
+    if (!vec) return residual_grad_kernel<TS, TD, false, true>(threads, block);
+    return bias ? residual_grad_kernel<TS, TD, true, true>(threads, block) : residual_grad_kernel<TS, TD, true, false>(threads, block);
 }
 // vec, bias: residual_vec, residual_bias of this call
 template <typename TS, typename TD> static void residual_grad_launch(Exec &ex, ResidualParams &p, const ResidualGrid &g, const ResidualSums &o, bool vec, bool bias, int accumulate)
 {
     p.team = g.team;
     const size_t smem = residual_pipe(p, g, vec, false, sizeof(TS), sizeof(TD), 190 * 1024 / (bias ? RN_GRAD_RESIDENT<true> : RN_GRAD_RESIDENT<false>));
-    if (!vec) residual_grad_dispatch<TS, TD, false, true>(ex, p, g, smem);
-    else if (bias) residual_grad_dispatch<TS, TD, true, true>(ex, p, g, smem);
-    else residual_grad_dispatch<TS, TD, true, false>(ex, p, g, smem);
+    launch_dep(residual_grad_kernel<TS, TD>(vec, bias, g.threads, g.block), dim3(g.blocks), dim3(g.threads), smem, ex.st, p);
     ex.launches += 1;
     int last = -1;
     for (int k = 0; k < RN_SUMS; ++k)
@@ -883,4 +884,22 @@ template <typename TS, typename TD> static void residual_grad_launch(Exec &ex, R
     if (last < 0) return;
     launch_dep(residual_sums_kernel, dim3((unsigned)ceil_div64(p.width, 32), (unsigned)(last + 1)), dim3(32, 32), 0, ex.st, p.partial, g.blocks, p.width, o, accumulate);
     ex.launches += 1;
+}
+
+// The shared memory limit of every variant, once for a device: a limit set for one call could be lowered by a call of another thread
+// before its launch.
+template <typename TS, typename TD> static bool residual_init_types()
+{
+    const int threads[] = {256, 128, 256, 1024};  // parts of warps, and blocks of each kind
+    for (int i = 0; i < 4; ++i)
+        for (int k = 0; k < 4; ++k)
+            for (ResidualKernel f : {residual_kernel<TS, TD>(i & 1, i & 2, threads[k], k > 0), residual_grad_kernel<TS, TD>(i & 1, i & 2, threads[k], k > 0)})
+                if (cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, RN_MAX_SMEM) != cudaSuccess) return false;
+    return true;
+}
+static bool residual_init(std::string &err)
+{
+    if (residual_init_types<float, float>() && residual_init_types<float, bf16>() && residual_init_types<bf16, bf16>()) return true;
+    err = "cannot raise the dynamic shared memory limit of the residual norms";
+    return false;
 }

@@ -312,7 +312,7 @@ extern "C" lp_status lp_create(lp_ctx **out, int32_t device, void *cuda_stream)
     ctx->embed_err = ctx->err_flag + 1;
     cudaMemset(ctx->exhausted_dev, 0, 256);
     std::string tc_err;
-    if (!tc_init(ctx->tc, tc_err) || !ns_init(ctx->ns, tc_err) || !grouped_init(tc_err)) {
+    if (!tc_init(ctx->tc, tc_err) || !ns_init(ctx->ns, tc_err) || !residual_init(tc_err) || !grouped_init(tc_err)) {
         lp_destroy(ctx);
         cudaGetLastError();
         return fail(nullptr, LP_ECUDA, "lp_create: " + tc_err);

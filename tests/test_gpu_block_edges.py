@@ -2,6 +2,8 @@
 
 Tolerances of the products are derived in the docstring of test_gpu_grouped, those of the norms in test_gpu_blocks.
 """
+import ctypes
+
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -52,3 +54,34 @@ def test_fp32_results_of_whole_and_short_tiles(ctx, n):
     assert ((first.double() - want).abs() <= per * mag + 2.0 ** -24 * want.abs()).all()
     for _ in range(20):
         assert torch.equal(ctx.grouped_linear(a, off, b, out=torch.zeros_like(first)), first)
+
+
+def test_two_threads_with_rows_of_different_widths(pkg):
+    """Two contexts on two host threads call the same kernel with different amounts of shared memory, without anything between the calls."""
+    import threading
+    failed, streams = [], [torch.cuda.Stream() for _ in range(2)]
+    contexts = [pkg.Context(0, s) for s in streams]
+
+    def calls(c, x, branch):
+        desc = pkg.ResidualDesc(rows=2, width=x.shape[1], stream_prec=pkg.LP_FP32, prec=pkg.LP_FP32, pre_norm=pkg.LP_NORM_RMS, eps=1e-6, scale=1.0)
+        n, y, ld = torch.empty_like(x), torch.empty_like(x), x.shape[1]
+        args = (c.h, ctypes.addressof(desc), x.data_ptr(), ld, x.data_ptr() if branch else None, ld, y.data_ptr() if branch else None, ld, n.data_ptr(), ld)
+        f = c.lib.lp_residual_norm
+        for i in range(40000):
+            if f(*args) != 0:
+                failed.append(c.lib.lp_last_error(c.h).decode())
+                return
+            if i % 500 == 499:
+                c.stream.synchronize()
+
+    torch.cuda.synchronize()
+    x = [torch.randn(2, width, device=DEV) for width in (8192, 2304)]
+    threads = [threading.Thread(target=calls, args=a) for a in ((contexts[0], x[0], True), (contexts[1], x[1], False))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    for c in contexts:
+        c.close()
+    assert not failed, failed
