@@ -3,10 +3,12 @@
 //   grouped linear       rows offsets[g] .. offsets[g + 1] - 1:  C = act(A B[g] + bias[g])    (B[g] [K, N], or [N, K]: transposed)
 //   grouped weight grad  dW[g] = A_g^T dZ_g,  dbias[g] = column sums of dZ_g
 //
-// BF16 operands go to the matrix instructions as they are.  FP32 operands are split into three BF16 numbers of eight bits each,
-// x = x0 + x1 + x2 exactly (the upper half of the word, of the rest, and of the rest's rest), and of the nine products the six
-// larger ones are taken, so that a product is off by about 2^-23; the accumulator of the matrix instructions rounds towards
-// zero, so it adds up 64 terms, small products first, and those sums are added in FP32 registers.
+// The accumulator of the matrix instructions rounds towards zero, so what it adds up drifts by up to 2^-23 per addition of 16 terms.  BF16
+// operands go to the matrix instructions as they are, 512 terms at a time, and these sums are added in FP32 registers (in one
+// accumulator 2^20 terms of one sign came out 0.6 % too small; 65,536 x 1,024 x 1,024 takes 109 us where one accumulator took 106).
+// FP32 operands are split into three BF16 numbers of eight bits each, x = x0 + x1 + x2 exactly (the upper half of the word, of the
+// rest, and of the rest's rest), and of the nine products the six larger ones are taken, so that a product is off by about 2^-23; the
+// accumulator adds up 64 terms, small products first.
 //
 // Persistent blocks of 20 warps, one per SM.  Sizes of the groups are on the device: one warp walks the offsets, 32 groups at a time,
 // and finds the block's tiles (linear) or its share of the 64-row blocks of all tiles (weight gradient) without any plan or host read.
@@ -51,6 +53,7 @@ template <bool WIDE> constexpr int GP_EXTRA_SMEM = WIDE ? 65536 : 32768;  // res
 constexpr int GP_JOBS = 4;  // tiles that are known ahead
 constexpr int GP_MAX_STAGES = 8;
 constexpr int GP_MAX_GROUPS = 1 << 20;
+template <typename T> constexpr int GP_FLUSH = sizeof(T) == 4 ? 1 : 8;  // blocks of 64 terms that an accumulator adds up
 
 struct GroupedSplit {  // a tile of the weight gradient that several blocks share, noted by the first of them; first_slot < 0: none
     int group, kt, nt, first_slot, last_block;
@@ -65,7 +68,7 @@ struct GroupedParams {
     int tiles_n, tiles_k;    // tiles_k: weight gradient only
     const float *reg;        // FP32: the operand that comes through registers (A; dZ of the weight gradient), rows on 16 bytes
     int64_t ld_reg;
-    int stages, flush;       // blocks of 64 terms that an accumulator adds up
+    int stages, flush;       // flush: GP_FLUSH
     // linear
     const float *bias;
     int relu;
@@ -729,7 +732,7 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
         };
         while (ok && next_job()) {
             const int c0 = j.nt * BN + part * COLS;  // first column of this warp
-            if (!WGRAD && PARTS == 1) {
+            if (!WGRAD && PARTS == 1 && j.kbs <= p.flush) {
                 // one accumulator holds all terms: from tensor memory straight to the result
                 const int row = j.row0 + rank * 128 + quarter * 32;
                 T *dst = (T *)p.C + (int64_t)row * p.ldc + c0;
@@ -801,7 +804,13 @@ __global__ void __launch_bounds__(GP_THREADS, 1) grouped_kernel(const __grid_con
                 ok = __all_sync(0xffffffffu, wait_bar(smem_u32(&bar_sum_empty), (summed - 1) & 1, p.wait_ns));
                 if (!ok) { if (lane == 0) atomicExch(p.err, 7); break; }
             }
-            if (!WGRAD) {
+            if (!WGRAD && PARTS == 1) {
+                const int row = j.row0 + rank * 128 + quarter * 32;
+                if (p.tma_c) stage_free<0>();
+                finish_columns<COLS>(v, p.bias ? p.bias + (int64_t)j.g * p.N + c0 : nullptr, p.vec_bias, p.N - c0, p.relu);
+                stage_columns<T, COLS * 2, COLS>(0, v, stage);
+                if (c0 < p.N) put_rows<T, COLS * 2>(p.tma_c ? &mapC : nullptr, c0, row, (T *)p.C + (int64_t)row * p.ldc + c0, p.ldc, j.row_end - row, p.N - c0, p.vec_c, stage);
+            } else if (!WGRAD) {
                 const int row = j.row0 + quarter * 32;
                 T *dst = (T *)p.C + (int64_t)row * p.ldc + c0;
                 constexpr int PC = PUT_COLS<T, 64>;

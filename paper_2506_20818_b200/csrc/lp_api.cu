@@ -2677,7 +2677,7 @@ extern "C" lp_status lp_grouped_linear(lp_ctx *ctx, int32_t prec, int64_t M, int
     auto run = [&](auto mode, auto elem) -> lp_status {
         constexpr int MODE = decltype(mode)::value;
         using T = decltype(elem);
-        p.flush = sizeof(T) == 4 ? 1 : (K + 63) / 64;
+        p.flush = GP_FLUSH<T>;
         p.vec_c = on_16_bytes<T>(C, ld_c) && N % (16 / (int)sizeof(T)) == 0;
         GroupedPlan g = grouped_plan<MODE, T>(M, groups, N, K, A, ld_a, B, ldb);
         uint8_t *ws = nullptr;
@@ -2724,7 +2724,7 @@ extern "C" lp_status lp_grouped_weight_grad(lp_ctx *ctx, int32_t prec, int64_t M
     p.offsets_err = ctx->embed_err;
     auto run = [&](auto elem) -> lp_status {
         using T = decltype(elem);
-        p.flush = sizeof(T) == 4 ? 1 : 8;
+        p.flush = GP_FLUSH<T>;
         GroupedPlan g = grouped_plan<GP_WGRAD, T>(M, groups, N, K, A, ld_a, dZ, ld_dz);
         uint8_t *ws = nullptr;
         const lp_status st = op_workspace(ctx, g.bytes, &ws);

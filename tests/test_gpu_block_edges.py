@@ -85,3 +85,20 @@ def test_two_threads_with_rows_of_different_widths(pkg):
     for c in contexts:
         c.close()
     assert not failed, failed
+
+
+@pytest.mark.parametrize("rows,k,n,trans", [(70, 65_536, 100, False), (1200, 65_536, 2000, False), (1200, 32_768, 2000, True), (33, 1 << 20, 8, False), (300, 2_049, 264, True), (9500, 513, 256, False)])
+def test_bf16_products_of_many_terms(ctx, rows, k, n, trans):
+    """Sums of one sign: every addition to the accumulator of the matrix instructions rounds towards zero, so a long one drifts.  It takes
+    512 terms: 32 additions of sixteen terms, off by at most 2^-22 of the sum each, and these sums are added in FP32, 2^-24 each: the
+    FP32 sum s lies within want (1 +- sums).  Rounding to BF16 is monotonic, so the result lies between the roundings of the two ends.
+    (The mean of the errors says nothing: these sums differ by less than a step of BF16, so their roundings are not spread evenly.)"""
+    g = torch.Generator(device=DEV).manual_seed(rows + k)
+    a = torch.rand(rows, k, generator=g, device=DEV).to(BF16)
+    b = torch.rand(2, *((n, k) if trans else (k, n)), generator=g, device=DEV).to(BF16)
+    cut = rows // 3
+    got = ctx.grouped_linear(a, torch.tensor([0, cut, rows], dtype=I32, device=DEV), b, trans_b=trans).double()
+    want = torch.cat([x.double() @ (w.double().T if trans else w.double()) for x, w in ((a[:cut], b[0]), (a[cut:], b[1]))])
+    sums = 32 * 2.0 ** -22 + (k / 512 + 1) * 2.0 ** -24
+    low, high = ((want * (1 + way)).to(BF16).double() for way in (-sums, sums))
+    assert (got >= low).all() and (got <= high).all()
