@@ -532,8 +532,9 @@ lp_status lp_residual_norm_grad(lp_ctx *ctx, const lp_residual_desc *desc, const
  *   A[M, K]    : DEVICE, row pitch ld_a;  C[M, N]: DEVICE, row pitch ld_c, does not overlap the inputs
  *   B          : DEVICE [groups, K, N] or [groups, N, K], matrices behind one another
  *   bias       : DEVICE float32 [groups, N] or NULL
- * Any width, pitch and alignment to the element is accepted.  Takes workspace from the context (growing synchronises) for the parts of
- * an FP32 B and for copies of operands whose rows do not start on multiples of 16 bytes.  Does not synchronise otherwise. */
+ * Any width, pitch and alignment to the element is accepted.  Takes workspace from the context (growing synchronises): LP_FP32: always
+ * 6 bytes per element for the parts of all matrices B, whose rows are rounded up to 8 elements; and copies of operands whose rows do not
+ * start on multiples of 16 bytes (both of LP_BF16, A of LP_FP32), whose rows are rounded up to 16 bytes.  Does not synchronise otherwise. */
 lp_status lp_grouped_linear(lp_ctx *ctx, int32_t prec, int64_t M, int32_t N, int32_t K, int64_t groups, const int32_t *offsets, const void *A, int64_t ld_a,
                             const void *B, int32_t trans_b, const float *bias, int32_t relu, void *C, int64_t ld_c);
 
@@ -541,8 +542,9 @@ lp_status lp_grouped_linear(lp_ctx *ctx, int32_t prec, int64_t M, int32_t N, int
  * group without rows.  FP32 sums in a fixed order: the same bits in every run.
  *   A[M, K], dZ[M, N] : DEVICE, row pitches ld_*, of `prec`
  *   dW[groups, K, N], dbias[groups, N] : DEVICE float32; dbias may be NULL.  accumulate != 0 adds to both
- * Takes workspace from the context (growing synchronises): at most 80 MB for partial sums, and copies of operands whose rows do not
- * start on multiples of 16 bytes.  Does not synchronise otherwise. */
+ * Takes workspace from the context (growing synchronises): at most 40 MB for partial sums; LP_FP32: always 6 bytes per element for the
+ * parts of A, whose rows are rounded up to 8 elements; and copies of operands whose rows do not start on multiples of 16 bytes (both of
+ * LP_BF16, dZ of LP_FP32), whose rows are rounded up to 16 bytes.  Does not synchronise otherwise. */
 lp_status lp_grouped_weight_grad(lp_ctx *ctx, int32_t prec, int64_t M, int32_t N, int32_t K, int64_t groups, const int32_t *offsets, const void *A, int64_t ld_a,
                                  const void *dZ, int64_t ld_dz, int32_t accumulate, float *dW, float *dbias);
 

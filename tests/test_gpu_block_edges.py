@@ -102,3 +102,28 @@ def test_bf16_products_of_many_terms(ctx, rows, k, n, trans):
     sums = 32 * 2.0 ** -22 + (k / 512 + 1) * 2.0 ** -24
     low, high = ((want * (1 + way)).to(BF16).double() for way in (-sums, sums))
     assert (got >= low).all() and (got <= high).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,k,n,extra", [(3000, 256, 64, 0), (3000, 250, 301, 1), (9000, 512, 520, 0)])
+def test_workspace_is_what_the_header_says(pkg, dtype, rows, k, n, extra):
+    size, up = 4 if dtype == F32 else 2, lambda cols, step: -(-cols // step) * step
+    a, dz = (torch.randn(rows, d + extra, device=DEV).to(dtype)[:, :d] for d in (k, n))
+    b = torch.randn(3, k, n, device=DEV).to(dtype)
+    off = torch.tensor([0, 100, 700, rows], dtype=I32, device=DEV)
+    aligned = lambda t: t.data_ptr() % 16 == 0 and t.stride(-2) * size % 16 == 0
+    copy = lambda t, cols, count: 0 if aligned(t) else up(cols, 16 // size) * size * count
+    places = 2 * 256   # of at most two operands, each rounded up to 256 bytes
+
+    def taken(call):
+        c = pkg.Context(0)
+        call(c)
+        torch.cuda.synchronize()
+        bytes_ = c.stats().workspace_bytes
+        c.close()
+        return bytes_
+
+    linear = 6 * up(n, 8) * 3 * k + copy(a, k, rows) if dtype == F32 else copy(a, k, rows) + copy(b, n, 3 * k)
+    assert linear <= taken(lambda c: c.grouped_linear(a, off, b)) <= linear + places
+    grad = 6 * up(k, 8) * rows + copy(dz, n, rows) if dtype == F32 else copy(a, k, rows) + copy(dz, n, rows)
+    assert grad <= taken(lambda c: c.grouped_weight_grad(a, dz, off, bias=True)) <= grad + places + 40_000_000
