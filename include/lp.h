@@ -529,7 +529,7 @@ lp_status lp_residual_norm_grad(lp_ctx *ctx, const lp_residual_desc *desc, const
  *   offsets    : DEVICE int32 [groups + 1], not decreasing, in [0, M].  Others are clamped to the nearest that are, and the next
  *                lp_get_stats returns LP_EINVAL once.  Rows before offsets[0] and from offsets[groups] on are neither read into any
  *                result nor written
- *   A[M, K]    : DEVICE, row pitch ld_a;  C[M, N]: DEVICE, row pitch ld_c, does not overlap the inputs
+ *   A[M, K]    : DEVICE, row pitch ld_a;  C[M, N]: DEVICE, row pitch ld_c; refused where it overlaps an input
  *   B          : DEVICE [groups, K, N] or [groups, N, K], matrices behind one another
  *   bias       : DEVICE float32 [groups, N] or NULL
  * Any width, pitch and alignment to the element is accepted.  Takes workspace from the context (growing synchronises): LP_FP32: always
@@ -541,7 +541,8 @@ lp_status lp_grouped_linear(lp_ctx *ctx, int32_t prec, int64_t M, int32_t N, int
 /* Weight gradients of lp_grouped_linear: dW[g] = A_g^T dZ_g and dbias[g] = column sums of dZ_g over the rows of group g, zeros for a
  * group without rows.  FP32 sums in a fixed order: the same bits in every run.
  *   A[M, K], dZ[M, N] : DEVICE, row pitches ld_*, of `prec`
- *   dW[groups, K, N], dbias[groups, N] : DEVICE float32; dbias may be NULL.  accumulate != 0 adds to both
+ *   dW[groups, K, N], dbias[groups, N] : DEVICE float32; dbias may be NULL.  accumulate != 0 adds to both.  Refused where they overlap
+ *                       an input or one another
  * Takes workspace from the context (growing synchronises): at most 40 MB for partial sums; LP_FP32: always 6 bytes per element for the
  * parts of A, whose rows are rounded up to 8 elements; and copies of operands whose rows do not start on multiples of 16 bytes (both of
  * LP_BF16, dZ of LP_FP32), whose rows are rounded up to 16 bytes.  Does not synchronise otherwise. */

@@ -2646,6 +2646,29 @@ extern "C" lp_status lp_residual_norm_grad(lp_ctx *ctx, const lp_residual_desc *
 // ----------------------------------------------------------------------------------------------
 // products by group
 // ----------------------------------------------------------------------------------------------
+struct Region {     // `rows` rows of `width` bytes, `pitch` bytes apart
+    const void *at;
+    int64_t rows, width, pitch;
+};
+static Region matrix_region(const void *at, int64_t rows, int64_t cols, int64_t ld, int32_t prec)
+{
+    const int64_t size = prec == LP_FP32 ? 4 : 2;
+    return {at, rows, cols * size, ld * size};
+}
+static Region block_region(const void *at, int64_t bytes) { return {at, 1, bytes, bytes}; }
+// A byte of both.  Columns of one buffer (rows of the same pitch) may lie beside one another; of rows of different pitches whose ranges
+// meet it is taken for granted.
+static bool regions_overlap(const Region &a, const Region &b)
+{
+    if (!a.at || !b.at || a.rows <= 0 || b.rows <= 0) return false;
+    const uintptr_t x = (uintptr_t)a.at, y = (uintptr_t)b.at;
+    if (x + (uintptr_t)((a.rows - 1) * a.pitch + a.width) <= y || y + (uintptr_t)((b.rows - 1) * b.pitch + b.width) <= x) return false;
+    if (a.rows > 1 && b.rows > 1 && a.pitch != b.pitch) return true;
+    const uintptr_t pitch = (uintptr_t)(a.rows > 1 ? a.pitch : b.rows > 1 ? b.pitch : std::max(a.width, b.width) * 2);
+    const uintptr_t d = x <= y ? (y - x) % pitch : (pitch - (x - y) % pitch) % pitch;  // from a column of a to the same of b
+    return d < (uintptr_t)a.width || d + (uintptr_t)b.width > pitch;
+}
+
 static lp_status grouped_check(lp_ctx *ctx, const std::string &who, int32_t prec, int64_t M, int32_t N, int32_t K, int64_t groups, const int32_t *offsets)
 {
     if (!prec_ok(prec)) return fail(ctx, LP_EINVAL, who + ": unknown precision");
@@ -2668,6 +2691,10 @@ extern "C" lp_status lp_grouped_linear(lp_ctx *ctx, int32_t prec, int64_t M, int
     if (M == 0 || groups == 0) return LP_OK;
     if (!A || !B || !C) return fail(ctx, LP_EINVAL, who + ": null array");
     if (misaligned(A, prec) || misaligned(B, prec) || misaligned(C, prec) || misaligned(bias, LP_FP32)) return fail(ctx, LP_EINVAL, who + ": an array is not aligned to its elements");
+    const Region result = matrix_region(C, M, N, ld_c, prec);
+    for (const Region &in : {matrix_region(A, M, K, ld_a, prec), block_region(B, groups * K * N * (prec == LP_FP32 ? 4 : 2)), block_region(bias, groups * N * 4),
+                             block_region(offsets, (groups + 1) * 4)})
+        if (regions_overlap(result, in)) return fail(ctx, LP_EINVAL, who + ": C overlaps an input");
     CK(cudaSetDevice(ctx->device));
     GroupedParams p{};
     p.offsets = offsets; p.groups = (int)groups; p.rows = (int)M; p.N = N; p.K = K;
@@ -2709,6 +2736,10 @@ extern "C" lp_status lp_grouped_weight_grad(lp_ctx *ctx, int32_t prec, int64_t M
     if (!dW || (M > 0 && (!A || !dZ))) return fail(ctx, LP_EINVAL, who + ": null array");
     if (misaligned(A, prec) || misaligned(dZ, prec) || misaligned(dW, LP_FP32) || misaligned(dbias, LP_FP32))
         return fail(ctx, LP_EINVAL, who + ": an array is not aligned to its elements");
+    const Region results[2] = {block_region(dW, groups * K * N * 4), block_region(dbias, groups * N * 4)};
+    for (const Region &in : {matrix_region(A, M, K, ld_a, prec), matrix_region(dZ, M, N, ld_dz, prec), block_region(offsets, (groups + 1) * 4)})
+        if (regions_overlap(results[0], in) || regions_overlap(results[1], in)) return fail(ctx, LP_EINVAL, who + ": a result overlaps an input");
+    if (regions_overlap(results[0], results[1])) return fail(ctx, LP_EINVAL, who + ": the results overlap");
     CK(cudaSetDevice(ctx->device));
     if (M == 0) {
         if (!accumulate) {

@@ -127,3 +127,31 @@ def test_workspace_is_what_the_header_says(pkg, dtype, rows, k, n, extra):
     assert linear <= taken(lambda c: c.grouped_linear(a, off, b)) <= linear + places
     grad = 6 * up(k, 8) * rows + copy(dz, n, rows) if dtype == F32 else copy(a, k, rows) + copy(dz, n, rows)
     assert grad <= taken(lambda c: c.grouped_weight_grad(a, dz, off, bias=True)) <= grad + places + 40_000_000
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_products_into_their_own_operands_are_refused(pkg, ctx, dtype):
+    off = torch.tensor([0, 30, 100], dtype=I32, device=DEV)
+    buf = torch.randn(140, 200, device=DEV).to(dtype)
+    a, b = buf[:100, :64], torch.randn(2, 64, 64, device=DEV).to(dtype)
+    flat = buf.view(-1)
+    f32 = torch.randn(3 * 64 * 64 + 100, device=DEV)
+    bad = [lambda: ctx.grouped_linear(a, off, b, out=a), lambda: ctx.grouped_linear(a, off, b, out=buf[:100, 63:127]), lambda: ctx.grouped_linear(a, off, b, out=buf[1:101, :64]),
+           lambda: ctx.grouped_linear(buf[1:101, 100:164], off, b, out=buf[:100, 40:104]), lambda: ctx.grouped_linear(a, off, b, out=flat[99 * 200:99 * 200 + 6400].view(100, 64)),
+           lambda: ctx.grouped_linear(a, off, flat[:2 * 64 * 64].view(2, 64, 64), out=buf[20:120, 100:164])]
+    if dtype == F32:
+        w = f32[:2 * 64 * 64].view(2, 64, 64)
+        x = f32[4096:4096 + 6400].view(100, 64)
+        bad += [lambda: ctx.grouped_weight_grad(x, a, off, dW=w), lambda: ctx.grouped_weight_grad(a, x, off, dW=w), lambda: ctx.grouped_linear(a, off, b, bias=w.view(-1)[:128].view(2, 64), out=f32[100:6500].view(100, 64)),
+                lambda: ctx.grouped_weight_grad(a, a, off, dW=w, dbias=f32[100:228].view(2, 64)), lambda: ctx.grouped_weight_grad(a, x, off, dW=torch.zeros_like(w), dbias=f32[4100:4228].view(2, 64))]
+    for i, call in enumerate(bad):
+        with pytest.raises(pkg.LpError) as e:
+            call()
+        assert e.value.status == -1, i
+    # beside one another in one buffer, and behind one another
+    want = ctx.grouped_linear(a, off, b)
+    assert torch.equal(ctx.grouped_linear(a, off, b, out=buf[:100, 64:128]), want)
+    assert torch.equal(ctx.grouped_linear(a, off, b, out=buf[:100, 136:200]), want)
+    assert torch.equal(ctx.grouped_linear(a, off, b, out=flat[99 * 200 + 64:99 * 200 + 64 + 6400].view(100, 64)), want)
+    one = ctx.grouped_linear(a[:1], torch.tensor([0, 0, 1], dtype=I32, device=DEV), b)
+    assert torch.equal(ctx.grouped_linear(buf[:1, :64], torch.tensor([0, 0, 1], dtype=I32, device=DEV), b, out=buf[:1, 64:128]), one)
