@@ -466,7 +466,8 @@ lp_status lp_muon_step(lp_ctx *ctx, const lp_muon_desc *desc, const lp_matrix *m
  * The gradient is the same call on the gradient.  Results do not depend on how rows are split over calls (row_base), on pitches
  * or on types.  Dropped elements are zero whatever they held, NaN included.
  *   prec      : LP_FP32 or LP_BF16, of in and out
- *   in, out   : DEVICE [rows, width], row pitch ld_*; out may be in itself.  rows < 2^31, width <= 2^20, pitches < 2^29
+ *   in, out   : DEVICE [rows, width], row pitch ld_*; out may be in itself (other overlaps are refused).  rows < 2^31,
+ *               width <= 2^20, pitches < 2^29
  *   p         : in [0, 1]
  * Does not synchronise. */
 lp_status lp_dropout(lp_ctx *ctx, int32_t prec, int64_t rows, int32_t width, const void *in, int64_t ld_in, double p, uint64_t seed, uint64_t step, int64_t row_base,
@@ -499,6 +500,7 @@ typedef struct {
  *   h[rows, width] : DEVICE; NULL: no block has run yet, y = x is not written and only n is
  *   y[rows, width] : DEVICE, may be x itself; NULL = not wanted
  *   n[rows, width] : DEVICE, may be h itself; NULL exactly when pre_norm is LP_NORM_NONE
+ * A result may take the place of any input of the same type and pitch; other overlaps, and results over one another, are refused.
  * Any pitch and alignment to the element is accepted; rows that start on multiples of 16 bytes are the fast ones.
  * Does not synchronise. */
 lp_status lp_residual_norm(lp_ctx *ctx, const lp_residual_desc *desc, const void *x, int64_t ld_x, const void *h, int64_t ld_h, void *y, int64_t ld_y, void *n,

@@ -2491,6 +2491,42 @@ static bool drop_args(double p, uint64_t seed, uint64_t step, int64_t row_base, 
     return true;
 }
 
+struct Region {     // `rows` rows of `width` bytes, `pitch` bytes apart
+    const void *at;
+    int64_t rows, width, pitch;
+};
+static Region matrix_region(const void *at, int64_t rows, int64_t cols, int64_t ld, int32_t prec)
+{
+    const int64_t size = prec == LP_FP32 ? 4 : 2;
+    return {at, rows, cols * size, ld * size};
+}
+static Region block_region(const void *at, int64_t bytes) { return {at, 1, bytes, bytes}; }
+// A byte of both.  Columns of one buffer (rows of the same pitch) may lie beside one another; of rows of different pitches whose ranges
+// meet it is taken for granted.
+static bool regions_overlap(const Region &a, const Region &b)
+{
+    if (!a.at || !b.at || a.rows <= 0 || b.rows <= 0) return false;
+    const uintptr_t x = (uintptr_t)a.at, y = (uintptr_t)b.at;
+    if (x + (uintptr_t)((a.rows - 1) * a.pitch + a.width) <= y || y + (uintptr_t)((b.rows - 1) * b.pitch + b.width) <= x) return false;
+    if (a.rows > 1 && b.rows > 1 && a.pitch != b.pitch) return true;
+    const uintptr_t pitch = (uintptr_t)(a.rows > 1 ? a.pitch : b.rows > 1 ? b.pitch : std::max(a.width, b.width) * 2);
+    const uintptr_t d = x <= y ? (y - x) % pitch : (pitch - (x - y) % pitch) % pitch;  // from a column of a to the same of b
+    return d < (uintptr_t)a.width || d + (uintptr_t)b.width > pitch;
+}
+// what a result may be written over: an input with the same rows at the same places
+static bool regions_same(const Region &a, const Region &b) { return a.at == b.at && a.rows == b.rows && a.width == b.width && (a.rows <= 1 || a.pitch == b.pitch); }
+// results that overlap one another, or an input that they are not in the place of
+static bool results_overlap(std::initializer_list<Region> results, std::initializer_list<Region> inputs)
+{
+    for (const Region &r : results) {
+        for (const Region &in : inputs)
+            if (regions_overlap(r, in) && !regions_same(r, in)) return true;
+        for (const Region &other : results)
+            if (&other < &r && regions_overlap(r, other)) return true;
+    }
+    return false;
+}
+
 static bool prec_ok(int32_t prec) { return prec == LP_FP32 || prec == LP_BF16; }
 
 extern "C" lp_status lp_dropout(lp_ctx *ctx, int32_t prec, int64_t rows, int32_t width, const void *in, int64_t ld_in, double p, uint64_t seed, uint64_t step,
@@ -2507,6 +2543,8 @@ extern "C" lp_status lp_dropout(lp_ctx *ctx, int32_t prec, int64_t rows, int32_t
     if (rows == 0) return LP_OK;
     if (!in || !out) return fail(ctx, LP_EINVAL, "lp_dropout: null array");
     if (misaligned(in, prec) || misaligned(out, prec)) return fail(ctx, LP_EINVAL, "lp_dropout: an array is not aligned to its elements");
+    if (results_overlap({matrix_region(out, rows, width, ld_out, prec)}, {matrix_region(in, rows, width, ld_in, prec)}))
+        return fail(ctx, LP_EINVAL, "lp_dropout: out overlaps in and is not in its place");
     CK(cudaSetDevice(ctx->device));
     k.in = in; k.out = out; k.rows = (int)rows; k.width = width; k.ld_in = (uint32_t)(ld_in * (prec == LP_FP32 ? 4 : 2)); k.ld_out = (uint32_t)(ld_out * (prec == LP_FP32 ? 4 : 2));
     if (prec == LP_FP32) dropout_launch<float>(ctx->ex, k);
@@ -2581,6 +2619,11 @@ extern "C" lp_status lp_residual_norm(lp_ctx *ctx, const lp_residual_desc *desc,
     if (desc->rows == 0) return LP_OK;
     if (!x || (n == nullptr) != (k.pre_norm == LP_NORM_NONE)) return fail(ctx, LP_EINVAL, "lp_residual_norm: x is missing, or n and pre_norm do not go together");
     if (!y && !n) return fail(ctx, LP_EINVAL, "lp_residual_norm: no result is wanted");
+    auto matrix = [&](const void *at, int64_t ld, int32_t prec) { return matrix_region(at, desc->rows, desc->width, ld, prec); };
+    auto vector = [&](const void *at) { return block_region(at, 4 * (int64_t)desc->width); };
+    if (results_overlap({matrix(h ? y : nullptr, ld_y, ps), matrix(n, ld_n, pd)}, {matrix(x, ld_x, ps), matrix(h, ld_h, pd), matrix(k.gate, desc->ld_gate, pd), vector(k.gate_vec),
+                                                                                     vector(k.pre), vector(k.pre_bias), vector(k.post), vector(k.post_bias)}))
+        return fail(ctx, LP_EINVAL, "lp_residual_norm: the results overlap, or an input that they are not in the place of");
     CK(cudaSetDevice(ctx->device));
     const uint32_t bs = ps == LP_FP32 ? 4 : 2, bd = pd == LP_FP32 ? 4 : 2;
     k.extra_tx = (uint32_t)ctx->tc.overdeclare_tx;
@@ -2624,6 +2667,12 @@ extern "C" lp_status lp_residual_norm_grad(lp_ctx *ctx, const lp_residual_desc *
     }
     if (k.pre_norm ? !dn || !y : dn != nullptr) return fail(ctx, LP_EINVAL, who + ": dn and y are needed with a norm before the next block, and dn only then");
     if (!dy && !dn) return fail(ctx, LP_EINVAL, who + ": neither dy nor dn");
+    auto matrix = [&](const void *at, int64_t ld, int32_t prec) { return matrix_region(at, desc->rows, desc->width, ld, prec); };
+    auto vector = [&](const void *at) { return block_region(at, 4 * (int64_t)desc->width); };
+    if (results_overlap({matrix(dx, ld_dx, ps), matrix(dh, ld_dh, pd), gate_sum ? vector(dgate) : matrix(dgate, ld_dgate, pd), vector(dpre), vector(dpre_bias), vector(dpost), vector(dpost_bias)},
+                        {matrix(dy, ld_dy, ps), matrix(dn, ld_dn, pd), matrix(y, ld_y, ps), matrix(h, ld_h, pd), matrix(k.gate, desc->ld_gate, pd), vector(k.gate_vec), vector(k.pre),
+                         vector(k.pre_bias), vector(k.post), vector(k.post_bias)}))
+        return fail(ctx, LP_EINVAL, who + ": the results overlap, or an input that they are not in the place of");
     const uint32_t bs = ps == LP_FP32 ? 4 : 2, bd = pd == LP_FP32 ? 4 : 2;
     k.dy = dy; k.ld_dy = (uint32_t)ld_dy * bs; k.dn = dn; k.ld_dn = (uint32_t)ld_dn * bd; k.y = (void *)y; k.ld_y = (uint32_t)ld_y * bs; k.h = h; k.ld_h = (uint32_t)ld_h * bd;
     k.dx = dx; k.ld_dx = (uint32_t)ld_dx * bs; k.dh = dh; k.ld_dh = (uint32_t)ld_dh * bd;
@@ -2646,29 +2695,6 @@ extern "C" lp_status lp_residual_norm_grad(lp_ctx *ctx, const lp_residual_desc *
 // ----------------------------------------------------------------------------------------------
 // products by group
 // ----------------------------------------------------------------------------------------------
-struct Region {     // `rows` rows of `width` bytes, `pitch` bytes apart
-    const void *at;
-    int64_t rows, width, pitch;
-};
-static Region matrix_region(const void *at, int64_t rows, int64_t cols, int64_t ld, int32_t prec)
-{
-    const int64_t size = prec == LP_FP32 ? 4 : 2;
-    return {at, rows, cols * size, ld * size};
-}
-static Region block_region(const void *at, int64_t bytes) { return {at, 1, bytes, bytes}; }
-// A byte of both.  Columns of one buffer (rows of the same pitch) may lie beside one another; of rows of different pitches whose ranges
-// meet it is taken for granted.
-static bool regions_overlap(const Region &a, const Region &b)
-{
-    if (!a.at || !b.at || a.rows <= 0 || b.rows <= 0) return false;
-    const uintptr_t x = (uintptr_t)a.at, y = (uintptr_t)b.at;
-    if (x + (uintptr_t)((a.rows - 1) * a.pitch + a.width) <= y || y + (uintptr_t)((b.rows - 1) * b.pitch + b.width) <= x) return false;
-    if (a.rows > 1 && b.rows > 1 && a.pitch != b.pitch) return true;
-    const uintptr_t pitch = (uintptr_t)(a.rows > 1 ? a.pitch : b.rows > 1 ? b.pitch : std::max(a.width, b.width) * 2);
-    const uintptr_t d = x <= y ? (y - x) % pitch : (pitch - (x - y) % pitch) % pitch;  // from a column of a to the same of b
-    return d < (uintptr_t)a.width || d + (uintptr_t)b.width > pitch;
-}
-
 static lp_status grouped_check(lp_ctx *ctx, const std::string &who, int32_t prec, int64_t M, int32_t N, int32_t K, int64_t groups, const int32_t *offsets)
 {
     if (!prec_ok(prec)) return fail(ctx, LP_EINVAL, who + ": unknown precision");

@@ -155,3 +155,33 @@ def test_products_into_their_own_operands_are_refused(pkg, ctx, dtype):
     assert torch.equal(ctx.grouped_linear(a, off, b, out=flat[99 * 200 + 64:99 * 200 + 64 + 6400].view(100, 64)), want)
     one = ctx.grouped_linear(a[:1], torch.tensor([0, 0, 1], dtype=I32, device=DEV), b)
     assert torch.equal(ctx.grouped_linear(buf[:1, :64], torch.tensor([0, 0, 1], dtype=I32, device=DEV), b, out=buf[:1, 64:128]), one)
+
+
+def test_overlapping_results_of_dropout_and_norms_are_refused(pkg, ctx):
+    buf, w = torch.randn(70, 200, device=DEV), torch.ones(64, device=DEV)
+    x, h, z = buf[:60, :64], buf[:60, 64:128], torch.randn(60, 64, device=DEV)
+    shifted, beside = buf[1:61, :64], buf[:60, 128:192]
+    half = z.view(BF16).view(60, 128)[:, :64]          # the same memory as another type
+    bad = [lambda: ctx.dropout(x, 0.5, 1, 1, out=shifted), lambda: ctx.dropout(x, 0.5, 1, 1, out=buf[:60, 1:65]), lambda: ctx.dropout(z, 0.5, 1, 1, out=z.view(-1)[8:8 + 58 * 64].view(58, 64)),
+           lambda: ctx.residual_norm(x, h, y=shifted), lambda: ctx.residual_norm(x, h, n=buf[:60, 65:129]), lambda: ctx.residual_norm(x, h, y=z, n=z), lambda: ctx.residual_norm(z, dtype=BF16, n=half),
+           lambda: ctx.residual_norm(z, gate=w, h=h, pre=z.view(-1)[:64], y=z), lambda: ctx.residual_norm_grad(x, h, z, z, dx=shifted), lambda: ctx.residual_norm_grad(x, h, z, z, dx=beside, dh=beside),
+           lambda: ctx.residual_norm_grad(x, h, z, z, pre=w, dpre=z.view(-1)[:64]), lambda: ctx.residual_norm_grad(x, h, z, z, pre=w, post_norm="rms", post=w, dpre=beside[0], dpost=beside[0]),
+           lambda: ctx.residual_norm_grad(x, h, z, z, gate=w, dgate=w[:64], pre=w, dpre=w)]
+    before = buf.clone(), z.clone()
+    for i, call in enumerate(bad):
+        with pytest.raises(pkg.LpError) as e:
+            call()
+        assert e.value.status == -1, i
+    assert torch.equal(buf, before[0]) and torch.equal(z, before[1])
+    y, n = ctx.residual_norm(x, h)
+    got = ctx.residual_norm(x, h, y=beside, n=torch.empty(60, 64, device=DEV))
+    assert torch.equal(got[0], y) and torch.equal(got[1], n)
+    a, b = x.clone(), h.clone()                          # results in each other's inputs' places
+    got = ctx.residual_norm(a, b, y=b, n=a)
+    assert torch.equal(got[0], y) and torch.equal(got[1], n)
+    want = ctx.residual_norm_grad(z, x, y, h)
+    dn, yy = x.clone(), y.clone()
+    got = ctx.residual_norm_grad(z, dn, yy, h, dx=dn, dh=yy)
+    assert torch.equal(got["dx"], want["dx"]) and torch.equal(got["dh"], want["dh"])
+    drop = ctx.dropout(x, 0.5, 1, 1)
+    assert torch.equal(ctx.dropout(x, 0.5, 1, 1, out=beside), drop) and torch.equal(ctx.dropout(x, 0.5, 1, 1, out=x), drop)
