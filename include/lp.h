@@ -482,7 +482,7 @@ typedef struct {
     int32_t prec;                /* of h, n, a gate per element, and their gradients                        */
     int32_t pre_norm, post_norm; /* LP_NORM_*                                                               */
     double eps;                  /* >= 1e-37                                                                */
-    double scale;                /* of the block's contribution                                             */
+    double scale;                /* of the block's contribution; finite in FP32, also times 1 / (1 - p)     */
     double p;                    /* dropout, as in lp_dropout                                               */
     uint64_t seed, step;
     int64_t row_base;

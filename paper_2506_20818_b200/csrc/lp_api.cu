@@ -2564,8 +2564,8 @@ static lp_status residual_params(lp_ctx *ctx, const std::string &who, const lp_r
     for (int32_t kind : {d->pre_norm, d->post_norm})
         if (kind != LP_NORM_NONE && kind != LP_NORM_RMS && kind != LP_NORM_LAYER) return fail(ctx, LP_EINVAL, who + ": unknown norm");
     if (!(d->eps >= 1e-37) || !std::isfinite((float)d->eps)) return fail(ctx, LP_EINVAL, who + ": eps must be at least 1e-37 and finite");
-    if (!std::isfinite(d->scale)) return fail(ctx, LP_EINVAL, who + ": scale is not finite");
     if (!drop_args(d->p, d->seed, d->step, d->row_base, k.drop)) return fail(ctx, LP_EINVAL, who + ": p must be in [0, 1] and row_base not negative");
+    if (!std::isfinite((float)d->scale) || !std::isfinite((float)d->scale * k.drop.factor)) return fail(ctx, LP_EINVAL, who + ": scale, times the factor of the dropout, is beyond FP32");
     if (d->gate && d->ld_gate >= RN_MAX_PITCH) return fail(ctx, LP_EINVAL, who + ": a row pitch is 2^29 elements or more");
     if (d->gate && d->ld_gate != 0 && d->ld_gate < d->width) return fail(ctx, LP_EINVAL, who + ": a row pitch is smaller than the width");
     if (!branch && d->pre_norm == LP_NORM_NONE) return fail(ctx, LP_EINVAL, who + ": neither a block nor a norm");

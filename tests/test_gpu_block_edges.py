@@ -185,3 +185,14 @@ def test_overlapping_results_of_dropout_and_norms_are_refused(pkg, ctx):
     assert torch.equal(got["dx"], want["dx"]) and torch.equal(got["dh"], want["dh"])
     drop = ctx.dropout(x, 0.5, 1, 1)
     assert torch.equal(ctx.dropout(x, 0.5, 1, 1, out=beside), drop) and torch.equal(ctx.dropout(x, 0.5, 1, 1, out=x), drop)
+
+
+def test_scales_beyond_fp32_are_refused(pkg, ctx):
+    x = torch.ones(4, 16, device=DEV)
+    for scale, p in ((1e39, 0.0), (-1e300, 0.0), (3e38, 0.5), (1e300, 1.0), (float("inf"), 0.0), (float("nan"), 0.1)):
+        for call in (lambda: ctx.residual_norm(x, x, scale=scale, p=p), lambda: ctx.residual_norm_grad(x, x, x, x, scale=scale, p=p)):
+            with pytest.raises(pkg.LpError) as e:
+                call()
+            assert e.value.status == -1
+    y, _ = ctx.residual_norm(x, x, scale=3e38)
+    assert (y == torch.tensor(3e38)).all() and (ctx.residual_norm(x, x, scale=3e38, p=1.0)[0] == 1.0).all()
