@@ -2611,7 +2611,8 @@ extern "C" lp_status lp_residual_norm(lp_ctx *ctx, const lp_residual_desc *desc,
 {
     if (!ctx) return LP_EINVAL;
     ResidualParams k{};
-    lp_status s = residual_params(ctx, "lp_residual_norm", desc, h != nullptr, k);
+    const bool branch = h != nullptr || (desc && desc->rows == 0);  // without rows there may be no arrays
+    lp_status s = residual_params(ctx, "lp_residual_norm", desc, branch, k);
     if (s != LP_OK) return s;
     const int32_t ps = desc->stream_prec, pd = desc->prec;
     s = residual_arrays(ctx, "lp_residual_norm", desc->width, {{x, ld_x, ps}, {h, ld_h, pd}, {y, ld_y, ps}, {n, ld_n, pd}});
@@ -2644,7 +2645,7 @@ extern "C" lp_status lp_residual_norm_grad(lp_ctx *ctx, const lp_residual_desc *
     const std::string who = "lp_residual_norm_grad";
     ResidualParams k{};
     // without rows there may be no arrays: the results of [width] are those that the descriptor allows
-    const bool branch = h != nullptr || (desc && desc->rows == 0 && (dh || dgate || dpost || dpost_bias));
+    const bool branch = h != nullptr || (desc && desc->rows == 0);
     lp_status s = residual_params(ctx, who, desc, branch, k);
     if (s != LP_OK) return s;
     const int32_t ps = desc->stream_prec, pd = desc->prec;

@@ -196,3 +196,19 @@ def test_scales_beyond_fp32_are_refused(pkg, ctx):
             assert e.value.status == -1
     y, _ = ctx.residual_norm(x, x, scale=3e38)
     assert (y == torch.tensor(3e38)).all() and (ctx.residual_norm(x, x, scale=3e38, p=1.0)[0] == 1.0).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_batches_without_rows_and_without_a_norm_before_the_next_block(ctx, dtype):
+    x, h, w = torch.zeros(0, 48, device=DEV), torch.zeros(0, 48, dtype=dtype, device=DEV), torch.full((48,), 3.0, device=DEV)
+    y, n = ctx.residual_norm(x, h, pre_norm=None)
+    assert y.shape == (0, 48) and n is None
+    assert ctx.residual_norm(x, h, pre_norm=None, post_norm="rms", post=w, gate=h)[0].shape == (0, 48)
+    got = ctx.residual_norm_grad(x, None, x, h, pre_norm=None)
+    assert set(got) == {"dx", "dh"} and got["dh"].dtype == dtype
+    got = ctx.residual_norm_grad(x, None, x, h, pre_norm=None, gate=h)
+    assert got["dgate"].shape == (0, 48)
+    got = ctx.residual_norm_grad(x, None, x, h, pre_norm=None, post_norm="layer", post=w, post_bias=w, gate=w)
+    assert all((got[k] == 0).all() and got[k].shape == (48,) for k in ("dpost", "dpost_bias", "dgate"))
+    ctx.residual_norm_grad(x, None, x, h, pre_norm=None, post_norm="layer", post=w, dpost=w, accumulate=True)
+    assert (w == 3.0).all()
