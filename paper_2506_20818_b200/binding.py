@@ -586,6 +586,10 @@ class Context:
         elif dgate is not None:
             self._refuse(f"{who}: a gradient of the gate is wanted and there is no gate")
         columns = [0, 0, 0, 0, 0]
+        if pre_norm is None:
+            pre = pre_bias = None  # residual_norm does not look at the parameters of a norm that is not taken
+        if post_norm is None or h is None:
+            post = post_bias = None
         for i, (name, param, given) in enumerate((("dpre", pre, dpre), ("dpre_bias", pre_bias, dpre_bias), ("dpost", post, dpost), ("dpost_bias", post_bias, dpost_bias),
                                                   ("dgate", gate if gate_column else None, dgate if gate_column else None))):
             if given is None:

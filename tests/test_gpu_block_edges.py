@@ -212,3 +212,21 @@ def test_batches_without_rows_and_without_a_norm_before_the_next_block(ctx, dtyp
     assert all((got[k] == 0).all() and got[k].shape == (48,) for k in ("dpost", "dpost_bias", "dgate"))
     ctx.residual_norm_grad(x, None, x, h, pre_norm=None, post_norm="layer", post=w, dpost=w, accumulate=True)
     assert (w == 3.0).all()
+
+
+def test_parameters_of_norms_that_are_not_taken(pkg, ctx):
+    """They change nothing forward and have no gradient; asking for one by name is refused."""
+    x, h, dy = (torch.randn(30, 40, generator=gen(s)).to(DEV) for s in (1, 2, 3))
+    w, params = torch.full((40,), 2.0, device=DEV), ("pre", "pre_bias", "post", "post_bias")
+    every = {k: w for k in params}
+    assert torch.equal(ctx.residual_norm(x, h, pre_norm=None, **every)[0], ctx.residual_norm(x, h, pre_norm=None)[0])
+    got, want = ctx.residual_norm_grad(dy, None, x, h, pre_norm=None, **every), ctx.residual_norm_grad(dy, None, x, h, pre_norm=None)
+    assert set(got) == set(want) == {"dx", "dh"} and all(torch.equal(got[k], want[k]) for k in want)
+    # before the first block there is only the norm before it
+    assert torch.equal(ctx.residual_norm(x, post_norm="rms", gate=w, **every)[1], ctx.residual_norm(x, pre=w, pre_bias=w)[1])
+    got, want = ctx.residual_norm_grad(dy, h, x, post_norm="rms", gate=w, **every), ctx.residual_norm_grad(dy, h, x, pre=w, pre_bias=w)
+    assert set(got) == set(want) == {"dx", "dpre", "dpre_bias"} and all(torch.equal(got[k], want[k]) for k in want)
+    for kw in (dict(pre_norm=None, dpre=w), dict(pre_norm=None, dpost_bias=w)):
+        with pytest.raises(pkg.LpError) as e:
+            ctx.residual_norm_grad(dy, None, x, h, **kw)
+        assert e.value.status == -1
