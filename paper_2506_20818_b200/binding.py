@@ -564,8 +564,9 @@ class Context:
     def residual_norm_grad(self, dy, dn, y, h=None, pre_norm: Optional[str] = "rms", pre=None, pre_bias=None, post_norm: Optional[str] = None, post=None,
                            post_bias=None, gate=None, scale: float = 1.0, p: float = 0.0, seed: int = 0, step: int = 0, row_base: int = 0, eps: float = 1e-6,
                            accumulate: bool = False, dx=None, dh=None, dgate=None, dpre=None, dpre_bias=None, dpost=None, dpost_bias=None):
-        """Gradients of residual_norm: dx, dh, dgate and those of the norms' parameters that were given, as a dict.  dy or dn may
-        be None (zero); results may be given (accumulate adds to the vectors among them).  See lp_residual_norm_grad."""
+        """Gradients of residual_norm: dx, dh, dgate and those of the norms' parameters that were given, as a dict.  dy may be None
+        (zero) where there is a pre_norm; dn is None exactly where there is none.  Results may be given (accumulate adds to the vectors
+        among them).  See lp_residual_norm_grad."""
         who = "residual_norm_grad"
         like = y if y is not None else dy
         if like is None:
