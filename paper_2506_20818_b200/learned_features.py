@@ -31,6 +31,10 @@ class LearnedFeatures:
     def __init__(self, ctx, nodes: int, width: int = 64, hidden: int = 128, out: int = 64, seed: int = 0, types: int = 1, blocks: int = 0, dropout: float = 0.0):
         import torch
 
+        if types < 1 or blocks < 0 or not 0.0 <= dropout <= 1.0:
+            raise ValueError("LearnedFeatures: at least one type, no negative number of blocks, dropout in [0, 1]")
+        if blocks == 0 and (types != 1 or dropout != 0.0):
+            raise ValueError("LearnedFeatures: types and dropout belong to the residual blocks, and there are none")
         self.ctx, self.torch = ctx, torch
         self.nodes, self.width, self.hidden, self.out = nodes, width, hidden, out
         self.types, self.blocks, self.dropout, self.seed = types, blocks, dropout, seed
@@ -164,6 +168,8 @@ def main() -> None:
     ap.add_argument("--blocks", type=int, default=0, help="residual blocks in the place of the first transform")
     ap.add_argument("--dropout", type=float, default=0.0, help="of the residual blocks")
     args = ap.parse_args()
+    if args.blocks <= 0 and (args.types != 1 or args.dropout != 0.0):
+        ap.error("--types and --dropout belong to the residual blocks: give --blocks, too")
 
     import torch
     import workloads as wl
