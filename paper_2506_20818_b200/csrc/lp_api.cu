@@ -1924,10 +1924,11 @@ extern "C" lp_status lp_get_stats(lp_ctx *ctx, lp_stats *out)
         if (words[0] & 2) return fail(ctx, LP_ETIMEOUT, "a bounded wait inside the scan of an earlier step expired (results of that call are invalid)");
         return fail(ctx, LP_EINVAL, "a node id outside [0, n) was passed to an earlier call (it was clamped; results of that call are invalid)");
     }
-    if (words[1]) {
-        cudaMemsetAsync(ctx->embed_err, 0, sizeof(int), ctx->ex.st);
-        if (words[1] & 2) return fail(ctx, LP_ETIMEOUT, "a bounded wait inside the sort of an earlier lp_embed_grad expired (its gradient is invalid)");
-        if (words[1] & 4) return fail(ctx, LP_EINVAL, "decreasing offsets, or offsets outside the rows, were passed to an earlier lp_grouped_linear or lp_grouped_weight_grad (they were clamped)");
+    if (words[1]) {  // one kind of error at a time: the others are the next call's
+        const int kind = words[1] & 2 ? 2 : words[1] & 4 ? 4 : words[1], left = words[1] & ~kind;
+        CK(cudaMemcpyAsync(ctx->embed_err, &left, sizeof left, cudaMemcpyHostToDevice, ctx->ex.st));
+        if (kind == 2) return fail(ctx, LP_ETIMEOUT, "a bounded wait inside the sort of an earlier lp_embed_grad expired (its gradient is invalid)");
+        if (kind == 4) return fail(ctx, LP_EINVAL, "decreasing offsets, or offsets outside the rows, were passed to an earlier lp_grouped_linear or lp_grouped_weight_grad (they were clamped)");
         return fail(ctx, LP_EINVAL, "an id outside the table was passed to an earlier lp_embed (its row is zero) or lp_embed_grad (its row went nowhere)");
     }
     out->negatives_exhausted = (int64_t)ex;

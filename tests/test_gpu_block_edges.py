@@ -230,3 +230,21 @@ def test_parameters_of_norms_that_are_not_taken(pkg, ctx):
         with pytest.raises(pkg.LpError) as e:
             ctx.residual_norm_grad(dy, None, x, h, **kw)
         assert e.value.status == -1
+
+
+def test_bad_ids_and_bad_offsets_are_both_reported(pkg):
+    c = pkg.Context(0)
+    table, a, b = torch.ones(5, 16, device=DEV), torch.ones(4, 16, device=DEV), torch.ones(1, 16, 16, device=DEV)
+    for order in (0, 1):
+        calls = [lambda: c.embed(table, torch.tensor([1, 9], dtype=I32, device=DEV)), lambda: c.grouped_linear(a, torch.tensor([3, 1], dtype=I32, device=DEV), b)]
+        for call in calls[::-1] if order else calls:
+            call()
+        said = []
+        for _ in range(2):
+            with pytest.raises(pkg.LpError) as e:
+                c.stats()
+            assert e.value.status == -1
+            said.append(str(e.value))
+        assert sorted("offsets" in s for s in said) == [False, True] and sorted("id outside" in s for s in said) == [False, True]
+        c.stats()
+    c.close()
