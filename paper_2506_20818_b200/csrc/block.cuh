@@ -109,21 +109,6 @@ template <bool VEC> struct Cols {
     }
 };
 
-template <typename T, bool VEC> LP_DEVINL void load8(const T *row, const Cols<VEC> &c, float *v)
-{
-    if (c.full()) {
-        constexpr int VN = Vec16<T>::N;
-#pragma unroll
-        for (int k = 0; k < 8 / VN; ++k) {
-            Vec16<T> x;
-            x.load_once(row + c.base + k * VN);
-            x.to_float(v + k * VN);
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = c.has(j) ? to_f<T>(row[c.at(j)]) : 0.f;
-    }
-}
 template <typename T, bool VEC> LP_DEVINL void store8(T *row, const Cols<VEC> &c, const float *v)
 {
     if (c.full()) {
@@ -216,7 +201,7 @@ template <typename T, bool VEC> __global__ void __launch_bounds__(DROP_THREADS, 
     const int team = 1 << p.shift, teams = DROP_THREADS >> p.shift, t = threadIdx.x & (team - 1), lane = threadIdx.x & 31;
     const uint32_t row0 = blockIdx.x * (uint32_t)(teams * DROP_ROWS) + (threadIdx.x >> p.shift);  // rows < 2^31: no overflow
     const bool drops = p.drop.threshold != 0;
-    if (VEC) {
+    if constexpr (VEC) {
         constexpr int VN = Vec16<T>::N, NV = 8 / VN;
         for (int c0 = 8 * t; c0 < p.width; c0 += 8 * team) {
             const char *in = (const char *)p.in + c0 * sizeof(T);
@@ -253,21 +238,23 @@ template <typename T, bool VEC> __global__ void __launch_bounds__(DROP_THREADS, 
                 }
             }
         }
-        return;
-    }
-    for (int i = 0; i < DROP_ROWS; ++i) {
-        const uint32_t row = row0 + i * teams;
-        for (int c0 = 0; c0 < p.width; c0 += 8 * team) {
-            Cols<VEC> c(t, team, p.width);
-            c.base += c0;
-            float v[8];
-            if (row < (uint32_t)p.rows) load8<T, VEC>((const T *)((const char *)p.in + (uint64_t)row * p.ld_in), c, v);
-            // the whole warp takes part in handing the bits round, rows that are not there too
-            const uint32_t keep = drops ? c.keep(p.drop, row, lane) : 0xffu;
-            if (row < (uint32_t)p.rows) {
+    } else {
+        for (int i = 0; i < DROP_ROWS; ++i) {
+            const uint32_t row = row0 + i * teams;
+            for (int c0 = 0; c0 < p.width; c0 += 8 * team) {
+                Cols<VEC> c(t, team, p.width);
+                c.base += c0;
+                float v[8];
+                const T *in = (const T *)((const char *)p.in + (uint64_t)row * p.ld_in);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = (keep >> j) & 1u ? v[j] * p.drop.factor : 0.f;
-                store8<T, VEC>((T *)((char *)p.out + (uint64_t)row * p.ld_out), c, v);
+                for (int j = 0; j < 8; ++j) v[j] = row < (uint32_t)p.rows && c.has(j) ? to_f<T>(in[c.at(j)]) : 0.f;
+                // the whole warp takes part in handing the bits round, rows that are not there too
+                const uint32_t keep = drops ? c.keep(p.drop, row, lane) : 0xffu;
+                if (row < (uint32_t)p.rows) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] = (keep >> j) & 1u ? v[j] * p.drop.factor : 0.f;
+                    store8<T, VEC>((T *)((char *)p.out + (uint64_t)row * p.ld_out), c, v);
+                }
             }
         }
     }
@@ -793,10 +780,9 @@ static ResidualGrid residual_grad_grid(int64_t rows, int width, bool bias)
 }
 
 // every row of every array starts on 16 bytes and is made of pieces of 16
-static bool residual_vec(const ResidualParams &p, int size_s, int size_d)
+static bool residual_vec(const ResidualParams &p, int size_d)
 {
-    const bool only_d = !p.x && !p.dy && !(p.pre_norm && p.y);
-    if (p.width * size_d % 16 != 0 || (!only_d && p.width * size_s % 16 != 0)) return false;
+    if (p.width * size_d % 16 != 0) return false;  // else rows of the sum's type, as wide or twice as wide, are too
     auto ok = [](const void *array, uint32_t ld) { return !array || (((uintptr_t)array | ld) & 15) == 0; };
     return ok(p.x, p.ld_x) && ok(p.h, p.ld_h) && ok(p.y, p.ld_y) && ok(p.n, p.ld_n) && ok(p.dy, p.ld_dy) && ok(p.dn, p.ld_dn) && ok(p.dx, p.ld_dx) && ok(p.dh, p.ld_dh) &&
            ok(p.gate, p.ld_gate) && ok(p.dgate, p.ld_dgate);
@@ -854,7 +840,7 @@ template <typename TS, typename TD> static void residual_launch(Exec &ex, Residu
 {
     const ResidualGrid g = residual_grid(p.rows, p.width, 256, 768);
     p.team = g.team;
-    const bool vec = residual_vec(p, sizeof(TS), sizeof(TD)), bias = residual_bias(p.pre_bias || p.post_bias, vec, p.width);
+    const bool vec = residual_vec(p, sizeof(TD)), bias = residual_bias(p.pre_bias || p.post_bias, vec, p.width);
     const size_t smem = residual_pipe(p, g, vec, true, sizeof(TS), sizeof(TD), 256);
     launch_dep(residual_kernel<TS, TD>(vec, bias, g.threads, g.block), dim3(g.blocks), dim3(g.threads), smem, ex.st, p);
     ex.launches += 1;

@@ -2679,7 +2679,7 @@ extern "C" lp_status lp_residual_norm_grad(lp_ctx *ctx, const lp_residual_desc *
     k.dy = dy; k.ld_dy = (uint32_t)ld_dy * bs; k.dn = dn; k.ld_dn = (uint32_t)ld_dn * bd; k.y = (void *)y; k.ld_y = (uint32_t)ld_y * bs; k.h = h; k.ld_h = (uint32_t)ld_h * bd;
     k.dx = dx; k.ld_dx = (uint32_t)ld_dx * bs; k.dh = dh; k.ld_dh = (uint32_t)ld_dh * bd;
     if (!gate_sum) { k.dgate = dgate; k.ld_dgate = (uint32_t)ld_dgate * bd; }
-    const bool vec = residual_vec(k, (int)bs, (int)bd), bias = residual_bias(o.out[3] || o.out[4] || k.post_bias, vec, desc->width);
+    const bool vec = residual_vec(k, (int)bd), bias = residual_bias(o.out[3] || o.out[4] || k.post_bias, vec, desc->width);
     const ResidualGrid g = residual_grad_grid(desc->rows, desc->width, bias);
     uint8_t *ws = nullptr;
     s = op_workspace(ctx, sizeof(float) * (size_t)g.blocks * RN_SUMS * desc->width, &ws);
