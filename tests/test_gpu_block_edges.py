@@ -248,3 +248,32 @@ def test_bad_ids_and_bad_offsets_are_both_reported(pkg):
         assert sorted("offsets" in s for s in said) == [False, True] and sorted("id outside" in s for s in said) == [False, True]
         c.stats()
     c.close()
+
+
+@pytest.mark.parametrize("dtype,rows,k,n,size", [(BF16, 9500, 256, 256, 1900), (BF16, 9500, 256, 256, 30), (BF16, 9500, 1024, 512, 700), (F32, 3000, 128, 128, 600), (F32, 3000, 200, 300, 30), (F32, 3001, 1024, 129, 100),
+                                                 (BF16, 700, 1024, 96, 50)])
+def test_waits_of_every_kind_of_product_that_run_out(pkg, dtype, rows, k, n, size):
+    """The operands' wait of one block expires (16 bytes more are announced than come): pairs of blocks, operands that are split on their
+    way, accumulators in turn, groups that end within the first block of rows.  Reported once, and the context goes on."""
+    c = pkg.Context(0)
+    g = gen(rows + k)
+    bounds = list(range(0, rows, size)) + [rows]
+    groups = len(bounds) - 1
+    a, dz = torch.randn(rows, k, generator=g).to(dtype).to(DEV), torch.randn(rows, n, generator=g).to(dtype).to(DEV)
+    b = torch.randn(groups, k, n, generator=g).to(dtype).to(DEV)
+    off = torch.tensor(bounds, dtype=I32, device=DEV)
+    calls = (lambda: [c.grouped_linear(a, off, b)], lambda: [c.grouped_linear(dz, off, b, trans_b=True)], lambda: [*c.grouped_weight_grad(a, dz, off, bias=True)], lambda: [c.grouped_weight_grad(a, dz, off)])
+    want = [call() for call in calls]
+    c.stats()
+    for call in calls:
+        c.set_wait_limit(2_000_000, 16)
+        call()
+        with pytest.raises(pkg.LpError) as e:
+            c.stats()
+        assert e.value.status == -6
+        c.set_wait_limit(2_000_000_000, 0)
+        c.stats()
+        for again, first in zip(calls, want):
+            assert all(torch.equal(x, y) for x, y in zip(again(), first))
+    c.stats()
+    c.close()
