@@ -277,3 +277,75 @@ def test_waits_of_every_kind_of_product_that_run_out(pkg, dtype, rows, k, n, siz
             assert all(torch.equal(x, y) for x, y in zip(again(), first))
     c.stats()
     c.close()
+
+
+@pytest.mark.parametrize("width", [1040, 1041])
+def test_residual_norm_offsets_beyond_32_bits(ctx, width):
+    """Rows do not depend on one another: those at both ends of 4.4e9 elements have the bits of a call of their own."""
+    rows = (1 << 22) + 3
+    g = torch.Generator(device=DEV).manual_seed(width)
+    x, h = (torch.empty(rows, width, dtype=BF16, device=DEV) for _ in range(2))
+    ends = [slice(0, 3), slice(rows // 2, rows // 2 + 2), slice(rows - 5, rows)]
+    for t in (x, h):
+        t.fill_(0.5)
+        for e in ends:
+            t[e].normal_(generator=g)
+    w = 1 + 0.1 * torch.randn(width, generator=g, device=DEV)
+    args = dict(pre=w, post_norm="layer", post=w, gate=w, scale=0.5, p=0.3, seed=5, step=6)
+    small = [(x[e].clone(), h[e].clone()) for e in ends]
+    want = [ctx.residual_norm(a, b, row_base=e.start, **args) for (a, b), e in zip(small, ends)]
+    y, n = ctx.residual_norm(x, h, **args)
+    for (wy, wn), e in zip(want, ends):
+        assert torch.equal(y[e], wy) and torch.equal(n[e], wn)
+    grads = [ctx.residual_norm_grad(a, b, wy, b, row_base=e.start, **args) for (a, b), (wy, _), e in zip(small, want, ends)]
+    got = ctx.residual_norm_grad(x, h, y, h, dx=x, dh=n, **args)
+    for first, e in zip(grads, ends):
+        assert torch.equal(got["dx"][e], first["dx"]) and torch.equal(got["dh"][e], first["dh"])
+    del x, h, y, n, got
+    torch.cuda.empty_cache()
+
+
+def products_close(got, a, w, dtype, terms):
+    want, mag = a.double() @ w.double(), a.double().abs() @ w.double().abs()
+    per = terms / 16 * 2.0 ** -22 + 2.0 ** -22 if dtype == BF16 else 2.0 ** -21 + 5 * 2.0 ** -22 + (terms / 64 + 3) * 2.0 ** -24
+    assert ((got.double() - want).abs() <= per * mag + (2.0 ** -8 if got.dtype == BF16 else 2.0 ** -24) * want.abs()).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("k", [520, 521])
+def test_products_of_rows_beyond_32_bits(ctx, dtype, k):
+    rows, n = (1 << 22) + 3, 520
+    a = torch.randn(rows, k, dtype=dtype, device=DEV)
+    b = torch.randn(3, k, n, device=DEV).to(dtype)
+    bounds = [0, 1000, rows - 900, rows]
+    off = torch.tensor(bounds, dtype=I32, device=DEV)
+    c = ctx.grouped_linear(a, off, b)
+    for part, i in ((slice(0, 300), 0), (slice(rows - 1300, rows - 900), 1), (slice(rows - 900, rows), 2)):
+        products_close(c[part], a[part], b[i], dtype, k)
+    dw = ctx.grouped_weight_grad(a, c, off)
+    for part, i in ((slice(0, 1000), 0), (slice(rows - 900, rows), 2)):
+        products_close(dw[i], a[part].T, c[part], dtype, 1000)
+    del a, c
+    torch.cuda.empty_cache()
+    ctx.stats()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n", [2048, 2047])
+def test_products_with_matrices_beyond_32_bits(ctx, dtype, n):
+    groups, k, each = 520, 2048, 12
+    b = torch.randn(groups, k, n, dtype=dtype, device=DEV)
+    a, dz = (torch.randn(groups * each, d, device=DEV).to(dtype) for d in (k, n))
+    off = torch.arange(groups + 1, dtype=I32, device=DEV) * each
+    c, da = ctx.grouped_linear(a, off, b), ctx.grouped_linear(dz, off, b, trans_b=True)
+    dw, db = ctx.grouped_weight_grad(a, dz, off, bias=True)
+    assert b.numel() > 1 << 31 and dw.numel() > 1 << 31
+    for i in (0, 1, groups - 9, groups - 1):
+        part = slice(i * each, (i + 1) * each)
+        products_close(c[part], a[part], b[i], dtype, k)
+        products_close(da[part], dz[part], b[i].T, dtype, n)
+        products_close(dw[i], a[part].T, dz[part], dtype, each)
+        assert ((db[i].double() - dz[part].double().sum(0)).abs() <= (each + 1) * 2.0 ** -24 * dz[part].double().abs().sum(0)).all()
+    del b, dw
+    torch.cuda.empty_cache()
+    ctx.stats()
