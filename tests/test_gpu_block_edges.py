@@ -349,3 +349,30 @@ def test_products_with_matrices_beyond_32_bits(ctx, dtype, n):
     del b, dw
     torch.cuda.empty_cache()
     ctx.stats()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("groups,rows,k,n", [(5_000, 40_000, 72, 40), (100_000, 60_000, 24, 16), (1 << 20, 30_000, 8, 8)])
+def test_very_many_groups(ctx, dtype, groups, rows, k, n):
+    """Up to the largest number of groups, most of them of a few rows or none."""
+    g = gen(groups)
+    bounds = torch.cat((torch.tensor([0]), torch.randint(0, rows + 1, (groups - 1,), generator=g).sort().values, torch.tensor([rows])))
+    a, dz = torch.randn(rows, k, generator=g).to(dtype).to(DEV), torch.randn(rows, n, generator=g).to(dtype).to(DEV)
+    b = torch.randn(groups, k, n, device=DEV).to(dtype)
+    off = bounds.to(I32).to(DEV)
+    group = torch.repeat_interleave(torch.arange(groups), bounds.diff()).to(DEV)
+    w = b[group].double()
+    want, mag = torch.einsum("rk,rkn->rn", a.double(), w), torch.einsum("rk,rkn->rn", a.double().abs(), w.abs())
+    per = lambda terms: terms / 16 * 2.0 ** -22 + 2.0 ** -22 if dtype == BF16 else 2.0 ** -21 + 5 * 2.0 ** -22 + (terms / 64 + 3) * 2.0 ** -24
+    got = ctx.grouped_linear(a, off, b)
+    assert ((got.double() - want).abs() <= per(k) * mag + (2.0 ** -8 if dtype == BF16 else 2.0 ** -24) * want.abs()).all()
+    dw, db = ctx.grouped_weight_grad(a, dz, off, bias=True)
+    outer = a.double()[:, :, None] * dz.double()[:, None, :]
+    want = torch.zeros(groups, k, n, dtype=torch.float64, device=DEV).index_add_(0, group, outer)
+    mag = torch.zeros(groups, k, n, dtype=torch.float64, device=DEV).index_add_(0, group, outer.abs())
+    longest = int(bounds.diff().max())
+    assert ((dw.double() - want).abs() <= per(longest) * mag).all()
+    want = torch.zeros(groups, n, dtype=torch.float64, device=DEV).index_add_(0, group, dz.double())
+    mag = torch.zeros(groups, n, dtype=torch.float64, device=DEV).index_add_(0, group, dz.double().abs())
+    assert ((db.double() - want).abs() <= (longest + 1) * 2.0 ** -24 * mag).all()
+    ctx.stats()
