@@ -376,3 +376,94 @@ def test_very_many_groups(ctx, dtype, groups, rows, k, n):
     mag = torch.zeros(groups, n, dtype=torch.float64, device=DEV).index_add_(0, group, dz.double().abs())
     assert ((db.double() - want).abs() <= (longest + 1) * 2.0 ** -24 * mag).all()
     ctx.stats()
+
+
+def block_of_calls(c, dtype, rows, width, seed):
+    """Inputs, and a function that runs a whole block and its gradients into given results (or new ones)."""
+    g = gen(seed)
+    x, dy = (torch.randn(rows, width, generator=g).to(DEV) for _ in range(2))
+    w = (1 + 0.1 * torch.randn(width, generator=g)).to(DEV)
+    b, bias = torch.randn(5, width, width, generator=g).to(dtype).to(DEV), torch.randn(5, width, generator=g).to(DEV)
+    off = torch.tensor([0, rows // 7, rows // 7, rows // 2, rows - 3, rows], dtype=I32, device=DEV)
+    args = dict(pre=w, post_norm="rms", post=w, gate=w, scale=0.5, p=0.2, seed=seed, step=4)
+
+    def run(o=None):
+        o = o or {}
+        n = c.dropout(x.to(dtype), 0.1, seed, 5, out=o.get("n"))
+        h = c.grouped_linear(n, off, b, bias=bias, relu=True, out=o.get("h"))
+        y, m = c.residual_norm(x, h, y=o.get("y"), n=o.get("m"), **args)
+        d = c.residual_norm_grad(dy, m, y, h, **{k: o.get(k) for k in ("dx", "dh", "dpre", "dpost", "dgate")}, **args)
+        da = c.grouped_linear(d["dh"], off, b, trans_b=True, out=o.get("da"))
+        dw, db = c.grouped_weight_grad(n, d["dh"], off, bias=True, dW=o.get("dw"), dbias=o.get("db"))
+        return dict(n=n, h=h, y=y, m=m, da=da, dw=dw, db=db, **d)
+
+    return off, run
+
+
+@pytest.mark.parametrize("dtype,rows,width", [(BF16, 10_000, 256), (F32, 3_000, 192), (BF16, 3_001, 100)])
+def test_two_captured_blocks_share_a_workspace(pkg, dtype, rows, width):
+    """Pairs of blocks and FP32 operands too; replayed in turn, with groups that change between replays."""
+    stream = torch.cuda.Stream()
+    c = pkg.Context(0, stream)
+    with torch.cuda.stream(stream):
+        calls = [block_of_calls(c, dtype, r, width, s) for r, s in ((rows, 1), (rows // 2, 2))]
+        want = [{k: v.clone() for k, v in run().items()} for _, run in calls]
+        outs = [{k: torch.zeros_like(v) for k, v in w.items()} for w in want]
+        stream.synchronize()
+        graphs = [torch.cuda.CUDAGraph() for _ in calls]
+        for graph, out, (_, run) in zip(graphs, outs, calls):
+            with torch.cuda.graph(graph, stream=stream):
+                run(out)
+        for _ in range(3):
+            for out in outs:
+                for v in out.values():
+                    v.zero_()
+            for graph in graphs:
+                graph.replay()
+            stream.synchronize()
+            for out, w in zip(outs, want):
+                assert all(torch.equal(out[k], w[k]) for k in w)
+        off, run = calls[0]
+        off.copy_(torch.tensor([0, 1, 700, 701, 701, rows], dtype=I32))
+        graphs[0].replay()
+        again = run()
+        stream.synchronize()
+        assert all(torch.equal(outs[0][k], again[k]) for k in again) and not torch.equal(again["dw"], want[0]["dw"])
+    c.stats()
+    del graphs
+    c.close()
+
+
+def test_two_contexts_at_once(pkg):
+    """Two streams run whole blocks beside one another, from two host threads; each gets the bits that it gets alone."""
+    import threading
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    contexts = [pkg.Context(0, s) for s in streams]
+    runs, want = [], []
+    for c, s, kind in zip(contexts, streams, ((BF16, 20_000, 256, 3), (F32, 8_000, 200, 4))):
+        with torch.cuda.stream(s):
+            runs.append(block_of_calls(c, *kind)[1])
+            want.append(runs[-1]())
+            s.synchronize()
+    failed = []
+
+    def loop(i):
+        try:
+            with torch.cuda.stream(streams[i]):
+                for _ in range(40):
+                    got = runs[i]()
+                    if not all(torch.equal(got[k], want[i][k]) for k in got):
+                        failed.append(i)
+                contexts[i].stats()
+        except Exception as e:
+            failed.append(e)
+
+    threads = [threading.Thread(target=loop, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    for c in contexts:
+        c.close()
+    assert not failed, failed
