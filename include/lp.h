@@ -495,7 +495,7 @@ typedef struct {
 /* The end of one residual block and the norm before the next, in one pass:
  *     y = x + scale * gate * dropout(post(h)),     n = pre(y)
  * RMS norm: v * weight / sqrt(mean(v^2) + eps) (+ bias); layer norm: the same of v - mean(v).  All arithmetic in FP32; y and n are
- * rounded once (n is taken from the unrounded y).
+ * rounded once (n is taken from the unrounded y).  A row whose sum of squares is beyond FP32 is divided by infinity: zeros (+ bias).
  *   x[rows, width] : DEVICE, row pitch ld_x
  *   h[rows, width] : DEVICE; NULL: no block has run yet, y = x is not written and only n is
  *   y[rows, width] : DEVICE, may be x itself; NULL = not wanted
@@ -527,7 +527,7 @@ lp_status lp_residual_norm_grad(lp_ctx *ctx, const lp_residual_desc *desc, const
  *     C[r] = act(A[r] B[g] + bias[g])    for offsets[g] <= r < offsets[g + 1]
  * B[g] is [K, N] row-major (trans_b = 0) or [N, K] (trans_b = 1: with A = dZ and the forward B, the input gradient).
  *   prec       : LP_FP32 or LP_BF16, of A, B and C; sums are FP32, C is rounded once.  The products run on the tensor cores: LP_FP32
- *                operands as three BF16 numbers each (24 bits; an infinity gives NaN)
+ *                operands as three BF16 numbers each (24 bits, fewer of elements below 2^-103; an infinity gives NaN)
  *   offsets    : DEVICE int32 [groups + 1], not decreasing, in [0, M].  Others are clamped to the nearest that are, and the next
  *                lp_get_stats returns LP_EINVAL once.  Rows before offsets[0] and from offsets[groups] on are neither read into any
  *                result nor written
