@@ -18,14 +18,17 @@
 // A team of T threads (a power of two, eight columns each) holds a row in registers, so every array is read once and written
 // once: bound by HBM.  Teams of up to 32 threads are parts of warps, larger ones whole blocks.
 //
-// Measured on the device (the copy rate is 6.55 TB/s):
-//   dropout, 1,000,000 x 256 BF16                                    179 us, 5.7 TB/s: 64 of 112 instructions per eight elements are the
+// Measured on the device, launches one after the other (the copy rate is 6.55 TB/s):
+//   dropout, 1,000,000 x 256 BF16                                    185 us, 5.5 TB/s: 64 of 112 instructions per eight elements are the
 //                                                                    generator's, whose multiplications keep their pipe busy
-//   residual norm, 196,608 x 256, FP32 sums, BF16 blocks, both norms, dropout, gate per column    104 us, 5.8 TB/s
-//   its gradient                                                     177 us, 5.1 TB/s, and 5 us for the column sums of the blocks: 580
+//   residual norm, 196,608 x 256, FP32 sums, BF16 blocks, both norms, dropout, gate per column    106 us, 5.7 TB/s
+//     FP32 blocks 156 us, 5.2 TB/s; BF16 sums 101 us, 4.0 TB/s: the same instructions for two thirds of the bytes
+//   its gradient                                                     173 us, 5.2 TB/s, and 4 us for the column sums of the blocks: 580
 //                                                                    instructions per row of a warp at 16 warps per SM (128 registers)
-//   gradient, 50,001 x 417 FP32, layer norms, gate per element       186 us, 3.6 TB/s, and 8 us: 53 of a team's 64 threads have columns,
+//     FP32 blocks 203 us, 5.9 TB/s; BF16 sums 173 us, 3.5 TB/s
+//   gradient, 50,001 x 417 FP32, layer norms, gate per element       183 us, 3.6 TB/s, and 6 us: 53 of a team's 64 threads have columns,
 //                                                                    single elements loaded from shared memory and stored, four barriers a row
+//     FP32 sums and BF16 blocks 179 us, BF16 sums 190 us: as many instructions for fewer bytes
 #pragma once
 #include "gemm_tc.cuh"
 

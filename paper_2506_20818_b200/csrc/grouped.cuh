@@ -24,17 +24,22 @@
 // The weight gradient deals out equal shares of 64-row blocks: a tile that lies in several shares is written as partial tiles,
 // added in a fixed order by a second kernel.  Bits do not depend on anything but the sizes.
 //
-// Measured on the device (copy rate 6.55 TB/s, BF16 products 1,648 TFLOP/s):
-//   linear, BF16, 196,608 rows, 256 -> 256, 8 groups       36 us: 5.7 TB/s
-//   linear, BF16, 30,011 rows, 1,999 -> 1,000, transposed, 40 groups   109 us: 1.1 PFLOP/s (610 cycles per block of 64 terms, 512 of them
-//                                                          products), after 87 us that copy both operands to aligned rows at 6.4 TB/s
-//   weight gradient, BF16, 196,608 rows, 256 x 256, 8 groups   63 us and 12 us for shared tiles: 1,200 cycles per block of 64 rows where HBM
+// Measured on the device at 1,965 MHz (copy rate 6.55 TB/s, BF16 products 1,648 TFLOP/s); thousands of the large calls in a row meet the
+// power cap, which takes the clock to 1,500 to 1,800 MHz:
+//   linear, BF16, 196,608 rows, 256 -> 256, 8 groups       37 us: 5.5 TB/s, either layout of B
+//   linear, BF16, 30,011 rows, 1,999 -> 1,000, transposed, 40 groups   111 us: 1.1 PFLOP/s (610 cycles per block of 64 terms, 512 of them
+//                                                          products), after 94 us that copy both operands to aligned rows; 230 us in all under the cap
+//   weight gradient, BF16, 196,608 rows, 256 x 256, 8 groups   59 us and 11 us for shared tiles: 1,200 cycles per block of 64 rows where HBM
 //                                                          allows 1,400 at best, then 3 us to start, 7 us to write 19 MB of partial tiles
-//   linear, FP32, 100,003 rows, 256 -> 512, 16 groups      212 us: 742 TFLOP/s of BF16 products, tensor pipe 35 % busy.  A block of 64 terms
+//   linear, FP32, 100,003 rows, 256 -> 512, 16 groups      199 us (216 under the cap): 790 TFLOP/s of BF16 products.  A block of 64 terms
 //                                                          takes 2,500 cycles, 1,536 of them products.  Without the loads of A 157 us, without its
-//                                                          stores either 141, with one of the six products 200: the ways through shared memory
-//                                                          (320 KB a block by count) and two stages share the time
-//   weight gradient, FP32, 30,011 rows, 417 x 1,000, 40 groups    360 us, and 30 us before and after it
+//                                                          stores either 141, with one of the six products 200 (of 212): the ways through shared
+//                                                          memory (320 KB a block by count) and two stages share the time.  Transposed, 512 -> 256: 209
+//   weight gradient, FP32, 30,011 rows, 417 x 1,000, 40 groups    362 us, and 29 us before and after it; 100,003 rows, 256 x 512, 16 groups
+//                                                          264 us, 36 us for the parts of A before it and 9 us after it
+//   196,608 rows, 64 -> 64 BF16 (weight gradient), rows spread evenly over 1,000 groups 38 us (59), 10,000 groups 207 us (345), 100,000
+//                                                          groups 2.6 ms (3.9): tiles of a few rows; the walk takes about half a microsecond per 32
+//                                                          groups, 16 ms (37, it walks twice) for 2^20
 // Tried for FP32 and not faster (product, weight gradient; 64 terms with two stages and all loaders on one block: 210 to 218, 425 to 433 us):
 // blocks of 32 terms with four stages 249, 558, and with four groups of loaders that take blocks in turn 235, 495; two such groups with
 // blocks of 64 terms 222, 413 (and 17 instead of 15 us for 768 rows); the next tile's rows asked into L2 one tile earlier 237, 469.
