@@ -514,6 +514,7 @@ lp_status lp_residual_norm(lp_ctx *ctx, const lp_residual_desc *desc, const void
  *   dgate           : DEVICE; float32 [width] for a gate per column (ld_dgate is not looked at), else [rows, width] of `prec`
  *   dpre, dpre_bias, dpost, dpost_bias : DEVICE float32 [width]
  *   accumulate != 0 : the results of [width] are added to
+ * Results may take the place of inputs as in lp_residual_norm; other overlaps, and results over one another, are refused.
  * Column sums are added in FP32 in a fixed order: the same bits in every run.  Takes workspace from the context (growing
  * synchronises).  Does not synchronise otherwise. */
 lp_status lp_residual_norm_grad(lp_ctx *ctx, const lp_residual_desc *desc, const void *dy, int64_t ld_dy, const void *dn, int64_t ld_dn, const void *y, int64_t ld_y,

@@ -616,9 +616,8 @@ class Context:
 
     # ---- products by group
     def _offsets(self, offsets, who: str) -> int:
-        self._ids(offsets, who)
-        if offsets.dim() != 1 or offsets.numel() < 1:
-            self._refuse(f"{who}: offsets must be a vector of one more element than there are groups")
+        if offsets.dtype is not self._torch.int32 or offsets.get_device() != self.device or not offsets.is_contiguous() or offsets.dim() != 1 or offsets.numel() < 1:
+            self._refuse(f"{who}: offsets must be a contiguous int32 vector on cuda:{self.device} of one more element than there are groups")
         return offsets.numel() - 1
 
     def grouped_linear(self, A, offsets, B, bias=None, relu: bool = False, trans_b: bool = False, out=None):

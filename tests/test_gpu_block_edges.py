@@ -467,3 +467,12 @@ def test_two_contexts_at_once(pkg):
     for c in contexts:
         c.close()
     assert not failed, failed
+
+
+def test_refused_offsets_are_named(pkg, ctx):
+    a, b = torch.zeros(4, 16, device=DEV), torch.zeros(2, 16, 16, device=DEV)
+    off = torch.tensor([0, 2, 4], dtype=I32, device=DEV)
+    for bad in (off.long(), off.cpu(), off[None], off[:0], torch.zeros(6, dtype=I32, device=DEV)[::2]):
+        for call in (lambda: ctx.grouped_linear(a, bad, b), lambda: ctx.grouped_weight_grad(a, a, bad)):
+            with pytest.raises(pkg.LpError, match="offsets"):
+                call()
