@@ -437,7 +437,7 @@ template <bool VEC, bool BLOCK> struct RowPipe {
 
 template <typename T> LP_DEVINL T *row_at(void *array, uint32_t row, uint32_t ld) { return (T *)((char *)array + (uint64_t)row * ld); }
 
-// 1 / sqrt(x) of a positive x: the hardware's estimate and one Newton step, off by about 1.5 2^-24 (the correctly rounded square root and
+// 1 / sqrt(x) of a positive x: the hardware's estimate and one step of Newton-Raphson (on 1 / r^2 - x), off by about 1.5 2^-24 (the correctly rounded square root and
 // division took 35 instructions); 0 for a sum that is infinite
 LP_DEVINL float inv_sqrt(float x)
 {
